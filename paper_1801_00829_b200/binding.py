@@ -84,6 +84,8 @@ EXPORTS = [
     "fused_cell_static", "fused_cell_static_limit_bytes",
     "fo_set_jit", "fo_jit_stats", "fo_jit_prepare", "fo_jit_prepare_call", "fo_jit_compile_check", "fo_jit_compile_check_outer", "fo_jit_compile_check_row",
     "fo_probe_out_len", "fo_probe_l2_gather", "fo_probe_bulk_gather", "fo_probe_fp64_fma", "fo_chain_describe", "fo_tune", "fo_cell_stamps",
+    "fused_block_norm", "fused_block_norm_grad", "fused_block_norm_grad_workspace_bytes",
+    "fused_grad_norm", "fused_grad_clip", "fused_grad_workspace_bytes", "fused_adamw",
 ]
 
 _lib = None
@@ -130,6 +132,20 @@ def load_library(path=None):
         lib.fused_cell_static.restype = C.c_int
         lib.fused_cell_static_limit_bytes.argtypes = []
         lib.fused_cell_static_limit_bytes.restype = C.c_size_t
+        # the training-step operators take their structs packed (training.py)
+        bp, dbl, i64 = C.c_char_p, C.c_double, C.c_int64
+        lib.fused_block_norm.argtypes = [bp, vp]
+        lib.fused_block_norm_grad.argtypes = [bp, vp, sz, vp]
+        lib.fused_grad_norm.argtypes = [bp, i32, i32, i32, dbl, dbl, vp, i32, vp, sz, vp]
+        lib.fused_grad_clip.argtypes = [bp, i32, i32, i32, i32, dbl, dbl, vp, i32, vp, sz, vp]
+        lib.fused_adamw.argtypes = [bp, i32, i32, i32, dbl, dbl, dbl, dbl, i64, vp, i32, vp]
+        for f in (lib.fused_block_norm, lib.fused_block_norm_grad, lib.fused_grad_norm, lib.fused_grad_clip,
+                  lib.fused_adamw):
+            f.restype = C.c_int
+        lib.fused_block_norm_grad_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.fused_block_norm_grad_workspace_bytes.restype = sz
+        lib.fused_grad_workspace_bytes.argtypes = []
+        lib.fused_grad_workspace_bytes.restype = sz
         lib.fo_set_jit.argtypes = [C.c_int]
         lib.fo_set_jit.restype = C.c_int
         ip = C.POINTER(C.c_int)

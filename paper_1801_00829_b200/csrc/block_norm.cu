@@ -1,0 +1,230 @@
+// Block norm and its gradient: argument checks, alignment, dispatch over element types, and the sum
+// of the gradient's column partials.
+#include "block_norm_launch.cuh"
+
+namespace fo {
+
+#define FO_PAIRS(X)                                                    \
+    X(FO_F64, FO_F64, double, double)                                  \
+    X(FO_F32, FO_F32, float, float)                                    \
+    X(FO_BF16, FO_BF16, __nv_bfloat16, __nv_bfloat16)                  \
+    X(FO_F16, FO_F16, __half, __half)                                  \
+    X(FO_F32, FO_BF16, float, __nv_bfloat16)                           \
+    X(FO_F32, FO_F16, float, __half)
+
+#define FO_EXTERN(s, b, TS, TB)                                                                    \
+    extern template cudaError_t launch_block_norm<TS, TB>(const BlockNormParams &, cudaStream_t);  \
+    extern template cudaError_t launch_block_norm_grad<TS, TB>(BlockNormGradParams, int, int, int *, cudaStream_t);
+FO_PAIRS(FO_EXTERN)
+#undef FO_EXTERN
+
+namespace {
+
+int elem_bytes(int type) { return type == FO_F64 ? 8 : type == FO_F32 ? 4 : 2; }
+
+bool types_ok(int stream, int block, int vec)
+{
+    bool ok = false;
+#define FO_CASE(s, b, TS, TB) ok = ok || (stream == s && block == b);
+    FO_PAIRS(FO_CASE)
+#undef FO_CASE
+    return ok && (vec == block || (vec == FO_F32 && elem_bytes(block) == 2));
+}
+
+bool spec_ok(const fo_norm &n)
+{
+    return n.kind >= FO_NORM_NONE && n.kind <= FO_NORM_LAYER && (n.kind == FO_NORM_NONE || n.eps >= 0.0);
+}
+
+NormSpec spec_of(const fo_norm &n)
+{
+    NormSpec s = {n.kind, 0, n.eps, nullptr, nullptr};
+    if (n.kind != FO_NORM_NONE) s.weight = n.weight, s.bias = n.bias;
+    return s;
+}
+
+// Collects whether every row of every matrix, and every vector, can move in 16-byte pieces.
+struct Pieces {
+    bool ok;
+    void matrix(const void *p, long long ld, int type)
+    {
+        if (p) ok = ok && ((uintptr_t)p & 15u) == 0 && (ld * elem_bytes(type)) % 16 == 0;
+    }
+    void vector(const void *p) { ok = ok && ((uintptr_t)p & 15u) == 0; }
+    void norm(const fo_norm &n)
+    {
+        if (n.kind != FO_NORM_NONE) vector(n.weight), vector(n.bias);
+    }
+};
+
+int check_shape(long long rows, long long cols)
+{
+    if (rows < 0 || cols < 0) return FO_ERR_SHAPE;
+    if (cols > FO_BLOCK_NORM_MAX_COLS || rows > 0x7fffffffLL) return FO_ERR_UNSUPPORTED;
+    return FO_OK;
+}
+
+// Gate and leading dimensions of the block's part.
+int check_gate(const void *gate, int access, int act, long long ld, long long rows, long long cols)
+{
+    if (!gate) return FO_OK;
+    if (access < FO_AT_CELL || access > FO_AT_COL || act < FO_ACT_LINEAR || act > FO_ACT_TANH) return FO_ERR_UNSUPPORTED;
+    if (access == FO_AT_CELL && ld < cols) return FO_ERR_SHAPE;
+    if (access == FO_AT_ROW && rows > 1 && ld < 1) return FO_ERR_SHAPE;
+    return FO_OK;
+}
+
+// Upper bound on the CTAs that leave a line of partial column sums: a few per SM for short rows,
+// one per SM for long ones, whose lines are long.
+int grad_ctas(long long rows, long long cols)
+{
+    const long long cap = cols <= 1024 ? 148 * 4 : cols <= 4096 ? 148 * 2 : 148;
+    const long long n = rows < cap ? rows : cap;
+    return (int)(n > 1 ? n : 1);
+}
+
+}  // namespace
+}  // namespace fo
+
+using namespace fo;
+
+extern "C" {
+
+int fused_block_norm(const fo_block_norm *a, void *stream)
+{
+    if (!a) return FO_ERR_NULL;
+    int rc = check_shape(a->rows, a->cols);
+    if (rc != FO_OK) return rc;
+    if (!types_ok(a->stream_type, a->block_type, a->vec_type) || !spec_ok(a->post) || !spec_ok(a->pre))
+        return FO_ERR_UNSUPPORTED;
+    if (a->rows == 0 || a->cols == 0) return FO_OK;
+    if (!a->x && !a->f) return FO_ERR_NULL;
+    if (!a->h && !a->y && !a->stats) return FO_ERR_NULL;
+    if (a->y && a->pre.kind == FO_NORM_NONE) return FO_ERR_NULL;      // y without a norm: h is that
+    if (!a->f && (a->gate || a->col_scale || a->post.kind != FO_NORM_NONE)) return FO_ERR_NULL;
+    if ((a->x && a->ld_x < a->cols) || (a->f && a->ld_f < a->cols) || (a->h && a->ld_h < a->cols)
+        || (a->y && a->ld_y < a->cols))
+        return FO_ERR_SHAPE;
+    rc = check_gate(a->gate, a->gate_access, a->gate_act, a->ld_gate, a->rows, a->cols);
+    if (rc != FO_OK) return rc;
+
+    BlockNormParams p = {};
+    p.rows = a->rows, p.cols = (int)a->cols;
+    p.wide_vec = a->vec_type != a->block_type;
+    p.gate_access = a->gate ? a->gate_access : -1, p.gate_act = a->gate_act;
+    p.x = a->x, p.f = a->f, p.gate = a->gate, p.col_scale = a->col_scale;
+    p.ld_x = a->ld_x, p.ld_f = a->ld_f, p.ld_gate = a->ld_gate, p.ld_h = a->ld_h, p.ld_y = a->ld_y;
+    p.scale = a->scale;
+    p.post = spec_of(a->post), p.pre = spec_of(a->pre);
+    p.h = a->h, p.y = a->y, p.stats = a->stats;
+    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0};
+    all.matrix(a->x, a->ld_x, a->stream_type);
+    all.matrix(a->h, a->ld_h, a->stream_type);
+    all.matrix(a->f, a->ld_f, a->block_type);
+    all.matrix(a->y, a->ld_y, a->block_type);
+    if (p.gate_access == FO_AT_CELL) all.matrix(a->gate, a->ld_gate, a->block_type);
+    if (p.gate_access == FO_AT_COL) all.vector(a->gate);
+    all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
+    p.vec = all.ok;
+
+    cudaError_t e = cudaErrorInvalidValue;
+#define FO_CASE(s, b, TS, TB) \
+    if (a->stream_type == s && a->block_type == b) e = launch_block_norm<TS, TB>(p, (cudaStream_t)stream);
+    FO_PAIRS(FO_CASE)
+#undef FO_CASE
+    return e == cudaSuccess ? FO_OK : cuda_fail(e);
+}
+
+size_t fused_block_norm_grad_workspace_bytes(int64_t rows, int64_t cols, int block_type)
+{
+    if (check_shape(rows, cols) != FO_OK || block_type < FO_F64 || block_type > FO_F16) return 0;
+    return sizeof(WsHead) + (size_t)kGradSlots * grad_ctas(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
+}
+
+int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!a) return FO_ERR_NULL;
+    int rc = check_shape(a->rows, a->cols);
+    if (rc != FO_OK) return rc;
+    if (!types_ok(a->stream_type, a->block_type, a->vec_type) || !spec_ok(a->post) || !spec_ok(a->pre))
+        return FO_ERR_UNSUPPORTED;
+    if (a->cols == 0) return FO_OK;
+    const cudaStream_t st = (cudaStream_t)stream;
+    void *const sums[kGradSlots] = {a->dpre_weight, a->dpre_bias, a->dpost_weight, a->dpost_bias, a->dcol_scale,
+                                    a->gate_access == FO_AT_COL ? a->dgate : nullptr};
+    if (a->rows == 0) {                                        // sums over no rows; nothing else has a size
+        for (void *s : sums) {
+            if (!s) continue;
+            const cudaError_t e = cudaMemsetAsync(s, 0, (size_t)a->cols * (a->block_type == FO_F64 ? 8 : 4), st);
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
+        return FO_OK;
+    }
+    const bool pre = a->dy != nullptr, post = a->f && a->post.kind != FO_NORM_NONE;
+    if (!a->dh && !a->dy) return FO_ERR_NULL;
+    if (pre && (a->pre.kind == FO_NORM_NONE || !a->h)) return FO_ERR_NULL;
+    if ((pre || post) && !a->stats) return FO_ERR_NULL;
+    if (!a->f && (a->gate || a->col_scale || a->post.kind != FO_NORM_NONE || a->df || a->dgate || a->dcol_scale
+                  || a->dpost_weight || a->dpost_bias))
+        return FO_ERR_NULL;
+    if ((a->dgate && !a->gate) || (!post && (a->dpost_weight || a->dpost_bias))
+        || (a->pre.kind == FO_NORM_NONE && (a->dpre_weight || a->dpre_bias)))
+        return FO_ERR_NULL;
+    if ((a->dh && a->ld_dh < a->cols) || (pre && (a->ld_dy < a->cols || a->ld_h < a->cols)) || (a->f && a->ld_f < a->cols)
+        || (a->dx && a->ld_dx < a->cols) || (a->df && a->ld_df < a->cols)
+        || (a->dgate && a->gate_access == FO_AT_CELL && a->ld_dgate < a->cols))
+        return FO_ERR_SHAPE;
+    rc = check_gate(a->gate, a->gate_access, a->gate_act, a->ld_gate, a->rows, a->cols);
+    if (rc != FO_OK) return rc;
+    rc = check_workspace(ws, ws_bytes, fused_block_norm_grad_workspace_bytes(a->rows, a->cols, a->block_type));
+    if (rc != FO_OK) return rc;
+    BlockNormGradParams p = {};
+    p.rows = a->rows, p.cols = (int)a->cols;
+    p.wide_vec = a->vec_type != a->block_type;
+    p.gate_access = a->gate ? a->gate_access : -1, p.gate_act = a->gate_act;
+    p.dh = a->dh, p.dy = a->dy, p.h = a->h, p.f = a->f, p.gate = a->gate, p.col_scale = a->col_scale, p.stats = a->stats;
+    p.ld_dh = a->ld_dh, p.ld_dy = a->ld_dy, p.ld_h = a->ld_h, p.ld_f = a->ld_f, p.ld_gate = a->ld_gate;
+    p.scale = a->scale;
+    p.post = spec_of(a->post), p.pre = spec_of(a->pre);
+    p.dx = a->dx, p.df = a->df, p.dgate = p.gate_access == FO_AT_COL ? nullptr : a->dgate;
+    p.ld_dx = a->ld_dx, p.ld_df = a->ld_df, p.ld_dgate = a->ld_dgate;
+    p.partial = static_cast<char *>(ws) + sizeof(WsHead);
+    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0};
+    all.matrix(a->dh, a->ld_dh, a->stream_type);
+    all.matrix(a->dx, a->ld_dx, a->stream_type);
+    if (pre) all.matrix(a->h, a->ld_h, a->stream_type), all.matrix(a->dy, a->ld_dy, a->block_type);
+    all.matrix(a->f, a->ld_f, a->block_type);
+    all.matrix(a->df, a->ld_df, a->block_type);
+    if (p.gate_access == FO_AT_CELL) all.matrix(a->gate, a->ld_gate, a->block_type);
+    if (p.gate_access == FO_AT_CELL) all.matrix(a->dgate, a->ld_dgate, a->block_type);
+    if (p.gate_access == FO_AT_COL) all.vector(a->gate);
+    all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
+    p.vec = all.ok;
+
+    int n_sums = 0;
+    ColumnSumParams cs = {};
+    for (int s = 0; s < kGradSlots; ++s) {
+        if (!sums[s]) continue;
+        p.slots |= 1u << s;
+        cs.out[n_sums++] = sums[s];
+    }
+    const unsigned lean = (1u << kPreW) | (1u << kPostW) | (1u << kColScale);
+    const int form = !a->f ? kGradStream : (p.slots & ~lean) == 0 ? kGradLean : kGradAll;
+    cudaError_t e = cudaErrorInvalidValue;
+    int ctas = 0;
+#define FO_CASE(s, b, TS, TB)                           \
+    if (a->stream_type == s && a->block_type == b)      \
+        e = launch_block_norm_grad<TS, TB>(p, form, grad_ctas(a->rows, a->cols), &ctas, st);
+    FO_PAIRS(FO_CASE)
+#undef FO_CASE
+    if (e == cudaSuccess && n_sums > 0) {
+        cs.partial = p.partial, cs.ctas = ctas, cs.cols = p.cols;
+        const dim3 grid((unsigned)((a->cols + 31) / 32), (unsigned)n_sums);
+        if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, 256, 0, st>>>(cs);
+        else column_sum_kernel<float><<<grid, 256, 0, st>>>(cs);
+        e = cudaGetLastError();
+    }
+    return e == cudaSuccess ? FO_OK : cuda_fail(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,8 @@
+// Block norm and its gradient: stream of float, block of __nv_bfloat16.
+#define FO_BLOCK_NORM_DEFINE
+#include "block_norm_launch.cuh"
+
+namespace fo {
+template cudaError_t launch_block_norm<float, __nv_bfloat16>(const BlockNormParams &, cudaStream_t);
+template cudaError_t launch_block_norm_grad<float, __nv_bfloat16>(BlockNormGradParams, int, int, int *, cudaStream_t);
+}  // namespace fo

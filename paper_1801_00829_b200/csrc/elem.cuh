@@ -1,0 +1,132 @@
+// Element types of the training-step operators (float64, float32, bfloat16, float16): rows held
+// packed in registers as they lie in memory, conversion to the type sums are held in, and the
+// gate's activations.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "../../include/fusedops_train.h"
+
+namespace fo {
+
+// Acc: what arithmetic, statistics and sums are held in.
+template <class T> struct Elem { using Acc = float; };
+template <> struct Elem<double> { using Acc = double; };
+template <class T> using Acc = typename Elem<T>::Acc;
+
+template <class T>
+__device__ __forceinline__ Acc<T> widen(T v)
+{
+    return (Acc<T>)v;
+}
+template <class T>
+__device__ __forceinline__ T narrow(Acc<T> v);
+template <> __device__ __forceinline__ double narrow<double>(double v) { return v; }
+template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
+
+// N elements as 32-bit words, the way they lie in memory.  N * sizeof(T) is a multiple of 16.
+template <class T, int N>
+struct Packed {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ Acc<T> get(int k) const
+    {
+        if constexpr (sizeof(T) == 8) return __hiloint2double((int)w[2 * k + 1], (int)w[2 * k]);
+        else if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+        else if constexpr (std::is_same<T, __nv_bfloat16>::value)
+            return __uint_as_float((k & 1) ? (w[k / 2] & 0xffff0000u) : (w[k / 2] << 16));
+        else return __half2float(__ushort_as_half((unsigned short)((k & 1) ? (w[k / 2] >> 16) : (w[k / 2] & 0xffffu))));
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    }
+    __device__ __forceinline__ void put(int k, T v)      // into a cleared place
+    {
+        if constexpr (sizeof(T) == 8) {
+            w[2 * k] = (uint32_t)__double2loint(v);
+            w[2 * k + 1] = (uint32_t)__double2hiint(v);
+        } else if constexpr (sizeof(T) == 4) {
+            w[k] = __float_as_uint(v);
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            w[k / 2] |= (uint32_t)__bfloat16_as_ushort(v) << (16 * (k & 1));
+        } else {
+            w[k / 2] |= (uint32_t)__half_as_ushort(v) << (16 * (k & 1));
+        }
+    }
+};
+
+// 16 bytes of data that is read once: no place in L1.  Not the read-only path: an output may be the
+// matrix it is computed from, element by element.
+__device__ __forceinline__ void load16(uint32_t *w, const void *p)
+{
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "l"(p));
+}
+__device__ __forceinline__ void store16(void *p, const uint32_t *w)
+{
+    asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                 : "memory");
+}
+
+__device__ __forceinline__ float group_rsqrt(float v) { return 1.0f / sqrtf(v); }
+__device__ __forceinline__ double group_rsqrt(double v) { return 1.0 / sqrt(v); }
+__device__ __forceinline__ float fused_ma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ double fused_ma(double a, double b, double c) { return fma(a, b, c); }
+
+// act(g) and its derivative.  FAST (results rounded to 16 bits): the hardware's exponential, with a
+// relative error of a few 2^-22 over the range where a sigmoid is not 0 or 1; the tangent is the
+// library's in every case, because near zero its relative error is what a gate that starts at zero sees.
+template <class A> __device__ __forceinline__ A exp_neg(A g);
+template <> __device__ __forceinline__ float exp_neg<float>(float g) { return expf(-g); }
+template <> __device__ __forceinline__ double exp_neg<double>(double g) { return exp(-g); }
+__device__ __forceinline__ float tanh_of(float g) { return tanhf(g); }
+__device__ __forceinline__ double tanh_of(double g) { return tanh(g); }
+
+template <bool FAST, class A>
+__device__ __forceinline__ A sigmoid(A g)
+{
+    if constexpr (FAST) return __fdividef(1.0f, 1.0f + __expf(-g));   // e^-g = inf gives 0
+    else return A(1) / (A(1) + exp_neg<A>(g));
+}
+
+template <bool FAST, class A>
+__device__ __forceinline__ A activate(int kind, A g)
+{
+    if (kind == FO_ACT_LINEAR) return g;
+    if (kind == FO_ACT_TANH) return tanh_of(g);
+    const A s = sigmoid<FAST, A>(g);
+    return kind == FO_ACT_SILU ? g * s : s;
+}
+
+template <bool FAST, class A>
+__device__ __forceinline__ A activate_slope(int kind, A g, A &slope)
+{
+    if (kind == FO_ACT_LINEAR) {
+        slope = A(1);
+        return g;
+    }
+    if (kind == FO_ACT_TANH) {
+        const A t = tanh_of(g);
+        slope = A(1) - t * t;
+        return t;
+    }
+    const A s = sigmoid<FAST, A>(g);
+    if (kind == FO_ACT_SIGMOID) {
+        slope = s * (A(1) - s);
+        return s;
+    }
+    slope = s * (A(1) + g * (A(1) - s));
+    return g * s;
+}
+
+}  // namespace fo
