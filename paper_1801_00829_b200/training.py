@@ -33,97 +33,120 @@ def _require(ok, text):
         raise ValueError(text)
 
 
-def _device(t):
-    _require(t.device.type == "cuda", "fused operators need CUDA tensors (no CPU path)")
-    return t.device
+# The current stream's handle as a number, without a Stream object around it where this torch has that call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-class _OnDevice:
-    """Makes `device` current for a call if another one is."""
-
-    def __init__(self, device):
-        self.other = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *error):
-        if self.other is not None:
-            self.other.__exit__(*error)
+def _index(t):
+    """Number of the GPU that a tensor is on."""
+    index = t.get_device()
+    _require(index >= 0, "fused operators need CUDA tensors (no CPU path)")
+    return index
 
 
-class _Rows:
-    """Checks of one call's matrices and vectors: all rows x cols on one device, rows contiguous."""
+def _call(name, index, *args):
+    """Calls a C entry on the current stream of GPU `index`, which is made current if another one is."""
+    fn = getattr(load_library(), name)
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        _check(status, name)
 
-    def __init__(self, like, cols_of):
-        _require(cols_of.dim() == 2, "matrices are 2-D")
-        self.rows, self.cols = cols_of.shape
-        self.device = _device(like)
-        self.vec_type = None
 
-    def matrix(self, t, dtype, name):
-        """(address, leading dimension) of a matrix of the call."""
-        if t is None:
-            return 0, 0
-        _require(t.shape == (self.rows, self.cols), "%s is not %d x %d" % (name, self.rows, self.cols))
-        _require(t.dtype == dtype, "%s is %s, not %s" % (name, t.dtype, dtype))
-        _require(t.device == self.device, "%s is on another device" % name)
-        ld, inner = t.stride()
-        _require(inner == 1 or self.cols <= 1, "rows of %s must be contiguous" % name)
-        if ld < self.cols:
-            _require(self.rows <= 1, "rows of %s overlap" % name)
-            ld = self.cols
-        return t.data_ptr(), ld
+_scratch = {}
 
-    def vector(self, t, name):
-        """Address of a vector over the columns; all of a call have one type."""
-        if t is None:
-            return 0
-        _require(t.shape == (self.cols,) and (self.cols <= 1 or t.stride(0) == 1), "%s is not a contiguous vector of %d"
-                 % (name, self.cols))
-        _require(t.device == self.device, "%s is on another device" % name)
-        if self.vec_type is None:
-            self.vec_type = t.dtype
-        _require(t.dtype == self.vec_type, "weights, biases and col_scale have different types")
-        return t.data_ptr()
 
-    def norm(self, spec, name):
-        if spec is None:
-            return _NO_NORM
-        kind, weight, bias, eps = spec
-        _require(kind in NORM_KIND, "norm kind %r" % (kind,))
-        return NORM_KIND[kind], 0, float(eps), self.vector(weight, name + " weight"), self.vector(bias, name + " bias")
+def _workspace(index, nbytes):
+    """(address, size) of the current stream's scratch (binding.workspace), looked up by numbers."""
+    key = (index, _raw_stream(index))
+    buf = _scratch.get(key)
+    if buf is None or buf.numel() < nbytes:
+        buf = _scratch[key] = workspace(torch.device("cuda", index), nbytes)
+    return buf.data_ptr(), buf.numel()
 
-    def gate(self, spec, dtype):
-        """(access, activation, address, leading dimension or stride)"""
-        if spec is None:
-            return 0, 0, 0, 0
-        access, t, act = spec
-        _require(access in ACCESS and act in ACTIVATION, "gate %r, activation %r" % (access, act))
-        if access == "cell":
-            ptr, ld = self.matrix(t, dtype, "gate")
-        else:
-            n = self.rows if access == "row" else self.cols
-            t = t.reshape(-1) if t.dim() == 2 and t.is_contiguous() else t
-            _require(t.shape == (n,) and t.dtype == dtype and t.device == self.device, "gate is not a vector of %d %s"
-                     % (n, dtype))
-            ld = t.stride(0) if n > 1 else 1
-            _require(ld >= 1 if access == "row" else ld == 1, "stride of the gate")
-            ptr = t.data_ptr()
-        return ACCESS[access], ACTIVATION[act], ptr, ld
 
-    def types(self, stream, block):
-        """(stream, block, vector) type codes; without vectors the block's type stands for theirs."""
-        _require((stream, block) in PAIRS, "no kernel for a %s stream and a %s block" % (stream, block))
-        vec = block if self.vec_type is None else self.vec_type
-        _require(vec == block or (vec == torch.float32 and block.itemsize == 2), "vectors of %s with a block of %s"
-                 % (vec, block))
-        return DTYPES[stream], DTYPES[block], DTYPES[vec]
+def _matrix(t, shape, dtype, index, name):
+    """(address, leading dimension) of a matrix of the call, zeros for None."""
+    if t is None:
+        return 0, 0
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError("%s: a %s matrix of %s on GPU %d is needed, not %s of %s on %s"
+                         % (name, dtype, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
+    ld, inner = t.stride()
+    if inner != 1 and shape[1] > 1:
+        raise ValueError("rows of %s must be contiguous" % name)
+    if ld < shape[1]:
+        if shape[0] > 1:
+            raise ValueError("rows of %s overlap" % name)
+        ld = shape[1]
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, dtype, index, name):
+    """Address of a contiguous vector of the call, 0 for None."""
+    if t is None:
+        return 0
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != index or not (n <= 1 or t.is_contiguous()):
+        raise ValueError("%s: a contiguous %s vector of %d on GPU %d is needed, not %s of %s on %s"
+                         % (name, dtype, n, index, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _norm(spec, cols, dtype, index, name):
+    if spec is None:
+        return _NO_NORM
+    kind, weight, bias, eps = spec
+    _require(kind in NORM_KIND, "norm kind %r" % (kind,))
+    return NORM_KIND[kind], 0, eps, _vector(weight, cols, dtype, index, name), _vector(bias, cols, dtype, index, name)
+
+
+def _gate(spec, shape, dtype, index):
+    """(access, activation, address, leading dimension or stride)"""
+    if spec is None:
+        return 0, 0, 0, 0
+    access, t, act = spec
+    _require(access in ACCESS and act in ACTIVATION, "gate %r, activation %r" % (access, act))
+    if access == "cell":
+        ptr, ld = _matrix(t, shape, dtype, index, "gate")
+    else:
+        n = shape[0] if access == "row" else shape[1]
+        if t.dim() == 2 and 1 in t.shape:                    # a column or row vector
+            t = t[:, 0] if t.shape[1] == 1 and access == "row" else t[0]
+        _require(t.shape == (n,) and t.dtype is dtype and t.get_device() == index, "gate is not a vector of %d %s"
+                 % (n, dtype))
+        ld = t.stride(0) if n > 1 else 1
+        _require(ld >= 1 if access == "row" else ld == 1, "stride of the gate")
+        ptr = t.data_ptr()
+    return ACCESS[access], ACTIVATION[act], ptr, ld
+
+
+def _types(stream, block, post, pre, col_scale):
+    """Type codes of stream, block and vectors, and the vectors' type: that of the first one, or the block's."""
+    vec = None if col_scale is None else col_scale.dtype
+    for spec in (post, pre):
+        if spec is not None and vec is None:
+            vec = spec[1].dtype if spec[1] is not None else spec[2].dtype if spec[2] is not None else None
+    vec = block if vec is None else vec
+    if (stream, block) not in PAIRS:
+        raise ValueError("no kernel for a %s stream and a %s block" % (stream, block))
+    if vec is not block and not (vec is torch.float32 and block.itemsize == 2):
+        raise ValueError("vectors of %s with a block of %s" % (vec, block))
+    return (DTYPES[stream], DTYPES[block], DTYPES[vec]), vec
 
 
 def _sum_type(block):
-    return torch.float64 if block == torch.float64 else torch.float32
+    return torch.float64 if block is torch.float64 else torch.float32
+
+
+def _new(like, shape, dtype):
+    """An uninitialised packed tensor on the GPU of `like`."""
+    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like)                        # the shorter way
+    return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def fused_block_norm(x=None, f=None, post=None, gate=None, scale=1.0, col_scale=None, pre=None, out_h=None, out_y=None,
@@ -134,38 +157,40 @@ def fused_block_norm(x=None, f=None, post=None, gate=None, scale=1.0, col_scale=
     x alone.  Returns (h, y, stats): h is x itself without f, y is None without `pre`; stats (float, 4 x
     rows, with stats=True) is what fused_block_norm_grad needs.  y has the type of f, or without f
     `block_type` (default: that of x).  out_h may be x.  x None: h has the type of f or of out_h."""
-    _require(x is not None or f is not None, "x or f is needed")
     first = x if x is not None else f
-    c = _Rows(first, first)
+    _require(first is not None, "x or f is needed")
+    index, shape = _index(first), first.shape
+    _require(len(shape) == 2, "matrices are 2-D")
+    rows, cols = shape
+    stream = first.dtype if x is not None or out_h is None else out_h.dtype
     if f is not None:
         block = f.dtype
-        stream = x.dtype if x is not None else out_h.dtype if out_h is not None else block
     else:
-        stream = x.dtype
         block = block_type if block_type is not None else out_y.dtype if out_y is not None else stream
         _require(post is None and gate is None and col_scale is None, "post, gate and col_scale need a block output f")
-    xp, ldx = c.matrix(x, stream, "x")
-    fp, ldf = c.matrix(f, block, "f")
-    access, act, gp, ldg = c.gate(gate, block)
-    post_s, pre_s, csp = c.norm(post, "post"), c.norm(pre, "pre"), c.vector(col_scale, "col_scale")
-    types = c.types(stream, block)
-    h = out_h
+    types, vec = _types(stream, block, post, pre, col_scale)
+    xp, ldx = _matrix(x, shape, stream, index, "x")
+    fp, ldf = _matrix(f, shape, block, index, "f")
+    access, act, gp, ldg = _gate(gate, shape, block, index)
+    post_s = _norm(post, cols, vec, index, "post")
+    pre_s = _norm(pre, cols, vec, index, "pre")
+    csp = _vector(col_scale, cols, vec, index, "col_scale")
+    h, y, st, stp = out_h, out_y, None, 0
     if h is None and f is not None:
-        h = torch.empty((c.rows, c.cols), dtype=stream, device=c.device)
-    y = out_y
+        h = _new(first, shape, stream)
     if y is None and pre is not None:
-        y = torch.empty((c.rows, c.cols), dtype=block, device=c.device)
+        y = _new(first if f is None else f, shape, block)
     _require(y is None or pre is not None, "out_y without a norm before the next block")
-    st = torch.empty((4, c.rows), dtype=_sum_type(block), device=c.device) if stats else None
-    hp, ldh = c.matrix(h, stream, "out_h")
-    yp, ldy = c.matrix(y, block, "out_y")
-    if hp or yp or stats:
-        packed = _BLOCK_NORM.pack(c.rows, c.cols, *types, access, act, 0, xp, fp, gp, csp, ldx, ldf, ldg, scale, *post_s,
-                                  *pre_s, hp, yp, st.data_ptr() if stats else 0, ldh, ldy)
-        with _OnDevice(c.device):
-            _check(load_library().fused_block_norm(packed, torch.cuda.current_stream(c.device).cuda_stream),
-                   "fused_block_norm")
-    return (x if f is None and h is None else h), y, st
+    if stats:
+        st = torch.empty((4, rows), dtype=_sum_type(block), device=first.device)
+        stp = st.data_ptr()
+    hp, ldh = _matrix(h, shape, stream, index, "out_h")
+    yp, ldy = _matrix(y, shape, block, index, "out_y")
+    if hp or yp or stp:
+        _call("fused_block_norm", index,
+              _BLOCK_NORM.pack(rows, cols, *types, access, act, 0, xp, fp, gp, csp, ldx, ldf, ldg, scale, *post_s, *pre_s,
+                               hp, yp, stp, ldh, ldy))
+    return (x if h is None else h), y, st
 
 
 def fused_block_norm_grad(dh=None, dy=None, h=None, f=None, stats=None, post=None, gate=None, scale=1.0, col_scale=None,
@@ -177,62 +202,69 @@ def fused_block_norm_grad(dh=None, dy=None, h=None, f=None, stats=None, post=Non
     "pre_b".  Gradients of vectors, and of a gate per row or column, are float (double for float64)."""
     first = dh if dh is not None else dy
     _require(first is not None, "dh or dy is needed")
-    c = _Rows(first, first)
-    _require(dy is None or (pre is not None and h is not None), "dy needs `pre` and h")
-    like_stream = dh if dh is not None else h
-    like_block = f if f is not None else dy
-    stream = like_stream.dtype
-    block = like_block.dtype if like_block is not None else stream
+    index, shape = _index(first), first.shape
+    _require(len(shape) == 2, "matrices are 2-D")
+    rows, cols = shape
+    if dy is not None:
+        _require(pre is not None and h is not None, "dy needs `pre` and h")
+    elif f is not None:
+        pre = None                                           # nothing reaches the norm of h
+    stream = dh.dtype if dh is not None else h.dtype
+    block = f.dtype if f is not None else dy.dtype if dy is not None else stream
     _require(f is not None or (post is None and gate is None and col_scale is None),
              "post, gate and col_scale need a block output f")
-    if dy is None:
-        pre = None if f is not None else pre
-    dhp, lddh = c.matrix(dh, stream, "dh")
-    dyp, lddy = c.matrix(dy, block, "dy")
-    hp, ldh = c.matrix(h if dy is not None else None, stream, "h")
-    fp, ldf = c.matrix(f, block, "f")
-    access, act, gp, ldg = c.gate(gate, block)
-    post_s, pre_s, csp = c.norm(post, "post"), c.norm(pre, "pre"), c.vector(col_scale, "col_scale")
-    types = c.types(stream, block)
-    sums = _sum_type(block)
+    types, vec = _types(stream, block, post, pre, col_scale)
+    dhp, lddh = _matrix(dh, shape, stream, index, "dh")
+    dyp, lddy = _matrix(dy, shape, block, index, "dy")
+    hp, ldh = _matrix(h if dy is not None else None, shape, stream, index, "h")
+    fp, ldf = _matrix(f, shape, block, index, "f")
+    access, act, gp, ldg = _gate(gate, shape, block, index)
+    post_s = _norm(post, cols, vec, index, "post")
+    pre_s = _norm(pre, cols, vec, index, "pre")
+    csp = _vector(col_scale, cols, vec, index, "col_scale")
+    sums, stp = _sum_type(block), 0
     if stats is not None:
-        _require(stats.shape == (4, c.rows) and stats.dtype == sums and stats.is_contiguous() and stats.device == c.device,
-                 "stats is not 4 x %d of %s" % (c.rows, sums))
-    got = {}
+        _require(stats.shape == (4, rows) and stats.dtype is sums and stats.is_contiguous() and stats.get_device() == index,
+                 "stats is not 4 x %d of %s" % (rows, sums))
+        stp = stats.data_ptr()
 
-    def make(name, shape, dtype, wanted):
-        if not wanted:
-            return 0
-        got[name] = t = torch.empty(shape, dtype=dtype, device=c.device)
-        return t.data_ptr()
-
-    cells, cols = (c.rows, c.cols), (c.cols,)
-    dxp = make("x", cells, stream, residual or f is None)
-    dfp = make("f", cells, block, f is not None)
-    dgp = 0
+    # the vectors' gradients lie in one buffer
+    names = [] if col_scale is None else ["col_scale"]
+    for part, spec in (("post", post), ("pre", pre)):
+        if spec is not None:
+            names += [part + end for end, t in (("_w", spec[1]), ("_b", spec[2])) if t is not None]
+    got, at = {}, {}
+    dxp = dfp = dgp = 0
+    if residual or f is None:
+        got["x"] = dx = _new(first, shape, stream)
+        dxp = dx.data_ptr()
+    if f is not None:
+        got["f"] = df = _new(f, shape, block)
+        dfp = df.data_ptr()
     if gate is not None:
-        dgp = make("gate", gate[1].shape, block if gate[0] == "cell" else sums, True)
-    dcsp = make("col_scale", cols, sums, col_scale is not None)
-    dpost, dpre = ([make(name + end, cols, sums, spec is not None and spec[at] is not None) for end, at in (("_w", 1), ("_b", 2))]
-                   for name, spec in (("post", post), ("pre", pre)))
-    packed = _BLOCK_NORM_GRAD.pack(c.rows, c.cols, *types, access, act, 0, dhp, dyp, hp, fp, gp, csp,
-                                   stats.data_ptr() if stats is not None else 0, lddh, lddy, ldh, ldf, ldg, scale,
-                                   *post_s, *pre_s, dxp, dfp, dgp, c.cols, c.cols, c.cols, dcsp, *dpost, *dpre)
-    lib = load_library()
-    with _OnDevice(c.device):
-        need = lib.fused_block_norm_grad_workspace_bytes(c.rows, c.cols, types[1])
-        ws = workspace(c.device, need)
-        _check(lib.fused_block_norm_grad(packed, ws.data_ptr(), ws.numel(),
-                                         torch.cuda.current_stream(c.device).cuda_stream), "fused_block_norm_grad")
+        got["gate"] = dg = _new(gate[1], gate[1].shape, block if gate[0] == "cell" else sums)
+        dgp = dg.data_ptr()
+    if names:
+        flat = torch.empty((len(names), cols), dtype=sums, device=first.device)
+        base, line = flat.data_ptr(), cols * sums.itemsize
+        got.update(zip(names, flat.unbind(0)))
+        at = {name: base + k * line for k, name in enumerate(names)}
+    packed = _BLOCK_NORM_GRAD.pack(rows, cols, *types, access, act, 0, dhp, dyp, hp, fp, gp, csp, stp, lddh, lddy, ldh, ldf,
+                                   ldg, scale, *post_s, *pre_s, dxp, dfp, dgp, cols, cols, cols, at.get("col_scale", 0),
+                                   at.get("post_w", 0), at.get("post_b", 0), at.get("pre_w", 0), at.get("pre_b", 0))
+    need = load_library().fused_block_norm_grad_workspace_bytes(rows, cols, types[1])
+    _call("fused_block_norm_grad", index, packed, *_workspace(index, need))
     return got
 
 
 # ------------------------------------------------------------------ many tensors
 def _same(tensors, name, dtype=None, device=None):
     """The type and device that the tensors of a list share; contiguous, all of them."""
+    if tensors:
+        _index(tensors[0])
+        dtype = tensors[0].dtype if dtype is None else dtype
+        device = tensors[0].device if device is None else device
     for t in tensors:
-        dtype = t.dtype if dtype is None else dtype
-        device = _device(t) if device is None else device
         _require(t.dtype == dtype and t.device == device, "%s: tensors of one type on one device are needed" % name)
         _require(t.is_contiguous(), "%s: tensors must be contiguous" % name)
     return dtype, device
@@ -260,6 +292,7 @@ class TensorList:
                      "clipped values of %s from gradients of %s" % (self.out_dtype, self.dtype))
         flat = [v for g, o in zip(self.grads, self.outs) for v in (g.data_ptr(), o.data_ptr(), g.numel())]
         self.packed = struct.pack("QQq" * len(self.grads), *flat)
+        self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.out_dtype, 1)
 
     def __len__(self):
         return len(self.grads)
@@ -270,37 +303,31 @@ def tensor_list(grads, outs=None):
     return TensorList(grads, outs)
 
 
-def _grad_call(grads, result_type, device):
+def _grad_call(name, grads, kind, max_norm, eps, result_type, device, types):
     grads = grads if isinstance(grads, TensorList) else TensorList(grads)
-    device = grads.device or device or torch.device("cuda", torch.cuda.current_device())
     _require(result_type in (torch.float32, torch.float64), "results are float32 or float64")
-    return grads, device, torch.empty(2, dtype=result_type, device=device)
+    _require(kind in GRAD_NORM_KIND, "norm kind %r" % (kind,))
+    if grads.device is not None:
+        device = grads.device
+    elif device is None:                                     # an empty list
+        device = torch.device("cuda", torch.cuda.current_device())
+    result = torch.empty(2, dtype=result_type, device=device)
+    index = result.get_device()
+    ws = _workspace(index, load_library().fused_grad_workspace_bytes())
+    _call(name, index, grads.packed, len(grads.grads), *grads.types[:types], GRAD_NORM_KIND[kind], max_norm, eps,
+          result.data_ptr(), DTYPES[result_type], *ws)
+    return result
 
 
 def fused_grad_norm(grads, max_norm, kind="l2", eps=1e-6, result_type=torch.float32, device=None):
     """(norm, factor) of all gradients together, as a tensor of two on the device: the "l2" or "max" norm and
-    min(1, max_norm / (norm + eps)).  grads: a TensorList or a list of tensors."""
-    grads, device, result = _grad_call(grads, result_type, device)
-    lib = load_library()
-    with _OnDevice(device):
-        ws = workspace(device, lib.fused_grad_workspace_bytes())
-        _check(lib.fused_grad_norm(grads.packed, len(grads), DTYPES.get(grads.dtype, 1), GRAD_NORM_KIND[kind], max_norm,
-                                   eps, result.data_ptr(), DTYPES[result_type], ws.data_ptr(), ws.numel(),
-                                   torch.cuda.current_stream(device).cuda_stream), "fused_grad_norm")
-    return result
+    min(1, max_norm / (norm + eps)).  grads: a TensorList or a list of tensors; device: for an empty list."""
+    return _grad_call("fused_grad_norm", grads, kind, max_norm, eps, result_type, device, 1)
 
 
 def fused_grad_clip(grads, max_norm, kind="l2", eps=1e-6, result_type=torch.float32, device=None):
     """fused_grad_norm, and every gradient times the factor into the list's outs (or in place)."""
-    grads, device, result = _grad_call(grads, result_type, device)
-    lib = load_library()
-    with _OnDevice(device):
-        ws = workspace(device, lib.fused_grad_workspace_bytes())
-        _check(lib.fused_grad_clip(grads.packed, len(grads), DTYPES.get(grads.dtype, 1), DTYPES.get(grads.out_dtype, 1),
-                                   GRAD_NORM_KIND[kind], max_norm, eps, result.data_ptr(), DTYPES[result_type],
-                                   ws.data_ptr(), ws.numel(), torch.cuda.current_stream(device).cuda_stream),
-               "fused_grad_clip")
-    return result
+    return _grad_call("fused_grad_clip", grads, kind, max_norm, eps, result_type, device, 2)
 
 
 class AdamList:
@@ -331,6 +358,7 @@ class AdamList:
         for k in range(n):
             flat += [ts[k].data_ptr() for ts in lists] + none + [self.grads[k].numel(), decay[k]]
         self.packed = struct.pack("8Qqd" * n, *flat)
+        self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.weight_dtype, 0)
 
     def __len__(self):
         return len(self.grads)
@@ -347,13 +375,10 @@ def fused_adamw(tensors, lr, betas=(0.9, 0.999), eps=1e-8, step=1, factor=None):
     gradients are multiplied by (result[1:2] of fused_grad_norm)."""
     if len(tensors) == 0:
         return
-    device, kind = tensors.device, 0
+    kind, at = 0, 0
     if factor is not None:
-        _require(factor.numel() == 1 and factor.device == device and factor.dtype in (torch.float32, torch.float64),
+        _require(factor.numel() == 1 and factor.device == tensors.device and factor.dtype in (torch.float32, torch.float64),
                  "factor is not one float on the gradients' device")
-        kind = DTYPES[factor.dtype]
-    with _OnDevice(device):
-        _check(load_library().fused_adamw(tensors.packed, len(tensors), DTYPES[tensors.dtype],
-                                          DTYPES.get(tensors.weight_dtype, 0), lr, betas[0], betas[1], eps, step,
-                                          factor.data_ptr() if factor is not None else 0, kind,
-                                          torch.cuda.current_stream(device).cuda_stream), "fused_adamw")
+        kind, at = DTYPES[factor.dtype], factor.data_ptr()
+    _call("fused_adamw", tensors.device.index, tensors.packed, len(tensors.grads), *tensors.types, lr, betas[0], betas[1],
+          eps, step, at, kind)
