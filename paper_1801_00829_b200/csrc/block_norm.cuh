@@ -53,36 +53,42 @@ struct BlockNormGradParams {
     void *partial;                           // [slot among the wanted][CTA][cols]
 };
 
-// Which columns a thread holds.  16-byte pieces: piece v of the thread covers columns
-// (v * T + t) * V .. + V - 1.  Single elements: element k is column k * T + t, so that the threads of a
-// warp touch neighbouring elements.
-template <int T, int V>
+// Which columns a thread holds.  VEC, 16-byte pieces of V elements: piece v of the thread covers columns
+// (v * T + t) * V .. + V - 1 and lies inside the row or outside it.  Else element k is column k * T + t,
+// so that the threads of a warp touch neighbouring elements.  A "part" is what is inside or outside as a
+// whole: a piece, or one element.
+template <int T, int V, bool VEC>
 struct Columns {
+    static constexpr int kPart = VEC ? V : 1;
     int t, cols;
-    bool vec;
-    __device__ __forceinline__ int of(int k) const
-    {
-        return vec ? ((k / V) * T + t) * V + k % V : k * T + t;
-    }
-    __device__ __forceinline__ bool has(int k) const     // a piece lies inside the row or outside it
-    {
-        return vec ? ((k / V) * T + t) * V < cols : k * T + t < cols;
-    }
+    __device__ __forceinline__ int of(int k) const { return VEC ? ((k / V) * T + t) * V + k % V : k * T + t; }
+    __device__ __forceinline__ bool has(int k) const { return of(k / kPart * kPart) < cols; }
 };
 
-template <class TE, int T, int V, int E>
-__device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, long long at, const Columns<T, V> &c,
+// for (every element k that lies in the row) body(k)
+template <int E, class Cols, class Body>
+__device__ __forceinline__ void for_columns(const Cols &c, Body body)
+{
+#pragma unroll
+    for (int k0 = 0; k0 < E; k0 += Cols::kPart) {
+        if (!c.has(k0)) continue;
+#pragma unroll
+        for (int e = 0; e < Cols::kPart; ++e) body(k0 + e);
+    }
+}
+
+template <class TE, int E, int T, int V, bool VEC>
+__device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, long long at, const Columns<T, V, VEC> &c,
                                          bool row_ok)
 {
     const TE *p = static_cast<const TE *>(base) + at;
-    constexpr int kStep = 16 / (int)sizeof(TE);
-    if (c.vec) {
+    if constexpr (VEC) {
+        constexpr int kStep = 16 / (int)sizeof(TE);
 #pragma unroll
         for (int k = 0; k < E; k += kStep) {
-            if (row_ok && c.has(k)) load16(r.w + k * (int)sizeof(TE) / 4, p + c.of(k));
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i) r.w[k * (int)sizeof(TE) / 4 + i] = 0u;
+            uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
+            w[0] = w[1] = w[2] = w[3] = 0u;
+            if (row_ok && c.has(k)) load16(w, p + c.of(k));
         }
     } else {
         r.clear();
@@ -92,19 +98,18 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
     }
 }
 
-template <class TE, int T, int V, int E>
-__device__ __forceinline__ void store_row(void *base, long long at, const Acc<TE> (&v)[E], const Columns<T, V> &c)
+template <class TE, int E, int T, int V, bool VEC>
+__device__ __forceinline__ void store_row(void *base, long long at, const Acc<TE> (&v)[E], const Columns<T, V, VEC> &c)
 {
     TE *p = static_cast<TE *>(base) + at;
-    constexpr int kStep = 16 / (int)sizeof(TE);
-    if (c.vec) {
+    if constexpr (VEC) {
+        constexpr int kStep = 16 / (int)sizeof(TE);
 #pragma unroll
         for (int k = 0; k < E; k += kStep) {
             if (!c.has(k)) continue;
             Packed<TE, kStep> r;
-            r.clear();
 #pragma unroll
-            for (int e = 0; e < kStep; ++e) r.put(e, narrow<TE>(v[k + e]));
+            for (int e = 0; e < kStep; e += 2) r.round2(e, v[k + e], v[k + e + 1]);
             store16(p + c.of(k), r.w);
         }
     } else {
@@ -114,49 +119,34 @@ __device__ __forceinline__ void store_row(void *base, long long at, const Acc<TE
     }
 }
 
-// A vector over the columns (weight, bias, scale, gate per column), `none` where there is none.
-template <class TE, int T, int V, int E>
-__device__ __forceinline__ void load_cols(Acc<TE> (&o)[E], const void *base, bool wide, const Columns<T, V> &c,
-                                          Acc<TE> none)
+// body(k, value) for the elements of a vector over the columns (weight, bias, scale, gate per column) that
+// lie in the row.  `wide`: the vector is float although the block has 16 bits.
+template <class TE, int E, int T, int V, bool VEC, class Body>
+__device__ __forceinline__ void for_vector(const void *base, bool wide, const Columns<T, V, VEC> &c, Body body)
 {
-    if (!base) {
+    if constexpr (!VEC) {
 #pragma unroll
-        for (int k = 0; k < E; ++k) o[k] = none;
-        return;
-    }
-    if (sizeof(TE) == 2 && wide) {
-        const float *p = static_cast<const float *>(base);
+        for (int k = 0; k < E; ++k) {
+            if (!c.has(k)) continue;
+            if (sizeof(TE) == 2 && wide) body(k, (Acc<TE>)__ldg(static_cast<const float *>(base) + c.of(k)));
+            else body(k, widen<TE>(static_cast<const TE *>(base)[c.of(k)]));
+        }
+    } else if (sizeof(TE) == 2 && wide) {
+#pragma unroll
+        for (int k = 0; k < E; k += 4) {
+            if (!c.has(k)) continue;
+            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(base) + c.of(k)));
+            body(k, (Acc<TE>)q.x), body(k + 1, (Acc<TE>)q.y), body(k + 2, (Acc<TE>)q.z), body(k + 3, (Acc<TE>)q.w);
+        }
+    } else {
 #pragma unroll
         for (int k = 0; k < E; k += V) {
-            if (c.vec) {
-                if (!c.has(k)) continue;
-#pragma unroll
-                for (int e = 0; e < V; e += 4) {
-                    const float4 q = __ldg(reinterpret_cast<const float4 *>(p + c.of(k) + e));
-                    o[k + e] = q.x, o[k + e + 1] = q.y, o[k + e + 2] = q.z, o[k + e + 3] = q.w;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (c.has(k + e)) o[k + e] = __ldg(p + c.of(k + e));
-            }
-        }
-        return;
-    }
-    const TE *p = static_cast<const TE *>(base);
-#pragma unroll
-    for (int k = 0; k < E; k += V) {
-        if (c.vec) {
             if (!c.has(k)) continue;
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(p + c.of(k)));
+            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + c.of(k)));
             Packed<TE, V> r;
             r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[k + e] = r.get(e);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (c.has(k + e)) o[k + e] = widen<TE>(p[c.of(k + e)]);
+            for (int e = 0; e < V; ++e) body(k + e, r.get(e));
         }
     }
 }
@@ -190,35 +180,36 @@ __device__ __forceinline__ void group_sum(A (&v)[N], A (*area)[3][32], int &buf)
     }
 }
 
-// Mean (0 for the root-mean-square norm) and 1 / sqrt(mean((t - mean)^2) + eps) of a row.  The mean
-// first and the centred squares after it, from registers: E[t^2] - mean^2 would cancel where a row's
-// mean is large against its spread.
-template <int T, int V, int E, class A>
-__device__ __forceinline__ void row_stats(const A (&t)[E], int kind, double eps, const Columns<T, V> &c,
-                                          A (*area)[3][32], int &buf, A &mean, A &r)
+// Mean (0 for the root-mean-square norm) and r = 1 / sqrt(mean((t - mean)^2) + eps) of a row, which is left
+// centred.  The mean first and the centred squares after it, from registers: E[t^2] - mean^2 would
+// cancel where a row's mean is large against its spread.
+template <class A>
+struct RowNorm {
+    A mean, r;
+};
+template <int E, class A, int T, int V, bool VEC>
+__device__ __forceinline__ RowNorm<A> row_norm(A (&t)[E], int kind, double eps, const Columns<T, V, VEC> &c,
+                                               A (*area)[3][32], int &buf)
 {
     const A inv = A(1) / A(c.cols);
+    RowNorm<A> n = {A(0), A(0)};
     A s[1] = {A(0)};
-    mean = A(0);
     if (kind == FO_NORM_LAYER) {
-#pragma unroll
-        for (int k = 0; k < E; ++k) s[0] += c.has(k) ? t[k] : A(0);
+        for_columns<E>(c, [&](int k) { s[0] += t[k]; });
         group_sum<T, 1, A>(s, area, buf);
-        mean = s[0] * inv;
+        n.mean = s[0] * inv;
         s[0] = A(0);
+        for_columns<E>(c, [&](int k) { t[k] -= n.mean; });
     }
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-        const A d = c.has(k) ? t[k] - mean : A(0);
-        s[0] = fused_ma(d, d, s[0]);
-    }
+    for_columns<E>(c, [&](int k) { s[0] = fused_ma(t[k], t[k], s[0]); });
     group_sum<T, 1, A>(s, area, buf);
-    r = group_rsqrt(fused_ma(s[0], inv, A(eps)));
+    n.r = group_rsqrt(fused_ma(s[0], inv, A(eps)));
+    return n;
 }
 
 // ------------------------------------------------------------------ forward
 // BLK: there is a block output f (else the norm of the stream alone).
-template <class TS, class TB, int T, int E, bool BLK>
+template <class TS, class TB, int T, int E, bool VEC, bool BLK>
 __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(const __grid_constant__ BlockNormParams p)
 {
     using A = Acc<TB>;
@@ -229,85 +220,64 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
     int buf = 0;
     const long long row = (long long)blockIdx.x * (kCta / T) + threadIdx.x / T;
     const bool ok = row < p.rows;
-    const Columns<T, V> c = {(int)(threadIdx.x % T), p.cols, p.vec != 0};
+    const Columns<T, V, VEC> c = {(int)(threadIdx.x % T), p.cols};
+    const bool wide = p.wide_vec != 0;
 
     Packed<TS, E> xr;
     Packed<TB, E> fr, gr;
-    if (BLK) load_row<TB, T, V, E>(fr, p.f, row * p.ld_f, c, ok);
-    if (p.x) load_row<TS, T, V, E>(xr, p.x, row * p.ld_x, c, ok);
+    if (BLK) load_row<TB, E>(fr, p.f, row * p.ld_f, c, ok);
+    if (!BLK || p.x) load_row<TS, E>(xr, p.x, row * p.ld_x, c, ok);
     else xr.clear();
-    if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, T, V, E>(gr, p.gate, row * p.ld_gate, c, ok);
+    if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
 
-    A stat[4] = {A(0), A(0), A(0), A(0)};
+    RowNorm<A> post = {A(0), A(0)}, pre = {A(0), A(0)};
     A h[E];
     if constexpr (BLK) {
-        A w[E];
+        A scale = A(p.scale);
 #pragma unroll
         for (int k = 0; k < E; ++k) h[k] = fr.get(k);
         if (p.post.kind != FO_NORM_NONE) {
-            row_stats<T, V, E, A>(h, p.post.kind, p.post.eps, c, area, buf, stat[0], stat[1]);
+            post = row_norm<E>(h, p.post.kind, p.post.eps, c, area, buf);
 #pragma unroll
-            for (int k = 0; k < E; ++k) h[k] = (h[k] - stat[0]) * stat[1];
-            if (p.post.weight) {
-                load_cols<TB, T, V, E>(w, p.post.weight, p.wide_vec, c, A(1));
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] *= w[k];
-            }
-            if (p.post.bias) {
-                load_cols<TB, T, V, E>(w, p.post.bias, p.wide_vec, c, A(0));
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] += w[k];
-            }
+            for (int k = 0; k < E; ++k) h[k] *= post.r;
+            if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { h[k] *= w; });
+            if (p.post.bias) for_vector<TB, E>(p.post.bias, wide, c, [&](int k, A b) { h[k] += b; });
         }
-        if (p.gate_access == FO_AT_CELL) {
-#pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= activate<kFast, A>(p.gate_act, gr.get(k));
-        } else if (p.gate_access == FO_AT_COL) {
-            load_cols<TB, T, V, E>(w, p.gate, false, c, A(0));
-#pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= activate<kFast, A>(p.gate_act, w[k]);
-        } else if (p.gate_access == FO_AT_ROW) {
+        if (p.gate_access == FO_AT_ROW) {
             const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
-            const A a = activate<kFast, A>(p.gate_act, g);
+            with_activation(p.gate_act, [&](auto kind) { scale *= activate<decltype(kind)::value, kFast, A>(g); });
+        } else if (p.gate_access == FO_AT_CELL) {
+            with_activation(p.gate_act, [&](auto kind) {
 #pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= a;
+                for (int k = 0; k < E; ++k) h[k] *= activate<decltype(kind)::value, kFast, A>(gr.get(k));
+            });
+        } else if (p.gate_access == FO_AT_COL) {
+            with_activation(p.gate_act, [&](auto kind) {
+                for_vector<TB, E>(p.gate, false, c,
+                                  [&](int k, A g) { h[k] *= activate<decltype(kind)::value, kFast, A>(g); });
+            });
         }
-        if (p.col_scale) {
-            load_cols<TB, T, V, E>(w, p.col_scale, p.wide_vec, c, A(1));
-#pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= w[k];
-        }
-        const A scale = A(p.scale);
+        if (p.col_scale) for_vector<TB, E>(p.col_scale, wide, c, [&](int k, A w) { h[k] *= w; });
 #pragma unroll
         for (int k = 0; k < E; ++k) h[k] = fused_ma(h[k], scale, A(xr.get(k)));
     } else {
 #pragma unroll
         for (int k = 0; k < E; ++k) h[k] = A(xr.get(k));
     }
-    if (p.h && ok) store_row<TS, T, V, E>(p.h, row * p.ld_h, h, c);
+    if (p.h && ok) store_row<TS, E>(p.h, row * p.ld_h, h, c);
     if (p.pre.kind != FO_NORM_NONE) {
-        A w[E];
-        row_stats<T, V, E, A>(h, p.pre.kind, p.pre.eps, c, area, buf, stat[2], stat[3]);
-        if (p.y) {
+        pre = row_norm<E>(h, p.pre.kind, p.pre.eps, c, area, buf);
+        if (p.y && ok) {
 #pragma unroll
-            for (int k = 0; k < E; ++k) h[k] = (h[k] - stat[2]) * stat[3];
-            if (p.pre.weight) {
-                load_cols<TB, T, V, E>(w, p.pre.weight, p.wide_vec, c, A(1));
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] *= w[k];
-            }
-            if (p.pre.bias) {
-                load_cols<TB, T, V, E>(w, p.pre.bias, p.wide_vec, c, A(0));
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] += w[k];
-            }
-            if (ok) store_row<TB, T, V, E>(p.y, row * p.ld_y, h, c);
+            for (int k = 0; k < E; ++k) h[k] *= pre.r;
+            if (p.pre.weight) for_vector<TB, E>(p.pre.weight, wide, c, [&](int k, A w) { h[k] *= w; });
+            if (p.pre.bias) for_vector<TB, E>(p.pre.bias, wide, c, [&](int k, A b) { h[k] += b; });
+            store_row<TB, E>(p.y, row * p.ld_y, h, c);
         }
     }
     if (p.stats && ok && c.t == 0) {
-        A *s = static_cast<A *>(p.stats);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) s[(long long)k * p.rows + row] = stat[k];
+        A *s = static_cast<A *>(p.stats) + row;
+        s[0] = post.mean, s[p.rows] = post.r, s[2 * p.rows] = pre.mean, s[3 * p.rows] = pre.r;
     }
 }
 
@@ -329,7 +299,7 @@ __host__ __device__ constexpr int slots_held()
     return FORM == kGradStream ? 2 : FORM == kGradLean ? 3 : kGradSlots;
 }
 
-template <class TS, class TB, int T, int E, int FORM>
+template <class TS, class TB, int T, int E, bool VEC, int FORM>
 __global__ void __launch_bounds__(T > 32 ? T : kGroupCta)
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
@@ -342,9 +312,10 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     constexpr int NS = slots_held<FORM>();
     __shared__ A area[2][3][32];
     int buf = 0;
-    const Columns<T, V> c = {(int)(threadIdx.x % T), p.cols, p.vec != 0};
+    const Columns<T, V, VEC> c = {(int)(threadIdx.x % T), p.cols};
     const A inv = A(1) / A(p.cols);
     const A *stats = static_cast<const A *>(p.stats);
+    const bool wide = p.wide_vec != 0;
 
     A acc[NS][E];
 #pragma unroll
@@ -367,93 +338,119 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         Packed<TS, E> dhr, hr;
         Packed<TB, E> dyr, fr, gr;
         if (p.dy) {
-            load_row<TB, T, V, E>(dyr, p.dy, row * p.ld_dy, c, ok);
-            load_row<TS, T, V, E>(hr, p.h, row * p.ld_h, c, ok);
+            load_row<TB, E>(dyr, p.dy, row * p.ld_dy, c, ok);
+            load_row<TS, E>(hr, p.h, row * p.ld_h, c, ok);
         }
-        if (p.dh) load_row<TS, T, V, E>(dhr, p.dh, row * p.ld_dh, c, ok);
+        if (p.dh) load_row<TS, E>(dhr, p.dh, row * p.ld_dh, c, ok);
         else dhr.clear();
-        if (BLK) load_row<TB, T, V, E>(fr, p.f, row * p.ld_f, c, ok);
-        if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, T, V, E>(gr, p.gate, row * p.ld_gate, c, ok);
+        if (BLK) load_row<TB, E>(fr, p.f, row * p.ld_f, c, ok);
+        if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
 
-        A t[E], w[E];
-#pragma unroll
-        for (int k = 0; k < E; ++k) t[k] = A(dhr.get(k));
+        A t[E];
         if (p.dy) {
             const A mean = ok ? stats[2 * p.rows + row] : A(0), r = ok ? stats[3 * p.rows + row] : A(0);
-            load_cols<TB, T, V, E>(w, p.pre.weight, p.wide_vec, c, A(1));
-            A s[2] = {A(0), A(0)};
 #pragma unroll
-            for (int k = 0; k < E; ++k) {
-                if (!c.has(k)) continue;
-                const A dy = dyr.get(k), n = (A(hr.get(k)) - mean) * r, a = dy * w[k];
-                s[0] = fused_ma(a, n, s[0]);
-                s[1] += a;
+            for (int k = 0; k < E; ++k) t[k] = dyr.get(k);
+            if (p.pre.weight) for_vector<TB, E>(p.pre.weight, wide, c, [&](int k, A w) { t[k] *= w; });
+            A s[2] = {A(0), A(0)};
+            for_columns<E>(c, [&](int k) {
+                const A dy = dyr.get(k), n = (A(hr.get(k)) - mean) * r;
+                s[0] = fused_ma(t[k], n, s[0]);
+                s[1] += t[k];
                 add_product(std::integral_constant<int, kPreW>(), k, dy, n);
                 add(std::integral_constant<int, kPreB>(), k, dy);
-            }
+            });
             group_sum<T, 2, A>(s, area, buf);
-            const A along = s[0] * inv, common = p.pre.kind == FO_NORM_LAYER ? s[1] * inv : A(0);
+            // dh + r (a - n along - common)
+            const A slope = -s[0] * inv * r * r, level = p.pre.kind == FO_NORM_LAYER ? -s[1] * inv * r : A(0);
 #pragma unroll
-            for (int k = 0; k < E; ++k) {
-                const A n = (A(hr.get(k)) - mean) * r;
-                t[k] = fused_ma(r, fused_ma(-n, along, A(dyr.get(k)) * w[k] - common), t[k]);
-            }
+            for (int k = 0; k < E; ++k)
+                t[k] = fused_ma(t[k], r, fused_ma(A(hr.get(k)) - mean, slope, A(dhr.get(k)) + level));
+        } else {
+#pragma unroll
+            for (int k = 0; k < E; ++k) t[k] = A(dhr.get(k));
         }
-        if (p.dx && ok) store_row<TS, T, V, E>(p.dx, row * p.ld_dx, t, c);
+        if (p.dx && ok) store_row<TS, E>(p.dx, row * p.ld_dx, t, c);
         if constexpr (BLK) {
             const bool normed = p.post.kind != FO_NORM_NONE;
-            const A mean = ok && normed ? stats[row] : A(0), r = ok ? (normed ? stats[p.rows + row] : A(1)) : A(0);
-            A gate = A(1), slope = A(0);
-            if (p.gate_access == FO_AT_ROW)
-                gate = activate_slope<kFast, A>(p.gate_act, ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate])
-                                                              : A(0), slope);
-            A cs[E], g[E], b[E];
-            load_cols<TB, T, V, E>(w, p.post.weight, p.wide_vec, c, A(1));
-            load_cols<TB, T, V, E>(b, p.post.bias, p.wide_vec, c, A(0));
-            load_cols<TB, T, V, E>(cs, p.col_scale, p.wide_vec, c, A(1));
-            if (p.gate_access == FO_AT_COL) load_cols<TB, T, V, E>(g, p.gate, false, c, A(0));
-            if (p.gate_access == FO_AT_CELL) {
-#pragma unroll
-                for (int k = 0; k < E; ++k) g[k] = gr.get(k);
-            }
-            A s[3] = {A(0), A(0), A(0)};
+            const A mean = ok && normed ? stats[row] : A(0), r = ok && normed ? stats[p.rows + row] : A(1);
             const A scale = A(p.scale);
+            A z[E];                                          // act(gate) z, then what of it reaches the sums
 #pragma unroll
             for (int k = 0; k < E; ++k) {
-                if (!c.has(k)) continue;
-                const A n = (fr.get(k) - mean) * r;
-                const A z = fused_ma(n, w[k], b[k]);
-                A a = gate, da = slope;
-                if (p.gate_access == FO_AT_CELL || p.gate_access == FO_AT_COL)
-                    a = activate_slope<kFast, A>(p.gate_act, g[k], da);
-                const A q = t[k] * scale;
-                add_product(std::integral_constant<int, kColScale>(), k, q, a * z);
-                const A qc = q * cs[k];
-                const A dg = qc * z * da;
-                add(std::integral_constant<int, kGateCol>(), k, dg);
-                s[2] += dg;
-                g[k] = dg;
-                const A d = qc * a;
-                add_product(std::integral_constant<int, kPostW>(), k, d, n);
-                add(std::integral_constant<int, kPostB>(), k, d);
-                t[k] = d;
-                const A aw = d * w[k];
-                s[0] = fused_ma(aw, n, s[0]);
-                s[1] += aw;
+                t[k] *= scale;
+                z[k] = (fr.get(k) - mean) * r;
             }
-            if (p.dgate && ok && p.gate_access == FO_AT_CELL)
-                store_row<TB, T, V, E>(p.dgate, row * p.ld_dgate, g, c);
+            if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { z[k] *= w; });
+            if (p.post.bias) for_vector<TB, E>(p.post.bias, wide, c, [&](int k, A b) { z[k] += b; });
+            A s[3] = {A(0), A(0), A(0)};
+            // q = t; col_scale's sum takes q act z; then q' = q col_scale, dgate = q' z act', d = q' act
+            auto through_gate = [&](auto gate_at) {
+                if (p.col_scale) {
+                    for_vector<TB, E>(p.col_scale, wide, c, [&](int k, A w) {
+                        A slope;
+                        const A a = gate_at(k, slope);
+                        add_product(std::integral_constant<int, kColScale>(), k, t[k], a * z[k]);
+                        const A q = t[k] * w;
+                        z[k] *= q * slope;
+                        t[k] = q * a;
+                    });
+                } else {
+                    for_columns<E>(c, [&](int k) {
+                        A slope;
+                        const A a = gate_at(k, slope);
+                        z[k] *= t[k] * slope;
+                        t[k] *= a;
+                    });
+                }
+            };
+            if (p.gate_access < 0) {
+                through_gate([&](int, A &slope) {
+                    slope = A(0);
+                    return A(1);
+                });
+            } else if (p.gate_access == FO_AT_ROW) {
+                const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
+                A a = A(0), da = A(0);
+                with_activation(p.gate_act, [&](auto kind) { a = activate_slope<decltype(kind)::value, kFast, A>(g, da); });
+                through_gate([&](int, A &slope) {
+                    slope = da;
+                    return a;
+                });
+                for_columns<E>(c, [&](int k) { s[2] += z[k]; });
+            } else if (p.gate_access == FO_AT_CELL) {
+                with_activation(p.gate_act, [&](auto kind) {
+                    through_gate(
+                        [&](int k, A &slope) { return activate_slope<decltype(kind)::value, kFast, A>(gr.get(k), slope); });
+                });
+                if (p.dgate && ok) store_row<TB, E>(p.dgate, row * p.ld_dgate, z, c);
+            } else {
+                A g[E];
+                for_vector<TB, E>(p.gate, false, c, [&](int k, A v) { g[k] = v; });
+                with_activation(p.gate_act, [&](auto kind) {
+                    through_gate([&](int k, A &slope) { return activate_slope<decltype(kind)::value, kFast, A>(g[k], slope); });
+                });
+                for_columns<E>(c, [&](int k) { add(std::integral_constant<int, kGateCol>(), k, z[k]); });
+            }
+            if (normed) {
+                for_columns<E>(c, [&](int k) {
+                    add_product(std::integral_constant<int, kPostW>(), k, t[k], (fr.get(k) - mean) * r);
+                    add(std::integral_constant<int, kPostB>(), k, t[k]);
+                });
+                if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { t[k] *= w; });
+                for_columns<E>(c, [&](int k) {
+                    s[0] = fused_ma(t[k], (fr.get(k) - mean) * r, s[0]);
+                    s[1] += t[k];
+                });
+            }
             if (normed || (p.dgate && p.gate_access == FO_AT_ROW)) group_sum<T, 3, A>(s, area, buf);
             if (p.dgate && ok && p.gate_access == FO_AT_ROW && c.t == 0) static_cast<A *>(p.dgate)[row] = s[2];
             if (normed) {
-                const A along = s[0] * inv, common = p.post.kind == FO_NORM_LAYER ? s[1] * inv : A(0);
+                const A slope = -s[0] * inv * r * r, level = p.post.kind == FO_NORM_LAYER ? -s[1] * inv * r : A(0);
 #pragma unroll
-                for (int k = 0; k < E; ++k) {
-                    const A n = (fr.get(k) - mean) * r;
-                    t[k] = r * fused_ma(-n, along, t[k] * w[k] - common);
-                }
+                for (int k = 0; k < E; ++k) t[k] = fused_ma(t[k], r, fused_ma(fr.get(k) - mean, slope, level));
             }
-            if (p.df && ok) store_row<TB, T, V, E>(p.df, row * p.ld_df, t, c);
+            if (p.df && ok) store_row<TB, E>(p.df, row * p.ld_df, t, c);
         }
     }
 

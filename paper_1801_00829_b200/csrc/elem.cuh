@@ -44,6 +44,20 @@ struct Packed {
             return __uint_as_float((k & 1) ? (w[k / 2] & 0xffff0000u) : (w[k / 2] << 16));
         else return __half2float(__ushort_as_half((unsigned short)((k & 1) ? (w[k / 2] >> 16) : (w[k / 2] & 0xffffu))));
     }
+    // elements k and k + 1 (k even) from sums, rounded once
+    __device__ __forceinline__ void round2(int k, Acc<T> a, Acc<T> b)
+    {
+        if constexpr (sizeof(T) >= 4) {
+            put(k, (T)a);
+            put(k + 1, (T)b);
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+            memcpy(&w[k / 2], &v, 4);
+        } else {
+            const __half2 v = __floats2half2_rn(a, b);
+            memcpy(&w[k / 2], &v, 4);
+        }
+    }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
@@ -99,34 +113,48 @@ __device__ __forceinline__ A sigmoid(A g)
     else return A(1) / (A(1) + exp_neg<A>(g));
 }
 
-template <bool FAST, class A>
-__device__ __forceinline__ A activate(int kind, A g)
+template <int KIND, bool FAST, class A>
+__device__ __forceinline__ A activate(A g)
 {
-    if (kind == FO_ACT_LINEAR) return g;
-    if (kind == FO_ACT_TANH) return tanh_of(g);
-    const A s = sigmoid<FAST, A>(g);
-    return kind == FO_ACT_SILU ? g * s : s;
+    if constexpr (KIND == FO_ACT_LINEAR) return g;
+    else if constexpr (KIND == FO_ACT_TANH) return tanh_of(g);
+    else {
+        const A s = sigmoid<FAST, A>(g);
+        return KIND == FO_ACT_SILU ? g * s : s;
+    }
 }
 
-template <bool FAST, class A>
-__device__ __forceinline__ A activate_slope(int kind, A g, A &slope)
+template <int KIND, bool FAST, class A>
+__device__ __forceinline__ A activate_slope(A g, A &slope)
 {
-    if (kind == FO_ACT_LINEAR) {
+    if constexpr (KIND == FO_ACT_LINEAR) {
         slope = A(1);
         return g;
-    }
-    if (kind == FO_ACT_TANH) {
+    } else if constexpr (KIND == FO_ACT_TANH) {
         const A t = tanh_of(g);
-        slope = A(1) - t * t;
+        slope = fused_ma(-t, t, A(1));
         return t;
+    } else {
+        const A s = sigmoid<FAST, A>(g);
+        if constexpr (KIND == FO_ACT_SIGMOID) {
+            slope = fused_ma(-s, s, s);
+            return s;
+        }
+        const A a = g * s;
+        slope = fused_ma(a, A(1) - s, s);
+        return a;
     }
-    const A s = sigmoid<FAST, A>(g);
-    if (kind == FO_ACT_SIGMOID) {
-        slope = s * (A(1) - s);
-        return s;
-    }
-    slope = s * (A(1) + g * (A(1) - s));
-    return g * s;
+}
+
+// Calls go(kind) with the activation as a compile-time number, so that loops over elements do not
+// branch on it.
+template <class Go>
+__device__ __forceinline__ void with_activation(int kind, Go go)
+{
+    if (kind == FO_ACT_LINEAR) go(std::integral_constant<int, FO_ACT_LINEAR>());
+    else if (kind == FO_ACT_SIGMOID) go(std::integral_constant<int, FO_ACT_SIGMOID>());
+    else if (kind == FO_ACT_SILU) go(std::integral_constant<int, FO_ACT_SILU>());
+    else go(std::integral_constant<int, FO_ACT_TANH>());
 }
 
 }  // namespace fo
