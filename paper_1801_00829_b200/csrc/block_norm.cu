@@ -14,7 +14,7 @@ namespace fo {
 
 #define FO_EXTERN(s, b, TS, TB)                                                                    \
     extern template cudaError_t launch_block_norm<TS, TB>(const BlockNormParams &, cudaStream_t);  \
-    extern template cudaError_t launch_block_norm_grad<TS, TB>(BlockNormGradParams, int, int, int *, cudaStream_t);
+    extern template cudaError_t launch_block_norm_grad<TS, TB>(BlockNormGradParams, GradSpace *, cudaStream_t);
 FO_PAIRS(FO_EXTERN)
 #undef FO_EXTERN
 
@@ -74,13 +74,27 @@ int check_gate(const void *gate, int access, int act, long long ld, long long ro
     return FO_OK;
 }
 
-// Upper bound on the CTAs that leave a line of partial column sums: a few per SM for short rows,
+// Upper bound on the CTAs (clusters) that leave a line of partial column sums: a few per SM for short rows,
 // one per SM for long ones, whose lines are long.
-int grad_ctas(long long rows, long long cols)
+int grad_lines(long long rows, long long cols)
 {
     const long long cap = cols <= 1024 ? 148 * 4 : cols <= 4096 ? 148 * 2 : 148;
     const long long n = rows < cap ? rows : cap;
     return (int)(n > 1 ? n : 1);
+}
+
+// Lines, and room for the sums of CTAs that shared memory does not hold: 8192 columns in each of a row's
+// one, two or four CTAs.
+size_t grad_line_bytes(long long rows, long long cols, int block_type)
+{
+    return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
+}
+size_t grad_sum_bytes(long long rows, long long cols, int block_type)
+{
+    const size_t bytes = block_type == FO_F64 ? 8 : 4, slot = (size_t)512 * 16 * bytes;
+    if (kGradSlots * slot <= 220 * 1024 || cols <= 4096) return 0;
+    const size_t held = cols <= 8192 ? 8192 : cols <= 16384 ? 16384 : 32768;
+    return (size_t)kGradSlots * grad_lines(rows, cols) * held * bytes;
 }
 
 }  // namespace
@@ -138,7 +152,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
 size_t fused_block_norm_grad_workspace_bytes(int64_t rows, int64_t cols, int block_type)
 {
     if (check_shape(rows, cols) != FO_OK || block_type < FO_F64 || block_type > FO_F16) return 0;
-    return sizeof(WsHead) + (size_t)kGradSlots * grad_ctas(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
+    return sizeof(WsHead) + (grad_line_bytes(rows, cols, block_type) + 255) / 256 * 256 + grad_sum_bytes(rows, cols, block_type);
 }
 
 int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes, void *stream)
@@ -208,17 +222,15 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
         p.slots |= 1u << s;
         cs.out[n_sums++] = sums[s];
     }
-    const unsigned lean = (1u << kPreW) | (1u << kPostW) | (1u << kColScale);
-    const int form = !a->f ? kGradStream : (p.slots & ~lean) == 0 ? kGradLean : kGradAll;
+    GradSpace space = {grad_lines(a->rows, a->cols), 0,
+                       static_cast<char *>(p.partial) + (grad_line_bytes(a->rows, a->cols, a->block_type) + 255) / 256 * 256};
     cudaError_t e = cudaErrorInvalidValue;
-    int ctas = 0;
-#define FO_CASE(s, b, TS, TB)                           \
-    if (a->stream_type == s && a->block_type == b)      \
-        e = launch_block_norm_grad<TS, TB>(p, form, grad_ctas(a->rows, a->cols), &ctas, st);
+#define FO_CASE(s, b, TS, TB) \
+    if (a->stream_type == s && a->block_type == b) e = launch_block_norm_grad<TS, TB>(p, &space, st);
     FO_PAIRS(FO_CASE)
 #undef FO_CASE
     if (e == cudaSuccess && n_sums > 0) {
-        cs.partial = p.partial, cs.ctas = ctas, cs.cols = p.cols;
+        cs.partial = p.partial, cs.lines = space.lines, cs.cols = p.cols;
         const dim3 grid((unsigned)((a->cols + 31) / 32), (unsigned)n_sums);
         if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, 256, 0, st>>>(cs);
         else column_sum_kernel<float><<<grid, 256, 0, st>>>(cs);
