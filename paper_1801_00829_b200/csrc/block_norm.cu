@@ -123,7 +123,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
     if (rc != FO_OK) return rc;
 
     BlockNormParams p = {};
-    p.rows = a->rows, p.cols = (int)a->cols;
+    p.rows = a->rows, p.cols = (int)a->cols, p.inv_cols = 1.0 / (double)a->cols;
     p.wide_vec = a->vec_type != a->block_type;
     p.gate_access = a->gate ? a->gate_access : -1, p.gate_act = a->gate_act;
     p.x = a->x, p.f = a->f, p.gate = a->gate, p.col_scale = a->col_scale;
@@ -193,7 +193,7 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     rc = check_workspace(ws, ws_bytes, fused_block_norm_grad_workspace_bytes(a->rows, a->cols, a->block_type));
     if (rc != FO_OK) return rc;
     BlockNormGradParams p = {};
-    p.rows = a->rows, p.cols = (int)a->cols;
+    p.rows = a->rows, p.cols = (int)a->cols, p.inv_cols = 1.0 / (double)a->cols;
     p.wide_vec = a->vec_type != a->block_type;
     p.gate_access = a->gate ? a->gate_access : -1, p.gate_act = a->gate_act;
     p.dh = a->dh, p.dy = a->dy, p.h = a->h, p.f = a->f, p.gate = a->gate, p.col_scale = a->col_scale, p.stats = a->stats;

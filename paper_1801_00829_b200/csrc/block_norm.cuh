@@ -28,6 +28,7 @@ struct BlockNormParams {
     long long rows;
     int cols;
     int vec;                                 // rows move in 16-byte pieces
+    double inv_cols;                         // 1 / cols
     int wide_vec;                            // vectors are float although the block has 16 bits
     int gate_access, gate_act;               // gate_access -1: none
     const void *x, *f, *gate, *col_scale;
@@ -42,6 +43,7 @@ struct BlockNormGradParams {
     long long rows;
     int cols;
     int vec, wide_vec;
+    double inv_cols;
     int gate_access, gate_act;
     const void *dh, *dy, *h, *f, *gate, *col_scale, *stats;
     long long ld_dh, ld_dy, ld_h, ld_f, ld_gate;
@@ -56,27 +58,20 @@ struct BlockNormGradParams {
 
 // Which columns a thread holds.  VEC, 16-byte pieces of V elements: piece v of the thread covers columns
 // (v * T + t) * V .. + V - 1 and lies inside the row or outside it.  Else element k is column k * T + t,
-// so that the threads of a warp touch neighbouring elements.  A "part" is what is inside or outside as a
-// whole: a piece, or one element.
+// so that the threads of a warp touch neighbouring elements.  Values outside the row are held as zeros.
 template <int T, int V, bool VEC>              // T: threads of the row, over all its CTAs
 struct Columns {
-    static constexpr int kPart = VEC ? V : 1;
     int t, cols;
     __device__ __forceinline__ int of(int k) const { return VEC ? ((k / V) * T + t) * V + k % V : k * T + t; }
-    __device__ __forceinline__ bool has(int k) const { return of(k / kPart * kPart) < cols; }
-};
-
-// for (every element k that lies in the row) body(k)
-template <int E, class Cols, class Body>
-__device__ __forceinline__ void for_columns(const Cols &c, Body body)
-{
-#pragma unroll
-    for (int k0 = 0; k0 < E; k0 += Cols::kPart) {
-        if (!c.has(k0)) continue;
-#pragma unroll
-        for (int e = 0; e < Cols::kPart; ++e) body(k0 + e);
+    __device__ __forceinline__ bool has(int k) const { return of(VEC ? k / V * V : k) < cols; }
+    // elements k and k + 1 (k even) with zeros outside the row
+    template <class A>
+    __device__ __forceinline__ Two<A> inside(int k, Two<A> v) const
+    {
+        if constexpr (VEC) return has(k) ? v : both(A(0));
+        else return two(has(k) ? first(v) : A(0), has(k + 1) ? second(v) : A(0));
     }
-}
+};
 
 template <class TE, int E, int T, int V, bool VEC>
 __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, long long at, const Columns<T, V, VEC> &c,
@@ -99,56 +94,78 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
     }
 }
 
-template <class TE, int E, int T, int V, bool VEC>
-__device__ __forceinline__ void store_row(void *base, long long at, const Acc<TE> (&v)[E], const Columns<T, V, VEC> &c)
+// Stores elements k0 .. k0 + N - 1 of the thread.
+template <class TE, int N, int T, int V, bool VEC>
+__device__ __forceinline__ void store_piece(TE *p, const Two<Acc<TE>> *v, int k0, const Columns<T, V, VEC> &c)
 {
-    TE *p = static_cast<TE *>(base) + at;
     if constexpr (VEC) {
         constexpr int kStep = 16 / (int)sizeof(TE);
 #pragma unroll
-        for (int k = 0; k < E; k += kStep) {
-            if (!c.has(k)) continue;
+        for (int k = 0; k < N; k += kStep) {
+            if (!c.has(k0 + k)) continue;
             Packed<TE, kStep> r;
 #pragma unroll
-            for (int e = 0; e < kStep; e += 2) r.round2(e, v[k + e], v[k + e + 1]);
-            store16(p + c.of(k), r.w);
+            for (int e = 0; e < kStep; e += 2) r.put2(e, v[(k + e) / 2]);
+            store16(p + c.of(k0 + k), r.w);
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < E; ++k)
-            if (c.has(k)) p[c.of(k)] = narrow<TE>(v[k]);
+        for (int k = 0; k < N; ++k)
+            if (c.has(k0 + k)) p[c.of(k0 + k)] = narrow<TE>(k & 1 ? second(v[k / 2]) : first(v[k / 2]));
     }
 }
 
-// body(k, value) for the elements of a vector over the columns (weight, bias, scale, gate per column) that
-// lie in the row.  `wide`: the vector is float although the block has 16 bits.
-template <class TE, int E, int T, int V, bool VEC, class Body>
-__device__ __forceinline__ void for_vector(const void *base, bool wide, const Columns<T, V, VEC> &c, Body body)
+// N elements from k0 of a vector over the columns (weight, bias, scale, gate per column).  `wide`: the
+// vector is float although the block has 16 bits.  Outside the row it gives some value of the vector,
+// which meets a zero there: no zeros have to be put where a load might not take place.
+template <class TE, int N, int T, int V, bool VEC>
+__device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void *base, bool wide, int k0,
+                                            const Columns<T, V, VEC> &c)
 {
+    using A = Acc<TE>;
     if constexpr (!VEC) {
+        auto at = [&](int k) -> A {
+            const int j = min(c.of(k), c.cols - 1);
+            if (sizeof(TE) == 2 && wide) return (A)__ldg(static_cast<const float *>(base) + j);
+            return widen<TE>(static_cast<const TE *>(base)[j]);
+        };
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-            if (!c.has(k)) continue;
-            if (sizeof(TE) == 2 && wide) body(k, (Acc<TE>)__ldg(static_cast<const float *>(base) + c.of(k)));
-            else body(k, widen<TE>(static_cast<const TE *>(base)[c.of(k)]));
-        }
+        for (int k = 0; k < N; k += 2) o[k / 2] = two(at(k0 + k), at(k0 + k + 1));
     } else if (sizeof(TE) == 2 && wide) {
 #pragma unroll
-        for (int k = 0; k < E; k += 4) {
-            if (!c.has(k)) continue;
-            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(base) + c.of(k)));
-            body(k, (Acc<TE>)q.x), body(k + 1, (Acc<TE>)q.y), body(k + 2, (Acc<TE>)q.z), body(k + 3, (Acc<TE>)q.w);
+        for (int k = 0; k < N; k += 4) {
+            const int j = min(c.of((k0 + k) / V * V), c.cols - V) + (k0 + k) % V;
+            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(base) + j));
+            o[k / 2] = two((A)q.x, (A)q.y), o[k / 2 + 1] = two((A)q.z, (A)q.w);
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < E; k += V) {
-            if (!c.has(k)) continue;
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + c.of(k)));
+        for (int k = 0; k < N; k += V) {
+            const int j = min(c.of(k0 + k), c.cols - V);
+            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + j));
             Packed<TE, V> r;
             r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
 #pragma unroll
-            for (int e = 0; e < V; ++e) body(k + e, r.get(e));
+            for (int e = 0; e < V; e += 2) o[(k + e) / 2] = r.get2(e);
         }
+    }
+}
+
+// Elements that are worked on at a time where vectors over the columns are read.
+template <class TB, bool VEC>
+constexpr int kPieceOf = VEC ? 16 / (int)sizeof(TB) : 16 / (int)sizeof(Acc<TB>);
+
+// h = op(h, vector) over the thread's elements
+template <class TE, int E, class Cols, class Op>
+__device__ __forceinline__ void with_vector(Two<Acc<TE>> (&h)[E / 2], const void *base, bool wide, const Cols &c, Op op)
+{
+    constexpr int P = 16 / (int)sizeof(TE);
+#pragma unroll
+    for (int k0 = 0; k0 < E; k0 += P) {
+        Two<Acc<TE>> w[P / 2];
+        load_vector<TE, P>(w, base, wide, k0, c);
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) h[k0 / 2 + i] = op(h[k0 / 2 + i], w[i]);
     }
 }
 
@@ -224,21 +241,27 @@ struct RowNorm {
     A mean, r;
 };
 template <int T, int C, int E, class A, class Cols>
-__device__ __forceinline__ RowNorm<A> row_norm(A (&t)[E], int kind, double eps, const Cols &c, Area<A> &area, int &buf)
+__device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, Area<A> &area, int &buf)
 {
-    const A inv = A(1) / A(c.cols);
     RowNorm<A> n = {A(0), A(0)};
-    A s[1] = {A(0)};
+    A s[1];
     if (kind == FO_NORM_LAYER) {
-        for_columns<E>(c, [&](int k) { s[0] += t[k]; });
+        Two<A> sum = t[0];
+#pragma unroll
+        for (int i = 1; i < E; ++i) sum = sum + t[i];
+        s[0] = joined(sum);
         group_sum<T, C, 1, A>(s, area, buf);
         n.mean = s[0] * inv;
-        s[0] = A(0);
-        for_columns<E>(c, [&](int k) { t[k] -= n.mean; });
+        const Two<A> minus = both(-n.mean);
+#pragma unroll
+        for (int i = 0; i < E; ++i) t[i] = c.inside(2 * i, t[i] + minus);
     }
-    for_columns<E>(c, [&](int k) { s[0] = fused_ma(t[k], t[k], s[0]); });
+    Two<A> sum = t[0] * t[0];
+#pragma unroll
+    for (int i = 1; i < E; ++i) sum = fused_ma(t[i], t[i], sum);
+    s[0] = joined(sum);
     group_sum<T, C, 1, A>(s, area, buf);
-    n.r = group_rsqrt(fused_ma(s[0], inv, A(eps)));
+    n.r = group_rsqrt(fused_ma(s[0], inv, eps));
     return n;
 }
 
@@ -257,6 +280,9 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
     const bool ok = row < p.rows;
     const Columns<T * C, V, VEC> c = {(int)(threadIdx.x % T + (C > 1 ? cluster_rank() * T : 0)), p.cols};
     const bool wide = p.wide_vec != 0;
+    const A inv = A(p.inv_cols);
+    const auto times = [](Two<A> h, Two<A> w) { return h * w; };
+    const auto plus = [](Two<A> h, Two<A> b) { return h + b; };
 
     Packed<TS, E> xr;
     Packed<TB, E> fr, gr;
@@ -266,48 +292,55 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
     if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
 
     RowNorm<A> post = {A(0), A(0)}, pre = {A(0), A(0)};
-    A h[E];
+    Two<A> h[E / 2];
     if constexpr (BLK) {
         A scale = A(p.scale);
 #pragma unroll
-        for (int k = 0; k < E; ++k) h[k] = fr.get(k);
+        for (int k = 0; k < E; k += 2) h[k / 2] = fr.get2(k);
         if (p.post.kind != FO_NORM_NONE) {
-            post = row_norm<T, C, E>(h, p.post.kind, p.post.eps, c, area, buf);
+            post = row_norm<T, C>(h, p.post.kind, A(p.post.eps), inv, c, area, buf);
+            const Two<A> r = both(post.r);
 #pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= post.r;
-            if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { h[k] *= w; });
-            if (p.post.bias) for_vector<TB, E>(p.post.bias, wide, c, [&](int k, A b) { h[k] += b; });
+            for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
+            if (p.post.weight) with_vector<TB, E>(h, p.post.weight, wide, c, times);
+            if (p.post.bias) with_vector<TB, E>(h, p.post.bias, wide, c, plus);
         }
         if (p.gate_access == FO_AT_ROW) {
             const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
-            with_activation(p.gate_act, [&](auto kind) { scale *= activate<decltype(kind)::value, kFast, A>(g); });
+            with_activation(p.gate_act, [&](auto kind) { scale *= first(activate<decltype(kind)::value, kFast, A>(both(g))); });
         } else if (p.gate_access == FO_AT_CELL) {
             with_activation(p.gate_act, [&](auto kind) {
 #pragma unroll
-                for (int k = 0; k < E; ++k) h[k] *= activate<decltype(kind)::value, kFast, A>(gr.get(k));
+                for (int k = 0; k < E; k += 2) h[k / 2] = h[k / 2] * activate<decltype(kind)::value, kFast, A>(gr.get2(k));
             });
         } else if (p.gate_access == FO_AT_COL) {
             with_activation(p.gate_act, [&](auto kind) {
-                for_vector<TB, E>(p.gate, false, c,
-                                  [&](int k, A g) { h[k] *= activate<decltype(kind)::value, kFast, A>(g); });
+                with_vector<TB, E>(h, p.gate, false, c,
+                                   [](Two<A> z, Two<A> g) { return z * activate<decltype(kind)::value, kFast, A>(g); });
             });
         }
-        if (p.col_scale) for_vector<TB, E>(p.col_scale, wide, c, [&](int k, A w) { h[k] *= w; });
+        if (p.col_scale) with_vector<TB, E>(h, p.col_scale, wide, c, times);
+        const Two<A> k2 = both(scale);
 #pragma unroll
-        for (int k = 0; k < E; ++k) h[k] = fused_ma(h[k], scale, A(xr.get(k)));
+        for (int k = 0; k < E; k += 2) h[k / 2] = fused_ma(h[k / 2], k2, xr.get2(k));
+        if (p.post.bias && p.cols != T * C * E) {            // a bias leaves no zeros outside the row
+#pragma unroll
+            for (int k = 0; k < E; k += 2) h[k / 2] = c.inside(k, h[k / 2]);
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < E; ++k) h[k] = A(xr.get(k));
+        for (int k = 0; k < E; k += 2) h[k / 2] = xr.get2(k);
     }
-    if (p.h && ok) store_row<TS, E>(p.h, row * p.ld_h, h, c);
+    if (p.h && ok) store_piece<TS, E>(static_cast<TS *>(p.h) + row * p.ld_h, h, 0, c);
     if (p.pre.kind != FO_NORM_NONE) {
-        pre = row_norm<T, C, E>(h, p.pre.kind, p.pre.eps, c, area, buf);
+        pre = row_norm<T, C>(h, p.pre.kind, A(p.pre.eps), inv, c, area, buf);
         if (p.y && ok) {
+            const Two<A> r = both(pre.r);
 #pragma unroll
-            for (int k = 0; k < E; ++k) h[k] *= pre.r;
-            if (p.pre.weight) for_vector<TB, E>(p.pre.weight, wide, c, [&](int k, A w) { h[k] *= w; });
-            if (p.pre.bias) for_vector<TB, E>(p.pre.bias, wide, c, [&](int k, A b) { h[k] += b; });
-            store_row<TB, E>(p.y, row * p.ld_y, h, c);
+            for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
+            if (p.pre.weight) with_vector<TB, E>(h, p.pre.weight, wide, c, times);
+            if (p.pre.bias) with_vector<TB, E>(h, p.pre.bias, wide, c, plus);
+            store_piece<TB, E>(static_cast<TB *>(p.y) + row * p.ld_y, h, 0, c);
         }
     }
     if (p.stats && ok && c.t == 0) {
@@ -324,30 +357,32 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
 // hold them (many sums of long rows, float64) they lie in the CTA's own part of the workspace instead.
 // At the end every CTA writes its line of partial sums, and column_sum_kernel adds the lines in order.
 
-// Calls body(k, sum) for the thread's elements of one column sum and stores `sum` back.
-template <int CTA, int E, class A, class Body>
-__device__ __forceinline__ void add_columns(A *sums, int place, Body body)
+// The thread's elements k0 .. k0 + N - 1 of the column sum at `place`.
+template <int CTA, int E, int N, class A, class Body>
+__device__ __forceinline__ void column_sums(A *sums, int place, int k0, Body body)
 {
     constexpr int kPiece = 16 / (int)sizeof(A);
     struct alignas(16) Piece {
-        A v[kPiece];
+        Two<A> v[kPiece / 2];
     };
-    Piece *q = reinterpret_cast<Piece *>(sums) + place * (E / kPiece) * CTA + threadIdx.x;
+    Piece *q = reinterpret_cast<Piece *>(sums) + (place * (E / kPiece) + k0 / kPiece) * CTA + threadIdx.x;
 #pragma unroll
-    for (int k = 0; k < E; k += kPiece) {
+    for (int k = 0; k < N; k += kPiece) {
         Piece s = q[k / kPiece * CTA];
 #pragma unroll
-        for (int e = 0; e < kPiece; ++e) body(k + e, s.v[e]);
+        for (int i = 0; i < kPiece / 2; ++i) s.v[i] = body(k / 2 + i, s.v[i]);
         q[k / kPiece * CTA] = s;
     }
 }
 
+// 128 registers a thread, so that 512 threads share an SM: with 140, which the compiler would take, it is half of that.
 template <class TS, class TB, int T, int C, int E, bool VEC, bool BLK>
-__global__ void __launch_bounds__(T > 32 ? T : kGroupCta)
+__global__ void __launch_bounds__(T > 32 ? T : kGroupCta, sizeof(Acc<TB>) == 8 ? 1 : 512 / (T > 32 ? T : kGroupCta))
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
+    constexpr int P = kPieceOf<TB, VEC>;
     constexpr int kCta = T > 32 ? T : kGroupCta;
     constexpr int kGroups = kCta / T;
     constexpr bool kFast = sizeof(TB) == 2;
@@ -355,22 +390,25 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     extern __shared__ __align__(16) unsigned char dynamic[];
     int buf = 0;
     const Columns<T * C, V, VEC> c = {(int)(threadIdx.x % T + (C > 1 ? cluster_rank() * T : 0)), p.cols};
-    const A inv = A(1) / A(p.cols);
+    const bool ragged = p.cols != T * C * E;
+    const A inv = A(p.inv_cols);
     const A *stats = static_cast<const A *>(p.stats);
     const bool wide = p.wide_vec != 0;
     const int n_slots = __popc(p.slots);
     A *const sums = p.sums ? static_cast<A *>(p.sums) + (size_t)blockIdx.x * n_slots * kCta * E
                            : reinterpret_cast<A *>(dynamic);
-    auto wanted = [&](int slot) { return ((p.slots >> slot) & 1u) != 0; };
-    auto place = [&](int slot) { return __popc(p.slots & ((1u << slot) - 1u)); };
-    for (int s = 0; s < n_slots; ++s)
-        add_columns<kCta, E, A>(sums, s, [&](int, A &sum) { sum = A(0); });
+    // adds term(i), for the pairs i of a piece from element k0, to a column sum that is wanted
+    auto add = [&](int slot, int k0, auto term) {
+        if (!((p.slots >> slot) & 1u)) return;
+        column_sums<kCta, E, P, A>(sums, __popc(p.slots & ((1u << slot) - 1u)), k0, term);
+    };
+    for (int s = 0; s < n_slots; ++s) column_sums<kCta, E, E, A>(sums, s, 0, [&](int, Two<A>) { return both(A(0)); });
 
     // all threads of a CTA, and all CTAs of a cluster, take the same number of turns: the sums meet at barriers
     for (long long row0 = (long long)(blockIdx.x / C) * kGroups; row0 < p.rows;
          row0 += (long long)(gridDim.x / C) * kGroups) {
         const long long row = row0 + threadIdx.x / T;
-        const bool ok = row < p.rows;
+        const bool ok = row < p.rows;                        // past the end all values are zero
         Packed<TS, E> dhr, hr;
         Packed<TB, E> dyr, fr, gr;
         if (p.dy) {
@@ -382,123 +420,150 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         if (BLK) load_row<TB, E>(fr, p.f, row * p.ld_f, c, ok);
         if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
 
-        A t[E];
+        Two<A> t[E / 2];
         if (p.dy) {
-            const A mean = ok ? stats[2 * p.rows + row] : A(0), r = ok ? stats[3 * p.rows + row] : A(0);
-            const bool layer = p.pre.kind == FO_NORM_LAYER;
-            A n[E];
+            const A r1 = ok ? stats[3 * p.rows + row] : A(0);
+            const Two<A> minus = both(ok ? -stats[2 * p.rows + row] : A(0)), r = both(r1);
+            Two<A> along = both(A(0)), level = both(A(0));
 #pragma unroll
-            for (int k = 0; k < E; ++k) {
-                t[k] = dyr.get(k);
-                n[k] = (A(hr.get(k)) - mean) * r;
+            for (int k0 = 0; k0 < E; k0 += P) {
+                Two<A> n[P / 2], *a = t + k0 / 2;
+#pragma unroll
+                for (int i = 0; i < P / 2; ++i) {
+                    a[i] = dyr.get2(k0 + 2 * i);
+                    n[i] = (hr.get2(k0 + 2 * i) + minus) * r;
+                }
+                add(kPreW, k0, [&](int i, Two<A> s) { return fused_ma(a[i], n[i], s); });
+                add(kPreB, k0, [&](int i, Two<A> s) { return s + a[i]; });
+                if (p.pre.weight) {
+                    Two<A> w[P / 2];
+                    load_vector<TB, P>(w, p.pre.weight, wide, k0, c);
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) a[i] = a[i] * w[i];
+                }
+#pragma unroll
+                for (int i = 0; i < P / 2; ++i) along = fused_ma(a[i], n[i], along);
+                if (p.pre.kind == FO_NORM_LAYER) {
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) level = level + a[i];
+                }
             }
-            if (wanted(kPreW) && ok)
-                add_columns<kCta, E, A>(sums, place(kPreW), [&](int k, A &sum) { sum = fused_ma(t[k], n[k], sum); });
-            if (wanted(kPreB) && ok) add_columns<kCta, E, A>(sums, place(kPreB), [&](int k, A &sum) { sum += t[k]; });
-            if (p.pre.weight) for_vector<TB, E>(p.pre.weight, wide, c, [&](int k, A w) { t[k] *= w; });
-            A s[2] = {A(0), A(0)};
-            for_columns<E>(c, [&](int k) { s[0] = fused_ma(t[k], n[k], s[0]); });
-            if (layer) {
-                for_columns<E>(c, [&](int k) { s[1] += t[k]; });
+            A s[2] = {joined(along), A(0)};
+            if (p.pre.kind == FO_NORM_LAYER) {
+                s[1] = joined(level);
                 group_sum<T, C, 2, A>(s, area, buf);
             } else {
-                A s0[1] = {s[0]};
-                group_sum<T, C, 1, A>(s0, area, buf);
-                s[0] = s0[0];
+                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), area, buf);
             }
-            // dh + r (a - n along - common)
-            const A along = -s[0] * inv * r, common = -s[1] * inv * r;
+            // dh + r (a - n mean(a n) - mean(a))
+            along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
-            for (int k = 0; k < E; ++k) t[k] = fused_ma(t[k], r, fused_ma(n[k], along, A(dhr.get(k)) + common));
+            for (int k = 0; k < E; k += 2)
+                t[k / 2] = fused_ma(t[k / 2], r, fused_ma(hr.get2(k) + minus, along, dhr.get2(k) + level));
+            if (ragged) {
+#pragma unroll
+                for (int k = 0; k < E; k += 2) t[k / 2] = c.inside(k, t[k / 2]);
+            }
         } else {
 #pragma unroll
-            for (int k = 0; k < E; ++k) t[k] = A(dhr.get(k));
+            for (int k = 0; k < E; k += 2) t[k / 2] = dhr.get2(k);
         }
-        if (p.dx && ok) store_row<TS, E>(p.dx, row * p.ld_dx, t, c);
+        if (p.dx && ok) store_piece<TS, E>(static_cast<TS *>(p.dx) + row * p.ld_dx, t, 0, c);
         if constexpr (BLK) {
             const bool normed = p.post.kind != FO_NORM_NONE, row_gate = p.gate_access == FO_AT_ROW;
-            const A mean = ok && normed ? stats[row] : A(0), r = ok && normed ? stats[p.rows + row] : A(1);
-            const A scale = A(p.scale);
-            A z[E];
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-                t[k] *= scale;
-                z[k] = (fr.get(k) - mean) * r;
+            const A r1 = ok && normed ? stats[p.rows + row] : A(1);
+            const Two<A> minus = both(ok && normed ? -stats[row] : A(0)), r = both(r1), scale = both(A(p.scale));
+            Two<A> row_act = both(A(1)), row_slope = both(A(0));
+            if (row_gate) {
+                const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
+                with_activation(p.gate_act, [&](auto kind) {
+                    row_act = activate_slope<decltype(kind)::value, kFast, A>(both(g), row_slope);
+                });
             }
-            if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { z[k] *= w; });
-            if (p.post.bias) for_vector<TB, E>(p.post.bias, wide, c, [&](int k, A b) { z[k] += b; });
-            A s[3] = {A(0), A(0), A(0)};
-            // with q = t: col_scale's sum takes q act z; then, q' = q col_scale, z becomes dgate = q' z act' and
-            // t becomes d = q' act
-            auto through_gate = [&](auto gate_at) {
-                if (p.col_scale) {
-                    if (wanted(kColScale) && ok)
-                        add_columns<kCta, E, A>(sums, place(kColScale), [&](int k, A &sum) {
-                            A slope;
-                            sum = fused_ma(t[k] * z[k], gate_at(k, slope), sum);
-                        });
-                    for_vector<TB, E>(p.col_scale, wide, c, [&](int k, A w) { t[k] *= w; });
-                }
+            Two<A> along = both(A(0)), level = both(A(0)), gate_sum = both(A(0));
 #pragma unroll
-                for (int k = 0; k < E; ++k) {
-                    A slope;
-                    const A a = gate_at(k, slope);
-                    z[k] *= t[k] * slope;
-                    t[k] *= a;
-                }
-            };
-            if (p.gate_access == FO_AT_CELL || p.gate_access == FO_AT_COL) {
-                A g[E];
-                if (p.gate_access == FO_AT_CELL) {
+            for (int k0 = 0; k0 < E; k0 += P) {
+                Two<A> n[P / 2], z[P / 2], w[P / 2], a[P / 2], slope[P / 2], *d = t + k0 / 2;
+                if (p.post.weight) load_vector<TB, P>(w, p.post.weight, wide, k0, c);
+                else
 #pragma unroll
-                    for (int k = 0; k < E; ++k) g[k] = gr.get(k);
+                    for (int i = 0; i < P / 2; ++i) w[i] = both(A(1));
+#pragma unroll
+                for (int i = 0; i < P / 2; ++i) {
+                    n[i] = (fr.get2(k0 + 2 * i) + minus) * r;
+                    z[i] = n[i] * w[i];
+                    d[i] = d[i] * scale;
+                }
+                if (p.post.bias) {
+                    Two<A> b[P / 2];
+                    load_vector<TB, P>(b, p.post.bias, wide, k0, c);
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) z[i] = z[i] + b[i];
+                }
+                if (p.gate_access == FO_AT_CELL || p.gate_access == FO_AT_COL) {
+                    Two<A> g[P / 2];
+                    if (p.gate_access == FO_AT_COL) load_vector<TB, P>(g, p.gate, false, k0, c);
+                    else
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) g[i] = gr.get2(k0 + 2 * i);
+                    with_activation(p.gate_act, [&](auto kind) {
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i)
+                            a[i] = activate_slope<decltype(kind)::value, kFast, A>(g[i], slope[i]);
+                    });
                 } else {
 #pragma unroll
-                    for (int k = 0; k < E; ++k) g[k] = A(0);
-                    for_vector<TB, E>(p.gate, false, c, [&](int k, A v) { g[k] = v; });
+                    for (int i = 0; i < P / 2; ++i) a[i] = row_act, slope[i] = row_slope;
                 }
-                with_activation(p.gate_act, [&](auto kind) {
-                    through_gate([&](int k, A &slope) { return activate_slope<decltype(kind)::value, kFast, A>(g[k], slope); });
-                });
-                if (p.dgate && ok && p.gate_access == FO_AT_CELL) store_row<TB, E>(p.dgate, row * p.ld_dgate, z, c);
-                if (wanted(kGateCol) && ok)
-                    add_columns<kCta, E, A>(sums, place(kGateCol), [&](int k, A &sum) { sum += z[k]; });
-            } else {
-                A a = A(1), da = A(0);
-                if (row_gate) {
-                    const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
-                    with_activation(p.gate_act, [&](auto kind) { a = activate_slope<decltype(kind)::value, kFast, A>(g, da); });
-                }
-                through_gate([&](int, A &slope) {
-                    slope = da;
-                    return a;
-                });
-                if (row_gate) for_columns<E>(c, [&](int k) { s[2] += z[k]; });
-            }
-            if (normed) {
+                if (p.col_scale) {
+                    add(kColScale, k0, [&](int i, Two<A> s) { return fused_ma(d[i] * z[i], a[i], s); });
+                    Two<A> cs[P / 2];
+                    load_vector<TB, P>(cs, p.col_scale, wide, k0, c);
 #pragma unroll
-                for (int k = 0; k < E; ++k) z[k] = (fr.get(k) - mean) * r;
-                if (wanted(kPostW) && ok)
-                    add_columns<kCta, E, A>(sums, place(kPostW), [&](int k, A &sum) { sum = fused_ma(t[k], z[k], sum); });
-                if (wanted(kPostB) && ok) add_columns<kCta, E, A>(sums, place(kPostB), [&](int k, A &sum) { sum += t[k]; });
-                if (p.post.weight) for_vector<TB, E>(p.post.weight, wide, c, [&](int k, A w) { t[k] *= w; });
-                for_columns<E>(c, [&](int k) { s[0] = fused_ma(t[k], z[k], s[0]); });
-                if (p.post.kind == FO_NORM_LAYER) for_columns<E>(c, [&](int k) { s[1] += t[k]; });
+                    for (int i = 0; i < P / 2; ++i) d[i] = d[i] * cs[i];
+                }
+                // z becomes the gate's gradient q' z act', d the normed output's q' act
+#pragma unroll
+                for (int i = 0; i < P / 2; ++i) {
+                    z[i] = d[i] * z[i] * slope[i];
+                    d[i] = d[i] * a[i];
+                }
+                if (p.dgate && ok && p.gate_access == FO_AT_CELL)
+                    store_piece<TB, P>(static_cast<TB *>(p.dgate) + row * p.ld_dgate, z, k0, c);
+                add(kGateCol, k0, [&](int i, Two<A> s) { return s + z[i]; });
+                if (row_gate) {
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) gate_sum = gate_sum + z[i];
+                }
+                if (normed) {
+                    add(kPostW, k0, [&](int i, Two<A> s) { return fused_ma(d[i], n[i], s); });
+                    add(kPostB, k0, [&](int i, Two<A> s) { return s + d[i]; });
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) {
+                        d[i] = d[i] * w[i];
+                        along = fused_ma(d[i], n[i], along);
+                    }
+                    if (p.post.kind == FO_NORM_LAYER) {
+#pragma unroll
+                        for (int i = 0; i < P / 2; ++i) level = level + d[i];
+                    }
+                }
             }
+            A s[3] = {joined(along), A(0), A(0)};
             if (row_gate || p.post.kind == FO_NORM_LAYER) {
+                s[1] = joined(level), s[2] = joined(gate_sum);
                 group_sum<T, C, 3, A>(s, area, buf);
                 if (p.dgate && ok && row_gate && c.t == 0) static_cast<A *>(p.dgate)[row] = s[2];
             } else if (normed) {
-                A s0[1] = {s[0]};
-                group_sum<T, C, 1, A>(s0, area, buf);
-                s[0] = s0[0];
+                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), area, buf);
             }
             if (normed) {
-                const A along = -s[0] * inv * r, common = -s[1] * inv * r;
+                along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
-                for (int k = 0; k < E; ++k) t[k] = fused_ma(t[k], r, fused_ma(z[k], along, common));
+                for (int k = 0; k < E; k += 2)
+                    t[k / 2] = fused_ma(t[k / 2], r, fused_ma(fr.get2(k) + minus, along, level));
             }
-            if (p.df && ok) store_row<TB, E>(p.df, row * p.ld_df, t, c);
+            if (p.df && ok) store_piece<TB, E>(static_cast<TB *>(p.df) + row * p.ld_df, t, 0, c);
         }
     }
 
@@ -507,8 +572,10 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     A *line = static_cast<A *>(p.partial) + (size_t)(blockIdx.x / C) * p.cols;
     if constexpr (T > 32) {
         for (int s = 0; s < n_slots; ++s, line += plane)
-            add_columns<kCta, E, A>(sums, s, [&](int k, A &sum) {
-                if (c.has(k)) line[c.of(k)] = sum;
+            column_sums<kCta, E, E, A>(sums, s, 0, [&](int i, Two<A> sum) {
+                if (c.has(2 * i)) line[c.of(2 * i)] = first(sum);
+                if (c.has(2 * i + 1)) line[c.of(2 * i + 1)] = second(sum);
+                return sum;
             });
     } else {
         constexpr int kPiece = 16 / (int)sizeof(A);

@@ -30,6 +30,65 @@ template <> __device__ __forceinline__ float narrow<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
+__device__ __forceinline__ float fused_ma(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ double fused_ma(double a, double b, double c) { return fma(a, b, c); }
+
+// Two neighbouring elements' values.  In 32 bits they are one 64-bit register pair, which the
+// packed instructions of sm_100 multiply and add with one issue slot.
+template <class A>
+struct Two {
+    A a, b;
+};
+template <>
+struct Two<float> {
+    unsigned long long v;
+};
+__device__ __forceinline__ Two<float> two(float a, float b)
+{
+    Two<float> t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t.v) : "f"(a), "f"(b));
+    return t;
+}
+__device__ __forceinline__ Two<double> two(double a, double b) { return {a, b}; }
+__device__ __forceinline__ float first(Two<float> t) { return __uint_as_float((unsigned)t.v); }
+__device__ __forceinline__ float second(Two<float> t) { return __uint_as_float((unsigned)(t.v >> 32)); }
+__device__ __forceinline__ double first(Two<double> t) { return t.a; }
+__device__ __forceinline__ double second(Two<double> t) { return t.b; }
+__device__ __forceinline__ Two<float> operator*(Two<float> x, Two<float> y)
+{
+    Two<float> t;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t.v) : "l"(x.v), "l"(y.v));
+    return t;
+}
+__device__ __forceinline__ Two<float> operator+(Two<float> x, Two<float> y)
+{
+    Two<float> t;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(t.v) : "l"(x.v), "l"(y.v));
+    return t;
+}
+__device__ __forceinline__ Two<float> fused_ma(Two<float> x, Two<float> y, Two<float> z)
+{
+    Two<float> t;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(t.v) : "l"(x.v), "l"(y.v), "l"(z.v));
+    return t;
+}
+__device__ __forceinline__ Two<double> operator*(Two<double> x, Two<double> y) { return {x.a * y.a, x.b * y.b}; }
+__device__ __forceinline__ Two<double> operator+(Two<double> x, Two<double> y) { return {x.a + y.a, x.b + y.b}; }
+__device__ __forceinline__ Two<double> fused_ma(Two<double> x, Two<double> y, Two<double> z)
+{
+    return {fma(x.a, y.a, z.a), fma(x.b, y.b, z.b)};
+}
+template <class A>
+__device__ __forceinline__ Two<A> both(A v)
+{
+    return two(v, v);
+}
+template <class A>
+__device__ __forceinline__ A joined(Two<A> t)
+{
+    return first(t) + second(t);
+}
+
 // N elements as 32-bit words, the way they lie in memory.  N * sizeof(T) is a multiple of 16.
 template <class T, int N>
 struct Packed {
@@ -44,9 +103,9 @@ struct Packed {
             return __uint_as_float((k & 1) ? (w[k / 2] & 0xffff0000u) : (w[k / 2] << 16));
         else return __half2float(__ushort_as_half((unsigned short)((k & 1) ? (w[k / 2] >> 16) : (w[k / 2] & 0xffffu))));
     }
-    // elements k and k + 1 (k even) from sums, rounded once
-    __device__ __forceinline__ void round2(int k, Acc<T> a, Acc<T> b)
+    __device__ __forceinline__ void put2(int k, Two<Acc<T>> v)      // k even; rounded once
     {
+        const Acc<T> a = first(v), b = second(v);
         if constexpr (sizeof(T) >= 4) {
             put(k, (T)a);
             put(k + 1, (T)b);
@@ -58,6 +117,7 @@ struct Packed {
             memcpy(&w[k / 2], &v, 4);
         }
     }
+    __device__ __forceinline__ Two<Acc<T>> get2(int k) const { return two(get(k), get(k + 1)); }      // k even
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
@@ -92,57 +152,70 @@ __device__ __forceinline__ void store16(void *p, const uint32_t *w)
                  : "memory");
 }
 
-__device__ __forceinline__ float group_rsqrt(float v) { return 1.0f / sqrtf(v); }
-__device__ __forceinline__ double group_rsqrt(double v) { return 1.0 / sqrt(v); }
-__device__ __forceinline__ float fused_ma(float a, float b, float c) { return fmaf(a, b, c); }
-__device__ __forceinline__ double fused_ma(double a, double b, double c) { return fma(a, b, c); }
+__device__ __forceinline__ float group_rsqrt(float v) { return rsqrtf(v); }      // within 2 units
+__device__ __forceinline__ double group_rsqrt(double v) { return rsqrt(v); }
 
-// act(g) and its derivative.  FAST (results rounded to 16 bits): the hardware's exponential, with a
-// relative error of a few 2^-22 over the range where a sigmoid is not 0 or 1; the tangent is the
-// library's in every case, because near zero its relative error is what a gate that starts at zero sees.
-template <class A> __device__ __forceinline__ A exp_neg(A g);
-template <> __device__ __forceinline__ float exp_neg<float>(float g) { return expf(-g); }
-template <> __device__ __forceinline__ double exp_neg<double>(double g) { return exp(-g); }
+// act(g) and its derivative.  FAST (results rounded to 16 bits): the hardware's exponential and
+// reciprocal, a relative error of a few 2^-22 over the range where a sigmoid is not 0 or 1; the tangent is
+// the library's in every case, because near zero its relative error is what a gate that starts at
+// zero sees.
 __device__ __forceinline__ float tanh_of(float g) { return tanhf(g); }
 __device__ __forceinline__ double tanh_of(double g) { return tanh(g); }
 
-template <bool FAST, class A>
-__device__ __forceinline__ A sigmoid(A g)
+template <bool FAST>
+__device__ __forceinline__ Two<float> sigmoid(Two<float> g)
 {
-    if constexpr (FAST) return __fdividef(1.0f, 1.0f + __expf(-g));   // e^-g = inf gives 0
-    else return A(1) / (A(1) + exp_neg<A>(g));
+    if constexpr (FAST) {
+        const Two<float> x = g * both(-1.4426950408889634f);
+        float ea, eb, a, b;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ea) : "f"(first(x)));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(eb) : "f"(second(x)));
+        const Two<float> d = two(ea, eb) + both(1.0f);            // infinity gives 0
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(d)));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(d)));
+        return two(a, b);
+    } else {
+        return two(1.0f / (1.0f + expf(-first(g))), 1.0f / (1.0f + expf(-second(g))));
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ Two<double> sigmoid(Two<double> g)
+{
+    return two(1.0 / (1.0 + exp(-g.a)), 1.0 / (1.0 + exp(-g.b)));
 }
 
 template <int KIND, bool FAST, class A>
-__device__ __forceinline__ A activate(A g)
+__device__ __forceinline__ Two<A> activate(Two<A> g)
 {
     if constexpr (KIND == FO_ACT_LINEAR) return g;
-    else if constexpr (KIND == FO_ACT_TANH) return tanh_of(g);
+    else if constexpr (KIND == FO_ACT_TANH) return two(tanh_of(first(g)), tanh_of(second(g)));
     else {
-        const A s = sigmoid<FAST, A>(g);
+        const Two<A> s = sigmoid<FAST>(g);
         return KIND == FO_ACT_SILU ? g * s : s;
     }
 }
 
 template <int KIND, bool FAST, class A>
-__device__ __forceinline__ A activate_slope(A g, A &slope)
+__device__ __forceinline__ Two<A> activate_slope(Two<A> g, Two<A> &slope)
 {
+    const Two<A> one = both(A(1)), minus = both(A(-1));
     if constexpr (KIND == FO_ACT_LINEAR) {
-        slope = A(1);
+        slope = one;
         return g;
     } else if constexpr (KIND == FO_ACT_TANH) {
-        const A t = tanh_of(g);
-        slope = fused_ma(-t, t, A(1));
+        const Two<A> t = two(tanh_of(first(g)), tanh_of(second(g)));
+        slope = fused_ma(t * minus, t, one);
         return t;
     } else {
-        const A s = sigmoid<FAST, A>(g);
+        const Two<A> s = sigmoid<FAST>(g), rest = fused_ma(s, minus, one);
         if constexpr (KIND == FO_ACT_SIGMOID) {
-            slope = fused_ma(-s, s, s);
+            slope = s * rest;
             return s;
+        } else {
+            const Two<A> a = g * s;
+            slope = fused_ma(a, rest, s);
+            return a;
         }
-        const A a = g * s;
-        slope = fused_ma(a, A(1) - s, s);
-        return a;
     }
 }
 
