@@ -74,11 +74,11 @@ int check_gate(const void *gate, int access, int act, long long ld, long long ro
     return FO_OK;
 }
 
-// Upper bound on the CTAs (clusters) that leave a line of partial column sums: a few per SM for short rows,
-// one per SM for long ones, whose lines are long.
+// Upper bound on the CTAs (clusters) that leave a line of partial column sums: what is resident of CTAs of 256
+// threads for short rows, of 512 for longer ones.
 int grad_lines(long long rows, long long cols)
 {
-    const long long cap = cols <= 1024 ? 148 * 4 : cols <= 4096 ? 148 * 2 : 148;
+    const long long cap = cols <= 4096 ? 148 * 2 : 148;
     const long long n = rows < cap ? rows : cap;
     return (int)(n > 1 ? n : 1);
 }
@@ -92,7 +92,7 @@ size_t grad_line_bytes(long long rows, long long cols, int block_type)
 size_t grad_sum_bytes(long long rows, long long cols, int block_type)
 {
     const size_t bytes = block_type == FO_F64 ? 8 : 4, slot = (size_t)512 * 16 * bytes;
-    if (kGradSlots * slot <= 220 * 1024 || cols <= 4096) return 0;
+    if (kGradSlots * slot <= 200 * 1024) return 0;
     const size_t held = cols <= 8192 ? 8192 : cols <= 16384 ? 16384 : 32768;
     return (size_t)kGradSlots * grad_lines(rows, cols) * held * bytes;
 }
@@ -139,7 +139,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
     if (p.gate_access == FO_AT_CELL) all.matrix(a->gate, a->ld_gate, a->block_type);
     if (p.gate_access == FO_AT_COL) all.vector(a->gate);
     all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
-    p.vec = all.ok;
+    p.aligned = all.ok;
 
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(s, b, TS, TB) \
@@ -213,7 +213,7 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     if (p.gate_access == FO_AT_CELL) all.matrix(a->dgate, a->ld_dgate, a->block_type);
     if (p.gate_access == FO_AT_COL) all.vector(a->gate);
     all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
-    p.vec = all.ok;
+    p.aligned = all.ok;
 
     int n_sums = 0;
     ColumnSumParams cs = {};
@@ -232,8 +232,8 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     if (e == cudaSuccess && n_sums > 0) {
         cs.partial = p.partial, cs.lines = space.lines, cs.cols = p.cols;
         const dim3 grid((unsigned)((a->cols + 31) / 32), (unsigned)n_sums);
-        if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, 256, 0, st>>>(cs);
-        else column_sum_kernel<float><<<grid, 256, 0, st>>>(cs);
+        if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, kSumWarps * 32, 0, st>>>(cs);
+        else column_sum_kernel<float><<<grid, kSumWarps * 32, 0, st>>>(cs);
         e = cudaGetLastError();
     }
     return e == cudaSuccess ? FO_OK : cuda_fail(e);

@@ -1,7 +1,7 @@
 // Block norm and its gradient (see fusedops_train.h for the mathematics): one pass over the rows,
 // each row held in registers between its sums.
 //
-// A row belongs to a group of T threads that hold E of its elements each.  Up to 32 threads the group
+// A row belongs to a group of threads that hold E of its elements each.  Up to 32 threads the group
 // is a part of a warp and its sums are shuffles; above, the group is the CTA, and a sum is a shuffle, one
 // exchange through shared memory and a shuffle; the longest rows are split over a cluster of C CTAs, which
 // exchange through each other's shared memory.  Rows are read and written once; what bounds the kernels
@@ -15,6 +15,7 @@
 namespace fo {
 
 constexpr int kGroupCta = 256;               // CTA size where a group is a warp or less
+constexpr int kMostCta = 512;                // and at most where it is the CTA
 constexpr int kGradSlots = 6;                // column sums of the gradient: see Slot
 enum Slot { kPreW = 0, kPreB = 1, kPostW = 2, kPostB = 3, kColScale = 4, kGateCol = 5 };
 
@@ -27,7 +28,7 @@ struct NormSpec {
 struct BlockNormParams {
     long long rows;
     int cols;
-    int vec;                                 // rows move in 16-byte pieces
+    int aligned;                             // rows and vectors are whole 16-byte pieces
     double inv_cols;                         // 1 / cols
     int wide_vec;                            // vectors are float although the block has 16 bits
     int gate_access, gate_act;               // gate_access -1: none
@@ -42,7 +43,7 @@ struct BlockNormParams {
 struct BlockNormGradParams {
     long long rows;
     int cols;
-    int vec, wide_vec;
+    int aligned, wide_vec;
     double inv_cols;
     int gate_access, gate_act;
     const void *dh, *dy, *h, *f, *gate, *col_scale, *stats;
@@ -51,79 +52,170 @@ struct BlockNormGradParams {
     NormSpec post, pre;
     void *dx, *df, *dgate;
     long long ld_dx, ld_df, ld_dgate;
+    int group;                               // threads of a row's group where that is more than a warp
     unsigned slots;                          // bit k: the sum of slot k is wanted
     void *sums;                              // where the CTAs hold their sums, NULL: in shared memory
     void *partial;                           // [slot among the wanted][CTA or cluster][cols]
 };
 
-// Which columns a thread holds.  VEC, 16-byte pieces of V elements: piece v of the thread covers columns
-// (v * T + t) * V .. + V - 1 and lies inside the row or outside it.  Else element k is column k * T + t,
-// so that the threads of a warp touch neighbouring elements.  Values outside the row are held as zeros.
-template <int T, int V, bool VEC>              // T: threads of the row, over all its CTAs
+// Which columns a thread holds: pieces of V elements, 16 bytes of the block's type.  Piece v of thread t covers
+// columns (v * threads + t) * V .. + V - 1.  ALIGNED: every row of every matrix begins on a 16-byte boundary
+// and is whole pieces long; else rows may begin and end anywhere, and 16 bytes that straddle a boundary are
+// put together from the two aligned 16 bytes they lie in.  Values outside the row are held as zeros.
+template <int T, int V>                        // T: threads of the row, 0: the CTAs' threads
 struct Columns {
-    int t, cols;
-    __device__ __forceinline__ int of(int k) const { return VEC ? ((k / V) * T + t) * V + k % V : k * T + t; }
-    __device__ __forceinline__ bool has(int k) const { return of(VEC ? k / V * V : k) < cols; }
+    int t, cols, count;                        // count: threads of the row
+    __device__ __forceinline__ int threads() const { return T > 0 ? T : count; }
+    __device__ __forceinline__ int of(int k) const { return ((k / V) * threads() + t) * V + k % V; }
     // elements k and k + 1 (k even) with zeros outside the row
-    template <class A>
+    template <bool ALIGNED, class A>
     __device__ __forceinline__ Two<A> inside(int k, Two<A> v) const
     {
-        if constexpr (VEC) return has(k) ? v : both(A(0));
-        else return two(has(k) ? first(v) : A(0), has(k + 1) ? second(v) : A(0));
+        if constexpr (ALIGNED) return of(k / V * V) < cols ? v : both(A(0));
+        else return two(of(k) < cols ? first(v) : A(0), of(k + 1) < cols ? second(v) : A(0));
     }
 };
 
-template <class TE, int E, int T, int V, bool VEC>
-__device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, long long at, const Columns<T, V, VEC> &c,
-                                         bool row_ok)
+// 16 bytes from byte `q` (0 .. 15, a multiple of the element's size) of 32.
+__device__ __forceinline__ void straddle(uint32_t *r, const uint32_t (&w)[8], unsigned q)
 {
-    const TE *p = static_cast<const TE *>(base) + at;
-    if constexpr (VEC) {
-        constexpr int kStep = 16 / (int)sizeof(TE);
+    uint32_t a[7], b[5];
 #pragma unroll
-        for (int k = 0; k < E; k += kStep) {
-            uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
-            w[0] = w[1] = w[2] = w[3] = 0u;
-            if (row_ok && c.has(k)) load16(w, p + c.of(k));
-        }
+    for (int i = 0; i < 7; ++i) a[i] = (q & 4u) ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) b[i] = (q & 8u) ? a[i + 2] : a[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = __funnelshift_r(b[i], b[i + 1], (q & 3u) * 8u);
+}
+
+// 16 bytes from any address, through L1 (the next thread reads the second half too).  Nothing outside
+// [begin, end), the matrix's own bytes, is read; what lies there is given as zeros.
+template <class TE>
+__device__ __forceinline__ void load16_any(uint32_t *r, const TE *p, const TE *begin, const TE *end)
+{
+    const unsigned q = (unsigned)((uintptr_t)p & 15u);
+    const char *base = reinterpret_cast<const char *>(p) - q;
+    const uint4 *a = reinterpret_cast<const uint4 *>(base);
+    if (base >= reinterpret_cast<const char *>(begin) && base + 32 <= reinterpret_cast<const char *>(end)) {
+        uint32_t w[8];
+        uint4 u = a[0];
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        if (q) u = a[1];
+        w[4] = u.x, w[5] = u.y, w[6] = u.z, w[7] = u.w;
+        straddle(r, w, q);
     } else {
-        r.clear();
+        constexpr int N = 16 / (int)sizeof(TE);
+        Packed<TE, N> v;
+        v.clear();
 #pragma unroll
-        for (int k = 0; k < E; ++k)
-            if (row_ok && c.has(k)) r.put(k, p[c.of(k)]);
+        for (int k = 0; k < N; ++k)
+            if (p + k >= begin && p + k < end) v.put(k, p[k]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = v.w[i];
     }
 }
 
-// Stores elements k0 .. k0 + N - 1 of the thread.
-template <class TE, int N, int T, int V, bool VEC>
-__device__ __forceinline__ void store_piece(TE *p, const Two<Acc<TE>> *v, int k0, const Columns<T, V, VEC> &c)
+// A matrix of the call: rows x cols at base, rows ld apart.
+template <bool ALIGNED, class TE, int E, int T, int V>
+__device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, long long rows, long long row, long long ld,
+                                         const Columns<T, V> &c, bool row_ok)
 {
-    if constexpr (VEC) {
-        constexpr int kStep = 16 / (int)sizeof(TE);
+    const TE *begin = static_cast<const TE *>(base), *p = begin + row * ld;
+    constexpr int kStep = 16 / (int)sizeof(TE);
+#pragma unroll
+    for (int k = 0; k < E; k += kStep) {
+        uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
+        const int j = c.of(k);
+        w[0] = w[1] = w[2] = w[3] = 0u;
+        if (!row_ok || j >= c.cols) continue;
+        if constexpr (ALIGNED) {
+            load16(w, p + j);
+        } else {
+            load16_any(w, p + j, begin, begin + (rows - 1) * ld + c.cols);
+            if (j + kStep > c.cols) {                        // the row ends inside: zeros from there
+                Packed<TE, kStep> whole, part;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) whole.w[i] = w[i];
+                part.clear();
+#pragma unroll
+                for (int e = 0; e < kStep; ++e)
+                    if (j + e < c.cols) part.put(e, whole.raw(e));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = part.w[i];
+            }
+        }
+    }
+}
+
+// Stores elements k0 .. k0 + N - 1 of the thread, whole pieces, into its row (`ok`: there is one).
+// Unaligned: the pieces of the row's threads in a warp are neighbours; they are exchanged through the warp's
+// `stage` so that full aligned 16 bytes can be written, and the ends singly.  All threads of the warp call it.
+template <bool ALIGNED, class TE, int N, int T, int V>
+__device__ __forceinline__ void store_piece(void *base, long long row, long long ld, const Two<Acc<TE>> *v, int k0,
+                                            const Columns<T, V> &c, bool ok, unsigned char *stage)
+{
+    TE *p = static_cast<TE *>(base) + row * ld;
+    constexpr int kStep = 16 / (int)sizeof(TE);
+    if constexpr (ALIGNED) {
 #pragma unroll
         for (int k = 0; k < N; k += kStep) {
-            if (!c.has(k0 + k)) continue;
+            if (!ok || c.of(k0 + k) >= c.cols) continue;
             Packed<TE, kStep> r;
 #pragma unroll
             for (int e = 0; e < kStep; e += 2) r.put2(e, v[(k + e) / 2]);
             store16(p + c.of(k0 + k), r.w);
         }
     } else {
+        constexpr int kLanes = T > 0 ? T : 32;               // threads of the row in this warp
+        constexpr int kChunks = V / kStep;                   // 16-byte chunks of a piece
+        const int lane = (threadIdx.x & 31) % kLanes;
+        unsigned char *mine = stage + (threadIdx.x & 31) / kLanes * (kLanes * V * (int)sizeof(TE));
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (c.has(k0 + k)) p[c.of(k0 + k)] = narrow<TE>(k & 1 ? second(v[k / 2]) : first(v[k / 2]));
+        for (int k = 0; k < N; k += V) {
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < V; h += kStep) {
+                Packed<TE, kStep> r;
+#pragma unroll
+                for (int e = 0; e < kStep; e += 2) r.put2(e, v[(k + h + e) / 2]);
+                *reinterpret_cast<uint4 *>(mine + (lane * V + h) * (int)sizeof(TE)) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+            }
+            __syncwarp();
+            const int first_col = c.of(k0 + k) - lane * V, left = c.cols - first_col;
+            const int n = !ok ? 0 : left < kLanes * V ? left : kLanes * V;       // elements to write, may be negative
+            TE *q = p + first_col;
+            const int head = (int)(((16u - (unsigned)((uintptr_t)q & 15u)) & 15u) / sizeof(TE));
+            const TE *held = reinterpret_cast<const TE *>(mine);
+            if (lane < head && lane < n) q[lane] = held[lane];
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) {
+                const int at = head + (lane + i * kLanes) * kStep;
+                if (at + kStep <= n) {
+                    const uint4 *a = reinterpret_cast<const uint4 *>(held + at / kStep * kStep);
+                    const uint4 x = a[0], y = head ? a[1] : x;
+                    const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    uint32_t r[4];
+                    straddle(r, w, (unsigned)(head * (int)sizeof(TE)));
+                    store16(q + at, r);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kStep; ++e)
+                        if (at + e < n) q[at + e] = held[at + e];
+                }
+            }
+        }
     }
 }
 
-// N elements from k0 of a vector over the columns (weight, bias, scale, gate per column).  `wide`: the
-// vector is float although the block has 16 bits.  Outside the row it gives some value of the vector,
-// which meets a zero there: no zeros have to be put where a load might not take place.
-template <class TE, int N, int T, int V, bool VEC>
+// N elements, whole pieces, from k0 of a vector over the columns (weight, bias, scale, gate per
+// column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives some value of
+// the vector, which meets a zero there: no zeros have to be put where a load might not take place.
+template <bool ALIGNED, class TE, int N, int T, int V>
 __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void *base, bool wide, int k0,
-                                            const Columns<T, V, VEC> &c)
+                                            const Columns<T, V> &c)
 {
     using A = Acc<TE>;
-    if constexpr (!VEC) {
+    if constexpr (!ALIGNED) {
         auto at = [&](int k) -> A {
             const int j = min(c.of(k), c.cols - 1);
             if (sizeof(TE) == 2 && wide) return (A)__ldg(static_cast<const float *>(base) + j);
@@ -151,19 +243,15 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
     }
 }
 
-// Elements that are worked on at a time where vectors over the columns are read.
-template <class TB, bool VEC>
-constexpr int kPieceOf = VEC ? 16 / (int)sizeof(TB) : 16 / (int)sizeof(Acc<TB>);
-
 // h = op(h, vector) over the thread's elements
-template <class TE, int E, class Cols, class Op>
+template <bool ALIGNED, class TE, int E, class Cols, class Op>
 __device__ __forceinline__ void with_vector(Two<Acc<TE>> (&h)[E / 2], const void *base, bool wide, const Cols &c, Op op)
 {
     constexpr int P = 16 / (int)sizeof(TE);
 #pragma unroll
     for (int k0 = 0; k0 < E; k0 += P) {
         Two<Acc<TE>> w[P / 2];
-        load_vector<TE, P>(w, base, wide, k0, c);
+        load_vector<ALIGNED, TE, P>(w, base, wide, k0, c);
 #pragma unroll
         for (int i = 0; i < P / 2; ++i) h[k0 / 2 + i] = op(h[k0 / 2 + i], w[i]);
     }
@@ -194,36 +282,42 @@ __device__ __forceinline__ void cluster_barrier()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// The group a thread belongs to where groups are larger than a warp: `threads` threads (a multiple of 32) of its
+// CTA, number `id` of that size, with C - 1 more CTAs.
+struct Group {
+    int id, threads;
+};
+
 template <int T, int C, int N, class A>
-__device__ __forceinline__ void group_sum(A (&v)[N], Area<A> &area, int &buf)
+__device__ __forceinline__ void group_sum(A (&v)[N], const Group &g, Area<A> &area, int &buf)
 {
-    constexpr int kLanes = T < 32 ? T : 32;
+    constexpr int kLanes = T > 0 ? T : 32;
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
-    if constexpr (T > 32) {
-        constexpr int kWarps = T / 32, kValues = kWarps * C;
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (T == 0) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = g.threads >> 5, first = g.id * warps;
         if constexpr (C == 1) {
             if (lane == 0) {
 #pragma unroll
                 for (int n = 0; n < N; ++n) area[buf][n][warp] = v[n];
             }
-            __syncthreads();
+            asm volatile("bar.sync %0, %1;" ::"r"(g.id + 1), "r"(g.threads) : "memory");
         } else {
             if (lane < C) {
-                const int at = (int)cluster_rank() * kWarps + warp;
+                const int at = (int)cluster_rank() * warps + warp;
 #pragma unroll
                 for (int n = 0; n < N; ++n) store_remote(&area[buf][n][at], (unsigned)lane, v[n]);
             }
             cluster_barrier();
         }
-        constexpr int kSpan = kValues < 32 ? kValues : 32;
+        constexpr int kSpan = C == 1 ? 16 : 32;              // at most 16 warps in a CTA
+        const int mine = lane & (kSpan - 1);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            v[n] = area[buf][n][lane & (kSpan - 1)];
-            if constexpr (kValues > 32) v[n] += area[buf][n][lane + 32];
+            v[n] = mine < warps * C ? area[buf][n][first + mine] : A(0);
+            if constexpr (C > 2) v[n] += mine + 32 < warps * C ? area[buf][n][mine + 32] : A(0);
         }
 #pragma unroll
         for (int o = kSpan / 2; o > 0; o >>= 1)
@@ -233,6 +327,32 @@ __device__ __forceinline__ void group_sum(A (&v)[N], Area<A> &area, int &buf)
     }
 }
 
+template <int T>
+constexpr int kDivisor = T > 0 ? T : 1;
+
+template <int T, int C, int V>
+__device__ __forceinline__ Columns<T, V> columns_of(int cols, const Group &g)
+{
+    if constexpr (T > 0) return {(int)(threadIdx.x % kDivisor<T>), cols, T};
+    else if constexpr (C == 1) return {(int)threadIdx.x - g.id * g.threads, cols, g.threads};
+    else return {(int)threadIdx.x + (int)cluster_rank() * g.threads, cols, g.threads * C};
+}
+
+// Where a warp exchanges the pieces of an unaligned store, and 16 bytes more.
+template <class TS, int V, int T, bool ALIGNED>
+struct Stage {
+    static constexpr int kWarps = (T > 0 ? kGroupCta : kMostCta) / 32, kBytes = 32 * V * (int)sizeof(TS) + 16;
+    uint4 room[kWarps * kBytes / 16];
+    __device__ __forceinline__ unsigned char *of_warp()
+    {
+        return reinterpret_cast<unsigned char *>(room) + (threadIdx.x >> 5) * kBytes;
+    }
+};
+template <class TS, int V, int T>
+struct Stage<TS, V, T, true> {
+    __device__ __forceinline__ unsigned char *of_warp() { return nullptr; }
+};
+
 // Mean (0 for the root-mean-square norm) and r = 1 / sqrt(mean((t - mean)^2) + eps) of a row, which is left
 // centred.  The mean first and the centred squares after it, from registers: E[t^2] - mean^2 would
 // cancel where a row's mean is large against its spread.
@@ -240,8 +360,8 @@ template <class A>
 struct RowNorm {
     A mean, r;
 };
-template <int T, int C, int E, class A, class Cols>
-__device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, Area<A> &area, int &buf)
+template <bool ALIGNED, int T, int C, int E, class A, class Cols>
+__device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, const Group &g, Area<A> &area, int &buf)
 {
     RowNorm<A> n = {A(0), A(0)};
     A s[1];
@@ -250,35 +370,38 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
 #pragma unroll
         for (int i = 1; i < E; ++i) sum = sum + t[i];
         s[0] = joined(sum);
-        group_sum<T, C, 1, A>(s, area, buf);
+        group_sum<T, C, 1, A>(s, g, area, buf);
         n.mean = s[0] * inv;
         const Two<A> minus = both(-n.mean);
 #pragma unroll
-        for (int i = 0; i < E; ++i) t[i] = c.inside(2 * i, t[i] + minus);
+        for (int i = 0; i < E; ++i) t[i] = c.template inside<ALIGNED>(2 * i, t[i] + minus);
     }
     Two<A> sum = t[0] * t[0];
 #pragma unroll
     for (int i = 1; i < E; ++i) sum = fused_ma(t[i], t[i], sum);
     s[0] = joined(sum);
-    group_sum<T, C, 1, A>(s, area, buf);
+    group_sum<T, C, 1, A>(s, g, area, buf);
     n.r = group_rsqrt(fused_ma(s[0], inv, eps));
     return n;
 }
 
 // ------------------------------------------------------------------ forward
 // BLK: there is a block output f (else the norm of the stream alone).
-template <class TS, class TB, int T, int C, int E, bool VEC, bool BLK>
-__global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(const __grid_constant__ BlockNormParams p)
+template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK>
+__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 4 ? (T > 0 ? 4 : 2) : 1)
+block_norm_kernel(const __grid_constant__ BlockNormParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
-    constexpr int kCta = T > 32 ? T : kGroupCta;
     constexpr bool kFast = sizeof(TB) == 2;
     __shared__ Area<A> area;
+    __shared__ Stage<TS, V, T, ALIGNED> stages;
+    unsigned char *const stage = stages.of_warp();
     int buf = 0;
-    const long long row = (long long)(blockIdx.x / C) * (kCta / T) + threadIdx.x / T;
+    const long long row = T > 0 ? (long long)blockIdx.x * (kGroupCta / kDivisor<T>) + threadIdx.x / kDivisor<T> : blockIdx.x / C;
     const bool ok = row < p.rows;
-    const Columns<T * C, V, VEC> c = {(int)(threadIdx.x % T + (C > 1 ? cluster_rank() * T : 0)), p.cols};
+    const Group group = {0, (int)blockDim.x};
+    const Columns<T, V> c = columns_of<T, C, V>(p.cols, group);
     const bool wide = p.wide_vec != 0;
     const A inv = A(p.inv_cols);
     const auto times = [](Two<A> h, Two<A> w) { return h * w; };
@@ -286,10 +409,10 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
 
     Packed<TS, E> xr;
     Packed<TB, E> fr, gr;
-    if (BLK) load_row<TB, E>(fr, p.f, row * p.ld_f, c, ok);
-    if (!BLK || p.x) load_row<TS, E>(xr, p.x, row * p.ld_x, c, ok);
+    if (BLK) load_row<ALIGNED, TB, E>(fr, p.f, p.rows, row, p.ld_f, c, ok);
+    if (!BLK || p.x) load_row<ALIGNED, TS, E>(xr, p.x, p.rows, row, p.ld_x, c, ok);
     else xr.clear();
-    if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
+    if (BLK && p.gate_access == FO_AT_CELL) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
 
     RowNorm<A> post = {A(0), A(0)}, pre = {A(0), A(0)};
     Two<A> h[E / 2];
@@ -298,12 +421,12 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fr.get2(k);
         if (p.post.kind != FO_NORM_NONE) {
-            post = row_norm<T, C>(h, p.post.kind, A(p.post.eps), inv, c, area, buf);
+            post = row_norm<ALIGNED, T, C>(h, p.post.kind, A(p.post.eps), inv, c, group, area, buf);
             const Two<A> r = both(post.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
-            if (p.post.weight) with_vector<TB, E>(h, p.post.weight, wide, c, times);
-            if (p.post.bias) with_vector<TB, E>(h, p.post.bias, wide, c, plus);
+            if (p.post.weight) with_vector<ALIGNED, TB, E>(h, p.post.weight, wide, c, times);
+            if (p.post.bias) with_vector<ALIGNED, TB, E>(h, p.post.bias, wide, c, plus);
         }
         if (p.gate_access == FO_AT_ROW) {
             const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
@@ -315,32 +438,32 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
             });
         } else if (p.gate_access == FO_AT_COL) {
             with_activation(p.gate_act, [&](auto kind) {
-                with_vector<TB, E>(h, p.gate, false, c,
+                with_vector<ALIGNED, TB, E>(h, p.gate, false, c,
                                    [](Two<A> z, Two<A> g) { return z * activate<decltype(kind)::value, kFast, A>(g); });
             });
         }
-        if (p.col_scale) with_vector<TB, E>(h, p.col_scale, wide, c, times);
+        if (p.col_scale) with_vector<ALIGNED, TB, E>(h, p.col_scale, wide, c, times);
         const Two<A> k2 = both(scale);
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fused_ma(h[k / 2], k2, xr.get2(k));
-        if (p.post.bias && p.cols != T * C * E) {            // a bias leaves no zeros outside the row
+        if (p.post.bias && p.cols != c.threads() * E) {            // a bias leaves no zeros outside the row
 #pragma unroll
-            for (int k = 0; k < E; k += 2) h[k / 2] = c.inside(k, h[k / 2]);
+            for (int k = 0; k < E; k += 2) h[k / 2] = c.template inside<ALIGNED>(k, h[k / 2]);
         }
     } else {
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = xr.get2(k);
     }
-    if (p.h && ok) store_piece<TS, E>(static_cast<TS *>(p.h) + row * p.ld_h, h, 0, c);
+    if (p.h) store_piece<ALIGNED, TS, E>(p.h, row, p.ld_h, h, 0, c, ok, stage);
     if (p.pre.kind != FO_NORM_NONE) {
-        pre = row_norm<T, C>(h, p.pre.kind, A(p.pre.eps), inv, c, area, buf);
-        if (p.y && ok) {
+        pre = row_norm<ALIGNED, T, C>(h, p.pre.kind, A(p.pre.eps), inv, c, group, area, buf);
+        if (p.y) {
             const Two<A> r = both(pre.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
-            if (p.pre.weight) with_vector<TB, E>(h, p.pre.weight, wide, c, times);
-            if (p.pre.bias) with_vector<TB, E>(h, p.pre.bias, wide, c, plus);
-            store_piece<TB, E>(static_cast<TB *>(p.y) + row * p.ld_y, h, 0, c);
+            if (p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
+            if (p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
+            store_piece<ALIGNED, TB, E>(p.y, row, p.ld_y, h, 0, c, ok, stage);
         }
     }
     if (p.stats && ok && c.t == 0) {
@@ -357,68 +480,94 @@ __global__ void __launch_bounds__(T > 32 ? T : kGroupCta) block_norm_kernel(cons
 // hold them (many sums of long rows, float64) they lie in the CTA's own part of the workspace instead.
 // At the end every CTA writes its line of partial sums, and column_sum_kernel adds the lines in order.
 
-// The thread's elements k0 .. k0 + N - 1 of the column sum at `place`.
-template <int CTA, int E, int N, class A, class Body>
-__device__ __forceinline__ void column_sums(A *sums, int place, int k0, Body body)
-{
-    constexpr int kPiece = 16 / (int)sizeof(A);
+// A thread's E values of one column sum: 16-byte pieces one behind the other, in an order that turns with the
+// thread's number so that the 8 threads of one shared-memory access meet 32 different banks.
+template <int E, class A>
+struct SumPieces {
+    static constexpr int kValues = 16 / (int)sizeof(A), kPieces = E / kValues;
     struct alignas(16) Piece {
-        Two<A> v[kPiece / 2];
+        Two<A> v[kValues / 2];
     };
-    Piece *q = reinterpret_cast<Piece *>(sums) + (place * (E / kPiece) + k0 / kPiece) * CTA + threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < N; k += kPiece) {
-        Piece s = q[k / kPiece * CTA];
-#pragma unroll
-        for (int i = 0; i < kPiece / 2; ++i) s.v[i] = body(k / 2 + i, s.v[i]);
-        q[k / kPiece * CTA] = s;
+    static __device__ __forceinline__ int turned(int thread, int piece)
+    {
+        constexpr int kTurns = kPieces < 8 ? kPieces : 8;
+        return piece ^ (thread / (8 / kTurns) % kTurns);
     }
-}
+    // elements k0 .. k0 + N - 1: v = body(pair, v)
+    template <int N, class Body>
+    static __device__ __forceinline__ void change(A *slot, int k0, Body body)
+    {
+        Piece *q = reinterpret_cast<Piece *>(slot) + threadIdx.x * kPieces;
+#pragma unroll
+        for (int k = 0; k < N; k += kValues) {
+            Piece &at = q[turned(threadIdx.x, (k0 + k) / kValues)];
+            Piece s = at;
+#pragma unroll
+            for (int i = 0; i < kValues / 2; ++i) s.v[i] = body(k / 2 + i, s.v[i]);
+            at = s;
+        }
+    }
+    static __device__ __forceinline__ A read(const A *slot, int thread, int k)
+    {
+        return slot[thread * E + turned(thread, k / kValues) * kValues + k % kValues];
+    }
+};
 
-// 128 registers a thread, so that 512 threads share an SM: with 140, which the compiler would take, it is half of that.
-template <class TS, class TB, int T, int C, int E, bool VEC, bool BLK>
-__global__ void __launch_bounds__(T > 32 ? T : kGroupCta, sizeof(Acc<TB>) == 8 ? 1 : 512 / (T > 32 ? T : kGroupCta))
+// 128 registers a thread, so that 512 threads share an SM (the compiler would take up to 140).
+template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK>
+__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, T > 0 && sizeof(Acc<TB>) == 4 ? 2 : 1)
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
-    constexpr int P = kPieceOf<TB, VEC>;
-    constexpr int kCta = T > 32 ? T : kGroupCta;
-    constexpr int kGroups = kCta / T;
+    constexpr int P = V;
+    constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
     constexpr bool kFast = sizeof(TB) == 2;
     __shared__ Area<A> area;
+    __shared__ Stage<TS, V, T, ALIGNED> stages;
+    unsigned char *const stage = stages.of_warp();
     extern __shared__ __align__(16) unsigned char dynamic[];
     int buf = 0;
-    const Columns<T * C, V, VEC> c = {(int)(threadIdx.x % T + (C > 1 ? cluster_rank() * T : 0)), p.cols};
-    const bool ragged = p.cols != T * C * E;
+    const Group group = {T > 0 ? 0 : (int)threadIdx.x / p.group, p.group};
+    const int groups = T > 0 ? kGroups : (int)blockDim.x / p.group, cta = T > 0 ? kGroupCta : (int)blockDim.x;
+    const Columns<T, V> c = columns_of<T, C, V>(p.cols, group);
+    const bool ragged = p.cols != c.threads() * E;
     const A inv = A(p.inv_cols);
     const A *stats = static_cast<const A *>(p.stats);
     const bool wide = p.wide_vec != 0;
+    using Sums = SumPieces<E, A>;
     const int n_slots = __popc(p.slots);
-    A *const sums = p.sums ? static_cast<A *>(p.sums) + (size_t)blockIdx.x * n_slots * kCta * E
-                           : reinterpret_cast<A *>(dynamic);
+    A *sums = reinterpret_cast<A *>(dynamic);
+    if constexpr (sizeof(A) == 8) {                          // of float sums there is always room
+        if (p.sums) sums = static_cast<A *>(p.sums) + (size_t)blockIdx.x * n_slots * cta * E;
+    }
+    // where each sum begins, -1: it is not wanted
+    int slot_at[kGradSlots];
+#pragma unroll
+    for (int s = 0; s < kGradSlots; ++s)
+        slot_at[s] = ((p.slots >> s) & 1u) ? __popc(p.slots & ((1u << s) - 1u)) * cta * E : -1;
     // adds term(i), for the pairs i of a piece from element k0, to a column sum that is wanted
     auto add = [&](int slot, int k0, auto term) {
-        if (!((p.slots >> slot) & 1u)) return;
-        column_sums<kCta, E, P, A>(sums, __popc(p.slots & ((1u << slot) - 1u)), k0, term);
+        if (slot_at[slot] >= 0) Sums::template change<P>(sums + slot_at[slot], k0, term);
     };
-    for (int s = 0; s < n_slots; ++s) column_sums<kCta, E, E, A>(sums, s, 0, [&](int, Two<A>) { return both(A(0)); });
+    for (int s = 0; s < n_slots; ++s)
+        Sums::template change<E>(sums + s * cta * E, 0, [](int, Two<A>) { return both(A(0)); });
 
-    // all threads of a CTA, and all CTAs of a cluster, take the same number of turns: the sums meet at barriers
-    for (long long row0 = (long long)(blockIdx.x / C) * kGroups; row0 < p.rows;
-         row0 += (long long)(gridDim.x / C) * kGroups) {
-        const long long row = row0 + threadIdx.x / T;
+    // all threads of a group, and all CTAs of a cluster, take the same number of turns: their sums meet at barriers
+    for (long long row0 = (long long)(blockIdx.x / C) * groups; row0 < p.rows;
+         row0 += (long long)(gridDim.x / C) * groups) {
+        const long long row = row0 + (T > 0 ? (int)threadIdx.x / kDivisor<T> : group.id);
         const bool ok = row < p.rows;                        // past the end all values are zero
         Packed<TS, E> dhr, hr;
         Packed<TB, E> dyr, fr, gr;
         if (p.dy) {
-            load_row<TB, E>(dyr, p.dy, row * p.ld_dy, c, ok);
-            load_row<TS, E>(hr, p.h, row * p.ld_h, c, ok);
+            load_row<ALIGNED, TB, E>(dyr, p.dy, p.rows, row, p.ld_dy, c, ok);
+            load_row<ALIGNED, TS, E>(hr, p.h, p.rows, row, p.ld_h, c, ok);
         }
-        if (p.dh) load_row<TS, E>(dhr, p.dh, row * p.ld_dh, c, ok);
+        if (p.dh) load_row<ALIGNED, TS, E>(dhr, p.dh, p.rows, row, p.ld_dh, c, ok);
         else dhr.clear();
-        if (BLK) load_row<TB, E>(fr, p.f, row * p.ld_f, c, ok);
-        if (BLK && p.gate_access == FO_AT_CELL) load_row<TB, E>(gr, p.gate, row * p.ld_gate, c, ok);
+        if (BLK) load_row<ALIGNED, TB, E>(fr, p.f, p.rows, row, p.ld_f, c, ok);
+        if (BLK && p.gate_access == FO_AT_CELL) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
 
         Two<A> t[E / 2];
         if (p.dy) {
@@ -437,7 +586,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 add(kPreB, k0, [&](int i, Two<A> s) { return s + a[i]; });
                 if (p.pre.weight) {
                     Two<A> w[P / 2];
-                    load_vector<TB, P>(w, p.pre.weight, wide, k0, c);
+                    load_vector<ALIGNED, TB, P>(w, p.pre.weight, wide, k0, c);
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) a[i] = a[i] * w[i];
                 }
@@ -451,9 +600,9 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
             A s[2] = {joined(along), A(0)};
             if (p.pre.kind == FO_NORM_LAYER) {
                 s[1] = joined(level);
-                group_sum<T, C, 2, A>(s, area, buf);
+                group_sum<T, C, 2, A>(s, group, area, buf);
             } else {
-                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), area, buf);
+                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), group, area, buf);
             }
             // dh + r (a - n mean(a n) - mean(a))
             along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
@@ -462,13 +611,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 t[k / 2] = fused_ma(t[k / 2], r, fused_ma(hr.get2(k) + minus, along, dhr.get2(k) + level));
             if (ragged) {
 #pragma unroll
-                for (int k = 0; k < E; k += 2) t[k / 2] = c.inside(k, t[k / 2]);
+                for (int k = 0; k < E; k += 2) t[k / 2] = c.template inside<ALIGNED>(k, t[k / 2]);
             }
         } else {
 #pragma unroll
             for (int k = 0; k < E; k += 2) t[k / 2] = dhr.get2(k);
         }
-        if (p.dx && ok) store_piece<TS, E>(static_cast<TS *>(p.dx) + row * p.ld_dx, t, 0, c);
+        if (p.dx) store_piece<ALIGNED, TS, E>(p.dx, row, p.ld_dx, t, 0, c, ok, stage);
         if constexpr (BLK) {
             const bool normed = p.post.kind != FO_NORM_NONE, row_gate = p.gate_access == FO_AT_ROW;
             const A r1 = ok && normed ? stats[p.rows + row] : A(1);
@@ -484,7 +633,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
             for (int k0 = 0; k0 < E; k0 += P) {
                 Two<A> n[P / 2], z[P / 2], w[P / 2], a[P / 2], slope[P / 2], *d = t + k0 / 2;
-                if (p.post.weight) load_vector<TB, P>(w, p.post.weight, wide, k0, c);
+                if (p.post.weight) load_vector<ALIGNED, TB, P>(w, p.post.weight, wide, k0, c);
                 else
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) w[i] = both(A(1));
@@ -496,13 +645,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 }
                 if (p.post.bias) {
                     Two<A> b[P / 2];
-                    load_vector<TB, P>(b, p.post.bias, wide, k0, c);
+                    load_vector<ALIGNED, TB, P>(b, p.post.bias, wide, k0, c);
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) z[i] = z[i] + b[i];
                 }
                 if (p.gate_access == FO_AT_CELL || p.gate_access == FO_AT_COL) {
                     Two<A> g[P / 2];
-                    if (p.gate_access == FO_AT_COL) load_vector<TB, P>(g, p.gate, false, k0, c);
+                    if (p.gate_access == FO_AT_COL) load_vector<ALIGNED, TB, P>(g, p.gate, false, k0, c);
                     else
 #pragma unroll
                         for (int i = 0; i < P / 2; ++i) g[i] = gr.get2(k0 + 2 * i);
@@ -518,7 +667,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 if (p.col_scale) {
                     add(kColScale, k0, [&](int i, Two<A> s) { return fused_ma(d[i] * z[i], a[i], s); });
                     Two<A> cs[P / 2];
-                    load_vector<TB, P>(cs, p.col_scale, wide, k0, c);
+                    load_vector<ALIGNED, TB, P>(cs, p.col_scale, wide, k0, c);
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) d[i] = d[i] * cs[i];
                 }
@@ -528,8 +677,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     z[i] = d[i] * z[i] * slope[i];
                     d[i] = d[i] * a[i];
                 }
-                if (p.dgate && ok && p.gate_access == FO_AT_CELL)
-                    store_piece<TB, P>(static_cast<TB *>(p.dgate) + row * p.ld_dgate, z, k0, c);
+                if (p.dgate && p.gate_access == FO_AT_CELL)
+                    store_piece<ALIGNED, TB, P>(p.dgate, row, p.ld_dgate, z, k0, c, ok, stage);
                 add(kGateCol, k0, [&](int i, Two<A> s) { return s + z[i]; });
                 if (row_gate) {
 #pragma unroll
@@ -552,10 +701,10 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
             A s[3] = {joined(along), A(0), A(0)};
             if (row_gate || p.post.kind == FO_NORM_LAYER) {
                 s[1] = joined(level), s[2] = joined(gate_sum);
-                group_sum<T, C, 3, A>(s, area, buf);
+                group_sum<T, C, 3, A>(s, group, area, buf);
                 if (p.dgate && ok && row_gate && c.t == 0) static_cast<A *>(p.dgate)[row] = s[2];
             } else if (normed) {
-                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), area, buf);
+                group_sum<T, C, 1, A>(*reinterpret_cast<A(*)[1]>(&s), group, area, buf);
             }
             if (normed) {
                 along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
@@ -563,61 +712,55 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 for (int k = 0; k < E; k += 2)
                     t[k / 2] = fused_ma(t[k / 2], r, fused_ma(fr.get2(k) + minus, along, level));
             }
-            if (p.df && ok) store_piece<TB, E>(static_cast<TB *>(p.df) + row * p.ld_df, t, 0, c);
+            if (p.df) store_piece<ALIGNED, TB, E>(p.df, row, p.ld_df, t, 0, c, ok, stage);
         }
     }
 
     // the CTA's line of every sum, its groups added in order
+    __syncthreads();
     const size_t plane = (size_t)(gridDim.x / C) * p.cols;
-    A *line = static_cast<A *>(p.partial) + (size_t)(blockIdx.x / C) * p.cols;
-    if constexpr (T > 32) {
-        for (int s = 0; s < n_slots; ++s, line += plane)
-            column_sums<kCta, E, E, A>(sums, s, 0, [&](int i, Two<A> sum) {
-                if (c.has(2 * i)) line[c.of(2 * i)] = first(sum);
-                if (c.has(2 * i + 1)) line[c.of(2 * i + 1)] = second(sum);
-                return sum;
-            });
-    } else {
-        constexpr int kPiece = 16 / (int)sizeof(A);
-        __syncthreads();
-        for (int i = threadIdx.x; i < n_slots * T * E; i += kCta) {
-            const int s = i / (T * E), k = i / T % E, t = i % T;
-            const Columns<T, V, VEC> own = {t, p.cols};
-            if (!own.has(k)) continue;
-            const A *q = sums + (size_t)(s * (E / kPiece) + k / kPiece) * kCta * kPiece + t * kPiece + k % kPiece;
-            A v = q[0];
-            for (int g = 1; g < kGroups; ++g) v += q[g * T * kPiece];
-            line[s * plane + own.of(k)] = v;
+    A *const line = static_cast<A *>(p.partial) + (size_t)(blockIdx.x / C) * p.cols;
+    const int threads = T > 0 ? T : p.group;
+    for (int i = threadIdx.x; i < threads * E; i += cta) {
+        const int t = i / V % threads, k = i / (V * threads) * V + i % V;
+        const Columns<T, V> own = {t + (C > 1 ? (int)cluster_rank() * threads : 0), p.cols, c.count};
+        const int j = own.of(k);
+        if (j >= p.cols) continue;
+        for (int s = 0; s < n_slots; ++s) {
+            A v = A(0);
+            for (int g = 0; g < groups; ++g) v += Sums::read(sums + s * cta * E, g * threads + t, k);
+            line[s * plane + j] = v;
         }
     }
 }
 
 // out[s][j] = sum over the lines of partial[s][line][j], in a fixed order: a CTA takes 32 columns of one
-// sum, its 8 warps every 8th line each (128-byte reads), then the warps' sums are added in order.
+// sum, its 32 warps every 32nd line each (128-byte reads), then a warp adds the 32 sums of each column.
 struct ColumnSumParams {
     const void *partial;
     void *out[kGradSlots];
     int lines, cols;
 };
 
+constexpr int kSumWarps = 32;
+
 template <class A>
-__global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ ColumnSumParams p)
+__global__ void __launch_bounds__(kSumWarps * 32) column_sum_kernel(const __grid_constant__ ColumnSumParams p)
 {
-    __shared__ A sum[8][32];
+    __shared__ A sum[kSumWarps][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
     const A *src = static_cast<const A *>(p.partial) + (size_t)blockIdx.y * p.lines * p.cols;
     A v = A(0);
     if (j < p.cols) {
-#pragma unroll 4
-        for (int g = warp; g < p.lines; g += 8) v += __ldcg(src + (size_t)g * p.cols + j);
+#pragma unroll 8
+        for (int g = warp; g < p.lines; g += kSumWarps) v += __ldcg(src + (size_t)g * p.cols + j);
     }
     sum[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && j < p.cols) {
+    v = sum[lane][warp];                                     // warp w: column w
 #pragma unroll
-        for (int g = 1; g < 8; ++g) v += sum[g][lane];
-        static_cast<A *>(p.out[blockIdx.y])[j] = v;
-    }
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0 && blockIdx.x * 32 + warp < (unsigned)p.cols) static_cast<A *>(p.out[blockIdx.y])[blockIdx.x * 32 + warp] = v;
 }
 
 }  // namespace fo

@@ -18,25 +18,25 @@ cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t st);
 template <class TS, class TB>
 cudaError_t launch_block_norm_grad(BlockNormGradParams p, GradSpace *space, cudaStream_t st);
 
-// Calls go(T, C, E) with the shape for `cols` columns: 16 elements a thread where a row has them.  A sum
-// over the group costs every thread about 25 instructions, which 16 elements share; 16 is also what 64 to 80
-// registers hold of a row's matrices.  Beyond 512 threads a row takes a cluster: CTAs of 1024 threads have
-// 64 registers a thread, and spill.
-template <class Go>
+// Calls go(T, C, E, threads) with the shape for `cols` columns in pieces of V: T threads of a warp and CTAs of
+// kGroupCta, or (T = 0) C CTAs of `threads` a row; 16 elements a thread where a row has them.  A sum over the
+// group costs every thread about 25 instructions, which 16 elements share; 16 is also what 64 (the gradient: 128)
+// registers hold of a row's matrices.  Beyond 512 threads a row takes a cluster: CTAs of 1024 threads would
+// have 64 registers a thread, and spill.
+template <int V, class Go>
 cudaError_t with_row_shape(int cols, Go go)
 {
-#define FO_SHAPE(t, c, e) \
-    go(std::integral_constant<int, t>(), std::integral_constant<int, c>(), std::integral_constant<int, e>())
-    if (cols <= 64) return FO_SHAPE(8, 1, 8);
-    if (cols <= 128) return FO_SHAPE(8, 1, 16);
-    if (cols <= 256) return FO_SHAPE(16, 1, 16);
-    if (cols <= 512) return FO_SHAPE(32, 1, 16);
-    if (cols <= 1024) return FO_SHAPE(64, 1, 16);
-    if (cols <= 2048) return FO_SHAPE(128, 1, 16);
-    if (cols <= 4096) return FO_SHAPE(256, 1, 16);
-    if (cols <= 8192) return FO_SHAPE(512, 1, 16);
-    if (cols <= 16384) return FO_SHAPE(512, 2, 16);
-    return FO_SHAPE(512, 4, 16);
+#define FO_SHAPE(t, c, e, n) \
+    go(std::integral_constant<int, t>(), std::integral_constant<int, c>(), std::integral_constant<int, e>(), n)
+    if (cols <= 64) return FO_SHAPE(8, 1, 8, kGroupCta);
+    if (cols <= 128) return FO_SHAPE(8, 1, 16, kGroupCta);
+    if (cols <= 256) return FO_SHAPE(16, 1, 16, kGroupCta);
+    if (cols <= 512) return FO_SHAPE(32, 1, 16, kGroupCta);
+    const int c = cols <= 8192 ? 1 : cols <= 16384 ? 2 : 4, pieces = (cols + V - 1) / V;
+    const int per_cta = 16 / V * c, threads = ((pieces + per_cta - 1) / per_cta + 31) / 32 * 32;
+    if (c == 1) return FO_SHAPE(0, 1, 16, threads);
+    if (c == 2) return FO_SHAPE(0, 2, 16, threads);
+    return FO_SHAPE(0, 4, 16, threads);
 #undef FO_SHAPE
 }
 
@@ -62,65 +62,79 @@ cudaError_t launch_rows(void (*kern)(Params), const Params &p, long long grid, i
 template <class TS, class TB>
 cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t st)
 {
-    return with_row_shape(p.cols, [&](auto tc, auto cc, auto ec) -> cudaError_t {
+    return with_row_shape<16 / (int)sizeof(TB)>(p.cols, [&](auto tc, auto cc, auto ec, int cta) -> cudaError_t {
         constexpr int T = decltype(tc)::value, C = decltype(cc)::value, E = decltype(ec)::value;
-        constexpr int kCta = T > 32 ? T : kGroupCta;
-        const long long grid = (p.rows + kCta / T - 1) / (kCta / T) * C;
-        auto go = [&](auto vec) {
-            constexpr bool VEC = decltype(vec)::value;
-            return p.f ? launch_rows(block_norm_kernel<TS, TB, T, C, E, VEC, true>, p, grid, kCta, C, 0, st)
-                       : launch_rows(block_norm_kernel<TS, TB, T, C, E, VEC, false>, p, grid, kCta, C, 0, st);
+        constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
+        const long long grid = (p.rows + kGroups - 1) / kGroups * C;
+        auto go = [&](auto aligned) {
+            constexpr bool ALIGNED = decltype(aligned)::value;
+            return p.f ? launch_rows(block_norm_kernel<TS, TB, T, C, E, ALIGNED, true>, p, grid, cta, C, 0, st)
+                       : launch_rows(block_norm_kernel<TS, TB, T, C, E, ALIGNED, false>, p, grid, cta, C, 0, st);
         };
-        return p.vec ? go(std::true_type()) : go(std::false_type());
+        return p.aligned ? go(std::true_type()) : go(std::false_type());
     });
 }
 
-// What a kernel needs to be asked once per device.
-struct GradKernelFacts {
-    bool known;
-    int per_sm[kGradSlots + 1];              // resident CTAs by number of sums in shared memory, 0: they do not fit
-};
+// Resident CTAs of a gradient kernel with `sums` column sums in shared memory, 0: they do not fit.  Asked once per
+// device and size of CTA.
+template <void (*KERNEL)(BlockNormGradParams)>
+cudaError_t grad_residency(int cta, int sums, size_t sum_bytes, int *per_sm)
+{
+    constexpr size_t kRoom = 200 * 1024;
+    static short cache[16][kMostCta / 32 + 1][kGradSlots + 1];       // + 1; the same whoever asks first
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    short &known = cache[dev & 15][cta / 32][sums];
+    if (known == 0) {
+        int found = 0;
+        if (sums * sum_bytes <= kRoom) {
+            e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRoom);
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&found, KERNEL, cta, sums * sum_bytes);
+            if (e != cudaSuccess) return e;
+        }
+        known = (short)(found + 1);
+    }
+    *per_sm = known - 1;
+    return cudaSuccess;
+}
 
 template <class TS, class TB>
 cudaError_t launch_block_norm_grad(BlockNormGradParams p, GradSpace *space, cudaStream_t st)
 {
-    return with_row_shape(p.cols, [&](auto tc, auto cc, auto ec) -> cudaError_t {
+    return with_row_shape<16 / (int)sizeof(TB)>(p.cols, [&](auto tc, auto cc, auto ec, int cta) -> cudaError_t {
         constexpr int T = decltype(tc)::value, C = decltype(cc)::value, E = decltype(ec)::value;
-        constexpr int kCta = T > 32 ? T : kGroupCta;
-        constexpr size_t kSum = (size_t)kCta * E * sizeof(Acc<TB>);
-        auto go = [&](auto vec, auto blk) -> cudaError_t {
-            const auto kern = block_norm_grad_kernel<TS, TB, T, C, E, decltype(vec)::value, decltype(blk)::value>;
-            static GradKernelFacts facts[64];                // the same whoever asks first
-            int dev = 0;
-            cudaError_t e = cudaGetDevice(&dev);
-            if (e != cudaSuccess) return e;
-            GradKernelFacts &f = facts[dev & 63];
-            if (!f.known) {
-                constexpr int kFit = (int)((size_t)(220 * 1024) / kSum);
-                constexpr int kMost = kFit < kGradSlots ? kFit : kGradSlots;
-                e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMost * kSum));
-                for (int n = 0; n <= kGradSlots && e == cudaSuccess; ++n) {
-                    f.per_sm[n] = 0;
-                    if (n <= kMost) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&f.per_sm[n], kern, kCta, n * kSum);
-                }
-                if (e != cudaSuccess) return e;
-                f.known = true;
+        constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
+        auto go = [&](auto aligned, auto blk) -> cudaError_t {
+            constexpr auto kern = block_norm_grad_kernel<TS, TB, T, C, E, decltype(aligned)::value, decltype(blk)::value>;
+            // as many groups as 512 threads hold, while there are rows for them on every SM
+            const int sms = sm_count();
+            int groups = kGroups, threads = cta;
+            if (T == 0 && C == 1) {
+                const long long each = (p.rows + sms - 1) / (sms > 0 ? sms : 1);
+                groups = kMostCta / cta;
+                if (groups > each) groups = (int)each;
+                threads = groups * cta;
             }
+            p.group = cta;
+            const size_t sum_bytes = (size_t)threads * E * sizeof(Acc<TB>);
             const int n = __builtin_popcount(p.slots);
-            const bool fits = f.per_sm[n] > 0;
-            p.sums = fits ? nullptr : space->sums;
-            long long lines = (long long)sm_count() * (fits ? f.per_sm[n] : 1) / C;
-            const long long groups = (p.rows + kCta / T - 1) / (kCta / T);
-            if (lines > groups) lines = groups;
+            int per_sm = 0;
+            const cudaError_t e = grad_residency<kern>(threads, n, sum_bytes, &per_sm);
+            if (e != cudaSuccess) return e;
+            p.sums = per_sm > 0 ? nullptr : space->sums;
+            long long lines = (long long)sms * (per_sm > 0 ? per_sm : 1) / C;
+            const long long turns = (p.rows + groups - 1) / groups;
+            if (lines > turns) lines = turns;
             if (lines > space->max_lines) lines = space->max_lines;
             if (lines < 1) lines = 1;
             space->lines = (int)lines;
-            return launch_rows(kern, p, lines * C, kCta, C, fits ? n * kSum : 0, st);
+            return launch_rows(kern, p, lines * C, threads, C, per_sm > 0 ? n * sum_bytes : 0, st);
         };
-        auto by_block = [&](auto vec) -> cudaError_t {
-            return p.f ? go(vec, std::true_type()) : go(vec, std::false_type());
+        auto by_block = [&](auto aligned) -> cudaError_t {
+            return p.f ? go(aligned, std::true_type()) : go(aligned, std::false_type());
         };
-        return p.vec ? by_block(std::true_type()) : by_block(std::false_type());
+        return p.aligned ? by_block(std::true_type()) : by_block(std::false_type());
     });
 }
 #endif

@@ -118,6 +118,13 @@ struct Packed {
         }
     }
     __device__ __forceinline__ Two<Acc<T>> get2(int k) const { return two(get(k), get(k + 1)); }      // k even
+    __device__ __forceinline__ T raw(int k) const                     // as it lies in memory
+    {
+        if constexpr (sizeof(T) >= 4) return (T)get(k);
+        else if constexpr (std::is_same<T, __nv_bfloat16>::value)
+            return __ushort_as_bfloat16((unsigned short)(w[k / 2] >> (16 * (k & 1))));
+        else return __ushort_as_half((unsigned short)(w[k / 2] >> (16 * (k & 1))));
+    }
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
