@@ -1,4 +1,5 @@
-"""Builds csrc/*.cu into libfusedops.so (sm_100a) next to this file.
+"""Builds csrc/*.cu into libfusedops.so (sm_100a) next to this file, and csrc/training_py.cpp, the CPython
+extension that training.py calls it through, into _training.so.
 
     python -m paper_1801_00829_b200.build [--force] [--verbose]
 
@@ -18,6 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libfusedops.so")
+EXTENSION_SOURCE = os.path.join(CSRC, "training_py.cpp")
+EXTENSION_PATH = os.path.join(HERE, "_training.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -110,6 +113,31 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB_PATH
 
 
+def build_extension(force: bool = False) -> str:
+    """Compile (if needed) the CPython extension against the installed torch; returns its path.  The library it
+    calls is looked for next to it."""
+    deps = [EXTENSION_SOURCE] + glob.glob(os.path.join(INCLUDE, "*.h"))
+    if not force and os.path.exists(EXTENSION_PATH) and all(os.path.getmtime(d) <= os.path.getmtime(EXTENSION_PATH) for d in deps):
+        return EXTENSION_PATH
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) if os.path.isabs(_nvcc()) else "/usr/local/cuda"
+    includes = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    tmp = EXTENSION_PATH + ".tmp%d" % os.getpid()
+    cmd = (["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+           + ["-I" + d for d in includes] + [EXTENSION_SOURCE, "-o", tmp, "-L" + HERE, "-l:libfusedops.so", "-Wl,-rpath,$ORIGIN",
+                                             "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda",
+                                             "-ltorch_python"])
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n%s" % res.stdout[-4000:])
+    os.replace(tmp, EXTENSION_PATH)
+    return EXTENSION_PATH
+
+
 if __name__ == "__main__":
     path = build_library(force="--force" in sys.argv, verbose="--verbose" in sys.argv)
     print(path)
+    print(build_extension(force="--force" in sys.argv))

@@ -78,23 +78,21 @@ int check_gate(const void *gate, int access, int act, long long ld, long long ro
 // threads for short rows, of 512 for longer ones.
 int grad_lines(long long rows, long long cols)
 {
-    const long long cap = cols <= 4096 ? 148 * 2 : 148;
+    const long long cap = cols <= 256 ? 148 * 4 : cols <= 8192 ? 148 * 2 : 148;
     const long long n = rows < cap ? rows : cap;
     return (int)(n > 1 ? n : 1);
 }
 
-// Lines, and room for the sums of CTAs that shared memory does not hold: 8192 columns in each of a row's
-// one, two or four CTAs.
+// Lines, and room for the sums of CTAs that shared memory does not hold: float64 sums of 512 threads with 16
+// elements each (rows beyond 8192 columns).
 size_t grad_line_bytes(long long rows, long long cols, int block_type)
 {
     return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
 }
 size_t grad_sum_bytes(long long rows, long long cols, int block_type)
 {
-    const size_t bytes = block_type == FO_F64 ? 8 : 4, slot = (size_t)512 * 16 * bytes;
-    if (kGradSlots * slot <= 200 * 1024) return 0;
-    const size_t held = cols <= 8192 ? 8192 : cols <= 16384 ? 16384 : 32768;
-    return (size_t)kGradSlots * grad_lines(rows, cols) * held * bytes;
+    if (block_type != FO_F64 || cols <= 8192) return 0;
+    return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)(cols <= 16384 ? 16384 : 32768) * sizeof(double);
 }
 
 }  // namespace

@@ -147,41 +147,44 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
     }
 }
 
-// Stores elements k0 .. k0 + N - 1 of the thread, whole pieces, into its row (`ok`: there is one).
+// The thread's elements, rounded once.
+template <class TE, int E>
+__device__ __forceinline__ Packed<TE, E> pack_row(const Two<Acc<TE>> (&v)[E / 2])
+{
+    Packed<TE, E> r;
+#pragma unroll
+    for (int k = 0; k < E; k += 2) r.put2(k, v[k / 2]);
+    return r;
+}
+
+// Stores the thread's elements into its row (`ok`: there is one).
 // Unaligned: the pieces of the row's threads in a warp are neighbours; they are exchanged through the warp's
 // `stage` so that full aligned 16 bytes can be written, and the ends singly.  All threads of the warp call it.
-template <bool ALIGNED, class TE, int N, int T, int V>
-__device__ __forceinline__ void store_piece(void *base, long long row, long long ld, const Two<Acc<TE>> *v, int k0,
-                                            const Columns<T, V> &c, bool ok, unsigned char *stage)
+template <bool ALIGNED, class TE, int E, int T, int V>
+__device__ __forceinline__ void store_row(void *base, long long row, long long ld, const Packed<TE, E> &v,
+                                          const Columns<T, V> &c, bool ok, unsigned char *stage)
 {
     TE *p = static_cast<TE *>(base) + row * ld;
-    constexpr int kStep = 16 / (int)sizeof(TE);
+    constexpr int kStep = 16 / (int)sizeof(TE), kWords = (int)sizeof(TE);      // kWords / 4 words per element
     if constexpr (ALIGNED) {
 #pragma unroll
-        for (int k = 0; k < N; k += kStep) {
-            if (!ok || c.of(k0 + k) >= c.cols) continue;
-            Packed<TE, kStep> r;
-#pragma unroll
-            for (int e = 0; e < kStep; e += 2) r.put2(e, v[(k + e) / 2]);
-            store16(p + c.of(k0 + k), r.w);
-        }
+        for (int k = 0; k < E; k += kStep)
+            if (ok && c.of(k) < c.cols) store16(p + c.of(k), v.w + k * kWords / 4);
     } else {
         constexpr int kLanes = T > 0 ? T : 32;               // threads of the row in this warp
         constexpr int kChunks = V / kStep;                   // 16-byte chunks of a piece
         const int lane = (threadIdx.x & 31) % kLanes;
         unsigned char *mine = stage + (threadIdx.x & 31) / kLanes * (kLanes * V * (int)sizeof(TE));
 #pragma unroll
-        for (int k = 0; k < N; k += V) {
+        for (int k = 0; k < E; k += V) {
             __syncwarp();
 #pragma unroll
             for (int h = 0; h < V; h += kStep) {
-                Packed<TE, kStep> r;
-#pragma unroll
-                for (int e = 0; e < kStep; e += 2) r.put2(e, v[(k + h + e) / 2]);
-                *reinterpret_cast<uint4 *>(mine + (lane * V + h) * (int)sizeof(TE)) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+                const uint32_t *w = v.w + (k + h) * kWords / 4;
+                *reinterpret_cast<uint4 *>(mine + (lane * V + h) * (int)sizeof(TE)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
             __syncwarp();
-            const int first_col = c.of(k0 + k) - lane * V, left = c.cols - first_col;
+            const int first_col = c.of(k) - lane * V, left = c.cols - first_col;
             const int n = !ok ? 0 : left < kLanes * V ? left : kLanes * V;       // elements to write, may be negative
             TE *q = p + first_col;
             const int head = (int)(((16u - (unsigned)((uintptr_t)q & 15u)) & 15u) / sizeof(TE));
@@ -193,9 +196,9 @@ __device__ __forceinline__ void store_piece(void *base, long long row, long long
                 if (at + kStep <= n) {
                     const uint4 *a = reinterpret_cast<const uint4 *>(held + at / kStep * kStep);
                     const uint4 x = a[0], y = head ? a[1] : x;
-                    const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                     uint32_t r[4];
-                    straddle(r, w, (unsigned)(head * (int)sizeof(TE)));
+                    straddle(r, u, (unsigned)(head * (int)sizeof(TE)));
                     store16(q + at, r);
                 } else {
 #pragma unroll
@@ -207,7 +210,7 @@ __device__ __forceinline__ void store_piece(void *base, long long row, long long
     }
 }
 
-// N elements, whole pieces, from k0 of a vector over the columns (weight, bias, scale, gate per
+// N elements, whole pieces or half ones, from k0 of a vector over the columns (weight, bias, scale, gate per
 // column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives some value of
 // the vector, which meets a zero there: no zeros have to be put where a load might not take place.
 template <bool ALIGNED, class TE, int N, int T, int V>
@@ -231,8 +234,16 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
             o[k / 2] = two((A)q.x, (A)q.y), o[k / 2 + 1] = two((A)q.z, (A)q.w);
         }
     } else {
+        if constexpr (N < V) {
+            static_assert(N * sizeof(TE) == 8, "half a piece");
+            const int j = min(c.of(k0 / V * V), c.cols - V) + k0 % V;
+            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(static_cast<const TE *>(base) + j));
+            Packed<TE, V> r;
+            r.w[0] = q.x, r.w[1] = q.y;
+            o[0] = r.get2(0), o[1] = r.get2(2);
+        }
 #pragma unroll
-        for (int k = 0; k < N; k += V) {
+        for (int k = 0; k + V <= N; k += V) {
             const int j = min(c.of(k0 + k), c.cols - V);
             const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + j));
             Packed<TE, V> r;
@@ -261,7 +272,7 @@ __device__ __forceinline__ void with_vector(Two<Acc<TE>> (&h)[E / 2], const void
 // `buf` alternates between two exchange areas, so one barrier per sum is enough: an area is written
 // again only after the barrier of the sum between.
 template <class A>
-using Area = A[2][3][64];
+using Area = A[2][3][128];
 
 __device__ __forceinline__ unsigned cluster_rank()
 {
@@ -317,7 +328,9 @@ __device__ __forceinline__ void group_sum(A (&v)[N], const Group &g, Area<A> &ar
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             v[n] = mine < warps * C ? area[buf][n][first + mine] : A(0);
-            if constexpr (C > 2) v[n] += mine + 32 < warps * C ? area[buf][n][mine + 32] : A(0);
+#pragma unroll
+            for (int more = 32; more < 16 * C; more += 32)
+                v[n] += mine + more < warps * C ? area[buf][n][mine + more] : A(0);
         }
 #pragma unroll
         for (int o = kSpan / 2; o > 0; o >>= 1)
@@ -454,7 +467,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = xr.get2(k);
     }
-    if (p.h) store_piece<ALIGNED, TS, E>(p.h, row, p.ld_h, h, 0, c, ok, stage);
+    if (p.h) store_row<ALIGNED, TS, E>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
     if (p.pre.kind != FO_NORM_NONE) {
         pre = row_norm<ALIGNED, T, C>(h, p.pre.kind, A(p.pre.eps), inv, c, group, area, buf);
         if (p.y) {
@@ -463,7 +476,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
             if (p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
             if (p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
-            store_piece<ALIGNED, TB, E>(p.y, row, p.ld_y, h, 0, c, ok, stage);
+            store_row<ALIGNED, TB, E>(p.y, row, p.ld_y, pack_row<TB, E>(h), c, ok, stage);
         }
     }
     if (p.stats && ok && c.t == 0) {
@@ -507,20 +520,20 @@ struct SumPieces {
             at = s;
         }
     }
-    static __device__ __forceinline__ A read(const A *slot, int thread, int k)
+    static __device__ __forceinline__ Piece at(const A *slot, int thread, int piece)
     {
-        return slot[thread * E + turned(thread, k / kValues) * kValues + k % kValues];
+        return reinterpret_cast<const Piece *>(slot)[thread * kPieces + turned(thread, piece)];
     }
 };
 
-// 128 registers a thread, so that 512 threads share an SM (the compiler would take up to 140).
+// 64 registers a thread with 8 elements, so that 1024 threads share an SM; 128 with 16.
 template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK>
-__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, T > 0 && sizeof(Acc<TB>) == 4 ? 2 : 1)
+__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 8 || E > 8 ? 1 : T > 0 ? 4 : 2)
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
-    constexpr int P = V;
+    constexpr int P = 16 / (int)sizeof(A);                   // elements worked on at a time: what registers hold
     constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
     constexpr bool kFast = sizeof(TB) == 2;
     __shared__ Area<A> area;
@@ -617,7 +630,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
             for (int k = 0; k < E; k += 2) t[k / 2] = dhr.get2(k);
         }
-        if (p.dx) store_piece<ALIGNED, TS, E>(p.dx, row, p.ld_dx, t, 0, c, ok, stage);
+        if (p.dx) store_row<ALIGNED, TS, E>(p.dx, row, p.ld_dx, pack_row<TS, E>(t), c, ok, stage);
         if constexpr (BLK) {
             const bool normed = p.post.kind != FO_NORM_NONE, row_gate = p.gate_access == FO_AT_ROW;
             const A r1 = ok && normed ? stats[p.rows + row] : A(1);
@@ -677,8 +690,10 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     z[i] = d[i] * z[i] * slope[i];
                     d[i] = d[i] * a[i];
                 }
-                if (p.dgate && p.gate_access == FO_AT_CELL)
-                    store_piece<ALIGNED, TB, P>(p.dgate, row, p.ld_dgate, z, k0, c, ok, stage);
+                if (p.gate_access == FO_AT_CELL) {           // in the gate's place
+#pragma unroll
+                    for (int i = 0; i < P / 2; ++i) gr.put2(k0 + 2 * i, z[i]);
+                }
                 add(kGateCol, k0, [&](int i, Two<A> s) { return s + z[i]; });
                 if (row_gate) {
 #pragma unroll
@@ -698,6 +713,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     }
                 }
             }
+            if (p.dgate && p.gate_access == FO_AT_CELL)
+                store_row<ALIGNED, TB, E>(p.dgate, row, p.ld_dgate, gr, c, ok, stage);
             A s[3] = {joined(along), A(0), A(0)};
             if (row_gate || p.post.kind == FO_NORM_LAYER) {
                 s[1] = joined(level), s[2] = joined(gate_sum);
@@ -712,24 +729,29 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 for (int k = 0; k < E; k += 2)
                     t[k / 2] = fused_ma(t[k / 2], r, fused_ma(fr.get2(k) + minus, along, level));
             }
-            if (p.df) store_piece<ALIGNED, TB, E>(p.df, row, p.ld_df, t, 0, c, ok, stage);
+            if (p.df) store_row<ALIGNED, TB, E>(p.df, row, p.ld_df, pack_row<TB, E>(t), c, ok, stage);
         }
     }
 
-    // the CTA's line of every sum, its groups added in order
+    // the CTA's line of every sum, its groups added in order: a thread takes the piece of one thread of all groups
     __syncthreads();
     const size_t plane = (size_t)(gridDim.x / C) * p.cols;
     A *const line = static_cast<A *>(p.partial) + (size_t)(blockIdx.x / C) * p.cols;
     const int threads = T > 0 ? T : p.group;
-    for (int i = threadIdx.x; i < threads * E; i += cta) {
-        const int t = i / V % threads, k = i / (V * threads) * V + i % V;
+    for (int i = threadIdx.x; i < threads * n_slots * Sums::kPieces; i += cta) {
+        const int t = i % threads, piece = i / threads % Sums::kPieces, s = i / threads / Sums::kPieces;
+        typename Sums::Piece v = Sums::at(sums + s * cta * E, t, piece);
+#pragma unroll 4
+        for (int g = 1; g < groups; ++g) {
+            const typename Sums::Piece more = Sums::at(sums + s * cta * E, g * threads + t, piece);
+#pragma unroll
+            for (int e = 0; e < Sums::kValues / 2; ++e) v.v[e] = v.v[e] + more.v[e];
+        }
         const Columns<T, V> own = {t + (C > 1 ? (int)cluster_rank() * threads : 0), p.cols, c.count};
-        const int j = own.of(k);
-        if (j >= p.cols) continue;
-        for (int s = 0; s < n_slots; ++s) {
-            A v = A(0);
-            for (int g = 0; g < groups; ++g) v += Sums::read(sums + s * cta * E, g * threads + t, k);
-            line[s * plane + j] = v;
+#pragma unroll
+        for (int e = 0; e < Sums::kValues; ++e) {
+            const int j = own.of(piece * Sums::kValues + e);
+            if (j < p.cols) line[s * plane + j] = e & 1 ? second(v.v[e / 2]) : first(v.v[e / 2]);
         }
     }
 }

@@ -40,6 +40,30 @@ cudaError_t with_row_shape(int cols, Go go)
 #undef FO_SHAPE
 }
 
+// The same for the gradient: 8 elements a thread, for more threads (32768 x 1024 mixed 153 us, with 16 elements 165;
+// 8192 x 5120 252 us, with 16 290).  Beyond 8192 columns that takes clusters of 4 and 8, and 16 elements are better
+// where half as many threads nearly fill an SM's 512 (16384 columns: 236 us, with 8 374; 20000: 577, with 8 417).
+template <int V, class Go>
+cudaError_t with_grad_shape(int cols, Go go)
+{
+#define FO_SHAPE(t, c, e, n) \
+    go(std::integral_constant<int, t>(), std::integral_constant<int, c>(), std::integral_constant<int, e>(), n)
+    if (cols <= 64) return FO_SHAPE(8, 1, 8, kGroupCta);
+    if (cols <= 128) return FO_SHAPE(16, 1, 8, kGroupCta);
+    if (cols <= 256) return FO_SHAPE(32, 1, 8, kGroupCta);
+    const int pieces = (cols + V - 1) / V;
+    auto threads = [&](int c, int e) { return ((pieces + e / V * c - 1) / (e / V * c) + 31) / 32 * 32; };
+    if (cols <= 4096) return FO_SHAPE(0, 1, 8, threads(1, 8));
+    if (cols <= 8192) return FO_SHAPE(0, 2, 8, threads(2, 8));
+    if (cols <= 16384) {
+        if (threads(2, 16) >= 448) return FO_SHAPE(0, 2, 16, threads(2, 16));
+        return FO_SHAPE(0, 4, 8, threads(4, 8));
+    }
+    if (threads(4, 16) >= 448) return FO_SHAPE(0, 4, 16, threads(4, 16));
+    return FO_SHAPE(0, 8, 8, threads(8, 8));
+#undef FO_SHAPE
+}
+
 #ifdef FO_BLOCK_NORM_DEFINE
 template <class Params>
 cudaError_t launch_rows(void (*kern)(Params), const Params &p, long long grid, int cta, int cluster, size_t smem,
@@ -102,7 +126,7 @@ cudaError_t grad_residency(int cta, int sums, size_t sum_bytes, int *per_sm)
 template <class TS, class TB>
 cudaError_t launch_block_norm_grad(BlockNormGradParams p, GradSpace *space, cudaStream_t st)
 {
-    return with_row_shape<16 / (int)sizeof(TB)>(p.cols, [&](auto tc, auto cc, auto ec, int cta) -> cudaError_t {
+    return with_grad_shape<16 / (int)sizeof(TB)>(p.cols, [&](auto tc, auto cc, auto ec, int cta) -> cudaError_t {
         constexpr int T = decltype(tc)::value, C = decltype(cc)::value, E = decltype(ec)::value;
         constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
         auto go = [&](auto aligned, auto blk) -> cudaError_t {

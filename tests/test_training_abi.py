@@ -1,12 +1,15 @@
 """Refusals of the training-step operators: found on the host, before anything is launched (no GPU needed)."""
 import math
+import struct
 
 import pytest
 import torch
 
 import paper_1801_00829_b200 as fo
-from paper_1801_00829_b200 import training as T
 
+# fo_block_norm and fo_block_norm_grad, field by field
+BLOCK_NORM = struct.Struct("qq6i4Q3qd" + "iidQQ" * 2 + "3Q2q")
+BLOCK_NORM_GRAD = struct.Struct("qq6i7Q5qd" + "iidQQ" * 2 + "3Q3q5Q")
 NONE = (0, 0, 0.0, 0, 0)
 RMS = (1, 0, 1e-6, 0x9000, 0)
 F64, F32, BF16, F16 = 0, 1, 2, 3
@@ -19,7 +22,7 @@ def lib():
 
 def norm(lib, rows=4, cols=64, types=(BF16, BF16, BF16), access=0, act=0, x=0x1000, f=0x2000, gate=0, col_scale=0,
          ld=(64, 64, 64), post=RMS, pre=RMS, h=0x3000, y=0x4000, stats=0, ld_out=(64, 64)):
-    return lib.fused_block_norm(T._BLOCK_NORM.pack(rows, cols, *types, access, act, 0, x, f, gate, col_scale, *ld, 1.0, *post,
+    return lib.fused_block_norm(BLOCK_NORM.pack(rows, cols, *types, access, act, 0, x, f, gate, col_scale, *ld, 1.0, *post,
                                                    *pre, h, y, stats, *ld_out), None)
 
 
@@ -49,7 +52,7 @@ def test_block_norm_refusals(lib):
 def grad(lib, rows=4, cols=64, types=(BF16, BF16, BF16), access=0, act=0, dh=0x1000, dy=0x1100, h=0x1200, f=0x1300, gate=0,
          col_scale=0, stats=0x1400, ld=(64,) * 5, post=RMS, pre=RMS, dx=0x1500, df=0x1600, dgate=0, ld_out=(64,) * 3,
          sums=(0, 0, 0, 0, 0), ws=0x10000, ws_bytes=1 << 30):
-    return lib.fused_block_norm_grad(T._BLOCK_NORM_GRAD.pack(rows, cols, *types, access, act, 0, dh, dy, h, f, gate, col_scale,
+    return lib.fused_block_norm_grad(BLOCK_NORM_GRAD.pack(rows, cols, *types, access, act, 0, dh, dy, h, f, gate, col_scale,
                                                              stats, *ld, 1.0, *post, *pre, dx, df, dgate, *ld_out, *sums),
                                      ws, ws_bytes, None)
 
@@ -77,7 +80,6 @@ def test_block_norm_grad_refusals(lib):
 
 
 def test_many_tensor_refusals(lib):
-    import struct
     one = struct.pack("QQq", 0x1000, 0x2000, 10)
     ws, big = 0x10000, 1 << 20
     norm_ = lambda t=one, n=1, it=F32, kind=0, mx=1.0, eps=0.0, res=0x3000, rt=F32, w=ws, wb=big: lib.fused_grad_norm(  # noqa: E731
