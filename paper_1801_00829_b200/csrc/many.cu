@@ -1,9 +1,11 @@
 // Operators over many tensors in one launch: the global gradient norm, clipping by it, and AdamW.
 //
 // The tensors' addresses and sizes travel as kernel parameters (no device table, nothing kept between
-// calls); a longer list takes several launches.  All tensors together are one line of tiles of kTile
-// elements, each CTA takes an equal, contiguous share of it and walks from tensor to tensor.  Inside a
-// tile the elements before the first 16-byte boundary and after the last whole piece are handled singly.
+// calls); a longer list takes several launches.  All tensors together are one line of tiles, of which each
+// CTA takes every gridDim-th: at any time the GPU works on one stretch of every stream, not on
+// one per CTA and stream.  Tiles begin where pieces are aligned; the elements of a tensor before the first
+// piece and after the last are handled singly.  What is written decides the pieces' alignment; what is read at
+// another one is put together from aligned 16 bytes.
 #include <math.h>
 
 #include "elem.cuh"
@@ -12,8 +14,14 @@ namespace fo {
 namespace {
 
 constexpr int kCta = 256;
-constexpr int kTile = 8192;                  // elements; a multiple of every piece
-constexpr int kCtasPerSm = 4;
+// Elements of a tile, and CTAs per SM.  Small tiles, so that 3 million elements still fill the SMs; of AdamW, one
+// piece of 8 per thread, seven or eight streams of it.
+constexpr int kTile = 4096, kCtasPerSm = 8;
+constexpr int kAdamTile = 2048, kAdamCtasPerSm = 4;
+
+// Kernel 2 of a pair is launched while kernel 1 runs, and waits for its results here.
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_later_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ------------------------------------------------------------------- lists
 template <int N>
@@ -58,28 +66,30 @@ __device__ __forceinline__ int tensor_of(const List &l, unsigned t)
     return lo;
 }
 
-// Elements of a tile by their place: `lead` single ones, `pieces` whole pieces of V, and the rest singly.
+// A tile of a tensor: `pieces` aligned pieces of V elements from element `at`, `head` single ones from the
+// tensor's beginning (its first tile) and `tail` behind the pieces (its last).  The host counts tiles without
+// the head, so a last tile may be empty.
 struct Cut {
-    int lead, pieces, len;
+    long long at;
+    int pieces, head, tail;
+    __device__ __forceinline__ long long single(int i, int v) const      // element of single number i, -1: none
+    {
+        return i < head ? i : i - head < tail ? at + (long long)pieces * v + (i - head) : -1;
+    }
 };
-template <int V>
-__device__ __forceinline__ Cut cut_tile(const void *p, int bytes, long long left)
+template <int V, int TILE>
+__device__ __forceinline__ Cut cut_tile(const void *p, int bytes, long long n, unsigned tile, int align = V)
 {
+    const int mis = (int)(((uintptr_t)p / bytes) & (align - 1));
+    const long long lead = min((long long)((align - mis) & (align - 1)), n);
     Cut c;
-    c.len = left < kTile ? (int)left : kTile;
-    const int mis = (int)(((uintptr_t)p / bytes) & (V - 1));
-    c.lead = (V - mis) & (V - 1);
-    if (c.lead > c.len) c.lead = c.len;
-    c.pieces = (c.len - c.lead) / V;
+    c.at = lead + (long long)tile * TILE;
+    const long long left = n - c.at;
+    const int len = left < TILE ? (left > 0 ? (int)left : 0) : TILE;
+    c.pieces = len / V;
+    c.head = tile == 0 ? (int)lead : 0;
+    c.tail = len - c.pieces * V;
     return c;
-}
-// Single element number i of a tile (fewer than 2 V of them), or -1.
-template <int V>
-__device__ __forceinline__ int single(const Cut &c, int i)
-{
-    if (i < c.lead) return i;
-    const int e = i + c.pieces * V;
-    return e < c.len ? e : -1;
 }
 
 // -------------------------------------------------------------------- norm
@@ -150,35 +160,30 @@ __device__ __forceinline__ double cta_join(double v, double *smem)     // result
 }
 
 template <class T, int N, int KIND>
-__global__ void __launch_bounds__(kCta) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
+__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kCtasPerSm) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    constexpr int kBatch = 4;                // pieces of a thread in flight
+    constexpr int kBatch = kTile / kCta / V > 0 ? kTile / kCta / V : 1;      // pieces of a thread in a tile
     __shared__ double smem[kCta / 32];
     __shared__ unsigned s_flag;
-    const unsigned lo = (unsigned)((unsigned long long)l.tiles * blockIdx.x / gridDim.x);
-    const unsigned hi = (unsigned)((unsigned long long)l.tiles * (blockIdx.x + 1) / gridDim.x);
     double acc = 0.0;
-    int k = lo < hi ? tensor_of(l, lo) : 0;
-    for (unsigned t = lo; t < hi; ++t) {
-        while (t >= l.first[k + 1]) ++k;
-        const long long at = (long long)(t - l.first[k]) * kTile;
-        const T *p = static_cast<const T *>(l.in[k]) + at;
-        const Cut c = cut_tile<V>(p, sizeof(T), l.n[k] - at);
-        for (int i0 = threadIdx.x; i0 < c.pieces; i0 += kBatch * kCta) {
-            Packed<T, V * kBatch> r;
-            r.clear();
+    for (unsigned t = blockIdx.x; t < l.tiles; t += gridDim.x) {
+        const int k = tensor_of(l, t);
+        const T *p = static_cast<const T *>(l.in[k]);
+        const Cut c = cut_tile<V, kTile>(p, sizeof(T), l.n[k], t - l.first[k]);
+        Packed<T, V * kBatch> r;
+        r.clear();
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (i0 + b * kCta < c.pieces) load16(r.w + 4 * b, p + c.lead + (i0 + b * kCta) * V);
-            acc = join<KIND>(acc, KIND == FO_NORM_L2 ? sum_squares<T>(r) : max_magnitude<T>(r));
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = threadIdx.x + b * kCta;
+            if (i < c.pieces) load16(r.w + 4 * b, p + c.at + i * V);
         }
-        const int e = single<V>(c, threadIdx.x);
-        if (e >= 0) {
-            const double g = (double)widen<T>(p[e]);
-            acc = join<KIND>(acc, KIND == FO_NORM_L2 ? g * g : fabs(g));
-        }
+        const long long e = c.single(threadIdx.x, V);
+        const double g = e >= 0 ? (double)widen<T>(p[e]) : 0.0;
+        acc = join<KIND>(acc, KIND == FO_NORM_L2 ? sum_squares<T>(r) : max_magnitude<T>(r));
+        if (e >= 0) acc = join<KIND>(acc, KIND == FO_NORM_L2 ? g * g : fabs(g));
     }
+    let_later_start();                                       // its CTAs wait for this kernel's end
     acc = cta_join<KIND>(acc, smem);
     if (threadIdx.x == 0) o.partial[blockIdx.x] = acc;
     if (!publish_and_is_last(o.head, &s_flag)) return;
@@ -204,43 +209,37 @@ __global__ void __launch_bounds__(kCta) grad_norm_kernel(const __grid_constant__
 }
 
 // -------------------------------------------------------------------- clip
-// V elements from any address: one load where it is aligned for it, else one by one (neighbouring
-// threads' elements share sectors, which L1 keeps).
+// V elements (16 or 32 bytes, or 64 of float64 beside float32) of a tensor that lies in [begin, end): whole 16 bytes
+// where they are aligned, else put together.
 template <class T, int V>
-__device__ __forceinline__ void load_some(Acc<T> (&o)[V], const T *p, bool aligned)
+__device__ __forceinline__ void load_some(Packed<T, V> &r, const T *p, bool aligned, const T *begin, const T *end)
 {
-    constexpr int kBytes = V * (int)sizeof(T);
-    if (aligned) {
-        Packed<T, V> r;
-        if constexpr (kBytes == 16) load16(r.w, p);
-        else asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+    constexpr int kStep = 16 / (int)sizeof(T);
 #pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = r.get(k);
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) o[k] = widen<T>(p[k]);
+    for (int k = 0; k < V; k += kStep) {
+        if (aligned) load16(r.w + k * (int)sizeof(T) / 4, p + k);
+        else load16_any(r.w + k * (int)sizeof(T) / 4, p + k, begin, end);
     }
 }
 template <class T, int V>
 __device__ __forceinline__ void store_some(T *p, const Acc<T> (&v)[V], bool aligned)
 {
-    constexpr int kBytes = V * (int)sizeof(T);
+    constexpr int kStep = 16 / (int)sizeof(T);
     if (aligned) {
         Packed<T, V> r;
-        r.clear();
 #pragma unroll
-        for (int k = 0; k < V; ++k) r.put(k, narrow<T>(v[k]));
-        if constexpr (kBytes == 16) store16(p, r.w);
-        else asm volatile("st.global.v2.u32 [%0], {%1, %2};" ::"l"(p), "r"(r.w[0]), "r"(r.w[1]) : "memory");
+        for (int k = 0; k < V; k += 2) r.put2(k, two(v[k], v[k + 1]));
+#pragma unroll
+        for (int k = 0; k < V; k += kStep) store16(p + k, r.w + k * (int)sizeof(T) / 4);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) p[k] = narrow<T>(v[k]);
     }
 }
-template <class T, int V>
-__device__ __forceinline__ bool aligned_for(const T *p)
+template <class T>
+__device__ __forceinline__ bool aligned16(const T *p)
 {
-    return ((uintptr_t)p & (V * sizeof(T) - 1)) == 0;
+    return ((uintptr_t)p & 15u) == 0;
 }
 
 __device__ __forceinline__ double read_factor(const void *factor, int type)
@@ -248,43 +247,52 @@ __device__ __forceinline__ double read_factor(const void *factor, int type)
     return type == FO_F64 ? *static_cast<const double *>(factor) : (double)*static_cast<const float *>(factor);
 }
 
-// Pieces of 4 elements (2 of float64), aligned for the output: single stores would reach L2 in parts.
+// The tiles in the opposite order of the norm's: what it read last is still in L2.
 template <class TI, class TO, int N>
-__global__ void __launch_bounds__(kCta) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
+__global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kCtasPerSm) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
                                                     int result_type)
 {
     using A = Acc<TI>;
-    constexpr int V = sizeof(A) == 8 ? 2 : 4;
-    constexpr int kBatch = 4;
-    const double wide = result_type == FO_F64 ? static_cast<const double *>(result)[1]
-                                              : (double)static_cast<const float *>(result)[1];
-    const A factor = (A)wide;
-    const unsigned lo = (unsigned)((unsigned long long)l.tiles * blockIdx.x / gridDim.x);
-    const unsigned hi = (unsigned)((unsigned long long)l.tiles * (blockIdx.x + 1) / gridDim.x);
-    int k = lo < hi ? tensor_of(l, lo) : 0;
-    for (unsigned t = lo; t < hi; ++t) {
-        while (t >= l.first[k + 1]) ++k;
-        const long long at = (long long)(t - l.first[k]) * kTile;
-        const TI *p = static_cast<const TI *>(l.in[k]) + at;
-        TO *q = static_cast<TO *>(l.out[k]) + at;
-        if ((const void *)p == (const void *)q && factor == A(1)) continue;
-        const Cut c = cut_tile<V>(q, sizeof(TO), l.n[k] - at);
-        const bool in_ok = aligned_for<TI, V>(p + c.lead), out_ok = aligned_for<TO, V>(q + c.lead);
-        for (int i0 = threadIdx.x; i0 < c.pieces; i0 += kBatch * kCta) {
-            A g[kBatch][V];
+    constexpr int V = 16 / (int)sizeof(TI);
+    constexpr int kBatch = kTile / kCta / V > 0 ? kTile / kCta / V : 1;
+    A factor = A(0);
+    bool known = false;
+    for (unsigned u = blockIdx.x; u < l.tiles; u += gridDim.x) {
+        const unsigned t = l.tiles - 1u - u;
+        const int k = tensor_of(l, t);
+        const TI *begin = static_cast<const TI *>(l.in[k]);
+        const long long n = l.n[k];
+        TO *out = static_cast<TO *>(l.out[k]);
+        constexpr int kAlign = 16 / (int)sizeof(TO) < V ? 16 / (int)sizeof(TO) : V;
+        const Cut c = cut_tile<V, kTile>(out, sizeof(TO), n, t - l.first[k], kAlign);
+        const TI *p = begin + c.at;
+        TO *q = out + c.at;
+        const bool in_ok = aligned16(p);
+        Packed<TI, V> g[kBatch];
 #pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-                if (i0 + b * kCta < c.pieces) load_some<TI, V>(g[b], p + c.lead + (i0 + b * kCta) * V, in_ok);
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                if (i0 + b * kCta >= c.pieces) continue;
-#pragma unroll
-                for (int e = 0; e < V; ++e) g[b][e] *= factor;
-                store_some<TO, V>(q + c.lead + (i0 + b * kCta) * V, g[b], out_ok);
-            }
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = threadIdx.x + b * kCta;
+            if (i < c.pieces) load_some<TI, V>(g[b], p + i * V, in_ok, begin, begin + n);
         }
-        const int e = single<V>(c, threadIdx.x);
-        if (e >= 0) q[e] = narrow<TO>(widen<TI>(p[e]) * factor);
+        const long long e = c.single(threadIdx.x, V);
+        const A one = e >= 0 ? widen<TI>(begin[e]) : A(0);
+        if (!known) {                                        // the first tile was on its way meanwhile
+            wait_for_earlier();
+            factor = (A)(result_type == FO_F64 ? static_cast<const double *>(result)[1]
+                                               : (double)static_cast<const float *>(result)[1]);
+            known = true;
+        }
+        if ((const void *)begin == (const void *)out && factor == A(1)) continue;
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int i = threadIdx.x + b * kCta;
+            if (i >= c.pieces) continue;
+            A v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = g[b].get(e) * factor;
+            store_some<TO, V>(q + i * V, v, true);
+        }
+        if (e >= 0) out[e] = narrow<TO>(one * factor);
     }
 }
 
@@ -306,50 +314,50 @@ __device__ __forceinline__ void adam_one(A &p, A g, A &m, A &v, A c, A b1, A b2,
     p = p - lr * fused_ma(decay, p, step);
 }
 
+// Pieces of 8 elements (2 of float64): two 16-byte loads of each 32-bit tensor are in flight at once.
 template <class TG, class TW, int N>
 __global__ void __launch_bounds__(kCta) adamw_kernel(const __grid_constant__ AdamList<N> l, const AdamHyper h)
 {
     using A = Acc<TG>;
-    constexpr int V = sizeof(A) == 8 ? 2 : 4;
+    constexpr int V = sizeof(A) == 8 ? 2 : 8;
     const A c = h.factor ? (A)read_factor(h.factor, h.factor_type) : A(1);
     const A b1 = (A)h.beta1, b2 = (A)h.beta2, u1 = (A)(1.0 - h.beta1), u2 = (A)(1.0 - h.beta2);
     const A fix1 = (A)h.fix1, fix2 = (A)h.fix2, eps = (A)h.eps, lr = (A)h.lr;
-    const unsigned lo = (unsigned)((unsigned long long)l.tiles * blockIdx.x / gridDim.x);
-    const unsigned hi = (unsigned)((unsigned long long)l.tiles * (blockIdx.x + 1) / gridDim.x);
-    int k = lo < hi ? tensor_of(l, lo) : 0;
-    for (unsigned t = lo; t < hi; ++t) {
-        while (t >= l.first[k + 1]) ++k;
-        const long long at = (long long)(t - l.first[k]) * kTile;
-        const A *p = static_cast<const A *>(l.p[k]) + at, *m = static_cast<const A *>(l.m[k]) + at,
-                *v = static_cast<const A *>(l.v[k]) + at;
-        const TG *g = static_cast<const TG *>(l.g[k]) + at;
-        A *po = static_cast<A *>(l.p_out[k]) + at, *mo = static_cast<A *>(l.m_out[k]) + at,
-          *vo = static_cast<A *>(l.v_out[k]) + at;
-        TW *wo = l.weights[k] ? static_cast<TW *>(l.weights[k]) + at : nullptr;
+    for (unsigned t = blockIdx.x; t < l.tiles; t += gridDim.x) {
+        const int k = tensor_of(l, t);
+        const long long n = l.n[k];
+        const A *p = static_cast<const A *>(l.p[k]), *m = static_cast<const A *>(l.m[k]), *v = static_cast<const A *>(l.v[k]);
+        const TG *g = static_cast<const TG *>(l.g[k]);
+        A *po = static_cast<A *>(l.p_out[k]), *mo = static_cast<A *>(l.m_out[k]), *vo = static_cast<A *>(l.v_out[k]);
+        TW *wo = static_cast<TW *>(l.weights[k]);
         const A decay = (A)l.decay[k];
-        const Cut cut = cut_tile<V>(po, sizeof(A), l.n[k] - at);
-        const int d = cut.lead;
-        const bool p_ok = aligned_for<A, V>(p + d), g_ok = aligned_for<TG, V>(g + d), m_ok = aligned_for<A, V>(m + d),
-                   v_ok = aligned_for<A, V>(v + d), po_ok = aligned_for<A, V>(po + d), mo_ok = aligned_for<A, V>(mo + d),
-                   vo_ok = aligned_for<A, V>(vo + d), wo_ok = aligned_for<TW, V>(wo + d);
+        const Cut cut = cut_tile<V, kAdamTile>(po, sizeof(A), n, t - l.first[k]);
+        const long long d = cut.at;
+        const bool p_ok = aligned16(p + d), g_ok = aligned16(g + d), m_ok = aligned16(m + d), v_ok = aligned16(v + d),
+                   mo_ok = aligned16(mo + d), vo_ok = aligned16(vo + d), wo_ok = aligned16(wo + d);
+#pragma unroll 1
         for (int i = threadIdx.x; i < cut.pieces; i += kCta) {
-            const int e0 = d + i * V;
-            A rp[V], rg[V], rm[V], rv[V];
-            load_some<A, V>(rp, p + e0, p_ok);
-            load_some<TG, V>(rg, g + e0, g_ok);
-            load_some<A, V>(rm, m + e0, m_ok);
-            load_some<A, V>(rv, v + e0, v_ok);
+            const long long e0 = d + i * V;
+            Packed<A, V> qp, qm, qv;
+            Packed<TG, V> qg;
+            load_some<A, V>(qp, p + e0, p_ok, p, p + n);
+            load_some<TG, V>(qg, g + e0, g_ok, g, g + n);
+            load_some<A, V>(qm, m + e0, m_ok, m, m + n);
+            load_some<A, V>(qv, v + e0, v_ok, v, v + n);
+            A rp[V], rm[V], rv[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                adam_one<A>(rp[e], rg[e], rm[e], rv[e], c, b1, b2, u1, u2, fix1, fix2, eps, lr, decay);
-            store_some<A, V>(po + e0, rp, po_ok);
+            for (int e = 0; e < V; ++e) {
+                rp[e] = qp.get(e), rm[e] = qm.get(e), rv[e] = qv.get(e);
+                adam_one<A>(rp[e], qg.get(e), rm[e], rv[e], c, b1, b2, u1, u2, fix1, fix2, eps, lr, decay);
+            }
+            store_some<A, V>(po + e0, rp, true);
             store_some<A, V>(mo + e0, rm, mo_ok);
             store_some<A, V>(vo + e0, rv, vo_ok);
             if constexpr (sizeof(TW) == 2) {
                 if (wo) store_some<TW, V>(wo + e0, rp, wo_ok);
             }
         }
-        const int e = single<V>(cut, threadIdx.x);
+        const long long e = cut.single(threadIdx.x, V);
         if (e >= 0) {
             A rp = p[e], rm = m[e], rv = v[e];
             adam_one<A>(rp, widen<TG>(g[e]), rm, rv, c, b1, b2, u1, u2, fix1, fix2, eps, lr, decay);
@@ -364,17 +372,17 @@ __global__ void __launch_bounds__(kCta) adamw_kernel(const __grid_constant__ Ada
 // -------------------------------------------------------------------- host
 constexpr int kFew = 40, kMany = 512, kManyAdam = 256;      // tensors of one launch: the parameters fit 32 KB
 
-unsigned tiles_of(long long n) { return (unsigned)((n + kTile - 1) / kTile); }
+unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
 
-unsigned grid_for(unsigned tiles)
+unsigned grid_for(unsigned tiles, int per_sm)
 {
-    const unsigned cap = (unsigned)(sm_count() * kCtasPerSm);
+    const unsigned cap = (unsigned)(sm_count() * per_sm);
     return tiles < cap ? (tiles ? tiles : 1u) : cap;
 }
 
 bool float_type(int t) { return t >= FO_F64 && t <= FO_F16; }
 
-// Sizes and addresses of a list; the tiles of all its tensors have to fit 31 bits (1.7e13 elements).
+// Sizes and addresses of a list; the tiles of all its tensors have to fit 31 bits (4e12 elements).
 template <class Tensor, class Bad>
 int check_list(const Tensor *t, int count, Bad bad)
 {
@@ -384,7 +392,7 @@ int check_list(const Tensor *t, int count, Bad bad)
     for (int k = 0; k < count; ++k) {
         if (t[k].n < 0) return FO_ERR_SHAPE;
         if (t[k].n > 0 && bad(t[k])) return FO_ERR_NULL;
-        tiles += (unsigned long long)(t[k].n / kTile + 1);
+        tiles += (unsigned long long)(t[k].n / kAdamTile + 1);
     }
     return tiles < (1ULL << 31) ? FO_OK : FO_ERR_UNSUPPORTED;
 }
@@ -396,10 +404,10 @@ cudaError_t launch_norm_part(const fo_tensor *t, int count, int kind, const Norm
     l.count = count, l.tiles = 0;
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.n[k] = t[k].n;
-        l.tiles += tiles_of(t[k].n);
+        l.tiles += tiles_of(t[k].n, kTile);
     }
     l.first[count] = l.tiles;
-    const unsigned grid = grid_for(l.tiles);
+    const unsigned grid = grid_for(l.tiles, kCtasPerSm);
     if (kind == FO_NORM_L2) grad_norm_kernel<T, N, FO_NORM_L2><<<grid, kCta, 0, st>>>(l, o);
     else grad_norm_kernel<T, N, FO_NORM_MAX><<<grid, kCta, 0, st>>>(l, o);
     return cudaGetLastError();
@@ -429,12 +437,20 @@ cudaError_t launch_clip_part(const fo_tensor *t, int count, const void *result, 
     l.count = count, l.tiles = 0;
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.out[k] = t[k].out, l.n[k] = t[k].n;
-        l.tiles += tiles_of(t[k].n);
+        l.tiles += tiles_of(t[k].n, kTile);
     }
     l.first[count] = l.tiles;
     if (l.tiles == 0) return cudaSuccess;
-    clip_kernel<TI, TO, N><<<grid_for(l.tiles), kCta, 0, st>>>(l, result, result_type);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid_for(l.tiles, kCtasPerSm));
+    cfg.blockDim = dim3(kCta);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, clip_kernel<TI, TO, N>, l, result, result_type);
 }
 
 template <class TI, class TO>
@@ -459,11 +475,11 @@ cudaError_t launch_adam_part(const fo_adam_tensor *t, int count, const AdamHyper
         l.p[k] = t[k].p, l.g[k] = t[k].g, l.m[k] = t[k].m, l.v[k] = t[k].v;
         l.p_out[k] = t[k].p_out, l.m_out[k] = t[k].m_out, l.v_out[k] = t[k].v_out, l.weights[k] = t[k].weights;
         l.n[k] = t[k].n, l.decay[k] = t[k].decay;
-        l.tiles += tiles_of(t[k].n);
+        l.tiles += tiles_of(t[k].n, kAdamTile);
     }
     l.first[count] = l.tiles;
     if (l.tiles == 0) return cudaSuccess;
-    adamw_kernel<TG, TW, N><<<grid_for(l.tiles), kCta, 0, st>>>(l, h);
+    adamw_kernel<TG, TW, N><<<grid_for(l.tiles, kAdamCtasPerSm), kCta, 0, st>>>(l, h);
     return cudaGetLastError();
 }
 
