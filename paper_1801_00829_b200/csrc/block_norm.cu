@@ -43,12 +43,15 @@ NormSpec spec_of(const fo_norm &n)
     return s;
 }
 
-// Collects whether every row of every matrix, and every vector, can move in 16-byte pieces.
+// Collects whether every row of every matrix can move in pieces (16 bytes of the block's type, the same number
+// of elements of the stream's), and every vector in 16 bytes.
 struct Pieces {
     bool ok;
+    int block_bytes;
     void matrix(const void *p, long long ld, int type)
     {
-        if (p) ok = ok && ((uintptr_t)p & 15u) == 0 && (ld * elem_bytes(type)) % 16 == 0;
+        const int piece = 16 * elem_bytes(type) / block_bytes;
+        if (p) ok = ok && ((uintptr_t)p & (unsigned)(piece - 1)) == 0 && (ld * elem_bytes(type)) % piece == 0;
     }
     void vector(const void *p) { ok = ok && ((uintptr_t)p & 15u) == 0; }
     void norm(const fo_norm &n)
@@ -129,7 +132,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
     p.scale = a->scale;
     p.post = spec_of(a->post), p.pre = spec_of(a->pre);
     p.h = a->h, p.y = a->y, p.stats = a->stats;
-    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0};
+    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0, elem_bytes(a->block_type)};
     all.matrix(a->x, a->ld_x, a->stream_type);
     all.matrix(a->h, a->ld_h, a->stream_type);
     all.matrix(a->f, a->ld_f, a->block_type);
@@ -201,7 +204,7 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     p.dx = a->dx, p.df = a->df, p.dgate = p.gate_access == FO_AT_COL ? nullptr : a->dgate;
     p.ld_dx = a->ld_dx, p.ld_df = a->ld_df, p.ld_dgate = a->ld_dgate;
     p.partial = static_cast<char *>(ws) + sizeof(WsHead);
-    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0};
+    Pieces all = {a->cols % (16 / elem_bytes(a->block_type)) == 0, elem_bytes(a->block_type)};
     all.matrix(a->dh, a->ld_dh, a->stream_type);
     all.matrix(a->dx, a->ld_dx, a->stream_type);
     if (pre) all.matrix(a->h, a->ld_h, a->stream_type), all.matrix(a->dy, a->ld_dy, a->block_type);

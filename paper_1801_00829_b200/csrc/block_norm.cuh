@@ -59,8 +59,8 @@ struct BlockNormGradParams {
 };
 
 // Which columns a thread holds: pieces of V elements, 16 bytes of the block's type.  Piece v of thread t covers
-// columns (v * threads + t) * V .. + V - 1.  ALIGNED: every row of every matrix begins on a 16-byte boundary
-// and is whole pieces long; else rows may begin and end anywhere, and 16 bytes that straddle a boundary are
+// columns (v * threads + t) * V .. + V - 1.  ALIGNED: every row of every matrix begins where a piece may (a
+// 16-byte boundary, 32 for a stream of wider elements) and is whole pieces long; else rows may begin and end anywhere, and 16 bytes that straddle a boundary are
 // put together from the two aligned 16 bytes they lie in.  Values outside the row are held as zeros.
 template <int T, int V>                        // T: threads of the row, 0: the CTAs' threads
 struct Columns {
@@ -83,6 +83,16 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
 {
     const TE *begin = static_cast<const TE *>(base), *p = begin + row * ld;
     constexpr int kStep = 16 / (int)sizeof(TE);
+    if constexpr (ALIGNED && V == 2 * kStep) {               // a float stream beside a block of 16 bits
+#pragma unroll
+        for (int k = 0; k < E; k += V) {
+            uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 0u;
+            if (row_ok && c.of(k) < c.cols) load32(w, p + c.of(k));
+        }
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < E; k += kStep) {
         uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
@@ -127,7 +137,11 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
 {
     TE *p = static_cast<TE *>(base) + row * ld;
     constexpr int kStep = 16 / (int)sizeof(TE), kWords = (int)sizeof(TE);      // kWords / 4 words per element
-    if constexpr (ALIGNED) {
+    if constexpr (ALIGNED && V == 2 * kStep) {
+#pragma unroll
+        for (int k = 0; k < E; k += V)
+            if (ok && c.of(k) < c.cols) store32(p + c.of(k), v.w + k * kWords / 4);
+    } else if constexpr (ALIGNED) {
 #pragma unroll
         for (int k = 0; k < E; k += kStep)
             if (ok && c.of(k) < c.cols) store16(p + c.of(k), v.w + k * kWords / 4);

@@ -14,10 +14,10 @@ namespace fo {
 namespace {
 
 constexpr int kCta = 256;
-// Elements of a tile, and CTAs per SM.  Small tiles, so that 3 million elements still fill the SMs; of AdamW, one
-// piece of 8 per thread, seven or eight streams of it.
-constexpr int kTile = 4096, kCtasPerSm = 8;
-constexpr int kAdamTile = 2048, kAdamCtasPerSm = 4;
+// A tile is 1 to 4 times kTile elements: small enough that a short list still fills the SMs, large enough that
+// finding a tile's tensor and addresses costs a long list little (AdamW over 25M, 50M and 130M parameters in up to 72
+// tensors: 119, 235 and 614 us with twice kTile, 122, 233 and 606 with 4 times, 124, 243 and 605 with 8 times).
+constexpr int kTile = 2048, kMostTile = 4 * kTile;
 
 // Kernel 2 of a pair is launched while kernel 1 runs, and waits for its results here.
 __device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -28,6 +28,7 @@ template <int N>
 struct NormList {
     int count;
     unsigned tiles;
+    int tile;                                // elements of one
     unsigned first[N + 1];                   // first tile of each tensor
     const void *in[N];
     long long n[N];
@@ -36,6 +37,7 @@ template <int N>
 struct ClipList {
     int count;
     unsigned tiles;
+    int tile;                                // elements of one
     unsigned first[N + 1];
     const void *in[N];
     void *out[N];
@@ -45,6 +47,7 @@ template <int N>
 struct AdamList {
     int count;
     unsigned tiles;
+    int tile;                                // elements of one
     unsigned first[N + 1];
     const void *p[N], *g[N], *m[N], *v[N];
     void *p_out[N], *m_out[N], *v_out[N], *weights[N];
@@ -77,15 +80,15 @@ struct Cut {
         return i < head ? i : i - head < tail ? at + (long long)pieces * v + (i - head) : -1;
     }
 };
-template <int V, int TILE>
-__device__ __forceinline__ Cut cut_tile(const void *p, int bytes, long long n, unsigned tile, int align = V)
+template <int V>
+__device__ __forceinline__ Cut cut_tile(const void *p, int bytes, long long n, unsigned tile, int size)
 {
-    const int mis = (int)(((uintptr_t)p / bytes) & (align - 1));
-    const long long lead = min((long long)((align - mis) & (align - 1)), n);
+    const int mis = (int)(((uintptr_t)p / bytes) & (V - 1));
+    const long long lead = min((long long)((V - mis) & (V - 1)), n);
     Cut c;
-    c.at = lead + (long long)tile * TILE;
+    c.at = lead + (long long)tile * size;
     const long long left = n - c.at;
-    const int len = left < TILE ? (left > 0 ? (int)left : 0) : TILE;
+    const int len = left < size ? (left > 0 ? (int)left : 0) : size;
     c.pieces = len / V;
     c.head = tile == 0 ? (int)lead : 0;
     c.tail = len - c.pieces * V;
@@ -160,27 +163,27 @@ __device__ __forceinline__ double cta_join(double v, double *smem)     // result
 }
 
 template <class T, int N, int KIND>
-__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kCtasPerSm) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
+__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : 6) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    constexpr int kBatch = kTile / kCta / V > 0 ? kTile / kCta / V : 1;      // pieces of a thread in a tile
+    constexpr int kBatch = 4;                // pieces of a thread in flight
     __shared__ double smem[kCta / 32];
     __shared__ unsigned s_flag;
     double acc = 0.0;
     for (unsigned t = blockIdx.x; t < l.tiles; t += gridDim.x) {
         const int k = tensor_of(l, t);
         const T *p = static_cast<const T *>(l.in[k]);
-        const Cut c = cut_tile<V, kTile>(p, sizeof(T), l.n[k], t - l.first[k]);
-        Packed<T, V * kBatch> r;
-        r.clear();
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int i = threadIdx.x + b * kCta;
-            if (i < c.pieces) load16(r.w + 4 * b, p + c.at + i * V);
-        }
+        const Cut c = cut_tile<V>(p, sizeof(T), l.n[k], t - l.first[k], l.tile);
         const long long e = c.single(threadIdx.x, V);
         const double g = e >= 0 ? (double)widen<T>(p[e]) : 0.0;
-        acc = join<KIND>(acc, KIND == FO_NORM_L2 ? sum_squares<T>(r) : max_magnitude<T>(r));
+        for (int i0 = threadIdx.x; i0 < c.pieces; i0 += kBatch * kCta) {
+            Packed<T, V * kBatch> r;
+            r.clear();
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (i0 + b * kCta < c.pieces) load16(r.w + 4 * b, p + c.at + (i0 + b * kCta) * V);
+            acc = join<KIND>(acc, KIND == FO_NORM_L2 ? sum_squares<T>(r) : max_magnitude<T>(r));
+        }
         if (e >= 0) acc = join<KIND>(acc, KIND == FO_NORM_L2 ? g * g : fabs(g));
     }
     let_later_start();                                       // its CTAs wait for this kernel's end
@@ -209,16 +212,18 @@ __global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kCtasPerSm) grad_no
 }
 
 // -------------------------------------------------------------------- clip
-// V elements (16 or 32 bytes, or 64 of float64 beside float32) of a tensor that lies in [begin, end): whole 16 bytes
-// where they are aligned, else put together.
+// V elements, 16 or 32 bytes, of a tensor that lies in [begin, end): at once where they are `aligned` to their size, else
+// put together from aligned 16 bytes.
 template <class T, int V>
 __device__ __forceinline__ void load_some(Packed<T, V> &r, const T *p, bool aligned, const T *begin, const T *end)
 {
     constexpr int kStep = 16 / (int)sizeof(T);
+    if (aligned) {
+        if constexpr (V == 2 * kStep) load32(r.w, p);
+        else load16(r.w, p);
+    } else {
 #pragma unroll
-    for (int k = 0; k < V; k += kStep) {
-        if (aligned) load16(r.w + k * (int)sizeof(T) / 4, p + k);
-        else load16_any(r.w + k * (int)sizeof(T) / 4, p + k, begin, end);
+        for (int k = 0; k < V; k += kStep) load16_any(r.w + k * (int)sizeof(T) / 4, p + k, begin, end);
     }
 }
 template <class T, int V>
@@ -229,17 +234,17 @@ __device__ __forceinline__ void store_some(T *p, const Acc<T> (&v)[V], bool alig
         Packed<T, V> r;
 #pragma unroll
         for (int k = 0; k < V; k += 2) r.put2(k, two(v[k], v[k + 1]));
-#pragma unroll
-        for (int k = 0; k < V; k += kStep) store16(p + k, r.w + k * (int)sizeof(T) / 4);
+        if constexpr (V == 2 * kStep) store32(p, r.w);
+        else store16(p, r.w);
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) p[k] = narrow<T>(v[k]);
     }
 }
-template <class T>
-__device__ __forceinline__ bool aligned16(const T *p)
+template <int V, class T>
+__device__ __forceinline__ bool aligned_for(const T *p)
 {
-    return ((uintptr_t)p & 15u) == 0;
+    return ((uintptr_t)p & (V * sizeof(T) - 1)) == 0;
 }
 
 __device__ __forceinline__ double read_factor(const void *factor, int type)
@@ -248,13 +253,15 @@ __device__ __forceinline__ double read_factor(const void *factor, int type)
 }
 
 // The tiles in the opposite order of the norm's: what it read last is still in L2.
+constexpr int kClipPerSm = 8;                // CTAs; with 4 pieces in flight and 5 CTAs, 260M bf16: 376 us, so 368
+
 template <class TI, class TO, int N>
-__global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kCtasPerSm) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
+__global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kClipPerSm) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
                                                     int result_type)
 {
     using A = Acc<TI>;
     constexpr int V = 16 / (int)sizeof(TI);
-    constexpr int kBatch = kTile / kCta / V > 0 ? kTile / kCta / V : 1;
+    constexpr int kBatch = 2;                // pieces of a thread in flight
     A factor = A(0);
     bool known = false;
     for (unsigned u = blockIdx.x; u < l.tiles; u += gridDim.x) {
@@ -263,34 +270,35 @@ __global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kCtasPerSm) clip_k
         const TI *begin = static_cast<const TI *>(l.in[k]);
         const long long n = l.n[k];
         TO *out = static_cast<TO *>(l.out[k]);
-        constexpr int kAlign = 16 / (int)sizeof(TO) < V ? 16 / (int)sizeof(TO) : V;
-        const Cut c = cut_tile<V, kTile>(out, sizeof(TO), n, t - l.first[k], kAlign);
+        const Cut c = cut_tile<V>(out, sizeof(TO), n, t - l.first[k], l.tile);
         const TI *p = begin + c.at;
         TO *q = out + c.at;
-        const bool in_ok = aligned16(p);
-        Packed<TI, V> g[kBatch];
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int i = threadIdx.x + b * kCta;
-            if (i < c.pieces) load_some<TI, V>(g[b], p + i * V, in_ok, begin, begin + n);
-        }
+        const bool in_ok = aligned_for<V>(p);
         const long long e = c.single(threadIdx.x, V);
         const A one = e >= 0 ? widen<TI>(begin[e]) : A(0);
-        if (!known) {                                        // the first tile was on its way meanwhile
-            wait_for_earlier();
-            factor = (A)(result_type == FO_F64 ? static_cast<const double *>(result)[1]
-                                               : (double)static_cast<const float *>(result)[1]);
-            known = true;
-        }
-        if ((const void *)begin == (const void *)out && factor == A(1)) continue;
+        for (int i0 = 0; i0 == 0 || i0 < c.pieces; i0 += kBatch * kCta) {
+            Packed<TI, V> g[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int i = threadIdx.x + b * kCta;
-            if (i >= c.pieces) continue;
-            A v[V];
+            for (int b = 0; b < kBatch; ++b) {
+                const int i = i0 + threadIdx.x + b * kCta;
+                if (i < c.pieces) load_some<TI, V>(g[b], p + i * V, in_ok, begin, begin + n);
+            }
+            if (!known) {                                    // the first elements were on their way meanwhile
+                wait_for_earlier();
+                factor = (A)(result_type == FO_F64 ? static_cast<const double *>(result)[1]
+                                                   : (double)static_cast<const float *>(result)[1]);
+                known = true;
+            }
+            if ((const void *)begin == (const void *)out && factor == A(1)) break;
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = g[b].get(e) * factor;
-            store_some<TO, V>(q + i * V, v, true);
+            for (int b = 0; b < kBatch; ++b) {
+                const int i = i0 + threadIdx.x + b * kCta;
+                if (i >= c.pieces) continue;
+                A v[V];
+#pragma unroll
+                for (int x = 0; x < V; ++x) v[x] = g[b].get(x) * factor;
+                store_some<TO, V>(q + i * V, v, true);
+            }
         }
         if (e >= 0) out[e] = narrow<TO>(one * factor);
     }
@@ -314,7 +322,12 @@ __device__ __forceinline__ void adam_one(A &p, A g, A &m, A &v, A c, A b1, A b2,
     p = p - lr * fused_ma(decay, p, step);
 }
 
-// Pieces of 8 elements (2 of float64): two 16-byte loads of each 32-bit tensor are in flight at once.
+// Pieces of 8 elements (2 of float64), 32 bytes of each 32-bit tensor.  CTAs per SM: where everything is aligned, two keep
+// enough in flight (57 KB), and more make the memory serve reads and writes of seven streams in more and smaller
+// turns (100M parameters in one tensor: 436 us, with three 475); misaligned gradients need three (130M in 72 tensors
+// behind each other: 606 us, with two 691), and lists that are soon through four (3M: 19 us, with three 21).
+constexpr long long kAdamLong = 8 << 20;
+
 template <class TG, class TW, int N>
 __global__ void __launch_bounds__(kCta) adamw_kernel(const __grid_constant__ AdamList<N> l, const AdamHyper h)
 {
@@ -331,10 +344,11 @@ __global__ void __launch_bounds__(kCta) adamw_kernel(const __grid_constant__ Ada
         A *po = static_cast<A *>(l.p_out[k]), *mo = static_cast<A *>(l.m_out[k]), *vo = static_cast<A *>(l.v_out[k]);
         TW *wo = static_cast<TW *>(l.weights[k]);
         const A decay = (A)l.decay[k];
-        const Cut cut = cut_tile<V, kAdamTile>(po, sizeof(A), n, t - l.first[k]);
+        const Cut cut = cut_tile<V>(po, sizeof(A), n, t - l.first[k], l.tile);
         const long long d = cut.at;
-        const bool p_ok = aligned16(p + d), g_ok = aligned16(g + d), m_ok = aligned16(m + d), v_ok = aligned16(v + d),
-                   mo_ok = aligned16(mo + d), vo_ok = aligned16(vo + d), wo_ok = aligned16(wo + d);
+        const bool p_ok = aligned_for<V>(p + d), g_ok = aligned_for<V>(g + d), m_ok = aligned_for<V>(m + d),
+                   v_ok = aligned_for<V>(v + d), mo_ok = aligned_for<V>(mo + d), vo_ok = aligned_for<V>(vo + d),
+                   wo_ok = aligned_for<V>(wo + d);
 #pragma unroll 1
         for (int i = threadIdx.x; i < cut.pieces; i += kCta) {
             const long long e0 = d + i * V;
@@ -374,6 +388,15 @@ constexpr int kFew = 40, kMany = 512, kManyAdam = 256;      // tensors of one la
 
 unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
 
+// Tile size and grid of a part of a list: about 4 tiles for each of `per_sm` CTAs on every SM.
+template <class Tensor>
+int tile_for(const Tensor *t, int count, int per_sm)
+{
+    long long total = 0;
+    for (int k = 0; k < count; ++k) total += t[k].n;
+    const long long each = total / ((long long)sm_count() * per_sm * 4 + 1) / kTile + 1;
+    return (int)(each * kTile < kMostTile ? each * kTile : kMostTile);
+}
 unsigned grid_for(unsigned tiles, int per_sm)
 {
     const unsigned cap = (unsigned)(sm_count() * per_sm);
@@ -392,7 +415,7 @@ int check_list(const Tensor *t, int count, Bad bad)
     for (int k = 0; k < count; ++k) {
         if (t[k].n < 0) return FO_ERR_SHAPE;
         if (t[k].n > 0 && bad(t[k])) return FO_ERR_NULL;
-        tiles += (unsigned long long)(t[k].n / kAdamTile + 1);
+        tiles += (unsigned long long)(t[k].n / kTile + 1);
     }
     return tiles < (1ULL << 31) ? FO_OK : FO_ERR_UNSUPPORTED;
 }
@@ -400,14 +423,15 @@ int check_list(const Tensor *t, int count, Bad bad)
 template <class T, int N>
 cudaError_t launch_norm_part(const fo_tensor *t, int count, int kind, const NormOut &o, cudaStream_t st)
 {
+    constexpr int kPerSm = 6;
     NormList<N> l;
-    l.count = count, l.tiles = 0;
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.n[k] = t[k].n;
-        l.tiles += tiles_of(t[k].n, kTile);
+        l.tiles += tiles_of(t[k].n, l.tile);
     }
     l.first[count] = l.tiles;
-    const unsigned grid = grid_for(l.tiles, kCtasPerSm);
+    const unsigned grid = grid_for(l.tiles, kPerSm);
     if (kind == FO_NORM_L2) grad_norm_kernel<T, N, FO_NORM_L2><<<grid, kCta, 0, st>>>(l, o);
     else grad_norm_kernel<T, N, FO_NORM_MAX><<<grid, kCta, 0, st>>>(l, o);
     return cudaGetLastError();
@@ -433,16 +457,17 @@ cudaError_t launch_norm(const fo_tensor *t, int count, int kind, NormOut o, cuda
 template <class TI, class TO, int N>
 cudaError_t launch_clip_part(const fo_tensor *t, int count, const void *result, int result_type, cudaStream_t st)
 {
+    constexpr int kPerSm = kClipPerSm;
     ClipList<N> l;
-    l.count = count, l.tiles = 0;
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.out[k] = t[k].out, l.n[k] = t[k].n;
-        l.tiles += tiles_of(t[k].n, kTile);
+        l.tiles += tiles_of(t[k].n, l.tile);
     }
     l.first[count] = l.tiles;
     if (l.tiles == 0) return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid_for(l.tiles, kCtasPerSm));
+    cfg.gridDim = dim3(grid_for(l.tiles, kPerSm));
     cfg.blockDim = dim3(kCta);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -468,18 +493,27 @@ cudaError_t launch_clip(const fo_tensor *t, int count, const void *result, int r
 template <class TG, class TW, int N>
 cudaError_t launch_adam_part(const fo_adam_tensor *t, int count, const AdamHyper &h, cudaStream_t st)
 {
+    long long total = 0;
+    bool aligned = true;
+    for (int k = 0; k < count; ++k) {
+        total += t[k].n;
+        for (const void *q : {t[k].p, t[k].g, t[k].m, t[k].v, (const void *)t[k].p_out, (const void *)t[k].m_out,
+                              (const void *)t[k].v_out, (const void *)t[k].weights})
+            aligned = aligned && ((uintptr_t)q & 31u) == 0;
+    }
+    const int per_sm = total < kAdamLong ? 4 : aligned ? 2 : 3;
     AdamList<N> l;
-    l.count = count, l.tiles = 0;
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, per_sm);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles;
         l.p[k] = t[k].p, l.g[k] = t[k].g, l.m[k] = t[k].m, l.v[k] = t[k].v;
         l.p_out[k] = t[k].p_out, l.m_out[k] = t[k].m_out, l.v_out[k] = t[k].v_out, l.weights[k] = t[k].weights;
         l.n[k] = t[k].n, l.decay[k] = t[k].decay;
-        l.tiles += tiles_of(t[k].n, kAdamTile);
+        l.tiles += tiles_of(t[k].n, l.tile);
     }
     l.first[count] = l.tiles;
     if (l.tiles == 0) return cudaSuccess;
-    adamw_kernel<TG, TW, N><<<grid_for(l.tiles, kAdamCtasPerSm), kCta, 0, st>>>(l, h);
+    adamw_kernel<TG, TW, N><<<grid_for(l.tiles, per_sm), kCta, 0, st>>>(l, h);
     return cudaGetLastError();
 }
 
