@@ -48,12 +48,13 @@ NormSpec spec_of(const fo_norm &n)
 struct Pieces {
     bool ok;
     int block_bytes;
+    bool vectors = true;
     void matrix(const void *p, long long ld, int type)
     {
         const int piece = 16 * elem_bytes(type) / block_bytes;
         if (p) ok = ok && ((uintptr_t)p & (unsigned)(piece - 1)) == 0 && (ld * elem_bytes(type)) % piece == 0;
     }
-    void vector(const void *p) { ok = ok && ((uintptr_t)p & 15u) == 0; }
+    void vector(const void *p) { vectors = vectors && ((uintptr_t)p & 15u) == 0; }
     void norm(const fo_norm &n)
     {
         if (n.kind != FO_NORM_NONE) vector(n.weight), vector(n.bias);
@@ -140,7 +141,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
     if (p.gate_access == FO_AT_CELL) all.matrix(a->gate, a->ld_gate, a->block_type);
     if (p.gate_access == FO_AT_COL) all.vector(a->gate);
     all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
-    p.aligned = all.ok;
+    p.aligned = all.ok && all.vectors, p.vectors = all.vectors;
 
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(s, b, TS, TB) \
@@ -214,7 +215,7 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     if (p.gate_access == FO_AT_CELL) all.matrix(a->dgate, a->ld_dgate, a->block_type);
     if (p.gate_access == FO_AT_COL) all.vector(a->gate);
     all.vector(a->col_scale), all.norm(a->post), all.norm(a->pre);
-    p.aligned = all.ok;
+    p.aligned = all.ok && all.vectors, p.vectors = all.vectors;
 
     int n_sums = 0;
     ColumnSumParams cs = {};

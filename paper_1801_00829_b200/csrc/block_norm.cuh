@@ -28,7 +28,8 @@ struct NormSpec {
 struct BlockNormParams {
     long long rows;
     int cols;
-    int aligned;                             // rows and vectors are whole 16-byte pieces
+    int aligned;                             // rows and vectors are whole pieces
+    int vectors;                             // vectors begin on 16-byte boundaries
     double inv_cols;                         // 1 / cols
     int wide_vec;                            // vectors are float although the block has 16 bits
     int gate_access, gate_act;               // gate_access -1: none
@@ -43,7 +44,7 @@ struct BlockNormParams {
 struct BlockNormGradParams {
     long long rows;
     int cols;
-    int aligned, wide_vec;
+    int aligned, vectors, wide_vec;
     double inv_cols;
     int gate_access, gate_act;
     const void *dh, *dy, *h, *f, *gate, *col_scale, *stats;
@@ -65,6 +66,7 @@ struct BlockNormGradParams {
 template <int T, int V>                        // T: threads of the row, 0: the CTAs' threads
 struct Columns {
     int t, cols, count;                        // count: threads of the row
+    bool vectors;                              // vectors over the columns begin on 16-byte boundaries
     __device__ __forceinline__ int threads() const { return T > 0 ? T : count; }
     __device__ __forceinline__ int of(int k) const { return ((k / V) * threads() + t) * V + k % V; }
     // elements k and k + 1 (k even) with zeros outside the row
@@ -193,7 +195,7 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
                                             const Columns<T, V> &c)
 {
     using A = Acc<TE>;
-    if constexpr (!ALIGNED) {
+    if (!ALIGNED && !(c.vectors && c.of((k0 + N - 1) / V * V) + V <= c.cols)) {      // not whole, or not aligned
         auto at = [&](int k) -> A {
             const int j = min(c.of(k), c.cols - 1);
             if (sizeof(TE) == 2 && wide) return (A)__ldg(static_cast<const float *>(base) + j);
@@ -319,11 +321,11 @@ template <int T>
 constexpr int kDivisor = T > 0 ? T : 1;
 
 template <int T, int C, int V>
-__device__ __forceinline__ Columns<T, V> columns_of(int cols, const Group &g)
+__device__ __forceinline__ Columns<T, V> columns_of(int cols, bool vectors, const Group &g)
 {
-    if constexpr (T > 0) return {(int)(threadIdx.x % kDivisor<T>), cols, T};
-    else if constexpr (C == 1) return {(int)threadIdx.x - g.id * g.threads, cols, g.threads};
-    else return {(int)threadIdx.x + (int)cluster_rank() * g.threads, cols, g.threads * C};
+    if constexpr (T > 0) return {(int)(threadIdx.x % kDivisor<T>), cols, T, vectors};
+    else if constexpr (C == 1) return {(int)threadIdx.x - g.id * g.threads, cols, g.threads, vectors};
+    else return {(int)threadIdx.x + (int)cluster_rank() * g.threads, cols, g.threads * C, vectors};
 }
 
 // Where a warp exchanges the pieces of an unaligned store, and 16 bytes more.
@@ -389,7 +391,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     const long long row = T > 0 ? (long long)blockIdx.x * (kGroupCta / kDivisor<T>) + threadIdx.x / kDivisor<T> : blockIdx.x / C;
     const bool ok = row < p.rows;
     const Group group = {0, (int)blockDim.x};
-    const Columns<T, V> c = columns_of<T, C, V>(p.cols, group);
+    const Columns<T, V> c = columns_of<T, C, V>(p.cols, p.vectors != 0, group);
     const bool wide = p.wide_vec != 0;
     const A inv = A(p.inv_cols);
     const auto times = [](Two<A> h, Two<A> w) { return h * w; };
@@ -518,7 +520,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     int buf = 0;
     const Group group = {T > 0 ? 0 : (int)threadIdx.x / p.group, p.group};
     const int groups = T > 0 ? kGroups : (int)blockDim.x / p.group, cta = T > 0 ? kGroupCta : (int)blockDim.x;
-    const Columns<T, V> c = columns_of<T, C, V>(p.cols, group);
+    const Columns<T, V> c = columns_of<T, C, V>(p.cols, p.vectors != 0, group);
     const bool ragged = p.cols != c.threads() * E;
     const A inv = A(p.inv_cols);
     const A *stats = static_cast<const A *>(p.stats);
@@ -722,7 +724,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
             for (int e = 0; e < Sums::kValues / 2; ++e) v.v[e] = v.v[e] + more.v[e];
         }
-        const Columns<T, V> own = {t + (C > 1 ? (int)cluster_rank() * threads : 0), p.cols, c.count};
+        const Columns<T, V> own = {t + (C > 1 ? (int)cluster_rank() * threads : 0), p.cols, c.count, c.vectors};
 #pragma unroll
         for (int e = 0; e < Sums::kValues; ++e) {
             const int j = own.of(piece * Sums::kValues + e);

@@ -162,8 +162,10 @@ __device__ __forceinline__ double cta_join(double v, double *smem)     // result
     return v;
 }
 
+constexpr int kNormPerSm = 5;                // CTAs, of 51 registers a thread: four 16-byte pieces and their sums
+
 template <class T, int N, int KIND>
-__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : 6) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
+__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kNormPerSm) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
 {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int kBatch = 4;                // pieces of a thread in flight
@@ -423,7 +425,7 @@ int check_list(const Tensor *t, int count, Bad bad)
 template <class T, int N>
 cudaError_t launch_norm_part(const fo_tensor *t, int count, int kind, const NormOut &o, cudaStream_t st)
 {
-    constexpr int kPerSm = 6;
+    constexpr int kPerSm = kNormPerSm;
     NormList<N> l;
     l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm);
     for (int k = 0; k < count; ++k) {
