@@ -503,8 +503,14 @@ struct SumPieces {
     }
 };
 
+// What a gradient kernel is compiled for.  kGradAny looks at everything at run time.  The lean forms are what
+// transformer blocks mostly have: dx, root-mean-square norms with weights and without biases, no gate
+// (kGradLean) or one per element (kGradLeanGate), a column scale or none; with nothing else to test or to hold,
+// GRADIENT_LEAN_FIGURES.
+enum GradForm { kGradAny = 0, kGradLean = 1, kGradLeanGate = 2 };
+
 // 64 registers a thread with 8 elements, so that 1024 threads share an SM; 128 with 16.
-template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK>
+template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int FORM>
 __global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 8 || E > 8 ? 1 : T > 0 ? 4 : 2)
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
@@ -526,6 +532,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     const A *stats = static_cast<const A *>(p.stats);
     const bool wide = p.wide_vec != 0;
     using Sums = SumPieces<E, A>;
+    constexpr bool kAny = FORM == kGradAny;
+    const bool pre = !kAny || p.dy != nullptr, pre_layer = kAny && p.pre.kind == FO_NORM_LAYER;
+    const bool pre_weight = !kAny || p.pre.weight != nullptr, post_weight = !kAny || p.post.weight != nullptr;
+    const bool post_bias = kAny && p.post.bias != nullptr, post_layer = kAny && p.post.kind == FO_NORM_LAYER;
+    const bool normed = !kAny || p.post.kind != FO_NORM_NONE;
+    const bool cell_gate = kAny ? p.gate_access == FO_AT_CELL : FORM == kGradLeanGate;
+    const bool row_gate = kAny && p.gate_access == FO_AT_ROW, col_gate = kAny && p.gate_access == FO_AT_COL;
     const int n_slots = __popc(p.slots);
     A *sums = reinterpret_cast<A *>(dynamic);
     if constexpr (sizeof(A) == 8) {                          // of float sums there is always room
@@ -535,7 +548,11 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     int slot_at[kGradSlots];
 #pragma unroll
     for (int s = 0; s < kGradSlots; ++s)
-        slot_at[s] = ((p.slots >> s) & 1u) ? __popc(p.slots & ((1u << s) - 1u)) * cta * E : -1;
+        slot_at[s] = !kAny && (s == kPreB || s == kPostB || s == kGateCol) ? -1
+                     : !kAny && s == kPreW                                 ? 0
+                     : !kAny && s == kPostW                                ? (BLK ? cta * E : -1)
+                     : ((p.slots >> s) & 1u)                               ? __popc(p.slots & ((1u << s) - 1u)) * cta * E
+                                                                           : -1;
     // adds term(i), for the pairs i of a piece from element k0, to a column sum that is wanted
     auto add = [&](int slot, int k0, auto term) {
         if (slot_at[slot] >= 0) Sums::template change<P>(sums + slot_at[slot], k0, term);
@@ -550,17 +567,17 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         const bool ok = row < p.rows;                        // past the end all values are zero
         Packed<TS, E> dhr, hr;
         Packed<TB, E> dyr, fr, gr;
-        if (p.dy) {
+        if (pre) {
             load_row<ALIGNED, TB, E>(dyr, p.dy, p.rows, row, p.ld_dy, c, ok);
             load_row<ALIGNED, TS, E>(hr, p.h, p.rows, row, p.ld_h, c, ok);
         }
         if (p.dh) load_row<ALIGNED, TS, E>(dhr, p.dh, p.rows, row, p.ld_dh, c, ok);
         else dhr.clear();
         if (BLK) load_row<ALIGNED, TB, E>(fr, p.f, p.rows, row, p.ld_f, c, ok);
-        if (BLK && p.gate_access == FO_AT_CELL) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
+        if (BLK && cell_gate) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
 
         Two<A> t[E / 2];
-        if (p.dy) {
+        if (pre) {
             const A r1 = ok ? stats[3 * p.rows + row] : A(0);
             const Two<A> minus = both(ok ? -stats[2 * p.rows + row] : A(0)), r = both(r1);
             Two<A> along = both(A(0)), level = both(A(0));
@@ -574,7 +591,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 }
                 add(kPreW, k0, [&](int i, Two<A> s) { return fused_ma(a[i], n[i], s); });
                 add(kPreB, k0, [&](int i, Two<A> s) { return s + a[i]; });
-                if (p.pre.weight) {
+                if (pre_weight) {
                     Two<A> w[P / 2];
                     load_vector<ALIGNED, TB, P>(w, p.pre.weight, wide, k0, c);
 #pragma unroll
@@ -582,13 +599,13 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 }
 #pragma unroll
                 for (int i = 0; i < P / 2; ++i) along = fused_ma(a[i], n[i], along);
-                if (p.pre.kind == FO_NORM_LAYER) {
+                if (pre_layer) {
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) level = level + a[i];
                 }
             }
             A s[2] = {joined(along), A(0)};
-            if (p.pre.kind == FO_NORM_LAYER) {
+            if (pre_layer) {
                 s[1] = joined(level);
                 group_sum<T, C, 2, A>(s, group, area, buf);
             } else {
@@ -607,9 +624,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
             for (int k = 0; k < E; k += 2) t[k / 2] = dhr.get2(k);
         }
-        if (p.dx) store_row<ALIGNED, TS, E>(p.dx, row, p.ld_dx, pack_row<TS, E>(t), c, ok, stage);
+        if (!kAny || p.dx) store_row<ALIGNED, TS, E>(p.dx, row, p.ld_dx, pack_row<TS, E>(t), c, ok, stage);
         if constexpr (BLK) {
-            const bool normed = p.post.kind != FO_NORM_NONE, row_gate = p.gate_access == FO_AT_ROW;
             const A r1 = ok && normed ? stats[p.rows + row] : A(1);
             const Two<A> minus = both(ok && normed ? -stats[row] : A(0)), r = both(r1), scale = both(A(p.scale));
             Two<A> row_act = both(A(1)), row_slope = both(A(0));
@@ -623,7 +639,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
             for (int k0 = 0; k0 < E; k0 += P) {
                 Two<A> n[P / 2], z[P / 2], w[P / 2], a[P / 2], slope[P / 2], *d = t + k0 / 2;
-                if (p.post.weight) load_vector<ALIGNED, TB, P>(w, p.post.weight, wide, k0, c);
+                if (post_weight) load_vector<ALIGNED, TB, P>(w, p.post.weight, wide, k0, c);
                 else
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) w[i] = both(A(1));
@@ -633,15 +649,15 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     z[i] = n[i] * w[i];
                     d[i] = d[i] * scale;
                 }
-                if (p.post.bias) {
+                if (post_bias) {
                     Two<A> b[P / 2];
                     load_vector<ALIGNED, TB, P>(b, p.post.bias, wide, k0, c);
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) z[i] = z[i] + b[i];
                 }
-                if (p.gate_access == FO_AT_CELL || p.gate_access == FO_AT_COL) {
+                if (cell_gate || col_gate) {
                     Two<A> g[P / 2];
-                    if (p.gate_access == FO_AT_COL) load_vector<ALIGNED, TB, P>(g, p.gate, false, k0, c);
+                    if (col_gate) load_vector<ALIGNED, TB, P>(g, p.gate, false, k0, c);
                     else
 #pragma unroll
                         for (int i = 0; i < P / 2; ++i) g[i] = gr.get2(k0 + 2 * i);
@@ -667,7 +683,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     z[i] = d[i] * z[i] * slope[i];
                     d[i] = d[i] * a[i];
                 }
-                if (p.gate_access == FO_AT_CELL) {           // in the gate's place
+                if (cell_gate) {                             // in the gate's place
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) gr.put2(k0 + 2 * i, z[i]);
                 }
@@ -684,16 +700,16 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                         d[i] = d[i] * w[i];
                         along = fused_ma(d[i], n[i], along);
                     }
-                    if (p.post.kind == FO_NORM_LAYER) {
+                    if (post_layer) {
 #pragma unroll
                         for (int i = 0; i < P / 2; ++i) level = level + d[i];
                     }
                 }
             }
-            if (p.dgate && p.gate_access == FO_AT_CELL)
+            if (cell_gate && p.dgate)
                 store_row<ALIGNED, TB, E>(p.dgate, row, p.ld_dgate, gr, c, ok, stage);
             A s[3] = {joined(along), A(0), A(0)};
-            if (row_gate || p.post.kind == FO_NORM_LAYER) {
+            if (row_gate || post_layer) {
                 s[1] = joined(level), s[2] = joined(gate_sum);
                 group_sum<T, C, 3, A>(s, group, area, buf);
                 if (p.dgate && ok && row_gate && c.t == 0) static_cast<A *>(p.dgate)[row] = s[2];
@@ -706,7 +722,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 for (int k = 0; k < E; k += 2)
                     t[k / 2] = fused_ma(t[k / 2], r, fused_ma(fr.get2(k) + minus, along, level));
             }
-            if (p.df) store_row<ALIGNED, TB, E>(p.df, row, p.ld_df, pack_row<TB, E>(t), c, ok, stage);
+            if (!kAny || p.df) store_row<ALIGNED, TB, E>(p.df, row, p.ld_df, pack_row<TB, E>(t), c, ok, stage);
         }
     }
 

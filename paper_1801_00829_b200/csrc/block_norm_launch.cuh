@@ -129,8 +129,9 @@ cudaError_t launch_block_norm_grad(BlockNormGradParams p, GradSpace *space, cuda
     return with_grad_shape<16 / (int)sizeof(TB)>(p.cols, [&](auto tc, auto cc, auto ec, int cta) -> cudaError_t {
         constexpr int T = decltype(tc)::value, C = decltype(cc)::value, E = decltype(ec)::value;
         constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
-        auto go = [&](auto aligned, auto blk) -> cudaError_t {
-            constexpr auto kern = block_norm_grad_kernel<TS, TB, T, C, E, decltype(aligned)::value, decltype(blk)::value>;
+        auto go = [&](auto aligned, auto blk, auto form) -> cudaError_t {
+            constexpr auto kern = block_norm_grad_kernel<TS, TB, T, C, E, decltype(aligned)::value, decltype(blk)::value,
+                                                         decltype(form)::value>;
             // as many groups as 512 threads hold, while there are rows for them on every SM
             const int sms = sm_count();
             int groups = kGroups, threads = cta;
@@ -155,10 +156,21 @@ cudaError_t launch_block_norm_grad(BlockNormGradParams p, GradSpace *space, cuda
             space->lines = (int)lines;
             return launch_rows(kern, p, lines * C, threads, C, per_sm > 0 ? n * sum_bytes : 0, st);
         };
-        auto by_block = [&](auto aligned) -> cudaError_t {
-            return p.f ? go(aligned, std::true_type()) : go(aligned, std::false_type());
-        };
-        return p.aligned ? by_block(std::true_type()) : by_block(std::false_type());
+        using Any = std::integral_constant<int, kGradAny>;
+        using Lean = std::integral_constant<int, kGradLean>;
+        using LeanGate = std::integral_constant<int, kGradLeanGate>;
+        const bool pre = p.dy && p.dx && p.pre.kind == FO_NORM_RMS && p.pre.weight && (p.slots & (1u << kPreW));
+        if (!p.f) {
+            if (p.aligned && pre && p.slots == (1u << kPreW)) return go(std::true_type(), std::false_type(), Lean());
+            return p.aligned ? go(std::true_type(), std::false_type(), Any()) : go(std::false_type(), std::false_type(), Any());
+        }
+        const unsigned both = (1u << kPreW) | (1u << kPostW);
+        if (p.aligned && pre && p.df && p.post.kind == FO_NORM_RMS && p.post.weight && !p.post.bias
+            && (p.slots & ~(1u << kColScale)) == both) {
+            if (p.gate_access < 0) return go(std::true_type(), std::true_type(), Lean());
+            if (p.gate_access == FO_AT_CELL) return go(std::true_type(), std::true_type(), LeanGate());
+        }
+        return p.aligned ? go(std::true_type(), std::true_type(), Any()) : go(std::false_type(), std::true_type(), Any());
     });
 }
 #endif
