@@ -14,7 +14,7 @@ namespace fo {
 
 #define FO_EXTERN(s, b, TS, TB)                                                                    \
     extern template cudaError_t launch_block_norm<TS, TB>(const BlockNormParams &, cudaStream_t);  \
-    extern template cudaError_t launch_block_norm_grad<TS, TB>(BlockNormGradParams, GradSpace *, cudaStream_t);
+    extern template cudaError_t launch_block_norm_grad<TS, TB>(BlockNormGradParams, int, int *, cudaStream_t);
 FO_PAIRS(FO_EXTERN)
 #undef FO_EXTERN
 
@@ -87,18 +87,10 @@ int grad_lines(long long rows, long long cols)
     return (int)(n > 1 ? n : 1);
 }
 
-// Lines, and room for the sums of CTAs that shared memory does not hold: float64 sums of 512 threads with 16
-// elements each (rows beyond 8192 columns).
 size_t grad_line_bytes(long long rows, long long cols, int block_type)
 {
     return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
 }
-size_t grad_sum_bytes(long long rows, long long cols, int block_type)
-{
-    if (block_type != FO_F64 || cols <= 8192) return 0;
-    return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)(cols <= 16384 ? 16384 : 32768) * sizeof(double);
-}
-
 }  // namespace
 }  // namespace fo
 
@@ -154,7 +146,7 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
 size_t fused_block_norm_grad_workspace_bytes(int64_t rows, int64_t cols, int block_type)
 {
     if (check_shape(rows, cols) != FO_OK || block_type < FO_F64 || block_type > FO_F16) return 0;
-    return sizeof(WsHead) + (grad_line_bytes(rows, cols, block_type) + 255) / 256 * 256 + grad_sum_bytes(rows, cols, block_type);
+    return sizeof(WsHead) + grad_line_bytes(rows, cols, block_type);
 }
 
 int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes, void *stream)
@@ -224,15 +216,14 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
         p.slots |= 1u << s;
         cs.out[n_sums++] = sums[s];
     }
-    GradSpace space = {grad_lines(a->rows, a->cols), 0,
-                       static_cast<char *>(p.partial) + (grad_line_bytes(a->rows, a->cols, a->block_type) + 255) / 256 * 256};
+    int lines = 0;
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(s, b, TS, TB) \
-    if (a->stream_type == s && a->block_type == b) e = launch_block_norm_grad<TS, TB>(p, &space, st);
+    if (a->stream_type == s && a->block_type == b) e = launch_block_norm_grad<TS, TB>(p, grad_lines(a->rows, a->cols), &lines, st);
     FO_PAIRS(FO_CASE)
 #undef FO_CASE
     if (e == cudaSuccess && n_sums > 0) {
-        cs.partial = p.partial, cs.lines = space.lines, cs.cols = p.cols;
+        cs.partial = p.partial, cs.lines = lines, cs.cols = p.cols;
         const dim3 grid((unsigned)((a->cols + 31) / 32), (unsigned)n_sums);
         if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, kSumWarps * 32, 0, st>>>(cs);
         else column_sum_kernel<float><<<grid, kSumWarps * 32, 0, st>>>(cs);

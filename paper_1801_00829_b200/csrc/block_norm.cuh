@@ -55,7 +55,6 @@ struct BlockNormGradParams {
     long long ld_dx, ld_df, ld_dgate;
     int group;                               // threads of a row's group where that is more than a warp
     unsigned slots;                          // bit k: the sum of slot k is wanted
-    void *sums;                              // where the CTAs hold their sums, NULL: in shared memory
     void *partial;                           // [slot among the wanted][CTA or cluster][cols]
 };
 
@@ -375,15 +374,22 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
     return n;
 }
 
+// What a kernel is compiled for besides types and shape; the rest it looks at at run time.
+// GATE: none, one per element, or one per row or column.  LEAN: every matrix read and written, root-mean-square norms
+// with weights and without biases, what transformer blocks mostly have.  Every test and every value that a form
+// does not need is one less where issuing instructions takes longer than waiting for memory (8192 x 4096
+// bf16, gate per element: gradient 131 us, with everything at run time 172; FORWARD_LEAN_FIG).
+enum GateForm { kNoGate = 0, kCellGate = 1, kSharedGate = 2 };
+
 // ------------------------------------------------------------------ forward
 // BLK: there is a block output f (else the norm of the stream alone).
-template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK>
+template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int GATE, bool LEAN>
 __global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 4 ? (T > 0 ? 4 : 2) : 1)
 block_norm_kernel(const __grid_constant__ BlockNormParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
-    constexpr bool kFast = sizeof(TB) == 2;
+    constexpr bool kFast = sizeof(TB) == 2, kAny = !LEAN;
     __shared__ Area<A> area;
     __shared__ Stage<TS, V, T, ALIGNED> stages;
     unsigned char *const stage = stages.of_warp();
@@ -400,33 +406,34 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     Packed<TS, E> xr;
     Packed<TB, E> fr, gr;
     if (BLK) load_row<ALIGNED, TB, E>(fr, p.f, p.rows, row, p.ld_f, c, ok);
-    if (!BLK || p.x) load_row<ALIGNED, TS, E>(xr, p.x, p.rows, row, p.ld_x, c, ok);
+    if (!BLK || !kAny || p.x) load_row<ALIGNED, TS, E>(xr, p.x, p.rows, row, p.ld_x, c, ok);
     else xr.clear();
-    if (BLK && p.gate_access == FO_AT_CELL) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
+    if (BLK && GATE == kCellGate) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
 
+    const int post_kind = kAny ? p.post.kind : FO_NORM_RMS, pre_kind = kAny ? p.pre.kind : FO_NORM_RMS;
     RowNorm<A> post = {A(0), A(0)}, pre = {A(0), A(0)};
     Two<A> h[E / 2];
     if constexpr (BLK) {
         A scale = A(p.scale);
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fr.get2(k);
-        if (p.post.kind != FO_NORM_NONE) {
-            post = row_norm<ALIGNED, T, C>(h, p.post.kind, A(p.post.eps), inv, c, group, area, buf);
+        if (post_kind != FO_NORM_NONE) {
+            post = row_norm<ALIGNED, T, C>(h, post_kind, A(p.post.eps), inv, c, group, area, buf);
             const Two<A> r = both(post.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
-            if (p.post.weight) with_vector<ALIGNED, TB, E>(h, p.post.weight, wide, c, times);
-            if (p.post.bias) with_vector<ALIGNED, TB, E>(h, p.post.bias, wide, c, plus);
+            if (!kAny || p.post.weight) with_vector<ALIGNED, TB, E>(h, p.post.weight, wide, c, times);
+            if (kAny && p.post.bias) with_vector<ALIGNED, TB, E>(h, p.post.bias, wide, c, plus);
         }
-        if (p.gate_access == FO_AT_ROW) {
+        if (GATE == kSharedGate && p.gate_access == FO_AT_ROW) {
             const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
             with_activation(p.gate_act, [&](auto kind) { scale *= first(activate<decltype(kind)::value, kFast, A>(both(g))); });
-        } else if (p.gate_access == FO_AT_CELL) {
+        } else if (GATE == kCellGate) {
             with_activation(p.gate_act, [&](auto kind) {
 #pragma unroll
                 for (int k = 0; k < E; k += 2) h[k / 2] = h[k / 2] * activate<decltype(kind)::value, kFast, A>(gr.get2(k));
             });
-        } else if (p.gate_access == FO_AT_COL) {
+        } else if (GATE == kSharedGate) {
             with_activation(p.gate_act, [&](auto kind) {
                 with_vector<ALIGNED, TB, E>(h, p.gate, false, c,
                                    [](Two<A> z, Two<A> g) { return z * activate<decltype(kind)::value, kFast, A>(g); });
@@ -436,7 +443,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
         const Two<A> k2 = both(scale);
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fused_ma(h[k / 2], k2, xr.get2(k));
-        if (p.post.bias && p.cols != c.threads() * E) {            // a bias leaves no zeros outside the row
+        if (kAny && p.post.bias && p.cols != c.threads() * E) {            // a bias leaves no zeros outside the row
 #pragma unroll
             for (int k = 0; k < E; k += 2) h[k / 2] = c.template inside<ALIGNED>(k, h[k / 2]);
         }
@@ -444,15 +451,15 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = xr.get2(k);
     }
-    if (p.h) store_row<ALIGNED, TS, E>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
-    if (p.pre.kind != FO_NORM_NONE) {
-        pre = row_norm<ALIGNED, T, C>(h, p.pre.kind, A(p.pre.eps), inv, c, group, area, buf);
-        if (p.y) {
+    if ((!kAny && BLK) || p.h) store_row<ALIGNED, TS, E>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
+    if (pre_kind != FO_NORM_NONE) {
+        pre = row_norm<ALIGNED, T, C>(h, pre_kind, A(p.pre.eps), inv, c, group, area, buf);
+        if (!kAny || p.y) {
             const Two<A> r = both(pre.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
-            if (p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
-            if (p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
+            if (!kAny || p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
+            if (kAny && p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
             store_row<ALIGNED, TB, E>(p.y, row, p.ld_y, pack_row<TB, E>(h), c, ok, stage);
         }
     }
@@ -466,9 +473,10 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 // The CTAs are persistent: each takes every gridDim-th row (or group of rows) and adds up what the rows give to the
 // column sums.  A thread's part of those sums lies in shared memory, E values per sum in 16-byte pieces
 // that neighbouring threads' pieces follow (no bank is hit twice): in registers, the two to six sums
-// would leave room for so few threads that loads no longer cover their latency.  Where shared memory does not
-// hold them (many sums of long rows, float64) they lie in the CTA's own part of the workspace instead.
+// would leave room for so few threads that loads no longer cover their latency.
 // At the end every CTA writes its line of partial sums, and column_sum_kernel adds the lines in order.
+
+constexpr int kGradE = 8;                    // elements of a row in a thread
 
 // A thread's E values of one column sum: 16-byte pieces one behind the other, in an order that turns with the
 // thread's number so that the 8 threads of one shared-memory access meet 32 different banks.
@@ -503,18 +511,15 @@ struct SumPieces {
     }
 };
 
-// What a gradient kernel is compiled for.  kGradAny looks at everything at run time.  The lean forms are what
-// transformer blocks mostly have: dx, root-mean-square norms with weights and without biases, no gate
-// (kGradLean) or one per element (kGradLeanGate), a column scale or none; with nothing else to test or to hold,
-// GRADIENT_LEAN_FIGURES.
-enum GradForm { kGradAny = 0, kGradLean = 1, kGradLeanGate = 2 };
-
-// 64 registers a thread with 8 elements, so that 1024 threads share an SM; 128 with 16.
-template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int FORM>
-__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 8 || E > 8 ? 1 : T > 0 ? 4 : 2)
+// 64 registers a thread, so that 1024 threads share an SM; for unaligned rows, too, although they spill (8192 x 4097: 405 us,
+// with 128 registers and half the threads 881).
+template <class TS, class TB, int T, int C, bool ALIGNED, bool BLK, int GATE, bool LEAN>
+__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta,
+                                  sizeof(Acc<TB>) == 8 ? 1 : T > 0 ? 4 : 2)
 block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 {
     using A = Acc<TB>;
+    constexpr int E = kGradE;
     constexpr int V = 16 / (int)sizeof(TB);
     constexpr int P = 16 / (int)sizeof(A);                   // elements worked on at a time: what registers hold
     constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
@@ -532,23 +537,21 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     const A *stats = static_cast<const A *>(p.stats);
     const bool wide = p.wide_vec != 0;
     using Sums = SumPieces<E, A>;
-    constexpr bool kAny = FORM == kGradAny;
+    constexpr bool kAny = !LEAN;
     const bool pre = !kAny || p.dy != nullptr, pre_layer = kAny && p.pre.kind == FO_NORM_LAYER;
     const bool pre_weight = !kAny || p.pre.weight != nullptr, post_weight = !kAny || p.post.weight != nullptr;
     const bool post_bias = kAny && p.post.bias != nullptr, post_layer = kAny && p.post.kind == FO_NORM_LAYER;
     const bool normed = !kAny || p.post.kind != FO_NORM_NONE;
-    const bool cell_gate = kAny ? p.gate_access == FO_AT_CELL : FORM == kGradLeanGate;
-    const bool row_gate = kAny && p.gate_access == FO_AT_ROW, col_gate = kAny && p.gate_access == FO_AT_COL;
+    constexpr bool cell_gate = GATE == kCellGate;
+    const bool row_gate = GATE == kSharedGate && p.gate_access == FO_AT_ROW;
+    const bool col_gate = GATE == kSharedGate && p.gate_access == FO_AT_COL;
     const int n_slots = __popc(p.slots);
-    A *sums = reinterpret_cast<A *>(dynamic);
-    if constexpr (sizeof(A) == 8) {                          // of float sums there is always room
-        if (p.sums) sums = static_cast<A *>(p.sums) + (size_t)blockIdx.x * n_slots * cta * E;
-    }
+    A *const sums = reinterpret_cast<A *>(dynamic);
     // where each sum begins, -1: it is not wanted
     int slot_at[kGradSlots];
 #pragma unroll
     for (int s = 0; s < kGradSlots; ++s)
-        slot_at[s] = !kAny && (s == kPreB || s == kPostB || s == kGateCol) ? -1
+        slot_at[s] = (s == kGateCol && GATE != kSharedGate) || (!kAny && (s == kPreB || s == kPostB)) ? -1
                      : !kAny && s == kPreW                                 ? 0
                      : !kAny && s == kPostW                                ? (BLK ? cta * E : -1)
                      : ((p.slots >> s) & 1u)                               ? __popc(p.slots & ((1u << s) - 1u)) * cta * E
@@ -666,31 +669,35 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                         for (int i = 0; i < P / 2; ++i)
                             a[i] = activate_slope<decltype(kind)::value, kFast, A>(g[i], slope[i]);
                     });
-                } else {
+                } else if (row_gate) {
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) a[i] = row_act, slope[i] = row_slope;
                 }
                 if (p.col_scale) {
-                    add(kColScale, k0, [&](int i, Two<A> s) { return fused_ma(d[i] * z[i], a[i], s); });
+                    add(kColScale, k0, [&](int i, Two<A> s) {
+                        return GATE == kNoGate ? fused_ma(d[i], z[i], s) : fused_ma(d[i] * z[i], a[i], s);
+                    });
                     Two<A> cs[P / 2];
                     load_vector<ALIGNED, TB, P>(cs, p.col_scale, wide, k0, c);
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) d[i] = d[i] * cs[i];
                 }
-                // z becomes the gate's gradient q' z act', d the normed output's q' act
+                if constexpr (GATE != kNoGate) {
+                    // z becomes the gate's gradient q' z act', d the normed output's q' act
 #pragma unroll
-                for (int i = 0; i < P / 2; ++i) {
-                    z[i] = d[i] * z[i] * slope[i];
-                    d[i] = d[i] * a[i];
-                }
-                if (cell_gate) {                             // in the gate's place
+                    for (int i = 0; i < P / 2; ++i) {
+                        z[i] = d[i] * z[i] * slope[i];
+                        d[i] = d[i] * a[i];
+                    }
+                    if constexpr (cell_gate) {               // in the gate's place
 #pragma unroll
-                    for (int i = 0; i < P / 2; ++i) gr.put2(k0 + 2 * i, z[i]);
-                }
-                add(kGateCol, k0, [&](int i, Two<A> s) { return s + z[i]; });
-                if (row_gate) {
+                        for (int i = 0; i < P / 2; ++i) gr.put2(k0 + 2 * i, z[i]);
+                    }
+                    add(kGateCol, k0, [&](int i, Two<A> s) { return s + z[i]; });
+                    if (row_gate) {
 #pragma unroll
-                    for (int i = 0; i < P / 2; ++i) gate_sum = gate_sum + z[i];
+                        for (int i = 0; i < P / 2; ++i) gate_sum = gate_sum + z[i];
+                    }
                 }
                 if (normed) {
                     add(kPostW, k0, [&](int i, Two<A> s) { return fused_ma(d[i], n[i], s); });

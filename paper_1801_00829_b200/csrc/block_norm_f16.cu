@@ -4,5 +4,5 @@
 
 namespace fo {
 template cudaError_t launch_block_norm<__half, __half>(const BlockNormParams &, cudaStream_t);
-template cudaError_t launch_block_norm_grad<__half, __half>(BlockNormGradParams, GradSpace *, cudaStream_t);
+template cudaError_t launch_block_norm_grad<__half, __half>(BlockNormGradParams, int, int *, cudaStream_t);
 }  // namespace fo

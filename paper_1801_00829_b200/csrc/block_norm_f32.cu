@@ -4,5 +4,5 @@
 
 namespace fo {
 template cudaError_t launch_block_norm<float, float>(const BlockNormParams &, cudaStream_t);
-template cudaError_t launch_block_norm_grad<float, float>(BlockNormGradParams, GradSpace *, cudaStream_t);
+template cudaError_t launch_block_norm_grad<float, float>(BlockNormGradParams, int, int *, cudaStream_t);
 }  // namespace fo

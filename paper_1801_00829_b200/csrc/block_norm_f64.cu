@@ -4,5 +4,5 @@
 
 namespace fo {
 template cudaError_t launch_block_norm<double, double>(const BlockNormParams &, cudaStream_t);
-template cudaError_t launch_block_norm_grad<double, double>(BlockNormGradParams, GradSpace *, cudaStream_t);
+template cudaError_t launch_block_norm_grad<double, double>(BlockNormGradParams, int, int *, cudaStream_t);
 }  // namespace fo
