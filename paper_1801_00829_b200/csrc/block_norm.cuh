@@ -132,7 +132,8 @@ __device__ __forceinline__ Packed<TE, E> pack_row(const Two<Acc<TE>> (&v)[E / 2]
 // Stores the thread's elements into its row (`ok`: there is one).
 // Unaligned: the pieces of the row's threads in a warp are neighbours; they are exchanged through the warp's
 // `stage` so that full aligned 16 bytes can be written, and the ends singly.  All threads of the warp call it.
-template <bool ALIGNED, class TE, int E, int T, int V>
+// DIRECT: without that where a row begins aligned (the gradient, short of registers, is slower with it: 24 us, so 22).
+template <bool ALIGNED, class TE, int E, bool DIRECT = false, int T, int V>
 __device__ __forceinline__ void store_row(void *base, long long row, long long ld, const Packed<TE, E> &v,
                                           const Columns<T, V> &c, bool ok, unsigned char *stage)
 {
@@ -150,6 +151,24 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
         constexpr int kLanes = T > 0 ? T : 32;               // threads of the row in this warp
         constexpr int kChunks = V / kStep;                   // 16-byte chunks of a piece
         const int lane = (threadIdx.x & 31) % kLanes;
+        if (DIRECT && ((uintptr_t)p & 15u) == 0) {           // the row begins aligned: only its end is singly
+#pragma unroll
+            for (int k = 0; k < E; k += kStep) {
+                const int j = c.of(k);
+                if (!ok || j >= c.cols) continue;
+                if (j + kStep <= c.cols) {
+                    store16(p + j, v.w + k * kWords / 4);
+                } else {
+                    Packed<TE, kStep> last;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) last.w[i] = v.w[k * kWords / 4 + i];
+#pragma unroll
+                    for (int e = 0; e < kStep; ++e)
+                        if (j + e < c.cols) p[j + e] = last.raw(e);
+                }
+            }
+            if (T == 0) return;                              // (the rows of a warp's other groups may not)
+        }
         unsigned char *mine = stage + (threadIdx.x & 31) / kLanes * (kLanes * V * (int)sizeof(TE));
 #pragma unroll
         for (int k = 0; k < E; k += V) {
@@ -161,7 +180,7 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
             }
             __syncwarp();
             const int first_col = c.of(k) - lane * V, left = c.cols - first_col;
-            const int n = !ok ? 0 : left < kLanes * V ? left : kLanes * V;       // elements to write, may be negative
+            const int n = !ok || (DIRECT && T > 0 && ((uintptr_t)p & 15u) == 0) ? 0 : left < kLanes * V ? left : kLanes * V;       // elements to write, may be negative
             TE *q = p + first_col;
             const int head = (int)(((16u - (unsigned)((uintptr_t)q & 15u)) & 15u) / sizeof(TE));
             const TE *held = reinterpret_cast<const TE *>(mine);
@@ -451,7 +470,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = xr.get2(k);
     }
-    if ((!kAny && BLK) || p.h) store_row<ALIGNED, TS, E>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
+    if ((!kAny && BLK) || p.h) store_row<ALIGNED, TS, E, true>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
     if (pre_kind != FO_NORM_NONE) {
         pre = row_norm<ALIGNED, T, C>(h, pre_kind, A(p.pre.eps), inv, c, group, area, buf);
         if (!kAny || p.y) {
@@ -460,7 +479,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
             if (!kAny || p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
             if (kAny && p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
-            store_row<ALIGNED, TB, E>(p.y, row, p.ld_y, pack_row<TB, E>(h), c, ok, stage);
+            store_row<ALIGNED, TB, E, true>(p.y, row, p.ld_y, pack_row<TB, E>(h), c, ok, stage);
         }
     }
     if (p.stats && ok && c.t == 0) {
