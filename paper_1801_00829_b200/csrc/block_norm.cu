@@ -225,9 +225,8 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     if (e == cudaSuccess && n_sums > 0) {
         cs.partial = p.partial, cs.lines = lines, cs.cols = p.cols;
         const dim3 grid((unsigned)((a->cols + 31) / 32), (unsigned)n_sums);
-        if (a->block_type == FO_F64) column_sum_kernel<double><<<grid, kSumWarps * 32, 0, st>>>(cs);
-        else column_sum_kernel<float><<<grid, kSumWarps * 32, 0, st>>>(cs);
-        e = cudaGetLastError();
+        e = a->block_type == FO_F64 ? launch_beside(column_sum_kernel<double>, grid, kSumWarps * 32, st, cs)
+                                    : launch_beside(column_sum_kernel<float>, grid, kSumWarps * 32, st, cs);
     }
     return e == cudaSuccess ? FO_OK : cuda_fail(e);
 }

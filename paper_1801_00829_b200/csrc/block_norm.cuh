@@ -752,6 +752,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         }
     }
 
+    let_later_start();                                       // the sum of the lines, which waits for this kernel's end
     // the CTA's line of every sum, its groups added in order: a thread takes the piece of one thread of all groups
     __syncthreads();
     const size_t plane = (size_t)(gridDim.x / C) * p.cols;
@@ -789,6 +790,7 @@ template <class A>
 __global__ void __launch_bounds__(kSumWarps * 32) column_sum_kernel(const __grid_constant__ ColumnSumParams p)
 {
     __shared__ A sum[kSumWarps][33];
+    wait_for_earlier();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
     const A *src = static_cast<const A *>(p.partial) + (size_t)blockIdx.y * p.lines * p.cols;
     A v = A(0);

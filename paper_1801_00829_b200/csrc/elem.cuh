@@ -212,6 +212,11 @@ __device__ __forceinline__ void load16_any(uint32_t *r, const TE *p, const TE *b
     }
 }
 
+// The second kernel of a pair is launched while the first still runs: it waits here for the first one's end and what it
+// wrote.
+__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_later_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 __device__ __forceinline__ float group_rsqrt(float v) { return rsqrtf(v); }      // within 2 units
 __device__ __forceinline__ double group_rsqrt(double v) { return rsqrt(v); }
 
@@ -288,6 +293,22 @@ __device__ __forceinline__ void with_activation(int kind, Go go)
     else if (kind == FO_ACT_SIGMOID) go(std::integral_constant<int, FO_ACT_SIGMOID>());
     else if (kind == FO_ACT_SILU) go(std::integral_constant<int, FO_ACT_SILU>());
     else go(std::integral_constant<int, FO_ACT_TANH>());
+}
+
+// Launches a kernel that calls wait_for_earlier(), beside the kernel before it on the stream.
+template <class... Params, class... Args>
+cudaError_t launch_beside(void (*kern)(Params...), dim3 grid, int cta, cudaStream_t st, const Args &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)cta);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
 }  // namespace fo

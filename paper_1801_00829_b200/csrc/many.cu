@@ -19,10 +19,6 @@ constexpr int kCta = 256;
 // tensors: 119, 235 and 614 us with twice kTile, 122, 233 and 606 with 4 times, 124, 243 and 605 with 8 times).
 constexpr int kTile = 2048, kMostTile = 4 * kTile;
 
-// Kernel 2 of a pair is launched while kernel 1 runs, and waits for its results here.
-__device__ __forceinline__ void wait_for_earlier() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_later_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // ------------------------------------------------------------------- lists
 template <int N>
 struct NormList {
@@ -468,16 +464,7 @@ cudaError_t launch_clip_part(const fo_tensor *t, int count, const void *result, 
     }
     l.first[count] = l.tiles;
     if (l.tiles == 0) return cudaSuccess;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid_for(l.tiles, kPerSm));
-    cfg.blockDim = dim3(kCta);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, clip_kernel<TI, TO, N>, l, result, result_type);
+    return launch_beside(clip_kernel<TI, TO, N>, dim3(grid_for(l.tiles, kPerSm)), kCta, st, l, result, result_type);
 }
 
 template <class TI, class TO>
