@@ -397,13 +397,18 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
 // GATE: none, one per element, or one per row or column.  LEAN: every matrix read and written, root-mean-square norms
 // with weights and without biases, what transformer blocks mostly have.  Every test and every value that a form
 // does not need is one less where issuing instructions takes longer than waiting for memory (8192 x 4096
-// bf16, gate per element: gradient 131 us, with everything at run time 172; FORWARD_LEAN_FIG).
+// bf16, gate per element: gradient 131 us, with everything at run time 172; 8192 x 8192 with a stream of 32 bits: forward 133 us
+// against 146).
 enum GateForm { kNoGate = 0, kCellGate = 1, kSharedGate = 2 };
 
 // ------------------------------------------------------------------ forward
-// BLK: there is a block output f (else the norm of the stream alone).
+// BLK: there is a block output f (else the norm of the stream alone).  1024 threads share an SM with 64 registers, 1536
+// with the 40 that the stream alone needs (8192 x 4096 bf16: 25 us, with 1024 threads 31).  A row's CTA does not stay for
+// another row: a new one starts its loads while the others reduce.  8192 x 4096 bf16, gate per element: 63 us, 5.3
+// TB/s; 8192 x 8192, stream of 32 bits: 132 us, 6.1 TB/s (peak of a copy: 6.5).
 template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int GATE, bool LEAN>
-__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta, sizeof(Acc<TB>) == 4 ? (T > 0 ? 4 : 2) : 1)
+__global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta,
+                                  sizeof(Acc<TB>) == 8 ? 1 : T > 0 ? (BLK ? 4 : 6) : (BLK ? 2 : 3))
 block_norm_kernel(const __grid_constant__ BlockNormParams p)
 {
     using A = Acc<TB>;

@@ -386,13 +386,13 @@ constexpr int kFew = 40, kMany = 512, kManyAdam = 256;      // tensors of one la
 
 unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
 
-// Tile size and grid of a part of a list: about 4 tiles for each of `per_sm` CTAs on every SM.
+// Tile size of a part of a list: about `per_cta` tiles for each of `per_sm` CTAs on every SM.
 template <class Tensor>
-int tile_for(const Tensor *t, int count, int per_sm)
+int tile_for(const Tensor *t, int count, int per_sm, int per_cta)
 {
     long long total = 0;
     for (int k = 0; k < count; ++k) total += t[k].n;
-    const long long each = total / ((long long)sm_count() * per_sm * 4 + 1) / kTile + 1;
+    const long long each = total / ((long long)sm_count() * per_sm * per_cta + 1) / kTile + 1;
     return (int)(each * kTile < kMostTile ? each * kTile : kMostTile);
 }
 unsigned grid_for(unsigned tiles, int per_sm)
@@ -423,7 +423,7 @@ cudaError_t launch_norm_part(const fo_tensor *t, int count, int kind, const Norm
 {
     constexpr int kPerSm = kNormPerSm;
     NormList<N> l;
-    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm);
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm, 4);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.n[k] = t[k].n;
         l.tiles += tiles_of(t[k].n, l.tile);
@@ -457,7 +457,7 @@ cudaError_t launch_clip_part(const fo_tensor *t, int count, const void *result, 
 {
     constexpr int kPerSm = kClipPerSm;
     ClipList<N> l;
-    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm);
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, kPerSm, 4);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles, l.in[k] = t[k].in, l.out[k] = t[k].out, l.n[k] = t[k].n;
         l.tiles += tiles_of(t[k].n, l.tile);
@@ -492,7 +492,7 @@ cudaError_t launch_adam_part(const fo_adam_tensor *t, int count, const AdamHyper
     }
     const int per_sm = total < kAdamLong ? 4 : aligned ? 2 : 3;
     AdamList<N> l;
-    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, per_sm);
+    l.count = count, l.tiles = 0, l.tile = tile_for(t, count, per_sm, 4);
     for (int k = 0; k < count; ++k) {
         l.first[k] = l.tiles;
         l.p[k] = t[k].p, l.g[k] = t[k].g, l.m[k] = t[k].m, l.v[k] = t[k].v;

@@ -1,6 +1,6 @@
 """The training-step operators (include/fusedops_train.h): block norm and its gradient, gradient
-clipping and AdamW over many tensors.  Argument checks and marshalling only, like binding.py; those of the block
-norm are in a CPython extension (csrc/training_py.cpp).
+clipping and AdamW over many tensors.  Argument checks and marshalling only, like binding.py; the calls
+themselves are in a CPython extension (csrc/training_py.cpp).
 
 Norms are given as ``(kind, weight, bias, eps)`` with kind "rms" or "layer" and weight / bias a vector
 or None; a gate as ``(access, tensor, activation)`` with access "cell", "row" or "col" as for
@@ -14,7 +14,7 @@ import struct
 import torch
 
 from . import build as _build
-from .binding import FusedOpsError, _check, load_library, workspace
+from .binding import FusedOpsError, load_library, workspace
 
 DTYPES = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
 GRAD_NORM_KIND = {"l2": 0, "max": 1}
@@ -25,40 +25,11 @@ def _require(ok, text):
         raise ValueError(text)
 
 
-# The current stream's handle as a number, without a Stream object around it where this torch has that call.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
 def _index(t):
     """Number of the GPU that a tensor is on."""
     index = t.get_device()
     _require(index >= 0, "fused operators need CUDA tensors (no CPU path)")
     return index
-
-
-def _call(name, index, *args):
-    """Calls a C entry on the current stream of GPU `index`, which is made current if another one is."""
-    fn = getattr(load_library(), name)
-    if index == torch.cuda.current_device():
-        status = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
-            status = fn(*args, _raw_stream(index))
-    if status:
-        _check(status, name)
-
-
-_scratch = {}
-
-
-def _workspace(index, nbytes):
-    """(address, size) of the current stream's scratch (binding.workspace), looked up by numbers."""
-    key = (index, _raw_stream(index))
-    buf = _scratch.get(key)
-    if buf is None or buf.numel() < nbytes:
-        buf = _scratch[key] = workspace(torch.device("cuda", index), nbytes)
-    return buf.data_ptr(), buf.numel()
 
 
 _extension = None
@@ -134,6 +105,7 @@ class TensorList:
         flat = [v for g, o in zip(self.grads, self.outs) for v in (g.data_ptr(), o.data_ptr(), g.numel())]
         self.packed = struct.pack("QQq" * len(self.grads), *flat)
         self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.out_dtype, 1)
+        self.index = None if self.device is None else self.device.index
 
     def __len__(self):
         return len(self.grads)
@@ -144,31 +116,27 @@ def tensor_list(grads, outs=None):
     return TensorList(grads, outs)
 
 
-def _grad_call(name, grads, kind, max_norm, eps, result_type, device, types):
+def _grad_call(grads, clip, kind, max_norm, eps, result_type, device):
     grads = grads if isinstance(grads, TensorList) else TensorList(grads)
-    _require(result_type in (torch.float32, torch.float64), "results are float32 or float64")
+    wide = result_type is torch.float64
+    _require(wide or result_type is torch.float32, "results are float32 or float64")
     _require(kind in GRAD_NORM_KIND, "norm kind %r" % (kind,))
-    if grads.device is not None:
-        device = grads.device
-    elif device is None:                                     # an empty list
-        device = torch.device("cuda", torch.cuda.current_device())
-    result = torch.empty(2, dtype=result_type, device=device)
-    index = result.get_device()
-    ws = _workspace(index, load_library().fused_grad_workspace_bytes())
-    _call(name, index, grads.packed, len(grads.grads), *grads.types[:types], GRAD_NORM_KIND[kind], max_norm, eps,
-          result.data_ptr(), DTYPES[result_type], *ws)
-    return result
+    index = grads.index
+    if index is None:                                        # an empty list
+        index = torch.cuda.current_device() if device is None else torch.device(device).index
+    return (_extension or _native()).grad_norm(grads.packed, clip, *grads.types, GRAD_NORM_KIND[kind], max_norm, eps,
+                                               0 if wide else 1, index)
 
 
 def fused_grad_norm(grads, max_norm, kind="l2", eps=1e-6, result_type=torch.float32, device=None):
     """(norm, factor) of all gradients together, as a tensor of two on the device: the "l2" or "max" norm and
     min(1, max_norm / (norm + eps)).  grads: a TensorList or a list of tensors; device: for an empty list."""
-    return _grad_call("fused_grad_norm", grads, kind, max_norm, eps, result_type, device, 1)
+    return _grad_call(grads, False, kind, max_norm, eps, result_type, device)
 
 
 def fused_grad_clip(grads, max_norm, kind="l2", eps=1e-6, result_type=torch.float32, device=None):
     """fused_grad_norm, and every gradient times the factor into the list's outs (or in place)."""
-    return _grad_call("fused_grad_clip", grads, kind, max_norm, eps, result_type, device, 2)
+    return _grad_call(grads, True, kind, max_norm, eps, result_type, device)
 
 
 class AdamList:
@@ -200,6 +168,7 @@ class AdamList:
             flat += [ts[k].data_ptr() for ts in lists] + none + [self.grads[k].numel(), decay[k]]
         self.packed = struct.pack("8Qqd" * n, *flat)
         self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.weight_dtype, 0)
+        self.index = None if self.device is None else self.device.index
 
     def __len__(self):
         return len(self.grads)
@@ -216,10 +185,4 @@ def fused_adamw(tensors, lr, betas=(0.9, 0.999), eps=1e-8, step=1, factor=None):
     gradients are multiplied by (result[1:2] of fused_grad_norm)."""
     if len(tensors) == 0:
         return
-    kind, at = 0, 0
-    if factor is not None:
-        _require(factor.numel() == 1 and factor.device == tensors.device and factor.dtype in (torch.float32, torch.float64),
-                 "factor is not one float on the gradients' device")
-        kind, at = DTYPES[factor.dtype], factor.data_ptr()
-    _call("fused_adamw", tensors.device.index, tensors.packed, len(tensors.grads), *tensors.types, lr, betas[0], betas[1],
-          eps, step, at, kind)
+    (_extension or _native()).adamw(tensors.packed, *tensors.types, lr, betas[0], betas[1], eps, step, factor, tensors.index)

@@ -224,6 +224,17 @@ def test_empty():
         assert got["x"].shape == (rows, cols) and bool((got["pre_w"] == 0).all()) and bool((got["post_w"] == 0).all())
 
 
+def test_without_a_gradient_of_y_or_of_h():
+    c = Case(19, 130, BF16, BF16, "rms", "cell", "silu", "layer", bias=True)
+    h, stats = c.check_forward()
+    c.check_backward(h, stats, dh=None)
+    got = fo.fused_block_norm_grad(c.dh, None, h, c.f, stats, **c.how())
+    want = ref.block_norm_grad(host(c.dh), None, host(h), host(c.f), host(stats), **c.host_how())
+    assert torch.equal(got["x"], c.dh) and bool((got["pre_w"] == 0).all()) and bool((got["pre_b"] == 0).all())
+    close(got["f"], *want["f"], unit(BF16), "f")
+    close(got["post_w"], *want["post_w"], unit(BF16), "post_w", rows=19)
+
+
 def test_the_same_bits_twice():
     c = Case(600, 1000, BF16, BF16, "layer", "col", "silu", "layer", bias=True)
     h, stats = c.check_forward()
