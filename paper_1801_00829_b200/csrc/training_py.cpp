@@ -223,6 +223,8 @@ PyObject *block_norm_impl(PyObject *const *a)
         if (a[10] != Py_None) {
             require(THPDtype_Check(a[10]), "block_type is not a dtype");
             block = reinterpret_cast<THPDtype *>(a[10])->scalar_type;
+        } else if (!out_y && stream == at::kFloat) {
+            block = vector_type(block, post, pre, col_scale);       // 16-bit weights: the next block's type
         }
     }
     require(!out_y || pre.given(), "out_y without a norm before the next block");

@@ -224,6 +224,15 @@ def test_empty():
         assert got["x"].shape == (rows, cols) and bool((got["pre_w"] == 0).all()) and bool((got["post_w"] == 0).all())
 
 
+@pytest.mark.parametrize("stream,vec,out", [(F32, BF16, BF16), (F32, F16, F16), (F32, F32, F32), (BF16, F32, BF16), (F64, F64, F64)])
+def test_type_of_the_norm_of_the_stream_alone(stream, vec, out):
+    x, w = torch.randn(5, 64, device="cuda").to(stream), torch.ones(64, dtype=vec, device="cuda")
+    _, y, _ = fo.fused_block_norm(x, pre=("rms", w, None, 1e-6))
+    assert y.dtype == out
+    want = ref.block_norm(host(x), None, None, None, 1.0, None, ("rms", host(w), None, 1e-6))
+    close(y, *want["y"], unit(stream), "y")
+
+
 def test_without_a_gradient_of_y_or_of_h():
     c = Case(19, 130, BF16, BF16, "rms", "cell", "silu", "layer", bias=True)
     h, stats = c.check_forward()
