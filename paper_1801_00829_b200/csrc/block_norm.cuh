@@ -103,7 +103,7 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
         if constexpr (ALIGNED) {
             load16(w, p + j);
         } else {
-            load16_any(w, p + j, begin, begin + (rows - 1) * ld + c.cols);
+            load16_any<true>(w, p + j, begin, begin + (rows - 1) * ld + c.cols);
             if (j + kStep > c.cols) {                        // the row ends inside: zeros from there
                 Packed<TE, kStep> whole, part;
 #pragma unroll

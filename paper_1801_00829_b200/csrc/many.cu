@@ -221,7 +221,7 @@ __device__ __forceinline__ void load_some(Packed<T, V> &r, const T *p, bool alig
         else load16(r.w, p);
     } else {
 #pragma unroll
-        for (int k = 0; k < V; k += kStep) load16_any(r.w + k * (int)sizeof(T) / 4, p + k, begin, end);
+        for (int k = 0; k < V; k += kStep) load16_any<false>(r.w + k * (int)sizeof(T) / 4, p + k, begin, end);
     }
 }
 template <class T, int V>
@@ -251,7 +251,7 @@ __device__ __forceinline__ double read_factor(const void *factor, int type)
 }
 
 // The tiles in the opposite order of the norm's: what it read last is still in L2.
-constexpr int kClipPerSm = 8;                // CTAs; with 4 pieces in flight and 5 CTAs, 260M bf16: 376 us, so 368
+constexpr int kClipPerSm = 7;                // CTAs (260M bf16, with the norm: 349 us; 8 of them 357; 5 with 4 pieces each 376)
 
 template <class TI, class TO, int N>
 __global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kClipPerSm) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
