@@ -561,6 +561,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     const A *stats = static_cast<const A *>(p.stats);
     const bool wide = p.wide_vec != 0;
     using Sums = SumPieces<E, A>;
+    // lean: the mean is 0
+    const auto centred = [](Two<A> v, Two<A> minus_mean) { return LEAN ? v : v + minus_mean; };
     constexpr bool kAny = !LEAN;
     const bool pre = !kAny || p.dy != nullptr, pre_layer = kAny && p.pre.kind == FO_NORM_LAYER;
     const bool pre_weight = !kAny || p.pre.weight != nullptr, post_weight = !kAny || p.post.weight != nullptr;
@@ -606,7 +608,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         Two<A> t[E / 2];
         if (pre) {
             const A r1 = ok ? stats[3 * p.rows + row] : A(0);
-            const Two<A> minus = both(ok ? -stats[2 * p.rows + row] : A(0)), r = both(r1);
+            const Two<A> minus = both(kAny && ok ? -stats[2 * p.rows + row] : A(0)), r = both(r1);
             Two<A> along = both(A(0)), level = both(A(0));
 #pragma unroll
             for (int k0 = 0; k0 < E; k0 += P) {
@@ -614,7 +616,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
                 for (int i = 0; i < P / 2; ++i) {
                     a[i] = dyr.get2(k0 + 2 * i);
-                    n[i] = (hr.get2(k0 + 2 * i) + minus) * r;
+                    n[i] = centred(hr.get2(k0 + 2 * i), minus) * r;
                 }
                 add(kPreW, k0, [&](int i, Two<A> s) { return fused_ma(a[i], n[i], s); });
                 add(kPreB, k0, [&](int i, Two<A> s) { return s + a[i]; });
@@ -642,7 +644,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
             along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
             for (int k = 0; k < E; k += 2)
-                t[k / 2] = fused_ma(t[k / 2], r, fused_ma(hr.get2(k) + minus, along, dhr.get2(k) + level));
+                t[k / 2] = fused_ma(t[k / 2], r, fused_ma(centred(hr.get2(k), minus), along, LEAN ? dhr.get2(k) : dhr.get2(k) + level));
             if (ragged) {
 #pragma unroll
                 for (int k = 0; k < E; k += 2) t[k / 2] = c.template inside<ALIGNED>(k, t[k / 2]);
@@ -654,7 +656,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
         if (!kAny || p.dx) store_row<ALIGNED, TS, E>(p.dx, row, p.ld_dx, pack_row<TS, E>(t), c, ok, stage);
         if constexpr (BLK) {
             const A r1 = ok && normed ? stats[p.rows + row] : A(1);
-            const Two<A> minus = both(ok && normed ? -stats[row] : A(0)), r = both(r1), scale = both(A(p.scale));
+            const Two<A> minus = both(kAny && ok && normed ? -stats[row] : A(0)), r = both(r1), scale = both(A(p.scale));
             Two<A> row_act = both(A(1)), row_slope = both(A(0));
             if (row_gate) {
                 const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
@@ -672,7 +674,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     for (int i = 0; i < P / 2; ++i) w[i] = both(A(1));
 #pragma unroll
                 for (int i = 0; i < P / 2; ++i) {
-                    n[i] = (fr.get2(k0 + 2 * i) + minus) * r;
+                    n[i] = centred(fr.get2(k0 + 2 * i), minus) * r;
                     z[i] = n[i] * w[i];
                     d[i] = d[i] * scale;
                 }
@@ -751,7 +753,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
                 for (int k = 0; k < E; k += 2)
-                    t[k / 2] = fused_ma(t[k / 2], r, fused_ma(fr.get2(k) + minus, along, level));
+                    t[k / 2] = fused_ma(t[k / 2], r, LEAN ? centred(fr.get2(k), minus) * along : fused_ma(centred(fr.get2(k), minus), along, level));
             }
             if (!kAny || p.df) store_row<ALIGNED, TB, E>(p.df, row, p.ld_df, pack_row<TB, E>(t), c, ok, stage);
         }

@@ -303,6 +303,36 @@ def test_on_a_stream_of_its_own():
     assert torch.equal(h0, h1) and torch.equal(y0, y1) and all(torch.equal(g0[k], g1[k]) for k in g0)
 
 
+def test_offsets_beyond_32_bits():
+    """2.2e9 elements: the last rows lie where a 32-bit offset would have wrapped."""
+    rows, cols = 270000, 8192
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB")
+    x = torch.ones(rows, cols, dtype=BF16, device="cuda")
+    tail = torch.randn(3, cols, device="cuda").to(BF16)
+    x[-3:] = tail
+    w = torch.ones(cols, dtype=BF16, device="cuda")
+    _, y, stats = fo.fused_block_norm(x, pre=("rms", w, None, 1e-6), stats=True)
+    want = ref.block_norm(host(tail), None, None, None, 1.0, None, ("rms", host(w), None, 1e-6))
+    close(y[-3:], *want["y"], unit(BF16), "y")
+    assert bool((y[:-3:1000] == 1).all())
+    got = fo.fused_block_norm_grad(None, y, x, None, stats, pre=("rms", w, None, 1e-6))
+    wide = ref.block_norm_grad(None, host(y[-3:]), host(tail), None, host(stats[:, -3:]), None, None, 1.0, None,
+                               ("rms", host(w), None, 1e-6))
+    close(got["x"][-3:], *wide["x"], unit(BF16), "x")
+
+
+def test_a_tensor_of_more_than_32_bits():
+    n = (1 << 31) + 12345
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("needs 12 GB")
+    g = torch.zeros(n, dtype=BF16, device="cuda")
+    g[-1], g[1 << 31], g[5] = 3.0, 4.0, 12.0
+    norm, factor = host(fo.fused_grad_clip([g], 6.5, eps=0.0))
+    assert norm == 13.0 and factor == 0.5
+    assert g[-1].item() == 1.5 and g[1 << 31].item() == 2.0 and g[5].item() == 6.0
+
+
 # ------------------------------------------------------------------ many tensors
 SIZES = {"one": [1], "tiny": [1, 0, 3, 7, 8, 9, 15, 16, 17, 31, 0], "tile": [8191, 8192, 8193, 16384, 5],
          "ragged": [100003, 64, 1, 33333, 7, 250000, 4097], "forty": [777] * 40, "many": [50 + 13 * (k % 29) for k in range(1100)]}
