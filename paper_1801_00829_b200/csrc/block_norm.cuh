@@ -185,22 +185,20 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
             const int head = (int)(((16u - (unsigned)((uintptr_t)q & 15u)) & 15u) / sizeof(TE));
             const TE *held = reinterpret_cast<const TE *>(mine);
             if (lane < head && lane < n) q[lane] = held[lane];
+            const int full = n > head ? (n - head) / kStep : 0;                  // aligned chunks
 #pragma unroll
             for (int i = 0; i < kChunks; ++i) {
-                const int at = head + (lane + i * kLanes) * kStep;
-                if (at + kStep <= n) {
-                    const uint4 *a = reinterpret_cast<const uint4 *>(held + at / kStep * kStep);
-                    const uint4 x = a[0], y = head ? a[1] : x;
-                    const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                    uint32_t r[4];
-                    straddle(r, u, (unsigned)(head * (int)sizeof(TE)));
-                    store16(q + at, r);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < kStep; ++e)
-                        if (at + e < n) q[at + e] = held[at + e];
-                }
+                const int chunk = lane + i * kLanes;
+                if (chunk >= full) continue;
+                const uint4 *a = reinterpret_cast<const uint4 *>(held + chunk * kStep);
+                const uint4 x = a[0], y = head ? a[1] : x;
+                const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                uint32_t r[4];
+                straddle(r, u, (unsigned)(head * (int)sizeof(TE)));
+                store16(q + head + chunk * kStep, r);
             }
+            const int last = head + full * kStep + lane;
+            if (lane < kStep && last < n) q[last] = held[last];
         }
     }
 }
