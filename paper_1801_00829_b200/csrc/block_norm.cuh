@@ -425,6 +425,8 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     const auto times = [](Two<A> h, Two<A> w) { return h * w; };
     const auto plus = [](Two<A> h, Two<A> b) { return h + b; };
 
+    wait_for_earlier();
+    let_later_start();
     Packed<TS, E> xr;
     Packed<TB, E> fr, gr;
     if (BLK) load_row<ALIGNED, TB, E>(fr, p.f, p.rows, row, p.ld_f, c, ok);
@@ -589,6 +591,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     for (int s = 0; s < n_slots; ++s)
         Sums::template change<E>(sums + s * cta * E, 0, [](int, Two<A>) { return both(A(0)); });
 
+    wait_for_earlier();
     // all threads of a group, and all CTAs of a cluster, take the same number of turns: their sums meet at barriers
     for (long long row0 = (long long)(blockIdx.x / C) * groups; row0 < p.rows;
          row0 += (long long)(gridDim.x / C) * groups) {
