@@ -94,6 +94,9 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
         }
         return;
     }
+    // an unaligned row's pieces reach 15 bytes before it and 47 behind its last whole one
+    const TE *end = begin + (rows - 1) * ld + c.cols;
+    const bool inner = !ALIGNED && p - begin >= 16 / (int)sizeof(TE) && end - (p + c.cols) >= 48 / (int)sizeof(TE);
 #pragma unroll
     for (int k = 0; k < E; k += kStep) {
         uint32_t *w = r.w + k * (int)sizeof(TE) / 4;
@@ -103,7 +106,7 @@ __device__ __forceinline__ void load_row(Packed<TE, E> &r, const void *base, lon
         if constexpr (ALIGNED) {
             load16(w, p + j);
         } else {
-            load16_any<true>(w, p + j, begin, begin + (rows - 1) * ld + c.cols);
+            load16_any<true>(w, p + j, begin, end, inner);
             if (j + kStep > c.cols) {                        // the row ends inside: zeros from there
                 Packed<TE, kStep> whole, part;
 #pragma unroll
@@ -194,7 +197,7 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
                 const uint4 x = a[0], y = head ? a[1] : x;
                 const uint32_t u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                 uint32_t r[4];
-                straddle(r, u, (unsigned)(head * (int)sizeof(TE)));
+                straddle<(int)sizeof(TE)>(r, u, (unsigned)(head * (int)sizeof(TE)));
                 store16(q + head + chunk * kStep, r);
             }
             const int last = head + full * kStep + lane;
@@ -402,8 +405,8 @@ enum GateForm { kNoGate = 0, kCellGate = 1, kSharedGate = 2 };
 // ------------------------------------------------------------------ forward
 // BLK: there is a block output f (else the norm of the stream alone).  1024 threads share an SM with 64 registers, 1536
 // with the 40 that the stream alone needs (8192 x 4096 bf16: 25 us, with 1024 threads 31).  A row's CTA does not stay for
-// another row: a new one starts its loads while the others reduce.  8192 x 4096 bf16, gate per element: 63 us, 5.3
-// TB/s; 8192 x 8192, stream of 32 bits: 132 us, 6.1 TB/s (peak of a copy: 6.5).
+// another row: a new one starts its loads while the others reduce.  8192 x 4096 bf16, gate per element: 61 us, 5.5
+// TB/s; 8192 x 8192, stream of 32 bits: 129 us, 6.2 TB/s (peak of a copy: 6.5).
 template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int GATE, bool LEAN>
 __global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta,
                                   sizeof(Acc<TB>) == 8 ? 1 : T > 0 ? (BLK ? 4 : 6) : (BLK ? 2 : 3))

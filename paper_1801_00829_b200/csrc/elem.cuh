@@ -173,38 +173,40 @@ __device__ __forceinline__ void store16(void *p, const uint32_t *w)
                  : "memory");
 }
 
-// 16 bytes from byte `q` (0 .. 15, a multiple of the element's size) of 32.
+// 16 bytes from byte `q` (0 .. 15, a multiple of the element's SIZE) of 32.
+template <int SIZE>
 __device__ __forceinline__ void straddle(uint32_t *r, const uint32_t (&w)[8], unsigned q)
 {
     uint32_t a[7], b[5];
 #pragma unroll
-    for (int i = 0; i < 7; ++i) a[i] = (q & 4u) ? w[i + 1] : w[i];
+    for (int i = 0; i < 7; ++i) a[i] = SIZE < 8 && (q & 4u) ? w[i + 1] : w[i];
 #pragma unroll
     for (int i = 0; i < 5; ++i) b[i] = (q & 8u) ? a[i + 2] : a[i];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __funnelshift_r(b[i], b[i + 1], (q & 3u) * 8u);
+    for (int i = 0; i < 4; ++i) r[i] = SIZE < 4 ? __funnelshift_r(b[i], b[i + 1], (q & 3u) * 8u) : b[i];
 }
 
 // 16 bytes from any address, through L1 (the next thread reads the second half too).  Nothing outside
 // [begin, end), the matrix's or tensor's own bytes, is read; what lies there is given as zeros.
 // OFTEN: addresses are often aligned, and then one load is all (where they seldom are, the second test costs more:
 // AdamW over 130M parameters 600 us without it, 640 with).
+// inner: known to be far enough from both ends.
 template <bool OFTEN, class TE>
-__device__ __forceinline__ void load16_any(uint32_t *r, const TE *p, const TE *begin, const TE *end)
+__device__ __forceinline__ void load16_any(uint32_t *r, const TE *p, const TE *begin, const TE *end, bool inner = false)
 {
     const unsigned q = (unsigned)((uintptr_t)p & 15u);
     const char *base = reinterpret_cast<const char *>(p) - q;
     const uint4 *a = reinterpret_cast<const uint4 *>(base);
-    if (OFTEN && q == 0 && base + 16 <= reinterpret_cast<const char *>(end)) {
+    if (OFTEN && q == 0 && (inner || base + 16 <= reinterpret_cast<const char *>(end))) {
         const uint4 u = a[0];
         r[0] = u.x, r[1] = u.y, r[2] = u.z, r[3] = u.w;
-    } else if (base >= reinterpret_cast<const char *>(begin) && base + 32 <= reinterpret_cast<const char *>(end)) {
+    } else if (inner || (base >= reinterpret_cast<const char *>(begin) && base + 32 <= reinterpret_cast<const char *>(end))) {
         uint32_t w[8];
         uint4 u = a[0];
         w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
         if (OFTEN || q) u = a[1];
         w[4] = u.x, w[5] = u.y, w[6] = u.z, w[7] = u.w;
-        straddle(r, w, q);
+        straddle<(int)sizeof(TE)>(r, w, q);
     } else {
         constexpr int N = 16 / (int)sizeof(TE);
         Packed<TE, N> v;
