@@ -9,7 +9,7 @@
  * pointers of the caller; the structs are HOST memory, copied at launch, free on return.  Calls
  * are asynchronous on `stream`, allocate nothing, never synchronise, and return FO_OK or a
  * negative fo_status; on an error nothing was launched.  Sums are deterministic: their order is
- * fixed by the sizes.  Workspaces are prepared once with fo_workspace_init().
+ * fixed by the sizes, the alignments and the GPU.  Workspaces are prepared once with fo_workspace_init().
  *
  * Element types: the templates' float64, and float32, bfloat16 and float16 as models use them.
  * Arithmetic, statistics and sums are in 32 bits (in 64 where a type is float64); a result in
@@ -116,9 +116,9 @@ size_t fused_block_norm_grad_workspace_bytes(int64_t rows, int64_t cols, int blo
  * fused_grad_norm writes `result` only (`out` is not looked at); fused_grad_clip also every `out`,
  * which may be `in` itself - a clip in place whose factor is 1 writes nothing.
  * The tensors of a call share in_type and out_type.  16-bit and 32-bit values are squared and
- * added in 32 bits within a tile and in 64 bits over the tiles; a tile whose 32-bit sum would
- * leave the normal range is added in 64 bits, so gradients near either end of the range have
- * their norm too.  A NaN anywhere makes norm and factor NaN; an infinity makes the norm infinite
+ * added in 32 bits for a few neighbouring values (at most 32) and in 64 bits over these; values whose
+ * 32-bit sum would leave the normal range are added in 64 bits from the start, so gradients near either end
+ * of the range have their norm too.  A NaN anywhere makes norm and factor NaN; an infinity makes the norm infinite
  * and the factor zero (out: zero, NaN where the infinity was).
  */
 enum { FO_NORM_L2 = 0, FO_NORM_MAX = 1 };

@@ -60,8 +60,9 @@ struct BlockNormGradParams {
 
 // Which columns a thread holds: pieces of V elements, 16 bytes of the block's type.  Piece v of thread t covers
 // columns (v * threads + t) * V .. + V - 1.  ALIGNED: every row of every matrix begins where a piece may (a
-// 16-byte boundary, 32 for a stream of wider elements) and is whole pieces long; else rows may begin and end anywhere, and 16 bytes that straddle a boundary are
-// put together from the two aligned 16 bytes they lie in.  Values outside the row are held as zeros.
+// 16-byte boundary, 32 for a stream of wider elements) and is whole pieces long; else rows may begin and end
+// anywhere, and 16 bytes that straddle a boundary are put together from the two aligned 16 bytes they lie in.
+// Values outside the row are held as zeros.
 template <int T, int V>                        // T: threads of the row, 0: the CTAs' threads
 struct Columns {
     int t, cols, count;                        // count: threads of the row
@@ -183,7 +184,8 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
             }
             __syncwarp();
             const int first_col = c.of(k) - lane * V, left = c.cols - first_col;
-            const int n = !ok || (DIRECT && T > 0 && ((uintptr_t)p & 15u) == 0) ? 0 : left < kLanes * V ? left : kLanes * V;       // elements to write, may be negative
+            const bool written = DIRECT && T > 0 && ((uintptr_t)p & 15u) == 0;
+            const int n = !ok || written ? 0 : left < kLanes * V ? left : kLanes * V;     // elements to write, may be negative
             TE *q = p + first_col;
             const int head = (int)(((16u - (unsigned)((uintptr_t)q & 15u)) & 15u) / sizeof(TE));
             const TE *held = reinterpret_cast<const TE *>(mine);
@@ -370,7 +372,8 @@ struct RowNorm {
     A mean, r;
 };
 template <bool ALIGNED, int T, int C, int E, class A, class Cols>
-__device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, const Group &g, Area<A> &area, int &buf)
+__device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, const Group &g,
+                                               Area<A> &area, int &buf)
 {
     RowNorm<A> n = {A(0), A(0)};
     A s[1];
@@ -398,8 +401,8 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
 // GATE: none, one per element, or one per row or column.  LEAN: every matrix read and written, root-mean-square norms
 // with weights and without biases, what transformer blocks mostly have.  Every test and every value that a form
 // does not need is one less where issuing instructions takes longer than waiting for memory (8192 x 4096
-// bf16, gate per element: gradient 126 us, with everything at run time 172; 8192 x 8192 with a stream of 32 bits: forward 133 us
-// against 146).
+// bf16, gate per element: gradient 126 us, with everything at run time 172; 8192 x 8192 with a stream of 32 bits:
+// forward 133 us against 146).
 enum GateForm { kNoGate = 0, kCellGate = 1, kSharedGate = 2 };
 
 // ------------------------------------------------------------------ forward
@@ -419,7 +422,8 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     __shared__ Stage<TS, V, T, ALIGNED> stages;
     unsigned char *const stage = stages.of_warp();
     int buf = 0;
-    const long long row = T > 0 ? (long long)blockIdx.x * (kGroupCta / kDivisor<T>) + threadIdx.x / kDivisor<T> : blockIdx.x / C;
+    const long long row = T > 0 ? (long long)blockIdx.x * (kGroupCta / kDivisor<T>) + threadIdx.x / kDivisor<T>
+                                : blockIdx.x / C;
     const bool ok = row < p.rows;
     const Group group = {0, (int)blockDim.x};
     const Columns<T, V> c = columns_of<T, C, V>(p.cols, p.vectors != 0, group);
@@ -650,7 +654,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
             along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
             for (int k = 0; k < E; k += 2)
-                t[k / 2] = fused_ma(t[k / 2], r, fused_ma(centred(hr.get2(k), minus), along, LEAN ? dhr.get2(k) : dhr.get2(k) + level));
+                t[k / 2] = fused_ma(t[k / 2], r, fused_ma(centred(hr.get2(k), minus), along,
+                                                          LEAN ? dhr.get2(k) : dhr.get2(k) + level));
             if (ragged) {
 #pragma unroll
                 for (int k = 0; k < E; k += 2) t[k / 2] = c.template inside<ALIGNED>(k, t[k / 2]);
@@ -759,7 +764,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                 along = both(-s[0] * inv * r1 * r1), level = both(-s[1] * inv * r1);
 #pragma unroll
                 for (int k = 0; k < E; k += 2)
-                    t[k / 2] = fused_ma(t[k / 2], r, LEAN ? centred(fr.get2(k), minus) * along : fused_ma(centred(fr.get2(k), minus), along, level));
+                    t[k / 2] = fused_ma(t[k / 2], r, LEAN ? centred(fr.get2(k), minus) * along
+                                                          : fused_ma(centred(fr.get2(k), minus), along, level));
             }
             if (!kAny || p.df) store_row<ALIGNED, TB, E>(p.df, row, p.ld_df, pack_row<TB, E>(t), c, ok, stage);
         }

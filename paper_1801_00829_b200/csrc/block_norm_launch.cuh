@@ -9,7 +9,7 @@ namespace fo {
 template <class TS, class TB>
 cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t st);
 template <class TS, class TB>
-cudaError_t launch_block_norm_grad(BlockNormGradParams p, int max_lines, int *lines, cudaStream_t st);      // lines: of partial sums
+cudaError_t launch_block_norm_grad(BlockNormGradParams p, int max_lines, int *lines, cudaStream_t st);   // of partial sums
 
 // Calls go(T, C, E, threads) with the shape for `cols` columns in pieces of V: T threads of a warp and CTAs of
 // kGroupCta, or (T = 0) C CTAs of `threads` a row; 16 elements a thread where a row has them.  A sum over the
@@ -44,7 +44,8 @@ cudaError_t with_grad_shape(int cols, Go go)
     if (cols <= 128) return FO_SHAPE(16, 1, kGroupCta);
     if (cols <= 256) return FO_SHAPE(32, 1, kGroupCta);
     const int c = cols <= 4096 ? 1 : cols <= 8192 ? 2 : cols <= 16384 ? 4 : 8;
-    const int pieces = (cols + V - 1) / V, per_cta = kGradE / V * c, threads = ((pieces + per_cta - 1) / per_cta + 31) / 32 * 32;
+    const int pieces = (cols + V - 1) / V, per_cta = kGradE / V * c;
+    const int threads = ((pieces + per_cta - 1) / per_cta + 31) / 32 * 32;
     if (c == 1) return FO_SHAPE(0, 1, threads);
     if (c == 2) return FO_SHAPE(0, 2, threads);
     if (c == 4) return FO_SHAPE(0, 4, threads);
@@ -86,7 +87,8 @@ cudaError_t launch_block_norm(const BlockNormParams &p, cudaStream_t st)
         };
         auto with_gate = [&](auto aligned, auto lean) -> cudaError_t {
             if (p.gate_access < 0) return go(aligned, std::true_type(), std::integral_constant<int, kNoGate>(), lean);
-            if (p.gate_access == FO_AT_CELL) return go(aligned, std::true_type(), std::integral_constant<int, kCellGate>(), lean);
+            if (p.gate_access == FO_AT_CELL)
+                return go(aligned, std::true_type(), std::integral_constant<int, kCellGate>(), lean);
             return go(aligned, std::true_type(), std::integral_constant<int, kSharedGate>(), lean);
         };
         const auto none = std::integral_constant<int, kNoGate>();
@@ -157,7 +159,8 @@ cudaError_t launch_block_norm_grad(BlockNormGradParams p, int max_lines, int *li
         };
         auto with_gate = [&](auto aligned, auto lean) -> cudaError_t {
             if (p.gate_access < 0) return go(aligned, std::true_type(), std::integral_constant<int, kNoGate>(), lean);
-            if (p.gate_access == FO_AT_CELL) return go(aligned, std::true_type(), std::integral_constant<int, kCellGate>(), lean);
+            if (p.gate_access == FO_AT_CELL)
+                return go(aligned, std::true_type(), std::integral_constant<int, kCellGate>(), lean);
             return go(aligned, std::true_type(), std::integral_constant<int, kSharedGate>(), std::false_type());
         };
         const auto none = std::integral_constant<int, kNoGate>();

@@ -162,7 +162,8 @@ __device__ __forceinline__ double cta_join(double v, double *smem)     // result
 constexpr int kNormPerSm = 5;                // CTAs, of 51 registers a thread: four 16-byte pieces and their sums
 
 template <class T, int N, int KIND>
-__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kNormPerSm) grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
+__global__ void __launch_bounds__(kCta, sizeof(T) == 8 ? 4 : kNormPerSm)
+grad_norm_kernel(const __grid_constant__ NormList<N> l, const NormOut o)
 {
     constexpr int V = 16 / (int)sizeof(T);
     constexpr int kBatch = 4;                // pieces of a thread in flight
@@ -255,8 +256,8 @@ __device__ __forceinline__ double read_factor(const void *factor, int type)
 constexpr int kClipPerSm = 7;                // CTAs (260M bf16, with the norm: 349 us; 8 of them 357; 5 with 4 pieces each 376)
 
 template <class TI, class TO, int N>
-__global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kClipPerSm) clip_kernel(const __grid_constant__ ClipList<N> l, const void *result,
-                                                    int result_type)
+__global__ void __launch_bounds__(kCta, sizeof(TI) == 8 ? 4 : kClipPerSm)
+clip_kernel(const __grid_constant__ ClipList<N> l, const void *result, int result_type)
 {
     using A = Acc<TI>;
     constexpr int V = 16 / (int)sizeof(TI);
