@@ -290,6 +290,18 @@ __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// A CTA's shared memory exists for the others of its cluster once it has started: each says so when it enters the kernel,
+// and before its first sum waits until all have.  The arrival orders no memory; what stands between hides the wait.
+template <int C>
+__device__ __forceinline__ void say_started()
+{
+    if constexpr (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+template <int C>
+__device__ __forceinline__ void wait_until_all_started()
+{
+    if constexpr (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // The group a thread belongs to where groups are larger than a warp: `threads` threads (a multiple of 32) of its
 // CTA, number `id` of that size, with C - 1 more CTAs.
@@ -432,6 +444,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     const auto times = [](Two<A> h, Two<A> w) { return h * w; };
     const auto plus = [](Two<A> h, Two<A> b) { return h + b; };
 
+    say_started<C>();
     wait_for_earlier();
     let_later_start();
     Packed<TS, E> xr;
@@ -440,6 +453,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     if (!BLK || !kAny || p.x) load_row<ALIGNED, TS, E>(xr, p.x, p.rows, row, p.ld_x, c, ok);
     else xr.clear();
     if (BLK && GATE == kCellGate) load_row<ALIGNED, TB, E>(gr, p.gate, p.rows, row, p.ld_gate, c, ok);
+    wait_until_all_started<C>();
 
     const int post_kind = kAny ? p.post.kind : FO_NORM_RMS, pre_kind = kAny ? p.pre.kind : FO_NORM_RMS;
     RowNorm<A> post = {A(0), A(0)}, pre = {A(0), A(0)};
@@ -595,10 +609,12 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     auto add = [&](int slot, int k0, auto term) {
         if (slot_at[slot] >= 0) Sums::template change<P>(sums + slot_at[slot], k0, term);
     };
+    say_started<C>();
     for (int s = 0; s < n_slots; ++s)
         Sums::template change<E>(sums + s * cta * E, 0, [](int, Two<A>) { return both(A(0)); });
 
     wait_for_earlier();
+    wait_until_all_started<C>();
     // all threads of a group, and all CTAs of a cluster, take the same number of turns: their sums meet at barriers
     for (long long row0 = (long long)(blockIdx.x / C) * groups; row0 < p.rows;
          row0 += (long long)(gridDim.x / C) * groups) {
