@@ -8,9 +8,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
 #include <map>
 #include <string>
 #include <utility>
+#include <vector>
 
 #include "fusedops_train.h"
 
@@ -372,53 +374,194 @@ long long whole(PyObject *o)
     if (PyErr_Occurred()) throw Raised();
     return v;
 }
-// The C structs of a list, packed by training.py
-template <class Tensor>
-const Tensor *packed_list(PyObject *o, int *count)
+
+// What the tensors of one list are: their type, on one GPU.
+struct Kind {
+    at::ScalarType type;
+    c10::DeviceIndex gpu;
+};
+
+// One Python list of tensors that belongs to a call.  Tensors can change under a list that is kept: `t.data = other` or a
+// storage that is resized moves them, to another size or type at that.  So every call looks at every tensor again, and
+// nothing of an earlier call is used.  That takes 7 to 10 ns a tensor on the host.
+class Tensors {
+    PyObject *list_;
+    const char *name_;
+
+    [[noreturn]] void refuse(const char *what) const { throw Refused(std::string(name_) + ": " + what); }
+
+public:
+    Tensors(PyObject *list, const char *name) : list_(list), name_(name)
+    {
+        require(PyList_Check(list), "tensors are given as a list");
+    }
+    size_t count() const { return (size_t)PyList_GET_SIZE(list_); }
+    bool is(PyObject *list) const { return list == list_; }
+    const at::Tensor &at(size_t k) const
+    {
+        PyObject *o = PyList_GET_ITEM(list_, (Py_ssize_t)k);
+        if (!THPVariable_Check(o)) refuse("not a tensor");
+        return THPVariable_Unpack(o);
+    }
+    void same_count(size_t n) const
+    {
+        if (count() != n) throw Refused(std::string(name_) + ": " + std::to_string(count()) + " tensors for " + std::to_string(n));
+    }
+    // put(k, address of tensor k's elements), of which there have to be n(k)
+    template <class Size, class Put>
+    void read(const Kind &kind, Size n, Put put) const
+    {
+        const caffe2::TypeMeta type = c10::scalarTypeToTypeMeta(kind.type);
+        const c10::Device device(c10::kCUDA, kind.gpu);
+        const size_t bytes = type.itemsize(), many = count();
+        PyTypeObject *known = nullptr;                       // the Python type of the tensor before
+        c10::StorageImpl *one = nullptr;                     // its storage: neighbours in a bucket share it
+        char *begin = nullptr;
+        size_t held = 0;
+        for (size_t k = 0; k < many; ++k) {
+            PyObject *o = PyList_GET_ITEM(list_, (Py_ssize_t)k);
+            if (Py_TYPE(o) != known) at(k), known = Py_TYPE(o);
+            const c10::TensorImpl &t = *THPVariable_Unpack(o).unsafeGetTensorImpl();
+            if (t.dtype() != type || t.device() != device) refuse("tensors of one type on one device are needed");
+            if (!t.is_contiguous()) refuse("tensors must be contiguous");
+            const int64_t want = n(k, t);
+            if (t.numel() != want) refuse("sizes differ");
+            c10::StorageImpl *const storage = t.storage().unsafeGetStorageImpl();
+            if (storage != one) one = storage, begin = static_cast<char *>(storage->mutable_data()), held = storage->nbytes();
+            const size_t at_byte = (size_t)t.storage_offset() * bytes;
+            if (want && held < at_byte + (size_t)want * bytes) refuse("a tensor's storage is smaller than the tensor");
+            put(k, want ? begin + at_byte : nullptr);
+        }
+    }
+};
+
+// The kind of a list's first tensor.
+Kind kind_of(const Tensors &grads)
 {
-    require(PyBytes_Check(o) && PyBytes_GET_SIZE(o) % (Py_ssize_t)sizeof(Tensor) == 0, "not a packed list");
-    *count = (int)(PyBytes_GET_SIZE(o) / (Py_ssize_t)sizeof(Tensor));
-    return reinterpret_cast<const Tensor *>(PyBytes_AS_STRING(o));
+    if (grads.count() == 0) return {at::kFloat, -1};
+    const at::Tensor &t = grads.at(0);
+    require(t.is_cuda(), "fused operators need CUDA tensors (no CPU path)");
+    type_code(t.scalar_type());
+    return {t.scalar_type(), t.get_device()};
 }
 
-// grad_norm(list, clip, in_type, out_type, norm_kind, max_norm, eps, result_type, gpu) -> (norm, factor)
+bool sixteen_bits(at::ScalarType t) { return t == at::kBFloat16 || t == at::kHalf; }
+
+// Gradients, and the tensors their clipped values go to (None: not wanted; the list itself: in place).
+struct GradTensors {
+    std::vector<fo_tensor> c;
+    Kind kind;
+    at::ScalarType out_type;
+
+    GradTensors(PyObject *grads, PyObject *outs)
+    {
+        const Tensors in(grads, "grads");
+        kind = kind_of(in), out_type = kind.type;
+        c.resize(in.count());
+        in.read(kind, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) { c[k].in = c[k].out = p; });
+        if (outs == Py_None || in.is(outs)) return;
+        const Tensors out(outs, "outs");
+        out.same_count(c.size());
+        if (c.empty()) return;
+        out_type = out.at(0).scalar_type();
+        if (out_type != kind.type && !(sixteen_bits(kind.type) && out_type == at::kFloat))
+            throw Refused(std::string("clipped values of ") + c10::toString(out_type) + " from gradients of " + c10::toString(kind.type));
+        out.read({out_type, kind.gpu}, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, [&](size_t k, void *p) { c[k].out = p; });
+    }
+};
+
+// The lists of an AdamW update: params, grads, m, v, the new params, m and v, weights (or None), decay (doubles, packed).
+struct AdamTensors {
+    std::vector<fo_adam_tensor> c;
+    Kind kind;
+    at::ScalarType weight_type = at::kBFloat16;
+
+    explicit AdamTensors(PyObject *const *a)
+    {
+        const Tensors grads(a[1], "grads");
+        kind = kind_of(grads);
+        c.resize(grads.count());
+        require(PyBytes_Check(a[8]) && (size_t)PyBytes_GET_SIZE(a[8]) == c.size() * sizeof(double), "decay: one value per tensor is needed");
+        grads.read(kind, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) {
+            c[k].g = p;
+            memcpy(&c[k].decay, PyBytes_AS_STRING(a[8]) + k * sizeof(double), sizeof(double));
+        });
+        const Kind wide = {kind.type == at::kDouble ? at::kDouble : at::kFloat, kind.gpu};
+        // the new values: every list may be the one it comes from
+        const auto both = [&](PyObject *in, const char *in_name, PyObject *out, const char *out_name, const void *fo_adam_tensor::*p,
+                              void *fo_adam_tensor::*q) {
+            take(in, in_name, wide, [&](size_t k, void *v) { c[k].*p = c[k].*q = v; });
+            if (out != in) take(out, out_name, wide, [&](size_t k, void *v) { c[k].*q = v; });
+        };
+        both(a[0], "params", a[4], "params out", &fo_adam_tensor::p, &fo_adam_tensor::p_out);
+        both(a[2], "m", a[5], "m out", &fo_adam_tensor::m, &fo_adam_tensor::m_out);
+        both(a[3], "v", a[6], "v out", &fo_adam_tensor::v, &fo_adam_tensor::v_out);
+        if (a[7] == Py_None || c.empty()) return;
+        const Tensors weights(a[7], "weights");
+        weights.same_count(c.size());
+        weight_type = weights.at(0).scalar_type();
+        require(sixteen_bits(weight_type), "weights are bfloat16 or float16");
+        require(kind.type != at::kDouble, "no 16-bit weights beside gradients of float64");
+        take(a[7], "weights", {weight_type, kind.gpu}, [&](size_t k, void *p) { c[k].weights = p; });
+    }
+
+private:
+    template <class Put>
+    void take(PyObject *list, const char *name, const Kind &of, Put put)
+    {
+        const Tensors ts(list, name);
+        ts.same_count(c.size());
+        ts.read(of, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, put);
+    }
+};
+
+// check_grads(grads, outs), check_adam(the nine of AdamTensors): refuse what a call would refuse
+PyObject *check_grads_impl(PyObject *const *a)
+{
+    GradTensors(a[0], a[1]);
+    Py_RETURN_NONE;
+}
+PyObject *check_adam_impl(PyObject *const *a)
+{
+    AdamTensors t(a);
+    Py_RETURN_NONE;
+}
+
+// grad_norm(grads, outs or None: no clipping, norm_kind, max_norm, eps, result_type, gpu of an empty list) -> (norm, factor)
 PyObject *grad_norm_impl(PyObject *const *a)
 {
-    int count;
-    const fo_tensor *list = packed_list<fo_tensor>(a[0], &count);
-    const bool clip = PyObject_IsTrue(a[1]) == 1;
-    const int in_type = (int)whole(a[2]), out_type = (int)whole(a[3]), kind = (int)whole(a[4]), wide = (int)whole(a[7]);
-    const double max_norm = number(a[5]), eps = number(a[6]);
-    const auto gpu = (c10::DeviceIndex)whole(a[8]);
+    const GradTensors t(a[0], a[1]);
+    const bool clip = a[1] != Py_None;
+    const int kind = (int)whole(a[2]), wide = (int)whole(a[5]), count = (int)t.c.size();
+    const double max_norm = number(a[3]), eps = number(a[4]);
+    const auto gpu = t.kind.gpu >= 0 ? t.kind.gpu : (c10::DeviceIndex)whole(a[6]);
     const at::Tensor result = at::detail::empty_cuda({2}, wide == FO_F64 ? at::kDouble : at::kFloat, c10::Device(c10::kCUDA, gpu),
                                                      c10::nullopt);
     const OnGpu on(gpu);
     const cudaStream_t st = c10::cuda::getCurrentCUDAStream(gpu).stream();
     const at::Tensor ws = workspace(gpu, st, fused_grad_workspace_bytes());
     if (clip)
-        check_status(fused_grad_clip(list, count, in_type, out_type, kind, max_norm, eps, result.data_ptr(), wide, ws.data_ptr(),
-                                     (size_t)ws.numel(), st), "fused_grad_clip");
+        check_status(fused_grad_clip(t.c.data(), count, type_code(t.kind.type), type_code(t.out_type), kind, max_norm, eps,
+                                     result.data_ptr(), wide, ws.data_ptr(), (size_t)ws.numel(), st), "fused_grad_clip");
     else
-        check_status(fused_grad_norm(list, count, in_type, kind, max_norm, eps, result.data_ptr(), wide, ws.data_ptr(),
-                                     (size_t)ws.numel(), st), "fused_grad_norm");
+        check_status(fused_grad_norm(t.c.data(), count, type_code(t.kind.type), kind, max_norm, eps, result.data_ptr(), wide,
+                                     ws.data_ptr(), (size_t)ws.numel(), st), "fused_grad_norm");
     return THPVariable_Wrap(result);
 }
 
-// adamw(list, grad_type, weight_type, lr, beta1, beta2, eps, step, factor, gpu)
+// adamw(the nine of AdamTensors, lr, beta1, beta2, eps, step, factor)
 PyObject *adamw_impl(PyObject *const *a)
 {
-    int count;
-    const fo_adam_tensor *list = packed_list<fo_adam_tensor>(a[0], &count);
-    const int grad_type = (int)whole(a[1]), weight_type = (int)whole(a[2]);
-    const at::Tensor *factor = tensor_of(a[8], "factor");
-    const auto gpu = (c10::DeviceIndex)whole(a[9]);
+    const AdamTensors t(a);
+    const at::Tensor *factor = tensor_of(a[14], "factor");
+    const c10::DeviceIndex gpu = t.kind.gpu;
     if (factor)
         require(factor->numel() == 1 && factor->is_cuda() && factor->get_device() == gpu
                     && (factor->scalar_type() == at::kFloat || factor->scalar_type() == at::kDouble),
                 "factor is not one float on the gradients' device");
     const OnGpu on(gpu);
-    check_status(fused_adamw(list, count, grad_type, weight_type, number(a[3]), number(a[4]), number(a[5]), number(a[6]),
-                             whole(a[7]), factor ? factor->data_ptr() : nullptr,
+    check_status(fused_adamw(t.c.data(), (int)t.c.size(), type_code(t.kind.type), type_code(t.weight_type), number(a[9]), number(a[10]),
+                             number(a[11]), number(a[12]), whole(a[13]), factor ? factor->data_ptr() : nullptr,
                              factor ? type_code(factor->scalar_type()) : FO_F32,
                              c10::cuda::getCurrentCUDAStream(gpu).stream()), "fused_adamw");
     Py_RETURN_NONE;
@@ -458,7 +601,8 @@ PyObject *connect(PyObject *, PyObject *args)
 }
 
 PyMethodDef g_methods[] = {method<block_norm_impl, 11>("block_norm"), method<block_norm_grad_impl, 11>("block_norm_grad"),
-                           method<grad_norm_impl, 9>("grad_norm"), method<adamw_impl, 10>("adamw"),
+                           method<grad_norm_impl, 7>("grad_norm"), method<adamw_impl, 15>("adamw"),
+                           method<check_grads_impl, 2>("check_grads"), method<check_adam_impl, 9>("check_adam"),
                            {"connect", connect, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_training", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

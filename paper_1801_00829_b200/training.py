@@ -16,20 +16,12 @@ import torch
 from . import build as _build
 from .binding import FusedOpsError, load_library, workspace
 
-DTYPES = {torch.float64: 0, torch.float32: 1, torch.bfloat16: 2, torch.float16: 3}
 GRAD_NORM_KIND = {"l2": 0, "max": 1}
 
 
 def _require(ok, text):
     if not ok:
         raise ValueError(text)
-
-
-def _index(t):
-    """Number of the GPU that a tensor is on."""
-    index = t.get_device()
-    _require(index >= 0, "fused operators need CUDA tensors (no CPU path)")
-    return index
 
 
 _extension = None
@@ -71,42 +63,25 @@ def fused_block_norm_grad(dh=None, dy=None, h=None, f=None, stats=None, post=Non
 
 
 # ------------------------------------------------------------------ many tensors
-def _same(tensors, name, dtype=None, device=None):
-    """The type and device that the tensors of a list share; contiguous, all of them."""
-    if tensors:
-        _index(tensors[0])
-        dtype = tensors[0].dtype if dtype is None else dtype
-        device = tensors[0].device if device is None else device
-    for t in tensors:
-        _require(t.dtype == dtype and t.device == device, "%s: tensors of one type on one device are needed" % name)
-        _require(t.is_contiguous(), "%s: tensors must be contiguous" % name)
-    return dtype, device
-
-
-def _same_sizes(tensors, others, name):
-    _require(len(tensors) == len(others), "%s: %d tensors for %d" % (name, len(others), len(tensors)))
-    _require(all(a.numel() == b.numel() for a, b in zip(tensors, others)), "%s: sizes differ" % name)
+def _first(tensors, name):
+    return getattr(tensors[0], name) if tensors else None
 
 
 class TensorList:
-    """Gradients, and where their clipped values go: built once for buffers that a program keeps, or per call."""
+    """Gradients, and where their clipped values go: built once for tensors that a program keeps, or per call.
+
+    A list holds the tensors themselves.  Every call looks at them again, so a tensor may get other storage between two calls
+    as long as type, device and size fit.  A program whose gradients are new tensors in every step (PyTorch's
+    default after ``zero_grad``) needs a new list in every step: the old one still means the old gradients."""
 
     def __init__(self, grads, outs=None):
         self.grads = list(grads)
         self.outs = self.grads if outs is None else list(outs)
-        self.dtype, self.device = _same(self.grads, "grads")
-        _require(self.dtype is None or self.dtype in DTYPES, "no kernel for gradients of %s" % self.dtype)
-        self.out_dtype = self.dtype
-        if outs is not None:
-            _same_sizes(self.grads, self.outs, "outs")
-            self.out_dtype, _ = _same(self.outs, "outs", device=self.device)
-            low = self.dtype in (torch.bfloat16, torch.float16)
-            _require(self.out_dtype == self.dtype or (low and self.out_dtype == torch.float32),
-                     "clipped values of %s from gradients of %s" % (self.out_dtype, self.dtype))
-        flat = [v for g, o in zip(self.grads, self.outs) for v in (g.data_ptr(), o.data_ptr(), g.numel())]
-        self.packed = struct.pack("QQq" * len(self.grads), *flat)
-        self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.out_dtype, 1)
-        self.index = None if self.device is None else self.device.index
+        (_extension or _native()).check_grads(self.grads, self.outs)
+
+    dtype = property(lambda self: _first(self.grads, "dtype"))
+    device = property(lambda self: _first(self.grads, "device"))
+    out_dtype = property(lambda self: _first(self.outs, "dtype"))
 
     def __len__(self):
         return len(self.grads)
@@ -122,10 +97,10 @@ def _grad_call(grads, clip, kind, max_norm, eps, result_type, device):
     wide = result_type is torch.float64
     _require(wide or result_type is torch.float32, "results are float32 or float64")
     _require(kind in GRAD_NORM_KIND, "norm kind %r" % (kind,))
-    index = grads.index
-    if index is None:                                        # an empty list
+    index = -1
+    if len(grads) == 0:
         index = torch.cuda.current_device() if device is None else torch.device(device).index
-    return (_extension or _native()).grad_norm(grads.packed, clip, *grads.types, GRAD_NORM_KIND[kind], max_norm, eps,
+    return (_extension or _native()).grad_norm(grads.grads, grads.outs if clip else None, GRAD_NORM_KIND[kind], max_norm, eps,
                                                0 if wide else 1, index)
 
 
@@ -141,35 +116,26 @@ def fused_grad_clip(grads, max_norm, kind="l2", eps=1e-6, result_type=torch.floa
 
 
 class AdamList:
-    """Parameters, gradients and moments of one AdamW update, and where the new values go."""
+    """Parameters, gradients and moments of one AdamW update, and where the new values go.  What TensorList says of
+    tensors that change holds here too."""
 
     def __init__(self, params, grads, m, v, decay=0.0, outs=None, weights=None):
         self.params, self.grads, self.m, self.v = list(params), list(grads), list(m), list(v)
         self.outs = [list(o) for o in outs] if outs is not None else [self.params, self.m, self.v]
         self.weights = list(weights) if weights is not None else None
-        self.dtype, self.device = _same(self.grads, "grads")
-        _require(self.dtype is None or self.dtype in DTYPES, "no kernel for gradients of %s" % self.dtype)
-        wide = torch.float64 if self.dtype == torch.float64 else torch.float32
         _require(len(self.outs) == 3, "outs are (params, m, v)")
-        for name, ts in zip(("params", "m", "v", "params out", "m out", "v out"), [self.params, self.m, self.v] + self.outs):
-            _same_sizes(self.grads, ts, name)
-            _same(ts, name, wide, self.device)
-        self.weight_dtype = None
-        if self.weights is not None:
-            _same_sizes(self.grads, self.weights, "weights")
-            self.weight_dtype, _ = _same(self.weights, "weights", device=self.device)
-            _require(self.weight_dtype in (None, torch.bfloat16, torch.float16), "weights are bfloat16 or float16")
         n = len(self.grads)
         decay = [float(decay)] * n if isinstance(decay, (int, float)) else [float(d) for d in decay]
         _require(len(decay) == n, "decay: %d values for %d tensors" % (len(decay), n))
-        lists = [self.params, self.grads, self.m, self.v] + self.outs + ([self.weights] if self.weights is not None else [])
-        none = [0] if self.weights is None else []
-        flat = []
-        for k in range(n):
-            flat += [ts[k].data_ptr() for ts in lists] + none + [self.grads[k].numel(), decay[k]]
-        self.packed = struct.pack("8Qqd" * n, *flat)
-        self.types = DTYPES.get(self.dtype, 1), DTYPES.get(self.weight_dtype, 0)
-        self.index = None if self.device is None else self.device.index
+        self._decay = struct.pack("%dd" % n, *decay)
+        (_extension or _native()).check_adam(*self._lists())
+
+    dtype = property(lambda self: _first(self.grads, "dtype"))
+    device = property(lambda self: _first(self.grads, "device"))
+    weight_dtype = property(lambda self: _first(self.weights or [], "dtype"))
+
+    def _lists(self):
+        return (self.params, self.grads, self.m, self.v, *self.outs, self.weights, self._decay)
 
     def __len__(self):
         return len(self.grads)
@@ -186,4 +152,4 @@ def fused_adamw(tensors, lr, betas=(0.9, 0.999), eps=1e-8, step=1, factor=None):
     gradients are multiplied by (result[1:2] of fused_grad_norm)."""
     if len(tensors) == 0:
         return
-    (_extension or _native()).adamw(tensors.packed, *tensors.types, lr, betas[0], betas[1], eps, step, factor, tensors.index)
+    (_extension or _native()).adamw(*tensors._lists(), lr, betas[0], betas[1], eps, step, factor)
