@@ -356,9 +356,16 @@ _ws = {}
 
 
 def workspace(device, nbytes):
-    """A cached, initialised scratch buffer of at least nbytes on `device`."""
+    """A cached, initialised scratch buffer of at least nbytes on `device`.  A call that is captured into a CUDA graph gets
+    a buffer of its own, in the graph's memory and cleared by the graph: the cached one may be given back while the
+    graph lives, and may be in use by another stream when the graph runs."""
     if device.type != "cuda":
         raise RuntimeError("fused operators need CUDA tensors (no CPU path)")
+    if device.index is not None and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return workspace(device, nbytes)
+    if torch.cuda.is_current_stream_capturing():
+        return _scratch(device, nbytes)
     # one buffer per (device, stream): calls that may overlap on the GPU must not share scratch
     stream = torch.cuda.current_stream(device)
     key = (device.index if device.index is not None else torch.cuda.current_device(), stream.cuda_stream)
@@ -366,12 +373,14 @@ def workspace(device, nbytes):
     if buf is None or buf.numel() < nbytes:
         if buf is not None:
             buf.record_stream(stream)         # kernels already queued may still use the old one
-        size = max(int(nbytes), 1 << 20)
-        buf = torch.empty(size, dtype=torch.uint8, device=device)
-        assert buf.data_ptr() % 256 == 0
-        _check(load_library().fo_workspace_init(C.c_void_p(buf.data_ptr()), buf.numel(),
-                                                _stream(device)), "fo_workspace_init")
-        _ws[key] = buf
+        buf = _ws[key] = _scratch(device, max(int(nbytes), 1 << 20))
+    return buf
+
+
+def _scratch(device, nbytes):
+    buf = torch.empty(int(nbytes), dtype=torch.uint8, device=device)
+    assert buf.data_ptr() % 256 == 0
+    _check(load_library().fo_workspace_init(C.c_void_p(buf.data_ptr()), buf.numel(), _stream(device)), "fo_workspace_init")
     return buf
 
 

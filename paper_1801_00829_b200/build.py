@@ -128,8 +128,8 @@ def build_extension(force: bool = False) -> str:
     tmp = EXTENSION_PATH + ".tmp%d" % os.getpid()
     cmd = (["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
            + ["-I" + d for d in includes] + [EXTENSION_SOURCE, "-o", tmp, "-L" + HERE, "-l:libfusedops.so", "-Wl,-rpath,$ORIGIN",
-                                             "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda",
-                                             "-ltorch_python"])
+                                             "-L" + os.path.join(root, "lib"), "-L" + os.path.join(cuda, "lib64"), "-lcudart", "-lc10", "-lc10_cuda",
+                                             "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"])
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n%s" % res.stdout[-4000:])

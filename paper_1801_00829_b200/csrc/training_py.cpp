@@ -274,16 +274,23 @@ PyObject *block_norm_impl(PyObject *const *a)
     return out;
 }
 
+at::Tensor new_workspace(c10::DeviceIndex gpu, size_t bytes)
+{
+    PyObject *o = PyObject_CallFunction(g_workspace, "in", (int)gpu, (Py_ssize_t)bytes);
+    if (!o) throw Raised();
+    const at::Tensor t = THPVariable_Unpack(o);
+    Py_DECREF(o);
+    return t;
+}
+// The stream's scratch; a call that is captured into a graph gets one of its own (binding.workspace).
 at::Tensor workspace(c10::DeviceIndex gpu, cudaStream_t stream, size_t bytes)
 {
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone)
+        return new_workspace(gpu, bytes);
     static auto *cache = new std::map<std::pair<int, cudaStream_t>, at::Tensor>();      // outlives the interpreter
     at::Tensor &buf = (*cache)[{gpu, stream}];
-    if (!buf.defined() || (size_t)buf.numel() < bytes) {
-        PyObject *o = PyObject_CallFunction(g_workspace, "in", (int)gpu, (Py_ssize_t)bytes);
-        if (!o) throw Raised();
-        buf = THPVariable_Unpack(o);
-        Py_DECREF(o);
-    }
+    if (!buf.defined() || (size_t)buf.numel() < bytes) buf = new_workspace(gpu, bytes);
     return buf;
 }
 
