@@ -726,10 +726,10 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
 #pragma unroll
                     for (int i = 0; i < P / 2; ++i) a[i] = row_act, slope[i] = row_slope;
                 }
+                add(kColScale, k0, [&](int i, Two<A> s) {    // without a col_scale it is the gradient at ones
+                    return GATE == kNoGate ? fused_ma(d[i], z[i], s) : fused_ma(d[i] * z[i], a[i], s);
+                });
                 if (p.col_scale) {
-                    add(kColScale, k0, [&](int i, Two<A> s) {
-                        return GATE == kNoGate ? fused_ma(d[i], z[i], s) : fused_ma(d[i] * z[i], a[i], s);
-                    });
                     Two<A> cs[P / 2];
                     load_vector<ALIGNED, TB, P>(cs, p.col_scale, wide, k0, c);
 #pragma unroll

@@ -1,0 +1,40 @@
+"""Results of the training-step operators that are easily left out: sums over nothing, gradients of arguments that were not
+given, values at the ends of the range.  Tolerances as in test_gpu_training.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1801_00829_b200 as fo
+from oracle import training as ref
+from paper_1801_00829_b200.binding import workspace
+from test_gpu_training import BF16, F16, F32, F64, Case, close, host, unit
+from test_training_abi import BLOCK_NORM_GRAD, NONE
+
+pytestmark = pytest.mark.gpu
+
+CODE = {F64: 0, F32: 1, BF16: 2, F16: 3}
+
+
+@pytest.mark.parametrize("stream,block", [(BF16, BF16), (F32, F16), (F64, F64)])
+@pytest.mark.parametrize("gate", [None, "cell", "row", "col"])
+@pytest.mark.parametrize("rows,cols", [(19, 130), (7, 1001)])
+def test_gradient_of_a_column_scale_that_is_not_there(stream, block, gate, rows, cols):
+    """The C call: dcol_scale with col_scale NULL is the gradient at a scale of ones."""
+    c = Case(rows, cols, stream, block, "rms", gate, "silu" if gate else "linear", None, col_scale=False)
+    _, _, stats = fo.fused_block_norm(c.x, c.f, stats=True, **c.how())
+    wide = F64 if block == F64 else F32
+    got = torch.full((cols,), float("nan"), dtype=wide, device="cuda")
+    lib = fo.load_library()
+    need = lib.fused_block_norm_grad_workspace_bytes(rows, cols, CODE[block])
+    ws = workspace(c.f.device, need)
+    access = {None: 0, "cell": 0, "row": 1, "col": 2}[gate]
+    g = c.gate[1] if gate else None
+    post = (1, 0, c.post[3], c.post[1].data_ptr(), 0)
+    packed = BLOCK_NORM_GRAD.pack(rows, cols, CODE[stream], CODE[block], CODE[block], access, 2 if gate else 0, 0, c.dh.data_ptr(), 0, 0,
+                                  c.f.data_ptr(), g.data_ptr() if gate else 0, 0, stats.data_ptr(), c.dh.stride(0), 0, 0,
+                                  c.f.stride(0), g.stride(0) if gate else 0, c.scale, *post, *NONE, 0, 0, 0, 0, 0, 0,
+                                  got.data_ptr(), 0, 0, 0, 0)
+    st = torch.cuda.current_stream().cuda_stream
+    assert lib.fused_block_norm_grad(packed, ws.data_ptr(), ws.numel(), st) == 0
+    want = ref.block_norm_grad(host(c.dh), None, None, host(c.f), host(stats), **c.host_how())["col_scale"]
+    close(got, *want, unit(block), "dcol_scale", rows=max(rows, cols))
