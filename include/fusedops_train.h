@@ -45,7 +45,8 @@ enum { FO_F64 = 0, FO_F32 = 1, FO_BF16 = 2, FO_F16 = 3 };
  * FO_AT_COL: one value per column, contiguous; NULL: no gate.  Vectors are contiguous.
  * h and y are NULL where they are not wanted; h may be x itself (same pointer and ld).
  * stats: NULL or 4 x rows values (float, or double where block_type is FO_F64), contiguous: mu and r
- * of the post norm, mu and r of the pre norm, zeros for a norm that is not there.  The gradient needs them.
+ * of the post norm, mu and r of the pre norm, zeros for a norm that is not there and for rows without columns.
+ * The gradient needs them.
  * Any alignment and any ld works; rows whose every pointer is 16-byte aligned move in 16-byte
  * pieces.  cols <= FO_BLOCK_NORM_MAX_COLS, else FO_ERR_UNSUPPORTED.  A single token is the call with rows = 1.
  * A row that holds a NaN or an infinity affects that row alone.

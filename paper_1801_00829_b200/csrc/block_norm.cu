@@ -87,6 +87,14 @@ int grad_lines(long long rows, long long cols)
     return (int)(n > 1 ? n : 1);
 }
 
+// Statistics or sums over no elements are zero.
+int clear_sums(void *p, long long values, int block_type, cudaStream_t st)
+{
+    if (!p || values == 0) return FO_OK;
+    const cudaError_t e = cudaMemsetAsync(p, 0, (size_t)values * (block_type == FO_F64 ? 8 : 4), st);
+    return e == cudaSuccess ? FO_OK : cuda_fail(e);
+}
+
 size_t grad_line_bytes(long long rows, long long cols, int block_type)
 {
     return (size_t)kGradSlots * grad_lines(rows, cols) * (size_t)cols * (block_type == FO_F64 ? 8 : 4);
@@ -105,7 +113,8 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
     if (rc != FO_OK) return rc;
     if (!types_ok(a->stream_type, a->block_type, a->vec_type) || !spec_ok(a->post) || !spec_ok(a->pre))
         return FO_ERR_UNSUPPORTED;
-    if (a->rows == 0 || a->cols == 0) return FO_OK;
+    if (a->rows == 0) return FO_OK;
+    if (a->cols == 0) return clear_sums(a->stats, 4 * a->rows, a->block_type, (cudaStream_t)stream);
     if (!a->x && !a->f) return FO_ERR_NULL;
     if (!a->h && !a->y && !a->stats) return FO_ERR_NULL;
     if (a->y && a->pre.kind == FO_NORM_NONE) return FO_ERR_NULL;      // y without a norm: h is that
@@ -156,16 +165,13 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
     if (rc != FO_OK) return rc;
     if (!types_ok(a->stream_type, a->block_type, a->vec_type) || !spec_ok(a->post) || !spec_ok(a->pre))
         return FO_ERR_UNSUPPORTED;
-    if (a->cols == 0) return FO_OK;
     const cudaStream_t st = (cudaStream_t)stream;
+    if (a->cols == 0) return clear_sums(a->gate_access == FO_AT_ROW ? a->dgate : nullptr, a->rows, a->block_type, st);
     void *const sums[kGradSlots] = {a->dpre_weight, a->dpre_bias, a->dpost_weight, a->dpost_bias, a->dcol_scale,
                                     a->gate_access == FO_AT_COL ? a->dgate : nullptr};
     if (a->rows == 0) {                                        // sums over no rows; nothing else has a size
-        for (void *s : sums) {
-            if (!s) continue;
-            const cudaError_t e = cudaMemsetAsync(s, 0, (size_t)a->cols * (a->block_type == FO_F64 ? 8 : 4), st);
-            if (e != cudaSuccess) return cuda_fail(e);
-        }
+        for (void *s : sums)
+            if ((rc = clear_sums(s, a->cols, a->block_type, st)) != FO_OK) return rc;
         return FO_OK;
     }
     const bool pre = a->dy != nullptr, post = a->f && a->post.kind != FO_NORM_NONE;

@@ -38,3 +38,23 @@ def test_gradient_of_a_column_scale_that_is_not_there(stream, block, gate, rows,
     assert lib.fused_block_norm_grad(packed, ws.data_ptr(), ws.numel(), st) == 0
     want = ref.block_norm_grad(host(c.dh), None, None, host(c.f), host(stats), **c.host_how())["col_scale"]
     close(got, *want, unit(block), "dcol_scale", rows=max(rows, cols))
+
+
+def leave_garbage(*shapes):
+    """Memory that the next tensors of these sizes are likely to get, full of NaN."""
+    for s in shapes:
+        torch.full(s, float("nan"), device="cuda")
+
+
+@pytest.mark.parametrize("block", [F32, BF16])
+def test_rows_without_columns(block):
+    """Sums over no columns are zero: the gradient of a gate per row, and the statistics."""
+    x = torch.zeros(300, 0, dtype=block, device="cuda")
+    g = torch.ones(300, dtype=block, device="cuda")
+    for _ in range(3):
+        leave_garbage((300,), (4, 300))
+        h, _, stats = fo.fused_block_norm(x, x, post=("rms", None, None, 1e-6), gate=("row", g, "silu"), stats=True)
+        assert bool((stats == 0).all())
+        leave_garbage((300,), (4, 300))
+        got = fo.fused_block_norm_grad(h, None, None, x, stats, post=("rms", None, None, 1e-6), gate=("row", g, "silu"))
+        assert got["gate"].shape == (300,) and bool((got["gate"] == 0).all())
