@@ -210,7 +210,8 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
 
 // N elements, whole pieces or half ones, from k0 of a vector over the columns (weight, bias, scale, gate per
 // column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives some value of
-// the vector, which meets a zero there: no zeros have to be put where a load might not take place.
+// the vector, so that no zeros have to be put where a load might not take place; it meets a zero there, and what an
+// infinite one makes of that is taken out before it is added up.
 template <bool ALIGNED, class TE, int N, int T, int V>
 __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void *base, bool wide, int k0,
                                             const Columns<T, V> &c)
@@ -488,7 +489,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
         const Two<A> k2 = both(scale);
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fused_ma(h[k / 2], k2, xr.get2(k));
-        if (kAny && p.post.bias && p.cols != c.threads() * E) {            // a bias leaves no zeros outside the row
+        if (p.cols != c.threads() * E) {     // zeros outside the row again: not what a bias or an infinite factor left there
 #pragma unroll
             for (int k = 0; k < E; k += 2) h[k / 2] = c.template inside<ALIGNED>(k, h[k / 2]);
         }

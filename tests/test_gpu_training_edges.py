@@ -58,3 +58,18 @@ def test_rows_without_columns(block):
         leave_garbage((300,), (4, 300))
         got = fo.fused_block_norm_grad(h, None, None, x, stats, post=("rms", None, None, 1e-6), gate=("row", g, "silu"))
         assert got["gate"].shape == (300,) and bool((got["gate"] == 0).all())
+
+
+@pytest.mark.parametrize("stream,block", [(F32, F32), (BF16, BF16), (F32, F16), (F64, F64)])
+@pytest.mark.parametrize("where", ["post", "col_scale", "gate"])
+@pytest.mark.parametrize("cols", [5, 100, 1000, 1001, 4104, 9000])
+def test_an_infinite_factor_stays_in_its_column(stream, block, where, cols):
+    """An infinite weight, column scale or gate in the last piece of rows that leave threads without elements: h is
+    infinite in that column, r is 0 and y is 0 in all others."""
+    c = Case(3, cols, stream, block, "rms", "col", "linear", "rms")
+    factor = {"post": c.post[1], "col_scale": c.col_scale, "gate": c.gate[1]}[where]
+    factor[cols - 1] = float("inf")
+    h, y, stats = fo.fused_block_norm(c.x, c.f, stats=True, **c.how())
+    assert bool(torch.isinf(h[:, -1]).all()) and bool(torch.isfinite(h[:, :-1]).all())
+    assert bool((y[:, :-1] == 0).all()) and bool(torch.isnan(y[:, -1]).all())
+    assert bool((stats[3] == 0).all()) and bool(torch.isfinite(stats).all())
