@@ -209,9 +209,9 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
 }
 
 // N elements, whole pieces or half ones, from k0 of a vector over the columns (weight, bias, scale, gate per
-// column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives some value of
-// the vector, so that no zeros have to be put where a load might not take place; it meets a zero there, and what an
-// infinite one makes of that is taken out before it is added up.
+// column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives zeros, or, ALIGNED, some
+// value of the vector, so that no zeros have to be put where a load might not take place: it meets a zero there, and
+// what an infinite one or a bias makes of that is not added up.
 template <bool ALIGNED, class TE, int N, int T, int V>
 __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void *base, bool wide, int k0,
                                             const Columns<T, V> &c)
@@ -219,7 +219,8 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
     using A = Acc<TE>;
     if (!ALIGNED && !(c.vectors && c.of((k0 + N - 1) / V * V) + V <= c.cols)) {      // not whole, or not aligned
         auto at = [&](int k) -> A {
-            const int j = min(c.of(k), c.cols - 1);
+            const int j = c.of(k);
+            if (j >= c.cols) return A(0);
             if (sizeof(TE) == 2 && wide) return (A)__ldg(static_cast<const float *>(base) + j);
             return widen<TE>(static_cast<const TE *>(base)[j]);
         };
@@ -384,7 +385,10 @@ template <class A>
 struct RowNorm {
     A mean, r;
 };
-template <bool ALIGNED, int T, int C, int E, class A, class Cols>
+// FACTORS: the row was multiplied by vectors, and an infinite one made NaN of the zeros outside the row (ALIGNED).  That is
+// looked for only where a sum is not finite: the same test in all threads of the group.  (A layer norm of a row with
+// an infinity is NaN anyway.)
+template <bool ALIGNED, bool FACTORS, int T, int C, int E, class A, class Cols>
 __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, A inv, const Cols &c, const Group &g,
                                                Area<A> &area, int &buf)
 {
@@ -401,11 +405,22 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
 #pragma unroll
         for (int i = 0; i < E; ++i) t[i] = c.template inside<ALIGNED>(2 * i, t[i] + minus);
     }
-    Two<A> sum = t[0] * t[0];
+    auto squares = [&] {
+        Two<A> sum = t[0] * t[0];
 #pragma unroll
-    for (int i = 1; i < E; ++i) sum = fused_ma(t[i], t[i], sum);
-    s[0] = joined(sum);
-    group_sum<T, C, 1, A>(s, g, area, buf);
+        for (int i = 1; i < E; ++i) sum = fused_ma(t[i], t[i], sum);
+        s[0] = joined(sum);
+        group_sum<T, C, 1, A>(s, g, area, buf);
+    };
+    squares();
+    if constexpr (FACTORS && ALIGNED) {
+        const bool finite = s[0] <= (sizeof(A) == 8 ? A(1.7976931348623157e308) : A(3.4028234e38f));
+        if (T > 0 ? __any_sync(0xffffffffu, !finite) : !finite) {       // the groups of a warp shuffle together
+#pragma unroll
+            for (int i = 0; i < E; ++i) t[i] = c.template inside<ALIGNED>(2 * i, t[i]);
+            squares();
+        }
+    }
     n.r = group_rsqrt(fused_ma(s[0], inv, eps));
     return n;
 }
@@ -464,7 +479,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fr.get2(k);
         if (post_kind != FO_NORM_NONE) {
-            post = row_norm<ALIGNED, T, C>(h, post_kind, A(p.post.eps), inv, c, group, area, buf);
+            post = row_norm<ALIGNED, false, T, C>(h, post_kind, A(p.post.eps), inv, c, group, area, buf);
             const Two<A> r = both(post.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
@@ -489,7 +504,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
         const Two<A> k2 = both(scale);
 #pragma unroll
         for (int k = 0; k < E; k += 2) h[k / 2] = fused_ma(h[k / 2], k2, xr.get2(k));
-        if (p.cols != c.threads() * E) {     // zeros outside the row again: not what a bias or an infinite factor left there
+        if (kAny && ALIGNED && p.post.bias && p.cols != c.threads() * E) {  // a bias leaves no zeros outside the row
 #pragma unroll
             for (int k = 0; k < E; k += 2) h[k / 2] = c.template inside<ALIGNED>(k, h[k / 2]);
         }
@@ -499,7 +514,7 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     }
     if ((!kAny && BLK) || p.h) store_row<ALIGNED, TS, E, true>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
     if (pre_kind != FO_NORM_NONE) {
-        pre = row_norm<ALIGNED, T, C>(h, pre_kind, A(p.pre.eps), inv, c, group, area, buf);
+        pre = row_norm<ALIGNED, BLK, T, C>(h, pre_kind, A(p.pre.eps), inv, c, group, area, buf);
         if (!kAny || p.y) {
             const Two<A> r = both(pre.r);
 #pragma unroll
