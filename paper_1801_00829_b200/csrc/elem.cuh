@@ -231,30 +231,53 @@ __device__ __forceinline__ double group_rsqrt(double v) { return rsqrt(v); }
 // reciprocal, a relative error of a few 2^-22 over the range where a sigmoid is not 0 or 1; the tangent is
 // the library's in every case, because near zero its relative error is what a gate that starts at
 // zero sees.
+// A slope is a product with the small side of the gate, which comes from the exponential itself: 1 - s of an s that is
+// rounded near 1 has few correct bits (at g = 12 one in a hundred is wrong, beyond 17 nothing is left).
 __device__ __forceinline__ float tanh_of(float g) { return tanhf(g); }
 __device__ __forceinline__ double tanh_of(double g) { return tanh(g); }
 
+// exp(g * factor)
 template <bool FAST>
-__device__ __forceinline__ Two<float> sigmoid(Two<float> g)
+__device__ __forceinline__ Two<float> exponential(Two<float> g, float factor)
 {
     if constexpr (FAST) {
-        const Two<float> x = g * both(-1.4426950408889634f);
-        float ea, eb, a, b;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ea) : "f"(first(x)));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(eb) : "f"(second(x)));
-        const Two<float> d = two(ea, eb) + both(1.0f);            // infinity gives 0
+        const Two<float> x = g * both(1.4426950408889634f * factor);
+        float a, b;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(x)));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(x)));
+        return two(a, b);
+    } else {
+        return two(expf(factor * first(g)), expf(factor * second(g)));
+    }
+}
+template <bool FAST>
+__device__ __forceinline__ Two<double> exponential(Two<double> g, double factor)
+{
+    return two(exp(factor * g.a), exp(factor * g.b));
+}
+// 1 / (1 + e)
+template <bool FAST>
+__device__ __forceinline__ Two<float> one_over_more(Two<float> e)
+{
+    const Two<float> d = e + both(1.0f);                      // infinity gives 0
+    if constexpr (FAST) {
+        float a, b;
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(d)));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(d)));
         return two(a, b);
     } else {
-        return two(1.0f / (1.0f + expf(-first(g))), 1.0f / (1.0f + expf(-second(g))));
+        return two(1.0f / first(d), 1.0f / second(d));
     }
 }
 template <bool FAST>
-__device__ __forceinline__ Two<double> sigmoid(Two<double> g)
+__device__ __forceinline__ Two<double> one_over_more(Two<double> e)
 {
-    return two(1.0 / (1.0 + exp(-g.a)), 1.0 / (1.0 + exp(-g.b)));
+    return two(1.0 / (1.0 + e.a), 1.0 / (1.0 + e.b));
 }
+__device__ __forceinline__ Two<float> finite(Two<float> e) { return two(fminf(first(e), 0x1p127f), fminf(second(e), 0x1p127f)); }
+__device__ __forceinline__ Two<double> finite(Two<double> e) { return two(fmin(e.a, 0x1p1023), fmin(e.b, 0x1p1023)); }
+__device__ __forceinline__ Two<float> magnitudes(Two<float> g) { return two(fabsf(first(g)), fabsf(second(g))); }
+__device__ __forceinline__ Two<double> magnitudes(Two<double> g) { return two(fabs(g.a), fabs(g.b)); }
 
 template <int KIND, bool FAST, class A>
 __device__ __forceinline__ Two<A> activate(Two<A> g)
@@ -262,7 +285,7 @@ __device__ __forceinline__ Two<A> activate(Two<A> g)
     if constexpr (KIND == FO_ACT_LINEAR) return g;
     else if constexpr (KIND == FO_ACT_TANH) return two(tanh_of(first(g)), tanh_of(second(g)));
     else {
-        const Two<A> s = sigmoid<FAST>(g);
+        const Two<A> s = one_over_more<FAST>(exponential<FAST>(g, A(-1)));
         return KIND == FO_ACT_SILU ? g * s : s;
     }
 }
@@ -270,16 +293,16 @@ __device__ __forceinline__ Two<A> activate(Two<A> g)
 template <int KIND, bool FAST, class A>
 __device__ __forceinline__ Two<A> activate_slope(Two<A> g, Two<A> &slope)
 {
-    const Two<A> one = both(A(1)), minus = both(A(-1));
     if constexpr (KIND == FO_ACT_LINEAR) {
-        slope = one;
+        slope = both(A(1));
         return g;
-    } else if constexpr (KIND == FO_ACT_TANH) {
-        const Two<A> t = two(tanh_of(first(g)), tanh_of(second(g)));
-        slope = fused_ma(t * minus, t, one);
-        return t;
+    } else if constexpr (KIND == FO_ACT_TANH) {              // 4 q / (1 + q)^2, q = exp(-2 |g|)
+        const Two<A> q = exponential<FAST>(magnitudes(g), A(-2)), r = one_over_more<FAST>(q);
+        slope = q * both(A(4)) * r * r;
+        return two(tanh_of(first(g)), tanh_of(second(g)));
     } else {
-        const Two<A> s = sigmoid<FAST>(g), rest = fused_ma(s, minus, one);
+        const Two<A> e = exponential<FAST>(g, A(-1)), s = one_over_more<FAST>(e);
+        const Two<A> rest = finite(e) * s;                   // 1 - s; anything where s is 0 and so the slope
         if constexpr (KIND == FO_ACT_SIGMOID) {
             slope = s * rest;
             return s;

@@ -73,3 +73,54 @@ def test_an_infinite_factor_stays_in_its_column(stream, block, where, cols):
     assert bool(torch.isinf(h[:, -1]).all()) and bool(torch.isfinite(h[:, :-1]).all())
     assert bool((y[:, :-1] == 0).all()) and bool(torch.isnan(y[:, -1]).all())
     assert bool((stats[3] == 0).all()) and bool(torch.isfinite(stats).all())
+
+
+def gate_parts(act, g):
+    """act(g), act'(g) and the magnitude act' is added up from, in float64 and without a difference that cancels."""
+    if act == "tanh":
+        q = np.exp(-2.0 * np.abs(g))
+        return np.tanh(g), 4.0 * q / (1.0 + q) ** 2, 4.0 * q / (1.0 + q) ** 2
+    e = np.exp(-np.abs(g))
+    small, large = e / (1.0 + e), 1.0 / (1.0 + e)
+    s, rest = np.where(g < 0, small, large), np.where(g < 0, large, small)
+    if act == "sigmoid":
+        return s, s * rest, s * rest
+    return g * s, s * (1.0 + g * rest), s * (1.0 + np.abs(g) * rest)
+
+
+PAIRS = [(F64, F64), (F32, F32), (BF16, BF16), (F16, F16), (F32, BF16), (F32, F16)]
+
+
+def gates(n, block, least=-40.0, most=40.0):
+    return torch.linspace(least, most, n, dtype=torch.float64).to(block).cuda()
+
+
+@pytest.mark.parametrize("stream,block", PAIRS)
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "tanh"])
+@pytest.mark.parametrize("cols", [256, 1001])
+def test_slopes_of_open_and_closed_gates(stream, block, act, cols):
+    """The gate's gradient relative to act'(g) itself: the slope of an open gate is a small number, not the difference of
+    two that are near 1.  Its factors: an exponential, a sum, a reciprocal and at most six products, within 64 rounding
+    units together."""
+    c = Case(5, cols, stream, block, None, None, "linear", None, col_scale=False)
+    g = gates(5 * cols, block).reshape(5, cols)
+    got = fo.fused_block_norm_grad(c.dh, None, None, c.f, None, gate=("cell", g, act), scale=c.scale)
+    qz = host(c.dh) * c.scale * host(c.f)
+    _, slope, size = gate_parts(act, host(g))
+    close(got["gate"], qz * slope, np.abs(qz) * size, unit(block), "gate")
+
+
+@pytest.mark.parametrize("stream,block", PAIRS)
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "tanh"])
+@pytest.mark.parametrize("access", ["row", "col"])
+def test_slopes_of_shared_gates(stream, block, act, access):
+    """A gate per row or column has its gradient in 32 bits (64): as many more units as terms are added."""
+    rows, cols = (300, 65) if access == "row" else (9, 300)
+    c = Case(rows, cols, stream, block, None, None, "linear", None, col_scale=False)
+    g = gates(300, block)
+    got = fo.fused_block_norm_grad(c.dh, None, None, c.f, None, gate=(access, g, act), scale=c.scale)
+    qz = host(c.dh) * c.scale * host(c.f)
+    _, slope, size = gate_parts(act, host(g)[:, None] if access == "row" else host(g))
+    axis = 1 if access == "row" else 0
+    close(got["gate"], (qz * slope).sum(axis=axis), (np.abs(qz) * size).sum(axis=axis), unit(block), "gate",
+          rows=qz.shape[axis])
