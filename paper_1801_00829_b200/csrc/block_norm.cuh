@@ -445,7 +445,8 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 {
     using A = Acc<TB>;
     constexpr int V = 16 / (int)sizeof(TB);
-    constexpr bool kFast = sizeof(TB) == 2, kAny = !LEAN;
+    constexpr int kHow = sizeof(TB) > 2 ? kExact : sizeof(TS) > 2 ? kClose : kRough;      // h has the stream's type
+    constexpr bool kAny = !LEAN;
     __shared__ Area<A> area;
     __shared__ Stage<TS, V, T, ALIGNED> stages;
     unsigned char *const stage = stages.of_warp();
@@ -488,16 +489,16 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
         }
         if (GATE == kSharedGate && p.gate_access == FO_AT_ROW) {
             const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
-            with_activation(p.gate_act, [&](auto kind) { scale *= first(activate<decltype(kind)::value, kFast, A>(both(g))); });
+            with_activation(p.gate_act, [&](auto kind) { scale *= first(activate<decltype(kind)::value, kHow, A>(both(g))); });
         } else if (GATE == kCellGate) {
             with_activation(p.gate_act, [&](auto kind) {
 #pragma unroll
-                for (int k = 0; k < E; k += 2) h[k / 2] = h[k / 2] * activate<decltype(kind)::value, kFast, A>(gr.get2(k));
+                for (int k = 0; k < E; k += 2) h[k / 2] = h[k / 2] * activate<decltype(kind)::value, kHow, A>(gr.get2(k));
             });
         } else if (GATE == kSharedGate) {
             with_activation(p.gate_act, [&](auto kind) {
                 with_vector<ALIGNED, TB, E>(h, p.gate, false, c,
-                                   [](Two<A> z, Two<A> g) { return z * activate<decltype(kind)::value, kFast, A>(g); });
+                                   [](Two<A> z, Two<A> g) { return z * activate<decltype(kind)::value, kHow, A>(g); });
             });
         }
         if (p.col_scale) with_vector<ALIGNED, TB, E>(h, p.col_scale, wide, c, times);
@@ -586,7 +587,8 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
     constexpr int V = 16 / (int)sizeof(TB);
     constexpr int P = 16 / (int)sizeof(A);                   // elements worked on at a time: what registers hold
     constexpr int kGroups = T > 0 ? kGroupCta / kDivisor<T> : 1;
-    constexpr bool kFast = sizeof(TB) == 2;
+    constexpr int kHow = sizeof(TB) > 2 ? kExact : kClose;   // sums have 32 bits or more
+    constexpr int kSlope = kHow == kClose && GATE == kCellGate ? kRough : kHow;    // the gate's own gradient has the block's type
     __shared__ Area<A> area;
     __shared__ Stage<TS, V, T, ALIGNED> stages;
     unsigned char *const stage = stages.of_warp();
@@ -704,7 +706,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
             if (row_gate) {
                 const A g = ok ? widen<TB>(static_cast<const TB *>(p.gate)[row * p.ld_gate]) : A(0);
                 with_activation(p.gate_act, [&](auto kind) {
-                    row_act = activate_slope<decltype(kind)::value, kFast, A>(both(g), row_slope);
+                    row_act = activate_slope<decltype(kind)::value, kHow, kHow, A>(both(g), row_slope);
                 });
             }
             Two<A> along = both(A(0)), level = both(A(0)), gate_sum = both(A(0));
@@ -736,7 +738,7 @@ block_norm_grad_kernel(const __grid_constant__ BlockNormGradParams p)
                     with_activation(p.gate_act, [&](auto kind) {
 #pragma unroll
                         for (int i = 0; i < P / 2; ++i)
-                            a[i] = activate_slope<decltype(kind)::value, kFast, A>(g[i], slope[i]);
+                            a[i] = activate_slope<decltype(kind)::value, kHow, kSlope, A>(g[i], slope[i]);
                     });
                 } else if (row_gate) {
 #pragma unroll

@@ -227,81 +227,85 @@ __device__ __forceinline__ void let_later_start() { asm volatile("griddepcontrol
 __device__ __forceinline__ float group_rsqrt(float v) { return rsqrtf(v); }      // within 2 units
 __device__ __forceinline__ double group_rsqrt(double v) { return rsqrt(v); }
 
-// act(g) and its derivative.  FAST (results rounded to 16 bits): the hardware's exponential and
-// reciprocal, a relative error of a few 2^-22 over the range where a sigmoid is not 0 or 1; the tangent is
-// the library's in every case, because near zero its relative error is what a gate that starts at
-// zero sees.
+// act(g) and its derivative, HOW exactly: by CUDA's functions (results of 32 or 64 bits); CLOSE by the hardware's exponential
+// and reciprocal (16-bit gates whose results have 32 bits), a relative error of a few 2^-22 over the range where a
+// sigmoid is not 0 or 1; ROUGH the same with a rounded exponent, which adds |g| 2^-24 (results that are rounded to
+// 16 bits).  The tangent is the library's in every case, because near zero its relative error is
+// what a gate that starts at zero sees.
 // A slope is a product with the small side of the gate, which comes from the exponential itself: 1 - s of an s that is
 // rounded near 1 has few correct bits (at g = 12 one in a hundred is wrong, beyond 17 nothing is left).
+enum How { kExact, kClose, kRough };
+
 __device__ __forceinline__ float tanh_of(float g) { return tanhf(g); }
 __device__ __forceinline__ double tanh_of(double g) { return tanh(g); }
-
-// exp(g * factor)
-template <bool FAST>
-__device__ __forceinline__ Two<float> exponential(Two<float> g, float factor)
-{
-    if constexpr (FAST) {
-        const Two<float> x = g * both(1.4426950408889634f * factor);
-        float a, b;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(x)));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(x)));
-        return two(a, b);
-    } else {
-        return two(expf(factor * first(g)), expf(factor * second(g)));
-    }
-}
-template <bool FAST>
-__device__ __forceinline__ Two<double> exponential(Two<double> g, double factor)
-{
-    return two(exp(factor * g.a), exp(factor * g.b));
-}
-// 1 / (1 + e)
-template <bool FAST>
-__device__ __forceinline__ Two<float> one_over_more(Two<float> e)
-{
-    const Two<float> d = e + both(1.0f);                      // infinity gives 0
-    if constexpr (FAST) {
-        float a, b;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(d)));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(d)));
-        return two(a, b);
-    } else {
-        return two(1.0f / first(d), 1.0f / second(d));
-    }
-}
-template <bool FAST>
-__device__ __forceinline__ Two<double> one_over_more(Two<double> e)
-{
-    return two(1.0 / (1.0 + e.a), 1.0 / (1.0 + e.b));
-}
 __device__ __forceinline__ Two<float> finite(Two<float> e) { return two(fminf(first(e), 0x1p127f), fminf(second(e), 0x1p127f)); }
 __device__ __forceinline__ Two<double> finite(Two<double> e) { return two(fmin(e.a, 0x1p1023), fmin(e.b, 0x1p1023)); }
 __device__ __forceinline__ Two<float> magnitudes(Two<float> g) { return two(fabsf(first(g)), fabsf(second(g))); }
 __device__ __forceinline__ Two<double> magnitudes(Two<double> g) { return two(fabs(g.a), fabs(g.b)); }
 
-template <int KIND, bool FAST, class A>
+__device__ __forceinline__ Two<float> hardware_exp2(Two<float> x)
+{
+    float a, b;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(x)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(x)));
+    return two(a, b);
+}
+// exp(factor * g), factor -1 or -2
+template <int HOW>
+__device__ __forceinline__ Two<float> exponential(Two<float> g, float factor)
+{
+    if constexpr (HOW == kExact) return two(expf(factor * first(g)), expf(factor * second(g)));
+    else if constexpr (HOW == kRough) return hardware_exp2(g * both(1.4426950408889634f * factor));
+    // log2(e) in two parts of one sign: times the first, of 13 bits, a number of 16 bits (11 of them significant) is
+    // exact, and where one power is 0 or infinite the other does not turn it
+    else return hardware_exp2(g * both(0x1.715p+0f * factor)) * hardware_exp2(g * both(0x1.1d94aep-14f * factor));
+}
+template <int HOW>
+__device__ __forceinline__ Two<double> exponential(Two<double> g, double factor)
+{
+    return two(exp(factor * g.a), exp(factor * g.b));
+}
+// 1 / (1 + e)
+template <int HOW>
+__device__ __forceinline__ Two<float> one_over_more(Two<float> e)
+{
+    const Two<float> d = e + both(1.0f);                      // infinity gives 0
+    if constexpr (HOW == kExact) return two(1.0f / first(d), 1.0f / second(d));
+    float a, b;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(first(d)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(second(d)));
+    return two(a, b);
+}
+template <int HOW>
+__device__ __forceinline__ Two<double> one_over_more(Two<double> e)
+{
+    return two(1.0 / (1.0 + e.a), 1.0 / (1.0 + e.b));
+}
+
+template <int KIND, int HOW, class A>
 __device__ __forceinline__ Two<A> activate(Two<A> g)
 {
     if constexpr (KIND == FO_ACT_LINEAR) return g;
     else if constexpr (KIND == FO_ACT_TANH) return two(tanh_of(first(g)), tanh_of(second(g)));
     else {
-        const Two<A> s = one_over_more<FAST>(exponential<FAST>(g, A(-1)));
+        const Two<A> s = one_over_more<HOW>(exponential<HOW>(g, A(-1)));
         return KIND == FO_ACT_SILU ? g * s : s;
     }
 }
 
-template <int KIND, bool FAST, class A>
+// SLOPE: how exactly the slope is needed, where it takes a computation of its own.
+template <int KIND, int HOW, int SLOPE, class A>
 __device__ __forceinline__ Two<A> activate_slope(Two<A> g, Two<A> &slope)
 {
     if constexpr (KIND == FO_ACT_LINEAR) {
         slope = both(A(1));
         return g;
     } else if constexpr (KIND == FO_ACT_TANH) {              // 4 q / (1 + q)^2, q = exp(-2 |g|)
-        const Two<A> q = exponential<FAST>(magnitudes(g), A(-2)), r = one_over_more<FAST>(q);
+        const Two<A> q = exponential<SLOPE>(magnitudes(g), A(-2)), r = one_over_more<SLOPE>(q);
         slope = q * both(A(4)) * r * r;
         return two(tanh_of(first(g)), tanh_of(second(g)));
     } else {
-        const Two<A> e = exponential<FAST>(g, A(-1)), s = one_over_more<FAST>(e);
+        const Two<A> e = exponential<HOW>(g, A(-1)), s = one_over_more<HOW>(e);
         const Two<A> rest = finite(e) * s;                   // 1 - s; anything where s is 0 and so the slope
         if constexpr (KIND == FO_ACT_SIGMOID) {
             slope = s * rest;

@@ -124,3 +124,60 @@ def test_slopes_of_shared_gates(stream, block, act, access):
     axis = 1 if access == "row" else 0
     close(got["gate"], (qz * slope).sum(axis=axis), (np.abs(qz) * size).sum(axis=axis), unit(block), "gate",
           rows=qz.shape[axis])
+
+
+@pytest.mark.parametrize("stream,block", [(F32, F32), (F32, BF16), (F32, F16)])
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+@pytest.mark.parametrize("access", ["cell", "row", "col"])
+def test_a_32_bit_stream_gets_32_bit_gates(stream, block, act, access):
+    """h in 32 bits, gate values of 4 to 60 in magnitude: the activation is an exponential within 2^-22 (four rounding
+    units), a sum and a reciprocal (three units), and h takes four more products: 16 units hold all of it."""
+    rows, cols = 40, 264
+    c = Case(rows, cols, stream, block, None, None, "linear", None, col_scale=False)
+    n = {"cell": rows * cols, "row": rows, "col": cols}[access]
+    g = gates(n, block, -60.0, 60.0)
+    g = g.reshape(rows, cols) if access == "cell" else g
+    h, _, _ = fo.fused_block_norm(torch.zeros(rows, cols, device="cuda"), c.f, gate=(access, g, act), scale=c.scale)
+    a, _, _ = gate_parts(act, host(g)[:, None] if access == "row" else host(g))
+    want = host(c.f) * c.scale * a
+    assert h.dtype == F32 and np.all(np.abs(host(h) - want) <= 16 * 2.0 ** -24 * np.abs(want))
+
+
+@pytest.mark.parametrize("block", [BF16, F16])
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+@pytest.mark.parametrize("access", ["cell", "row", "col"])
+def test_summed_gradients_get_32_bit_gates(block, act, access):
+    """The gradient of a column scale is in 32 bits beside 16-bit blocks: one row, so that its only term is seen.  As
+    above, two products more."""
+    cols = 264
+    c = Case(1, cols, block, block, None, None, "linear", None)
+    for value in (-60.0, -25.5, -11.25, -4.5, 4.5, 30.0):
+        g = torch.full((1, cols) if access == "cell" else (1,) if access == "row" else (cols,), value, dtype=block, device="cuda")
+        got = fo.fused_block_norm_grad(c.dh, None, None, c.f, None, gate=(access, g, act), scale=c.scale, col_scale=c.col_scale)
+        want = (host(c.dh) * c.scale * host(c.f) * gate_parts(act, np.full((1, cols), value))[0])[0]
+        assert np.all(np.abs(host(got["col_scale"]) - want) <= 18 * 2.0 ** -24 * np.abs(want)), value
+
+
+@pytest.mark.parametrize("stream,block", PAIRS)
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "tanh"])
+def test_gates_at_the_ends_of_the_range(stream, block, act):
+    """Gates of the type's largest values, infinities and NaN: a closed gate lets nothing through, and an open one's slope
+    is nothing (SiLU's is one)."""
+    top = torch.finfo(block).max
+    values = torch.tensor([-top, -1e4, -200.0, 200.0, 1e4, top, float("inf"), float("-inf"), float("nan")], dtype=torch.float64)
+    g = values.to(block).cuda()
+    x = torch.zeros(4, 9, dtype=stream, device="cuda")
+    f = torch.ones(4, 9, dtype=block, device="cuda")
+    h, _, _ = fo.fused_block_norm(x, f, gate=("col", g, act))
+    got = fo.fused_block_norm_grad(torch.ones_like(x), None, None, f, None, gate=("col", g, act))
+    a, slope = host(h)[0], host(got["gate"])
+    assert np.isnan(a[8]) and np.isnan(slope[8]) and np.array_equal(host(got["f"])[0], a, equal_nan=True)
+    none = 1e4 * np.exp(-200.0)                             # what +-200 leave in float64; less than 32 bits hold
+    closed = {"sigmoid": [0, 1, 2, 7], "silu": [0, 1, 2], "tanh": []}[act]
+    assert (np.abs(a[closed]) <= none).all()
+    if act == "tanh":
+        assert a[:8].tolist() == [-1, -1, -1, 1, 1, 1, 1, -1]
+    else:
+        assert a[3:7].tolist() == ([1.0] * 4 if act == "sigmoid" else host(g)[3:7].tolist())
+    flat = [0, 1, 2] if act == "silu" else list(range(8))
+    assert (np.abs(slope[flat]) <= none).all() and (act != "silu" or (slope[3:6] == 4.0).all())
