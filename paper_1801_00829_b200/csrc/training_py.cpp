@@ -51,6 +51,12 @@ const at::Tensor *tensor_of(PyObject *o, const char *name)
     return &THPVariable_Unpack(o);
 }
 
+at::ScalarType dtype_of(PyObject *o, const char *name)
+{
+    if (!THPDtype_Check(o)) throw Refused(std::string(name) + " is not a dtype");
+    return reinterpret_cast<THPDtype *>(o)->scalar_type;
+}
+
 // What every matrix and vector of one call has to agree with.
 struct Call {
     int64_t rows, cols;
@@ -205,7 +211,7 @@ PyObject *or_none(const at::Tensor &t)
     Py_RETURN_NONE;
 }
 
-// block_norm(x, f, post, gate, scale, col_scale, pre, out_h, out_y, stats, block_type)
+// block_norm(x, f, post, gate, scale, col_scale, pre, out_h, out_y, stats, block_type, stream_type)
 PyObject *block_norm_impl(PyObject *const *a)
 {
     const at::Tensor *x = tensor_of(a[0], "x"), *f = tensor_of(a[1], "f"), *col_scale = tensor_of(a[5], "col_scale");
@@ -218,13 +224,17 @@ PyObject *block_norm_impl(PyObject *const *a)
     const double scale = PyFloat_AsDouble(a[4]);
     const int want_stats = PyObject_IsTrue(a[9]);
     if (PyErr_Occurred()) throw Raised();
-    const at::ScalarType stream = x || !out_h ? first.scalar_type() : out_h->scalar_type();
+    at::ScalarType stream = x || !out_h ? first.scalar_type() : out_h->scalar_type();
+    if (a[11] != Py_None) {
+        const at::ScalarType wanted = dtype_of(a[11], "stream_type");
+        require((!x && !out_h) || wanted == stream, "stream_type is not the type of x and out_h");
+        stream = wanted;
+    }
     at::ScalarType block = f ? f->scalar_type() : out_y ? out_y->scalar_type() : stream;
     if (!f) {
         require(!post.given() && !gate.t && !col_scale, "post, gate and col_scale need a block output f");
         if (a[10] != Py_None) {
-            require(THPDtype_Check(a[10]), "block_type is not a dtype");
-            block = reinterpret_cast<THPDtype *>(a[10])->scalar_type;
+            block = dtype_of(a[10], "block_type");
         } else if (!out_y && stream == at::kFloat) {
             block = vector_type(block, post, pre, col_scale);       // 16-bit weights: the next block's type
         }
@@ -607,7 +617,7 @@ PyObject *connect(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
-PyMethodDef g_methods[] = {method<block_norm_impl, 11>("block_norm"), method<block_norm_grad_impl, 11>("block_norm_grad"),
+PyMethodDef g_methods[] = {method<block_norm_impl, 12>("block_norm"), method<block_norm_grad_impl, 11>("block_norm_grad"),
                            method<grad_norm_impl, 7>("grad_norm"), method<adamw_impl, 15>("adamw"),
                            method<check_grads_impl, 2>("check_grads"), method<check_adam_impl, 9>("check_adam"),
                            {"connect", connect, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};

@@ -41,15 +41,15 @@ def _native():
 
 
 def fused_block_norm(x=None, f=None, post=None, gate=None, scale=1.0, col_scale=None, pre=None, out_h=None, out_y=None,
-                     stats=False, block_type=None):
+                     stats=False, block_type=None, stream_type=None):
     """h = x + scale * col_scale * act(gate) * norm(f; post),  y = norm(h; pre), row by row in one pass.
 
     x (the residual stream) or f (the block's output) may be None; without f the result is the norm of
     x alone.  Returns (h, y, stats): h is x itself without f, y is None without `pre`; stats (float, 4 x
     rows, with stats=True) is what fused_block_norm_grad needs.  y has the type of f, or without f
     `block_type` (default: that of x; beside a float32 x that of the norm's weights).  out_h may be x.  x None: h has
-    the type of f or of out_h."""
-    return (_extension or _native()).block_norm(x, f, post, gate, scale, col_scale, pre, out_h, out_y, stats, block_type)
+    `stream_type` (float32 beside an f of 16 bits, where the stream begins with this block), or else the type of out_h or f."""
+    return (_extension or _native()).block_norm(x, f, post, gate, scale, col_scale, pre, out_h, out_y, stats, block_type, stream_type)
 
 
 def fused_block_norm_grad(dh=None, dy=None, h=None, f=None, stats=None, post=None, gate=None, scale=1.0, col_scale=None,

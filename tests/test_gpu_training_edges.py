@@ -181,3 +181,31 @@ def test_gates_at_the_ends_of_the_range(stream, block, act):
         assert a[3:7].tolist() == ([1.0] * 4 if act == "sigmoid" else host(g)[3:7].tolist())
     flat = [0, 1, 2] if act == "silu" else list(range(8))
     assert (np.abs(slope[flat]) <= none).all() and (act != "silu" or (slope[3:6] == 4.0).all())
+
+
+@pytest.mark.parametrize("block", [BF16, F16])
+@pytest.mark.parametrize("mode", [("rms", "cell", "sigmoid", "rms"), (None, "row", "silu", "layer"), ("layer", None, "linear", None)])
+@pytest.mark.parametrize("rows,cols", [(1, 64), (33, 1000), (5, 1001)])
+def test_a_32_bit_stream_that_begins_with_the_block(block, mode, rows, cols):
+    """Without x the type of h is asked for: not rounded to the block's 16 bits."""
+    c = Case(rows, cols, F32, block, *mode, residual=False)
+    h, y, stats = fo.fused_block_norm(None, c.f, stats=True, stream_type=F32, **c.how())
+    want = ref.block_norm(None, host(c.f), **c.host_how())
+    assert h.dtype == F32 and (y is None or y.dtype == block)
+    close(h, *want["h"], unit(F32), "h")
+    if c.pre:
+        close(y, *want["y"], unit(F32), "y")
+    c.check_backward(h, stats)
+    out = torch.empty(rows, cols, device="cuda")
+    again, _, _ = fo.fused_block_norm(None, c.f, out_h=out, stream_type=F32, **c.how())
+    assert again is out and torch.equal(out, h)
+
+
+def test_stream_types_that_are_refused():
+    x, f = torch.zeros(3, 8, device="cuda"), torch.zeros(3, 8, dtype=BF16, device="cuda")
+    h, _, _ = fo.fused_block_norm(x, f, stream_type=F32)
+    assert h.dtype == F32
+    for kw in (dict(x=x, f=f, stream_type=BF16), dict(f=f, stream_type=F16), dict(f=f, stream_type=F64), dict(f=f, stream_type="float32"),
+               dict(f=f, out_h=x, stream_type=BF16)):
+        with pytest.raises(ValueError):
+            fo.fused_block_norm(**kw)
