@@ -2,6 +2,7 @@
 // for small inputs take less time on the GPU than a call assembled in Python takes on the host (block norm 15 us, its
 // gradient 30, clipping and AdamW 13 to 16; here 7, 12 and less than the GPU takes).  Nothing here computes.
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -57,6 +58,19 @@ at::ScalarType dtype_of(PyObject *o, const char *name)
     return reinterpret_cast<THPDtype *>(o)->scalar_type;
 }
 
+// The operators record no graph: a tensor that autograd follows would lose its gradient without a word.
+void outside_graph(const at::Tensor &t, const char *name)
+{
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        throw Refused(std::string(name) + " requires a gradient, and this call records none: call it under torch.no_grad(), or in an "
+                                          "autograd.Function whose backward is fused_block_norm_grad");
+}
+// `t` was written: what autograd saved of it is no longer what it was.
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // What every matrix and vector of one call has to agree with.
 struct Call {
     int64_t rows, cols;
@@ -82,6 +96,7 @@ struct Call {
         if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || t->scalar_type() != type || !t->is_cuda()
             || t->get_device() != gpu)
             refuse(*t, name, "a matrix of the call's shape", type);
+        outside_graph(*t, name);
         if (cols > 1 && t->stride(1) != 1) throw Refused(std::string("rows of ") + name + " must be contiguous");
         *ld = t->stride(0);
         if (*ld < cols) {
@@ -96,6 +111,7 @@ struct Call {
         if (t->dim() != 1 || t->size(0) != cols || t->scalar_type() != type || !t->is_cuda() || t->get_device() != gpu
             || !t->is_contiguous())
             refuse(*t, name, "a contiguous vector over the columns", type);
+        outside_graph(*t, name);
         return t->data_ptr();
     }
     at::Tensor make(at::IntArrayRef sizes, at::ScalarType type) const
@@ -162,6 +178,7 @@ struct Gate {
         const bool shaped = t->dim() == 1 || (t->dim() == 2 && t->size(1 - along) == 1);
         if (!shaped || t->size(along) != n || t->scalar_type() != type || !t->is_cuda() || t->get_device() != call.gpu)
             call.refuse(*t, "gate", access == FO_AT_ROW ? "a vector over the rows" : "a vector over the columns", type);
+        outside_graph(*t, "gate");
         ld = n > 1 ? t->stride(along) : 1;
         require(access == FO_AT_ROW ? ld >= 1 : ld == 1, "stride of the gate");
         p = t->data_ptr();
@@ -272,6 +289,8 @@ PyObject *block_norm_impl(PyObject *const *a)
         const OnGpu on(call.gpu);
         check_status(fused_block_norm(&n, c10::cuda::getCurrentCUDAStream(call.gpu).stream()), "fused_block_norm");
     }
+    if (out_h) written(*out_h);
+    if (out_y) written(*out_y);
     PyObject *ho;
     if (h.defined()) {
         ho = out_h ? (Py_INCREF(a[7]), a[7]) : THPVariable_Wrap(h);
@@ -342,6 +361,7 @@ PyObject *block_norm_grad_impl(PyObject *const *a)
         if (stats->dim() != 2 || stats->size(0) != 4 || stats->size(1) != call.rows || stats->scalar_type() != sums
             || !stats->is_contiguous() || !stats->is_cuda() || stats->get_device() != call.gpu)
             call.refuse(*stats, "stats", "4 x rows", sums);
+        outside_graph(*stats, "stats");
         n.stats = stats->data_ptr();
     }
 
@@ -424,9 +444,9 @@ public:
     {
         if (count() != n) throw Refused(std::string(name_) + ": " + std::to_string(count()) + " tensors for " + std::to_string(n));
     }
-    // put(k, address of tensor k's elements), of which there have to be n(k)
+    // put(k, address of tensor k's elements), of which there have to be n(k); `write`: the call will write them
     template <class Size, class Put>
-    void read(const Kind &kind, Size n, Put put) const
+    void read(const Kind &kind, bool write, Size n, Put put) const
     {
         const caffe2::TypeMeta type = c10::scalarTypeToTypeMeta(kind.type);
         const c10::Device device(c10::kCUDA, kind.gpu);
@@ -448,6 +468,7 @@ public:
             const size_t at_byte = (size_t)t.storage_offset() * bytes;
             if (want && held < at_byte + (size_t)want * bytes) refuse("a tensor's storage is smaller than the tensor");
             put(k, want ? begin + at_byte : nullptr);
+            if (write) written(THPVariable_Unpack(o));
         }
     }
 };
@@ -470,12 +491,12 @@ struct GradTensors {
     Kind kind;
     at::ScalarType out_type;
 
-    GradTensors(PyObject *grads, PyObject *outs)
+    GradTensors(PyObject *grads, PyObject *outs, bool write)
     {
         const Tensors in(grads, "grads");
         kind = kind_of(in), out_type = kind.type;
         c.resize(in.count());
-        in.read(kind, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) { c[k].in = c[k].out = p; });
+        in.read(kind, write && in.is(outs), [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) { c[k].in = c[k].out = p; });
         if (outs == Py_None || in.is(outs)) return;
         const Tensors out(outs, "outs");
         out.same_count(c.size());
@@ -483,7 +504,7 @@ struct GradTensors {
         out_type = out.at(0).scalar_type();
         if (out_type != kind.type && !(sixteen_bits(kind.type) && out_type == at::kFloat))
             throw Refused(std::string("clipped values of ") + c10::toString(out_type) + " from gradients of " + c10::toString(kind.type));
-        out.read({out_type, kind.gpu}, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, [&](size_t k, void *p) { c[k].out = p; });
+        out.read({out_type, kind.gpu}, write, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, [&](size_t k, void *p) { c[k].out = p; });
     }
 };
 
@@ -493,13 +514,13 @@ struct AdamTensors {
     Kind kind;
     at::ScalarType weight_type = at::kBFloat16;
 
-    explicit AdamTensors(PyObject *const *a)
+    AdamTensors(PyObject *const *a, bool write)
     {
         const Tensors grads(a[1], "grads");
         kind = kind_of(grads);
         c.resize(grads.count());
         require(PyBytes_Check(a[8]) && (size_t)PyBytes_GET_SIZE(a[8]) == c.size() * sizeof(double), "decay: one value per tensor is needed");
-        grads.read(kind, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) {
+        grads.read(kind, false, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) {
             c[k].g = p;
             memcpy(&c[k].decay, PyBytes_AS_STRING(a[8]) + k * sizeof(double), sizeof(double));
         });
@@ -507,8 +528,8 @@ struct AdamTensors {
         // the new values: every list may be the one it comes from
         const auto both = [&](PyObject *in, const char *in_name, PyObject *out, const char *out_name, const void *fo_adam_tensor::*p,
                               void *fo_adam_tensor::*q) {
-            take(in, in_name, wide, [&](size_t k, void *v) { c[k].*p = c[k].*q = v; });
-            if (out != in) take(out, out_name, wide, [&](size_t k, void *v) { c[k].*q = v; });
+            take(in, in_name, wide, write && out == in, [&](size_t k, void *v) { c[k].*p = c[k].*q = v; });
+            if (out != in) take(out, out_name, wide, write, [&](size_t k, void *v) { c[k].*q = v; });
         };
         both(a[0], "params", a[4], "params out", &fo_adam_tensor::p, &fo_adam_tensor::p_out);
         both(a[2], "m", a[5], "m out", &fo_adam_tensor::m, &fo_adam_tensor::m_out);
@@ -519,35 +540,35 @@ struct AdamTensors {
         weight_type = weights.at(0).scalar_type();
         require(sixteen_bits(weight_type), "weights are bfloat16 or float16");
         require(kind.type != at::kDouble, "no 16-bit weights beside gradients of float64");
-        take(a[7], "weights", {weight_type, kind.gpu}, [&](size_t k, void *p) { c[k].weights = p; });
+        take(a[7], "weights", {weight_type, kind.gpu}, write, [&](size_t k, void *p) { c[k].weights = p; });
     }
 
 private:
     template <class Put>
-    void take(PyObject *list, const char *name, const Kind &of, Put put)
+    void take(PyObject *list, const char *name, const Kind &of, bool write, Put put)
     {
         const Tensors ts(list, name);
         ts.same_count(c.size());
-        ts.read(of, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, put);
+        ts.read(of, write, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, put);
     }
 };
 
 // check_grads(grads, outs), check_adam(the nine of AdamTensors): refuse what a call would refuse
 PyObject *check_grads_impl(PyObject *const *a)
 {
-    GradTensors(a[0], a[1]);
+    GradTensors(a[0], a[1], false);
     Py_RETURN_NONE;
 }
 PyObject *check_adam_impl(PyObject *const *a)
 {
-    AdamTensors t(a);
+    AdamTensors(a, false);
     Py_RETURN_NONE;
 }
 
 // grad_norm(grads, outs or None: no clipping, norm_kind, max_norm, eps, result_type, gpu of an empty list) -> (norm, factor)
 PyObject *grad_norm_impl(PyObject *const *a)
 {
-    const GradTensors t(a[0], a[1]);
+    const GradTensors t(a[0], a[1], true);
     const bool clip = a[1] != Py_None;
     const int kind = (int)whole(a[2]), wide = (int)whole(a[5]), count = (int)t.c.size();
     const double max_norm = number(a[3]), eps = number(a[4]);
@@ -569,7 +590,7 @@ PyObject *grad_norm_impl(PyObject *const *a)
 // adamw(the nine of AdamTensors, lr, beta1, beta2, eps, step, factor)
 PyObject *adamw_impl(PyObject *const *a)
 {
-    const AdamTensors t(a);
+    const AdamTensors t(a, true);
     const at::Tensor *factor = tensor_of(a[14], "factor");
     const c10::DeviceIndex gpu = t.kind.gpu;
     if (factor)

@@ -5,6 +5,10 @@ themselves are in a CPython extension (csrc/training_py.cpp).
 Norms are given as ``(kind, weight, bias, eps)`` with kind "rms" or "layer" and weight / bias a vector
 or None; a gate as ``(access, tensor, activation)`` with access "cell", "row" or "col" as for
 side inputs, and activation "linear", "sigmoid", "silu" or "tanh".
+
+The calls record nothing for autograd: fused_block_norm and its gradient refuse tensors that require a gradient while gradients
+are recorded, and are meant for an autograd.Function or for training code that goes backwards itself.  Clipping and AdamW
+write their tensors as an optimiser does.
 """
 from __future__ import annotations
 
