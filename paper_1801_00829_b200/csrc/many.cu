@@ -276,6 +276,7 @@ clip_kernel(const __grid_constant__ ClipList<N> l, const void *result, int resul
         const bool in_ok = aligned_for<V>(p);
         const long long e = c.single(threadIdx.x, V);
         const A one = e >= 0 ? widen<TI>(begin[e]) : A(0);
+        bool keep = false;                                   // in place, and nothing to clip
         for (int i0 = 0; i0 == 0 || i0 < c.pieces; i0 += kBatch * kCta) {
             Packed<TI, V> g[kBatch];
 #pragma unroll
@@ -289,7 +290,8 @@ clip_kernel(const __grid_constant__ ClipList<N> l, const void *result, int resul
                                                    : (double)static_cast<const float *>(result)[1]);
                 known = true;
             }
-            if ((const void *)begin == (const void *)out && factor == A(1)) break;
+            keep = (const void *)begin == (const void *)out && factor == A(1);
+            if (keep) break;
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const int i = i0 + threadIdx.x + b * kCta;
@@ -300,7 +302,7 @@ clip_kernel(const __grid_constant__ ClipList<N> l, const void *result, int resul
                 store_some<TO, V>(q + i * V, v, true);
             }
         }
-        if (e >= 0) out[e] = narrow<TO>(one * factor);
+        if (e >= 0 && !keep) out[e] = narrow<TO>(one * factor);
     }
 }
 

@@ -120,3 +120,26 @@ def test_refused_lists():
         fo.tensor_list([z(3), 1.0])
     with pytest.raises(ValueError):
         fo.tensor_list([z(3, torch.float64)], [z(3)])
+
+
+@pytest.mark.parametrize("dtype", [torch.float64, F32, BF16, torch.float16])
+@pytest.mark.parametrize("kind", ["l2", "max"])
+@pytest.mark.parametrize("most", [0.75, 1e9])
+def test_clipped_in_place(dtype, kind, most):
+    """In place the values are those of the same call into other tensors, bit for bit, and with a factor of 1 the ones that
+    were there; beside float32 outs, the same rounded once."""
+    torch.manual_seed(7)
+    sizes = (1, 0, 3, 7, 17, 8193, 100003)
+    wide = torch.float64 if dtype == torch.float64 else F32
+    for shift in (0, 1):
+        flat = torch.randn(sum(sizes) + shift, device="cuda").to(dtype)[shift:]
+        for g in (list(torch.split(flat, sizes)), [t.clone() for t in torch.split(flat, sizes)]):
+            was = [t.clone() for t in g]
+            same, more = [torch.zeros_like(t) for t in g], [torch.zeros(t.shape, dtype=wide, device="cuda") for t in g]
+            a = fo.fused_grad_clip(fo.tensor_list(g, same), most, kind=kind, result_type=wide)
+            b = fo.fused_grad_clip(fo.tensor_list(g, more), most, kind=kind, result_type=wide)
+            c = fo.fused_grad_clip(g, most, kind=kind, result_type=wide)
+            assert torch.equal(a, b) and torch.equal(a, c) and (c[1].item() == 1.0) == (most == 1e9)
+            for now, other, wider, before in zip(g, same, more, was):
+                assert torch.equal(now, other) and torch.equal(now, wider.to(dtype)) and torch.equal(wider, before.to(wide) * c[1])
+                assert most < 1.0 or torch.equal(now, before)
