@@ -103,7 +103,9 @@ def _grad_call(grads, clip, kind, max_norm, eps, result_type, device):
     _require(kind in GRAD_NORM_KIND, "norm kind %r" % (kind,))
     index = -1
     if len(grads) == 0:
-        index = torch.cuda.current_device() if device is None else torch.device(device).index
+        device = torch.device("cuda" if device is None else device)
+        _require(device.type == "cuda", "fused operators need CUDA tensors (no CPU path)")
+        index = torch.cuda.current_device() if device.index is None else device.index
     return (_extension or _native()).grad_norm(grads.grads, grads.outs if clip else None, GRAD_NORM_KIND[kind], max_norm, eps,
                                                0 if wide else 1, index)
 

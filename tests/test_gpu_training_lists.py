@@ -143,3 +143,16 @@ def test_clipped_in_place(dtype, kind, most):
             for now, other, wider, before in zip(g, same, more, was):
                 assert torch.equal(now, other) and torch.equal(now, wider.to(dtype)) and torch.equal(wider, before.to(wide) * c[1])
                 assert most < 1.0 or torch.equal(now, before)
+
+
+@pytest.mark.parametrize("device", ["cuda", "cuda:0", 0, torch.device("cuda"), None])
+def test_the_device_of_an_empty_list(device):
+    for call in (fo.fused_grad_norm, fo.fused_grad_clip):
+        result = call([], 1.0, device=device)
+        assert result.device == torch.device("cuda", 0) and result.tolist() == [0.0, 1.0]
+
+
+def test_a_device_without_kernels_is_refused():
+    for call in (fo.fused_grad_norm, fo.fused_grad_clip):
+        with pytest.raises(ValueError, match="CUDA"):
+            call([], 1.0, device="cpu")
