@@ -338,7 +338,8 @@ PyObject *block_norm_grad_impl(PyObject *const *a)
     if (dy) require(pre.given() && h, "dy needs `pre` and h");
     require(f || (!post.given() && !gate.t && !col_scale), "post, gate and col_scale need a block output f");
     const at::ScalarType stream = (dh ? dh : h)->scalar_type();
-    const at::ScalarType block = f ? f->scalar_type() : dy ? dy->scalar_type() : stream;
+    const at::ScalarType block = f ? f->scalar_type() : dy ? dy->scalar_type()      // else as in the forward call
+                                 : stream == at::kFloat ? vector_type(stream, post, pre, col_scale) : stream;
     const at::ScalarType vec = vector_type(block, post, pre, col_scale), sums = sum_type(block);
 
     fo_block_norm_grad n = {};

@@ -209,3 +209,13 @@ def test_stream_types_that_are_refused():
                dict(f=f, out_h=x, stream_type=BF16)):
         with pytest.raises(ValueError):
             fo.fused_block_norm(**kw)
+
+
+@pytest.mark.parametrize("vec", [BF16, F16, F32])
+def test_no_gradient_of_y_for_the_norm_of_a_32_bit_stream(vec):
+    """What the forward call takes the gradient takes too: 16-bit weights of a float32 stream, y not used further."""
+    x = torch.randn(5, 64, device="cuda")
+    pre = ("layer", torch.ones(64, dtype=vec, device="cuda"), torch.ones(64, dtype=vec, device="cuda"), 1e-6)
+    h, y, stats = fo.fused_block_norm(x, pre=pre, stats=True)
+    got = fo.fused_block_norm_grad(torch.ones_like(x), None, h, None, stats, pre=pre)
+    assert y.dtype == vec and bool((got["x"] == 1).all()) and bool((got["pre_w"] == 0).all()) and bool((got["pre_b"] == 0).all())
