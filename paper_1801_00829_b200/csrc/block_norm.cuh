@@ -211,7 +211,8 @@ __device__ __forceinline__ void store_row(void *base, long long row, long long l
 // N elements, whole pieces or half ones, from k0 of a vector over the columns (weight, bias, scale, gate per
 // column).  `wide`: the vector is float although the block has 16 bits.  Outside the row it gives zeros, or, ALIGNED, some
 // value of the vector, so that no zeros have to be put where a load might not take place: it meets a zero there, and
-// what an infinite one or a bias makes of that is not added up.
+// what an infinite one or a bias makes of that is not added up.  Ordinary loads: a kernel that is launched while the one
+// before it ends may be given that one's result as a vector, and the read-only path is for what no kernel writes meanwhile.
 template <bool ALIGNED, class TE, int N, int T, int V>
 __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void *base, bool wide, int k0,
                                             const Columns<T, V> &c)
@@ -221,7 +222,7 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
         auto at = [&](int k) -> A {
             const int j = c.of(k);
             if (j >= c.cols) return A(0);
-            if (sizeof(TE) == 2 && wide) return (A)__ldg(static_cast<const float *>(base) + j);
+            if (sizeof(TE) == 2 && wide) return (A)static_cast<const float *>(base)[j];
             return widen<TE>(static_cast<const TE *>(base)[j]);
         };
 #pragma unroll
@@ -230,14 +231,14 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
 #pragma unroll
         for (int k = 0; k < N; k += 4) {
             const int j = min(c.of((k0 + k) / V * V), c.cols - V) + (k0 + k) % V;
-            const float4 q = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(base) + j));
+            const float4 q = *reinterpret_cast<const float4 *>(static_cast<const float *>(base) + j);
             o[k / 2] = two((A)q.x, (A)q.y), o[k / 2 + 1] = two((A)q.z, (A)q.w);
         }
     } else {
         if constexpr (N < V) {
             static_assert(N * sizeof(TE) == 8, "half a piece");
             const int j = min(c.of(k0 / V * V), c.cols - V) + k0 % V;
-            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(static_cast<const TE *>(base) + j));
+            const uint2 q = *reinterpret_cast<const uint2 *>(static_cast<const TE *>(base) + j);
             Packed<TE, V> r;
             r.w[0] = q.x, r.w[1] = q.y;
             o[0] = r.get2(0), o[1] = r.get2(2);
@@ -245,7 +246,7 @@ __device__ __forceinline__ void load_vector(Two<Acc<TE>> (&o)[N / 2], const void
 #pragma unroll
         for (int k = 0; k + V <= N; k += V) {
             const int j = min(c.of(k0 + k), c.cols - V);
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + j));
+            const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const TE *>(base) + j);
             Packed<TE, V> r;
             r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
 #pragma unroll

@@ -42,3 +42,32 @@ def test_rows_over_clusters_one_call_behind_the_other():
         again = both_ways(c)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("cols", [96, 1000, 1001, 4096, 9000])
+def test_the_result_of_one_call_as_a_vector_of_the_next(cols):
+    """Each call starts while the one before it ends, and takes its result as a gate, a scale and a weight."""
+    torch.manual_seed(3)
+    x, f = torch.randn(64, cols, device="cuda"), torch.randn(64, cols, device="cuda")
+    seeds = torch.rand(12, cols, device="cuda") + 0.5
+    v, w = torch.empty(1, cols, device="cuda"), torch.empty(1, cols, device="cuda")
+
+    def chain(between):
+        out = []
+        for k in range(12):
+            fo.fused_block_norm(seeds[k:k + 1], pre=("rms", None, None, 1e-6), out_y=v)
+            between()
+            fo.fused_block_norm(seeds[k:k + 1], pre=("layer", v[0], None, 1e-6), out_y=w)
+            between()
+            h, y, stats = fo.fused_block_norm(x, f, post=("rms", v[0], None, 1e-6), gate=("col", w[0], "sigmoid"), col_scale=v[0],
+                                              pre=("rms", w[0], None, 1e-6), stats=True)
+            between()
+            got = fo.fused_block_norm_grad(h, y, h, f, stats, post=("rms", v[0], None, 1e-6), gate=("col", w[0], "sigmoid"),
+                                           col_scale=v[0], pre=("rms", w[0], None, 1e-6))
+            between()
+            out += [h, y] + list(got.values())
+        return out
+
+    want = chain(torch.cuda.synchronize)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(want, chain(lambda: None)))
