@@ -516,12 +516,28 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
     }
     if ((!kAny && BLK) || p.h) store_row<ALIGNED, TS, E, true>(p.h, row, p.ld_h, pack_row<TS, E>(h), c, ok, stage);
     if (pre_kind != FO_NORM_NONE) {
+        // the short form has the weights on their way while the row is added up
+        Packed<TB, E> early;
+        const bool ready = LEAN && !wide;
+        if (ready) {
+#pragma unroll
+            for (int k = 0; k < E; k += V) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const TB *>(p.pre.weight) + min(c.of(k), c.cols - V));
+                uint32_t *w = early.w + k * (int)sizeof(TB) / 4;
+                w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+            }
+        }
         pre = row_norm<ALIGNED, BLK, T, C>(h, pre_kind, A(p.pre.eps), inv, c, group, area, buf);
         if (!kAny || p.y) {
             const Two<A> r = both(pre.r);
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) h[i] = h[i] * r;
-            if (!kAny || p.pre.weight) with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
+            if (ready) {
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) h[i] = h[i] * early.get2(2 * i);
+            } else if (!kAny || p.pre.weight) {
+                with_vector<ALIGNED, TB, E>(h, p.pre.weight, wide, c, times);
+            }
             if (kAny && p.pre.bias) with_vector<ALIGNED, TB, E>(h, p.pre.bias, wide, c, plus);
             store_row<ALIGNED, TB, E, true>(p.y, row, p.ld_y, pack_row<TB, E>(h), c, ok, stage);
         }
