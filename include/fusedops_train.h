@@ -47,8 +47,9 @@ enum { FO_F64 = 0, FO_F32 = 1, FO_BF16 = 2, FO_F16 = 3 };
  * stats: NULL or 4 x rows values (float, or double where block_type is FO_F64), contiguous: mu and r
  * of the post norm, mu and r of the pre norm, zeros for a norm that is not there and for rows without columns.
  * The gradient needs them.
- * Any alignment and any ld works; rows whose every pointer is 16-byte aligned move in 16-byte
- * pieces.  cols <= FO_BLOCK_NORM_MAX_COLS, else FO_ERR_UNSUPPORTED.  A single token is the call with rows = 1.
+ * Any alignment and any ld works.  Fast is a call of which every row begins and ends on a piece: 16 bytes of the block's
+ * type, as many elements of the stream's (32 bytes of FO_F32 beside a 16-bit block), with vectors at 16-byte
+ * boundaries; one matrix or vector that does not takes the whole call the slower way.  cols <= FO_BLOCK_NORM_MAX_COLS, else FO_ERR_UNSUPPORTED.  A single token is the call with rows = 1.
  * A row that holds a NaN or an infinity affects that row alone.
  */
 #define FO_BLOCK_NORM_MAX_COLS 32768
@@ -120,7 +121,7 @@ size_t fused_block_norm_grad_workspace_bytes(int64_t rows, int64_t cols, int blo
  * added in 32 bits for a few neighbouring values (at most 32) and in 64 bits over these; values whose
  * 32-bit sum would leave the normal range are added in 64 bits from the start, so gradients near either end
  * of the range have their norm too.  A NaN anywhere makes norm and factor NaN; an infinity makes the norm infinite
- * and the factor zero (out: zero, NaN where the infinity was).
+ * and, with a finite max_norm, the factor zero (out: zero, NaN where the infinity was).
  */
 enum { FO_NORM_L2 = 0, FO_NORM_MAX = 1 };
 

@@ -136,7 +136,7 @@ __device__ __forceinline__ Packed<TE, E> pack_row(const Two<Acc<TE>> (&v)[E / 2]
 // Stores the thread's elements into its row (`ok`: there is one).
 // Unaligned: the pieces of the row's threads in a warp are neighbours; they are exchanged through the warp's
 // `stage` so that full aligned 16 bytes can be written, and the ends singly.  All threads of the warp call it.
-// DIRECT: without that where a row begins aligned (the gradient, short of registers, is slower with it: 24 us, so 22).
+// DIRECT: without that where a row begins aligned (the gradient, short of registers, was slower with it: 24 us against 22).
 template <bool ALIGNED, class TE, int E, bool DIRECT = false, int T, int V>
 __device__ __forceinline__ void store_row(void *base, long long row, long long ld, const Packed<TE, E> &v,
                                           const Columns<T, V> &c, bool ok, unsigned char *stage)
@@ -429,16 +429,15 @@ __device__ __forceinline__ RowNorm<A> row_norm(Two<A> (&t)[E], int kind, A eps, 
 // What a kernel is compiled for besides types and shape; the rest it looks at at run time.
 // GATE: none, one per element, or one per row or column.  LEAN: every matrix read and written, root-mean-square norms
 // with weights and without biases, what transformer blocks mostly have.  Every test and every value that a form
-// does not need is one less where issuing instructions takes longer than waiting for memory (8192 x 4096
-// bf16, gate per element: gradient 126 us, with everything at run time 172; 8192 x 8192 with a stream of 32 bits:
-// forward 133 us against 146).
+// does not need is one less between a row's loads and its stores (8192 x 4096 bf16, gate per element: the gradient went
+// from 172 us with everything at run time to 131; 8192 x 8192 with a stream of 32 bits forward from 146 to 133).
 enum GateForm { kNoGate = 0, kCellGate = 1, kSharedGate = 2 };
 
 // ------------------------------------------------------------------ forward
 // BLK: there is a block output f (else the norm of the stream alone).  1024 threads share an SM with 64 registers, 1536
-// with the 40 that the stream alone needs (8192 x 4096 bf16: 25 us, with 1024 threads 31).  A row's CTA does not stay for
-// another row: a new one starts its loads while the others reduce.  8192 x 4096 bf16, gate per element: 61 us, 5.5
-// TB/s; 8192 x 8192, stream of 32 bits: 129 us, 6.2 TB/s (peak of a copy: 6.5).
+// with the 40 that the stream alone needs (8192 x 4096 bf16: 24 us, with 1024 threads 31).  A row's CTA does not stay for
+// another row: a new one starts its loads while the others reduce.  8192 x 4096 bf16, gate per element: 61 to 65 us, 5.2
+// to 5.5 TB/s; 8192 x 8192, stream of 32 bits, gate per row: 132 to 139 us, 5.8 to 6.1 TB/s (peak of a copy: 6.5).
 template <class TS, class TB, int T, int C, int E, bool ALIGNED, bool BLK, int GATE, bool LEAN>
 __global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta,
                                   sizeof(Acc<TB>) == 8 ? 1 : T > 0 ? (BLK ? 4 : 6) : (BLK ? 2 : 3))
@@ -554,8 +553,10 @@ block_norm_kernel(const __grid_constant__ BlockNormParams p)
 // that neighbouring threads' pieces follow (no bank is hit twice): in registers, the two to six sums
 // would leave room for so few threads that loads no longer cover their latency.
 // At the end every CTA writes its line of partial sums, and column_sum_kernel adds the lines in order.
-// What bounds it is the issue of instructions: 8192 x 4096 bf16 with a gate per element, 126 us, 4.3 TB/s (about 73
-// instructions per element, 55 % of the issue slots); without a gate and with a stream of 32 bits 113 us, 5.3 TB/s.
+// 8192 x 4096 bf16 with a gate per element: 129 to 133 us, 4.0 to 4.2 TB/s; without a gate and with a stream of 32 bits 112
+// us, 5.4 TB/s.  What bounds it is latency: warps wait for loads first (3.5 of the 12.9 cycles between a warp's instructions),
+// then for shared memory, issue slots and barriers; 55 % of the issue slots are taken (75 instructions per
+// element), DRAM is at 0.62 of a copy, and with two rows of 512 threads on an SM nothing is loaded during a row's sums.
 
 constexpr int kGradE = 8;                    // elements of a row in a thread
 
@@ -592,8 +593,8 @@ struct SumPieces {
     }
 };
 
-// 64 registers a thread, so that 1024 threads share an SM; for unaligned rows, too, although they spill (8192 x 4097: 405 us,
-// with 128 registers and half the threads 881).
+// 64 registers a thread, so that 1024 threads share an SM; for unaligned rows, too, although they spill (8192 x 4097: 392 us;
+// with 128 registers and half the threads it took 881 when it took 405 with 64).
 template <class TS, class TB, int T, int C, bool ALIGNED, bool BLK, int GATE, bool LEAN>
 __global__ void __launch_bounds__(T > 0 ? kGroupCta : kMostCta,
                                   sizeof(Acc<TB>) == 8 ? 1 : T > 0 ? 4 : 2)

@@ -13,7 +13,7 @@ cudaError_t launch_block_norm_grad(BlockNormGradParams p, int max_lines, int *li
 
 // Calls go(T, C, E, threads) with the shape for `cols` columns in pieces of V: T threads of a warp and CTAs of
 // kGroupCta, or (T = 0) C CTAs of `threads` a row; 16 elements a thread where a row has them.  A sum over the
-// group costs every thread about 25 instructions, which 16 elements share; 16 is also what 64 (the gradient: 128)
+// group costs every thread about 25 instructions, which 16 elements share; 16 is also what 64
 // registers hold of a row's matrices.  Beyond 512 threads a row takes a cluster: CTAs of 1024 threads would
 // have 64 registers a thread, and spill.
 template <int V, class Go>

@@ -112,7 +112,7 @@ __device__ __forceinline__ double larger(double a, double b)     // of two magni
     return magnitude(a) > magnitude(b) ? a : b;
 }
 
-// The norm reads 520 MB of bf16 in 90 us, 5.8 TB/s: DRAM.
+// The norm reads 520 MB of bf16 in 86 us, 6.0 TB/s: DRAM.
 // Sum of squares of N values.  In 32 bits, and again in 64 where the 32-bit sum is so small or so
 // large that squares may have left the normal range: below 2^-60 what underflowed (each square under
 // 2^-126) could show, above 2^100 an overflow is near.
