@@ -1,5 +1,7 @@
 // Block norm and its gradient: argument checks, alignment, dispatch over element types, and the sum
 // of the gradient's column partials.
+#include <initializer_list>
+
 #include "block_norm_launch.cuh"
 
 namespace fo {
@@ -20,8 +22,6 @@ FO_PAIRS(FO_EXTERN)
 
 namespace {
 
-int elem_bytes(int type) { return type == FO_F64 ? 8 : type == FO_F32 ? 4 : 2; }
-
 bool types_ok(int stream, int block, int vec)
 {
     bool ok = false;
@@ -35,6 +35,15 @@ bool spec_ok(const fo_norm &n)
 {
     return n.kind >= FO_NORM_NONE && n.kind <= FO_NORM_LAYER && (n.kind == FO_NORM_NONE || n.eps >= 0.0);
 }
+
+// Every pointer of `ps` is one to elements of a type.
+bool all_on(int type, std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (!on_elements(p, type)) return false;
+    return true;
+}
+int sum_code(int block_type) { return block_type == FO_F64 ? FO_F64 : FO_F32; }
 
 NormSpec spec_of(const fo_norm &n)
 {
@@ -124,6 +133,10 @@ int fused_block_norm(const fo_block_norm *a, void *stream)
         return FO_ERR_SHAPE;
     rc = check_gate(a->gate, a->gate_access, a->gate_act, a->ld_gate, a->rows, a->cols);
     if (rc != FO_OK) return rc;
+    if (!all_on(a->stream_type, {a->x, a->h}) || !all_on(a->block_type, {a->f, a->gate, a->y})
+        || !all_on(a->vec_type, {a->col_scale, a->post.weight, a->post.bias, a->pre.weight, a->pre.bias})
+        || !all_on(sum_code(a->block_type), {a->stats}))
+        return FO_ERR_UNSUPPORTED;
 
     BlockNormParams p = {};
     p.rows = a->rows, p.cols = (int)a->cols, p.inv_cols = 1.0 / (double)a->cols;
@@ -190,6 +203,12 @@ int fused_block_norm_grad(const fo_block_norm_grad *a, void *ws, size_t ws_bytes
         return FO_ERR_SHAPE;
     rc = check_gate(a->gate, a->gate_access, a->gate_act, a->ld_gate, a->rows, a->cols);
     if (rc != FO_OK) return rc;
+    const int dgate_type = a->gate_access == FO_AT_CELL ? a->block_type : sum_code(a->block_type);
+    if (!all_on(a->stream_type, {a->dh, a->h, a->dx}) || !all_on(a->block_type, {a->dy, a->f, a->gate, a->df})
+        || !all_on(a->vec_type, {a->col_scale, a->post.weight, a->post.bias, a->pre.weight, a->pre.bias})
+        || !all_on(sum_code(a->block_type), {a->stats, a->dcol_scale, a->dpost_weight, a->dpost_bias, a->dpre_weight, a->dpre_bias})
+        || !all_on(dgate_type, {a->dgate}))
+        return FO_ERR_UNSUPPORTED;
     rc = check_workspace(ws, ws_bytes, fused_block_norm_grad_workspace_bytes(a->rows, a->cols, a->block_type));
     if (rc != FO_OK) return rc;
     BlockNormGradParams p = {};

@@ -13,6 +13,10 @@
 
 namespace fo {
 
+// Host: bytes of an element type, and whether a pointer may point to such elements.
+inline int elem_bytes(int type) { return type == FO_F64 ? 8 : type == FO_F32 ? 4 : 2; }
+inline bool on_elements(const void *p, int type) { return ((uintptr_t)p & (uintptr_t)(elem_bytes(type) - 1)) == 0; }
+
 // Acc: what arithmetic, statistics and sums are held in.
 template <class T> struct Elem { using Acc = float; };
 template <> struct Elem<double> { using Acc = double; };

@@ -422,6 +422,15 @@ int check_list(const Tensor *t, int count, Bad bad)
     return tiles < (1ULL << 31) ? FO_OK : FO_ERR_UNSUPPORTED;
 }
 
+// The pointers of a list are to elements of their types.
+template <class Tensor, class Good>
+int check_elements(const Tensor *t, int count, Good good)
+{
+    for (int k = 0; k < count; ++k)
+        if (t[k].n > 0 && !good(t[k])) return FO_ERR_UNSUPPORTED;
+    return FO_OK;
+}
+
 template <class T, int N>
 cudaError_t launch_norm_part(const fo_tensor *t, int count, int kind, const NormOut &o, cudaStream_t st)
 {
@@ -530,7 +539,9 @@ int run_norm(const fo_tensor *t, int count, int in_type, int kind, double max_no
         return FO_ERR_UNSUPPORTED;
     if (!(max_norm >= 0.0) || !(eps >= 0.0)) return FO_ERR_SHAPE;
     if (!result) return FO_ERR_NULL;
-    const int rc = check_workspace(ws, ws_bytes, fused_grad_workspace_bytes());
+    if (!on_elements(result, result_type)) return FO_ERR_UNSUPPORTED;
+    int rc = check_elements(t, count, [=](const fo_tensor &x) { return on_elements(x.in, in_type); });
+    if (rc == FO_OK) rc = check_workspace(ws, ws_bytes, fused_grad_workspace_bytes());
     if (rc != FO_OK) return rc;
     NormOut o = {};
     o.head = static_cast<WsHead *>(ws);
@@ -570,6 +581,8 @@ int fused_grad_clip(const fo_tensor *t, int count, int in_type, int out_type, in
     if (rc != FO_OK) return rc;
     if (!float_type(out_type) || (out_type != in_type && !(out_type == FO_F32 && (in_type == FO_BF16 || in_type == FO_F16))))
         return FO_ERR_UNSUPPORTED;
+    rc = check_elements(t, count, [=](const fo_tensor &x) { return on_elements(x.out, out_type); });
+    if (rc != FO_OK) return rc;
     const cudaStream_t st = (cudaStream_t)stream;
     rc = run_norm(t, count, in_type, norm_kind, max_norm, eps, result, result_type, ws, ws_bytes, st);
     if (rc != FO_OK) return rc;
@@ -587,7 +600,7 @@ int fused_adamw(const fo_adam_tensor *t, int count, int grad_type, int weight_ty
                 double beta2, double eps, int64_t step, const void *factor, int factor_type, void *stream)
 {
     bool any_weights = false;
-    const int rc = check_list(t, count, [&](const fo_adam_tensor &x) {
+    int rc = check_list(t, count, [&](const fo_adam_tensor &x) {
         any_weights = any_weights || x.weights;
         return !x.p || !x.g || !x.m || !x.v || !x.p_out || !x.m_out || !x.v_out;
     });
@@ -596,6 +609,13 @@ int fused_adamw(const fo_adam_tensor *t, int count, int grad_type, int weight_ty
     if (any_weights && weight_type != FO_BF16 && weight_type != FO_F16) return FO_ERR_UNSUPPORTED;
     if (any_weights && grad_type == FO_F64) return FO_ERR_UNSUPPORTED;
     if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0)) return FO_ERR_SHAPE;
+    const int wide = grad_type == FO_F64 ? FO_F64 : FO_F32;
+    rc = check_elements(t, count, [=](const fo_adam_tensor &x) {
+        for (const void *p : {x.p, x.m, x.v, (const void *)x.p_out, (const void *)x.m_out, (const void *)x.v_out})
+            if (!on_elements(p, wide)) return false;
+        return on_elements(x.g, grad_type) && on_elements(x.weights, weight_type);
+    });
+    if (rc != FO_OK || (factor && !on_elements(factor, factor_type))) return FO_ERR_UNSUPPORTED;
     AdamHyper h = {lr, beta1, beta2, eps, 1.0 / (1.0 - pow(beta1, (double)step)), 1.0 / (1.0 - pow(beta2, (double)step)),
                    factor, factor_type};
     const cudaStream_t st = (cudaStream_t)stream;
