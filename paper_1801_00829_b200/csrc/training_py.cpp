@@ -59,6 +59,18 @@ at::ScalarType dtype_of(PyObject *o, const char *name)
     return reinterpret_cast<THPDtype *>(o)->scalar_type;
 }
 
+// The address of a tensor of which `reach` elements from its first one on are used; its storage may have been resized.
+void *data_of(const at::Tensor &t, int64_t reach, const char *name)
+{
+    if (reach <= 0) return nullptr;
+    const c10::TensorImpl &impl = *t.unsafeGetTensorImpl();
+    c10::StorageImpl &held = *impl.storage().unsafeGetStorageImpl();
+    const size_t bytes = impl.dtype().itemsize(), at_byte = (size_t)impl.storage_offset() * bytes;
+    if (held.nbytes() < at_byte + (size_t)reach * bytes)
+        throw Refused(std::string(name) + ": the tensor's storage is smaller than the tensor");
+    return static_cast<char *>(held.mutable_data()) + at_byte;
+}
+
 // The operators record no graph: a tensor that autograd follows would lose its gradient without a word.
 void outside_graph(const at::Tensor &t, const char *name)
 {
@@ -104,7 +116,7 @@ struct Call {
             if (rows > 1) throw Refused(std::string("rows of ") + name + " overlap");
             *ld = cols;
         }
-        return t->data_ptr();
+        return data_of(*t, cols > 0 ? (rows - 1) * *ld + cols : 0, name);
     }
     void *vector(const at::Tensor *t, at::ScalarType type, const char *name) const
     {
@@ -113,7 +125,7 @@ struct Call {
             || !t->is_contiguous())
             refuse(*t, name, "a contiguous vector over the columns", type);
         outside_graph(*t, name);
-        return t->data_ptr();
+        return data_of(*t, cols, name);
     }
     at::Tensor make(at::IntArrayRef sizes, at::ScalarType type) const
     {
@@ -182,7 +194,7 @@ struct Gate {
         outside_graph(*t, "gate");
         ld = n > 1 ? t->stride(along) : 1;
         require(access == FO_AT_ROW ? ld >= 1 : ld == 1, "stride of the gate");
-        p = t->data_ptr();
+        p = data_of(*t, (n - 1) * ld + 1, "gate");
     }
 };
 
@@ -364,7 +376,7 @@ PyObject *block_norm_grad_impl(PyObject *const *a)
             || !stats->is_contiguous() || !stats->is_cuda() || stats->get_device() != call.gpu)
             call.refuse(*stats, "stats", "4 x rows", sums);
         outside_graph(*stats, "stats");
-        n.stats = stats->data_ptr();
+        n.stats = data_of(*stats, 4 * call.rows, "stats");
     }
 
     PyObject *got = PyDict_New();
@@ -601,7 +613,7 @@ PyObject *adamw_impl(PyObject *const *a)
                 "factor is not one float on the gradients' device");
     const OnGpu on(gpu);
     check_status(fused_adamw(t.c.data(), (int)t.c.size(), type_code(t.kind.type), type_code(t.weight_type), number(a[9]), number(a[10]),
-                             number(a[11]), number(a[12]), whole(a[13]), factor ? factor->data_ptr() : nullptr,
+                             number(a[11]), number(a[12]), whole(a[13]), factor ? data_of(*factor, 1, "factor") : nullptr,
                              factor ? type_code(factor->scalar_type()) : FO_F32,
                              c10::cuda::getCurrentCUDAStream(gpu).stream()), "fused_adamw");
     Py_RETURN_NONE;

@@ -156,3 +156,28 @@ def test_a_device_without_kernels_is_refused():
     for call in (fo.fused_grad_norm, fo.fused_grad_clip):
         with pytest.raises(ValueError, match="CUDA"):
             call([], 1.0, device="cpu")
+
+
+@pytest.mark.parametrize("name", ["x", "f", "post", "gate", "row gate", "col_scale", "pre", "out_h", "out_y", "dh", "dy", "h", "stats", "factor"])
+def test_a_tensor_without_its_storage_is_refused(name):
+    """What sharded trainers leave of a parameter between two uses: a tensor whose storage was resized to nothing."""
+    z = lambda *s: torch.rand(*s, device="cuda") + 0.1  # noqa: E731
+    t = {k: z(4, 8) for k in ("x", "f", "gate", "out_h", "out_y", "dh", "dy", "h")}
+    t.update({k: z(8) for k in ("post", "col_scale", "pre")}, stats=z(4, 4), factor=z(1), **{"row gate": z(4)})
+    gate = ("row", t["row gate"], "silu") if name == "row gate" else ("cell", t["gate"], "silu")
+    how = dict(post=("rms", t["post"], None, 1e-6), gate=gate, col_scale=t["col_scale"], pre=("rms", t["pre"], None, 1e-6))
+    adam = fo.adam_list(*[[z(5)] for _ in range(4)])
+    calls = [lambda: fo.fused_block_norm(t["x"], t["f"], out_h=t["out_h"], out_y=t["out_y"], **how),
+             lambda: fo.fused_block_norm_grad(t["dh"], t["dy"], t["h"], t["f"], t["stats"], **how),
+             lambda: fo.fused_adamw(adam, lr=0.1, factor=t["factor"])]
+    for call in calls:
+        call()
+    t[name].untyped_storage().resize_(0)
+    refused = 0
+    for call in calls:
+        try:
+            call()
+        except ValueError as e:
+            assert "storage" in str(e)
+            refused += 1
+    assert refused == (2 if name in ("f", "post", "gate", "row gate", "col_scale", "pre") else 1)
