@@ -126,7 +126,7 @@ def build_extension(force: bool = False) -> str:
     includes = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
                 os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     tmp = EXTENSION_PATH + ".tmp%d" % os.getpid()
-    cmd = (["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd = (["g++", "-O3", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
            + ["-I" + d for d in includes] + [EXTENSION_SOURCE, "-o", tmp, "-L" + HERE, "-l:libfusedops.so", "-Wl,-rpath,$ORIGIN",
                                              "-L" + os.path.join(root, "lib"), "-L" + os.path.join(cuda, "lib64"), "-lcudart", "-lc10", "-lc10_cuda",
                                              "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"])
