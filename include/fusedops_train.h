@@ -47,9 +47,11 @@ enum { FO_F64 = 0, FO_F32 = 1, FO_BF16 = 2, FO_F16 = 3 };
  * stats: NULL or 4 x rows values (float, or double where block_type is FO_F64), contiguous: mu and r
  * of the post norm, mu and r of the pre norm, zeros for a norm that is not there and for rows without columns.
  * The gradient needs them.
- * Any address of an element and any ld works (another address: FO_ERR_UNSUPPORTED).  Fast is a call of which every row begins and ends on a piece: 16 bytes of the block's
- * type, as many elements of the stream's (32 bytes of FO_F32 beside a 16-bit block), with vectors at 16-byte
- * boundaries; one matrix or vector that does not takes the whole call the slower way.  cols <= FO_BLOCK_NORM_MAX_COLS, else FO_ERR_UNSUPPORTED.  A single token is the call with rows = 1.
+ * Any address of an element and any ld works (another address: FO_ERR_UNSUPPORTED).  Fast is a call of which
+ * every row begins and ends on a piece: 16 bytes of the block's type, as many elements of the stream's (32 bytes
+ * of FO_F32 beside a 16-bit block), with vectors at 16-byte boundaries; one matrix or vector that does not takes
+ * the whole call the slower way.
+ * cols <= FO_BLOCK_NORM_MAX_COLS, else FO_ERR_UNSUPPORTED.  A single token is the call with rows = 1.
  * A row that holds a NaN or an infinity affects that row alone.
  */
 #define FO_BLOCK_NORM_MAX_COLS 32768

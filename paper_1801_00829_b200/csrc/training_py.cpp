@@ -511,15 +511,18 @@ struct GradTensors {
         const Tensors in(grads, "grads");
         kind = kind_of(in), out_type = kind.type;
         c.resize(in.count());
-        in.read(kind, write && in.is(outs), [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) { c[k].in = c[k].out = p; });
+        in.read(kind, write && in.is(outs), [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); },
+                [&](size_t k, void *p) { c[k].in = c[k].out = p; });
         if (outs == Py_None || in.is(outs)) return;
         const Tensors out(outs, "outs");
         out.same_count(c.size());
         if (c.empty()) return;
         out_type = out.at(0).scalar_type();
         if (out_type != kind.type && !(sixteen_bits(kind.type) && out_type == at::kFloat))
-            throw Refused(std::string("clipped values of ") + c10::toString(out_type) + " from gradients of " + c10::toString(kind.type));
-        out.read({out_type, kind.gpu}, write, [&](size_t k, const c10::TensorImpl &) { return c[k].n; }, [&](size_t k, void *p) { c[k].out = p; });
+            throw Refused(std::string("clipped values of ") + c10::toString(out_type) + " from gradients of "
+                          + c10::toString(kind.type));
+        out.read({out_type, kind.gpu}, write, [&](size_t k, const c10::TensorImpl &) { return c[k].n; },
+                 [&](size_t k, void *p) { c[k].out = p; });
     }
 };
 
@@ -534,7 +537,8 @@ struct AdamTensors {
         const Tensors grads(a[1], "grads");
         kind = kind_of(grads);
         c.resize(grads.count());
-        require(PyBytes_Check(a[8]) && (size_t)PyBytes_GET_SIZE(a[8]) == c.size() * sizeof(double), "decay: one value per tensor is needed");
+        require(PyBytes_Check(a[8]) && (size_t)PyBytes_GET_SIZE(a[8]) == c.size() * sizeof(double),
+                "decay: one value per tensor is needed");
         grads.read(kind, false, [&](size_t k, const c10::TensorImpl &t) { return c[k].n = t.numel(); }, [&](size_t k, void *p) {
             c[k].g = p;
             memcpy(&c[k].decay, PyBytes_AS_STRING(a[8]) + k * sizeof(double), sizeof(double));

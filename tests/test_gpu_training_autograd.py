@@ -19,8 +19,9 @@ def test_a_tensor_that_requires_a_gradient_is_refused(name):
     t = {k: z(4, 8) for k in ("x", "f", "gate", "out_h", "out_y")}
     t.update({k: z(8) for k in ("post", "post bias", "col gate", "col_scale", "pre")}, **{"row gate": z(4)})
     t[name].requires_grad_()
-    access, gate = ("row", t["row gate"]) if name == "row gate" else ("col", t["col gate"]) if name == "col gate" else ("cell", t["gate"])
-    how = dict(post=("layer", t["post"], t["post bias"], EPS), gate=(access, gate, "silu"), col_scale=t["col_scale"], pre=("rms", t["pre"], None, EPS))
+    access = name.split()[0] if name in ("row gate", "col gate") else "cell"
+    gate = (access, t["gate" if access == "cell" else name], "silu")
+    how = dict(post=("layer", t["post"], t["post bias"], EPS), gate=gate, col_scale=t["col_scale"], pre=("rms", t["pre"], None, EPS))
     with pytest.raises(ValueError, match="requires a gradient"):
         fo.fused_block_norm(t["x"], t["f"], out_h=t["out_h"], out_y=t["out_y"], **how)
     with torch.no_grad():

@@ -30,7 +30,8 @@ def test_gradient_of_a_column_scale_that_is_not_there(stream, block, gate, rows,
     access = {None: 0, "cell": 0, "row": 1, "col": 2}[gate]
     g = c.gate[1] if gate else None
     post = (1, 0, c.post[3], c.post[1].data_ptr(), 0)
-    packed = BLOCK_NORM_GRAD.pack(rows, cols, CODE[stream], CODE[block], CODE[block], access, 2 if gate else 0, 0, c.dh.data_ptr(), 0, 0,
+    types = CODE[stream], CODE[block], CODE[block]
+    packed = BLOCK_NORM_GRAD.pack(rows, cols, *types, access, 2 if gate else 0, 0, c.dh.data_ptr(), 0, 0,
                                   c.f.data_ptr(), g.data_ptr() if gate else 0, 0, stats.data_ptr(), c.dh.stride(0), 0, 0,
                                   c.f.stride(0), g.stride(0) if gate else 0, c.scale, *post, *NONE, 0, 0, 0, 0, 0, 0,
                                   got.data_ptr(), 0, 0, 0, 0)

@@ -158,7 +158,8 @@ def test_a_device_without_kernels_is_refused():
             call([], 1.0, device="cpu")
 
 
-@pytest.mark.parametrize("name", ["x", "f", "post", "gate", "row gate", "col_scale", "pre", "out_h", "out_y", "dh", "dy", "h", "stats", "factor"])
+@pytest.mark.parametrize("name", ["x", "f", "post", "gate", "row gate", "col_scale", "pre", "out_h", "out_y", "dh", "dy", "h", "stats",
+                                  "factor"])
 def test_a_tensor_without_its_storage_is_refused(name):
     """What sharded trainers leave of a parameter between two uses: a tensor whose storage was resized to nothing."""
     z = lambda *s: torch.rand(*s, device="cuda") + 0.1  # noqa: E731
