@@ -1,5 +1,5 @@
-"""Builds csrc/*.cu into libfusedops.so (sm_100a) next to this file, and csrc/training_py.cpp, the CPython
-extension that training.py calls it through, into _training.so.
+"""Builds csrc/*.cu into libfusedops.so (sm_100a) next to this file, and csrc/training_py.cpp and lm_py.cpp, the CPython
+extension that training.py and lm.py call it through, into _training.so.
 
     python -m paper_1801_00829_b200.build [--force] [--verbose]
 
@@ -19,7 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libfusedops.so")
-EXTENSION_SOURCE = os.path.join(CSRC, "training_py.cpp")
+EXTENSION_SOURCES = [os.path.join(CSRC, "training_py.cpp"), os.path.join(CSRC, "lm_py.cpp")]
 EXTENSION_PATH = os.path.join(HERE, "_training.so")
 
 NVCC_FLAGS = [
@@ -116,7 +116,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
 def build_extension(force: bool = False) -> str:
     """Compile (if needed) the CPython extension against the installed torch; returns its path.  The library it
     calls is looked for next to it."""
-    deps = [EXTENSION_SOURCE] + glob.glob(os.path.join(INCLUDE, "*.h"))
+    deps = EXTENSION_SOURCES + glob.glob(os.path.join(CSRC, "*_py.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
     if not force and os.path.exists(EXTENSION_PATH) and all(os.path.getmtime(d) <= os.path.getmtime(EXTENSION_PATH) for d in deps):
         return EXTENSION_PATH
     import sysconfig
@@ -127,7 +127,7 @@ def build_extension(force: bool = False) -> str:
                 os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
     tmp = EXTENSION_PATH + ".tmp%d" % os.getpid()
     cmd = (["g++", "-O3", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
-           + ["-I" + d for d in includes] + [EXTENSION_SOURCE, "-o", tmp, "-L" + HERE, "-l:libfusedops.so", "-Wl,-rpath,$ORIGIN",
+           + ["-I" + d for d in includes] + EXTENSION_SOURCES + ["-o", tmp, "-L" + HERE, "-l:libfusedops.so", "-Wl,-rpath,$ORIGIN",
                                              "-L" + os.path.join(root, "lib"), "-L" + os.path.join(cuda, "lib64"), "-lcudart", "-lc10", "-lc10_cuda",
                                              "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"])
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

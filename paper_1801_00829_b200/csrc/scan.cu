@@ -1,0 +1,120 @@
+// Gated linear recurrence: argument checks, alignment, dispatch over element types.
+#include <initializer_list>
+
+#include "scan.cuh"
+
+namespace fo {
+
+#define FO_SCAN_PAIRS(X)                           \
+    X(FO_F64, FO_F64, double, double)              \
+    X(FO_F32, FO_F32, float, float)                \
+    X(FO_BF16, FO_BF16, __nv_bfloat16, __nv_bfloat16) \
+    X(FO_BF16, FO_F32, __nv_bfloat16, float)       \
+    X(FO_F16, FO_F16, __half, __half)              \
+    X(FO_F16, FO_F32, __half, float)
+
+#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(const ScanParams &, bool, bool, long long, cudaStream_t);
+FO_SCAN_PAIRS(FO_EXTERN)
+#undef FO_EXTERN
+
+namespace {
+
+int state_code(int type) { return type == FO_F64 ? FO_F64 : FO_F32; }
+
+int check_scan(long long batch, long long tokens, long long channels, int type, int gate_type, int decay, int mix, const void *lengths,
+               int lengths_type, std::initializer_list<fo_rows> strides)
+{
+    if (batch < 0 || tokens < 0 || channels < 0) return FO_ERR_SHAPE;
+    bool ok = false;
+#define FO_CASE(t, g, T, G) ok = ok || (type == t && gate_type == g);
+    FO_SCAN_PAIRS(FO_CASE)
+#undef FO_CASE
+    if (!ok || decay < FO_DECAY_VALUE || decay > FO_DECAY_EXP || mix < FO_MIX_ONE || mix > FO_MIX_ROOT) return FO_ERR_UNSUPPORTED;
+    if (lengths && lengths_type != FO_I32 && lengths_type != FO_I64) return FO_ERR_UNSUPPORTED;
+    if (lengths && ((uintptr_t)lengths & (lengths_type == FO_I64 ? 7u : 3u))) return FO_ERR_UNSUPPORTED;
+    for (const fo_rows &s : strides)
+        if (s.batch < 0 || s.token < 0) return FO_ERR_SHAPE;
+    // CTAs are counted in 31 bits
+    const long long tiles = (channels + 31) / 32;
+    if (tiles && batch > (0x7fffffffLL / kScanMostCluster) / tiles) return FO_ERR_UNSUPPORTED;
+    return FO_OK;
+}
+bool all_on(int type, std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (!on_elements(p, type)) return false;
+    return true;
+}
+// Every piece of two channels of a matrix begins at a multiple of its size.
+bool in_pairs(const void *p, const fo_rows &s, int type)
+{
+    return ((uintptr_t)p & (unsigned)(2 * elem_bytes(type) - 1)) == 0 && s.batch % 2 == 0 && s.token % 2 == 0;
+}
+
+int launch(const ScanParams &p, int type, int gate_type, bool wide, bool grad, long long batch, cudaStream_t st)
+{
+    cudaError_t e = cudaErrorInvalidValue;
+#define FO_CASE(t, g, T, G) \
+    if (type == t && gate_type == g) e = launch_scan<T, G>(p, wide, grad, batch, st);
+    FO_SCAN_PAIRS(FO_CASE)
+#undef FO_CASE
+    return e == cudaSuccess ? FO_OK : cuda_fail(e);
+}
+
+}  // namespace
+}  // namespace fo
+
+using namespace fo;
+
+extern "C" {
+
+int fused_scan(const fo_scan *a, void *stream)
+{
+    if (!a) return FO_ERR_NULL;
+    const int rc = check_scan(a->batch, a->tokens, a->channels, a->type, a->gate_type, a->decay, a->mix, a->lengths, a->lengths_type,
+                              {a->x_at, a->gate_at, a->h_at, a->reset_at});
+    if (rc != FO_OK) return rc;
+    if (a->batch == 0 || a->channels == 0) return FO_OK;
+    if (a->tokens > 0 && (!a->x || !a->gate || !a->h)) return FO_ERR_NULL;
+    if (!all_on(a->type, {a->x, a->h}) || !all_on(a->gate_type, {a->gate}) || !all_on(state_code(a->type), {a->state, a->last}))
+        return FO_ERR_UNSUPPORTED;
+    if (a->tokens == 0 && !a->last) return FO_OK;
+    ScanParams p = {};
+    p.tokens = a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
+    p.reset = static_cast<const unsigned char *>(a->reset);
+    p.h = a->h, p.last = a->last;
+    p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->h_at;
+    const bool wide = a->channels % 2 == 0 && in_pairs(a->x, a->x_at, a->type) && in_pairs(a->gate, a->gate_at, a->gate_type)
+                      && in_pairs(a->h, a->h_at, a->type);
+    return launch(p, a->type, a->gate_type, wide, false, a->batch, (cudaStream_t)stream);
+}
+
+int fused_scan_grad(const fo_scan_grad *a, void *stream)
+{
+    if (!a) return FO_ERR_NULL;
+    const int rc = check_scan(a->batch, a->tokens, a->channels, a->type, a->gate_type, a->decay, a->mix, a->lengths, a->lengths_type,
+                              {a->dh_at, a->x_at, a->gate_at, a->h_at, a->reset_at, a->dx_at, a->dgate_at});
+    if (rc != FO_OK) return rc;
+    if (a->batch == 0 || a->channels == 0) return FO_OK;
+    const bool mixes = a->mix != FO_MIX_ONE;
+    if (a->tokens > 0 && ((mixes && !a->x) || !a->gate || !a->h || !a->dx || !a->dgate)) return FO_ERR_NULL;
+    if (!all_on(a->type, {a->dh, a->h, a->dx}) || (mixes && !all_on(a->type, {a->x})) || !all_on(a->gate_type, {a->gate, a->dgate})
+        || !all_on(state_code(a->type), {a->dlast, a->state, a->dstate}))
+        return FO_ERR_UNSUPPORTED;
+    if (a->tokens == 0 && !a->dstate) return FO_OK;
+    ScanParams p = {};
+    p.tokens = a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
+    p.reset = static_cast<const unsigned char *>(a->reset);
+    p.h = a->dx, p.last = a->dstate, p.dh = a->dh, p.dlast = a->dlast, p.h_in = a->h, p.dgate = a->dgate;
+    p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->dx_at;
+    p.dh_at = a->dh_at, p.h_in_at = a->h_at, p.dgate_at = a->dgate_at;
+    bool wide = a->channels % 2 == 0 && in_pairs(a->gate, a->gate_at, a->gate_type) && in_pairs(a->dgate, a->dgate_at, a->gate_type)
+                && in_pairs(a->h, a->h_at, a->type) && in_pairs(a->dx, a->dx_at, a->type);
+    if (a->dh) wide = wide && in_pairs(a->dh, a->dh_at, a->type);
+    if (mixes) wide = wide && in_pairs(a->x, a->x_at, a->type);
+    return launch(p, a->type, a->gate_type, wide, true, a->batch, (cudaStream_t)stream);
+}
+
+}  // extern "C"

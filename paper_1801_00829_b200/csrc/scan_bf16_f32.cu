@@ -1,0 +1,8 @@
+// Gated linear recurrence: the kernels for x of __nv_bfloat16 with gates of float.
+#include "scan_launch.cuh"
+
+namespace fo {
+
+template cudaError_t launch_scan<__nv_bfloat16, float>(const ScanParams &, bool, bool, long long, cudaStream_t);
+
+}  // namespace fo

@@ -1,0 +1,8 @@
+// Gated linear recurrence: the kernels for x of __half with gates of __half.
+#include "scan_launch.cuh"
+
+namespace fo {
+
+template cudaError_t launch_scan<__half, __half>(const ScanParams &, bool, bool, long long, cudaStream_t);
+
+}  // namespace fo
