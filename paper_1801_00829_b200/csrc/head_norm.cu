@@ -83,6 +83,7 @@ int check_rotation(const fo_rotation &r, int dim, int type)
         if (r.section[k] < 0) return FO_ERR_SHAPE;
         sum += r.section[k];
     }
+    if (r.rows > 0x7fffffffLL) return FO_ERR_UNSUPPORTED;
     if (sum != r.pairs || r.rows < 0 || r.ld_cos < r.pairs || r.ld_sin < r.pairs || r.position_axis < 0 || r.position_batch < 0
         || r.position_token < 0)
         return FO_ERR_SHAPE;

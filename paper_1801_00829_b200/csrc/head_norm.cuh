@@ -1,9 +1,10 @@
 // Head norms with rotation: y = R(position) norm(x) for every head's vector of queries and keys, and the gradient.
 //
-// A vector belongs to L lanes (a power of two up to 32), so that a warp works on 32 / L heads of one token at a time; a lane
-// holds I items of two pieces of V elements each: with halves the two pieces that are turned against each other, else two
+// A vector belongs to L lanes (a power of two up to 32), so that a warp works on 32 / L heads of one token at a time (a turn); a
+// lane holds I items of two pieces of V elements each: with halves the two pieces that are turned against each other, else two
 // neighbouring ones.  Everything of a vector stays in registers between its one load and its one store, and what a token's heads
-// share (cosines, sines, weights) is loaded once per token or once per CTA.
+// share (cosines, sines, weights) is loaded once per token or once per CTA.  A lane's pieces of the next turns are on their way to
+// a ring of its own in shared memory (asynchronous copies that no other thread has to wait for).
 #pragma once
 
 #include "elem.cuh"
@@ -11,6 +12,9 @@
 
 namespace fo {
 
+#ifndef HM
+#define HM 2
+#endif
 constexpr int kHeadCta = 256;
 constexpr int kHeadWarps = kHeadCta / 32;
 
@@ -41,37 +45,35 @@ template <class T, int V>
 struct HeadPiece {
     alignas(V * sizeof(T)) T v[V];
 };
-
 template <class T, int V>
 __device__ __forceinline__ HeadPiece<T, V> head_load(const T *p)
 {
     HeadPiece<T, V> r;
-    if constexpr (V * sizeof(T) == 16) load16(reinterpret_cast<uint32_t *>(&r), p);
+    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(&r) = *reinterpret_cast<const uint4 *>(p);
     else if constexpr (V * sizeof(T) == 8 && V > 1) *reinterpret_cast<uint2 *>(&r) = *reinterpret_cast<const uint2 *>(p);
     else
 #pragma unroll
         for (int j = 0; j < V; ++j) r.v[j] = p[j];
     return r;
 }
-template <class T, int V>
-__device__ __forceinline__ void head_store(T *p, const Acc<T> (&f)[V])
+
+// The unit of arithmetic: two neighbouring values in one register pair, or a single one where elements move alone.
+__device__ __forceinline__ float joined(float v) { return v; }
+__device__ __forceinline__ double joined(double v) { return v; }
+template <class U, class A>
+__device__ __forceinline__ U head_all(A v)
 {
-    HeadPiece<T, V> r;
-#pragma unroll
-    for (int j = 0; j < V; ++j) r.v[j] = narrow<T>(f[j]);
-    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(&r);
-    else if constexpr (V * sizeof(T) == 8 && V > 1) *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(&r);
-    else
-#pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = r.v[j];
+    if constexpr (std::is_same<U, A>::value) return v;
+    else return both(v);
 }
+template <class A> __device__ __forceinline__ Two<A> head_swap(Two<A> u) { return two(second(u), first(u)); }
 
 // What a lane holds of a vector: item i is the pieces at a[i] and b[i] (-1: none), of which ta and tb are turned; its first pair.
 template <int V, int I, int PAIRING>
 struct HeadItems {
-    int a[I], b[I], pair[I];
-    bool ta[I], tb[I];
-    __device__ __forceinline__ HeadItems(int lane, int lanes, int dim, int pairs)
+    int a[I], b[I];
+    int pairs, lane, lanes;
+    __device__ __forceinline__ HeadItems(int lane_, int lanes_, int dim, int pairs_) : pairs(pairs_), lane(lane_), lanes(lanes_)
     {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
@@ -80,348 +82,511 @@ struct HeadItems {
                 if (u * V < pairs) {
                     a[i] = PAIRING == FO_PAIR_HALVES ? u * V : 2 * u;
                     b[i] = PAIRING == FO_PAIR_HALVES ? pairs + u * V : 2 * u + 1;
-                    ta[i] = tb[i] = true;
                 } else {
                     a[i] = 2 * pairs + (u * V - pairs) * 2;
                     b[i] = a[i] + V;
-                    ta[i] = tb[i] = false;
                 }
             } else {
                 a[i] = u * 2 * V, b[i] = a[i] + V;
-                ta[i] = a[i] < 2 * pairs, tb[i] = b[i] < 2 * pairs;
             }
-            pair[i] = u * V;
             if (a[i] >= dim) a[i] = -1;
             if (a[i] < 0 || b[i] >= dim) b[i] = -1;
         }
     }
+    __device__ __forceinline__ int pair(int i) const { return (lane + i * lanes) * V; }
+    __device__ __forceinline__ bool ta(int i) const
+    {
+        return PAIRING == FO_PAIR_HALVES || V == 1 ? pair(i) < pairs : a[i] >= 0 && a[i] < 2 * pairs;
+    }
+    __device__ __forceinline__ bool tb(int i) const { return PAIRING == FO_PAIR_HALVES || V == 1 ? ta(i) : b[i] >= 0 && b[i] < 2 * pairs; }
 };
 
-// Cosines and sines of a lane's pairs for token (b, t).
-template <class A, int V, int I, int PAIRING>
-__device__ __forceinline__ void head_angles(const HeadParams &p, const HeadItems<V, I, PAIRING> &at, long long b, long long t,
-                                            A (&c)[I][V], A (&s)[I][V])
+// The rows of the tables at which a token's positions lie; -1: outside.
+struct HeadRows {
+    int at[FO_MAX_AXES];
+};
+__device__ __forceinline__ HeadRows head_rows(const HeadParams &p, unsigned token)
 {
-    long long row[FO_MAX_AXES];
+    HeadRows r;
+    const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
     const long long place = b * p.position_batch + t * p.position_token;
 #pragma unroll
     for (int k = 0; k < FO_MAX_AXES; ++k) {
-        row[k] = -1;
+        r.at[k] = -1;
         if (k < p.axes) {
-            const long long at_k = place + k * p.position_axis;
-            row[k] = p.long_positions ? static_cast<const long long *>(p.positions)[at_k] : static_cast<const int *>(p.positions)[at_k];
-            if (row[k] >= p.rows) row[k] = -1;
+            const long long at = place + k * p.position_axis;
+            const long long row = p.long_positions ? static_cast<const long long *>(p.positions)[at] : static_cast<const int *>(p.positions)[at];
+            if (row >= 0 && row < p.rows) r.at[k] = (int)row;
         }
     }
-    const A *const ct = static_cast<const A *>(p.cos_table), *const st = static_cast<const A *>(p.sin_table);
-    auto row_of = [&](int pair) {
-        long long r = row[0];
-#pragma unroll
-        for (int k = 1; k < FO_MAX_AXES; ++k)
-            if (k < p.axes && pair >= p.section_end[k - 1]) r = row[k];
-        return r;
-    };
-    constexpr int W = 16 / (int)sizeof(A) < V ? 16 / (int)sizeof(A) : V;         // table values in one load
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-#pragma unroll
-        for (int j0 = 0; j0 < V; j0 += W) {
-            const int pair = at.pair[i] + j0;
-            const bool on = at.a[i] >= 0 && at.ta[i] && pair < p.pairs;
-            const long long r = on ? row_of(pair) : -1;
-#pragma unroll
-            for (int j = 0; j < W; ++j) c[i][j0 + j] = s[i][j0 + j] = A(NAN);    // a position outside the table
-            if (W > 1 && p.table_pieces) {
-                if (r >= 0) {
-                    const HeadPiece<A, W> u = *reinterpret_cast<const HeadPiece<A, W> *>(ct + r * p.ld_cos + pair);
-                    const HeadPiece<A, W> v = *reinterpret_cast<const HeadPiece<A, W> *>(st + r * p.ld_sin + pair);
-#pragma unroll
-                    for (int j = 0; j < W; ++j) c[i][j0 + j] = u.v[j], s[i][j0 + j] = v.v[j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const long long q = on && pair + j < p.pairs ? row_of(pair + j) : -1;
-                    if (q >= 0) c[i][j0 + j] = ct[q * p.ld_cos + pair + j], s[i][j0 + j] = st[q * p.ld_sin + pair + j];
-                }
-            }
-        }
-    }
-}
-
-// Turns an item's pieces; SIGN -1: back.
-template <int V, int PAIRING, int SIGN, class A>
-__device__ __forceinline__ void head_turn(A (&a)[V], A (&b)[V], bool ta, bool tb, const A (&c)[V], const A (&s)[V])
-{
-    if constexpr (PAIRING == FO_PAIR_HALVES || V == 1) {
-        if (!ta) return;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const A sn = SIGN < 0 ? -s[j] : s[j], x = a[j], y = b[j];
-            a[j] = fused_ma(x, c[j], -(y * sn));
-            b[j] = fused_ma(x, sn, y * c[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-            const A sa = SIGN < 0 ? -s[j / 2] : s[j / 2], sb = SIGN < 0 ? -s[(V + j) / 2] : s[(V + j) / 2];
-            A x = a[j], y = a[j + 1];
-            if (ta) a[j] = fused_ma(x, c[j / 2], -(y * sa)), a[j + 1] = fused_ma(x, sa, y * c[j / 2]);
-            x = b[j], y = b[j + 1];
-            if (tb) b[j] = fused_ma(x, c[(V + j) / 2], -(y * sb)), b[j + 1] = fused_ma(x, sb, y * c[(V + j) / 2]);
-        }
-    }
-}
-
-template <class A>
-__device__ __forceinline__ A head_sum(A v, int lanes)
-{
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-// V values of a weight or bias vector.
-template <class T, int V>
-__device__ __forceinline__ void head_vector(const void *p, int wide, int at, Acc<T> (&f)[V])
-{
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        f[j] = wide ? (Acc<T>)static_cast<const float *>(p)[at + j] : widen(static_cast<const T *>(p)[at + j]);
+    return r;
 }
 
 template <class T, int V, int I, int PAIRING>
 struct HeadWork {
     using A = Acc<T>;
+    using U = typename std::conditional<V == 1, A, Two<A>>::type;
     using Piece = HeadPiece<T, V>;
+    using Items = HeadItems<V, I, PAIRING>;
+    static constexpr int N = V == 1 ? 1 : V / 2;             // units of a piece
+    static constexpr bool HALVES = PAIRING == FO_PAIR_HALVES || V == 1;
 
+    // Cosines and sines of a lane's pairs.  Halves: of the units of a piece, with the sine's negative; neighbours: (c, c) and (-s, s) for
+    // every unit, which is a pair, of both pieces.
+    struct Angles {
+        U c[I][HALVES ? N : 2 * N], s[I][HALVES ? N : 2 * N], minus[HALVES ? I : 1][N];
+    };
+    template <int SIGN>
+    static __device__ __forceinline__ void angles(const HeadParams &p, const Items &at, const HeadRows &rows, Angles &g)
+    {
+        const A *const ct = static_cast<const A *>(p.cos_table), *const st = static_cast<const A *>(p.sin_table);
+        auto row_of = [&](int pair) {
+            int r = rows.at[0];
+#pragma unroll
+            for (int k = 1; k < FO_MAX_AXES; ++k)
+                if (k < p.axes && pair >= p.section_end[k - 1]) r = rows.at[k];
+            return r;
+        };
+        constexpr int W = 16 / (int)sizeof(A) < V ? 16 / (int)sizeof(A) : V;         // table values in one load
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            A c[V], s[V];
+#pragma unroll
+            for (int j0 = 0; j0 < V; j0 += W) {
+                const int pair = at.pair(i) + j0;
+                const bool on = at.a[i] >= 0 && at.ta(i) && pair < p.pairs;
+                const int r = on ? row_of(pair) : -1;
+#pragma unroll
+                for (int j = 0; j < W; ++j) c[j0 + j] = s[j0 + j] = A(NAN);          // a position outside the table
+                if (W > 1 && p.table_pieces) {
+                    if (r >= 0) {
+                        const HeadPiece<A, W> u = head_load<A, W>(ct + r * p.ld_cos + pair), v = head_load<A, W>(st + r * p.ld_sin + pair);
+#pragma unroll
+                        for (int j = 0; j < W; ++j) c[j0 + j] = u.v[j], s[j0 + j] = v.v[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        const int q = on && pair + j < p.pairs ? row_of(pair + j) : -1;
+                        if (q >= 0) c[j0 + j] = ct[q * p.ld_cos + pair + j], s[j0 + j] = st[q * p.ld_sin + pair + j];
+                    }
+                }
+            }
+            if constexpr (V == 1) {
+                g.c[i][0] = c[0], g.s[i][0] = A(SIGN) * s[0], g.minus[i][0] = A(-SIGN) * s[0];
+            } else if constexpr (HALVES) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    g.c[i][j] = two(c[2 * j], c[2 * j + 1]);
+                    g.s[i][j] = two(A(SIGN) * s[2 * j], A(SIGN) * s[2 * j + 1]), g.minus[i][j] = two(A(-SIGN) * s[2 * j], A(-SIGN) * s[2 * j + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2 * N; ++j) g.c[i][j] = both(c[j]), g.s[i][j] = two(A(-SIGN) * s[j], A(SIGN) * s[j]);
+            }
+        }
+    }
+    // Turns a lane's pieces.
+    static __device__ __forceinline__ void turn(const Items &at, const Angles &g, U (&a)[I][N], U (&b)[I][N])
+    {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if constexpr (HALVES) {
+                if (at.ta(i))
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const U x = a[i][j], y = b[i][j];
+                        a[i][j] = fused_ma(y, g.minus[i][j], x * g.c[i][j]);
+                        b[i][j] = fused_ma(x, g.s[i][j], y * g.c[i][j]);
+                    }
+            } else {
+                if (at.ta(i))
+#pragma unroll
+                    for (int j = 0; j < N; ++j) a[i][j] = fused_ma(head_swap(a[i][j]), g.s[i][j], a[i][j] * g.c[i][j]);
+                if (at.tb(i))
+#pragma unroll
+                    for (int j = 0; j < N; ++j) b[i][j] = fused_ma(head_swap(b[i][j]), g.s[i][N + j], b[i][j] * g.c[i][N + j]);
+            }
+        }
+    }
+
+    static __device__ __forceinline__ A sum(U v, int lanes)
+    {
+        A s = joined(v);
+        for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    }
     // n = (x - mu) r of a vector, in place; returns r
-    static __device__ __forceinline__ A normalise(const HeadParams &p, const HeadItems<V, I, PAIRING> &at, int kind, A eps,
-                                                  A (&a)[I][V], A (&b)[I][V])
+    static __device__ __forceinline__ A normalise(const HeadParams &p, const Items &at, int kind, A eps, U (&a)[I][N], U (&b)[I][N])
     {
         if (kind == FO_NORM_LAYER) {
-            A sum = A(0);
+            U s = head_all<U>(A(0));
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum += a[i][j] + b[i][j];            // absent pieces are zeros
-            const A mean = head_sum(sum, p.lanes) * A(p.inv_dim);
+                for (int j = 0; j < N; ++j) s = s + (a[i][j] + b[i][j]);             // absent pieces are zeros
+            const U mean = head_all<U>(-sum(s, p.lanes) * A(p.inv_dim));
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    a[i][j] = at.a[i] >= 0 ? a[i][j] - mean : A(0);
-                    b[i][j] = at.b[i] >= 0 ? b[i][j] - mean : A(0);
+                for (int j = 0; j < N; ++j) {
+                    if (at.a[i] >= 0) a[i][j] = a[i][j] + mean;
+                    if (at.b[i] >= 0) b[i][j] = b[i][j] + mean;
                 }
         }
-        A sq = A(0);
+        U sq = head_all<U>(A(0)), sr = sq;
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) sq = fused_ma(a[i][j], a[i][j], fused_ma(b[i][j], b[i][j], sq));
-        const A r = group_rsqrt(fused_ma(head_sum(sq, p.lanes), A(p.inv_dim), eps));
+            for (int j = 0; j < N; ++j) sq = fused_ma(a[i][j], a[i][j], sq), sr = fused_ma(b[i][j], b[i][j], sr);
+        const A r = group_rsqrt(fused_ma(sum(sq + sr, p.lanes), A(p.inv_dim), eps));
+        const U all = head_all<U>(r);
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[i][j] *= r, b[i][j] *= r;
+            for (int j = 0; j < N; ++j) a[i][j] = a[i][j] * all, b[i][j] = b[i][j] * all;
         return r;
     }
-    static __device__ __forceinline__ void fetch(const T *row, const HeadItems<V, I, PAIRING> &at, Piece (&a)[I], Piece (&b)[I], bool on)
+    static __device__ __forceinline__ void widen_piece(const Piece &q, U (&f)[N])
     {
+        if constexpr (V == 1) {
+            f[0] = widen(q.v[0]);
+        } else if constexpr (V * sizeof(T) == 16) {
+            const Packed<T, V> &w = reinterpret_cast<const Packed<T, V> &>(q);
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-            a[i] = b[i] = Piece{};
-            if (on && at.a[i] >= 0) a[i] = head_load<T, V>(row + at.a[i]);
-            if (on && at.b[i] >= 0) b[i] = head_load<T, V>(row + at.b[i]);
+            for (int j = 0; j < N; ++j) f[j] = w.get2(2 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = two(widen(q.v[2 * j]), widen(q.v[2 * j + 1]));
         }
     }
-    static __device__ __forceinline__ void widen_all(const Piece (&p)[I], A (&f)[I][V])
+    static __device__ __forceinline__ void store_piece(T *to, const U (&f)[N])
     {
+        if constexpr (V == 1) {
+            to[0] = narrow<T>(f[0]);
+        } else {
+            Packed<T, V * sizeof(T) == 8 ? 2 * V : V> w;
+            w.clear();
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[i][j] = widen(p[i].v[j]);
-    }
-    static __device__ __forceinline__ void store(T *row, const HeadItems<V, I, PAIRING> &at, const A (&a)[I][V], const A (&b)[I][V])
-    {
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            if (at.a[i] >= 0) head_store<T, V>(row + at.a[i], a[i]);
-            if (at.b[i] >= 0) head_store<T, V>(row + at.b[i], b[i]);
+            for (int j = 0; j < N; ++j) w.put2(2 * j, f[j]);
+            if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(&w);
+            else store16(to, w.w);
         }
     }
-    static __device__ __forceinline__ void weights(const HeadParams &p, const HeadTensor &t, const HeadItems<V, I, PAIRING> &at,
-                                                   A (&a)[I][V], A (&b)[I][V])
+    static __device__ __forceinline__ void store(T *row, const Items &at, const U (&a)[I][N], const U (&b)[I][N])
+    {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (at.a[i] >= 0) store_piece(row + at.a[i], a[i]);
+            if (at.b[i] >= 0) store_piece(row + at.b[i], b[i]);
+        }
+    }
+    // A piece of a weight or bias vector.
+    static __device__ __forceinline__ void vector_piece(const HeadParams &p, const void *v, int at, U (&f)[N])
+    {
+        A s[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = p.wide_vec ? (A) static_cast<const float *>(v)[at + j] : widen(static_cast<const T *>(v)[at + j]);
+        if constexpr (V == 1) f[0] = s[0];
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j) f[j] = two(s[2 * j], s[2 * j + 1]);
+    }
+    static __device__ __forceinline__ void weights(const HeadParams &p, const HeadTensor &t, const Items &at, U (&a)[I][N], U (&b)[I][N])
     {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[i][j] = b[i][j] = A(1);
-            if (t.weight && at.a[i] >= 0) head_vector<T, V>(t.weight, p.wide_vec, at.a[i], a[i]);
-            if (t.weight && at.b[i] >= 0) head_vector<T, V>(t.weight, p.wide_vec, at.b[i], b[i]);
+            for (int j = 0; j < N; ++j) a[i][j] = b[i][j] = head_all<U>(A(1));
+            if (t.weight && at.a[i] >= 0) vector_piece(p, t.weight, at.a[i], a[i]);
+            if (t.weight && at.b[i] >= 0) vector_piece(p, t.weight, at.b[i], b[i]);
         }
     }
 };
 
+// The pieces of a lane's next turns, of TENSORS tensors.  Pieces of 8 and 16 bytes go through a ring in shared memory: piece k
+// of turn s of thread t lies at ((s * pieces + k) * CTA + t) pieces, so that a warp's accesses meet all banks alike.  Single elements are fetched
+// into registers a turn ahead.
+template <class T, int V, int I, int TENSORS>
+struct HeadRing {
+    using Piece = HeadPiece<T, V>;
+    static constexpr bool RING = V > 1;
+    static constexpr int kTurns = RING ? (TENSORS == 1 ? 4 : 3) : 1;
+    static constexpr int kPieces = 2 * I * TENSORS;
+    static constexpr size_t kBytes = RING ? (size_t)kTurns * kPieces * kHeadCta * sizeof(Piece) : 0;
+    Piece held[RING ? 1 : TENSORS][RING ? 1 : 2 * I];
+    Piece *ring;
+    int in = 0, out = 0;                // turns modulo kTurns
+
+    __device__ __forceinline__ explicit HeadRing(void *memory) : ring(static_cast<Piece *>(memory) + threadIdx.x) {}
+
+    template <class Items>
+    __device__ __forceinline__ void issue(const T *const (&row)[TENSORS], const Items &at, bool on)
+    {
+#pragma unroll
+        for (int n = 0; n < TENSORS; ++n)
+#pragma unroll
+            for (int k = 0; k < 2 * I; ++k) {
+                const int e = k & 1 ? at.b[k / 2] : at.a[k / 2];
+                const bool there = on && row[n] && e >= 0;
+                if constexpr (RING) {
+                    Piece *to = ring + (in * kPieces + n * 2 * I + k) * kHeadCta;
+                    if (there) {
+                        const unsigned s = (unsigned)__cvta_generic_to_shared(to);
+                        if constexpr (sizeof(Piece) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(row[n] + e) : "memory");
+                        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(s), "l"(row[n] + e) : "memory");
+                    } else {
+                        *to = Piece{};
+                    }
+                } else {
+                    held[n][k] = there ? head_load<T, V>(row[n] + e) : Piece{};
+                }
+            }
+        if constexpr (RING) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            in = in + 1 == kTurns ? 0 : in + 1;
+        }
+    }
+    // Before a turn's take(): what it takes has arrived.
+    __device__ __forceinline__ void arrived() const
+    {
+        if constexpr (RING) asm volatile("cp.async.wait_group %0;" ::"n"(kTurns - 1) : "memory");
+    }
+    __device__ __forceinline__ Piece take(int n, int k) const
+    {
+        if constexpr (RING) return head_load<T, V>(reinterpret_cast<const T *>(ring + (out * kPieces + n * 2 * I + k) * kHeadCta));
+        else return held[n][k];
+    }
+    __device__ __forceinline__ void taken()
+    {
+        if constexpr (RING) out = out + 1 == kTurns ? 0 : out + 1;
+    }
+};
+
+// The turns of a warp, one behind the other: `h0` is the turn's first head (of the warp's first group), `end` the end of
+// the task's heads.
+struct HeadTurns {
+    unsigned task, tasks, step, token;
+    int h0, end, groups;
+    __device__ __forceinline__ HeadTurns(const HeadParams &p, const HeadTensor &t, int cta, int ctas)
+        : task(cta * kHeadWarps + threadIdx.x / 32), tasks((unsigned)p.all_tokens * (unsigned)t.chunks), step(ctas * kHeadWarps), groups(32 / p.lanes)
+    {
+        enter(t);
+    }
+    __device__ __forceinline__ bool there() const { return task < tasks; }
+    __device__ __forceinline__ void enter(const HeadTensor &t)
+    {
+        token = task / (unsigned)t.chunks;
+        h0 = (int)((task - token * (unsigned)t.chunks) * (unsigned)t.per_chunk);
+        end = min(t.heads, h0 + t.per_chunk);
+    }
+    // true: a new task, of another token
+    __device__ __forceinline__ bool next(const HeadTensor &t)
+    {
+        h0 += groups;
+        if (h0 < end) return false;
+        task += step;
+        if (there()) enter(t);
+        return true;
+    }
+};
+template <class T>
+__device__ __forceinline__ const T *head_row(const HeadParams &p, const void *x, const fo_strides &s, unsigned token)
+{
+    const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
+    return static_cast<const T *>(x) + b * s.batch + t * s.token;
+}
+
+// 8192 tokens with 32 + 8 heads of 128 in bfloat16
 template <class T, int V, int I, int PAIRING>
-__global__ void __launch_bounds__(kHeadCta) head_norm_kernel(const __grid_constant__ HeadParams p)
+__global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : HM) head_norm_kernel(const __grid_constant__ HeadParams p)
 {
     using W = HeadWork<T, V, I, PAIRING>;
     using A = Acc<T>;
+    using U = typename W::U;
+    constexpr int N = W::N;
+    extern __shared__ __align__(16) unsigned char head_memory[];
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
     const HeadTensor &t = p.t[which];
-    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, groups = 32 / p.lanes;
+    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes;
     const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
-    const HeadItems<V, I, PAIRING> at(lane, p.lanes, p.dim, p.pairs);
-    A wa[I][V], wb[I][V], c[I][V], s[I][V];
+    const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
+    HeadTurns ahead(p, t, cta, ctas), now = ahead;
+    if (!now.there()) return;
+    HeadRing<T, V, I, 1> ring(head_memory);
+    const T *x = head_row<T>(p, t.x, t.x_at, ahead.token);
+    auto issue = [&]() {
+        const T *const rows[1] = {x + (ahead.h0 + group) * t.x_at.head};
+        ring.issue(rows, at, ahead.there() && ahead.h0 + group < ahead.end);
+        if (ahead.there() && ahead.next(t) && ahead.there()) x = head_row<T>(p, t.x, t.x_at, ahead.token);
+    };
+    for (int k = 0; k < ring.kTurns; ++k) issue();
+    U wa[I][N], wb[I][N];
     W::weights(p, t, at, wa, wb);
-    const unsigned tasks = (unsigned)p.all_tokens * (unsigned)t.chunks;
-    for (unsigned task = cta * kHeadWarps + threadIdx.x / 32; task < tasks; task += ctas * kHeadWarps) {
-        const unsigned token = task / (unsigned)t.chunks, h0 = (task - token * (unsigned)t.chunks) * (unsigned)t.per_chunk;
-        const long long bt = token / (unsigned)p.tokens, tt = token - bt * p.tokens;
-        const int h1 = min(t.heads, (int)h0 + t.per_chunk);
-        const T *x = static_cast<const T *>(t.x) + bt * t.x_at.batch + tt * t.x_at.token;
-        T *y = static_cast<T *>(t.y) + bt * t.y_at.batch + tt * t.y_at.token;
-        typename W::Piece na[I], nb[I];
-        int h = (int)h0 + group;
-        W::fetch(x + h * t.x_at.head, at, na, nb, h < h1);
-        if (p.pairs) head_angles<A>(p, at, bt, tt, c, s);
-        for (int first = (int)h0; first < h1; first += groups, h += groups) {
-            A a[I][V], b[I][V];
-            W::widen_all(na, a), W::widen_all(nb, b);
-            W::fetch(x + (h + groups) * t.x_at.head, at, na, nb, h + groups < h1);
-            if (t.kind != FO_NORM_NONE) {
-                W::normalise(p, at, t.kind, A(t.eps), a, b);
+    typename W::Angles g;
+    HeadRows rows = {};
+    if (p.pairs) rows = head_rows(p, now.token);
+    for (bool fresh = true; now.there();) {
+        if (fresh && p.pairs) {
+            W::template angles<1>(p, at, rows, g);
+            const unsigned later = now.task + now.step;
+            if (later < now.tasks) rows = head_rows(p, later / (unsigned)t.chunks);
+        }
+        U a[I][N], b[I][N];
+        ring.arrived();
 #pragma unroll
-                for (int i = 0; i < I; ++i) {
+        for (int i = 0; i < I; ++i) W::widen_piece(ring.take(0, 2 * i), a[i]), W::widen_piece(ring.take(0, 2 * i + 1), b[i]);
+        ring.taken();
+        issue();
+        if (t.kind != FO_NORM_NONE) {
+            W::normalise(p, at, t.kind, A(t.eps), a, b);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) a[i][j] *= wa[i][j], b[i][j] *= wb[i][j];
-                    if (t.bias) {
-                        A ba[V], bb[V];
-                        if (at.a[i] >= 0) {
-                            head_vector<T, V>(t.bias, p.wide_vec, at.a[i], ba);
+            for (int i = 0; i < I; ++i) {
 #pragma unroll
-                            for (int j = 0; j < V; ++j) a[i][j] += ba[j];
-                        }
-                        if (at.b[i] >= 0) {
-                            head_vector<T, V>(t.bias, p.wide_vec, at.b[i], bb);
+                for (int j = 0; j < N; ++j) a[i][j] = a[i][j] * wa[i][j], b[i][j] = b[i][j] * wb[i][j];
+                if (t.bias) {
+                    U bias[N];
+                    if (at.a[i] >= 0) {
+                        W::vector_piece(p, t.bias, at.a[i], bias);
 #pragma unroll
-                            for (int j = 0; j < V; ++j) b[i][j] += bb[j];
-                        }
+                        for (int j = 0; j < N; ++j) a[i][j] = a[i][j] + bias[j];
+                    }
+                    if (at.b[i] >= 0) {
+                        W::vector_piece(p, t.bias, at.b[i], bias);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) b[i][j] = b[i][j] + bias[j];
                     }
                 }
             }
-            if (p.pairs)
-#pragma unroll
-                for (int i = 0; i < I; ++i) head_turn<V, PAIRING, 1>(a[i], b[i], at.ta[i], at.tb[i], c[i], s[i]);
-            if (h < h1) W::store(y + h * t.y_at.head, at, a, b);
         }
+        if (p.pairs) W::turn(at, g, a, b);
+        if (now.h0 + group < now.end)
+            W::store(const_cast<T *>(head_row<T>(p, t.y, t.y_at, now.token)) + (now.h0 + group) * t.y_at.head, at, a, b);
+        fresh = now.next(t);
     }
 }
 
 // The gradient.  Every lane keeps the sums of its own elements of dweight and dbias; at the end a CTA writes a line of
 // them, and head_sum_kernel adds the lines in order.
 template <class T, int V, int I, int PAIRING, bool BIAS>
-__global__ void __launch_bounds__(kHeadCta) head_norm_grad_kernel(const __grid_constant__ HeadParams p)
+__global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_norm_grad_kernel(const __grid_constant__ HeadParams p)
 {
     using W = HeadWork<T, V, I, PAIRING>;
     using A = Acc<T>;
+    using U = typename W::U;
+    constexpr int N = W::N;
     __shared__ A line[2][FO_HEAD_MAX_DIM];
+    extern __shared__ __align__(16) unsigned char head_memory[];
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
     const HeadTensor &t = p.t[which];
-    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, groups = 32 / p.lanes;
+    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes;
     const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
-    const HeadItems<V, I, PAIRING> at(lane, p.lanes, p.dim, p.pairs);
-    A wa[I][V], wb[I][V], c[I][V], s[I][V], da[I][V], db[I][V], ea[BIAS ? I : 1][V], eb[BIAS ? I : 1][V];
-    W::weights(p, t, at, wa, wb);
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            da[i][j] = db[i][j] = A(0);
-            if (BIAS) ea[i][j] = eb[i][j] = A(0);
-        }
+    const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
     const bool normed = t.kind != FO_NORM_NONE;
-    const unsigned tasks = (unsigned)p.all_tokens * (unsigned)t.chunks;
-    for (unsigned task = cta * kHeadWarps + threadIdx.x / 32; task < tasks; task += ctas * kHeadWarps) {
-        const unsigned token = task / (unsigned)t.chunks, h0 = (task - token * (unsigned)t.chunks) * (unsigned)t.per_chunk;
-        const long long bt = token / (unsigned)p.tokens, tt = token - bt * p.tokens;
-        const int h1 = min(t.heads, (int)h0 + t.per_chunk);
-        const T *x = static_cast<const T *>(t.x) + bt * t.x_at.batch + tt * t.x_at.token;
-        const T *dy = static_cast<const T *>(t.dy) + bt * t.dy_at.batch + tt * t.dy_at.token;
-        T *dx = static_cast<T *>(t.y) + bt * t.y_at.batch + tt * t.y_at.token;
-        typename W::Piece na[I], nb[I], ga[I], gb[I];
-        int h = (int)h0 + group;
-        W::fetch(x + h * t.x_at.head, at, na, nb, normed && h < h1);
-        W::fetch(dy + h * t.dy_at.head, at, ga, gb, h < h1);
-        if (p.pairs) head_angles<A>(p, at, bt, tt, c, s);
-        for (int first = (int)h0; first < h1; first += groups, h += groups) {
-            A a[I][V], b[I][V], u[I][V], v[I][V];
-            W::widen_all(na, a), W::widen_all(nb, b), W::widen_all(ga, u), W::widen_all(gb, v);
-            const bool more = h + groups < h1;
-            W::fetch(x + (h + groups) * t.x_at.head, at, na, nb, normed && more);
-            W::fetch(dy + (h + groups) * t.dy_at.head, at, ga, gb, more);
-            if (p.pairs)
-#pragma unroll
-                for (int i = 0; i < I; ++i) head_turn<V, PAIRING, -1>(u[i], v[i], at.ta[i], at.tb[i], c[i], s[i]);
-            if (normed) {
-                // a lane without a head has zeros throughout; its r is finite only with eps > 0, so it must not be multiplied in
-                const A r = W::normalise(p, at, t.kind, h < h1 ? A(t.eps) : A(1), a, b);
-                A with_n = A(0), alone = A(0);
-#pragma unroll
-                for (int i = 0; i < I; ++i)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        da[i][j] = fused_ma(u[i][j], a[i][j], da[i][j]);
-                        db[i][j] = fused_ma(v[i][j], b[i][j], db[i][j]);
-                        if (BIAS) ea[i][j] += u[i][j], eb[i][j] += v[i][j];
-                        u[i][j] *= wa[i][j], v[i][j] *= wb[i][j];
-                        with_n = fused_ma(u[i][j], a[i][j], fused_ma(v[i][j], b[i][j], with_n));
-                        alone += u[i][j] + v[i][j];
-                    }
-                with_n = head_sum(with_n, p.lanes) * A(p.inv_dim);
-                alone = t.kind == FO_NORM_LAYER ? head_sum(alone, p.lanes) * A(p.inv_dim) : A(0);
-#pragma unroll
-                for (int i = 0; i < I; ++i)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        u[i][j] = r * (fused_ma(-with_n, a[i][j], u[i][j]) - alone);
-                        v[i][j] = r * (fused_ma(-with_n, b[i][j], v[i][j]) - alone);
-                    }
-            }
-            if (h < h1) W::store(dx + h * t.y_at.head, at, u, v);
-        }
-    }
-    if (!t.partial_w && !t.partial_b) return;
-    // the warp's groups, then the CTA's warps one after the other
+    HeadTurns ahead(p, t, cta, ctas), now = ahead;
+    HeadRing<T, V, I, 2> ring(head_memory);
+    const T *x = nullptr, *dy = nullptr;
+    auto enter = [&]() {
+        if (!ahead.there()) return;
+        if (normed) x = head_row<T>(p, t.x, t.x_at, ahead.token);
+        dy = head_row<T>(p, t.dy, t.dy_at, ahead.token);
+    };
+    enter();
+    auto issue = [&]() {
+        const T *const rows[2] = {dy + (ahead.h0 + group) * t.dy_at.head, normed ? x + (ahead.h0 + group) * t.x_at.head : nullptr};
+        ring.issue(rows, at, ahead.there() && ahead.h0 + group < ahead.end);
+        if (ahead.there() && ahead.next(t)) enter();
+    };
+    for (int k = 0; k < ring.kTurns; ++k) issue();
+    U wa[I][N], wb[I][N], da[I][N], db[I][N], ea[BIAS ? I : 1][N], eb[BIAS ? I : 1][N];
+    W::weights(p, t, at, wa, wb);
+    const U zero = head_all<U>(A(0));
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            for (int o = p.lanes; o < 32; o <<= 1) {
-                da[i][j] += __shfl_xor_sync(0xffffffffu, da[i][j], o);
-                db[i][j] += __shfl_xor_sync(0xffffffffu, db[i][j], o);
-                if (BIAS) {
-                    ea[i][j] += __shfl_xor_sync(0xffffffffu, ea[i][j], o);
-                    eb[i][j] += __shfl_xor_sync(0xffffffffu, eb[i][j], o);
-                }
-            }
-    for (int w = 0; w < kHeadWarps; ++w) {
-        if ((int)threadIdx.x / 32 == w && group == 0) {
+        for (int j = 0; j < N; ++j) {
+            da[i][j] = db[i][j] = zero;
+            if (BIAS) ea[i][j] = eb[i][j] = zero;
+        }
+    typename W::Angles g;
+    HeadRows rows = {};
+    if (p.pairs && now.there()) rows = head_rows(p, now.token);
+    for (bool fresh = true; now.there();) {
+        if (fresh && p.pairs) {
+            W::template angles<-1>(p, at, rows, g);
+            const unsigned later = now.task + now.step;
+            if (later < now.tasks) rows = head_rows(p, later / (unsigned)t.chunks);
+        }
+        U a[I][N], b[I][N], u[I][N], v[I][N];
+        ring.arrived();
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            W::widen_piece(ring.take(0, 2 * i), u[i]), W::widen_piece(ring.take(0, 2 * i + 1), v[i]);
+            W::widen_piece(ring.take(1, 2 * i), a[i]), W::widen_piece(ring.take(1, 2 * i + 1), b[i]);
+        }
+        ring.taken();
+        issue();
+        const bool on = now.h0 + group < now.end;
+        if (p.pairs) W::turn(at, g, u, v);
+        if (normed) {
+            // a group without a head has zeros throughout, and with eps 0 its r would not be finite
+            const A r = W::normalise(p, at, t.kind, on ? A(t.eps) : A(1), a, b);
+            U with_n = zero, alone = zero;
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if (at.a[i] >= 0) {
-                        line[0][at.a[i] + j] = (w ? line[0][at.a[i] + j] : A(0)) + da[i][j];
-                        if (BIAS) line[1][at.a[i] + j] = (w ? line[1][at.a[i] + j] : A(0)) + ea[i][j];
-                    }
-                    if (at.b[i] >= 0) {
-                        line[0][at.b[i] + j] = (w ? line[0][at.b[i] + j] : A(0)) + db[i][j];
-                        if (BIAS) line[1][at.b[i] + j] = (w ? line[1][at.b[i] + j] : A(0)) + eb[i][j];
-                    }
+                for (int j = 0; j < N; ++j) {
+                    da[i][j] = fused_ma(u[i][j], a[i][j], da[i][j]);
+                    db[i][j] = fused_ma(v[i][j], b[i][j], db[i][j]);
+                    if (BIAS) ea[i][j] = ea[i][j] + u[i][j], eb[i][j] = eb[i][j] + v[i][j];
+                    u[i][j] = u[i][j] * wa[i][j], v[i][j] = v[i][j] * wb[i][j];
+                    with_n = fused_ma(u[i][j], a[i][j], fused_ma(v[i][j], b[i][j], with_n));
+                    alone = alone + (u[i][j] + v[i][j]);
                 }
+            const U back = head_all<U>(-W::sum(with_n, p.lanes) * A(p.inv_dim)), all = head_all<U>(r);
+            const U mean = t.kind == FO_NORM_LAYER ? head_all<U>(-W::sum(alone, p.lanes) * A(p.inv_dim)) : zero;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    u[i][j] = (fused_ma(back, a[i][j], u[i][j]) + mean) * all;
+                    v[i][j] = (fused_ma(back, b[i][j], v[i][j]) + mean) * all;
+                }
+        }
+        if (on) W::store(const_cast<T *>(head_row<T>(p, t.y, t.y_at, now.token)) + (now.h0 + group) * t.y_at.head, at, u, v);
+        fresh = now.next(t);
+    }
+    if (!t.partial_w && !t.partial_b) return;
+    // the warp's groups, then the CTA's warps one after the other
+    auto groups_sum = [&](U f, int k) {
+        A s;
+        if constexpr (V == 1) s = f;
+        else s = k ? second(f) : first(f);
+        for (int o = p.lanes; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    };
+    for (int w = 0; w < kHeadWarps; ++w) {
+        if ((int)threadIdx.x / 32 == w) {
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+#pragma unroll
+                    for (int k = 0; k < V / N; ++k) {
+                        const int e = j * (V / N) + k;
+                        const A sa = groups_sum(da[i][j], k), sb = groups_sum(db[i][j], k);
+                        const A ta = BIAS ? groups_sum(ea[BIAS ? i : 0][j], k) : A(0), tb = BIAS ? groups_sum(eb[BIAS ? i : 0][j], k) : A(0);
+                        if (group == 0 && at.a[i] >= 0) {
+                            line[0][at.a[i] + e] = (w ? line[0][at.a[i] + e] : A(0)) + sa;
+                            if (BIAS) line[1][at.a[i] + e] = (w ? line[1][at.a[i] + e] : A(0)) + ta;
+                        }
+                        if (group == 0 && at.b[i] >= 0) {
+                            line[0][at.b[i] + e] = (w ? line[0][at.b[i] + e] : A(0)) + sb;
+                            if (BIAS) line[1][at.b[i] + e] = (w ? line[1][at.b[i] + e] : A(0)) + tb;
+                        }
+                    }
         }
         __syncthreads();
     }

@@ -2,15 +2,28 @@
 #pragma once
 
 #include "head_norm.cuh"
+#include "launch.cuh"
 
 namespace fo {
+
+template <class T, int V, int I, int TENSORS>
+cudaError_t head_go(void (*kernel)(HeadParams), const HeadParams &p, int grid, cudaStream_t st, OncePerGpu &once)
+{
+    constexpr size_t bytes = HeadRing<T, V, I, TENSORS>::kBytes;
+    if (bytes > 40 * 1024) {                              // with the static part
+        const cudaError_t e = once.allow(kernel, bytes);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_beside(kernel, dim3((unsigned)grid), kHeadCta, st, bytes, p);
+}
 
 template <class T, int V, int I, int PAIRING>
 cudaError_t head_launch(const HeadParams &p, bool grad, bool bias, int grid, cudaStream_t st)
 {
-    if (!grad) return launch_beside(head_norm_kernel<T, V, I, PAIRING>, dim3((unsigned)grid), kHeadCta, st, p);
-    if (bias) return launch_beside(head_norm_grad_kernel<T, V, I, PAIRING, true>, dim3((unsigned)grid), kHeadCta, st, p);
-    return launch_beside(head_norm_grad_kernel<T, V, I, PAIRING, false>, dim3((unsigned)grid), kHeadCta, st, p);
+    static OncePerGpu once[3];
+    if (!grad) return head_go<T, V, I, 1>(head_norm_kernel<T, V, I, PAIRING>, p, grid, st, once[0]);
+    if (bias) return head_go<T, V, I, 2>(head_norm_grad_kernel<T, V, I, PAIRING, true>, p, grid, st, once[1]);
+    return head_go<T, V, I, 2>(head_norm_grad_kernel<T, V, I, PAIRING, false>, p, grid, st, once[2]);
 }
 
 template <class T, int V, int I>

@@ -1,6 +1,7 @@
 // How a recurrence is cut into CTAs and clusters, for one pair of element types.
 #pragma once
 
+#include "launch.cuh"
 #include "scan.cuh"
 
 namespace fo {
@@ -24,20 +25,10 @@ cudaError_t scan_launch(ScanParams p, long long batch, cudaStream_t st)
     while (warps < 8 && (long long)warps * S < p.tokens) warps *= 2;
     // a round of all CTAs together is to occupy the GPU, and no more than that
     while (cluster < kScanMostCluster && items * cluster * 2 <= (long long)sms * 3 && (long long)cluster * warps * S < p.tokens) cluster *= 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * cluster));
-    cfg.blockDim = dim3((unsigned)(32 * warps));
-    cfg.dynamicSmemBytes = ScanShared<Acc<T>, V>::bytes(warps, cluster);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if constexpr (GRAD) return cudaLaunchKernelEx(&cfg, scan_grad_kernel<T, G, V, S>, p);
-    else return cudaLaunchKernelEx(&cfg, scan_kernel<T, G, V, S>, p);
+    const size_t shared = ScanShared<Acc<T>, V>::bytes(warps, cluster);
+    const dim3 grid((unsigned)(items * cluster));
+    if constexpr (GRAD) return launch_beside(scan_grad_kernel<T, G, V, S>, grid, 32 * warps, st, shared, p, cluster);
+    else return launch_beside(scan_kernel<T, G, V, S>, grid, 32 * warps, st, shared, p, cluster);
 }
 
 // wide: channels can move in pairs (16-bit types)
