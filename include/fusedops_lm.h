@@ -108,8 +108,11 @@ size_t fused_head_norm_grad_workspace_bytes(int dim, int type);
  * `last` may be `state`.  1 - a is computed without the cancellation; 16-bit x goes through the hardware's
  * exponential and reciprocal, decays near 1 rounded to 32 bits all the same.
  * Element (b, t, c) of x, gate, h is at p[b * batch + t * token + c].  state and last: float (double for FO_F64), contiguous.
- * gate_type: `type`, or FO_F32 with a 16-bit type.  h may be x itself.  A decoding step is the call with tokens = 1.
+ * gate_type: `type`, or FO_F32 with a 16-bit type.  channels <= FO_SCAN_MAX_CHANNELS, tokens <= FO_SCAN_MAX_TOKENS.  h may be
+ * x itself.  A decoding step is the call with tokens = 1.
  */
+#define FO_SCAN_MAX_CHANNELS (1 << 28)
+#define FO_SCAN_MAX_TOKENS (1 << 30)
 enum { FO_DECAY_VALUE = 0, FO_DECAY_SIGMOID = 1, FO_DECAY_EXP = 2 };
 enum { FO_MIX_ONE = 0, FO_MIX_REST = 1, FO_MIX_ROOT = 2 };
 

@@ -13,7 +13,7 @@ namespace fo {
     X(FO_F16, FO_F16, __half, __half)              \
     X(FO_F16, FO_F32, __half, float)
 
-#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(const ScanParams &, bool, bool, long long, cudaStream_t);
+#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(ScanParams, bool, long long, cudaStream_t);
 FO_SCAN_PAIRS(FO_EXTERN)
 #undef FO_EXTERN
 
@@ -25,6 +25,7 @@ int check_scan(long long batch, long long tokens, long long channels, int type, 
                int lengths_type, std::initializer_list<fo_rows> strides)
 {
     if (batch < 0 || tokens < 0 || channels < 0) return FO_ERR_SHAPE;
+    if (channels > FO_SCAN_MAX_CHANNELS || tokens > FO_SCAN_MAX_TOKENS) return FO_ERR_UNSUPPORTED;
     bool ok = false;
 #define FO_CASE(t, g, T, G) ok = ok || (type == t && gate_type == g);
     FO_SCAN_PAIRS(FO_CASE)
@@ -45,17 +46,19 @@ bool all_on(int type, std::initializer_list<const void *> ps)
         if (!on_elements(p, type)) return false;
     return true;
 }
-// Every piece of two channels of a matrix begins at a multiple of its size.
-bool in_pairs(const void *p, const fo_rows &s, int type)
+// Every row begins at a multiple of `bytes`.
+bool rows_at(const void *p, const fo_rows &s, int type, int bytes)
 {
-    return ((uintptr_t)p & (unsigned)(2 * elem_bytes(type) - 1)) == 0 && s.batch % 2 == 0 && s.token % 2 == 0;
+    return (((uintptr_t)p | (unsigned long long)(s.batch | s.token) * (unsigned)elem_bytes(type)) & (unsigned)(bytes - 1)) == 0;
 }
+int whole_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 16) ? bit : 0; }
+int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 2 * elem_bytes(type)) ? bit : 0; }
 
-int launch(const ScanParams &p, int type, int gate_type, bool wide, bool grad, long long batch, cudaStream_t st)
+int launch(const ScanParams &p, int type, int gate_type, bool grad, long long batch, cudaStream_t st)
 {
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(t, g, T, G) \
-    if (type == t && gate_type == g) e = launch_scan<T, G>(p, wide, grad, batch, st);
+    if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, batch, st);
     FO_SCAN_PAIRS(FO_CASE)
 #undef FO_CASE
     return e == cudaSuccess ? FO_OK : cuda_fail(e);
@@ -80,14 +83,14 @@ int fused_scan(const fo_scan *a, void *stream)
         return FO_ERR_UNSUPPORTED;
     if (a->tokens == 0 && !a->last) return FO_OK;
     ScanParams p = {};
-    p.tokens = a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.tokens = (int)a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
     p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
     p.reset = static_cast<const unsigned char *>(a->reset);
     p.h = a->h, p.last = a->last;
     p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->h_at;
-    const bool wide = a->channels % 2 == 0 && in_pairs(a->x, a->x_at, a->type) && in_pairs(a->gate, a->gate_at, a->gate_type)
-                      && in_pairs(a->h, a->h_at, a->type);
-    return launch(p, a->type, a->gate_type, wide, false, a->batch, (cudaStream_t)stream);
+    p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
+              | pairs_if(a->h, a->h_at, a->type, kScanOut);
+    return launch(p, a->type, a->gate_type, false, a->batch, (cudaStream_t)stream);
 }
 
 int fused_scan_grad(const fo_scan_grad *a, void *stream)
@@ -104,17 +107,16 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
         return FO_ERR_UNSUPPORTED;
     if (a->tokens == 0 && !a->dstate) return FO_OK;
     ScanParams p = {};
-    p.tokens = a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.tokens = (int)a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
     p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
     p.reset = static_cast<const unsigned char *>(a->reset);
     p.h = a->dx, p.last = a->dstate, p.dh = a->dh, p.dlast = a->dlast, p.h_in = a->h, p.dgate = a->dgate;
     p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->dx_at;
     p.dh_at = a->dh_at, p.h_in_at = a->h_at, p.dgate_at = a->dgate_at;
-    bool wide = a->channels % 2 == 0 && in_pairs(a->gate, a->gate_at, a->gate_type) && in_pairs(a->dgate, a->dgate_at, a->gate_type)
-                && in_pairs(a->h, a->h_at, a->type) && in_pairs(a->dx, a->dx_at, a->type);
-    if (a->dh) wide = wide && in_pairs(a->dh, a->dh_at, a->type);
-    if (mixes) wide = wide && in_pairs(a->x, a->x_at, a->type);
-    return launch(p, a->type, a->gate_type, wide, true, a->batch, (cudaStream_t)stream);
+    p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
+              | whole_if(a->dh, a->dh_at, a->type, kScanDh) | whole_if(a->h, a->h_at, a->type, kScanH)
+              | pairs_if(a->dx, a->dx_at, a->type, kScanOut) | pairs_if(a->dgate, a->dgate_at, a->gate_type, kScanOutGate);
+    return launch(p, a->type, a->gate_type, true, a->batch, (cudaStream_t)stream);
 }
 
 }  // extern "C"

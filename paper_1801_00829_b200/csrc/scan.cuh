@@ -5,7 +5,8 @@
 // the sequence.  In a round every warp runs its segment from zero, which gives the map h -> A h + H of the whole segment, the maps
 // are put one behind the other in the order of the tokens, and with the state that comes in the segment is run again, from
 // registers.  So the inputs are read once and no CTA waits for another outside its cluster, whose CTAs run together.
-// The next round's inputs are on their way meanwhile.
+// The inputs of the next rounds are on their way meanwhile, to a ring in shared memory: asynchronous copies, which a warp makes
+// for itself.
 #pragma once
 
 #include "elem.cuh"
@@ -13,12 +14,17 @@
 
 namespace fo {
 
-constexpr int kScanMostWarps = 16;
+constexpr int kScanCta = 256;
+constexpr int kScanMostWarps = kScanCta / 32;
 constexpr int kScanMostCluster = 8;
 
+enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32 };
+
 struct ScanParams {
-    long long tokens, channels, tiles;  // tiles: of 32 V channels
+    long long channels;
+    int tokens, tiles;                  // tiles: of 32 V channels
     int mode, long_lengths;             // mode: decay * 3 + mix
+    int whole;                          // which tensors' rows begin at 16-byte boundaries (ScanTensor); of outputs, at those of two channels
     const void *x, *gate, *state, *lengths;
     const unsigned char *reset;
     void *h, *last;                     // gradient: dx, dstate
@@ -57,22 +63,129 @@ struct ScanPiece {
     alignas(V * sizeof(T)) T v[V];
 };
 template <class T, int V>
-__device__ __forceinline__ ScanPiece<T, V> scan_load(const T *p)
+__device__ __forceinline__ ScanPiece<T, V> scan_piece(const char *p)
 {
     ScanPiece<T, V> r;
     if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t *>(&r) = *reinterpret_cast<const uint32_t *>(p);
     else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2 *>(&r) = *reinterpret_cast<const uint2 *>(p);
-    else if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(&r) = *reinterpret_cast<const uint4 *>(p);
-    else r.v[0] = p[0];
+    else r.v[0] = *reinterpret_cast<const T *>(p);
     return r;
 }
+// A lane's channels of a row, which is found by a base that is the same for the whole warp and the lane's offset.  count: of
+// the channels that there are; whole: they can move together.
 template <class T, int V>
-__device__ __forceinline__ void scan_store(T *p, const ScanPiece<T, V> &r)
+__device__ __forceinline__ void scan_store(char *row, unsigned offset, const ScanPiece<T, V> &r, int count, bool whole)
 {
-    if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(&r);
-    else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(&r);
-    else if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(&r);
-    else p[0] = r.v[0];
+    char *p = row + offset;
+    if constexpr (V == 1) {
+        if (count > 0) *reinterpret_cast<T *>(p) = r.v[0];
+    } else {
+        if (whole) {
+            if (count == 2) {
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(&r);
+                else *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(&r);
+                return;
+            }
+        }
+        if (count > 0) reinterpret_cast<T *>(p)[0] = r.v[0];
+        if (count > 1) reinterpret_cast<T *>(p)[1] = r.v[1];
+    }
+}
+
+// Copies of a warp's segment, S rows of W channels, into its place in the ring.  Row r is at base + r * stride (the stride is
+// negative where segments run backwards).  Pieces of 16 bytes where all rows begin at such a boundary, the last one of a row
+// cut off where its channels end; else single elements of 4 or 8 bytes; those of 2 bytes, which no asynchronous copy can
+// move, by loads.
+template <class T, int S, int W>
+struct ScanCopy {
+    static constexpr int kBytes = S * W * (int)sizeof(T);
+    static constexpr int kRowPieces = W * (int)sizeof(T) / 16, kRows = 32 / kRowPieces, kTurns = S / kRows;
+    int row, bytes, channels;
+    unsigned place;
+    long long offset;
+    bool whole;
+    __device__ __forceinline__ ScanCopy(bool whole_, int lane, int channels_, long long stride) : channels(channels_), whole(whole_)
+    {
+        row = lane / kRowPieces;
+        const int at = lane % kRowPieces * 16;
+        bytes = min(16, channels * (int)sizeof(T) - at);
+        place = row * W * (int)sizeof(T) + at, offset = row * stride + at;
+    }
+    template <class Valid>
+    __device__ __forceinline__ void issue(char *to, const char *base, long long stride, Valid valid) const
+    {
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < kTurns; ++j)
+                if (valid(row + j * kRows) && bytes > 0)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(to) + place + j * 512),
+                                 "l"(base + j * kRows * stride + offset), "r"(bytes) : "memory");
+            return;
+        }
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int j = 0; j < S; ++j)
+#pragma unroll
+            for (int v = 0; v < W / 32; ++v) {
+                const int c = v * 32 + lane;
+                if (!valid(j) || c >= channels) continue;
+                const T *from = reinterpret_cast<const T *>(base + j * stride) + c;
+                T *dst = reinterpret_cast<T *>(to) + j * W + c;
+                if constexpr (sizeof(T) == 2) *dst = *from;
+                else
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((unsigned)__cvta_generic_to_shared(dst)), "l"(from), "n"((int)sizeof(T)) : "memory");
+            }
+    }
+};
+template <int N>
+__device__ __forceinline__ void scan_arrived()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void scan_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+// The unit of arithmetic: a lane's V channels, two of them in one register pair.
+template <class A, int V> struct ScanUnit { using U = Two<A>; };
+template <class A> struct ScanUnit<A, 1> { using U = A; };
+__device__ __forceinline__ float scan_part(float u, int) { return u; }
+__device__ __forceinline__ double scan_part(double u, int) { return u; }
+template <class A> __device__ __forceinline__ A scan_part(Two<A> u, int v) { return v ? second(u) : first(u); }
+template <class U, class A>
+__device__ __forceinline__ U scan_all(A v)
+{
+    if constexpr (std::is_same<U, A>::value) return v;
+    else return both(v);
+}
+// f of every channel
+template <class F> __device__ __forceinline__ float scan_each(float u, F f) { return f(u); }
+template <class F> __device__ __forceinline__ double scan_each(double u, F f) { return f(u); }
+template <class A, class F> __device__ __forceinline__ Two<A> scan_each(Two<A> u, F f) { return two(f(first(u)), f(second(u))); }
+template <class F> __device__ __forceinline__ float scan_each(float u, float w, F f) { return f(u, w); }
+template <class F> __device__ __forceinline__ double scan_each(double u, double w, F f) { return f(u, w); }
+template <class A, class F> __device__ __forceinline__ Two<A> scan_each(Two<A> u, Two<A> w, F f) { return two(f(first(u), first(w)), f(second(u), second(w))); }
+template <class U, class T, int V>
+__device__ __forceinline__ U scan_widen(const ScanPiece<T, V> &p)
+{
+    if constexpr (V == 1) return (U)widen(p.v[0]);
+    else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(&p);
+        return two(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    } else return two(widen(p.v[0]), widen(p.v[1]));
+}
+template <class T, int V, class U>
+__device__ __forceinline__ ScanPiece<T, V> scan_narrow(U u)
+{
+    ScanPiece<T, V> r;
+    if constexpr (V == 2 && sizeof(T) == 2) {
+        Packed<T, 8> w;
+        w.put2(0, u);
+        *reinterpret_cast<uint32_t *>(&r) = w.w[0];
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) r.v[v] = narrow<T>(scan_part(u, v));
+    }
+    return r;
 }
 
 // ------------------------------------------------------------------------------------------------ decays
@@ -101,19 +214,15 @@ template <bool EXACT> __device__ __forceinline__ float scan_root(float v) { retu
 template <bool EXACT> __device__ __forceinline__ double scan_root(double v) { return sqrt(v); }
 template <bool EXACT> __device__ __forceinline__ float scan_over(float v) { return EXACT ? 1.0f / v : scan_rcp(v); }
 template <bool EXACT> __device__ __forceinline__ double scan_over(double v) { return 1.0 / v; }
+// exp(-|g|)
+template <bool EXACT> __device__ __forceinline__ float scan_exp_down(float g) { return EXACT ? expf(-fabsf(g)) : scan_exp2(fabsf(g) * -1.4426950408889634f); }
+template <bool EXACT> __device__ __forceinline__ double scan_exp_down(double g) { return exp(-fabs(g)); }
 
-constexpr float kLog2e = 1.4426950408889634f;
-
-template <int DECAY, bool EXACT>
-__device__ __forceinline__ void scan_decay(float g, float &a, float &rest)
+// exp(g) and 1 - exp(g)
+template <bool EXACT>
+__device__ __forceinline__ void scan_exponential(float g, float &a, float &rest)
 {
-    if constexpr (DECAY == FO_DECAY_VALUE) {
-        a = g, rest = 1.0f - g;
-    } else if constexpr (DECAY == FO_DECAY_SIGMOID) {
-        const float e = EXACT ? expf(-fabsf(g)) : scan_exp2(-fabsf(g) * kLog2e);
-        const float small = e * scan_over<EXACT>(1.0f + e), big = 1.0f - small;
-        a = g >= 0.0f ? big : small, rest = g >= 0.0f ? small : big;
-    } else if constexpr (EXACT) {
+    if constexpr (EXACT) {
         rest = -expm1f(g);
         a = g > -0.5f ? 1.0f - rest : expf(g);
     } else {
@@ -123,41 +232,63 @@ __device__ __forceinline__ void scan_decay(float g, float &a, float &rest)
         m = fused_ma(m, g, 1.0f / 6.0f);
         m = fused_ma(m, g, 0.5f);
         m = fused_ma(m * g, g, g);
-        const float e = scan_exp2(g * kLog2e);
+        const float e = scan_exp2(g * 1.4426950408889634f);
         const bool near = fabsf(g) < 0.25f;
         a = near ? 1.0f + m : e, rest = near ? -m : 1.0f - e;
     }
 }
-template <int DECAY, bool EXACT>
-__device__ __forceinline__ void scan_decay(double g, double &a, double &rest)
+template <bool EXACT>
+__device__ __forceinline__ void scan_exponential(double g, double &a, double &rest)
 {
+    rest = -expm1(g);
+    a = g > -0.5 ? 1.0 - rest : exp(g);
+}
+template <int DECAY, bool EXACT, class A, class U>
+__device__ __forceinline__ void scan_decay(U g, U &a, U &rest)
+{
+    const U one = scan_all<U>(A(1)), less = scan_all<U>(A(-1));
     if constexpr (DECAY == FO_DECAY_VALUE) {
-        a = g, rest = 1.0 - g;
+        a = g, rest = fused_ma(g, less, one);
     } else if constexpr (DECAY == FO_DECAY_SIGMOID) {
-        const double e = exp(-fabs(g)), small = e / (1.0 + e), big = 1.0 - small;
-        a = g >= 0.0 ? big : small, rest = g >= 0.0 ? small : big;
+        const U e = scan_each(g, [](A v) { return scan_exp_down<EXACT>(v); });
+        const U small = e * scan_each(e + one, [](A v) { return scan_over<EXACT>(v); }), big = fused_ma(small, less, one);
+        if constexpr (std::is_same<U, A>::value) {
+            a = g >= A(0) ? big : small, rest = g >= A(0) ? small : big;
+        } else {
+            const bool p = first(g) >= A(0), q = second(g) >= A(0);
+            a = two(p ? first(big) : first(small), q ? second(big) : second(small));
+            rest = two(p ? first(small) : first(big), q ? second(small) : second(big));
+        }
+    } else if constexpr (std::is_same<U, A>::value) {
+        scan_exponential<EXACT>(g, a, rest);
     } else {
-        rest = -expm1(g);
-        a = g > -0.5 ? 1.0 - rest : exp(g);
+        A a0, a1, r0, r1;
+        scan_exponential<EXACT>(first(g), a0, r0);
+        scan_exponential<EXACT>(second(g), a1, r1);
+        a = two(a0, a1), rest = two(r0, r1);
     }
 }
 // m(a)
-template <int MIX, bool EXACT, class A>
-__device__ __forceinline__ A scan_mix(A a, A rest)
+template <int MIX, bool EXACT, class A, class U>
+__device__ __forceinline__ U scan_mix(U a, U rest)
 {
-    if constexpr (MIX == FO_MIX_ONE) return A(1);
+    if constexpr (MIX == FO_MIX_ONE) return scan_all<U>(A(1));
     else if constexpr (MIX == FO_MIX_REST) return rest;
-    else return scan_root<EXACT>(rest * (A(1) + a));
+    else return scan_each(fused_ma(rest, a, rest), [](A v) { return scan_root<EXACT>(v); });
 }
 // The derivatives of a and of m to the gate.
-template <int DECAY, int MIX, bool EXACT, class A>
-__device__ __forceinline__ void scan_slopes(A a, A rest, A m, A &da, A &dm)
+template <int DECAY, int MIX, bool EXACT, class A, class U>
+__device__ __forceinline__ void scan_slopes(U a, U rest, U m, U &da, U &dm)
 {
-    da = DECAY == FO_DECAY_VALUE ? A(1) : DECAY == FO_DECAY_EXP ? a : a * rest;
-    if constexpr (MIX == FO_MIX_ONE) dm = A(0);
-    else if constexpr (MIX == FO_MIX_REST) dm = -da;
-    else if constexpr (DECAY == FO_DECAY_SIGMOID) dm = -a * a * m * scan_over<EXACT>(A(1) + a);      // a' = a (1 - a) has m in it
-    else dm = -a * da * scan_over<EXACT>(m);
+    const U less = scan_all<U>(A(-1));
+    if constexpr (DECAY == FO_DECAY_VALUE) da = scan_all<U>(A(1));
+    else if constexpr (DECAY == FO_DECAY_EXP) da = a;
+    else da = a * rest;
+    if constexpr (MIX == FO_MIX_ONE) dm = scan_all<U>(A(0));
+    else if constexpr (MIX == FO_MIX_REST) dm = da * less;
+    else if constexpr (DECAY == FO_DECAY_SIGMOID)            // a' = a (1 - a) has m in it
+        dm = a * (a * less) * m * scan_each(a + scan_all<U>(A(1)), [](A v) { return scan_over<EXACT>(v); });
+    else dm = a * (da * less) * scan_each(m, [](A v) { return scan_over<EXACT>(v); });
 }
 
 // Calls go(decay, mix) with compile-time numbers.
@@ -171,328 +302,416 @@ __device__ __forceinline__ void with_mode(int mode, Go go)
     }
 #undef FO_MODE
 }
+template <class Go>
+__device__ __forceinline__ void with_decay(int mode, Go go)
+{
+    if (mode < 3) go(std::integral_constant<int, FO_DECAY_VALUE>());
+    else if (mode < 6) go(std::integral_constant<int, FO_DECAY_SIGMOID>());
+    else go(std::integral_constant<int, FO_DECAY_EXP>());
+}
 
 // ------------------------------------------------------------------------------------------------ segments put together
-template <class A>
-struct alignas(2 * sizeof(A)) ScanMap {
-    A a, h;
+// h -> a h + h of V channels
+template <class U>
+struct ScanMap {
+    U a, h;
 };
 
 // The shared memory of a CTA, twice (one round's is written while another warp still reads the last one's).
-template <class A, int V>
+template <class U>
 struct ScanShared {
-    ScanMap<A> *warp_maps, *cta_maps;                    // of every warp's segment, and of every CTA's segments
+    ScanMap<U> *warp_maps, *cta_maps;                    // of every warp's segment, and of every CTA's segments
+    U *carry;                                            // what comes into the round
     int *warp_drops, *cta_drops;                         // a reset lies in them: nothing comes through
     int warps, ctas;
 
     static __host__ __device__ size_t bytes(int warps, int ctas)
     {
-        return warps * ctas == 1 ? 0 : 2 * (warps + ctas) * (V * 32 * sizeof(ScanMap<A>) + sizeof(int));
+        if (warps * ctas == 1) return 0;
+        return 2 * ((warps + ctas) * 32 * sizeof(ScanMap<U>) + 32 * sizeof(U) + (kScanMostCluster + kScanMostWarps) * sizeof(int));
     }
     __device__ __forceinline__ ScanShared(void *at, int w, int c) : warps(w), ctas(c)
     {
-        warp_maps = static_cast<ScanMap<A> *>(at), cta_maps = warp_maps + 2 * w * V * 32;
-        warp_drops = reinterpret_cast<int *>(cta_maps + 2 * c * V * 32), cta_drops = warp_drops + 2 * w;
+        warp_maps = static_cast<ScanMap<U> *>(at) + (threadIdx.x & 31), cta_maps = warp_maps + 2 * w * 32;
+        carry = reinterpret_cast<U *>(static_cast<ScanMap<U> *>(at) + 2 * (w + c) * 32) + (threadIdx.x & 31);
+        cta_drops = reinterpret_cast<int *>(reinterpret_cast<U *>(static_cast<ScanMap<U> *>(at) + 2 * (w + c) * 32) + 2 * 32);
+        warp_drops = cta_drops + 2 * kScanMostCluster;
     }
-    __device__ __forceinline__ ScanMap<A> &warp(int parity, int w, int v) const { return warp_maps[((parity * warps + w) * V + v) * 32 + (threadIdx.x & 31)]; }
-    __device__ __forceinline__ ScanMap<A> &cta(int parity, int c, int v) const { return cta_maps[((parity * ctas + c) * V + v) * 32 + (threadIdx.x & 31)]; }
-    __device__ __forceinline__ int &warp_drop(int parity, int w) const { return warp_drops[parity * warps + w]; }
-    __device__ __forceinline__ int &cta_drop(int parity, int c) const { return cta_drops[parity * ctas + c]; }
+    __device__ __forceinline__ ScanMap<U> *warp(int parity) const { return warp_maps + parity * warps * 32; }
+    __device__ __forceinline__ ScanMap<U> *cta(int parity) const { return cta_maps + parity * ctas * 32; }
 };
 
-template <class A>
-__device__ __forceinline__ A scan_apply(const ScanMap<A> &m, int drops, A c)
+template <class U>
+__device__ __forceinline__ U scan_apply(const ScanMap<U> &m, int drops, U c)
 {
     return drops ? m.h : fused_ma(m.a, c, m.h);
 }
-__device__ __forceinline__ void scan_push(unsigned to, const ScanMap<float> &m)
+template <class U>
+__device__ __forceinline__ void scan_push(unsigned to, const ScanMap<U> &m)
 {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m.a), "f"(m.h) : "memory");
+    const uint32_t *w = reinterpret_cast<const uint32_t *>(&m);
+    if constexpr (sizeof(m) == 8) asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(w[0]), "r"(w[1]) : "memory");
+    else asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
-__device__ __forceinline__ void scan_push(unsigned to, const ScanMap<double> &m)
+// `c` through maps [from, to), where any of them drops what comes (DROPS) by their marks.
+template <bool DROPS, class U>
+__device__ __forceinline__ U scan_through(const ScanMap<U> *maps, const int *drops, int from, int to, U c)
 {
-    asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(to), "d"(m.a), "d"(m.h) : "memory");
+#pragma unroll 4
+    for (int k = from; k < to; ++k) c = scan_apply(maps[k * 32], DROPS ? drops[k] : 0, c);
+    return c;
 }
 
-// Every warp gives its segment's map (and whether it drops what comes in); carry is what comes into the round.  Returns what
-// comes into the warp's segment, and sets carry to what leaves the round.  One barrier, a second one of the cluster.
-template <class A, int V>
-__device__ __forceinline__ void scan_join(const ScanShared<A, V> &sh, int parity, unsigned rank, unsigned cluster, const A (&a)[V],
-                                          const A (&h)[V], int drops, A (&carry)[V], A (&in)[V])
+// Before the first round: `carry` is what comes into it, in every warp and CTA.
+template <class U>
+__device__ __forceinline__ void scan_begin(const ScanShared<U> &sh, int warp, U carry)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = sh.warps;
-    if (warps == 1 && cluster == 1) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) in[v] = carry[v], carry[v] = scan_apply({a[v], h[v]}, drops, carry[v]);
-        return;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) sh.warp(parity, warp, v) = {a[v], h[v]};
-    if (lane == 0) sh.warp_drop(parity, warp) = drops;
-    __syncthreads();
+    if (sh.warps * sh.ctas == 1) return;
+    if (warp == sh.warps - 1) sh.carry[0] = carry;
+    if (threadIdx.x < 2 * kScanMostCluster) sh.cta_drops[threadIdx.x] = 0;
+}
+template <bool DROPS, class A, class U>
+__device__ __forceinline__ U scan_joined(const ScanShared<U> &sh, int parity, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own, int drops)
+{
+    const ScanMap<U> *const maps = sh.warp(parity);
+    const int *const marks = sh.warp_drops + parity * kScanMostWarps;
+    const bool last = warp == sh.warps - 1;
+    U in = sh.carry[parity * 32];
     if (cluster > 1) {
-        if (warp == 0) {
-            int any = 0;
-            ScanMap<A> m[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) m[v] = {A(1), A(0)};
-            for (int w = 0; w < warps; ++w) {
-                const int d = sh.warp_drop(parity, w);
-                any |= d;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const ScanMap<A> s = sh.warp(parity, w, v);
-                    m[v].h = scan_apply(s, d, m[v].h);
-                    m[v].a *= s.a;
-                }
+        const ScanMap<U> *const ctas = sh.cta(parity);
+        const int *const cta_marks = sh.cta_drops + parity * kScanMostCluster;
+        in = scan_through<DROPS>(ctas, cta_marks, 0, (int)rank, in);
+        if (last) sh.carry[(parity ^ 1) * 32] = scan_through<DROPS>(ctas, cta_marks, (int)rank, (int)cluster, in);
+        return scan_through<DROPS>(maps, marks, 0, warp, in);
+    }
+    in = scan_through<DROPS>(maps, marks, 0, warp, in);
+    if (last) sh.carry[(parity ^ 1) * 32] = scan_apply(own, DROPS ? drops : 0, in);
+    return in;
+}
+
+// Every warp gives its segment's map (and whether it drops what comes in); returns what comes into the segment.  `carry` is
+// what comes into the round and what leaves it where a warp is alone; otherwise the last warp of each CTA writes what leaves the round
+// for the next one, whose barrier lies between.  One barrier, a second one of the cluster.
+template <class A, class U>
+__device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int parity, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own,
+                                       int drops, U &carry)
+{
+    const int lane = threadIdx.x & 31, warps = sh.warps;
+    if (warps == 1 && cluster == 1) {
+        const U in = carry;
+        carry = scan_apply(own, drops, carry);
+        return in;
+    }
+    sh.warp(parity)[warp * 32] = own;
+    if (lane == 0) sh.warp_drops[parity * kScanMostWarps + warp] = drops;
+    int any = __syncthreads_or(drops);
+    if (cluster > 1) {
+        if (warp == warps - 1) {
+            const ScanMap<U> *const maps = sh.warp(parity);
+            const int *const marks = sh.warp_drops + parity * kScanMostWarps;
+            ScanMap<U> m = maps[0];
+#pragma unroll 4
+            for (int w = 1; w < warps; ++w) {
+                const ScanMap<U> s = maps[w * 32];
+                m.h = scan_apply(s, any ? marks[w] : 0, m.h);
+                m.a = m.a * s.a;
             }
             for (unsigned k = 0; k < cluster; ++k) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) scan_push(scan_peer(&sh.cta(parity, rank, v), k), m[v]);
+                scan_push(scan_peer(sh.cta(parity) + rank * 32, k), m);
                 if (lane == 0)
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(scan_peer(&sh.cta_drop(parity, rank), k)), "r"(any) : "memory");
+                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(scan_peer(sh.cta_drops + parity * kScanMostCluster + rank, k)), "r"(any) : "memory");
             }
         }
         __syncwarp();
         scan_arrive();
         scan_wait();
-        A c[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = in[v] = carry[v];
-        for (unsigned k = 0; k < cluster; ++k) {
-            const int d = sh.cta_drop(parity, k);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (k == rank) in[v] = c[v];
-                c[v] = scan_apply(sh.cta(parity, k, v), d, c[v]);
-            }
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) carry[v] = c[v];
-        for (int w = 0; w < warp; ++w) {
-            const int d = sh.warp_drop(parity, w);
-#pragma unroll
-            for (int v = 0; v < V; ++v) in[v] = scan_apply(sh.warp(parity, w, v), d, in[v]);
-        }
-        return;
+        const int4 *const q = reinterpret_cast<const int4 *>(sh.cta_drops + parity * kScanMostCluster);
+        const int4 d = q[0], e = q[1];
+        any = d.x | d.y | d.z | d.w | e.x | e.y | e.z | e.w;
     }
-    A c[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) c[v] = in[v] = carry[v];
-    for (int w = 0; w < warps; ++w) {
-        const int d = sh.warp_drop(parity, w);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (w == warp) in[v] = c[v];
-            c[v] = scan_apply(sh.warp(parity, w, v), d, c[v]);
-        }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = c[v];
+    return any ? scan_joined<true, A>(sh, parity, rank, cluster, warp, own, drops) : scan_joined<false, A>(sh, parity, rank, cluster, warp, own, drops);
+}
+// After the last round, whose parity was the other one: what has left it.
+template <class U>
+__device__ __forceinline__ U scan_left(const ScanShared<U> &sh, int parity, U carry)
+{
+    if (sh.warps * sh.ctas == 1) return carry;
+    __syncthreads();
+    return sh.carry[parity * 32];
 }
 
 // The tokens of sequence b.
-__device__ __forceinline__ long long scan_length(const ScanParams &p, long long b)
+__device__ __forceinline__ int scan_length(const ScanParams &p, long long b)
 {
     if (!p.lengths) return p.tokens;
     const long long n = p.long_lengths ? static_cast<const long long *>(p.lengths)[b] : static_cast<const int *>(p.lengths)[b];
-    return n < 0 ? 0 : n > p.tokens ? p.tokens : n;
+    return n < 0 ? 0 : n > p.tokens ? p.tokens : (int)n;
 }
 
+// A lane's channels of a state.
+template <class U, class A, int V>
+__device__ __forceinline__ U scan_state(const void *p, long long at, int count)
+{
+    const A *s = static_cast<const A *>(p) + at;
+    const A s0 = p && count > 0 ? s[0] : A(0);
+    if constexpr (V == 1) return s0;
+    else return two(s0, p && count > 1 ? s[1] : A(0));
+}
+template <class U, class A, int V>
+__device__ __forceinline__ void scan_keep(void *p, long long at, U u, int count)
+{
+    A *s = static_cast<A *>(p) + at;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v < count) s[v] = scan_part(u, v);
+}
+
+// Where a warp is in the call.
+template <int V>
+struct ScanPlace {
+    unsigned rank, cluster;
+    int lane, warp, warps;
+    long long b, state;                 // state: of the lane's first channel
+    int first, channel, count;          // first channel of the tile and of the lane, channels of the lane
+    __device__ __forceinline__ explicit ScanPlace(const ScanParams &p) : rank(scan_rank()), cluster(scan_cluster())
+    {
+        // the same for all lanes, and known to be: the addresses of rows are then computed once for the warp
+        warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+        const unsigned item = blockIdx.x / cluster;
+        b = item / (unsigned)p.tiles;
+        first = (int)(item - (unsigned)b * (unsigned)p.tiles) * 32 * V, channel = first + lane * V;
+        count = max(0, min(V, (int)p.channels - channel));
+        state = b * p.channels + channel;
+    }
+};
+
 template <class T, class G, int V, int S>
-__global__ void __launch_bounds__(kScanMostWarps * 32) scan_kernel(const __grid_constant__ ScanParams p)
+struct ScanRing {
+    static constexpr int kStages = 3;
+    // of a warp in one stage
+    static constexpr int kForward = ScanCopy<T, S, 32 * V>::kBytes + ScanCopy<G, S, 32 * V>::kBytes;
+    static constexpr int kBackward = 3 * ScanCopy<T, S, 32 * V>::kBytes + ScanCopy<G, S, 32 * V>::kBytes;
+    static size_t bytes(int warps, bool grad) { return (size_t)kStages * warps * (grad ? kBackward : kForward); }
+};
+
+template <class T, class G, int V, int S>
+__global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(const __grid_constant__ ScanParams p)
 {
     using A = Acc<T>;
+    using U = typename ScanUnit<A, V>::U;
+    using Ring = ScanRing<T, G, V, S>;
     constexpr bool EXACT = sizeof(T) >= 4;
-    extern __shared__ __align__(16) unsigned char scan_memory[];
-    const unsigned rank = scan_rank(), cluster = scan_cluster();
-    const ScanShared<A, V> sh(scan_memory, blockDim.x >> 5, cluster);
-    if (cluster > 1) scan_arrive();                      // waited for before the first push: every CTA has started by then
+    extern __shared__ __align__(16) char scan_memory[];
+    const ScanPlace<V> at(p);
     wait_for_earlier();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const long long item = blockIdx.x / cluster, b = item / p.tiles, c = (item - b * p.tiles) * (32 * V) + lane * V;
-    const bool on = c < p.channels;
-    const long long end = scan_length(p, b);
-    const T *x = static_cast<const T *>(p.x) + b * p.x_at.batch + c;
-    const G *gate = static_cast<const G *>(p.gate) + b * p.gate_at.batch + c;
-    const unsigned char *reset = p.reset ? p.reset + b * p.reset_at.batch : nullptr;
-    T *h = static_cast<T *>(p.h) + b * p.h_at.batch + c;
-    A carry[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = p.state && on ? static_cast<const A *>(p.state)[b * p.channels + c + v] : A(0);
-    if (cluster > 1) scan_wait();
-
-    ScanPiece<T, V> xn[S];
-    ScanPiece<G, V> gn[S];
-    unsigned char mark = 0;
-    const long long round = (long long)cluster * warps * S;
-    long long t0 = ((long long)rank * warps + warp) * S;
-    auto fetch = [&](long long t) {
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            if (on && t + s < end) {
-                xn[s] = scan_load<T, V>(x + (t + s) * p.x_at.token);
-                gn[s] = scan_load<G, V>(gate + (t + s) * p.gate_at.token);
-            }
-        }
-        mark = reset && lane < S && t + lane < end ? reset[(t + lane) * p.reset_at.token] : 0;
+    char *const ring = scan_memory + at.warp * Ring::kStages * Ring::kForward;
+    const ScanShared<U> sh(scan_memory + at.warps * Ring::kStages * Ring::kForward, at.warps, at.cluster);
+    const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
+    int t0 = (at.rank * at.warps + at.warp) * S;
+    const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), hs = p.h_at.token * (int)sizeof(T);
+    const unsigned ho = at.channel * (unsigned)sizeof(T);
+    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + t0 * xs;
+    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + t0 * gs;
+    char *h = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + t0 * hs;
+    const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, (int)p.channels - at.first, xs);
+    const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, (int)p.channels - at.first, gs);
+    const bool pairs = p.whole & kScanOut;
+    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
+    int ahead = t0, in_stage = 0, stage = 0;
+    auto issue = [&]() {
+        char *to = ring + in_stage * Ring::kForward;
+        const auto valid = [&](int r) { return ahead + r < end; };
+        copy_x.issue(to, x, xs, valid);
+        copy_gate.issue(to + copy_x.kBytes, gate, gs, valid);
+        scan_issued();
+        ahead += round, x += round * xs, gate += round * gs, in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
-    fetch(t0);
+    for (int k = 0; k < Ring::kStages - 1; ++k) issue();
+    U carry = scan_state<U, A, V>(p.state, at.state, at.count);
+    scan_begin(sh, at.warp, carry);
+    if (at.cluster > 1) {
+        __syncthreads();                                 // every CTA has started, and the marks are cleared
+        scan_arrive();
+        scan_wait();
+    }
+    auto marks = [&](int t) -> unsigned char { return reset && at.lane < S && t + at.lane < end ? reset[(t + at.lane) * p.reset_at.token] : 0; };
+    unsigned char mark = marks(t0);
     int parity = 0;
-    for (long long first = 0; first < p.tokens; first += round, t0 += round, parity ^= 1) {
+    for (int first = 0; first < p.tokens; first += round, parity ^= 1) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
-        A a[S][V], m[S][V];                              // m becomes m(a) x
+        scan_arrived<Ring::kStages - 2>();
+        issue();                                         // where the stage before was
+        const char *const from = ring + stage * Ring::kForward + at.lane * V * (int)sizeof(T);
+        const char *const from_gate = ring + stage * Ring::kForward + copy_x.kBytes + at.lane * V * (int)sizeof(G);
+        stage = stage + 1 == Ring::kStages ? 0 : stage + 1;
+        U a[S], m[S];                                    // m becomes m(a) x
         with_mode(p.mode, [&](auto decay, auto mix) {
 #pragma unroll
-            for (int s = 0; s < S; ++s)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    A rest;
-                    scan_decay<decay.value, EXACT>((A)widen(gn[s].v[v]), a[s][v], rest);
-                    m[s][v] = scan_mix<mix.value, EXACT>(a[s][v], rest) * widen(xn[s].v[v]);
-                    if (!on || t0 + s >= end) a[s][v] = A(1), m[s][v] = A(0);    // the state stays as it is
-                }
+            for (int s = 0; s < S; ++s) {
+                U rest;
+                scan_decay<decay.value, EXACT, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * 32 * V * (int)sizeof(G))), a[s], rest);
+                m[s] = scan_mix<mix.value, EXACT, A>(a[s], rest) * scan_widen<U>(scan_piece<T, V>(from + s * 32 * V * (int)sizeof(T)));
+            }
         });
-        fetch(t0 + round);
-        A through[V], hs[V], in[V];
+        mark = marks(t0 + round);
+        const bool full = t0 + S <= end;
+        if (!full)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            through[v] = A(1), hs[v] = A(0);
+            for (int s = 0; s < S; ++s)
+                if (t0 + s >= end) a[s] = scan_all<U>(A(1)), m[s] = scan_all<U>(A(0));      // the state stays as it is
+        ScanMap<U> own = {a[0], m[0]};
+        if (drops == 0) {
+#pragma unroll
+            for (int s = 1; s < S; ++s) own.h = fused_ma(a[s], own.h, m[s]), own.a = own.a * a[s];
+        } else {
+#pragma unroll
+            for (int s = 1; s < S; ++s) own.h = (drops >> s) & 1u ? m[s] : fused_ma(a[s], own.h, m[s]), own.a = own.a * a[s];
+        }
+        U in = scan_join<A>(sh, parity, at.rank, at.cluster, at.warp, own, drops != 0, carry);
+        if (full && drops == 0) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                const bool drop = (drops >> s) & 1u;
-                hs[v] = drop ? m[s][v] : fused_ma(a[s][v], hs[v], m[s][v]);
-                through[v] *= a[s][v];
+                in = fused_ma(a[s], in, m[s]);
+                scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(in), at.count, pairs);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                in = (drops >> s) & 1u ? m[s] : fused_ma(a[s], in, m[s]);
+                if (t0 + s < p.tokens) scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(t0 + s < end ? in : scan_all<U>(A(0))), at.count, pairs);
             }
         }
-        scan_join(sh, parity, rank, cluster, through, hs, drops != 0, carry, in);
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            ScanPiece<T, V> out;
-            const bool drop = (drops >> s) & 1u;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                in[v] = drop ? m[s][v] : fused_ma(a[s][v], in[v], m[s][v]);
-                out.v[v] = narrow<T>(t0 + s < end ? in[v] : A(0));
-            }
-            if (on && t0 + s < p.tokens) scan_store<T, V>(h + (t0 + s) * p.h_at.token, out);
-        }
+        t0 += round, h += round * hs;
     }
-    if (p.last && on && rank == 0 && warp == 0)
-#pragma unroll
-        for (int v = 0; v < V; ++v) static_cast<A *>(p.last)[b * p.channels + c + v] = carry[v];
+    carry = scan_left(sh, parity, carry);
+    if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
 // The gradient: l_t = dh_t + u_{t+1}, u_t = a_t l_t is what comes to the token before (nothing through a reset), from the last token to
 // the first.  Segments are counted from the end, and a segment's map is that of u.
 template <class T, class G, int V, int S>
-__global__ void __launch_bounds__(kScanMostWarps * 32) scan_grad_kernel(const __grid_constant__ ScanParams p)
+__global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_constant__ ScanParams p)
 {
     using A = Acc<T>;
+    using U = typename ScanUnit<A, V>::U;
+    using Ring = ScanRing<T, G, V, S>;
     constexpr bool EXACT = sizeof(T) >= 4;
-    extern __shared__ __align__(16) unsigned char scan_memory[];
-    const unsigned rank = scan_rank(), cluster = scan_cluster();
-    const ScanShared<A, V> sh(scan_memory, blockDim.x >> 5, cluster);
-    if (cluster > 1) scan_arrive();
+    constexpr int kPart = ScanCopy<T, S, 32 * V>::kBytes, kRow = 32 * V * (int)sizeof(T), kGateRow = 32 * V * (int)sizeof(G);
+    extern __shared__ __align__(16) char scan_memory[];
+    const ScanPlace<V> at(p);
     wait_for_earlier();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const long long item = blockIdx.x / cluster, b = item / p.tiles, c = (item - b * p.tiles) * (32 * V) + lane * V;
-    const bool on = c < p.channels;
-    const long long end = scan_length(p, b);
-    const T *x = static_cast<const T *>(p.x) + b * p.x_at.batch + c;
-    const T *dh = static_cast<const T *>(p.dh) + b * p.dh_at.batch + c;
-    const T *hin = static_cast<const T *>(p.h_in) + b * p.h_in_at.batch + c;
-    const G *gate = static_cast<const G *>(p.gate) + b * p.gate_at.batch + c;
-    const unsigned char *reset = p.reset ? p.reset + b * p.reset_at.batch : nullptr;
-    T *dx = static_cast<T *>(p.h) + b * p.h_at.batch + c;
-    G *dgate = static_cast<G *>(p.dgate) + b * p.dgate_at.batch + c;
-    const bool with_x = p.mode % 3 != FO_MIX_ONE, with_dh = p.dh != nullptr;
-    A carry[V], start[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        carry[v] = p.dlast && on ? static_cast<const A *>(p.dlast)[b * p.channels + c + v] : A(0);
-        start[v] = p.state && on ? static_cast<const A *>(p.state)[b * p.channels + c + v] : A(0);
-    }
-    if (cluster > 1) scan_wait();
-
-    ScanPiece<T, V> xn[S], dn[S], hn[S];
-    ScanPiece<G, V> gn[S];
-    unsigned char mark = 0;
-    const long long round = (long long)cluster * warps * S;
+    char *const ring = scan_memory + at.warp * Ring::kStages * Ring::kBackward;
+    const ScanShared<U> sh(scan_memory + at.warps * Ring::kStages * Ring::kBackward, at.warps, at.cluster);
+    const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
     // element s of a segment is token t0 - s
-    long long t0 = p.tokens - 1 - ((long long)rank * warps + warp) * S;
-    auto fetch = [&](long long t) {
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const long long at = t - s;
-            if (on && at >= 0 && at < end) {
-                gn[s] = scan_load<G, V>(gate + at * p.gate_at.token);
-                if (with_x) xn[s] = scan_load<T, V>(x + at * p.x_at.token);
-                if (with_dh) dn[s] = scan_load<T, V>(dh + at * p.dh_at.token);
-                if (at > 0) hn[s] = scan_load<T, V>(hin + (at - 1) * p.h_in_at.token);
-            }
-        }
-        mark = reset && lane < S && t - lane >= 0 && t - lane < end ? reset[(t - lane) * p.reset_at.token] : 0;
+    int t0 = p.tokens - 1 - (int)(at.rank * at.warps + at.warp) * S;
+    const long long xs = -p.x_at.token * (int)sizeof(T), gs = -p.gate_at.token * (int)sizeof(G), ds = -p.dh_at.token * (int)sizeof(T),
+                    hs = -p.h_in_at.token * (int)sizeof(T), dxs = -p.h_at.token * (int)sizeof(T), dgs = -p.dgate_at.token * (int)sizeof(G);
+    const unsigned xo = at.channel * (unsigned)sizeof(T), go = at.channel * (unsigned)sizeof(G);
+    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) - t0 * xs;
+    const char *dh = static_cast<const char *>(p.dh) + (at.b * p.dh_at.batch + at.first) * (int)sizeof(T) - t0 * ds;
+    const char *hin = static_cast<const char *>(p.h_in) + (at.b * p.h_in_at.batch + at.first) * (int)sizeof(T) - (t0 - 1) * hs;   // of the token before
+    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) - t0 * gs;
+    char *dx = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) - t0 * dxs;
+    char *dgate = static_cast<char *>(p.dgate) + at.b * p.dgate_at.batch * (int)sizeof(G) - t0 * dgs;
+    const int channels = (int)p.channels - at.first;
+    const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, channels, gs);
+    const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, channels, xs), copy_dh(p.whole & kScanDh, at.lane, channels, ds),
+        copy_h(p.whole & kScanH, at.lane, channels, hs);
+    const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate;
+    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
+    const bool with_x = p.mode % 3 != FO_MIX_ONE, with_dh = p.dh != nullptr;
+    int ahead = t0, in_stage = 0, stage = 0;
+    auto issue = [&]() {
+        char *to = ring + in_stage * Ring::kBackward;
+        const auto valid = [&](int r) { return ahead - r >= 0 && ahead - r < end; };
+        if (with_dh) copy_dh.issue(to, dh, ds, valid);
+        if (with_x) copy_x.issue(to + kPart, x, xs, valid);
+        copy_h.issue(to + 2 * kPart, hin, hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
+        copy_gate.issue(to + 3 * kPart, gate, gs, valid);
+        scan_issued();
+        ahead -= round, x += round * xs, dh += round * ds, hin += round * hs, gate += round * gs;
+        in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
-    fetch(t0);
+    for (int k = 0; k < Ring::kStages - 1; ++k) issue();
+    U carry = scan_state<U, A, V>(p.dlast, at.state, at.count);
+    const U start = scan_state<U, A, V>(p.state, at.state, at.count), none = scan_all<U>(A(0));
+    scan_begin(sh, at.warp, carry);
+    if (at.cluster > 1) {
+        __syncthreads();                                 // every CTA has started, and the marks are cleared
+        scan_arrive();
+        scan_wait();
+    }
+    auto marks = [&](int t) -> unsigned char {
+        return reset && at.lane < S && t - at.lane >= 0 && t - at.lane < end ? reset[(t - at.lane) * p.reset_at.token] : 0;
+    };
+    unsigned char mark = marks(t0);
     int parity = 0;
-    for (long long first = 0; first < p.tokens; first += round, t0 -= round, parity ^= 1) {
+    for (int first = 0; first < p.tokens; first += round, parity ^= 1) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
-        ScanPiece<T, V> xs[S], ds[S], hs[S];
-        ScanPiece<G, V> gs[S];
+        scan_arrived<Ring::kStages - 2>();
+        issue();                                         // where the stage before was
+        const char *const from = ring + stage * Ring::kBackward + at.lane * V * (int)sizeof(T);
+        const char *const from_gate = ring + stage * Ring::kBackward + 3 * kPart + at.lane * V * (int)sizeof(G);
+        stage = stage + 1 == Ring::kStages ? 0 : stage + 1;
+        auto d_of = [&](int s) { return with_dh ? scan_widen<U>(scan_piece<T, V>(from + s * kRow)) : none; };
+        auto x_of = [&](int s) { return scan_widen<U>(scan_piece<T, V>(from + kPart + s * kRow)); };
+        auto h_of = [&](int s) { return scan_widen<U>(scan_piece<T, V>(from + 2 * kPart + s * kRow)); };
+        U a[S], rest[S];
+        with_decay(p.mode, [&](auto decay) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) xs[s] = xn[s], ds[s] = dn[s], hs[s] = hn[s], gs[s] = gn[s];
-        fetch(t0 - round);
-        A through[V], u[V], in[V];
+            for (int s = 0; s < S; ++s) scan_decay<decay.value, EXACT, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * kGateRow)), a[s], rest[s]);
+        });
+        mark = marks(t0 - round);
+        // plain: all of the segment's tokens are the sequence's, and none of them its first one or drops what comes
+        const bool plain = t0 < end && t0 >= S && drops == 0;
+        ScanMap<U> own = {scan_all<U>(A(1)), none};
+        if (plain) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) through[v] = A(1), u[v] = A(0);
-        with_mode(p.mode, [&](auto decay, auto) {
+            for (int s = 0; s < S; ++s) own.h = a[s] * (d_of(s) + own.h), own.a = own.a * a[s];
+        } else {
 #pragma unroll
             for (int s = 0; s < S; ++s)
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    A a, rest;
-                    scan_decay<decay.value, EXACT>((A)widen(gs[s].v[v]), a, rest);
-                    const bool live = on && t0 - s >= 0 && t0 - s < end;
-                    const A l = (with_dh ? widen(ds[s].v[v]) : A(0)) + u[v];
-                    if (live) u[v] = (drops >> s) & 1u ? A(0) : a * l, through[v] *= a;
-                }
-        });
-        scan_join(sh, parity, rank, cluster, through, u, drops != 0, carry, in);
-        with_mode(p.mode, [&](auto decay, auto mix) {
+                if (t0 - s >= 0 && t0 - s < end) own.h = (drops >> s) & 1u ? none : a[s] * (d_of(s) + own.h), own.a = own.a * a[s];
+        }
+        U in = scan_join<A>(sh, parity, at.rank, at.cluster, at.warp, own, drops != 0, carry);
+        auto finish = [&](auto decay, auto mix, auto masked) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                ScanPiece<T, V> to_x;
-                ScanPiece<G, V> to_g;
-                const bool live = on && t0 - s >= 0 && t0 - s < end, drop = (drops >> s) & 1u;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    A a, rest, da, dm;
-                    scan_decay<decay.value, EXACT>((A)widen(gs[s].v[v]), a, rest);
-                    const A m = scan_mix<mix.value, EXACT>(a, rest);
-                    scan_slopes<decay.value, mix.value, EXACT>(a, rest, m, da, dm);
-                    const A l = (with_dh ? widen(ds[s].v[v]) : A(0)) + in[v];
-                    const A before = t0 - s > 0 ? widen(hs[s].v[v]) : start[v];
-                    A slope = drop ? A(0) : da * before;
-                    if (mix.value != FO_MIX_ONE) slope = fused_ma(dm, widen(xs[s].v[v]), slope);
-                    to_x.v[v] = narrow<T>(live ? m * l : A(0));
-                    to_g.v[v] = narrow<G>(live ? l * slope : A(0));
-                    if (live) in[v] = drop ? A(0) : a * l;
+                U da, dm;
+                const U m = scan_mix<mix.value, EXACT, A>(a[s], rest[s]), l = d_of(s) + in;
+                scan_slopes<decay.value, mix.value, EXACT, A>(a[s], rest[s], m, da, dm);
+                U to_x = m * l, before = h_of(s), through = a[s] * l, slope;
+                if constexpr (masked.value) {
+                    const bool drop = (drops >> s) & 1u;
+                    if (t0 - s == 0) before = start;
+                    if (drop) before = none, through = none;
                 }
-                if (on && t0 - s >= 0) {
-                    scan_store<T, V>(dx + (t0 - s) * p.h_at.token, to_x);
-                    scan_store<G, V>(dgate + (t0 - s) * p.dgate_at.token, to_g);
+                if constexpr (mix.value == FO_MIX_ONE) slope = da * before;
+                else if constexpr (mix.value == FO_MIX_REST) slope = da * fused_ma(x_of(s), scan_all<U>(A(-1)), before);
+                else slope = fused_ma(dm, x_of(s), da * before);
+                U to_g = l * slope;
+                if constexpr (masked.value) {
+                    const bool live = t0 - s >= 0 && t0 - s < end;
+                    if (!live) to_x = none, to_g = none, through = in;
                 }
+                if (!masked.value || t0 - s >= 0) {
+                    scan_store<T, V>(dx + s * dxs, xo, scan_narrow<T, V>(to_x), at.count, pairs);
+                    scan_store<G, V>(dgate + s * dgs, go, scan_narrow<G, V>(to_g), at.count, gate_pairs);
+                }
+                in = through;
             }
-        });
+        };
+        if (plain) with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::false_type()); });
+        else with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::true_type()); });
+        t0 -= round, dx += round * dxs, dgate += round * dgs;
     }
-    if (p.last && on && rank == 0 && warp == 0)
-#pragma unroll
-        for (int v = 0; v < V; ++v) static_cast<A *>(p.last)[b * p.channels + c + v] = carry[v];
+    carry = scan_left(sh, parity, carry);
+    if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
 // Host: one kernel of a pair of types; scan_*.cu instantiate it.
 template <class T, class G>
-cudaError_t launch_scan(const ScanParams &p, bool wide, bool grad, long long batch, cudaStream_t st);
+cudaError_t launch_scan(ScanParams p, bool grad, long long batch, cudaStream_t st);
 
 }  // namespace fo
