@@ -116,6 +116,8 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
     p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
               | whole_if(a->dh, a->dh_at, a->type, kScanDh) | whole_if(a->h, a->h_at, a->type, kScanH)
               | pairs_if(a->dx, a->dx_at, a->type, kScanOut) | pairs_if(a->dgate, a->dgate_at, a->gate_type, kScanOutGate);
+    if (!mixes) p.whole |= kScanX;                           // not looked at
+    if (!a->dh) p.whole |= kScanDh;
     return launch(p, a->type, a->gate_type, true, a->batch, (cudaStream_t)stream);
 }
 

@@ -71,6 +71,14 @@ __device__ __forceinline__ ScanPiece<T, V> scan_piece(const char *p)
     else r.v[0] = *reinterpret_cast<const T *>(p);
     return r;
 }
+template <class T, int V>
+__device__ __forceinline__ void scan_store(char *row, unsigned offset, const ScanPiece<T, V> &r)
+{
+    char *p = row + offset;
+    if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(&r);
+    else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(&r);
+    else *reinterpret_cast<T *>(p) = r.v[0];
+}
 // A lane's channels of a row, which is found by a base that is the same for the whole warp and the lane's offset.  count: of
 // the channels that there are; whole: they can move together.
 template <class T, int V>
@@ -110,6 +118,15 @@ struct ScanCopy {
         const int at = lane % kRowPieces * 16;
         bytes = min(16, channels * (int)sizeof(T) - at);
         place = row * W * (int)sizeof(T) + at, offset = row * stride + at;
+    }
+    // All rows and all channels of the tile are there, and whole.
+    __device__ __forceinline__ void issue_all(char *to, const char *base, long long stride) const
+    {
+        const unsigned at = (unsigned)__cvta_generic_to_shared(to) + place;
+        const char *from = base + offset;
+#pragma unroll
+        for (int j = 0; j < kTurns; ++j)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + j * 512), "l"(from + j * kRows * stride) : "memory");
     }
     template <class Valid>
     __device__ __forceinline__ void issue(char *to, const char *base, long long stride, Valid valid) const
@@ -322,13 +339,14 @@ template <class U>
 struct ScanShared {
     ScanMap<U> *warp_maps, *cta_maps;                    // of every warp's segment, and of every CTA's segments
     U *carry;                                            // what comes into the round
+    unsigned long long *bars;                            // of the maps that the cluster's CTAs send
     int *warp_drops, *cta_drops;                         // a reset lies in them: nothing comes through
     int warps, ctas;
 
     static __host__ __device__ size_t bytes(int warps, int ctas)
     {
         if (warps * ctas == 1) return 0;
-        return 2 * ((warps + ctas) * 32 * sizeof(ScanMap<U>) + 32 * sizeof(U) + (kScanMostCluster + kScanMostWarps) * sizeof(int));
+        return 2 * ((warps + ctas) * 32 * sizeof(ScanMap<U>) + 32 * sizeof(U) + (kScanMostCluster + kScanMostWarps) * sizeof(int) + sizeof(unsigned long long));
     }
     __device__ __forceinline__ ScanShared(void *at, int w, int c) : warps(w), ctas(c)
     {
@@ -336,9 +354,11 @@ struct ScanShared {
         carry = reinterpret_cast<U *>(static_cast<ScanMap<U> *>(at) + 2 * (w + c) * 32) + (threadIdx.x & 31);
         cta_drops = reinterpret_cast<int *>(reinterpret_cast<U *>(static_cast<ScanMap<U> *>(at) + 2 * (w + c) * 32) + 2 * 32);
         warp_drops = cta_drops + 2 * kScanMostCluster;
+        bars = reinterpret_cast<unsigned long long *>(warp_drops + 2 * kScanMostWarps);
     }
     __device__ __forceinline__ ScanMap<U> *warp(int parity) const { return warp_maps + parity * warps * 32; }
     __device__ __forceinline__ ScanMap<U> *cta(int parity) const { return cta_maps + parity * ctas * 32; }
+    __device__ __forceinline__ unsigned bar(int parity) const { return (unsigned)__cvta_generic_to_shared(bars + parity); }
 };
 
 template <class U>
@@ -346,19 +366,48 @@ __device__ __forceinline__ U scan_apply(const ScanMap<U> &m, int drops, U c)
 {
     return drops ? m.h : fused_ma(m.a, c, m.h);
 }
+// To another CTA of the cluster, which counts the bytes that have come at its barrier `bar`.  A barrier of the cluster in every
+// round would have each thread wait until all that it has stored has arrived, the results among it (7 us a round).
 template <class U>
-__device__ __forceinline__ void scan_push(unsigned to, const ScanMap<U> &m)
+__device__ __forceinline__ void scan_push(unsigned to, unsigned bar, const ScanMap<U> &m)
 {
+    static_assert(sizeof(m) == 16, "a map is 16 bytes");
     const uint32_t *w = reinterpret_cast<const uint32_t *>(&m);
-    if constexpr (sizeof(m) == 8) asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(to), "r"(w[0]), "r"(w[1]) : "memory");
-    else asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to), "r"(w[0]), "r"(w[1]),
+                 "r"(w[2]), "r"(w[3]), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void scan_push(unsigned to, unsigned bar, int v)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void scan_expect(unsigned bar, unsigned bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// False if what is waited for has not come after very many polls: then the results are NaN.
+__device__ __forceinline__ bool scan_await(unsigned bar, unsigned phase)
+{
+    for (unsigned i = 0; i < (1u << 22); ++i) {
+        unsigned ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(phase)
+            : "memory");
+        if (ok) return true;
+    }
+    return false;
 }
 // `c` through maps [from, to), where any of them drops what comes (DROPS) by their marks.
 template <bool DROPS, class U>
 __device__ __forceinline__ U scan_through(const ScanMap<U> *maps, const int *drops, int from, int to, U c)
 {
-#pragma unroll 4
-    for (int k = from; k < to; ++k) c = scan_apply(maps[k * 32], DROPS ? drops[k] : 0, c);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (k >= from && k < to) c = scan_apply(maps[k * 32], DROPS ? drops[k] : 0, c);
     return c;
 }
 
@@ -368,7 +417,15 @@ __device__ __forceinline__ void scan_begin(const ScanShared<U> &sh, int warp, U 
 {
     if (sh.warps * sh.ctas == 1) return;
     if (warp == sh.warps - 1) sh.carry[0] = carry;
+    if (sh.ctas == 1) return;
     if (threadIdx.x < 2 * kScanMostCluster) sh.cta_drops[threadIdx.x] = 0;
+    if (threadIdx.x < 2) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(sh.bar(threadIdx.x)) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();                                     // and every CTA has started
+    scan_arrive();
+    scan_wait();
 }
 template <bool DROPS, class A, class U>
 __device__ __forceinline__ U scan_joined(const ScanShared<U> &sh, int parity, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own, int drops)
@@ -391,20 +448,25 @@ __device__ __forceinline__ U scan_joined(const ScanShared<U> &sh, int parity, un
 
 // Every warp gives its segment's map (and whether it drops what comes in); returns what comes into the segment.  `carry` is
 // what comes into the round and what leaves it where a warp is alone; otherwise the last warp of each CTA writes what leaves the round
-// for the next one, whose barrier lies between.  One barrier, a second one of the cluster.
+// for the next one, whose barrier lies between.  turn: the round's number.
 template <class A, class U>
-__device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int parity, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own,
-                                       int drops, U &carry)
+__device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int turn, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own,
+                                       bool resets, int drops, U &carry)
 {
-    const int lane = threadIdx.x & 31, warps = sh.warps;
+    const int lane = threadIdx.x & 31, warps = sh.warps, parity = turn & 1;
     if (warps == 1 && cluster == 1) {
         const U in = carry;
         carry = scan_apply(own, drops, carry);
         return in;
     }
     sh.warp(parity)[warp * 32] = own;
-    if (lane == 0) sh.warp_drops[parity * kScanMostWarps + warp] = drops;
-    int any = __syncthreads_or(drops);
+    int any = 0;
+    if (resets) {
+        if (lane == 0) sh.warp_drops[parity * kScanMostWarps + warp] = drops;
+        any = __syncthreads_or(drops);
+    } else {
+        __syncthreads();
+    }
     if (cluster > 1) {
         if (warp == warps - 1) {
             const ScanMap<U> *const maps = sh.warp(parity);
@@ -416,18 +478,24 @@ __device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int parity, unsi
                 m.h = scan_apply(s, any ? marks[w] : 0, m.h);
                 m.a = m.a * s.a;
             }
+            if (lane == 0) scan_expect(sh.bar(parity), cluster * (32 * sizeof(ScanMap<U>) + (resets ? sizeof(int) : 0)));
             for (unsigned k = 0; k < cluster; ++k) {
-                scan_push(scan_peer(sh.cta(parity) + rank * 32, k), m);
-                if (lane == 0)
-                    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(scan_peer(sh.cta_drops + parity * kScanMostCluster + rank, k)), "r"(any) : "memory");
+                const unsigned bar = scan_peer(sh.bars + parity, k);
+                scan_push(scan_peer(sh.cta(parity) + rank * 32, k), bar, m);
+                if (resets && lane == 0) scan_push(scan_peer(sh.cta_drops + parity * kScanMostCluster + rank, k), bar, any);
             }
         }
         __syncwarp();
-        scan_arrive();
-        scan_wait();
-        const int4 *const q = reinterpret_cast<const int4 *>(sh.cta_drops + parity * kScanMostCluster);
-        const int4 d = q[0], e = q[1];
-        any = d.x | d.y | d.z | d.w | e.x | e.y | e.z | e.w;
+        if (!scan_await(sh.bar(parity), (turn >> 1) & 1)) {
+            const U lost = scan_all<U>(A(NAN));
+            if (warp == warps - 1) sh.carry[(parity ^ 1) * 32] = lost;
+            return lost;
+        }
+        if (resets) {
+            const int4 *const q = reinterpret_cast<const int4 *>(sh.cta_drops + parity * kScanMostCluster);
+            const int4 d = q[0], e = q[1];
+            any = d.x | d.y | d.z | d.w | e.x | e.y | e.z | e.w;
+        }
     }
     return any ? scan_joined<true, A>(sh, parity, rank, cluster, warp, own, drops) : scan_joined<false, A>(sh, parity, rank, cluster, warp, own, drops);
 }
@@ -515,29 +583,31 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
     char *h = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + t0 * hs;
     const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, (int)p.channels - at.first, xs);
     const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, (int)p.channels - at.first, gs);
-    const bool pairs = p.whole & kScanOut;
+    // easy: of everything whole pieces, and the tile's channels are all there
+    const bool pairs = p.whole & kScanOut, easy = (p.whole & 19) == 19 && at.first + 32 * V <= p.channels;
+    const long long x_round = round * xs, gate_round = round * gs, h_round = round * hs;
     const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kForward;
-        const auto valid = [&](int r) { return ahead + r < end; };
-        copy_x.issue(to, x, xs, valid);
-        copy_gate.issue(to + copy_x.kBytes, gate, gs, valid);
+        if (easy && ahead + S <= end) {
+            copy_x.issue_all(to, x, xs);
+            copy_gate.issue_all(to + copy_x.kBytes, gate, gs);
+        } else {
+            const auto valid = [&](int r) { return ahead + r < end; };
+            copy_x.issue(to, x, xs, valid);
+            copy_gate.issue(to + copy_x.kBytes, gate, gs, valid);
+        }
         scan_issued();
-        ahead += round, x += round * xs, gate += round * gs, in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
+        ahead += round, x += x_round, gate += gate_round, in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
     for (int k = 0; k < Ring::kStages - 1; ++k) issue();
     U carry = scan_state<U, A, V>(p.state, at.state, at.count);
     scan_begin(sh, at.warp, carry);
-    if (at.cluster > 1) {
-        __syncthreads();                                 // every CTA has started, and the marks are cleared
-        scan_arrive();
-        scan_wait();
-    }
     auto marks = [&](int t) -> unsigned char { return reset && at.lane < S && t + at.lane < end ? reset[(t + at.lane) * p.reset_at.token] : 0; };
     unsigned char mark = marks(t0);
-    int parity = 0;
-    for (int first = 0; first < p.tokens; first += round, parity ^= 1) {
+    int turn = 0;
+    for (int first = 0; first < p.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
@@ -567,12 +637,12 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
 #pragma unroll
             for (int s = 1; s < S; ++s) own.h = (drops >> s) & 1u ? m[s] : fused_ma(a[s], own.h, m[s]), own.a = own.a * a[s];
         }
-        U in = scan_join<A>(sh, parity, at.rank, at.cluster, at.warp, own, drops != 0, carry);
-        if (full && drops == 0) {
+        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry);
+        if (easy && full && drops == 0) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 in = fused_ma(a[s], in, m[s]);
-                scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(in), at.count, pairs);
+                scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(in));
             }
         } else {
 #pragma unroll
@@ -581,9 +651,9 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
                 if (t0 + s < p.tokens) scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(t0 + s < end ? in : scan_all<U>(A(0))), at.count, pairs);
             }
         }
-        t0 += round, h += round * hs;
+        t0 += round, h += h_round;
     }
-    carry = scan_left(sh, parity, carry);
+    carry = scan_left(sh, turn & 1, carry);
     if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
@@ -618,36 +688,41 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, channels, gs);
     const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, channels, xs), copy_dh(p.whole & kScanDh, at.lane, channels, ds),
         copy_h(p.whole & kScanH, at.lane, channels, hs);
-    const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate;
+    // easy: of everything whole pieces, and the tile's channels are all there
+    const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate, easy = p.whole == 63 && at.first + 32 * V <= p.channels;
+    const long long x_round = round * xs, dh_round = round * ds, h_round = round * hs, gate_round = round * gs, dx_round = round * dxs,
+                    dgate_round = round * dgs;
     const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
     const bool with_x = p.mode % 3 != FO_MIX_ONE, with_dh = p.dh != nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kBackward;
-        const auto valid = [&](int r) { return ahead - r >= 0 && ahead - r < end; };
-        if (with_dh) copy_dh.issue(to, dh, ds, valid);
-        if (with_x) copy_x.issue(to + kPart, x, xs, valid);
-        copy_h.issue(to + 2 * kPart, hin, hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
-        copy_gate.issue(to + 3 * kPart, gate, gs, valid);
+        if (easy && ahead < end && ahead >= S) {
+            if (with_dh) copy_dh.issue_all(to, dh, ds);
+            if (with_x) copy_x.issue_all(to + kPart, x, xs);
+            copy_h.issue_all(to + 2 * kPart, hin, hs);
+            copy_gate.issue_all(to + 3 * kPart, gate, gs);
+        } else {
+            const auto valid = [&](int r) { return ahead - r >= 0 && ahead - r < end; };
+            if (with_dh) copy_dh.issue(to, dh, ds, valid);
+            if (with_x) copy_x.issue(to + kPart, x, xs, valid);
+            copy_h.issue(to + 2 * kPart, hin, hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
+            copy_gate.issue(to + 3 * kPart, gate, gs, valid);
+        }
         scan_issued();
-        ahead -= round, x += round * xs, dh += round * ds, hin += round * hs, gate += round * gs;
+        ahead -= round, x += x_round, dh += dh_round, hin += h_round, gate += gate_round;
         in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
     for (int k = 0; k < Ring::kStages - 1; ++k) issue();
     U carry = scan_state<U, A, V>(p.dlast, at.state, at.count);
     const U start = scan_state<U, A, V>(p.state, at.state, at.count), none = scan_all<U>(A(0));
     scan_begin(sh, at.warp, carry);
-    if (at.cluster > 1) {
-        __syncthreads();                                 // every CTA has started, and the marks are cleared
-        scan_arrive();
-        scan_wait();
-    }
     auto marks = [&](int t) -> unsigned char {
         return reset && at.lane < S && t - at.lane >= 0 && t - at.lane < end ? reset[(t - at.lane) * p.reset_at.token] : 0;
     };
     unsigned char mark = marks(t0);
-    int parity = 0;
-    for (int first = 0; first < p.tokens; first += round, parity ^= 1) {
+    int turn = 0;
+    for (int first = 0; first < p.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
@@ -674,7 +749,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
             for (int s = 0; s < S; ++s)
                 if (t0 - s >= 0 && t0 - s < end) own.h = (drops >> s) & 1u ? none : a[s] * (d_of(s) + own.h), own.a = own.a * a[s];
         }
-        U in = scan_join<A>(sh, parity, at.rank, at.cluster, at.warp, own, drops != 0, carry);
+        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry);
         auto finish = [&](auto decay, auto mix, auto masked) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -695,18 +770,21 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
                     const bool live = t0 - s >= 0 && t0 - s < end;
                     if (!live) to_x = none, to_g = none, through = in;
                 }
-                if (!masked.value || t0 - s >= 0) {
+                if constexpr (!masked.value) {
+                    scan_store<T, V>(dx + s * dxs, xo, scan_narrow<T, V>(to_x));
+                    scan_store<G, V>(dgate + s * dgs, go, scan_narrow<G, V>(to_g));
+                } else if (t0 - s >= 0) {
                     scan_store<T, V>(dx + s * dxs, xo, scan_narrow<T, V>(to_x), at.count, pairs);
                     scan_store<G, V>(dgate + s * dgs, go, scan_narrow<G, V>(to_g), at.count, gate_pairs);
                 }
                 in = through;
             }
         };
-        if (plain) with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::false_type()); });
+        if (plain && easy) with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::false_type()); });
         else with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::true_type()); });
-        t0 -= round, dx += round * dxs, dgate += round * dgs;
+        t0 -= round, dx += dx_round, dgate += dgate_round;
     }
-    carry = scan_left(sh, parity, carry);
+    carry = scan_left(sh, turn & 1, carry);
     if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
