@@ -52,6 +52,13 @@ bool rows_at(const void *p, const fo_rows &s, int type, int bytes)
     return (((uintptr_t)p | (unsigned long long)(s.batch | s.token) * (unsigned)elem_bytes(type)) & (unsigned)(bytes - 1)) == 0;
 }
 int whole_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 16) ? bit : 0; }
+// S = 8 rows of every tensor lie within 2^30 bytes, and so do their channels.
+int near_if(std::initializer_list<fo_rows> strides, long long channels)
+{
+    for (const fo_rows &s : strides)
+        if (s.token > (1LL << 30) / (8 * 8)) return 0;
+    return channels <= (1LL << 27) ? kScanNear : 0;
+}
 int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 2 * elem_bytes(type)) ? bit : 0; }
 
 int launch(const ScanParams &p, int type, int gate_type, bool grad, long long batch, cudaStream_t st)
@@ -89,7 +96,7 @@ int fused_scan(const fo_scan *a, void *stream)
     p.h = a->h, p.last = a->last;
     p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->h_at;
     p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
-              | pairs_if(a->h, a->h_at, a->type, kScanOut);
+              | pairs_if(a->h, a->h_at, a->type, kScanOut) | near_if({a->x_at, a->gate_at, a->h_at}, a->channels);
     return launch(p, a->type, a->gate_type, false, a->batch, (cudaStream_t)stream);
 }
 
@@ -115,7 +122,8 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
     p.dh_at = a->dh_at, p.h_in_at = a->h_at, p.dgate_at = a->dgate_at;
     p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
               | whole_if(a->dh, a->dh_at, a->type, kScanDh) | whole_if(a->h, a->h_at, a->type, kScanH)
-              | pairs_if(a->dx, a->dx_at, a->type, kScanOut) | pairs_if(a->dgate, a->dgate_at, a->gate_type, kScanOutGate);
+              | pairs_if(a->dx, a->dx_at, a->type, kScanOut) | pairs_if(a->dgate, a->dgate_at, a->gate_type, kScanOutGate)
+              | near_if({a->x_at, a->gate_at, a->dh_at, a->h_at, a->dx_at, a->dgate_at}, a->channels);
     if (!mixes) p.whole |= kScanX;                           // not looked at
     if (!a->dh) p.whole |= kScanDh;
     return launch(p, a->type, a->gate_type, true, a->batch, (cudaStream_t)stream);

@@ -18,13 +18,14 @@ constexpr int kScanCta = 256;
 constexpr int kScanMostWarps = kScanCta / 32;
 constexpr int kScanMostCluster = 8;
 
-enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32 };
+enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32, kScanNear = 64, kScanAll = 127 };
 
 struct ScanParams {
     long long channels;
     int tokens, tiles;                  // tiles: of 32 V channels
     int mode, long_lengths;             // mode: decay * 3 + mix
-    int whole;                          // which tensors' rows begin at 16-byte boundaries (ScanTensor); of outputs, at those of two channels
+    int whole;                          // which tensors' rows begin at 16-byte boundaries (ScanTensor), outputs' at those of two channels; near:
+                                        // the rows of a segment lie within 32 bits of each other
     const void *x, *gate, *state, *lengths;
     const unsigned char *reset;
     void *h, *last;                     // gradient: dx, dstate
@@ -109,24 +110,27 @@ struct ScanCopy {
     static constexpr int kBytes = S * W * (int)sizeof(T);
     static constexpr int kRowPieces = W * (int)sizeof(T) / 16, kRows = 32 / kRowPieces, kTurns = S / kRows;
     int row, bytes, channels;
-    unsigned place;
-    long long offset;
+    unsigned place, from[kTurns];       // from: offsets from the segment's lowest row in memory
     bool whole;
     __device__ __forceinline__ ScanCopy(bool whole_, int lane, int channels_, long long stride) : channels(channels_), whole(whole_)
     {
         row = lane / kRowPieces;
         const int at = lane % kRowPieces * 16;
         bytes = min(16, channels * (int)sizeof(T) - at);
-        place = row * W * (int)sizeof(T) + at, offset = row * stride + at;
+        place = row * W * (int)sizeof(T) + at;
+#pragma unroll
+        for (int j = 0; j < kTurns; ++j) {
+            const int r = row + j * kRows;
+            from[j] = (unsigned)((stride < 0 ? (S - 1 - r) * -stride : r * stride) + at);
+        }
     }
-    // All rows and all channels of the tile are there, and whole.
-    __device__ __forceinline__ void issue_all(char *to, const char *base, long long stride) const
+    // All rows and all channels of the tile are there, and whole, and within 32 bits of `lowest`.
+    __device__ __forceinline__ void issue_all(char *to, const char *lowest) const
     {
         const unsigned at = (unsigned)__cvta_generic_to_shared(to) + place;
-        const char *from = base + offset;
 #pragma unroll
         for (int j = 0; j < kTurns; ++j)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + j * 512), "l"(from + j * kRows * stride) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + j * 512), "l"(lowest + from[j]) : "memory");
     }
     template <class Valid>
     __device__ __forceinline__ void issue(char *to, const char *base, long long stride, Valid valid) const
@@ -136,7 +140,7 @@ struct ScanCopy {
             for (int j = 0; j < kTurns; ++j)
                 if (valid(row + j * kRows) && bytes > 0)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((unsigned)__cvta_generic_to_shared(to) + place + j * 512),
-                                 "l"(base + j * kRows * stride + offset), "r"(bytes) : "memory");
+                                 "l"(base + (row + j * kRows) * stride + (place - row * W * (int)sizeof(T))), "r"(bytes) : "memory");
             return;
         }
         const int lane = threadIdx.x & 31;
@@ -260,12 +264,18 @@ __device__ __forceinline__ void scan_exponential(double g, double &a, double &re
     rest = -expm1(g);
     a = g > -0.5 ? 1.0 - rest : exp(g);
 }
-template <int DECAY, bool EXACT, class A, class U>
+// SLOPES: a product of a and rest is wanted, to which a small a counts by its own size; otherwise by that of what it multiplies.
+template <int DECAY, bool EXACT, bool SLOPES, class A, class U>
 __device__ __forceinline__ void scan_decay(U g, U &a, U &rest)
 {
     const U one = scan_all<U>(A(1)), less = scan_all<U>(A(-1));
     if constexpr (DECAY == FO_DECAY_VALUE) {
         a = g, rest = fused_ma(g, less, one);
+    } else if constexpr (DECAY == FO_DECAY_SIGMOID && !EXACT && !SLOPES) {
+        // 1 / (1 + exp(g)) is right to a few 2^-23 of itself; a, 1 minus that, to one rounding of 1
+        rest = scan_each(scan_each(g * scan_all<U>(A(1.4426950408889634)), [](A v) { return scan_exp2(v); }) + one,
+                         [](A v) { return scan_over<EXACT>(v); });
+        a = fused_ma(rest, less, one);
     } else if constexpr (DECAY == FO_DECAY_SIGMOID) {
         const U e = scan_each(g, [](A v) { return scan_exp_down<EXACT>(v); });
         const U small = e * scan_each(e + one, [](A v) { return scan_over<EXACT>(v); }), big = fused_ma(small, less, one);
@@ -392,7 +402,7 @@ __device__ __forceinline__ bool scan_await(unsigned bar, unsigned phase)
         unsigned ok;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
             "selp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(ok)
             : "r"(bar), "r"(phase)
@@ -577,22 +587,23 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
     const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
     int t0 = (at.rank * at.warps + at.warp) * S;
     const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), hs = p.h_at.token * (int)sizeof(T);
-    const unsigned ho = at.channel * (unsigned)sizeof(T);
+    const unsigned ho = at.channel * (unsigned)sizeof(T), hs_near = (unsigned)hs;
     const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + t0 * xs;
     const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + t0 * gs;
     char *h = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + t0 * hs;
     const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, (int)p.channels - at.first, xs);
     const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, (int)p.channels - at.first, gs);
-    // easy: of everything whole pieces, and the tile's channels are all there
-    const bool pairs = p.whole & kScanOut, easy = (p.whole & 19) == 19 && at.first + 32 * V <= p.channels;
+    // easy: everything is in whole pieces and near, and the tile's channels are all there
+    constexpr int kEasy = kScanX | kScanGate | kScanOut | kScanNear;
+    const bool pairs = p.whole & kScanOut, easy = (p.whole & kEasy) == kEasy && at.first + 32 * V <= p.channels;
     const long long x_round = round * xs, gate_round = round * gs, h_round = round * hs;
     const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kForward;
         if (easy && ahead + S <= end) {
-            copy_x.issue_all(to, x, xs);
-            copy_gate.issue_all(to + copy_x.kBytes, gate, gs);
+            copy_x.issue_all(to, x);
+            copy_gate.issue_all(to + copy_x.kBytes, gate);
         } else {
             const auto valid = [&](int r) { return ahead + r < end; };
             copy_x.issue(to, x, xs, valid);
@@ -619,8 +630,10 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 U rest;
-                scan_decay<decay.value, EXACT, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * 32 * V * (int)sizeof(G))), a[s], rest);
-                m[s] = scan_mix<mix.value, EXACT, A>(a[s], rest) * scan_widen<U>(scan_piece<T, V>(from + s * 32 * V * (int)sizeof(T)));
+                scan_decay<decay.value, EXACT, false, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * 32 * V * (int)sizeof(G))), a[s], rest);
+                const U v = scan_widen<U>(scan_piece<T, V>(from + s * 32 * V * (int)sizeof(T)));
+                if constexpr (mix.value == FO_MIX_ONE) m[s] = v;
+                else m[s] = scan_mix<mix.value, EXACT, A>(a[s], rest) * v;
             }
         });
         mark = marks(t0 + round);
@@ -642,7 +655,7 @@ __global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 in = fused_ma(a[s], in, m[s]);
-                scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(in));
+                scan_store<T, V>(h, ho + s * hs_near, scan_narrow<T, V>(in));
             }
         } else {
 #pragma unroll
@@ -675,21 +688,23 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
     // element s of a segment is token t0 - s
     int t0 = p.tokens - 1 - (int)(at.rank * at.warps + at.warp) * S;
-    const long long xs = -p.x_at.token * (int)sizeof(T), gs = -p.gate_at.token * (int)sizeof(G), ds = -p.dh_at.token * (int)sizeof(T),
-                    hs = -p.h_in_at.token * (int)sizeof(T), dxs = -p.h_at.token * (int)sizeof(T), dgs = -p.dgate_at.token * (int)sizeof(G);
-    const unsigned xo = at.channel * (unsigned)sizeof(T), go = at.channel * (unsigned)sizeof(G);
-    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) - t0 * xs;
-    const char *dh = static_cast<const char *>(p.dh) + (at.b * p.dh_at.batch + at.first) * (int)sizeof(T) - t0 * ds;
-    const char *hin = static_cast<const char *>(p.h_in) + (at.b * p.h_in_at.batch + at.first) * (int)sizeof(T) - (t0 - 1) * hs;   // of the token before
-    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) - t0 * gs;
-    char *dx = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) - t0 * dxs;
-    char *dgate = static_cast<char *>(p.dgate) + at.b * p.dgate_at.batch * (int)sizeof(G) - t0 * dgs;
+    const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), ds = p.dh_at.token * (int)sizeof(T),
+                    hs = p.h_in_at.token * (int)sizeof(T), dxs = p.h_at.token * (int)sizeof(T), dgs = p.dgate_at.token * (int)sizeof(G);
+    const unsigned xo = at.channel * (unsigned)sizeof(T), go = at.channel * (unsigned)sizeof(G), dxs_near = (unsigned)dxs, dgs_near = (unsigned)dgs;
+    // pointers are to the segment's last element, the lowest in memory
+    const int lowest = t0 - (S - 1);
+    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + lowest * xs;
+    const char *dh = static_cast<const char *>(p.dh) + (at.b * p.dh_at.batch + at.first) * (int)sizeof(T) + lowest * ds;
+    const char *hin = static_cast<const char *>(p.h_in) + (at.b * p.h_in_at.batch + at.first) * (int)sizeof(T) + (lowest - 1) * hs;  // of the token before
+    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + lowest * gs;
+    char *dx = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + lowest * dxs;
+    char *dgate = static_cast<char *>(p.dgate) + at.b * p.dgate_at.batch * (int)sizeof(G) + lowest * dgs;
     const int channels = (int)p.channels - at.first;
-    const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, channels, gs);
-    const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, channels, xs), copy_dh(p.whole & kScanDh, at.lane, channels, ds),
-        copy_h(p.whole & kScanH, at.lane, channels, hs);
-    // easy: of everything whole pieces, and the tile's channels are all there
-    const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate, easy = p.whole == 63 && at.first + 32 * V <= p.channels;
+    const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, channels, -gs);
+    const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, channels, -xs), copy_dh(p.whole & kScanDh, at.lane, channels, -ds),
+        copy_h(p.whole & kScanH, at.lane, channels, -hs);
+    // easy: everything is in whole pieces and near, and the tile's channels are all there
+    const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate, easy = p.whole == kScanAll && at.first + 32 * V <= p.channels;
     const long long x_round = round * xs, dh_round = round * ds, h_round = round * hs, gate_round = round * gs, dx_round = round * dxs,
                     dgate_round = round * dgs;
     const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
@@ -698,19 +713,19 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kBackward;
         if (easy && ahead < end && ahead >= S) {
-            if (with_dh) copy_dh.issue_all(to, dh, ds);
-            if (with_x) copy_x.issue_all(to + kPart, x, xs);
-            copy_h.issue_all(to + 2 * kPart, hin, hs);
-            copy_gate.issue_all(to + 3 * kPart, gate, gs);
+            if (with_dh) copy_dh.issue_all(to, dh);
+            if (with_x) copy_x.issue_all(to + kPart, x);
+            copy_h.issue_all(to + 2 * kPart, hin);
+            copy_gate.issue_all(to + 3 * kPart, gate);
         } else {
             const auto valid = [&](int r) { return ahead - r >= 0 && ahead - r < end; };
-            if (with_dh) copy_dh.issue(to, dh, ds, valid);
-            if (with_x) copy_x.issue(to + kPart, x, xs, valid);
-            copy_h.issue(to + 2 * kPart, hin, hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
-            copy_gate.issue(to + 3 * kPart, gate, gs, valid);
+            if (with_dh) copy_dh.issue(to, dh + (S - 1) * ds, -ds, valid);
+            if (with_x) copy_x.issue(to + kPart, x + (S - 1) * xs, -xs, valid);
+            copy_h.issue(to + 2 * kPart, hin + (S - 1) * hs, -hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
+            copy_gate.issue(to + 3 * kPart, gate + (S - 1) * gs, -gs, valid);
         }
         scan_issued();
-        ahead -= round, x += x_round, dh += dh_round, hin += h_round, gate += gate_round;
+        ahead -= round, x -= x_round, dh -= dh_round, hin -= h_round, gate -= gate_round;
         in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
     for (int k = 0; k < Ring::kStages - 1; ++k) issue();
@@ -735,7 +750,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
         U a[S], rest[S];
         with_decay(p.mode, [&](auto decay) {
 #pragma unroll
-            for (int s = 0; s < S; ++s) scan_decay<decay.value, EXACT, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * kGateRow)), a[s], rest[s]);
+            for (int s = 0; s < S; ++s) scan_decay<decay.value, EXACT, true, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * kGateRow)), a[s], rest[s]);
         });
         mark = marks(t0 - round);
         // plain: all of the segment's tokens are the sequence's, and none of them its first one or drops what comes
@@ -771,18 +786,18 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
                     if (!live) to_x = none, to_g = none, through = in;
                 }
                 if constexpr (!masked.value) {
-                    scan_store<T, V>(dx + s * dxs, xo, scan_narrow<T, V>(to_x));
-                    scan_store<G, V>(dgate + s * dgs, go, scan_narrow<G, V>(to_g));
+                    scan_store<T, V>(dx, xo + (S - 1 - s) * dxs_near, scan_narrow<T, V>(to_x));
+                    scan_store<G, V>(dgate, go + (S - 1 - s) * dgs_near, scan_narrow<G, V>(to_g));
                 } else if (t0 - s >= 0) {
-                    scan_store<T, V>(dx + s * dxs, xo, scan_narrow<T, V>(to_x), at.count, pairs);
-                    scan_store<G, V>(dgate + s * dgs, go, scan_narrow<G, V>(to_g), at.count, gate_pairs);
+                    scan_store<T, V>(dx + (S - 1 - s) * dxs, xo, scan_narrow<T, V>(to_x), at.count, pairs);
+                    scan_store<G, V>(dgate + (S - 1 - s) * dgs, go, scan_narrow<G, V>(to_g), at.count, gate_pairs);
                 }
                 in = through;
             }
         };
         if (plain && easy) with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::false_type()); });
         else with_mode(p.mode, [&](auto decay, auto mix) { finish(decay, mix, std::true_type()); });
-        t0 -= round, dx += dx_round, dgate += dgate_round;
+        t0 -= round, dx -= dx_round, dgate -= dgate_round;
     }
     carry = scan_left(sh, turn & 1, carry);
     if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);

@@ -1,6 +1,8 @@
 // How a recurrence is cut into CTAs and clusters, for one pair of element types.
 #pragma once
 
+#include <algorithm>
+
 #include <stdlib.h>
 #include "launch.cuh"
 #include "scan.cuh"
@@ -24,14 +26,16 @@ cudaError_t launch_scan(ScanParams p, bool grad, long long batch, cudaStream_t s
     p.tiles = (int)((p.channels + 32 * V - 1) / (32 * V));
     const long long items = p.tiles * batch;
     const int sms = sm_count();
-    const char *tw = getenv("SCAN_W") ? getenv("SCAN_W") : "", *tk = getenv("SCAN_K") ? getenv("SCAN_K") : "";
-    int warps = 1, cluster = 1;
-    const int most = tw[0] ? atoi(tw) : kScanMostWarps;
+    int warps = 1;
+    // half of the warps where the gradient's ring would leave room for one CTA on an SM
+    const int most = grad && Ring::kBackward > 4096 ? kScanMostWarps / 2 : kScanMostWarps;
     while (warps < most && warps * S < p.tokens) warps *= 2;
-    // a round of all CTAs together is to occupy the GPU, and no more than that
-    while (cluster < kScanMostCluster && items * cluster * 2 <= (long long)sms * 3 && cluster * warps * S < p.tokens) cluster *= 2;
-    if (tk[0]) cluster = atoi(tk);
-    return launch_beside(kernel, dim3((unsigned)(items * cluster)), 32 * warps, st, Ring::bytes(warps, grad) + Shared::bytes(warps, cluster), p, cluster);
+    // as many CTAs as can work at once, two on an SM, where the sequences are long enough
+    long long cluster = std::min<long long>(kScanMostCluster, 2LL * sms / items);
+    cluster = std::max<long long>(1, std::min<long long>(cluster, (p.tokens + warps * S - 1) / (warps * S)));
+    if (getenv("SCAN_W")) warps = atoi(getenv("SCAN_W"));
+    if (getenv("SCAN_K")) cluster = atoi(getenv("SCAN_K"));
+    return launch_beside(kernel, dim3((unsigned)(items * cluster)), 32 * warps, st, Ring::bytes(warps, grad) + Shared::bytes(warps, (int)cluster), p, (int)cluster);
 }
 
 }  // namespace fo
