@@ -52,11 +52,11 @@ bool rows_at(const void *p, const fo_rows &s, int type, int bytes)
     return (((uintptr_t)p | (unsigned long long)(s.batch | s.token) * (unsigned)elem_bytes(type)) & (unsigned)(bytes - 1)) == 0;
 }
 int whole_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 16) ? bit : 0; }
-// S = 8 rows of every tensor lie within 2^30 bytes, and so do their channels.
+// 16 rows of every tensor lie within 2^30 bytes, and so do their channels.
 int near_if(std::initializer_list<fo_rows> strides, long long channels)
 {
     for (const fo_rows &s : strides)
-        if (s.token > (1LL << 30) / (8 * 8)) return 0;
+        if (s.token > (1LL << 30) / (16 * 8)) return 0;
     return channels <= (1LL << 27) ? kScanNear : 0;
 }
 int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 2 * elem_bytes(type)) ? bit : 0; }

@@ -573,7 +573,7 @@ struct ScanRing {
 };
 
 template <class T, class G, int V, int S>
-__global__ void __launch_bounds__(kScanCta, sizeof(T) == 8 ? 2 : 3) scan_kernel(const __grid_constant__ ScanParams p)
+__global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant__ ScanParams p)
 {
     using A = Acc<T>;
     using U = typename ScanUnit<A, V>::U;
