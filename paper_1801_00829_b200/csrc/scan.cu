@@ -13,7 +13,7 @@ namespace fo {
     X(FO_F16, FO_F16, __half, __half)              \
     X(FO_F16, FO_F32, __half, float)
 
-#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(ScanParams, bool, long long, cudaStream_t);
+#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(ScanParams, bool, cudaStream_t);
 FO_SCAN_PAIRS(FO_EXTERN)
 #undef FO_EXTERN
 
@@ -61,11 +61,11 @@ int near_if(std::initializer_list<fo_rows> strides, long long channels)
 }
 int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 2 * elem_bytes(type)) ? bit : 0; }
 
-int launch(const ScanParams &p, int type, int gate_type, bool grad, long long batch, cudaStream_t st)
+int launch(const ScanParams &p, int type, int gate_type, bool grad, cudaStream_t st)
 {
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(t, g, T, G) \
-    if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, batch, st);
+    if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, st);
     FO_SCAN_PAIRS(FO_CASE)
 #undef FO_CASE
     return e == cudaSuccess ? FO_OK : cuda_fail(e);
@@ -90,14 +90,14 @@ int fused_scan(const fo_scan *a, void *stream)
         return FO_ERR_UNSUPPORTED;
     if (a->tokens == 0 && !a->last) return FO_OK;
     ScanParams p = {};
-    p.tokens = (int)a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.tokens = (int)a->tokens, p.channels = a->channels, p.batch = a->batch, p.mode = a->decay * 3 + a->mix;
     p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
     p.reset = static_cast<const unsigned char *>(a->reset);
     p.h = a->h, p.last = a->last;
     p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->h_at;
     p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
               | pairs_if(a->h, a->h_at, a->type, kScanOut) | near_if({a->x_at, a->gate_at, a->h_at}, a->channels);
-    return launch(p, a->type, a->gate_type, false, a->batch, (cudaStream_t)stream);
+    return launch(p, a->type, a->gate_type, false, (cudaStream_t)stream);
 }
 
 int fused_scan_grad(const fo_scan_grad *a, void *stream)
@@ -114,7 +114,7 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
         return FO_ERR_UNSUPPORTED;
     if (a->tokens == 0 && !a->dstate) return FO_OK;
     ScanParams p = {};
-    p.tokens = (int)a->tokens, p.channels = a->channels, p.mode = a->decay * 3 + a->mix;
+    p.tokens = (int)a->tokens, p.channels = a->channels, p.batch = a->batch, p.mode = a->decay * 3 + a->mix;
     p.x = a->x, p.gate = a->gate, p.state = a->state, p.lengths = a->lengths, p.long_lengths = a->lengths_type == FO_I64;
     p.reset = static_cast<const unsigned char *>(a->reset);
     p.h = a->dx, p.last = a->dstate, p.dh = a->dh, p.dlast = a->dlast, p.h_in = a->h, p.dgate = a->dgate;
@@ -126,7 +126,7 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
               | near_if({a->x_at, a->gate_at, a->dh_at, a->h_at, a->dx_at, a->dgate_at}, a->channels);
     if (!mixes) p.whole |= kScanX;                           // not looked at
     if (!a->dh) p.whole |= kScanDh;
-    return launch(p, a->type, a->gate_type, true, a->batch, (cudaStream_t)stream);
+    return launch(p, a->type, a->gate_type, true, (cudaStream_t)stream);
 }
 
 }  // extern "C"

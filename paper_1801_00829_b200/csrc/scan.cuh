@@ -21,7 +21,7 @@ constexpr int kScanMostCluster = 8;
 enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32, kScanNear = 64, kScanAll = 127 };
 
 struct ScanParams {
-    long long channels;
+    long long channels, batch;
     int tokens, tiles;                  // tiles: of 32 V channels
     int mode, long_lengths;             // mode: decay * 3 + mix
     int whole;                          // which tensors' rows begin at 16-byte boundaries (ScanTensor), outputs' at those of two channels; near:
@@ -563,13 +563,13 @@ struct ScanPlace {
     }
 };
 
-template <class T, class G, int V, int S>
+// A warp's ring: the segment that is worked on and one or two on their way, as leave two CTAs room on an SM.
+template <class T, class G, int V, int S, bool GRAD>
 struct ScanRing {
-    static constexpr int kStages = 3;
-    // of a warp in one stage
-    static constexpr int kForward = ScanCopy<T, S, 32 * V>::kBytes + ScanCopy<G, S, 32 * V>::kBytes;
-    static constexpr int kBackward = 3 * ScanCopy<T, S, 32 * V>::kBytes + ScanCopy<G, S, 32 * V>::kBytes;
-    static size_t bytes(int warps, bool grad) { return (size_t)kStages * warps * (grad ? kBackward : kForward); }
+    static constexpr int kPart = ScanCopy<T, S, 32 * V>::kBytes;
+    static constexpr int kSegment = (GRAD ? 3 : 1) * kPart + ScanCopy<G, S, 32 * V>::kBytes;
+    static constexpr int kStages = kSegment <= 4096 ? 3 : 2;
+    static constexpr int kBytes = kStages * kSegment;        // of a warp
 };
 
 template <class T, class G, int V, int S>
@@ -577,13 +577,13 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
 {
     using A = Acc<T>;
     using U = typename ScanUnit<A, V>::U;
-    using Ring = ScanRing<T, G, V, S>;
+    using Ring = ScanRing<T, G, V, S, false>;
     constexpr bool EXACT = sizeof(T) >= 4;
     extern __shared__ __align__(16) char scan_memory[];
     const ScanPlace<V> at(p);
     wait_for_earlier();
-    char *const ring = scan_memory + at.warp * Ring::kStages * Ring::kForward;
-    const ScanShared<U> sh(scan_memory + at.warps * Ring::kStages * Ring::kForward, at.warps, at.cluster);
+    char *const ring = scan_memory + at.warp * Ring::kBytes;
+    const ScanShared<U> sh(scan_memory + at.warps * Ring::kBytes, at.warps, at.cluster);
     const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
     int t0 = (at.rank * at.warps + at.warp) * S;
     const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), hs = p.h_at.token * (int)sizeof(T);
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
     const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
-        char *to = ring + in_stage * Ring::kForward;
+        char *to = ring + in_stage * Ring::kSegment;
         if (easy && ahead + S <= end) {
             copy_x.issue_all(to, x);
             copy_gate.issue_all(to + copy_x.kBytes, gate);
@@ -622,8 +622,8 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
-        const char *const from = ring + stage * Ring::kForward + at.lane * V * (int)sizeof(T);
-        const char *const from_gate = ring + stage * Ring::kForward + copy_x.kBytes + at.lane * V * (int)sizeof(G);
+        const char *const from = ring + stage * Ring::kSegment + at.lane * V * (int)sizeof(T);
+        const char *const from_gate = ring + stage * Ring::kSegment + copy_x.kBytes + at.lane * V * (int)sizeof(G);
         stage = stage + 1 == Ring::kStages ? 0 : stage + 1;
         U a[S], m[S];                                    // m becomes m(a) x
         with_mode(p.mode, [&](auto decay, auto mix) {
@@ -677,14 +677,14 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
 {
     using A = Acc<T>;
     using U = typename ScanUnit<A, V>::U;
-    using Ring = ScanRing<T, G, V, S>;
+    using Ring = ScanRing<T, G, V, S, true>;
     constexpr bool EXACT = sizeof(T) >= 4;
     constexpr int kPart = ScanCopy<T, S, 32 * V>::kBytes, kRow = 32 * V * (int)sizeof(T), kGateRow = 32 * V * (int)sizeof(G);
     extern __shared__ __align__(16) char scan_memory[];
     const ScanPlace<V> at(p);
     wait_for_earlier();
-    char *const ring = scan_memory + at.warp * Ring::kStages * Ring::kBackward;
-    const ScanShared<U> sh(scan_memory + at.warps * Ring::kStages * Ring::kBackward, at.warps, at.cluster);
+    char *const ring = scan_memory + at.warp * Ring::kBytes;
+    const ScanShared<U> sh(scan_memory + at.warps * Ring::kBytes, at.warps, at.cluster);
     const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
     // element s of a segment is token t0 - s
     int t0 = p.tokens - 1 - (int)(at.rank * at.warps + at.warp) * S;
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     const bool with_x = p.mode % 3 != FO_MIX_ONE, with_dh = p.dh != nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
-        char *to = ring + in_stage * Ring::kBackward;
+        char *to = ring + in_stage * Ring::kSegment;
         if (easy && ahead < end && ahead >= S) {
             if (with_dh) copy_dh.issue_all(to, dh);
             if (with_x) copy_x.issue_all(to + kPart, x);
@@ -741,8 +741,8 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
-        const char *const from = ring + stage * Ring::kBackward + at.lane * V * (int)sizeof(T);
-        const char *const from_gate = ring + stage * Ring::kBackward + 3 * kPart + at.lane * V * (int)sizeof(G);
+        const char *const from = ring + stage * Ring::kSegment + at.lane * V * (int)sizeof(T);
+        const char *const from_gate = ring + stage * Ring::kSegment + 3 * kPart + at.lane * V * (int)sizeof(G);
         stage = stage + 1 == Ring::kStages ? 0 : stage + 1;
         auto d_of = [&](int s) { return with_dh ? scan_widen<U>(scan_piece<T, V>(from + s * kRow)) : none; };
         auto x_of = [&](int s) { return scan_widen<U>(scan_piece<T, V>(from + kPart + s * kRow)); };
@@ -803,8 +803,52 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
+// A few tokens (a decoding step): every thread takes its channels through them, one after the other.
+template <class T, class G, int V>
+__global__ void __launch_bounds__(kScanCta) scan_step_kernel(const __grid_constant__ ScanParams p)
+{
+    using A = Acc<T>;
+    using U = typename ScanUnit<A, V>::U;
+    constexpr bool EXACT = sizeof(T) >= 4;
+    wait_for_earlier();
+    const long long per = (p.channels + V - 1) / V, at = (long long)blockIdx.x * kScanCta + threadIdx.x, b = at / per;
+    if (b >= p.batch) return;
+    const int c = (int)(at - b * per) * V, count = min(V, (int)(p.channels - c));
+    const int end = scan_length(p, b);
+    const T *x = static_cast<const T *>(p.x) + b * p.x_at.batch + c;
+    const G *gate = static_cast<const G *>(p.gate) + b * p.gate_at.batch + c;
+    T *h = static_cast<T *>(p.h) + b * p.h_at.batch + c;
+    const unsigned char *reset = p.reset ? p.reset + b * p.reset_at.batch : nullptr;
+    constexpr int kPairs = kScanX | kScanGate | kScanOut;
+    const bool whole = count == V && (p.whole & kPairs) == kPairs;
+    U state = scan_state<U, A, V>(p.state, b * p.channels + c, count);
+    for (int t = 0; t < p.tokens; ++t, x += p.x_at.token, gate += p.gate_at.token, h += p.h_at.token) {
+        U out = scan_all<U>(A(0));
+        if (t < end) {
+            ScanPiece<T, V> xv;
+            ScanPiece<G, V> gv;
+            if (whole) {
+                xv = scan_piece<T, V>(reinterpret_cast<const char *>(x)), gv = scan_piece<G, V>(reinterpret_cast<const char *>(gate));
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) xv.v[v] = x[v < count ? v : 0], gv.v[v] = gate[v < count ? v : 0];
+            }
+            const bool drop = reset && reset[t * p.reset_at.token];
+            with_mode(p.mode, [&](auto decay, auto mix) {
+                U a, rest;
+                scan_decay<decay.value, EXACT, false, A>(scan_widen<U>(gv), a, rest);
+                const U m = scan_mix<mix.value, EXACT, A>(a, rest) * scan_widen<U>(xv);
+                state = drop ? m : fused_ma(a, state, m);
+            });
+            out = state;
+        }
+        scan_store<T, V>(reinterpret_cast<char *>(h), 0, scan_narrow<T, V>(out), count, whole);
+    }
+    if (p.last) scan_keep<U, A, V>(p.last, b * p.channels + c, state, count);
+}
+
 // Host: one kernel of a pair of types; scan_*.cu instantiate it.
 template <class T, class G>
-cudaError_t launch_scan(ScanParams p, bool grad, long long batch, cudaStream_t st);
+cudaError_t launch_scan(ScanParams p, bool grad, cudaStream_t st);
 
 }  // namespace fo
