@@ -12,9 +12,6 @@
 
 namespace fo {
 
-#ifndef HM
-#define HM 2
-#endif
 constexpr int kHeadCta = 256;
 constexpr int kHeadWarps = kHeadCta / 32;
 
@@ -210,6 +207,11 @@ struct HeadWork {
         }
     }
 
+    static __device__ __forceinline__ A part(U v, int k)
+    {
+        if constexpr (V == 1) return v;
+        else return k ? second(v) : first(v);
+    }
     static __device__ __forceinline__ A sum(U v, int lanes)
     {
         A s = joined(v);
@@ -315,11 +317,17 @@ struct HeadRing {
     static constexpr int kPieces = 2 * I * TENSORS;
     static constexpr size_t kBytes = RING ? (size_t)kTurns * kPieces * kHeadCta * sizeof(Piece) : 0;
     Piece held[RING ? 1 : TENSORS][RING ? 1 : 2 * I];
-    Piece *ring;
-    int in = 0, out = 0;                // turns modulo kTurns
+    unsigned in, out, base;             // places of the next turn to come and to take, in bytes
+    const Piece *memory;
+    static constexpr unsigned kTurn = kPieces * kHeadCta * sizeof(Piece);
 
-    __device__ __forceinline__ explicit HeadRing(void *memory) : ring(static_cast<Piece *>(memory) + threadIdx.x) {}
+    __device__ __forceinline__ explicit HeadRing(void *m) : memory(static_cast<const Piece *>(m))
+    {
+        base = (unsigned)__cvta_generic_to_shared(m) + threadIdx.x * (unsigned)sizeof(Piece);
+        in = out = 0;
+    }
 
+    // row[n]: the lane's vector of tensor n, or NULL for zeros
     template <class Items>
     __device__ __forceinline__ void issue(const T *const (&row)[TENSORS], const Items &at, bool on)
     {
@@ -328,23 +336,19 @@ struct HeadRing {
 #pragma unroll
             for (int k = 0; k < 2 * I; ++k) {
                 const int e = k & 1 ? at.b[k / 2] : at.a[k / 2];
-                const bool there = on && row[n] && e >= 0;
                 if constexpr (RING) {
-                    Piece *to = ring + (in * kPieces + n * 2 * I + k) * kHeadCta;
-                    if (there) {
-                        const unsigned s = (unsigned)__cvta_generic_to_shared(to);
-                        if constexpr (sizeof(Piece) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(row[n] + e) : "memory");
-                        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(s), "l"(row[n] + e) : "memory");
-                    } else {
-                        *to = Piece{};
-                    }
+                    // with nothing to copy the place becomes zeros
+                    const unsigned to = base + in + (n * 2 * I + k) * (unsigned)(kHeadCta * sizeof(Piece)), bytes = on && row[n] && e >= 0 ? sizeof(Piece) : 0;
+                    const T *from = row[n] + (e >= 0 ? e : 0);
+                    if constexpr (sizeof(Piece) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+                    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
                 } else {
-                    held[n][k] = there ? head_load<T, V>(row[n] + e) : Piece{};
+                    held[n][k] = on && row[n] && e >= 0 ? head_load<T, V>(row[n] + e) : Piece{};
                 }
             }
         if constexpr (RING) {
             asm volatile("cp.async.commit_group;" ::: "memory");
-            in = in + 1 == kTurns ? 0 : in + 1;
+            in = in == (kTurns - 1) * kTurn ? 0 : in + kTurn;
         }
     }
     // Before a turn's take(): what it takes has arrived.
@@ -354,12 +358,19 @@ struct HeadRing {
     }
     __device__ __forceinline__ Piece take(int n, int k) const
     {
-        if constexpr (RING) return head_load<T, V>(reinterpret_cast<const T *>(ring + (out * kPieces + n * 2 * I + k) * kHeadCta));
-        else return held[n][k];
+        if constexpr (RING) {
+            Piece r;
+            uint32_t *w = reinterpret_cast<uint32_t *>(&r);
+            const unsigned from = base + out + (n * 2 * I + k) * (unsigned)(kHeadCta * sizeof(Piece));
+            if constexpr (sizeof(Piece) == 16)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from) : "memory");
+            else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from) : "memory");
+            return r;
+        } else return held[n][k];
     }
     __device__ __forceinline__ void taken()
     {
-        if constexpr (RING) out = out + 1 == kTurns ? 0 : out + 1;
+        if constexpr (RING) out = out == (kTurns - 1) * kTurn ? 0 : out + kTurn;
     }
 };
 
@@ -390,16 +401,23 @@ struct HeadTurns {
         return true;
     }
 };
+// A lane's way through a tensor along its warp's turns: the vector of its group's head.
 template <class T>
-__device__ __forceinline__ const T *head_row(const HeadParams &p, const void *x, const fo_strides &s, unsigned token)
-{
-    const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
-    return static_cast<const T *>(x) + b * s.batch + t * s.token;
-}
+struct HeadWay {
+    T *at = nullptr;
+    long long step;
+    __device__ __forceinline__ void enter(const HeadParams &p, const void *x, const fo_strides &s, const HeadTurns &turn, int group)
+    {
+        const long long b = turn.token / (unsigned)p.tokens, t = turn.token - b * p.tokens;
+        at = static_cast<T *>(const_cast<void *>(x)) + b * s.batch + t * s.token + (turn.h0 + group) * s.head;
+        step = turn.groups * s.head;
+    }
+    __device__ __forceinline__ void next() { at += step; }
+};
 
 // 8192 tokens with 32 + 8 heads of 128 in bfloat16
 template <class T, int V, int I, int PAIRING>
-__global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : HM) head_norm_kernel(const __grid_constant__ HeadParams p)
+__global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_norm_kernel(const __grid_constant__ HeadParams p)
 {
     using W = HeadWork<T, V, I, PAIRING>;
     using A = Acc<T>;
@@ -415,11 +433,15 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : HM) head_n
     HeadTurns ahead(p, t, cta, ctas), now = ahead;
     if (!now.there()) return;
     HeadRing<T, V, I, 1> ring(head_memory);
-    const T *x = head_row<T>(p, t.x, t.x_at, ahead.token);
+    HeadWay<T> x, y;
+    x.enter(p, t.x, t.x_at, ahead, group), y.enter(p, t.y, t.y_at, now, group);
     auto issue = [&]() {
-        const T *const rows[1] = {x + (ahead.h0 + group) * t.x_at.head};
-        ring.issue(rows, at, ahead.there() && ahead.h0 + group < ahead.end);
-        if (ahead.there() && ahead.next(t) && ahead.there()) x = head_row<T>(p, t.x, t.x_at, ahead.token);
+        const T *const rows[1] = {x.at};
+        const bool there = ahead.there();
+        ring.issue(rows, at, there && ahead.h0 + group < ahead.end);
+        if (!there) return;
+        if (!ahead.next(t)) x.next();
+        else if (ahead.there()) x.enter(p, t.x, t.x_at, ahead, group);
     };
     for (int k = 0; k < ring.kTurns; ++k) issue();
     U wa[I][N], wb[I][N];
@@ -461,9 +483,10 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : HM) head_n
             }
         }
         if (p.pairs) W::turn(at, g, a, b);
-        if (now.h0 + group < now.end)
-            W::store(const_cast<T *>(head_row<T>(p, t.y, t.y_at, now.token)) + (now.h0 + group) * t.y_at.head, at, a, b);
+        if (now.h0 + group < now.end) W::store(y.at, at, a, b);
         fresh = now.next(t);
+        if (!fresh) y.next();
+        else if (now.there()) y.enter(p, t.y, t.y_at, now, group);
     }
 }
 
@@ -476,7 +499,6 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     using A = Acc<T>;
     using U = typename W::U;
     constexpr int N = W::N;
-    __shared__ A line[2][FO_HEAD_MAX_DIM];
     extern __shared__ __align__(16) unsigned char head_memory[];
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
@@ -487,17 +509,21 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     const bool normed = t.kind != FO_NORM_NONE;
     HeadTurns ahead(p, t, cta, ctas), now = ahead;
     HeadRing<T, V, I, 2> ring(head_memory);
-    const T *x = nullptr, *dy = nullptr;
+    HeadWay<T> x, dy, dx;
     auto enter = [&]() {
-        if (!ahead.there()) return;
-        if (normed) x = head_row<T>(p, t.x, t.x_at, ahead.token);
-        dy = head_row<T>(p, t.dy, t.dy_at, ahead.token);
+        if (normed) x.enter(p, t.x, t.x_at, ahead, group);
+        dy.enter(p, t.dy, t.dy_at, ahead, group);
     };
-    enter();
+    if (now.there()) enter(), dx.enter(p, t.y, t.y_at, now, group);
     auto issue = [&]() {
-        const T *const rows[2] = {dy + (ahead.h0 + group) * t.dy_at.head, normed ? x + (ahead.h0 + group) * t.x_at.head : nullptr};
-        ring.issue(rows, at, ahead.there() && ahead.h0 + group < ahead.end);
-        if (ahead.there() && ahead.next(t)) enter();
+        const T *const rows[2] = {dy.at, x.at};
+        const bool there = ahead.there();
+        ring.issue(rows, at, there && ahead.h0 + group < ahead.end);
+        if (!there) return;
+        if (!ahead.next(t)) {
+            if (normed) x.next();
+            dy.next();
+        } else if (ahead.there()) enter();
     };
     for (int k = 0; k < ring.kTurns; ++k) issue();
     U wa[I][N], wb[I][N], da[I][N], db[I][N], ea[BIAS ? I : 1][N], eb[BIAS ? I : 1][N];
@@ -555,44 +581,37 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
                     v[i][j] = (fused_ma(back, b[i][j], v[i][j]) + mean) * all;
                 }
         }
-        if (on) W::store(const_cast<T *>(head_row<T>(p, t.y, t.y_at, now.token)) + (now.h0 + group) * t.y_at.head, at, u, v);
+        if (on) W::store(dx.at, at, u, v);
         fresh = now.next(t);
+        if (!fresh) dx.next();
+        else if (now.there()) dx.enter(p, t.y, t.y_at, now, group);
     }
     if (!t.partial_w && !t.partial_b) return;
-    // the warp's groups, then the CTA's warps one after the other
-    auto groups_sum = [&](U f, int k) {
-        A s;
-        if constexpr (V == 1) s = f;
-        else s = k ? second(f) : first(f);
-        for (int o = p.lanes; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        return s;
-    };
-    for (int w = 0; w < kHeadWarps; ++w) {
-        if ((int)threadIdx.x / 32 == w) {
-#pragma unroll
-            for (int i = 0; i < I; ++i)
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int k = 0; k < V / N; ++k) {
-                        const int e = j * (V / N) + k;
-                        const A sa = groups_sum(da[i][j], k), sb = groups_sum(db[i][j], k);
-                        const A ta = BIAS ? groups_sum(ea[BIAS ? i : 0][j], k) : A(0), tb = BIAS ? groups_sum(eb[BIAS ? i : 0][j], k) : A(0);
-                        if (group == 0 && at.a[i] >= 0) {
-                            line[0][at.a[i] + e] = (w ? line[0][at.a[i] + e] : A(0)) + sa;
-                            if (BIAS) line[1][at.a[i] + e] = (w ? line[1][at.a[i] + e] : A(0)) + ta;
-                        }
-                        if (group == 0 && at.b[i] >= 0) {
-                            line[0][at.b[i] + e] = (w ? line[0][at.b[i] + e] : A(0)) + sb;
-                            if (BIAS) line[1][at.b[i] + e] = (w ? line[1][at.b[i] + e] : A(0)) + tb;
-                        }
-                    }
-        }
+    // every group of lanes writes its sums (where the ring was), and they are added in order
+    A *const lines = reinterpret_cast<A *>(head_memory);
+    const int count = kHeadWarps * (32 / p.lanes), mine = threadIdx.x / p.lanes;
+    if constexpr (V > 1) asm volatile("cp.async.wait_all;" ::: "memory");
+    for (int which_sum = 0; which_sum < (BIAS ? 2 : 1); ++which_sum) {
         __syncthreads();
-    }
-    for (int j = threadIdx.x; j < p.dim; j += kHeadCta) {
-        if (t.partial_w) static_cast<A *>(t.partial_w)[(size_t)cta * p.dim + j] = line[0][j];
-        if (BIAS && t.partial_b) static_cast<A *>(t.partial_b)[(size_t)cta * p.dim + j] = line[1][j];
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int k = 0; k < V / N; ++k) {
+                    const int e = j * (V / N) + k;
+                    const U sa = BIAS && which_sum ? ea[BIAS ? i : 0][j] : da[i][j], sb = BIAS && which_sum ? eb[BIAS ? i : 0][j] : db[i][j];
+                    if (at.a[i] >= 0) lines[mine * p.dim + at.a[i] + e] = W::part(sa, k);
+                    if (at.b[i] >= 0) lines[mine * p.dim + at.b[i] + e] = W::part(sb, k);
+                }
+        __syncthreads();
+        A *const to = static_cast<A *>(which_sum ? t.partial_b : t.partial_w);
+        if (to)
+            for (int j = threadIdx.x; j < p.dim; j += kHeadCta) {
+                A s = A(0);
+                for (int l = 0; l < count; ++l) s += lines[l * p.dim + j];
+                to[(size_t)cta * p.dim + j] = s;
+            }
     }
 }
 

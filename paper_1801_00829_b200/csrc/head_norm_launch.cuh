@@ -9,8 +9,10 @@ namespace fo {
 template <class T, int V, int I, int TENSORS>
 cudaError_t head_go(void (*kernel)(HeadParams), const HeadParams &p, int grid, cudaStream_t st, OncePerGpu &once)
 {
-    constexpr size_t bytes = HeadRing<T, V, I, TENSORS>::kBytes;
-    if (bytes > 40 * 1024) {                              // with the static part
+    // the ring; in its place at the end the gradient's sums, a line for every group of lanes
+    constexpr size_t lines = TENSORS == 2 ? (size_t)kHeadWarps * 64 * I * V * sizeof(Acc<T>) : 0, ring = HeadRing<T, V, I, TENSORS>::kBytes;
+    constexpr size_t bytes = ring > lines ? ring : lines;
+    if (bytes > 48 * 1024) {
         const cudaError_t e = once.allow(kernel, bytes);
         if (e != cudaSuccess) return e;
     }
