@@ -15,7 +15,7 @@ extern template cudaError_t launch_head_norm<__half>(const HeadParams &, int, in
 namespace {
 
 constexpr int kSumWarps = 32;
-constexpr int kHeadCtas = 4;            // CTAs per SM that a call spreads over
+constexpr int kHeadCtas = 2;            // CTAs per SM: as many as work at once
 constexpr int kMostSms = 256;           // bound of the workspace, whatever the GPU
 
 int wide_code(int type) { return type == FO_F64 ? FO_F64 : FO_F32; }
@@ -116,7 +116,8 @@ void set_rotation(HeadParams &p, const fo_rotation &r, int type, int piece)
 {
     p.pairs = r.pairs;
     if (!r.pairs) return;
-    const int table = 16 / elem_bytes(wide_code(type)), width = std::min(table, piece);      // values in one load
+    // values in one load: of a piece's pairs, which are as many as its elements or half of them
+    const int table = 16 / elem_bytes(wide_code(type)), width = std::max(1, std::min(table, r.pairing == FO_PAIR_HALVES ? piece : piece / 2));
     p.axes = r.axes, p.rows = r.rows, p.ld_cos = r.ld_cos, p.ld_sin = r.ld_sin;
     p.cos_table = r.cos_table, p.sin_table = r.sin_table, p.positions = r.positions;
     p.position_axis = r.position_axis, p.position_batch = r.position_batch, p.position_token = r.position_token;
@@ -147,6 +148,7 @@ int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
     const int groups = 32 / p.lanes;
     p.tokens = (int)std::max<long long>(tokens, 1), p.all_tokens = (int)(batch * tokens);
     const long long warps = (long long)sms * kHeadCtas * kHeadWarps;
+    // a task costs its turns and, for its token's cosines and sines, about one more
     long long turns[2] = {0, 0}, ctas[2] = {0, 0};
     for (int k = 0; k < count; ++k) turns[k] = (p.t[k].heads + groups - 1) / groups;
     const long long all = p.all_tokens * (turns[0] + turns[1]), each = std::max<long long>(1, all / warps);
@@ -155,7 +157,8 @@ int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
         t.per_chunk = (int)std::max<long long>(1, std::min(each, turns[k])) * groups;
         t.chunks = std::max(1, (t.heads + t.per_chunk - 1) / t.per_chunk);
         const long long tasks = (long long)p.all_tokens * (t.heads ? t.chunks : 0);
-        const long long share = all ? std::max<long long>(1, (long long)sms * kHeadCtas * turns[k] / std::max<long long>(1, turns[0] + turns[1])) : 0;
+        const long long cost = turns[k] ? turns[k] + 1 : 0, both = (turns[0] ? turns[0] + 1 : 0) + (turns[1] ? turns[1] + 1 : 0);
+        const long long share = all ? std::max<long long>(1, (long long)sms * kHeadCtas * cost / std::max<long long>(1, both)) : 0;
         ctas[k] = std::min((tasks + kHeadWarps - 1) / kHeadWarps, share);
     }
     p.ctas0 = (int)ctas[0];

@@ -65,37 +65,35 @@ __device__ __forceinline__ U head_all(A v)
 }
 template <class A> __device__ __forceinline__ Two<A> head_swap(Two<A> u) { return two(second(u), first(u)); }
 
-// What a lane holds of a vector: item i is the pieces at a[i] and b[i] (-1: none), of which ta and tb are turned; its first pair.
+// What a lane holds of a vector: item i is the pieces at a[i] and b[i] (-1: none), of which ta and tb are turned.  Pieces that are
+// not turned against each other are dealt out so that neighbouring lanes have neighbouring pieces.
 template <int V, int I, int PAIRING>
 struct HeadItems {
+    static constexpr bool HALVES = PAIRING == FO_PAIR_HALVES || V == 1;
     int a[I], b[I];
-    int pairs, lane, lanes;
-    __device__ __forceinline__ HeadItems(int lane_, int lanes_, int dim, int pairs_) : pairs(pairs_), lane(lane_), lanes(lanes_)
+    int pairs;
+    __device__ __forceinline__ HeadItems(int lane, int lanes, int dim, int pairs_) : pairs(pairs_)
     {
+        const int turned = HALVES ? pairs / V : 0;             // items whose pieces are halves of pairs
+        const int rest = (dim + V - 1) / V - 2 * turned, half = (rest + 1) / 2;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int u = lane + i * lanes;
-            if (PAIRING == FO_PAIR_HALVES || V == 1) {
-                if (u * V < pairs) {
-                    a[i] = PAIRING == FO_PAIR_HALVES ? u * V : 2 * u;
-                    b[i] = PAIRING == FO_PAIR_HALVES ? pairs + u * V : 2 * u + 1;
-                } else {
-                    a[i] = 2 * pairs + (u * V - pairs) * 2;
-                    b[i] = a[i] + V;
-                }
+            if (u < turned) {
+                a[i] = PAIRING == FO_PAIR_HALVES ? u * V : 2 * u;
+                b[i] = PAIRING == FO_PAIR_HALVES ? pairs + u * V : 2 * u + 1;
             } else {
-                a[i] = u * 2 * V, b[i] = a[i] + V;
+                a[i] = (2 * turned + u - turned) * V, b[i] = a[i] + half * V;
+                if (u - turned >= half) a[i] = -1;
+                if (a[i] < 0 || b[i] >= dim) b[i] = -1;
             }
-            if (a[i] >= dim) a[i] = -1;
-            if (a[i] < 0 || b[i] >= dim) b[i] = -1;
         }
     }
-    __device__ __forceinline__ int pair(int i) const { return (lane + i * lanes) * V; }
-    __device__ __forceinline__ bool ta(int i) const
-    {
-        return PAIRING == FO_PAIR_HALVES || V == 1 ? pair(i) < pairs : a[i] >= 0 && a[i] < 2 * pairs;
-    }
-    __device__ __forceinline__ bool tb(int i) const { return PAIRING == FO_PAIR_HALVES || V == 1 ? ta(i) : b[i] >= 0 && b[i] < 2 * pairs; }
+    __device__ __forceinline__ bool ta(int i) const { return a[i] >= 0 && a[i] < 2 * pairs; }
+    __device__ __forceinline__ bool tb(int i) const { return b[i] >= 0 && b[i] < 2 * pairs; }
+    // the first pair of a piece
+    __device__ __forceinline__ int pair_a(int i) const { return PAIRING == FO_PAIR_HALVES ? a[i] : a[i] / 2; }
+    __device__ __forceinline__ int pair_b(int i) const { return b[i] / 2; }
 };
 
 // The rows of the tables at which a token's positions lie; -1: outside.
@@ -107,15 +105,14 @@ __device__ __forceinline__ HeadRows head_rows(const HeadParams &p, unsigned toke
     HeadRows r;
     const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
     const long long place = b * p.position_batch + t * p.position_token;
+    const auto row_at = [&](long long at) {
+        const long long row = p.long_positions ? static_cast<const long long *>(p.positions)[at] : static_cast<const int *>(p.positions)[at];
+        return row >= 0 && row < p.rows ? (int)row : -1;
+    };
+    r.at[0] = row_at(place);
+    if (p.axes > 1)
 #pragma unroll
-    for (int k = 0; k < FO_MAX_AXES; ++k) {
-        r.at[k] = -1;
-        if (k < p.axes) {
-            const long long at = place + k * p.position_axis;
-            const long long row = p.long_positions ? static_cast<const long long *>(p.positions)[at] : static_cast<const int *>(p.positions)[at];
-            if (row >= 0 && row < p.rows) r.at[k] = (int)row;
-        }
-    }
+        for (int k = 1; k < FO_MAX_AXES; ++k) r.at[k] = k < p.axes ? row_at(place + k * p.position_axis) : -1;
     return r;
 }
 
@@ -133,45 +130,53 @@ struct HeadWork {
     struct Angles {
         U c[I][HALVES ? N : 2 * N], s[I][HALVES ? N : 2 * N], minus[HALVES ? I : 1][N];
     };
+    // n values of both tables from `pair` on, of which the first `there` exist; NaN outside the table
+    template <int M>
+    static __device__ __forceinline__ void table(const HeadParams &p, const HeadRows &rows, int pair, bool on, A (&c)[M], A (&s)[M])
+    {
+        const A *const ct = static_cast<const A *>(p.cos_table), *const st = static_cast<const A *>(p.sin_table);
+        constexpr int W = 16 / (int)sizeof(A) < M ? 16 / (int)sizeof(A) : M;         // values in one load
+        auto row_of = [&](int q) {
+            int r = rows.at[0];
+            if (p.axes > 1)
+#pragma unroll
+                for (int k = 1; k < FO_MAX_AXES; ++k)
+                    if (k < p.axes && q >= p.section_end[k - 1]) r = rows.at[k];
+            return r;
+        };
+#pragma unroll
+        for (int j0 = 0; j0 < M; j0 += W) {
+            const int q0 = pair + j0;
+#pragma unroll
+            for (int j = 0; j < W; ++j) c[j0 + j] = s[j0 + j] = A(NAN);
+            if (W > 1 && p.table_pieces) {
+                const int r = row_of(q0);
+                if (on && q0 < p.pairs && r >= 0) {
+                    const HeadPiece<A, W> u = head_load<A, W>(ct + r * p.ld_cos + q0), v = head_load<A, W>(st + r * p.ld_sin + q0);
+#pragma unroll
+                    for (int j = 0; j < W; ++j) c[j0 + j] = u.v[j], s[j0 + j] = v.v[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    const int r = row_of(q0 + j);
+                    if (on && q0 + j < p.pairs && r >= 0) c[j0 + j] = ct[r * p.ld_cos + q0 + j], s[j0 + j] = st[r * p.ld_sin + q0 + j];
+                }
+            }
+        }
+    }
     template <int SIGN>
     static __device__ __forceinline__ void angles(const HeadParams &p, const Items &at, const HeadRows &rows, Angles &g)
     {
-        const A *const ct = static_cast<const A *>(p.cos_table), *const st = static_cast<const A *>(p.sin_table);
-        auto row_of = [&](int pair) {
-            int r = rows.at[0];
-#pragma unroll
-            for (int k = 1; k < FO_MAX_AXES; ++k)
-                if (k < p.axes && pair >= p.section_end[k - 1]) r = rows.at[k];
-            return r;
-        };
-        constexpr int W = 16 / (int)sizeof(A) < V ? 16 / (int)sizeof(A) : V;         // table values in one load
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            A c[V], s[V];
-#pragma unroll
-            for (int j0 = 0; j0 < V; j0 += W) {
-                const int pair = at.pair(i) + j0;
-                const bool on = at.a[i] >= 0 && at.ta(i) && pair < p.pairs;
-                const int r = on ? row_of(pair) : -1;
-#pragma unroll
-                for (int j = 0; j < W; ++j) c[j0 + j] = s[j0 + j] = A(NAN);          // a position outside the table
-                if (W > 1 && p.table_pieces) {
-                    if (r >= 0) {
-                        const HeadPiece<A, W> u = head_load<A, W>(ct + r * p.ld_cos + pair), v = head_load<A, W>(st + r * p.ld_sin + pair);
-#pragma unroll
-                        for (int j = 0; j < W; ++j) c[j0 + j] = u.v[j], s[j0 + j] = v.v[j];
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < W; ++j) {
-                        const int q = on && pair + j < p.pairs ? row_of(pair + j) : -1;
-                        if (q >= 0) c[j0 + j] = ct[q * p.ld_cos + pair + j], s[j0 + j] = st[q * p.ld_sin + pair + j];
-                    }
-                }
-            }
             if constexpr (V == 1) {
+                A c[1], s[1];
+                table<1>(p, rows, at.pair_a(i), at.ta(i), c, s);
                 g.c[i][0] = c[0], g.s[i][0] = A(SIGN) * s[0], g.minus[i][0] = A(-SIGN) * s[0];
             } else if constexpr (HALVES) {
+                A c[V], s[V];
+                table<V>(p, rows, at.pair_a(i), at.ta(i), c, s);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     g.c[i][j] = two(c[2 * j], c[2 * j + 1]);
@@ -179,9 +184,26 @@ struct HeadWork {
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 2 * N; ++j) g.c[i][j] = both(c[j]), g.s[i][j] = two(A(-SIGN) * s[j], A(SIGN) * s[j]);
+                for (int k = 0; k < 2; ++k) {
+                    A c[N], s[N];
+                    table<N>(p, rows, k ? at.pair_b(i) : at.pair_a(i), k ? at.tb(i) : at.ta(i), c, s);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) g.c[i][k * N + j] = both(c[j]), g.s[i][k * N + j] = two(A(-SIGN) * s[j], A(SIGN) * s[j]);
+                }
             }
         }
+    }
+    // Asks for what angles() will load of the next task's token.
+    static __device__ __forceinline__ void expect(const HeadParams &p, const Items &at, const HeadRows &rows)
+    {
+        if (p.axes > 1 || rows.at[0] < 0) return;
+        const A *const ct = static_cast<const A *>(p.cos_table) + rows.at[0] * p.ld_cos, *const st = static_cast<const A *>(p.sin_table) + rows.at[0] * p.ld_sin;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (at.ta(i)) {
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(ct + at.pair_a(i)));
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(st + at.pair_a(i)));
+            }
     }
     // Turns a lane's pieces.
     static __device__ __forceinline__ void turn(const Items &at, const Angles &g, U (&a)[I][N], U (&b)[I][N])
@@ -215,11 +237,17 @@ struct HeadWork {
     static __device__ __forceinline__ A sum(U v, int lanes)
     {
         A s = joined(v);
-        for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        if (lanes > 8) {
+            if (lanes > 16) s += __shfl_xor_sync(0xffffffffu, s, 16);
+            s += __shfl_xor_sync(0xffffffffu, s, 8);
+        }
+        if (lanes > 4) s += __shfl_xor_sync(0xffffffffu, s, 4);
+        if (lanes > 2) s += __shfl_xor_sync(0xffffffffu, s, 2);
+        if (lanes > 1) s += __shfl_xor_sync(0xffffffffu, s, 1);
         return s;
     }
     // n = (x - mu) r of a vector, in place; returns r
-    static __device__ __forceinline__ A normalise(const HeadParams &p, const Items &at, int kind, A eps, U (&a)[I][N], U (&b)[I][N])
+    static __device__ __forceinline__ A normalise(int lanes, A inv_dim, const Items &at, int kind, A eps, U (&a)[I][N], U (&b)[I][N])
     {
         if (kind == FO_NORM_LAYER) {
             U s = head_all<U>(A(0));
@@ -227,7 +255,7 @@ struct HeadWork {
             for (int i = 0; i < I; ++i)
 #pragma unroll
                 for (int j = 0; j < N; ++j) s = s + (a[i][j] + b[i][j]);             // absent pieces are zeros
-            const U mean = head_all<U>(-sum(s, p.lanes) * A(p.inv_dim));
+            const U mean = head_all<U>(-sum(s, lanes) * inv_dim);
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -241,7 +269,7 @@ struct HeadWork {
         for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) sq = fused_ma(a[i][j], a[i][j], sq), sr = fused_ma(b[i][j], b[i][j], sr);
-        const A r = group_rsqrt(fused_ma(sum(sq + sr, p.lanes), A(p.inv_dim), eps));
+        const A r = group_rsqrt(fused_ma(sum(sq + sr, lanes), inv_dim, eps));
         const U all = head_all<U>(r);
 #pragma unroll
         for (int i = 0; i < I; ++i)
@@ -427,11 +455,13 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
     const HeadTensor &t = p.t[which];
-    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes;
+    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, kind = t.kind;
+    const A eps = A(t.eps), inv_dim = A(p.inv_dim);
     const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
     const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
     HeadTurns ahead(p, t, cta, ctas), now = ahead;
     if (!now.there()) return;
+    const bool bias = t.bias != nullptr;
     HeadRing<T, V, I, 1> ring(head_memory);
     HeadWay<T> x, y;
     x.enter(p, t.x, t.x_at, ahead, group), y.enter(p, t.y, t.y_at, now, group);
@@ -461,13 +491,13 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         for (int i = 0; i < I; ++i) W::widen_piece(ring.take(0, 2 * i), a[i]), W::widen_piece(ring.take(0, 2 * i + 1), b[i]);
         ring.taken();
         issue();
-        if (t.kind != FO_NORM_NONE) {
-            W::normalise(p, at, t.kind, A(t.eps), a, b);
+        if (kind != FO_NORM_NONE) {
+            W::normalise(p.lanes, inv_dim, at, kind, eps, a, b);
 #pragma unroll
             for (int i = 0; i < I; ++i) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) a[i][j] = a[i][j] * wa[i][j], b[i][j] = b[i][j] * wb[i][j];
-                if (t.bias) {
+                if (bias) {
                     U bias[N];
                     if (at.a[i] >= 0) {
                         W::vector_piece(p, t.bias, at.a[i], bias);
@@ -484,6 +514,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         }
         if (p.pairs) W::turn(at, g, a, b);
         if (now.h0 + group < now.end) W::store(y.at, at, a, b);
+        if (fresh && p.pairs) W::expect(p, at, rows);
         fresh = now.next(t);
         if (!fresh) y.next();
         else if (now.there()) y.enter(p, t.y, t.y_at, now, group);
@@ -503,10 +534,11 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
     const HeadTensor &t = p.t[which];
-    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes;
+    const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, kind = t.kind;
+    const A eps = A(t.eps), inv_dim = A(p.inv_dim);
     const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
     const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
-    const bool normed = t.kind != FO_NORM_NONE;
+    const bool normed = kind != FO_NORM_NONE;
     HeadTurns ahead(p, t, cta, ctas), now = ahead;
     HeadRing<T, V, I, 2> ring(head_memory);
     HeadWay<T> x, dy, dx;
@@ -558,7 +590,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         if (p.pairs) W::turn(at, g, u, v);
         if (normed) {
             // a group without a head has zeros throughout, and with eps 0 its r would not be finite
-            const A r = W::normalise(p, at, t.kind, on ? A(t.eps) : A(1), a, b);
+            const A r = W::normalise(p.lanes, inv_dim, at, kind, on ? eps : A(1), a, b);
             U with_n = zero, alone = zero;
 #pragma unroll
             for (int i = 0; i < I; ++i)
@@ -571,8 +603,8 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
                     with_n = fused_ma(u[i][j], a[i][j], fused_ma(v[i][j], b[i][j], with_n));
                     alone = alone + (u[i][j] + v[i][j]);
                 }
-            const U back = head_all<U>(-W::sum(with_n, p.lanes) * A(p.inv_dim)), all = head_all<U>(r);
-            const U mean = t.kind == FO_NORM_LAYER ? head_all<U>(-W::sum(alone, p.lanes) * A(p.inv_dim)) : zero;
+            const U back = head_all<U>(-W::sum(with_n, p.lanes) * inv_dim), all = head_all<U>(r);
+            const U mean = kind == FO_NORM_LAYER ? head_all<U>(-W::sum(alone, p.lanes) * inv_dim) : zero;
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -582,6 +614,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
                 }
         }
         if (on) W::store(dx.at, at, u, v);
+        if (fresh && p.pairs) W::expect(p, at, rows);
         fresh = now.next(t);
         if (!fresh) dx.next();
         else if (now.there()) dx.enter(p, t.y, t.y_at, now, group);
