@@ -15,6 +15,8 @@
 
 namespace fo {
 
+constexpr int kDistillCta = 256;
+
 struct DistillParams {
     long long rows;
     int vocab, top;
@@ -72,11 +74,22 @@ __device__ __forceinline__ double cta_max(double v, double *room)
 
 // The teacher's entries of one row, in shared memory.
 struct Teacher {
-    int *id;                            // -1: no entry
-    double *p, *z;                      // shares, and the student's logits
+    int *id;                            // -1: no entry; padded to a multiple of 4
+    double *p, *share, *z;              // shares, those of a place, and the student's logits
+    int *place;                         // of an entry that is the first of its place; -1
     double top_max, log_sum;            // log p = v / temperature - top_max - log_sum
     double sum, rest;                   // of p, and P
 };
+
+constexpr int kTeacherBytes = 32;       // of an entry in shared memory
+__device__ __forceinline__ Teacher teacher_at(void *memory, int top)
+{
+    const int room = (top + 3) / 4 * 4;
+    Teacher t;
+    t.p = static_cast<double *>(memory), t.share = t.p + room, t.z = t.share + room;
+    t.id = reinterpret_cast<int *>(t.z + room), t.place = t.id + room;
+    return t;
+}
 
 template <class T>
 __device__ __forceinline__ double teacher_value(const DistillParams &p, long long row, int k)
@@ -99,6 +112,7 @@ __device__ __forceinline__ void teacher_shares(const DistillParams &p, long long
         bad = bad || id >= p.vocab;
         if (id >= 0) most = fmax(most, teacher_value<T>(p, row, k));
     }
+    if (threadIdx.x < ((4 - p.top % 4) & 3)) t.id[p.top + threadIdx.x] = -1;
     if (p.tail) t.top_max = (double)static_cast<const Acc<T> *>(p.tail)[row];
     else t.top_max = cta_max(most, room);
     for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
@@ -111,22 +125,35 @@ __device__ __forceinline__ void teacher_shares(const DistillParams &p, long long
         t.rest = sum < 1.0 ? 1.0 - sum : sum >= 1.0 ? 0.0 : sum;
     } else if (sum != 0.0) {                              // 0: no entries
         t.log_sum = log(sum);
-        for (int k = threadIdx.x; k < p.top; k += blockDim.x) t.p[k] /= sum;
-        t.sum = sum / sum;
+        const double inverse = 1.0 / sum;
+        for (int k = threadIdx.x; k < p.top; k += blockDim.x) t.p[k] *= inverse;
+        t.sum = sum * inverse;
     }
     __syncthreads();
-}
-
-// True for the first of the entries with this one's place; its share becomes that of all of them.
-__device__ __forceinline__ bool first_of_place(const Teacher &t, int top, int k, double &share)
-{
-    const int id = t.id[k];
-    for (int j = 0; j < k; ++j)
-        if (t.id[j] == id) return false;
-    share = t.p[k];
-    for (int j = k + 1; j < top; ++j)
-        if (t.id[j] == id) share += t.p[j];
-    return true;
+    // of entries with the same place the first one takes the shares of all, the others have no place
+    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
+        const int id = t.id[k];
+        t.share[k] = t.p[k], t.place[k] = id;
+        if (id < 0) continue;
+        int same = 0, first = k;
+        const int4 *const four = reinterpret_cast<const int4 *>(t.id);
+#pragma unroll 4
+        for (int j = 0; j < (p.top + 3) / 4; ++j) {
+            const int4 v = four[j];
+            const int hits = (v.x == id) | (v.y == id) << 1 | (v.z == id) << 2 | (v.w == id) << 3;
+            same += __popc(hits);
+            if (hits && 4 * j + __ffs(hits) - 1 < first) first = 4 * j + __ffs(hits) - 1;
+        }
+        if (same == 1) continue;
+        if (first != k) {
+            t.place[k] = -1;
+            continue;
+        }
+        double all = 0.0;
+        for (int j = 0; j < p.top; ++j)
+            if (t.id[j] == id) all += t.p[j];
+        t.share[k] = all;
+    }
 }
 
 // Where a row lies: pieces of 16 bytes from the boundary before its first element.
@@ -172,20 +199,36 @@ __device__ __forceinline__ void distill_put(const RowPieces<T> &at, int i, T *dz
     }
 }
 
+// The largest value of a piece and `most`; a NaN is passed over (the sum finds it).
+template <class T>
+__device__ __forceinline__ Acc<T> distill_largest(const Packed<T, 16 / sizeof(T)> &v, Acc<T> most)
+{
+    if constexpr (std::is_same<T, __nv_bfloat16>::value || std::is_same<T, __half>::value) {
+        using Pair = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const Pair *const w = reinterpret_cast<const Pair *>(v.w);
+        const Pair m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+        return larger(most, larger(widen(m.x), widen(m.y)));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16 / (int)sizeof(T); ++e) most = larger(most, v.get(e));
+        return most;
+    }
+}
+
 // What the CTAs of a cluster tell each other.
 struct DistillPart {
     double rest_max, rest_sum, top_max, top_sum, entries;
 };
 
 template <class T, bool STEP>
-__global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ DistillParams p)
+__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_kernel(const __grid_constant__ DistillParams p)
 {
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char distill_memory[];
     __shared__ double room[5][32];
     __shared__ DistillPart parts[8];
-    __shared__ double result[5];
+    __shared__ double result[3];
     unsigned rank, cluster;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
@@ -194,33 +237,30 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
     const long long row = blockIdx.x / cluster;
     const T *z = static_cast<const T *>(p.logits) + row * p.ld_logits;
     T *dz = STEP ? static_cast<T *>(p.dz) + row * p.ld_dz : nullptr;
-    const int first = (int)rank * p.slice;
+    const int first_piece = (int)rank * p.slice;
     A weight = A(1);
     if (STEP) {
         if (p.dloss) weight = static_cast<const A *>(p.dloss)[row];
         if (weight == A(0)) {                                 // the row is not looked at
             if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             // one piece more than the logits' can be the gradient's, at another offset: the last CTA has it
-            distill_zero(dz, p.vocab, first, rank + 1 == cluster ? p.slice + 1 : p.slice);
+            distill_zero(dz, p.vocab, first_piece, rank + 1 == cluster ? p.slice + 1 : p.slice);
             if (rank == 0 && threadIdx.x == 0) static_cast<A *>(p.loss)[row] = A(0);
             return;
         }
     }
     const RowPieces<T> at(z, p.vocab);
-    const int count = max(0, min(p.slice, at.pieces - first));
+    const int count = max(0, min(p.slice, at.pieces - first_piece));
     T *const held = reinterpret_cast<T *>(distill_memory);
-    Teacher t;
-    t.p = reinterpret_cast<double *>(distill_memory + (size_t)p.slice * 16);
-    t.z = t.p + p.top;
-    t.id = reinterpret_cast<int *>(t.z + p.top);
+    Teacher t = teacher_at(distill_memory + (size_t)p.slice * 16, p.top);
     const T *const base = z - at.skip;
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
-        if (at.whole(first + i)) {
+        if (at.whole(first_piece + i)) {
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(held + i * E)),
-                         "l"(base + (long long)(first + i) * E) : "memory");
+                         "l"(base + (long long)(first_piece + i) * E) : "memory");
         } else {
             for (int e = 0; e < E; ++e) {
-                const int j = (first + i) * E + e;
+                const int j = (first_piece + i) * E + e;
                 held[i * E + e] = at.holds(j) ? base[j] : narrow<T>(distill_floor<A>());
             }
         }
@@ -231,22 +271,20 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
     __syncthreads();
 
     // the entries in this CTA's part: the largest, then out of the row
-    const int from = first * E - at.skip, to = from + count * E;      // elements of the row
+    const int from = first_piece * E - at.skip, to = from + count * E;      // elements of the row
     double most = -CUDART_INF, entries = 0.0, top_sum = 0.0;
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.id[k] >= from && t.id[k] < to && t.id[k] >= 0) most = fmax(most, (double)widen(held[t.id[k] - from]));
-    most = cta_max(most, room[2]);
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
-        if (t.id[k] < from || t.id[k] >= to || t.id[k] < 0) continue;
-        const double v = (double)widen(held[t.id[k] - from]), share = t.p[k];
-        t.z[k] = v;
-        if (share != 0.0) entries += share * (teacher_value<T>(p, row, k) - t.top_max - t.log_sum - v * p.inv_t);
-        double whole;
-        if (first_of_place(t, p.top, k, whole)) top_sum += exp((v - most) * p.inv_t);
-    }
-    __syncthreads();
+        if (t.id[k] >= 0 && t.id[k] >= from && t.id[k] < to) {
+            const double v = (double)widen(held[t.id[k] - from]), share = t.p[k];
+            t.z[k] = v, most = fmax(most, v);
+            if (share != 0.0) entries += share * (teacher_value<T>(p, row, k) - t.top_max - t.log_sum - v * p.inv_t);
+        }
+    most = cta_max(most, room[2]);                            // and all of them have been read
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.id[k] >= from && t.id[k] < to && t.id[k] >= 0) held[t.id[k] - from] = narrow<T>(distill_floor<A>());
+        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
+            top_sum += exp((t.z[k] - most) * p.inv_t);
+            held[t.place[k] - from] = narrow<T>(distill_floor<A>());
+        }
     __syncthreads();
 
     // all the rest: every thread keeps the largest so far and the sum relative to it
@@ -262,26 +300,29 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
             if (i < count) {
                 const uint4 w = *reinterpret_cast<const uint4 *>(held + i * E);
                 v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
-#pragma unroll
-                for (int e = 0; e < E; ++e) top = larger(top, v[u].get(e));
+                top = distill_largest<T>(v[u], top);
             }
         }
         const A ref = top == distill_floor<A>() ? A(0) : top;
-        A more = A(0);
+        Two<A> more = both(A(0));
+        const Two<A> less = both(-ref), scale = both(unit);
 #pragma unroll
         for (int u = 0; u < kTogether; ++u)
             if (i0 + u * (int)blockDim.x < count) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) more += distill_exp<T>((v[u].get(e) - ref) * unit);
+                for (int e = 0; e < E; e += 2) {
+                    const Two<A> x = (v[u].get2(e) + less) * scale;
+                    more = more + two(distill_exp<T>(first(x)), distill_exp<T>(second(x)));
+                }
             }
-        sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), more);
+        sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), joined(more));
         largest = top;
     }
     // the CTA's
-    double rest_max = (double)largest;
+    A rest_max = largest;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) rest_max = fmax(rest_max, __shfl_xor_sync(0xffffffffu, rest_max, o));
-    double rest_sum = sum == A(0) ? 0.0 : (double)(sum * distill_exp<T>((largest - A(rest_max)) * unit));
+    for (int o = 16; o > 0; o >>= 1) rest_max = larger(rest_max, __shfl_xor_sync(0xffffffffu, rest_max, o));
+    double rest_sum = sum == A(0) ? 0.0 : (double)(sum * distill_exp<T>((largest - rest_max) * unit));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
@@ -289,7 +330,7 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
         entries += __shfl_xor_sync(0xffffffffu, entries, o);
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if (lane == 0) room[0][warp] = rest_max, room[1][warp] = rest_sum, room[3][warp] = top_sum, room[4][warp] = entries;
+    if (lane == 0) room[0][warp] = (double)rest_max, room[1][warp] = rest_sum, room[3][warp] = top_sum, room[4][warp] = entries;
     __syncthreads();
     if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA has started
     if (warp == 0) {
@@ -298,7 +339,7 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
         double all = m;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) all = fmax(all, __shfl_xor_sync(0xffffffffu, all, o));
-        if (s != 0.0) s *= exp((m - all) * p.inv_t);
+        if (s != 0.0) s *= (double)distill_exp<T>(A(m - all) * unit);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -318,38 +359,25 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
         __syncwarp();
     }
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    // the row's
+    // the row's: lanes below 16 have the CTAs' rests, the others their entries
+    double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0;
     if (warp == 0) {
-        const bool in = lane < (int)cluster;
-        const DistillPart d = in ? parts[lane] : DistillPart{-CUDART_INF, 0.0, -CUDART_INF, 0.0, 0.0};
-        double m = fmax(d.rest_max, d.top_max), en = d.entries;
+        const int c = lane & 15;
+        double m = -CUDART_INF, s = 0.0;
+        if (c < (int)cluster) m = lane < 16 ? parts[c].rest_max : parts[c].top_max, s = lane < 16 ? parts[c].rest_sum : parts[c].top_sum;
+        row_max = m;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-        double s = d.rest_sum != 0.0 ? d.rest_sum * exp((d.rest_max - m) * p.inv_t) : 0.0;
-        double ts = d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - m) * p.inv_t) : 0.0;
+        for (int o = 16; o > 0; o >>= 1) row_max = fmax(row_max, __shfl_xor_sync(0xffffffffu, row_max, o));
+        if (s != 0.0) s *= exp((m - row_max) * p.inv_t);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            s += __shfl_xor_sync(0xffffffffu, s, o);
-            ts += __shfl_xor_sync(0xffffffffu, ts, o);
-            en += __shfl_xor_sync(0xffffffffu, en, o);
-        }
-        const double total = s + ts, log_total = m * p.inv_t + log(total);
-        double loss = t.sum != 0.0 ? en + t.sum * log_total : 0.0, factor = t.sum + t.rest;
-        if (t.rest > 0.0) {                                   // P (log P - log Q), Q = s / total
-            const double ratio = t.rest * total / s;
-            loss += t.rest * log(ratio), factor -= ratio;
-        }
-        if (!(t.sum == t.sum)) loss = factor = CUDART_NAN;    // an id outside the row
-        if (lane == 0) {
-            result[0] = m, result[1] = total, result[2] = factor;
-            if (rank == 0) {
-                if (p.loss) static_cast<A *>(p.loss)[row] = A(loss);
-                if (!STEP && p.stats) {
-                    A *const st = static_cast<A *>(p.stats);
-                    st[row] = A(m), st[p.rows + row] = A(total), st[2 * p.rows + row] = A(factor);
-                }
-            }
-        }
+        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        rest_of_row = __shfl_sync(0xffffffffu, s, 0);
+        total = rest_of_row + __shfl_sync(0xffffffffu, s, 16);
+        for (int k = 0; k < (int)cluster; ++k) row_entries += parts[k].entries;
+        double factor = t.sum + t.rest;
+        if (t.rest > 0.0) factor -= t.rest * total / rest_of_row;
+        if (!(t.sum == t.sum)) factor = CUDART_NAN;           // an id outside the row
+        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor;
     }
     if constexpr (STEP) {
         __syncthreads();
@@ -357,21 +385,37 @@ __global__ void __launch_bounds__(512) distill_kernel(const __grid_constant__ Di
         const double scale = (double)weight * p.inv_t, s_all = t.sum + t.rest;
         const A coef = A(scale * result[2] / result[1]);
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
+        const Two<A> less = both(-m), units = both(unit), coefs = both(coef);
+#pragma unroll 2
         for (int i = threadIdx.x; i < count; i += blockDim.x) {
             Packed<T, E> v, out;
-            out.clear();
+            if constexpr (sizeof(T) >= 4) out.clear();
             const uint4 w = *reinterpret_cast<const uint4 *>(held + i * E);
             v.w[0] = w.x, v.w[1] = w.y, v.w[2] = w.z, v.w[3] = w.w;
 #pragma unroll
-            for (int e = 0; e < E; e += 2) out.put2(e, two(distill_exp<T>((v.get(e) - m) * unit) * coef, distill_exp<T>((v.get(e + 1) - m) * unit) * coef));
-            distill_put(at, first + i, dz, alike, out);
+            for (int e = 0; e < E; e += 2) {
+                const Two<A> x = (v.get2(e) + less) * units;
+                out.put2(e, two(distill_exp<T>(first(x)), distill_exp<T>(second(x))) * coefs);
+            }
+            distill_put(at, first_piece + i, dz, alike, out);
         }
         __syncthreads();                                      // the entries' places have been written with zeros
-        for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
-            double share;
-            if (t.id[k] < from || t.id[k] >= to || t.id[k] < 0 || !first_of_place(t, p.top, k, share)) continue;
-            const double q = exp((t.z[k] - result[0]) * p.inv_t) / result[1];
-            dz[t.id[k]] = narrow<T>(A(scale * (q * s_all - share)));
+        for (int k = threadIdx.x; k < p.top; k += blockDim.x)
+            if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
+                const double q = exp((t.z[k] - result[0]) * p.inv_t) / result[1];
+                dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
+            }
+    }
+    // what only the loss needs comes last
+    if (rank == 0 && threadIdx.x == 0) {
+        const double log_total = row_max * p.inv_t + log(total);
+        double loss = t.sum != 0.0 ? row_entries + t.sum * log_total : 0.0;
+        if (t.rest > 0.0) loss += t.rest * log(t.rest * total / rest_of_row);        // P (log P - log Q)
+        if (!(t.sum == t.sum)) loss = CUDART_NAN;
+        if (p.loss) static_cast<A *>(p.loss)[row] = A(loss);
+        if (!STEP && p.stats) {
+            A *const st = static_cast<A *>(p.stats);
+            st[row] = A(row_max), st[p.rows + row] = A(total), st[2 * p.rows + row] = A(result[2]);
         }
     }
 }
@@ -397,10 +441,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     const RowPieces<T> at(z, p.vocab);
     const T *const base = z - at.skip;
     const int last = min(first + p.slice, at.pieces);
-    Teacher t;
-    t.p = reinterpret_cast<double *>(distill_memory);
-    t.z = t.p + p.top;
-    t.id = reinterpret_cast<int *>(t.z + p.top);
+    Teacher t = teacher_at(distill_memory, p.top);
     constexpr int kTogether = 4;
     Packed<T, E> v[kTogether];
     auto fetch = [&](int i0) {
@@ -423,12 +464,13 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     teacher_shares<T>(p, row, &room[0][0], t);
     const int from = first * E - at.skip, to = last * E - at.skip;
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.id[k] >= from && t.id[k] < to && t.id[k] >= 0) t.z[k] = (double)widen(z[t.id[k]]);
+        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) t.z[k] = (double)widen(z[t.place[k]]);
     __syncthreads();                                          // before anything is written: dz may be the logits
     const double scale = (double)weight * p.inv_t, s_all = t.sum + t.rest;
     // an id outside the row is one in the statistics too, and makes them NaN
     const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (double)factor / (double)total);
     const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
+    const Two<A> less = both(-m), units = both(unit), coefs = both(coef);
     for (int i0 = first + threadIdx.x; i0 < last; i0 += kTogether * blockDim.x) {
         if (i0 != first + (int)threadIdx.x) fetch(i0);
 #pragma unroll
@@ -436,20 +478,21 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
             const int i = i0 + u * (int)blockDim.x;
             if (i >= last) continue;
             Packed<T, E> out;
-            out.clear();
+            if constexpr (sizeof(T) >= 4) out.clear();
 #pragma unroll
-            for (int e = 0; e < E; e += 2)
-                out.put2(e, two(distill_exp<T>((v[u].get(e) - m) * unit) * coef, distill_exp<T>((v[u].get(e + 1) - m) * unit) * coef));
+            for (int e = 0; e < E; e += 2) {
+                const Two<A> x = (v[u].get2(e) + less) * units;
+                out.put2(e, two(distill_exp<T>(fo::first(x)), distill_exp<T>(second(x))) * coefs);
+            }
             distill_put(at, i, dz, alike, out);
         }
     }
     __syncthreads();
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
-        double share;
-        if (t.id[k] < from || t.id[k] >= to || t.id[k] < 0 || !first_of_place(t, p.top, k, share)) continue;
-        const double q = exp((t.z[k] - (double)m) * p.inv_t) / (double)total;
-        dz[t.id[k]] = narrow<T>(A(scale * (q * s_all - share)));
-    }
+    for (int k = threadIdx.x; k < p.top; k += blockDim.x)
+        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
+            const double q = exp((t.z[k] - (double)m) * p.inv_t) / (double)total;
+            dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
+        }
 }
 
 // Host: the kernels of one element type; distill_*.cu instantiate them.
