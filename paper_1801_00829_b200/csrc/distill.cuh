@@ -48,28 +48,29 @@ template <class A> __device__ __forceinline__ A distill_floor() { return -A(CUDA
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 
-// Reductions of a CTA in a fixed order; `room`: 32 values, free again after the next barrier.
-__device__ __forceinline__ double cta_sum(double v, double *room)
+__device__ __forceinline__ double distill_warp_sum(double v)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = (threadIdx.x & 31) < (blockDim.x >> 5) ? room[threadIdx.x & 31] : 0.0;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-__device__ __forceinline__ double cta_max(double v, double *room)
+__device__ __forceinline__ double distill_warp_max(double v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
-    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = (threadIdx.x & 31) < (blockDim.x >> 5) ? room[threadIdx.x & 31] : -CUDART_INF;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
+}
+// Sums s relative to maxima m, added up over each half of a warp (the rests', and the entries'): relative to each half's maximum,
+// which m becomes.
+__device__ __forceinline__ double distill_halves(double &m, double s, double inv_t)
+{
+    const double own = m;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (s != 0.0) s *= exp((own - m) * inv_t);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
 }
 
 // The teacher's entries of one row, in shared memory.
@@ -77,8 +78,6 @@ struct Teacher {
     int *id;                            // -1: no entry; padded to a multiple of 4
     double *p, *share, *z;              // shares, those of a place, and the student's logits
     int *place;                         // of an entry that is the first of its place; -1
-    double top_max, log_sum;            // log p = v / temperature - top_max - log_sum
-    double sum, rest;                   // of p, and P
 };
 
 constexpr int kTeacherBytes = 32;       // of an entry in shared memory
@@ -99,50 +98,59 @@ __device__ __forceinline__ double teacher_value(const DistillParams &p, long lon
     return v * p.inv_t;
 }
 
-// Fills t (barriers inside; room: 3 x 32 values).  An id that is no place of the row makes the sum NaN, and with it everything.
+// What all threads need to know of the entries besides the arrays.
+struct TeacherSums {
+    double top_max, log_sum;            // log p = v / temperature - top_max - log_sum
+    double sum, rest;                   // of p, and P
+};
+// The first warp's part: ids, shares and their sums.  An id that is no place of the row makes the sum NaN, and with it everything.
 template <class T>
-__device__ __forceinline__ void teacher_shares(const DistillParams &p, long long row, double *room, Teacher &t)
+__device__ __forceinline__ void teacher_shares(const DistillParams &p, long long row, const Teacher &t, TeacherSums &out)
 {
+    const int lane = threadIdx.x & 31;
     double most = -CUDART_INF, sum = 0.0;
     bool bad = false;
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
+    for (int k = lane; k < p.top; k += 32) {
         const long long at = row * p.ld_ids + k;
         const long long id = p.ids_long ? static_cast<const long long *>(p.ids)[at] : static_cast<const int *>(p.ids)[at];
+        const double v = teacher_value<T>(p, row, k);
         t.id[k] = id < 0 || id >= p.vocab ? -1 : (int)id;
+        t.z[k] = v;
         bad = bad || id >= p.vocab;
-        if (id >= 0) most = fmax(most, teacher_value<T>(p, row, k));
+        if (id >= 0) most = fmax(most, v);
     }
-    if (threadIdx.x < ((4 - p.top % 4) & 3)) t.id[p.top + threadIdx.x] = -1;
-    if (p.tail) t.top_max = (double)static_cast<const Acc<T> *>(p.tail)[row];
-    else t.top_max = cta_max(most, room);
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
-        const double e = t.id[k] >= 0 ? exp(teacher_value<T>(p, row, k) - t.top_max) : 0.0;
+    if (lane < ((4 - p.top % 4) & 3)) t.id[p.top + lane] = -1;
+    const double reference = p.tail ? (double)static_cast<const Acc<T> *>(p.tail)[row] : distill_warp_max(most);
+    for (int k = lane; k < p.top; k += 32) {
+        const double e = t.id[k] >= 0 ? exp(t.z[k] - reference) : 0.0;
         t.p[k] = e, sum += e;
     }
-    sum = cta_sum(bad ? CUDART_NAN : sum, room + 32);
-    t.log_sum = 0.0, t.sum = sum, t.rest = 0.0;
+    sum = distill_warp_sum(bad ? CUDART_NAN : sum);
+    TeacherSums s = {reference, 0.0, sum, 0.0};
     if (p.tail) {
-        t.rest = sum < 1.0 ? 1.0 - sum : sum >= 1.0 ? 0.0 : sum;
+        s.rest = sum < 1.0 ? 1.0 - sum : sum >= 1.0 ? 0.0 : sum;
     } else if (sum != 0.0) {                              // 0: no entries
-        t.log_sum = log(sum);
         const double inverse = 1.0 / sum;
-        for (int k = threadIdx.x; k < p.top; k += blockDim.x) t.p[k] *= inverse;
-        t.sum = sum * inverse;
+        for (int k = lane; k < p.top; k += 32) t.p[k] *= inverse;
+        s.log_sum = log(sum), s.sum = sum * inverse;
     }
-    __syncthreads();
-    // of entries with the same place the first one takes the shares of all, the others have no place
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
+    if (lane == 0) out = s;
+}
+// Of entries with the same place the first one takes the shares of all, the others have no place.
+__device__ __forceinline__ void teacher_places(const Teacher &t, int top)
+{
+    for (int k = threadIdx.x; k < top; k += blockDim.x) {
         const int id = t.id[k];
         t.share[k] = t.p[k], t.place[k] = id;
         if (id < 0) continue;
         int same = 0, first = k;
         const int4 *const four = reinterpret_cast<const int4 *>(t.id);
 #pragma unroll 4
-        for (int j = 0; j < (p.top + 3) / 4; ++j) {
+        for (int j = 0; j < (top + 3) / 4; ++j) {
             const int4 v = four[j];
             const int hits = (v.x == id) | (v.y == id) << 1 | (v.z == id) << 2 | (v.w == id) << 3;
             same += __popc(hits);
-            if (hits && 4 * j + __ffs(hits) - 1 < first) first = 4 * j + __ffs(hits) - 1;
+            if (hits) first = min(first, 4 * j + __ffs(hits) - 1);
         }
         if (same == 1) continue;
         if (first != k) {
@@ -150,7 +158,7 @@ __device__ __forceinline__ void teacher_shares(const DistillParams &p, long long
             continue;
         }
         double all = 0.0;
-        for (int j = 0; j < p.top; ++j)
+        for (int j = 0; j < top; ++j)
             if (t.id[j] == id) all += t.p[j];
         t.share[k] = all;
     }
@@ -226,9 +234,9 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char distill_memory[];
-    __shared__ double room[5][32];
-    __shared__ DistillPart parts[8];
+    __shared__ DistillPart warp_parts[kDistillCta / 32], parts[8];
     __shared__ double result[3];
+    __shared__ TeacherSums teacher;
     unsigned rank, cluster;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
@@ -252,7 +260,8 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     const RowPieces<T> at(z, p.vocab);
     const int count = max(0, min(p.slice, at.pieces - first_piece));
     T *const held = reinterpret_cast<T *>(distill_memory);
-    Teacher t = teacher_at(distill_memory + (size_t)p.slice * 16, p.top);
+    const Teacher t = teacher_at(distill_memory + (size_t)p.slice * 16, p.top);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const T *const base = z - at.skip;
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
         if (at.whole(first_piece + i)) {
@@ -266,25 +275,32 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
         }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    teacher_shares<T>(p, row, &room[0][0], t);
+    if (warp == 0) teacher_shares<T>(p, row, t, teacher);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
 
-    // the entries in this CTA's part: the largest, then out of the row
+    // the entries in this CTA's part are taken out of the row
     const int from = first_piece * E - at.skip, to = from + count * E;      // elements of the row
-    double most = -CUDART_INF, entries = 0.0, top_sum = 0.0;
+    const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
+    const bool with_entries = warp * 32 < p.top;
+    double entries = 0.0, top_max = -CUDART_INF, top_sum = 0.0;
+    teacher_places(t, p.top);
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.id[k] >= 0 && t.id[k] >= from && t.id[k] < to) {
+        if (here(t.id[k])) {
             const double v = (double)widen(held[t.id[k] - from]), share = t.p[k];
-            t.z[k] = v, most = fmax(most, v);
-            if (share != 0.0) entries += share * (teacher_value<T>(p, row, k) - t.top_max - t.log_sum - v * p.inv_t);
+            if (share != 0.0) entries += share * (t.z[k] - teacher.top_max - teacher.log_sum - v * p.inv_t);
+            t.z[k] = v, top_max = fmax(top_max, v);
         }
-    most = cta_max(most, room[2]);                            // and all of them have been read
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
-            top_sum += exp((t.z[k] - most) * p.inv_t);
-            held[t.place[k] - from] = narrow<T>(distill_floor<A>());
-        }
+    __syncthreads();                                          // all of them have been read
+    if (with_entries) {
+        top_max = distill_warp_max(top_max), entries = distill_warp_sum(entries);
+        for (int k = threadIdx.x; k < p.top; k += blockDim.x)
+            if (here(t.place[k])) {
+                held[t.place[k] - from] = narrow<T>(distill_floor<A>());
+                top_sum += exp((t.z[k] - top_max) * p.inv_t);
+            }
+        top_sum = distill_warp_sum(top_sum);
+    }
     __syncthreads();
 
     // all the rest: every thread keeps the largest so far and the sum relative to it
@@ -318,71 +334,63 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
         sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), joined(more));
         largest = top;
     }
-    // the CTA's
+    // the warp's, the CTA's
     A rest_max = largest;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) rest_max = larger(rest_max, __shfl_xor_sync(0xffffffffu, rest_max, o));
-    double rest_sum = sum == A(0) ? 0.0 : (double)(sum * distill_exp<T>((largest - rest_max) * unit));
+    A rest_sum = sum == A(0) ? A(0) : sum * distill_exp<T>((largest - rest_max) * unit);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
-        top_sum += __shfl_xor_sync(0xffffffffu, top_sum, o);
-        entries += __shfl_xor_sync(0xffffffffu, entries, o);
-    }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if (lane == 0) room[0][warp] = (double)rest_max, room[1][warp] = rest_sum, room[3][warp] = top_sum, room[4][warp] = entries;
+    for (int o = 16; o > 0; o >>= 1) rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
+    if (lane == 0) warp_parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
     __syncthreads();
     if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA has started
+    const int half = lane & 15;
     if (warp == 0) {
-        const bool in = lane < warps;
-        double m = in ? room[0][lane] : -CUDART_INF, s = in ? room[1][lane] : 0.0, ts = in ? room[3][lane] : 0.0, en = in ? room[4][lane] : 0.0;
-        double all = m;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) all = fmax(all, __shfl_xor_sync(0xffffffffu, all, o));
-        if (s != 0.0) s *= (double)distill_exp<T>(A(m - all) * unit);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            s += __shfl_xor_sync(0xffffffffu, s, o);
-            ts += __shfl_xor_sync(0xffffffffu, ts, o);
-            en += __shfl_xor_sync(0xffffffffu, en, o);
+        double m = -CUDART_INF, s = 0.0, en = 0.0;
+        if (half < warps) {
+            const DistillPart d = warp_parts[half];
+            m = lane < 16 ? d.rest_max : d.top_max, s = lane < 16 ? d.rest_sum : d.top_sum, en = d.entries;
         }
-        const double mine[5] = {all, s, most, ts, en};
-        if (cluster == 1) {
-            if (lane == 0) parts[0] = {all, s, most, ts, en};
-        } else if (lane < (int)cluster) {                     // lane k tells CTA k
-            unsigned to_peer;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_peer) : "r"((unsigned)__cvta_generic_to_shared(&parts[rank])), "r"(lane));
+        s = distill_halves(m, s, p.inv_t);
 #pragma unroll
-            for (int k = 0; k < 5; ++k)
-                asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer + 8 * k), "d"(mine[k]) : "memory");
+        for (int o = 8; o > 0; o >>= 1) en += __shfl_xor_sync(0xffffffffu, en, o);
+        // lanes k and 16 + k tell CTA k
+        if (cluster == 1) {
+            if (lane == 0) parts[0].rest_max = m, parts[0].rest_sum = s, parts[0].entries = en;
+            if (lane == 16) parts[0].top_max = m, parts[0].top_sum = s;
+        } else if (half < (int)cluster) {
+            unsigned to_peer;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_peer) : "r"((unsigned)__cvta_generic_to_shared(&parts[rank])), "r"(half));
+            to_peer += lane < 16 ? 0 : 16;
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer), "d"(m) : "memory");
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer + 8), "d"(s) : "memory");
+            if (lane < 16) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer + 32), "d"(en) : "memory");
         }
         __syncwarp();
     }
     if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    // the row's: lanes below 16 have the CTAs' rests, the others their entries
+    // the row's
     double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0;
     if (warp == 0) {
-        const int c = lane & 15;
         double m = -CUDART_INF, s = 0.0;
-        if (c < (int)cluster) m = lane < 16 ? parts[c].rest_max : parts[c].top_max, s = lane < 16 ? parts[c].rest_sum : parts[c].top_sum;
-        row_max = m;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) row_max = fmax(row_max, __shfl_xor_sync(0xffffffffu, row_max, o));
-        if (s != 0.0) s *= exp((m - row_max) * p.inv_t);
+        if (half < (int)cluster) m = lane < 16 ? parts[half].rest_max : parts[half].top_max, s = lane < 16 ? parts[half].rest_sum : parts[half].top_sum;
+        const double own = m;
+        row_max = distill_warp_max(m);
+        if (s != 0.0) s *= exp((own - row_max) * p.inv_t);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         rest_of_row = __shfl_sync(0xffffffffu, s, 0);
         total = rest_of_row + __shfl_sync(0xffffffffu, s, 16);
         for (int k = 0; k < (int)cluster; ++k) row_entries += parts[k].entries;
-        double factor = t.sum + t.rest;
-        if (t.rest > 0.0) factor -= t.rest * total / rest_of_row;
-        if (!(t.sum == t.sum)) factor = CUDART_NAN;           // an id outside the row
+        double factor = teacher.sum + teacher.rest;
+        if (teacher.rest > 0.0) factor -= teacher.rest * total / rest_of_row;
+        if (!(teacher.sum == teacher.sum)) factor = CUDART_NAN;           // an id outside the row
         if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor;
     }
     if constexpr (STEP) {
         __syncthreads();
         const A m = A(result[0]);
-        const double scale = (double)weight * p.inv_t, s_all = t.sum + t.rest;
+        const double scale = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
         const A coef = A(scale * result[2] / result[1]);
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
         const Two<A> less = both(-m), units = both(unit), coefs = both(coef);
@@ -401,7 +409,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
         }
         __syncthreads();                                      // the entries' places have been written with zeros
         for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-            if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
+            if (here(t.place[k])) {
                 const double q = exp((t.z[k] - result[0]) * p.inv_t) / result[1];
                 dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
             }
@@ -409,9 +417,9 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     // what only the loss needs comes last
     if (rank == 0 && threadIdx.x == 0) {
         const double log_total = row_max * p.inv_t + log(total);
-        double loss = t.sum != 0.0 ? row_entries + t.sum * log_total : 0.0;
-        if (t.rest > 0.0) loss += t.rest * log(t.rest * total / rest_of_row);        // P (log P - log Q)
-        if (!(t.sum == t.sum)) loss = CUDART_NAN;
+        double loss = teacher.sum != 0.0 ? row_entries + teacher.sum * log_total : 0.0;
+        if (teacher.rest > 0.0) loss += teacher.rest * log(teacher.rest * total / rest_of_row);        // P (log P - log Q)
+        if (!(teacher.sum == teacher.sum)) loss = CUDART_NAN;
         if (p.loss) static_cast<A *>(p.loss)[row] = A(loss);
         if (!STEP && p.stats) {
             A *const st = static_cast<A *>(p.stats);
@@ -427,7 +435,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T);
     extern __shared__ __align__(16) unsigned char distill_memory[];
-    __shared__ double room[2][32];
+    __shared__ TeacherSums teacher;
     wait_for_earlier();
     const long long row = blockIdx.x;
     const int first = (int)blockIdx.y * p.slice;
@@ -441,7 +449,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     const RowPieces<T> at(z, p.vocab);
     const T *const base = z - at.skip;
     const int last = min(first + p.slice, at.pieces);
-    Teacher t = teacher_at(distill_memory, p.top);
+    const Teacher t = teacher_at(distill_memory, p.top);
     constexpr int kTogether = 4;
     Packed<T, E> v[kTogether];
     auto fetch = [&](int i0) {
@@ -461,12 +469,15 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     fetch(first + threadIdx.x);
     const A *const stats = static_cast<const A *>(p.stats);
     const A m = stats[row], total = stats[p.rows + row], factor = stats[2 * p.rows + row];
-    teacher_shares<T>(p, row, &room[0][0], t);
+    if (threadIdx.x < 32) teacher_shares<T>(p, row, t, teacher);
+    __syncthreads();
+    teacher_places(t, p.top);
     const int from = first * E - at.skip, to = last * E - at.skip;
+    const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) t.z[k] = (double)widen(z[t.place[k]]);
+        if (here(t.place[k])) t.z[k] = (double)widen(z[t.place[k]]);
     __syncthreads();                                          // before anything is written: dz may be the logits
-    const double scale = (double)weight * p.inv_t, s_all = t.sum + t.rest;
+    const double scale = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
     // an id outside the row is one in the statistics too, and makes them NaN
     const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (double)factor / (double)total);
     const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
@@ -489,7 +500,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     }
     __syncthreads();
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (t.place[k] >= 0 && t.place[k] >= from && t.place[k] < to) {
+        if (here(t.place[k])) {
             const double q = exp((t.z[k] - (double)m) * p.inv_t) / (double)total;
             dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
         }
