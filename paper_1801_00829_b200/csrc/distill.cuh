@@ -263,16 +263,18 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     const Teacher t = teacher_at(distill_memory + (size_t)p.slice * 16, p.top);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const T *const base = z - at.skip;
-    for (int i = threadIdx.x; i < count; i += blockDim.x) {
-        if (at.whole(first_piece + i)) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(held + i * E)),
-                         "l"(base + (long long)(first_piece + i) * E) : "memory");
-        } else {
+    // whole pieces of this CTA's part: [begin, stop); of the others there is at most one at each end
+    const int begin = max(0, (at.skip ? 1 : 0) - first_piece), stop = max(begin, min(count, at.end / E - first_piece));
+    {
+        unsigned to = (unsigned)__cvta_generic_to_shared(held) + (begin + threadIdx.x) * 16;
+        const T *source = base + (long long)(first_piece + begin + threadIdx.x) * E;
+        for (int i = begin + threadIdx.x; i < stop; i += blockDim.x, to += blockDim.x * 16, source += blockDim.x * E)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(source) : "memory");
+        for (int i = threadIdx.x < 2 ? (threadIdx.x ? stop : 0) : count; i < count && (i < begin || i >= stop); i += count)
             for (int e = 0; e < E; ++e) {
                 const int j = (first_piece + i) * E + e;
                 held[i * E + e] = at.holds(j) ? base[j] : narrow<T>(distill_floor<A>());
             }
-        }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     if (warp == 0) teacher_shares<T>(p, row, t, teacher);
@@ -306,33 +308,36 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     // all the rest: every thread keeps the largest so far and the sum relative to it
     const A unit = distill_unit<T>(p.inv_t);
     A largest = distill_floor<A>(), sum = A(0);
-    constexpr int kTogether = 4;
-    for (int i0 = threadIdx.x; i0 < count; i0 += kTogether * blockDim.x) {
-        Packed<T, E> v[kTogether];
+    const Two<A> scale = both(unit);
+    auto take = [&](auto many, const uint4 *from16, int step) {
+        constexpr int M = many.value;
+        Packed<T, E> v[M];
         A top = largest;
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u) {
-            const int i = i0 + u * blockDim.x;
-            if (i < count) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(held + i * E);
-                v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
-                top = distill_largest<T>(v[u], top);
-            }
+        for (int u = 0; u < M; ++u) {
+            const uint4 w = from16[u * step];
+            v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
+            top = distill_largest<T>(v[u], top);
         }
         const A ref = top == distill_floor<A>() ? A(0) : top;
         Two<A> more = both(A(0));
-        const Two<A> less = both(-ref), scale = both(unit);
+        const Two<A> less = both(-ref);
 #pragma unroll
-        for (int u = 0; u < kTogether; ++u)
-            if (i0 + u * (int)blockDim.x < count) {
+        for (int u = 0; u < M; ++u)
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const Two<A> x = (v[u].get2(e) + less) * scale;
-                    more = more + two(distill_exp<T>(first(x)), distill_exp<T>(second(x)));
-                }
+            for (int e = 0; e < E; e += 2) {
+                const Two<A> x = (v[u].get2(e) + less) * scale;
+                more = more + two(distill_exp<T>(first(x)), distill_exp<T>(second(x)));
             }
         sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), joined(more));
         largest = top;
+    };
+    {
+        const int step = blockDim.x;
+        const uint4 *from16 = reinterpret_cast<const uint4 *>(held) + threadIdx.x;
+        int i = threadIdx.x;
+        for (; i + 3 * step < count; i += 4 * step, from16 += 4 * step) take(std::integral_constant<int, 4>(), from16, step);
+        for (; i < count; i += step, from16 += step) take(std::integral_constant<int, 1>(), from16, step);
     }
     // the warp's, the CTA's
     A rest_max = largest;
@@ -390,28 +395,36 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
     if constexpr (STEP) {
         __syncthreads();
         const A m = A(result[0]);
-        const double scale = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
-        const A coef = A(scale * result[2] / result[1]);
+        const double factor = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
+        const A coef = A(factor * result[2] / result[1]);
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
-        const Two<A> less = both(-m), units = both(unit), coefs = both(coef);
-#pragma unroll 2
-        for (int i = threadIdx.x; i < count; i += blockDim.x) {
+        const Two<A> less = both(-m), coefs = both(coef);
+        auto gradient = [&](int i) {
             Packed<T, E> v, out;
             if constexpr (sizeof(T) >= 4) out.clear();
-            const uint4 w = *reinterpret_cast<const uint4 *>(held + i * E);
+            const uint4 w = reinterpret_cast<const uint4 *>(held)[i];
             v.w[0] = w.x, v.w[1] = w.y, v.w[2] = w.z, v.w[3] = w.w;
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                const Two<A> x = (v.get2(e) + less) * units;
+                const Two<A> x = (v.get2(e) + less) * scale;
                 out.put2(e, two(distill_exp<T>(first(x)), distill_exp<T>(second(x))) * coefs);
             }
-            distill_put(at, first_piece + i, dz, alike, out);
+            return out;
+        };
+        int i = threadIdx.x;
+        if (alike) {
+            T *out = dz - at.skip + (long long)(first_piece + begin + threadIdx.x) * E;
+#pragma unroll 2
+            for (i = begin + threadIdx.x; i < stop; i += blockDim.x, out += blockDim.x * E) store16(out, gradient(i).w);
+            i = threadIdx.x < 2 ? (threadIdx.x ? stop : 0) : count;              // pieces that are not whole
+            if (i >= begin && i < stop) i = count;
         }
+        for (; i < count; i += alike ? count : blockDim.x) distill_put(at, first_piece + i, dz, alike, gradient(i));
         __syncthreads();                                      // the entries' places have been written with zeros
         for (int k = threadIdx.x; k < p.top; k += blockDim.x)
             if (here(t.place[k])) {
                 const double q = exp((t.z[k] - result[0]) * p.inv_t) / result[1];
-                dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
+                dz[t.place[k]] = narrow<T>(A(factor * (q * s_all - t.share[k])));
             }
     }
     // what only the loss needs comes last
