@@ -168,11 +168,10 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream);
  * values_type: `type`, or FO_F32 with a 16-bit type.  What concerns the entries is computed in 64 bits.
  * dz may be the logits themselves.  Any address of an element and any ld >= vocab works; fast are logits and dz whose rows lie at
  * the same offset from a 16-byte boundary.
- * top <= FO_DISTILL_MAX_TOP and vocab <= 2^27; a row of fused_distill and fused_distill_step has at most
- * FO_DISTILL_MAX_ROW_BYTES, else FO_ERR_UNSUPPORTED.
+ * top <= FO_DISTILL_MAX_TOP and vocab <= FO_DISTILL_MAX_VOCAB, else FO_ERR_UNSUPPORTED.
  */
 #define FO_DISTILL_MAX_TOP 1024
-#define FO_DISTILL_MAX_ROW_BYTES 1572864
+#define FO_DISTILL_MAX_VOCAB (1 << 20)
 
 typedef struct fo_distill {
     int64_t rows, vocab, top;

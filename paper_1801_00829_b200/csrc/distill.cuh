@@ -1,10 +1,11 @@
 // The distillation loss from a teacher's top logits and its gradient.
 //
-// Loss, or loss and gradient at once: a row of logits belongs to a cluster of 1 to 8 CTAs, whose shared memory holds it while the
-// sums are made and the gradient is written, so that it is read once.  The row lies there as it does in memory, at the same
-// offset from a 16-byte boundary, so that rows that begin anywhere move in whole 16-byte pieces but for their ends.  The entries' logits are
-// taken out of the row (and replaced by minus infinity) before the sum is made: what the teacher's entries leave is then added up by itself, not as
-// 1 minus their sum, and the entries, which hold most of the probability, are summed in 64 bits.
+// Loss, or loss and gradient at once: a CTA to a row, which it goes through once for the sums and a second time, backwards and
+// out of L2, for the gradient: what all CTAs of the GPU work on at once is smaller than that, and what is written is marked as
+// not needed again.  (Rows held in the shared memory of clusters were read once, but a cluster's exchange of its sums and the entries'
+// work in each of its CTAs took longer than the second reading: 4096 x 128000 in bfloat16 542 us.)  The entries' places are marked
+// in a map of bits and passed over in the sums: what the teacher's entries leave is added up by itself, not as 1 minus their sum, and
+// the entries, which hold most of the probability, are summed in 64 bits.
 // The gradient alone is elementwise from the saved statistics, a CTA to a part of a row.
 #pragma once
 
@@ -15,7 +16,7 @@
 
 namespace fo {
 
-constexpr int kDistillCta = 256;
+constexpr int kDistillCta = 512;
 
 struct DistillParams {
     long long rows;
@@ -60,19 +61,6 @@ __device__ __forceinline__ double distill_warp_max(double v)
     for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-// Sums s relative to maxima m, added up over each half of a warp (the rests', and the entries'): relative to each half's maximum,
-// which m becomes.
-__device__ __forceinline__ double distill_halves(double &m, double s, double inv_t)
-{
-    const double own = m;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (s != 0.0) s *= exp((own - m) * inv_t);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s;
-}
-
 // The teacher's entries of one row, in shared memory.
 struct Teacher {
     int *id;                            // -1: no entry; padded to a multiple of 4
@@ -223,102 +211,88 @@ __device__ __forceinline__ Acc<T> distill_largest(const Packed<T, 16 / sizeof(T)
     }
 }
 
-// What the CTAs of a cluster tell each other.
+// 16 bytes that are not needed again.
+__device__ __forceinline__ void store16_last(void *p, const uint32_t *w)
+{
+    asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+// A whole piece of logits, kept for the second time.
+template <class T>
+__device__ __forceinline__ Packed<T, 16 / sizeof(T)> distill_piece(const T *at)
+{
+    Packed<T, 16 / sizeof(T)> v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at) : "memory");
+    return v;
+}
+
 struct DistillPart {
     double rest_max, rest_sum, top_max, top_sum, entries;
 };
 
 template <class T, bool STEP>
-__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_kernel(const __grid_constant__ DistillParams p)
+__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 2) distill_kernel(const __grid_constant__ DistillParams p)
 {
     using A = Acc<T>;
-    constexpr int E = 16 / (int)sizeof(T);
+    constexpr int E = 16 / (int)sizeof(T), kTogether = 4;
     extern __shared__ __align__(16) unsigned char distill_memory[];
-    __shared__ DistillPart warp_parts[kDistillCta / 32], parts[8];
-    __shared__ double result[3];
+    __shared__ DistillPart parts[kDistillCta / 32];
+    __shared__ double result[5];
     __shared__ TeacherSums teacher;
-    unsigned rank, cluster;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
-    if (cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     wait_for_earlier();
-    const long long row = blockIdx.x / cluster;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, step = blockDim.x;
+    const long long row = blockIdx.x;
     const T *z = static_cast<const T *>(p.logits) + row * p.ld_logits;
     T *dz = STEP ? static_cast<T *>(p.dz) + row * p.ld_dz : nullptr;
-    const int first_piece = (int)rank * p.slice;
+    const Teacher t = teacher_at(distill_memory, p.top);
+    uint32_t *const marks = reinterpret_cast<uint32_t *>(distill_memory + (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes);
     A weight = A(1);
-    if (STEP) {
-        if (p.dloss) weight = static_cast<const A *>(p.dloss)[row];
-        if (weight == A(0)) {                                 // the row is not looked at
-            if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            // one piece more than the logits' can be the gradient's, at another offset: the last CTA has it
-            distill_zero(dz, p.vocab, first_piece, rank + 1 == cluster ? p.slice + 1 : p.slice);
-            if (rank == 0 && threadIdx.x == 0) static_cast<A *>(p.loss)[row] = A(0);
-            return;
-        }
-    }
+    if (STEP && p.dloss) weight = static_cast<const A *>(p.dloss)[row];
+    if (warp == 0) teacher_shares<T>(p, row, t, teacher);     // while the weight comes
     const RowPieces<T> at(z, p.vocab);
-    const int count = max(0, min(p.slice, at.pieces - first_piece));
-    T *const held = reinterpret_cast<T *>(distill_memory);
-    const Teacher t = teacher_at(distill_memory + (size_t)p.slice * 16, p.top);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const T *const base = z - at.skip;
-    // whole pieces of this CTA's part: [begin, stop); of the others there is at most one at each end
-    const int begin = max(0, (at.skip ? 1 : 0) - first_piece), stop = max(begin, min(count, at.end / E - first_piece));
-    {
-        unsigned to = (unsigned)__cvta_generic_to_shared(held) + (begin + threadIdx.x) * 16;
-        const T *source = base + (long long)(first_piece + begin + threadIdx.x) * E;
-        for (int i = begin + threadIdx.x; i < stop; i += blockDim.x, to += blockDim.x * 16, source += blockDim.x * E)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(source) : "memory");
-        for (int i = threadIdx.x < 2 ? (threadIdx.x ? stop : 0) : count; i < count && (i < begin || i >= stop); i += count)
-            for (int e = 0; e < E; ++e) {
-                const int j = (first_piece + i) * E + e;
-                held[i * E + e] = at.holds(j) ? base[j] : narrow<T>(distill_floor<A>());
-            }
+    if (STEP && weight == A(0)) {                             // the row is not looked at
+        distill_zero(dz, p.vocab, 0, at.pieces + 1);          // (the gradient's may be one piece more, at another offset)
+        if (threadIdx.x == 0) static_cast<A *>(p.loss)[row] = A(0);
+        return;
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    if (warp == 0) teacher_shares<T>(p, row, t, teacher);
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    for (int i = threadIdx.x; i < (at.end + 127) / 128; i += step) reinterpret_cast<uint4 *>(marks)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
 
-    // the entries in this CTA's part are taken out of the row
-    const int from = first_piece * E - at.skip, to = from + count * E;      // elements of the row
-    const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
-    const bool with_entries = warp * 32 < p.top;
+    // the entries: a mark at each place, and what they add
     double entries = 0.0, top_max = -CUDART_INF, top_sum = 0.0;
     teacher_places(t, p.top);
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (here(t.id[k])) {
-            const double v = (double)widen(held[t.id[k] - from]), share = t.p[k];
+    for (int k = threadIdx.x; k < p.top; k += step)
+        if (t.id[k] >= 0) {
+            const double v = (double)widen(z[t.id[k]]), share = t.p[k];
             if (share != 0.0) entries += share * (t.z[k] - teacher.top_max - teacher.log_sum - v * p.inv_t);
             t.z[k] = v, top_max = fmax(top_max, v);
+            const int place = at.skip + t.id[k];
+            atomicOr(&marks[place >> 5], 1u << (place & 31));
         }
-    __syncthreads();                                          // all of them have been read
-    if (with_entries) {
+    if (warp * 32 < p.top) {
         top_max = distill_warp_max(top_max), entries = distill_warp_sum(entries);
-        for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-            if (here(t.place[k])) {
-                held[t.place[k] - from] = narrow<T>(distill_floor<A>());
-                top_sum += exp((t.z[k] - top_max) * p.inv_t);
-            }
+        for (int k = threadIdx.x; k < p.top; k += step)
+            if (t.place[k] >= 0) top_sum += exp((t.z[k] - top_max) * p.inv_t);
         top_sum = distill_warp_sum(top_sum);
     }
     __syncthreads();
 
     // all the rest: every thread keeps the largest so far and the sum relative to it
     const A unit = distill_unit<T>(p.inv_t);
-    A largest = distill_floor<A>(), sum = A(0);
     const Two<A> scale = both(unit);
-    auto take = [&](auto many, const uint4 *from16, int step) {
+    A largest = distill_floor<A>(), sum = A(0);
+    auto marked = [&](int i) { return (marks[i * E >> 5] >> (i * E & 31)) & ((1u << E) - 1u); };
+    auto without = [&](Packed<T, E> v, unsigned bits) {       // minus infinity at the marked places
+        Packed<T, E> r;
+        r.clear();
+#pragma unroll
+        for (int e = 0; e < E; ++e) r.put(e, (bits >> e) & 1u ? narrow<T>(distill_floor<A>()) : v.raw(e));
+        return r;
+    };
+    auto take = [&](auto many, const Packed<T, E> *v) {
         constexpr int M = many.value;
-        Packed<T, E> v[M];
         A top = largest;
 #pragma unroll
-        for (int u = 0; u < M; ++u) {
-            const uint4 w = from16[u * step];
-            v[u].w[0] = w.x, v[u].w[1] = w.y, v[u].w[2] = w.z, v[u].w[3] = w.w;
-            top = distill_largest<T>(v[u], top);
-        }
+        for (int u = 0; u < M; ++u) top = distill_largest<T>(v[u], top);
         const A ref = top == distill_floor<A>() ? A(0) : top;
         Two<A> more = both(A(0));
         const Two<A> less = both(-ref);
@@ -332,78 +306,77 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
         sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), joined(more));
         largest = top;
     };
+    // whole pieces of the row: [begin, stop); of the others there is at most one at each end
+    const T *const base = z - at.skip;
+    const int begin = at.skip ? 1 : 0, stop = max(begin, at.end / E), mine = begin + threadIdx.x;
     {
-        const int step = blockDim.x;
-        const uint4 *from16 = reinterpret_cast<const uint4 *>(held) + threadIdx.x;
-        int i = threadIdx.x;
-        for (; i + 3 * step < count; i += 4 * step, from16 += 4 * step) take(std::integral_constant<int, 4>(), from16, step);
-        for (; i < count; i += step, from16 += step) take(std::integral_constant<int, 1>(), from16, step);
+        int i = mine;
+        const T *from = base + (long long)i * E;
+        for (; i + (kTogether - 1) * step < stop; i += kTogether * step, from += (long long)kTogether * step * E) {
+            Packed<T, E> v[kTogether];
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) v[u] = distill_piece(from + (long long)u * step * E);
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) {
+                const unsigned bits = marked(i + u * step);
+                if (bits) v[u] = without(v[u], bits);
+            }
+            take(std::integral_constant<int, kTogether>(), v);
+        }
+        for (; i < stop; i += step, from += (long long)step * E) {
+            Packed<T, E> v = distill_piece(from);
+            const unsigned bits = marked(i);
+            if (bits) v = without(v, bits);
+            take(std::integral_constant<int, 1>(), &v);
+        }
     }
-    // the warp's, the CTA's
+    // pieces that are not whole: their elements outside the row are minus infinity
+    auto ragged = [&](int i) {
+        Packed<T, E> v;
+        v.clear();
+#pragma unroll
+        for (int e = 0; e < E; ++e) v.put(e, at.holds(i * E + e) ? base[i * E + e] : narrow<T>(distill_floor<A>()));
+        return v;
+    };
+    const int other = threadIdx.x == 0 ? (begin ? 0 : at.pieces) : threadIdx.x == 1 ? stop : at.pieces;
+    const bool ends = other < at.pieces && (other < begin || other >= stop);
+    if (ends) {
+        const Packed<T, E> v = without(ragged(other), marked(other));
+        take(std::integral_constant<int, 1>(), &v);
+    }
+    // the warp's
     A rest_max = largest;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) rest_max = larger(rest_max, __shfl_xor_sync(0xffffffffu, rest_max, o));
     A rest_sum = sum == A(0) ? A(0) : sum * distill_exp<T>((largest - rest_max) * unit);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
-    if (lane == 0) warp_parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
+    if (lane == 0) parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
     __syncthreads();
-    if (cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA has started
-    const int half = lane & 15;
-    if (warp == 0) {
-        double m = -CUDART_INF, s = 0.0, en = 0.0;
-        if (half < warps) {
-            const DistillPart d = warp_parts[half];
-            m = lane < 16 ? d.rest_max : d.top_max, s = lane < 16 ? d.rest_sum : d.top_sum, en = d.entries;
-        }
-        s = distill_halves(m, s, p.inv_t);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) en += __shfl_xor_sync(0xffffffffu, en, o);
-        // lanes k and 16 + k tell CTA k
-        if (cluster == 1) {
-            if (lane == 0) parts[0].rest_max = m, parts[0].rest_sum = s, parts[0].entries = en;
-            if (lane == 16) parts[0].top_max = m, parts[0].top_sum = s;
-        } else if (half < (int)cluster) {
-            unsigned to_peer;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_peer) : "r"((unsigned)__cvta_generic_to_shared(&parts[rank])), "r"(half));
-            to_peer += lane < 16 ? 0 : 16;
-            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer), "d"(m) : "memory");
-            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer + 8), "d"(s) : "memory");
-            if (lane < 16) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to_peer + 32), "d"(en) : "memory");
-        }
-        __syncwarp();
-    }
-    if (cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     // the row's
     double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0;
     if (warp == 0) {
-        double m = -CUDART_INF, s = 0.0;
-        if (half < (int)cluster) m = lane < 16 ? parts[half].rest_max : parts[half].top_max, s = lane < 16 ? parts[half].rest_sum : parts[half].top_sum;
-        const double own = m;
-        row_max = distill_warp_max(m);
-        if (s != 0.0) s *= exp((own - row_max) * p.inv_t);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        rest_of_row = __shfl_sync(0xffffffffu, s, 0);
-        total = rest_of_row + __shfl_sync(0xffffffffu, s, 16);
-        for (int k = 0; k < (int)cluster; ++k) row_entries += parts[k].entries;
+        DistillPart d = {-CUDART_INF, 0.0, -CUDART_INF, 0.0, 0.0};
+        if (lane < warps) d = parts[lane];
+        row_max = distill_warp_max(fmax(d.rest_max, d.top_max));
+        if (d.rest_sum != 0.0) rest_of_row = d.rest_sum * (double)distill_exp<T>(A(d.rest_max - row_max) * unit);
+        rest_of_row = distill_warp_sum(rest_of_row);
+        total = rest_of_row + distill_warp_sum(d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - row_max) * p.inv_t) : 0.0);
+        row_entries = distill_warp_sum(d.entries);
         double factor = teacher.sum + teacher.rest;
         if (teacher.rest > 0.0) factor -= teacher.rest * total / rest_of_row;
         if (!(teacher.sum == teacher.sum)) factor = CUDART_NAN;           // an id outside the row
-        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor;
+        const double inverse = 1.0 / total;
+        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor, result[3] = inverse, result[4] = (double)weight * p.inv_t * factor * inverse;
     }
     if constexpr (STEP) {
         __syncthreads();
-        const A m = A(result[0]);
-        const double factor = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
-        const A coef = A(factor * result[2] / result[1]);
+        const A m = A(result[0]), coef = A(result[4]);
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
         const Two<A> less = both(-m), coefs = both(coef);
-        auto gradient = [&](int i) {
-            Packed<T, E> v, out;
+        auto gradient = [&](const Packed<T, E> &v) {
+            Packed<T, E> out;
             if constexpr (sizeof(T) >= 4) out.clear();
-            const uint4 w = reinterpret_cast<const uint4 *>(held)[i];
-            v.w[0] = w.x, v.w[1] = w.y, v.w[2] = w.z, v.w[3] = w.w;
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
                 const Two<A> x = (v.get2(e) + less) * scale;
@@ -411,24 +384,35 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 2 : 5) distill_k
             }
             return out;
         };
-        int i = threadIdx.x;
+        // what was read last is read first
+        int i = mine + (stop - 1 - mine) / step * step;
+        if (stop - 1 < mine) i = -1;
         if (alike) {
-            T *out = dz - at.skip + (long long)(first_piece + begin + threadIdx.x) * E;
-#pragma unroll 2
-            for (i = begin + threadIdx.x; i < stop; i += blockDim.x, out += blockDim.x * E) store16(out, gradient(i).w);
-            i = threadIdx.x < 2 ? (threadIdx.x ? stop : 0) : count;              // pieces that are not whole
-            if (i >= begin && i < stop) i = count;
+            const T *from = base + (long long)i * E;
+            T *to = dz - at.skip + (long long)i * E;
+            const long long back = (long long)step * E;
+            for (; i - (kTogether - 1) * step >= begin; i -= kTogether * step, from -= kTogether * back, to -= kTogether * back) {
+                Packed<T, E> v[kTogether];
+#pragma unroll
+                for (int u = 0; u < kTogether; ++u) v[u] = distill_piece(from - u * back);
+#pragma unroll
+                for (int u = 0; u < kTogether; ++u) store16_last(to - u * back, gradient(v[u]).w);
+            }
+            for (; i >= begin; i -= step, from -= back, to -= back) store16_last(to, gradient(distill_piece(from)).w);
+        } else {
+            for (; i >= begin; i -= step) distill_put(at, i, dz, false, gradient(distill_piece(base + (long long)i * E)));
         }
-        for (; i < count; i += alike ? count : blockDim.x) distill_put(at, first_piece + i, dz, alike, gradient(i));
-        __syncthreads();                                      // the entries' places have been written with zeros
-        for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-            if (here(t.place[k])) {
-                const double q = exp((t.z[k] - result[0]) * p.inv_t) / result[1];
-                dz[t.place[k]] = narrow<T>(A(factor * (q * s_all - t.share[k])));
+        if (ends) distill_put(at, other, dz, false, gradient(ragged(other)));
+        __syncthreads();                                      // the entries' places have been written like the others
+        const double by = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
+        for (int k = threadIdx.x; k < p.top; k += step)
+            if (t.place[k] >= 0) {
+                const double q = exp((t.z[k] - result[0]) * p.inv_t) * result[3];
+                dz[t.place[k]] = narrow<T>(A(by * (q * s_all - t.share[k])));
             }
     }
     // what only the loss needs comes last
-    if (rank == 0 && threadIdx.x == 0) {
+    if (threadIdx.x == 0) {
         const double log_total = row_max * p.inv_t + log(total);
         double loss = teacher.sum != 0.0 ? row_entries + teacher.sum * log_total : 0.0;
         if (teacher.rest > 0.0) loss += teacher.rest * log(teacher.rest * total / rest_of_row);        // P (log P - log Q)

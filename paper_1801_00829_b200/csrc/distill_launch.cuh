@@ -1,4 +1,4 @@
-// How rows are spread over CTAs and clusters, for one element type.
+// How rows are spread over CTAs, for one element type.
 #pragma once
 
 #include "distill.cuh"
@@ -6,21 +6,20 @@
 
 namespace fo {
 
-constexpr int kDistillMostBytes = 196640;                 // of a row in one CTA's shared memory
-
 template <class T, bool STEP>
-cudaError_t distill_row_launch(DistillParams p, cudaStream_t st)
+cudaError_t distill_row_launch(const DistillParams &p, cudaStream_t st)
 {
     static OncePerGpu once;
-    cudaError_t e = once.allow(distill_kernel<T, STEP>, kDistillMostBytes + kTeacherBytes * FO_DISTILL_MAX_TOP);
+    constexpr size_t most = FO_DISTILL_MAX_VOCAB / 8 + 16 + kTeacherBytes * FO_DISTILL_MAX_TOP;
+    const cudaError_t e = once.allow(distill_kernel<T, STEP>, most);
     if (e != cudaSuccess) return e;
-    // a row may begin anywhere in its first piece
-    const long long pieces = ((long long)p.vocab * (int)sizeof(T) + 15 - (int)sizeof(T)) / 16 + 1;
-    int cluster = 1;
-    while (cluster < 8 && (pieces + cluster - 1) / cluster > 32768 / 16) cluster *= 2;
-    p.slice = (int)((pieces + cluster - 1) / cluster);
-    const int threads = p.slice >= 512 ? kDistillCta : 128;
-    return launch_beside(distill_kernel<T, STEP>, dim3((unsigned)(p.rows * cluster)), threads, st, (size_t)p.slice * 16 + (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes, p, cluster);
+    // the entries, and a bit for each of the row's places and those before it in its first piece
+    const size_t shared = (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes + (size_t)(p.vocab + 16 / (int)sizeof(T) - 1 + 127) / 128 * 16;
+    // four pieces a thread, or more
+    const int pieces = (int)(((long long)p.vocab * (int)sizeof(T) + 15) / 16);
+    int threads = 64;
+    while (threads < kDistillCta && threads * 4 < pieces) threads *= 2;
+    return launch_beside(distill_kernel<T, STEP>, dim3((unsigned)p.rows), threads, st, shared, p);
 }
 
 template <class T>
