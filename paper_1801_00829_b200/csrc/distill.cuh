@@ -16,7 +16,7 @@
 
 namespace fo {
 
-constexpr int kDistillCta = 512;
+constexpr int kDistillCta = 256;
 
 struct DistillParams {
     long long rows;
@@ -64,17 +64,17 @@ __device__ __forceinline__ double distill_warp_max(double v)
 // The teacher's entries of one row, in shared memory.
 struct Teacher {
     int *id;                            // -1: no entry; padded to a multiple of 4
-    double *p, *share, *z;              // shares, those of a place, and the student's logits
+    double *p, *share, *z, *v;          // shares, those of a place, the student's logits, and the teacher's over temperature
     int *place;                         // of an entry that is the first of its place; -1
 };
 
-constexpr int kTeacherBytes = 32;       // of an entry in shared memory
+constexpr int kTeacherBytes = 40;       // of an entry in shared memory
 __device__ __forceinline__ Teacher teacher_at(void *memory, int top)
 {
     const int room = (top + 3) / 4 * 4;
     Teacher t;
-    t.p = static_cast<double *>(memory), t.share = t.p + room, t.z = t.share + room;
-    t.id = reinterpret_cast<int *>(t.z + room), t.place = t.id + room;
+    t.p = static_cast<double *>(memory), t.share = t.p + room, t.z = t.share + room, t.v = t.z + room;
+    t.id = reinterpret_cast<int *>(t.v + room), t.place = t.id + room;
     return t;
 }
 
@@ -91,29 +91,35 @@ struct TeacherSums {
     double top_max, log_sum;            // log p = v / temperature - top_max - log_sum
     double sum, rest;                   // of p, and P
 };
-// The first warp's part: ids, shares and their sums.  An id that is no place of the row makes the sum NaN, and with it everything.
+// All threads: the entries as they lie in memory.  An id that is no place of the row makes the sum of the shares NaN, and with it
+// everything.
 template <class T>
-__device__ __forceinline__ void teacher_shares(const DistillParams &p, long long row, const Teacher &t, TeacherSums &out)
+__device__ __forceinline__ void teacher_read(const DistillParams &p, long long row, const Teacher &t)
 {
-    const int lane = threadIdx.x & 31;
-    double most = -CUDART_INF, sum = 0.0;
-    bool bad = false;
-    for (int k = lane; k < p.top; k += 32) {
+    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
         const long long at = row * p.ld_ids + k;
         const long long id = p.ids_long ? static_cast<const long long *>(p.ids)[at] : static_cast<const int *>(p.ids)[at];
-        const double v = teacher_value<T>(p, row, k);
-        t.id[k] = id < 0 || id >= p.vocab ? -1 : (int)id;
-        t.z[k] = v;
-        bad = bad || id >= p.vocab;
-        if (id >= 0) most = fmax(most, v);
+        t.v[k] = id >= p.vocab ? CUDART_NAN : teacher_value<T>(p, row, k);
+        t.id[k] = id < 0 ? -1 : id >= p.vocab ? -2 : (int)id;
     }
-    if (lane < ((4 - p.top % 4) & 3)) t.id[p.top + lane] = -1;
-    const double reference = p.tail ? (double)static_cast<const Acc<T> *>(p.tail)[row] : distill_warp_max(most);
+    if (threadIdx.x < ((4 - p.top % 4) & 3)) t.id[p.top + threadIdx.x] = -1;
+}
+// The first warp, after a barrier: shares and their sums.  tail: the row's.
+__device__ __forceinline__ void teacher_shares(const DistillParams &p, const Teacher &t, double tail, TeacherSums &out)
+{
+    const int lane = threadIdx.x & 31;
+    double reference = tail, sum = 0.0;
+    if (!p.tail) {
+        reference = -CUDART_INF;
+        for (int k = lane; k < p.top; k += 32)
+            if (t.id[k] >= 0) reference = fmax(reference, t.v[k]);
+        reference = distill_warp_max(reference);
+    }
     for (int k = lane; k < p.top; k += 32) {
-        const double e = t.id[k] >= 0 ? exp(t.z[k] - reference) : 0.0;
+        const double e = t.id[k] == -1 ? 0.0 : exp(t.v[k] - reference);
         t.p[k] = e, sum += e;
     }
-    sum = distill_warp_sum(bad ? CUDART_NAN : sum);
+    sum = distill_warp_sum(sum);
     TeacherSums s = {reference, 0.0, sum, 0.0};
     if (p.tail) {
         s.rest = sum < 1.0 ? 1.0 - sum : sum >= 1.0 ? 0.0 : sum;
@@ -124,32 +130,39 @@ __device__ __forceinline__ void teacher_shares(const DistillParams &p, long long
     }
     if (lane == 0) out = s;
 }
-// Of entries with the same place the first one takes the shares of all, the others have no place.
-__device__ __forceinline__ void teacher_places(const Teacher &t, int top)
+// Meanwhile, from the last thread on: the student's logits, and of entries with the same place the first one (place; the others have
+// none).
+template <class T>
+__device__ __forceinline__ void teacher_places(const Teacher &t, int top, const T *z)
 {
-    for (int k = threadIdx.x; k < top; k += blockDim.x) {
+    for (int k = blockDim.x - 1 - threadIdx.x; k < top; k += blockDim.x) {
         const int id = t.id[k];
-        t.share[k] = t.p[k], t.place[k] = id;
-        if (id < 0) continue;
-        int same = 0, first = k;
+        const double own = id >= 0 ? (double)widen(z[id]) : 0.0;
+        bool again = false;
         const int4 *const four = reinterpret_cast<const int4 *>(t.id);
 #pragma unroll 4
-        for (int j = 0; j < (top + 3) / 4; ++j) {
+        for (int j = 0; j < (k + 3) / 4; ++j) {
             const int4 v = four[j];
-            const int hits = (v.x == id) | (v.y == id) << 1 | (v.z == id) << 2 | (v.w == id) << 3;
-            same += __popc(hits);
-            if (hits) first = min(first, 4 * j + __ffs(hits) - 1);
+            again = again || (v.x == id && 4 * j < k) || (v.y == id && 4 * j + 1 < k) || (v.z == id && 4 * j + 2 < k) || (v.w == id && 4 * j + 3 < k);
         }
-        if (same == 1) continue;
-        if (first != k) {
-            t.place[k] = -1;
-            continue;
-        }
-        double all = 0.0;
-        for (int j = 0; j < top; ++j)
-            if (t.id[j] == id) all += t.p[j];
-        t.share[k] = all;
+        t.place[k] = again || id < 0 ? -1 : id;
+        t.z[k] = own;
     }
+}
+// After another barrier: the share of the first entry of a place, which is that of all of them.
+__device__ __forceinline__ double teacher_share(const Teacher &t, int top, int k)
+{
+    double all = t.p[k];
+    const int id = t.id[k];
+    const int4 *const four = reinterpret_cast<const int4 *>(t.id);
+#pragma unroll 4
+    for (int j = k / 4; j < (top + 3) / 4; ++j) {
+        const int4 v = four[j];
+        if (v.x == id || v.y == id || v.z == id || v.w == id)
+            for (int q = max(k + 1, 4 * j); q < min(top, 4 * j + 4); ++q)
+                if (t.id[q] == id) all += t.p[q];
+    }
+    return all;
 }
 
 // Where a row lies: pieces of 16 bytes from the boundary before its first element.
@@ -230,7 +243,7 @@ struct DistillPart {
 };
 
 template <class T, bool STEP>
-__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 2) distill_kernel(const __grid_constant__ DistillParams p)
+__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_kernel(const __grid_constant__ DistillParams p)
 {
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T), kTogether = 4;
@@ -247,34 +260,54 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 2) distill_k
     uint32_t *const marks = reinterpret_cast<uint32_t *>(distill_memory + (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes);
     A weight = A(1);
     if (STEP && p.dloss) weight = static_cast<const A *>(p.dloss)[row];
-    if (warp == 0) teacher_shares<T>(p, row, t, teacher);     // while the weight comes
+    const double tail = p.tail ? (double)static_cast<const A *>(p.tail)[row] : 0.0;
+    teacher_read<T>(p, row, t);
     const RowPieces<T> at(z, p.vocab);
     if (STEP && weight == A(0)) {                             // the row is not looked at
         distill_zero(dz, p.vocab, 0, at.pieces + 1);          // (the gradient's may be one piece more, at another offset)
         if (threadIdx.x == 0) static_cast<A *>(p.loss)[row] = A(0);
         return;
     }
-    for (int i = threadIdx.x; i < (at.end + 127) / 128; i += step) reinterpret_cast<uint4 *>(marks)[i] = make_uint4(0, 0, 0, 0);
+    // whole pieces of the row: [begin, stop); of the others there is at most one at each end
+    const T *const base = z - at.skip;
+    const int begin = at.skip ? 1 : 0, stop = max(begin, at.end / E), mine = begin + threadIdx.x;
+    int i = mine;
+    const T *from = base + (long long)i * E;
+    Packed<T, E> next[kTogether];                             // the first pieces are on their way while the entries are seen to
+    auto fetch = [&]() {
+        if (i + (kTogether - 1) * step < stop)
+#pragma unroll
+            for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from + (long long)u * step * E);
+    };
+    fetch();
+    for (int k = threadIdx.x; k < (at.end + 127) / 128; k += step) reinterpret_cast<uint4 *>(marks)[k] = make_uint4(0, 0, 0, 0);
     __syncthreads();
 
     // the entries: a mark at each place, and what they add
-    double entries = 0.0, top_max = -CUDART_INF, top_sum = 0.0;
-    teacher_places(t, p.top);
-    for (int k = threadIdx.x; k < p.top; k += step)
-        if (t.id[k] >= 0) {
-            const double v = (double)widen(z[t.id[k]]), share = t.p[k];
-            if (share != 0.0) entries += share * (t.z[k] - teacher.top_max - teacher.log_sum - v * p.inv_t);
-            t.z[k] = v, top_max = fmax(top_max, v);
-            const int place = at.skip + t.id[k];
+    if (warp == 0) teacher_shares(p, t, tail, teacher);
+    teacher_places(t, p.top, z);
+    for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+        if (t.place[k] >= 0) {
+            const int place = at.skip + t.place[k];
             atomicOr(&marks[place >> 5], 1u << (place & 31));
         }
-    if (warp * 32 < p.top) {
+    __syncthreads();
+    double entries = 0.0, top_max = -CUDART_INF, top_sum = 0.0;
+    if ((warps - 1 - warp) * 32 < p.top) {
+        for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+            if (t.id[k] >= 0) {
+                const double share = t.p[k];
+                if (share != 0.0) entries += share * (t.v[k] - teacher.top_max - teacher.log_sum - t.z[k] * p.inv_t);
+                if (t.place[k] >= 0) top_max = fmax(top_max, t.z[k]);
+            }
         top_max = distill_warp_max(top_max), entries = distill_warp_sum(entries);
-        for (int k = threadIdx.x; k < p.top; k += step)
-            if (t.place[k] >= 0) top_sum += exp((t.z[k] - top_max) * p.inv_t);
+        for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+            if (t.place[k] >= 0) {
+                top_sum += exp((t.z[k] - top_max) * p.inv_t);
+                if (STEP) t.share[k] = teacher_share(t, p.top, k);
+            }
         top_sum = distill_warp_sum(top_sum);
     }
-    __syncthreads();
 
     // all the rest: every thread keeps the largest so far and the sum relative to it
     const A unit = distill_unit<T>(p.inv_t);
@@ -306,19 +339,17 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 2) distill_k
         sum = fused_ma(sum, distill_exp<T>((largest - ref) * unit), joined(more));
         largest = top;
     };
-    // whole pieces of the row: [begin, stop); of the others there is at most one at each end
-    const T *const base = z - at.skip;
-    const int begin = at.skip ? 1 : 0, stop = max(begin, at.end / E), mine = begin + threadIdx.x;
     {
-        int i = mine;
-        const T *from = base + (long long)i * E;
-        for (; i + (kTogether - 1) * step < stop; i += kTogether * step, from += (long long)kTogether * step * E) {
+        while (i + (kTogether - 1) * step < stop) {
             Packed<T, E> v[kTogether];
+            const int now = i;
 #pragma unroll
-            for (int u = 0; u < kTogether; ++u) v[u] = distill_piece(from + (long long)u * step * E);
+            for (int u = 0; u < kTogether; ++u) v[u] = next[u];
+            i += kTogether * step, from += (long long)kTogether * step * E;
+            fetch();
 #pragma unroll
             for (int u = 0; u < kTogether; ++u) {
-                const unsigned bits = marked(i + u * step);
+                const unsigned bits = marked(now + u * step);
                 if (bits) v[u] = without(v[u], bits);
             }
             take(std::integral_constant<int, kTogether>(), v);
@@ -385,18 +416,27 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 2) distill_k
             return out;
         };
         // what was read last is read first
-        int i = mine + (stop - 1 - mine) / step * step;
+        i = mine + (stop - 1 - mine) / step * step;
         if (stop - 1 < mine) i = -1;
         if (alike) {
-            const T *from = base + (long long)i * E;
+            from = base + (long long)i * E;
             T *to = dz - at.skip + (long long)i * E;
             const long long back = (long long)step * E;
-            for (; i - (kTogether - 1) * step >= begin; i -= kTogether * step, from -= kTogether * back, to -= kTogether * back) {
+            auto fetch_back = [&]() {
+                if (i - (kTogether - 1) * step >= begin)
+#pragma unroll
+                    for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from - u * back);
+            };
+            fetch_back();
+            while (i - (kTogether - 1) * step >= begin) {
                 Packed<T, E> v[kTogether];
 #pragma unroll
-                for (int u = 0; u < kTogether; ++u) v[u] = distill_piece(from - u * back);
+                for (int u = 0; u < kTogether; ++u) v[u] = next[u];
+                i -= kTogether * step, from -= kTogether * back;
+                fetch_back();
 #pragma unroll
                 for (int u = 0; u < kTogether; ++u) store16_last(to - u * back, gradient(v[u]).w);
+                to -= kTogether * back;
             }
             for (; i >= begin; i -= step, from -= back, to -= back) store16_last(to, gradient(distill_piece(from)).w);
         } else {
@@ -466,14 +506,14 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     fetch(first + threadIdx.x);
     const A *const stats = static_cast<const A *>(p.stats);
     const A m = stats[row], total = stats[p.rows + row], factor = stats[2 * p.rows + row];
-    if (threadIdx.x < 32) teacher_shares<T>(p, row, t, teacher);
+    teacher_read<T>(p, row, t);
+    const double tail = p.tail ? (double)static_cast<const A *>(p.tail)[row] : 0.0;
     __syncthreads();
-    teacher_places(t, p.top);
+    if (threadIdx.x < 32) teacher_shares(p, t, tail, teacher);
+    teacher_places(t, p.top, z);                              // before anything is written: dz may be the logits
     const int from = first * E - at.skip, to = last * E - at.skip;
     const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x)
-        if (here(t.place[k])) t.z[k] = (double)widen(z[t.place[k]]);
-    __syncthreads();                                          // before anything is written: dz may be the logits
+    __syncthreads();
     const double scale = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
     // an id outside the row is one in the statistics too, and makes them NaN
     const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (double)factor / (double)total);
@@ -499,7 +539,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
         if (here(t.place[k])) {
             const double q = exp((t.z[k] - (double)m) * p.inv_t) / (double)total;
-            dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - t.share[k])));
+            dz[t.place[k]] = narrow<T>(A(scale * (q * s_all - teacher_share(t, p.top, k))));
         }
 }
 

@@ -15,10 +15,10 @@ cudaError_t distill_row_launch(const DistillParams &p, cudaStream_t st)
     if (e != cudaSuccess) return e;
     // the entries, and a bit for each of the row's places and those before it in its first piece
     const size_t shared = (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes + (size_t)(p.vocab + 16 / (int)sizeof(T) - 1 + 127) / 128 * 16;
-    // four pieces a thread, or more
+    // eight pieces a thread, or more: what a row costs besides is hidden by other rows on the SM
     const int pieces = (int)(((long long)p.vocab * (int)sizeof(T) + 15) / 16);
     int threads = 64;
-    while (threads < kDistillCta && threads * 4 < pieces) threads *= 2;
+    while (threads < kDistillCta && threads * 8 < pieces) threads *= 2;
     return launch_beside(distill_kernel<T, STEP>, dim3((unsigned)p.rows), threads, st, shared, p);
 }
 
