@@ -1,11 +1,11 @@
 // The distillation loss from a teacher's top logits and its gradient.
 //
-// Loss, or loss and gradient at once: a CTA to a row, which it goes through once for the sums and a second time, backwards and
-// out of L2, for the gradient: what all CTAs of the GPU work on at once is smaller than that, and what is written is marked as
-// not needed again.  (Rows held in the shared memory of clusters were read once, but a cluster's exchange of its sums and the entries'
-// work in each of its CTAs took longer than the second reading: 4096 x 128000 in bfloat16 542 us.)  The entries' places are marked
-// in a map of bits and passed over in the sums: what the teacher's entries leave is added up by itself, not as 1 minus their sum, and
-// the entries, which hold most of the probability, are summed in 64 bits.
+// Loss, or loss and gradient at once: a CTA, or of short rows a team of its warps, goes through a row once for the sums and a second
+// time, backwards, for the gradient; the first time the row is marked to be kept in L2, the second time, and what is written, as not
+// needed again (4096 x 128000 in bfloat16 494 us, without the marks 571: of the second reading 0.45 hit L2, without them none).  Rows
+// kept in the shared memory of clusters are read once, but leave room for few CTAs, and what they do besides reading and writing is then
+// not hidden (542 us).  The entries' places are marked in a map of bits and passed over in the sums: what the teacher's entries leave is
+// added up by itself, not as 1 minus their sum, and the entries, which hold most of the probability, are summed in 64 bits.
 // The gradient alone is elementwise from the saved statistics, a CTA to a part of a row.
 #pragma once
 
@@ -16,13 +16,16 @@
 
 namespace fo {
 
-constexpr int kDistillCta = 256;
+// Threads of a CTA, of which three work on an SM; of a row where there are few rows; and the bound on threads that keeps registers
+// for 3 x 256 of them.
+constexpr int kDistillCta = 256, kDistillRow = 512, kDistillBound = 768;
 
 struct DistillParams {
     long long rows;
     int vocab, top;
     int ids_long, wide_values;
-    int slice;                          // pieces of a CTA
+    int slice;                          // pieces of a CTA (gradient)
+    int team, shared;                   // threads of a row, and their shared memory
     long long ld_logits, ld_ids, ld_values, ld_dz;
     const void *logits, *ids, *values, *tail, *dloss;
     void *loss, *stats, *dz;
@@ -48,6 +51,16 @@ template <class A> __device__ __forceinline__ A distill_floor() { return -A(CUDA
 
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+
+// The threads of one row: a CTA's, or a part of them that has barriers of its own.
+struct Team {
+    int thread, threads, number;        // this thread, all of them, and the team's number in its CTA
+    __device__ __forceinline__ void sync() const
+    {
+        if (threads == 32) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(number + 1), "r"(threads) : "memory");
+    }
+};
 
 __device__ __forceinline__ double distill_warp_sum(double v)
 {
@@ -94,15 +107,15 @@ struct TeacherSums {
 // All threads: the entries as they lie in memory.  An id that is no place of the row makes the sum of the shares NaN, and with it
 // everything.
 template <class T>
-__device__ __forceinline__ void teacher_read(const DistillParams &p, long long row, const Teacher &t)
+__device__ __forceinline__ void teacher_read(const DistillParams &p, long long row, const Teacher &t, const Team &team)
 {
-    for (int k = threadIdx.x; k < p.top; k += blockDim.x) {
+    for (int k = team.thread; k < p.top; k += team.threads) {
         const long long at = row * p.ld_ids + k;
         const long long id = p.ids_long ? static_cast<const long long *>(p.ids)[at] : static_cast<const int *>(p.ids)[at];
         t.v[k] = id >= p.vocab ? CUDART_NAN : teacher_value<T>(p, row, k);
         t.id[k] = id < 0 ? -1 : id >= p.vocab ? -2 : (int)id;
     }
-    if (threadIdx.x < ((4 - p.top % 4) & 3)) t.id[p.top + threadIdx.x] = -1;
+    if (team.thread < ((4 - p.top % 4) & 3)) t.id[p.top + team.thread] = -1;
 }
 // The first warp, after a barrier: shares and their sums.  tail: the row's.
 __device__ __forceinline__ void teacher_shares(const DistillParams &p, const Teacher &t, double tail, TeacherSums &out)
@@ -133,9 +146,9 @@ __device__ __forceinline__ void teacher_shares(const DistillParams &p, const Tea
 // Meanwhile, from the last thread on: the student's logits, and of entries with the same place the first one (place; the others have
 // none).
 template <class T>
-__device__ __forceinline__ void teacher_places(const Teacher &t, int top, const T *z)
+__device__ __forceinline__ void teacher_places(const Teacher &t, int top, const T *z, const Team &team)
 {
-    for (int k = blockDim.x - 1 - threadIdx.x; k < top; k += blockDim.x) {
+    for (int k = team.threads - 1 - team.thread; k < top; k += team.threads) {
         const int id = t.id[k];
         const double own = id >= 0 ? (double)widen(z[id]) : 0.0;
         bool again = false;
@@ -180,12 +193,12 @@ struct RowPieces {
 };
 
 template <class T>
-__device__ __forceinline__ void distill_zero(T *dz, int vocab, int first, int count)
+__device__ __forceinline__ void distill_zero(T *dz, int vocab, int first, int count, const Team &team)
 {
     const RowPieces<T> out(dz, vocab);
     T *const base = dz - out.skip;
     const uint32_t none[4] = {0, 0, 0, 0};
-    for (int i = first + threadIdx.x; i < min(first + count, out.pieces); i += blockDim.x) {
+    for (int i = first + team.thread; i < min(first + count, out.pieces); i += team.threads) {
         if (out.whole(i)) store16(base + i * RowPieces<T>::E, none);
         else
             for (int e = i * RowPieces<T>::E; e < (i + 1) * RowPieces<T>::E; ++e)
@@ -224,17 +237,30 @@ __device__ __forceinline__ Acc<T> distill_largest(const Packed<T, 16 / sizeof(T)
     }
 }
 
-// 16 bytes that are not needed again.
-__device__ __forceinline__ void store16_last(void *p, const uint32_t *w)
+// Ways through L2: what is kept for the second reading, and what is not needed again.
+__device__ __forceinline__ unsigned long long distill_keep()
 {
-    asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    unsigned long long policy;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
 }
-// A whole piece of logits, kept for the second time.
+__device__ __forceinline__ unsigned long long distill_drop()
+{
+    unsigned long long policy;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
+__device__ __forceinline__ void distill_store(void *p, const uint32_t *w, unsigned long long policy)
+{
+    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(policy) : "memory");
+}
+// A whole piece of logits.
 template <class T>
-__device__ __forceinline__ Packed<T, 16 / sizeof(T)> distill_piece(const T *at)
+__device__ __forceinline__ Packed<T, 16 / sizeof(T)> distill_piece(const T *at, unsigned long long policy)
 {
     Packed<T, 16 / sizeof(T)> v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at) : "memory");
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(at), "l"(policy) : "memory");
     return v;
 }
 
@@ -243,65 +269,73 @@ struct DistillPart {
 };
 
 template <class T, bool STEP>
-__global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_kernel(const __grid_constant__ DistillParams p)
+__global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_constant__ DistillParams p)
 {
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T), kTogether = 4;
     extern __shared__ __align__(16) unsigned char distill_memory[];
-    __shared__ DistillPart parts[kDistillCta / 32];
-    __shared__ double result[5];
-    __shared__ TeacherSums teacher;
+    __shared__ DistillPart all_parts[kDistillRow / 32];
+    __shared__ double results[kDistillCta / 32][5];
+    __shared__ TeacherSums teachers[kDistillCta / 32];
     wait_for_earlier();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, step = blockDim.x;
-    const long long row = blockIdx.x;
+    const int number = threadIdx.x / p.team, lane = threadIdx.x & 31, step = p.team;
+    const Team team = {(int)threadIdx.x - number * p.team, p.team, number};
+    const int warp = team.thread >> 5, warps = p.team >> 5;
+    DistillPart *const parts = all_parts + number * warps;
+    double *const result = results[number];
+    TeacherSums &teacher = teachers[number];
+    const long long row = (long long)blockIdx.x * (blockDim.x / p.team) + number;
+    if (row >= p.rows) return;
     const T *z = static_cast<const T *>(p.logits) + row * p.ld_logits;
     T *dz = STEP ? static_cast<T *>(p.dz) + row * p.ld_dz : nullptr;
-    const Teacher t = teacher_at(distill_memory, p.top);
-    uint32_t *const marks = reinterpret_cast<uint32_t *>(distill_memory + (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes);
+    unsigned char *const memory = distill_memory + (size_t)number * p.shared;
+    const Teacher t = teacher_at(memory, p.top);
+    uint32_t *const marks = reinterpret_cast<uint32_t *>(memory + (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes);
     A weight = A(1);
     if (STEP && p.dloss) weight = static_cast<const A *>(p.dloss)[row];
     const double tail = p.tail ? (double)static_cast<const A *>(p.tail)[row] : 0.0;
-    teacher_read<T>(p, row, t);
+    teacher_read<T>(p, row, t, team);
     const RowPieces<T> at(z, p.vocab);
     if (STEP && weight == A(0)) {                             // the row is not looked at
-        distill_zero(dz, p.vocab, 0, at.pieces + 1);          // (the gradient's may be one piece more, at another offset)
-        if (threadIdx.x == 0) static_cast<A *>(p.loss)[row] = A(0);
+        distill_zero(dz, p.vocab, 0, at.pieces + 1, team);          // (the gradient's may be one piece more, at another offset)
+        if (team.thread == 0) static_cast<A *>(p.loss)[row] = A(0);
         return;
     }
     // whole pieces of the row: [begin, stop); of the others there is at most one at each end
     const T *const base = z - at.skip;
-    const int begin = at.skip ? 1 : 0, stop = max(begin, at.end / E), mine = begin + threadIdx.x;
+    const int begin = at.skip ? 1 : 0, stop = max(begin, at.end / E), mine = begin + team.thread;
+    const unsigned long long drop = distill_drop(), keep = STEP ? distill_keep() : drop;
     int i = mine;
     const T *from = base + (long long)i * E;
     Packed<T, E> next[kTogether];                             // the first pieces are on their way while the entries are seen to
     auto fetch = [&]() {
         if (i + (kTogether - 1) * step < stop)
 #pragma unroll
-            for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from + (long long)u * step * E);
+            for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from + (long long)u * step * E, keep);
     };
     fetch();
-    for (int k = threadIdx.x; k < (at.end + 127) / 128; k += step) reinterpret_cast<uint4 *>(marks)[k] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
+    for (int k = team.thread; k < (at.end + 127) / 128; k += step) reinterpret_cast<uint4 *>(marks)[k] = make_uint4(0, 0, 0, 0);
+    team.sync();
 
     // the entries: a mark at each place, and what they add
     if (warp == 0) teacher_shares(p, t, tail, teacher);
-    teacher_places(t, p.top, z);
-    for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+    teacher_places(t, p.top, z, team);
+    for (int k = step - 1 - team.thread; k < p.top; k += step)
         if (t.place[k] >= 0) {
             const int place = at.skip + t.place[k];
             atomicOr(&marks[place >> 5], 1u << (place & 31));
         }
-    __syncthreads();
+    team.sync();
     double entries = 0.0, top_max = -CUDART_INF, top_sum = 0.0;
     if ((warps - 1 - warp) * 32 < p.top) {
-        for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+        for (int k = step - 1 - team.thread; k < p.top; k += step)
             if (t.id[k] >= 0) {
                 const double share = t.p[k];
                 if (share != 0.0) entries += share * (t.v[k] - teacher.top_max - teacher.log_sum - t.z[k] * p.inv_t);
                 if (t.place[k] >= 0) top_max = fmax(top_max, t.z[k]);
             }
         top_max = distill_warp_max(top_max), entries = distill_warp_sum(entries);
-        for (int k = blockDim.x - 1 - threadIdx.x; k < p.top; k += step)
+        for (int k = step - 1 - team.thread; k < p.top; k += step)
             if (t.place[k] >= 0) {
                 top_sum += exp((t.z[k] - top_max) * p.inv_t);
                 if (STEP) t.share[k] = teacher_share(t, p.top, k);
@@ -355,7 +389,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
             take(std::integral_constant<int, kTogether>(), v);
         }
         for (; i < stop; i += step, from += (long long)step * E) {
-            Packed<T, E> v = distill_piece(from);
+            Packed<T, E> v = distill_piece(from, keep);
             const unsigned bits = marked(i);
             if (bits) v = without(v, bits);
             take(std::integral_constant<int, 1>(), &v);
@@ -369,7 +403,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
         for (int e = 0; e < E; ++e) v.put(e, at.holds(i * E + e) ? base[i * E + e] : narrow<T>(distill_floor<A>()));
         return v;
     };
-    const int other = threadIdx.x == 0 ? (begin ? 0 : at.pieces) : threadIdx.x == 1 ? stop : at.pieces;
+    const int other = team.thread == 0 ? (begin ? 0 : at.pieces) : team.thread == 1 ? stop : at.pieces;
     const bool ends = other < at.pieces && (other < begin || other >= stop);
     if (ends) {
         const Packed<T, E> v = without(ragged(other), marked(other));
@@ -383,7 +417,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) rest_sum += __shfl_xor_sync(0xffffffffu, rest_sum, o);
     if (lane == 0) parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
-    __syncthreads();
+    team.sync();
     // the row's
     double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0;
     if (warp == 0) {
@@ -401,7 +435,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
         if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor, result[3] = inverse, result[4] = (double)weight * p.inv_t * factor * inverse;
     }
     if constexpr (STEP) {
-        __syncthreads();
+        team.sync();
         const A m = A(result[0]), coef = A(result[4]);
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
         const Two<A> less = both(-m), coefs = both(coef);
@@ -425,7 +459,7 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
             auto fetch_back = [&]() {
                 if (i - (kTogether - 1) * step >= begin)
 #pragma unroll
-                    for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from - u * back);
+                    for (int u = 0; u < kTogether; ++u) next[u] = distill_piece(from - u * back, drop);
             };
             fetch_back();
             while (i - (kTogether - 1) * step >= begin) {
@@ -435,24 +469,24 @@ __global__ void __launch_bounds__(kDistillCta, sizeof(T) == 8 ? 1 : 3) distill_k
                 i -= kTogether * step, from -= kTogether * back;
                 fetch_back();
 #pragma unroll
-                for (int u = 0; u < kTogether; ++u) store16_last(to - u * back, gradient(v[u]).w);
+                for (int u = 0; u < kTogether; ++u) distill_store(to - u * back, gradient(v[u]).w, drop);
                 to -= kTogether * back;
             }
-            for (; i >= begin; i -= step, from -= back, to -= back) store16_last(to, gradient(distill_piece(from)).w);
+            for (; i >= begin; i -= step, from -= back, to -= back) distill_store(to, gradient(distill_piece(from, drop)).w, drop);
         } else {
-            for (; i >= begin; i -= step) distill_put(at, i, dz, false, gradient(distill_piece(base + (long long)i * E)));
+            for (; i >= begin; i -= step) distill_put(at, i, dz, false, gradient(distill_piece(base + (long long)i * E, drop)));
         }
         if (ends) distill_put(at, other, dz, false, gradient(ragged(other)));
-        __syncthreads();                                      // the entries' places have been written like the others
+        team.sync();                                      // the entries' places have been written like the others
         const double by = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
-        for (int k = threadIdx.x; k < p.top; k += step)
+        for (int k = team.thread; k < p.top; k += step)
             if (t.place[k] >= 0) {
                 const double q = exp((t.z[k] - result[0]) * p.inv_t) * result[3];
                 dz[t.place[k]] = narrow<T>(A(by * (q * s_all - t.share[k])));
             }
     }
     // what only the loss needs comes last
-    if (threadIdx.x == 0) {
+    if (team.thread == 0) {
         const double log_total = row_max * p.inv_t + log(total);
         double loss = teacher.sum != 0.0 ? row_entries + teacher.sum * log_total : 0.0;
         if (teacher.rest > 0.0) loss += teacher.rest * log(teacher.rest * total / rest_of_row);        // P (log P - log Q)
@@ -474,13 +508,14 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     extern __shared__ __align__(16) unsigned char distill_memory[];
     __shared__ TeacherSums teacher;
     wait_for_earlier();
+    const Team team = {(int)threadIdx.x, (int)blockDim.x, 0};
     const long long row = blockIdx.x;
     const int first = (int)blockIdx.y * p.slice;
     const T *z = static_cast<const T *>(p.logits) + row * p.ld_logits;
     T *dz = static_cast<T *>(p.dz) + row * p.ld_dz;
     const A weight = p.dloss ? static_cast<const A *>(p.dloss)[row] : A(1);
     if (weight == A(0)) {
-        distill_zero(dz, p.vocab, first, blockIdx.y + 1 == gridDim.y ? p.slice + 1 : p.slice);
+        distill_zero(dz, p.vocab, first, blockIdx.y + 1 == gridDim.y ? p.slice + 1 : p.slice, team);
         return;
     }
     const RowPieces<T> at(z, p.vocab);
@@ -506,11 +541,11 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant
     fetch(first + threadIdx.x);
     const A *const stats = static_cast<const A *>(p.stats);
     const A m = stats[row], total = stats[p.rows + row], factor = stats[2 * p.rows + row];
-    teacher_read<T>(p, row, t);
+    teacher_read<T>(p, row, t, team);
     const double tail = p.tail ? (double)static_cast<const A *>(p.tail)[row] : 0.0;
     __syncthreads();
     if (threadIdx.x < 32) teacher_shares(p, t, tail, teacher);
-    teacher_places(t, p.top, z);                              // before anything is written: dz may be the logits
+    teacher_places(t, p.top, z, team);                              // before anything is written: dz may be the logits
     const int from = first * E - at.skip, to = last * E - at.skip;
     const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
     __syncthreads();
