@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
 
 // dz from saved statistics: p.slice pieces of a row (blockIdx.x, blockIdx.y) a CTA.
 template <class T>
-__global__ void __launch_bounds__(256) distill_grad_kernel(const __grid_constant__ DistillParams p)
+__global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __grid_constant__ DistillParams p)
 {
     using A = Acc<T>;
     constexpr int E = 16 / (int)sizeof(T);

@@ -32,10 +32,12 @@ cudaError_t launch_distill(DistillParams p, DistillWay way, cudaStream_t st)
     if (way == kDistillLoss) return distill_row_launch<T, false>(p, st);
     if (way == kDistillStep) return distill_row_launch<T, true>(p, st);
     const long long pieces = ((long long)p.vocab * (int)sizeof(T) + 15 - (int)sizeof(T)) / 16 + 1;
-    constexpr int kThreads = 256, kMost = kThreads * 8;
-    const int parts = (int)((pieces + kMost - 1) / kMost);
+    // eight pieces a thread at most, and of short rows four
+    int threads = 32;
+    while (threads < kDistillCta && threads * 4 < pieces) threads *= 2;
+    const int parts = (int)((pieces + threads * 8 - 1) / (threads * 8));
     p.slice = (int)((pieces + parts - 1) / parts);
-    return launch_beside(distill_grad_kernel<T>, dim3((unsigned)p.rows, (unsigned)parts), kThreads, st, (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes, p);
+    return launch_beside(distill_grad_kernel<T>, dim3((unsigned)p.rows, (unsigned)parts), threads, st, (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes, p);
 }
 
 }  // namespace fo

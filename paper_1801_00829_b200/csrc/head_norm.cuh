@@ -196,14 +196,22 @@ struct HeadWork {
     // Asks for what angles() will load of the next task's token.
     static __device__ __forceinline__ void expect(const HeadParams &p, const Items &at, const HeadRows &rows)
     {
-        if (p.axes > 1 || rows.at[0] < 0) return;
-        const A *const ct = static_cast<const A *>(p.cos_table) + rows.at[0] * p.ld_cos, *const st = static_cast<const A *>(p.sin_table) + rows.at[0] * p.ld_sin;
+        const A *const ct = static_cast<const A *>(p.cos_table), *const st = static_cast<const A *>(p.sin_table);
+        auto ask = [&](int pair) {
+            int r = rows.at[0];
+            if (p.axes > 1)
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (at.ta(i)) {
-                asm volatile("prefetch.global.L1 [%0];" ::"l"(ct + at.pair_a(i)));
-                asm volatile("prefetch.global.L1 [%0];" ::"l"(st + at.pair_a(i)));
-            }
+                for (int k = 1; k < FO_MAX_AXES; ++k)
+                    if (k < p.axes && pair >= p.section_end[k - 1]) r = rows.at[k];
+            if (r < 0) return;
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(ct + r * p.ld_cos + pair));
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(st + r * p.ld_sin + pair));
+        };
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (at.ta(i)) ask(at.pair_a(i));
+            if (!HALVES && at.tb(i)) ask(at.pair_b(i));
+        }
     }
     // Turns a lane's pieces.
     static __device__ __forceinline__ void turn(const Items &at, const Angles &g, U (&a)[I][N], U (&b)[I][N])
