@@ -130,7 +130,9 @@ typedef struct fo_scan {
     fo_rows h_at;
 } fo_scan;
 
-int fused_scan(const fo_scan *a, void *stream);
+int fused_scan(const fo_scan *a, void *ws, size_t ws_bytes, void *stream);
+/* Bytes of scratch for fused_scan and fused_scan_grad. */
+size_t fused_scan_workspace_bytes(void);
 
 /* The gradient from dh and dlast (either may be NULL: zero) and the forward pass's inputs and h:
  *     l_t = dh_t + a_{t+1} l_{t+1}   (dlast where the sequence ends; nothing through a reset)
@@ -148,7 +150,7 @@ typedef struct fo_scan_grad {
     fo_rows dx_at, dgate_at;
 } fo_scan_grad;
 
-int fused_scan_grad(const fo_scan_grad *a, void *stream);
+int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------- distillation from a teacher's top logits
  * For every row z of `vocab` logits, with q = softmax(z / temperature) and the teacher's `top` entries (id_k, v_k):

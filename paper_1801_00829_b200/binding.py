@@ -86,7 +86,7 @@ EXPORTS = [
     "fo_probe_out_len", "fo_probe_l2_gather", "fo_probe_bulk_gather", "fo_probe_fp64_fma", "fo_chain_describe", "fo_tune", "fo_cell_stamps",
     "fused_block_norm", "fused_block_norm_grad", "fused_block_norm_grad_workspace_bytes",
     "fused_grad_norm", "fused_grad_clip", "fused_grad_workspace_bytes", "fused_adamw",
-    "fused_head_norm", "fused_head_norm_grad", "fused_head_norm_grad_workspace_bytes", "fused_scan", "fused_scan_grad",
+    "fused_head_norm", "fused_head_norm_grad", "fused_head_norm_grad_workspace_bytes", "fused_scan", "fused_scan_grad", "fused_scan_workspace_bytes",
     "fused_distill", "fused_distill_grad", "fused_distill_step",
 ]
 
@@ -152,7 +152,10 @@ def load_library(path=None):
         lib.fused_head_norm_grad.argtypes = [bp, vp, sz, vp]
         lib.fused_head_norm_grad_workspace_bytes.argtypes = [i32, i32]
         lib.fused_head_norm_grad_workspace_bytes.restype = sz
-        for f in (lib.fused_head_norm, lib.fused_scan, lib.fused_scan_grad, lib.fused_distill, lib.fused_distill_grad,
+        lib.fused_scan.argtypes = lib.fused_scan_grad.argtypes = [bp, vp, sz, vp]
+        lib.fused_scan_workspace_bytes.argtypes = []
+        lib.fused_scan_workspace_bytes.restype = sz
+        for f in (lib.fused_head_norm, lib.fused_distill, lib.fused_distill_grad,
                   lib.fused_distill_step):
             f.argtypes = [bp, vp]
         lib.fo_set_jit.argtypes = [C.c_int]

@@ -400,7 +400,9 @@ PyObject *scan_impl(PyObject *const *a)
     n.h = c.rows(out ? out : &h, c.type, "out", &n.h_at, out != nullptr);
     n.last = c.state(out_state ? out_state : &last, "out_state", out_state != nullptr);
     const OnGpu on(c.gpu);
-    check_status(fused_scan(&n, stream_of(c.gpu)), "fused_scan");
+    const cudaStream_t st = stream_of(c.gpu);
+    const at::Tensor ws = workspace(c.gpu, st, fused_scan_workspace_bytes());
+    check_status(fused_scan(&n, ws.data_ptr(), (size_t)ws.numel(), st), "fused_scan");
     if (out) written(*out);
     if (out_state) written(*out_state);
     PyObject *ho = given_or_new(a[7], h);
@@ -438,7 +440,9 @@ PyObject *scan_grad_impl(PyObject *const *a)
         n.dstate = c.state(&dstate, "dstate");
     }
     const OnGpu on(c.gpu);
-    check_status(fused_scan_grad(&n, stream_of(c.gpu)), "fused_scan_grad");
+    const cudaStream_t st = stream_of(c.gpu);
+    const at::Tensor ws = workspace(c.gpu, st, fused_scan_workspace_bytes());
+    check_status(fused_scan_grad(&n, ws.data_ptr(), (size_t)ws.numel(), st), "fused_scan_grad");
     return got.release();
 }
 

@@ -13,7 +13,7 @@ namespace fo {
     X(FO_F16, FO_F16, __half, __half)              \
     X(FO_F16, FO_F32, __half, float)
 
-#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(ScanParams, bool, cudaStream_t);
+#define FO_EXTERN(t, g, T, G) extern template cudaError_t launch_scan<T, G>(ScanParams, bool, void *, cudaStream_t);
 FO_SCAN_PAIRS(FO_EXTERN)
 #undef FO_EXTERN
 
@@ -37,7 +37,7 @@ int check_scan(long long batch, long long tokens, long long channels, int type, 
         if (s.batch < 0 || s.token < 0) return FO_ERR_SHAPE;
     // CTAs are counted in 31 bits
     const long long tiles = (channels + 31) / 32;
-    if (tiles && batch > (0x7fffffffLL / kScanMostCluster) / tiles) return FO_ERR_UNSUPPORTED;
+    if (tiles && batch > 0x7fffffffLL / tiles) return FO_ERR_UNSUPPORTED;
     return FO_OK;
 }
 bool all_on(int type, std::initializer_list<const void *> ps)
@@ -61,11 +61,13 @@ int near_if(std::initializer_list<fo_rows> strides, long long channels)
 }
 int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return rows_at(p, s, type, 2 * elem_bytes(type)) ? bit : 0; }
 
-int launch(const ScanParams &p, int type, int gate_type, bool grad, cudaStream_t st)
+int launch(const ScanParams &p, int type, int gate_type, bool grad, void *ws, size_t ws_bytes, cudaStream_t st)
 {
+    const int rc = check_workspace(ws, ws_bytes, fused_scan_workspace_bytes());
+    if (rc != FO_OK) return rc;
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(t, g, T, G) \
-    if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, st);
+    if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, ws, st);
     FO_SCAN_PAIRS(FO_CASE)
 #undef FO_CASE
     return e == cudaSuccess ? FO_OK : cuda_fail(e);
@@ -78,7 +80,13 @@ using namespace fo;
 
 extern "C" {
 
-int fused_scan(const fo_scan *a, void *stream)
+size_t fused_scan_workspace_bytes(void)
+{
+    // three states and a mark of every chunk: of at most 64 channels each, and of as many as there are CTAs on all SMs
+    return sizeof(WsHead) + (size_t)2 * kScanMostSms * (64 * 3 * sizeof(double) + sizeof(int));
+}
+
+int fused_scan(const fo_scan *a, void *ws, size_t ws_bytes, void *stream)
 {
     if (!a) return FO_ERR_NULL;
     const int rc = check_scan(a->batch, a->tokens, a->channels, a->type, a->gate_type, a->decay, a->mix, a->lengths, a->lengths_type,
@@ -97,10 +105,10 @@ int fused_scan(const fo_scan *a, void *stream)
     p.x_at = a->x_at, p.gate_at = a->gate_at, p.reset_at = a->reset_at, p.h_at = a->h_at;
     p.whole = whole_if(a->x, a->x_at, a->type, kScanX) | whole_if(a->gate, a->gate_at, a->gate_type, kScanGate)
               | pairs_if(a->h, a->h_at, a->type, kScanOut) | near_if({a->x_at, a->gate_at, a->h_at}, a->channels);
-    return launch(p, a->type, a->gate_type, false, (cudaStream_t)stream);
+    return launch(p, a->type, a->gate_type, false, ws, ws_bytes, (cudaStream_t)stream);
 }
 
-int fused_scan_grad(const fo_scan_grad *a, void *stream)
+int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stream)
 {
     if (!a) return FO_ERR_NULL;
     const int rc = check_scan(a->batch, a->tokens, a->channels, a->type, a->gate_type, a->decay, a->mix, a->lengths, a->lengths_type,
@@ -126,7 +134,7 @@ int fused_scan_grad(const fo_scan_grad *a, void *stream)
               | near_if({a->x_at, a->gate_at, a->dh_at, a->h_at, a->dx_at, a->dgate_at}, a->channels);
     if (!mixes) p.whole |= kScanX;                           // not looked at
     if (!a->dh) p.whole |= kScanDh;
-    return launch(p, a->type, a->gate_type, true, (cudaStream_t)stream);
+    return launch(p, a->type, a->gate_type, true, ws, ws_bytes, (cudaStream_t)stream);
 }
 
 }  // extern "C"

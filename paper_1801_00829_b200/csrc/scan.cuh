@@ -7,6 +7,9 @@
 // registers.  So the inputs are read once and no CTA waits for another outside its cluster, whose CTAs run together.
 // The inputs of the next rounds are on their way meanwhile, to a ring in shared memory: asynchronous copies, which a warp makes
 // for itself.
+// A round in a cluster takes 2.5 us or more, however few its channels are.  So long sequences of few channels are cut into chunks instead, as many as
+// make CTAs for all SMs: a first kernel reads the chunks and leaves the map of each, a second one puts these together to the states that
+// come into them, and then the chunks are run like sequences of their own.
 #pragma once
 
 #include "elem.cuh"
@@ -17,6 +20,7 @@ namespace fo {
 constexpr int kScanCta = 256;
 constexpr int kScanMostWarps = kScanCta / 32;
 constexpr int kScanMostCluster = 8;
+constexpr int kScanMostSms = 256;       // chunks make CTAs for two on each of these at most
 
 enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32, kScanNear = 64, kScanAll = 127 };
 
@@ -33,6 +37,10 @@ struct ScanParams {
     // the gradient's own
     const void *dh, *dlast, *h_in;
     void *dgate;
+    // chunks of `chunk` tokens each (the last one's are what is left), their maps and the states that come into them
+    int chunks, chunk;
+    void *map_a, *map_h, *carry;        // batch x chunks x channels
+    int *map_drops;                     // batch x chunks: a reset lies in it
     fo_rows dh_at, h_in_at, dgate_at;
 };
 
@@ -526,6 +534,12 @@ __device__ __forceinline__ int scan_length(const ScanParams &p, long long b)
     return n < 0 ? 0 : n > p.tokens ? p.tokens : (int)n;
 }
 
+// The end of the sequence, counted from the chunk's first token.
+template <class Place>
+__device__ __forceinline__ int scan_end(const ScanParams &p, const Place &at)
+{
+    return min(max(scan_length(p, at.b) - at.base, 0), at.tokens);
+}
 // A lane's channels of a state.
 template <class U, class A, int V>
 __device__ __forceinline__ U scan_state(const void *p, long long at, int count)
@@ -545,21 +559,23 @@ __device__ __forceinline__ void scan_keep(void *p, long long at, U u, int count)
 }
 
 // Where a warp is in the call.
-template <int V>
+template <int V, bool CLUSTER>
 struct ScanPlace {
     unsigned rank, cluster;
     int lane, warp, warps;
-    long long b, state;                 // state: of the lane's first channel
+    long long b, state, piece;          // state: of the lane's first channel; piece: the same of its chunk's
+    int base, tokens;                   // the chunk's first token, and its number of them
     int first, channel, count;          // first channel of the tile and of the lane, channels of the lane
-    __device__ __forceinline__ explicit ScanPlace(const ScanParams &p) : rank(scan_rank()), cluster(scan_cluster())
+    __device__ __forceinline__ explicit ScanPlace(const ScanParams &p) : rank(CLUSTER ? scan_rank() : 0), cluster(CLUSTER ? scan_cluster() : 1)
     {
         // the same for all lanes, and known to be: the addresses of rows are then computed once for the warp
         warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-        const unsigned item = blockIdx.x / cluster;
-        b = item / (unsigned)p.tiles;
-        first = (int)(item - (unsigned)b * (unsigned)p.tiles) * 32 * V, channel = first + lane * V;
+        const unsigned item = blockIdx.x / cluster, part = item / (unsigned)p.tiles, sequence = part / (unsigned)p.chunks;
+        b = sequence;
+        base = (int)(part - sequence * (unsigned)p.chunks) * p.chunk, tokens = min(p.chunk, p.tokens - base);
+        first = (int)(item - part * (unsigned)p.tiles) * 32 * V, channel = first + lane * V;
         count = max(0, min(V, (int)p.channels - channel));
-        state = b * p.channels + channel;
+        state = b * p.channels + channel, piece = part * p.channels + channel;
     }
 };
 
@@ -572,7 +588,8 @@ struct ScanRing {
     static constexpr int kBytes = kStages * kSegment;        // of a warp
 };
 
-template <class T, class G, int V, int S>
+// CLUSTER: launched in clusters.  Without them the code for them costs 3 to 5 us of 75 to 163 (8 x 4096 x 2048 in bfloat16).
+template <class T, class G, int V, int S, bool CLUSTER>
 __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant__ ScanParams p)
 {
     using A = Acc<T>;
@@ -580,24 +597,25 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
     using Ring = ScanRing<T, G, V, S, false>;
     constexpr bool EXACT = sizeof(T) >= 4;
     extern __shared__ __align__(16) char scan_memory[];
-    const ScanPlace<V> at(p);
+    const ScanPlace<V, CLUSTER> at(p);
     wait_for_earlier();
     char *const ring = scan_memory + at.warp * Ring::kBytes;
     const ScanShared<U> sh(scan_memory + at.warps * Ring::kBytes, at.warps, at.cluster);
-    const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
+    // tokens are counted from the chunk's first one
+    const int end = scan_end(p, at), round = at.cluster * at.warps * S;
     int t0 = (at.rank * at.warps + at.warp) * S;
     const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), hs = p.h_at.token * (int)sizeof(T);
     const unsigned ho = at.channel * (unsigned)sizeof(T), hs_near = (unsigned)hs;
-    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + t0 * xs;
-    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + t0 * gs;
-    char *h = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + t0 * hs;
+    const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + (at.base + t0) * xs;
+    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + (at.base + t0) * gs;
+    char *h = static_cast<char *>(p.h) + at.b * p.h_at.batch * (int)sizeof(T) + (at.base + t0) * hs;
     const ScanCopy<T, S, 32 * V> copy_x(p.whole & kScanX, at.lane, (int)p.channels - at.first, xs);
     const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, (int)p.channels - at.first, gs);
     // easy: everything is in whole pieces and near, and the tile's channels are all there
     constexpr int kEasy = kScanX | kScanGate | kScanOut | kScanNear;
     const bool pairs = p.whole & kScanOut, easy = (p.whole & kEasy) == kEasy && at.first + 32 * V <= p.channels;
     const long long x_round = round * xs, gate_round = round * gs, h_round = round * hs;
-    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
+    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch + at.base * p.reset_at.token : nullptr;
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kSegment;
@@ -613,12 +631,12 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
         ahead += round, x += x_round, gate += gate_round, in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
     for (int k = 0; k < Ring::kStages - 1; ++k) issue();
-    U carry = scan_state<U, A, V>(p.state, at.state, at.count);
+    U carry = p.chunks > 1 ? scan_state<U, A, V>(p.carry, at.piece, at.count) : scan_state<U, A, V>(p.state, at.state, at.count);
     scan_begin(sh, at.warp, carry);
     auto marks = [&](int t) -> unsigned char { return reset && at.lane < S && t + at.lane < end ? reset[(t + at.lane) * p.reset_at.token] : 0; };
     unsigned char mark = marks(t0);
     int turn = 0;
-    for (int first = 0; first < p.tokens; first += round, ++turn) {
+    for (int first = 0; first < at.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
@@ -661,18 +679,18 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 in = (drops >> s) & 1u ? m[s] : fused_ma(a[s], in, m[s]);
-                if (t0 + s < p.tokens) scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(t0 + s < end ? in : scan_all<U>(A(0))), at.count, pairs);
+                if (t0 + s < at.tokens) scan_store<T, V>(h + s * hs, ho, scan_narrow<T, V>(t0 + s < end ? in : scan_all<U>(A(0))), at.count, pairs);
             }
         }
         t0 += round, h += h_round;
     }
     carry = scan_left(sh, turn & 1, carry);
-    if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
+    if (p.last && p.chunks == 1 && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
 }
 
 // The gradient: l_t = dh_t + u_{t+1}, u_t = a_t l_t is what comes to the token before (nothing through a reset), from the last token to
 // the first.  Segments are counted from the end, and a segment's map is that of u.
-template <class T, class G, int V, int S>
+template <class T, class G, int V, int S, bool CLUSTER>
 __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_constant__ ScanParams p)
 {
     using A = Acc<T>;
@@ -681,18 +699,19 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     constexpr bool EXACT = sizeof(T) >= 4;
     constexpr int kPart = ScanCopy<T, S, 32 * V>::kBytes, kRow = 32 * V * (int)sizeof(T), kGateRow = 32 * V * (int)sizeof(G);
     extern __shared__ __align__(16) char scan_memory[];
-    const ScanPlace<V> at(p);
+    const ScanPlace<V, CLUSTER> at(p);
     wait_for_earlier();
     char *const ring = scan_memory + at.warp * Ring::kBytes;
     const ScanShared<U> sh(scan_memory + at.warps * Ring::kBytes, at.warps, at.cluster);
-    const int end = scan_length(p, at.b), round = at.cluster * at.warps * S;
+    // tokens are counted from the chunk's first one
+    const int end = scan_end(p, at), round = at.cluster * at.warps * S;
     // element s of a segment is token t0 - s
-    int t0 = p.tokens - 1 - (int)(at.rank * at.warps + at.warp) * S;
+    int t0 = at.tokens - 1 - (int)(at.rank * at.warps + at.warp) * S;
     const long long xs = p.x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G), ds = p.dh_at.token * (int)sizeof(T),
                     hs = p.h_in_at.token * (int)sizeof(T), dxs = p.h_at.token * (int)sizeof(T), dgs = p.dgate_at.token * (int)sizeof(G);
     const unsigned xo = at.channel * (unsigned)sizeof(T), go = at.channel * (unsigned)sizeof(G), dxs_near = (unsigned)dxs, dgs_near = (unsigned)dgs;
     // pointers are to the segment's last element, the lowest in memory
-    const int lowest = t0 - (S - 1);
+    const int lowest = at.base + t0 - (S - 1);
     const char *x = static_cast<const char *>(p.x) + (at.b * p.x_at.batch + at.first) * (int)sizeof(T) + lowest * xs;
     const char *dh = static_cast<const char *>(p.dh) + (at.b * p.dh_at.batch + at.first) * (int)sizeof(T) + lowest * ds;
     const char *hin = static_cast<const char *>(p.h_in) + (at.b * p.h_in_at.batch + at.first) * (int)sizeof(T) + (lowest - 1) * hs;  // of the token before
@@ -707,12 +726,13 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     const bool pairs = p.whole & kScanOut, gate_pairs = p.whole & kScanOutGate, easy = p.whole == kScanAll && at.first + 32 * V <= p.channels;
     const long long x_round = round * xs, dh_round = round * ds, h_round = round * hs, gate_round = round * gs, dx_round = round * dxs,
                     dgate_round = round * dgs;
-    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch : nullptr;
+    const unsigned char *reset = p.reset ? p.reset + at.b * p.reset_at.batch + at.base * p.reset_at.token : nullptr;
     const bool with_x = p.mode % 3 != FO_MIX_ONE, with_dh = p.dh != nullptr;
+    const int lead = at.base == 0 ? S : S - 1;           // segments from this token on have a token of the sequence before each of theirs
     int ahead = t0, in_stage = 0, stage = 0;
     auto issue = [&]() {
         char *to = ring + in_stage * Ring::kSegment;
-        if (easy && ahead < end && ahead >= S) {
+        if (easy && ahead < end && ahead >= lead) {
             if (with_dh) copy_dh.issue_all(to, dh);
             if (with_x) copy_x.issue_all(to + kPart, x);
             copy_h.issue_all(to + 2 * kPart, hin);
@@ -721,7 +741,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
             const auto valid = [&](int r) { return ahead - r >= 0 && ahead - r < end; };
             if (with_dh) copy_dh.issue(to, dh + (S - 1) * ds, -ds, valid);
             if (with_x) copy_x.issue(to + kPart, x + (S - 1) * xs, -xs, valid);
-            copy_h.issue(to + 2 * kPart, hin + (S - 1) * hs, -hs, [&](int r) { return ahead - r > 0 && ahead - r < end; });
+            copy_h.issue(to + 2 * kPart, hin + (S - 1) * hs, -hs, [&](int r) { return at.base + ahead - r > 0 && ahead - r >= 0 && ahead - r < end; });
             copy_gate.issue(to + 3 * kPart, gate + (S - 1) * gs, -gs, valid);
         }
         scan_issued();
@@ -729,7 +749,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
         in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
     };
     for (int k = 0; k < Ring::kStages - 1; ++k) issue();
-    U carry = scan_state<U, A, V>(p.dlast, at.state, at.count);
+    U carry = p.chunks > 1 ? scan_state<U, A, V>(p.carry, at.piece, at.count) : scan_state<U, A, V>(p.dlast, at.state, at.count);
     const U start = scan_state<U, A, V>(p.state, at.state, at.count), none = scan_all<U>(A(0));
     scan_begin(sh, at.warp, carry);
     auto marks = [&](int t) -> unsigned char {
@@ -737,7 +757,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     };
     unsigned char mark = marks(t0);
     int turn = 0;
-    for (int first = 0; first < p.tokens; first += round, ++turn) {
+    for (int first = 0; first < at.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
         issue();                                         // where the stage before was
@@ -754,7 +774,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
         });
         mark = marks(t0 - round);
         // plain: all of the segment's tokens are the sequence's, and none of them its first one or drops what comes
-        const bool plain = t0 < end && t0 >= S && drops == 0;
+        const bool plain = t0 < end && t0 >= lead && drops == 0;
         ScanMap<U> own = {scan_all<U>(A(1)), none};
         if (plain) {
 #pragma unroll
@@ -774,7 +794,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
                 U to_x = m * l, before = h_of(s), through = a[s] * l, slope;
                 if constexpr (masked.value) {
                     const bool drop = (drops >> s) & 1u;
-                    if (t0 - s == 0) before = start;
+                    if (at.base + t0 - s == 0) before = start;
                     if (drop) before = none, through = none;
                 }
                 if constexpr (mix.value == FO_MIX_ONE) slope = da * before;
@@ -800,7 +820,143 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
         t0 -= round, dx -= dx_round, dgate -= dgate_round;
     }
     carry = scan_left(sh, turn & 1, carry);
-    if (p.last && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
+    if (p.last && p.chunks == 1 && at.rank == 0 && at.warp == 0) scan_keep<U, A, V>(p.last, at.state, carry, at.count);
+}
+
+// The map of each chunk: its warps take an equal part of its tokens each, segment after segment, and put their maps together.
+// GRAD: the map of u, from the last token to the first.
+template <class T, class G, int V>
+struct ScanMapRing {
+    static constexpr int S = 8;
+    static constexpr int kPart = ScanCopy<T, S, 32 * V>::kBytes, kSegment = kPart + ScanCopy<G, S, 32 * V>::kBytes;
+    static constexpr int kStages = 12288 / kSegment < 6 ? 12288 / kSegment : 6;
+    static constexpr int kBytes = kStages * kSegment;        // of a warp
+};
+template <class T, class G, int V, bool GRAD>
+__global__ void __launch_bounds__(kScanCta, 2) scan_map_kernel(const __grid_constant__ ScanParams p)
+{
+    using A = Acc<T>;
+    using U = typename ScanUnit<A, V>::U;
+    using Ring = ScanMapRing<T, G, V>;
+    constexpr bool EXACT = sizeof(T) >= 4;
+    constexpr int S = Ring::S;
+    extern __shared__ __align__(16) char scan_memory[];
+    const ScanPlace<V, false> at(p);
+    wait_for_earlier();
+    char *const ring = scan_memory + at.warp * Ring::kBytes;
+    // the part is tokens low .. high - 1 of the chunk; element s of a segment is token t0 + s, of the gradient's t0 - s
+    const int part = (at.tokens + at.warps * S - 1) / (at.warps * S) * S;
+    const int low = min(at.tokens, at.warp * part), high = max(low, min(scan_end(p, at), low + part));
+    constexpr int kWay = GRAD ? -1 : 1;
+    int t0 = GRAD ? high - 1 : low;
+    const int lowest = at.base + (GRAD ? t0 - (S - 1) : t0);         // the pointers' token, the segment's first in memory
+    const fo_rows x_at = GRAD ? p.dh_at : p.x_at;
+    const long long xs = x_at.token * (int)sizeof(T), gs = p.gate_at.token * (int)sizeof(G);
+    const char *x = static_cast<const char *>(GRAD ? p.dh : p.x) + (at.b * x_at.batch + at.first) * (int)sizeof(T) + lowest * xs;
+    const char *gate = static_cast<const char *>(p.gate) + (at.b * p.gate_at.batch + at.first) * (int)sizeof(G) + lowest * gs;
+    constexpr int kX = GRAD ? kScanDh : kScanX, kEasy = kX | kScanGate | kScanNear;
+    const ScanCopy<T, S, 32 * V> copy_x(p.whole & kX, at.lane, (int)p.channels - at.first, kWay * xs);
+    const ScanCopy<G, S, 32 * V> copy_gate(p.whole & kScanGate, at.lane, (int)p.channels - at.first, kWay * gs);
+    const bool easy = (p.whole & kEasy) == kEasy && at.first + 32 * V <= p.channels, with_x = !GRAD || p.dh;
+    const unsigned char *const reset = p.reset ? p.reset + at.b * p.reset_at.batch + at.base * p.reset_at.token : nullptr;
+    int left = high - low, to_come = left, in_stage = 0, stage = 0;       // tokens of the part that are not worked on, not asked for
+    auto issue = [&]() {
+        char *const to = ring + in_stage * Ring::kSegment;
+        if (easy && to_come >= S) {
+            if (with_x) copy_x.issue_all(to, x);
+            copy_gate.issue_all(to + Ring::kPart, gate);
+        } else {
+            const auto valid = [&](int r) { return r < to_come; };
+            if (with_x) copy_x.issue(to, GRAD ? x + (S - 1) * xs : x, kWay * xs, valid);
+            copy_gate.issue(to + Ring::kPart, GRAD ? gate + (S - 1) * gs : gate, kWay * gs, valid);
+        }
+        scan_issued();
+        to_come -= S, x += kWay * S * xs, gate += kWay * S * gs, in_stage = in_stage + 1 == Ring::kStages ? 0 : in_stage + 1;
+    };
+    for (int k = 0; k < Ring::kStages - 1; ++k) issue();
+    auto marks = [&](int t, int there) -> unsigned char { return reset && at.lane < S && at.lane < there ? reset[(t + kWay * at.lane) * p.reset_at.token] : 0; };
+    unsigned char mark = marks(t0, left);
+    ScanMap<U> own = {scan_all<U>(A(1)), scan_all<U>(A(0))};
+    unsigned dropped = 0;
+    for (; left > 0; left -= S) {
+        const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
+        dropped |= drops;
+        scan_arrived<Ring::kStages - 2>();
+        issue();                                         // where the stage before was
+        const char *const from = ring + stage * Ring::kSegment + at.lane * V * (int)sizeof(T);
+        const char *const from_gate = ring + stage * Ring::kSegment + Ring::kPart + at.lane * V * (int)sizeof(G);
+        stage = stage + 1 == Ring::kStages ? 0 : stage + 1;
+        U a[S], m[S];                                    // m: m(a) x forwards, dh backwards
+        with_mode(p.mode, [&](auto decay, auto mix) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                U rest;
+                scan_decay<decay.value, EXACT, GRAD, A>(scan_widen<U>(scan_piece<G, V>(from_gate + s * 32 * V * (int)sizeof(G))), a[s], rest);
+                m[s] = with_x ? scan_widen<U>(scan_piece<T, V>(from + s * 32 * V * (int)sizeof(T))) : scan_all<U>(A(0));
+                if constexpr (!GRAD && mix.value != FO_MIX_ONE) m[s] = scan_mix<mix.value, EXACT, A>(a[s], rest) * m[s];
+            }
+        });
+        t0 += kWay * S;
+        mark = marks(t0, left - S);
+        if (left < S)
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+                if (s >= left) a[s] = scan_all<U>(A(1)), m[s] = scan_all<U>(A(0));      // the state stays as it is
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const bool drop = (drops >> s) & 1u;
+            if constexpr (GRAD) own.h = drop ? scan_all<U>(A(0)) : a[s] * (m[s] + own.h);
+            else own.h = drop ? m[s] : fused_ma(a[s], own.h, m[s]);
+            own.a = own.a * a[s];
+        }
+    }
+    scan_arrived<0>();
+    __syncthreads();                                     // the rings' memory is taken for the maps
+    ScanMap<U> *const maps = reinterpret_cast<ScanMap<U> *>(scan_memory);
+    int *const parts_drop = reinterpret_cast<int *>(maps + kScanMostWarps * 32);
+    maps[at.warp * 32 + at.lane] = own;
+    if (at.lane == 0) parts_drop[at.warp] = dropped != 0;
+    __syncthreads();
+    if (at.warp) return;
+    int any = 0;
+    ScanMap<U> all = {scan_all<U>(A(1)), scan_all<U>(A(0))};
+    for (int k = 0; k < at.warps; ++k) {
+        const int w = GRAD ? at.warps - 1 - k : k;
+        any |= parts_drop[w];
+        all.h = scan_apply(maps[w * 32 + at.lane], parts_drop[w], all.h), all.a = all.a * maps[w * 32 + at.lane].a;
+    }
+    scan_keep<U, A, V>(p.map_a, at.piece, all.a, at.count);
+    scan_keep<U, A, V>(p.map_h, at.piece, all.h, at.count);
+    if (at.first == 0 && at.lane == 0) p.map_drops[at.b * p.chunks + at.base / p.chunk] = any;
+}
+// What comes into every chunk, and what leaves the last one: a thread to a channel of a sequence.
+template <class A, bool GRAD>
+__global__ void __launch_bounds__(kScanCta) scan_carry_kernel(const __grid_constant__ ScanParams p)
+{
+    constexpr int kAhead = 16;                           // maps that are on their way together
+    wait_for_earlier();
+    const long long at = (long long)blockIdx.x * kScanCta + threadIdx.x, b = at / p.channels, c = at - b * p.channels;
+    if (b >= p.batch) return;
+    const void *const in = GRAD ? p.dlast : p.state;
+    A carry = in ? static_cast<const A *>(in)[at] : A(0);
+    for (int first = 0; first < p.chunks; first += kAhead) {
+        ScanMap<A> m[kAhead];
+        int drops[kAhead];
+        const auto part = [&](int k) { return b * p.chunks + (GRAD ? p.chunks - 1 - k : k); };
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (first + k >= p.chunks) continue;
+            const long long q = part(first + k) * p.channels + c;
+            m[k] = {static_cast<const A *>(p.map_a)[q], static_cast<const A *>(p.map_h)[q]}, drops[k] = p.map_drops[part(first + k)];
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (first + k >= p.chunks) continue;
+            static_cast<A *>(p.carry)[part(first + k) * p.channels + c] = carry;
+            carry = scan_apply(m[k], drops[k], carry);
+        }
+    }
+    if (p.last) static_cast<A *>(p.last)[at] = carry;
 }
 
 // A few tokens (a decoding step): every thread takes its channels through them, one after the other.
@@ -849,6 +1005,6 @@ __global__ void __launch_bounds__(kScanCta) scan_step_kernel(const __grid_consta
 
 // Host: one kernel of a pair of types; scan_*.cu instantiate it.
 template <class T, class G>
-cudaError_t launch_scan(ScanParams p, bool grad, cudaStream_t st);
+cudaError_t launch_scan(ScanParams p, bool grad, void *ws, cudaStream_t st);
 
 }  // namespace fo

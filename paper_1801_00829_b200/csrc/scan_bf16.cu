@@ -3,6 +3,6 @@
 
 namespace fo {
 
-template cudaError_t launch_scan<__nv_bfloat16, __nv_bfloat16>(ScanParams, bool, cudaStream_t);
+template cudaError_t launch_scan<__nv_bfloat16, __nv_bfloat16>(ScanParams, bool, void *, cudaStream_t);
 
 }  // namespace fo

@@ -3,6 +3,6 @@
 
 namespace fo {
 
-template cudaError_t launch_scan<float, float>(ScanParams, bool, cudaStream_t);
+template cudaError_t launch_scan<float, float>(ScanParams, bool, void *, cudaStream_t);
 
 }  // namespace fo

@@ -14,6 +14,14 @@ namespace fo {
 template <class T> constexpr int scan_channels() { return sizeof(T) == 8 ? 1 : 2; }
 template <class T> constexpr int scan_tokens(bool grad) { return (sizeof(T) == 2 ? 8 : 4) * (grad || sizeof(T) == 8 ? 1 : 2); }
 
+// Whether a call's sequences are cut into chunks.  `room`: CTAs for each 32 V channels of a sequence that find a place at once; `rounds`: how
+// many the largest clusters would take.  Below eight the two more launches and the second reading cost more than they give
+// (bfloat16, 1 x 2048 x 512: in clusters 10 us forwards and 20 backwards, in chunks 16 and 24; 1 x 8192 x 1024: 33 and 70, 26 and
+// 40), and forwards, where all inputs are read twice, so it is when the clusters fill the GPU (1 x 65536 x 2560: 374 and 440;
+// backwards, where two of four are, 660 and 478).
+inline bool scan_chunked(bool grad, long long room, long long rounds) { return rounds >= 8 && room >= (grad ? 4 : 16); }
+constexpr int kScanLeastChunk = 4;      // rounds; 1 x 65536 x 32 forwards: with four 39 us, two 41, eight 54
+
 // How many clusters of 1 .. kScanMostCluster CTAs the GPU works on at once, asked once for each GPU, kernel and number of warps.
 // What does not fit runs after the rest, and doubles the time (65536 x 2560: 6 CTAs a cluster 301 us, 7 486).
 template <class K>
@@ -43,18 +51,21 @@ public:
 };
 
 template <class T, class G, bool GRAD>
-cudaError_t scan_launch(ScanParams p, cudaStream_t st)
+cudaError_t scan_launch(ScanParams p, void *ws, cudaStream_t st)
 {
     constexpr int V = scan_channels<T>(), S = scan_tokens<T>(GRAD);
-    using Shared = ScanShared<typename ScanUnit<Acc<T>, V>::U>;
+    using A = Acc<T>;
+    using Shared = ScanShared<typename ScanUnit<A, V>::U>;
     using Ring = ScanRing<T, G, V, S, GRAD>;
     using Kernel = void (*)(ScanParams);
-    static OncePerGpu once;
+    static OncePerGpu once, cluster_once;
     static ScanFit<Kernel> fit;
-    Kernel kernel;
-    if constexpr (GRAD) kernel = scan_grad_kernel<T, G, V, S>;
-    else kernel = scan_kernel<T, G, V, S>;
-    cudaError_t e = once.allow(kernel, Ring::kBytes * kScanMostWarps + Shared::bytes(kScanMostWarps, kScanMostCluster));
+    Kernel kernel, cluster_kernel;
+    if constexpr (GRAD) kernel = scan_grad_kernel<T, G, V, S, false>, cluster_kernel = scan_grad_kernel<T, G, V, S, true>;
+    else kernel = scan_kernel<T, G, V, S, false>, cluster_kernel = scan_kernel<T, G, V, S, true>;
+    const size_t most_shared = Ring::kBytes * kScanMostWarps + Shared::bytes(kScanMostWarps, kScanMostCluster);
+    cudaError_t e = once.allow(kernel, most_shared);
+    if (e == cudaSuccess) e = cluster_once.allow(cluster_kernel, most_shared);
     int gpu = 0;
     if (e == cudaSuccess) e = cudaGetDevice(&gpu);
     if (e != cudaSuccess) return e;
@@ -63,16 +74,34 @@ cudaError_t scan_launch(ScanParams p, cudaStream_t st)
     int warps = 1, cluster = 1;
     while (warps < kScanMostWarps && warps * S < p.tokens) warps *= 2;
     const auto shared = [&](int k) { return Ring::kBytes * warps + Shared::bytes(warps, k); };
-    // longer sequences of few channels over as many CTAs as all work at once
-    if (warps == kScanMostWarps)
+    const long long room = 2LL * std::min(sm_count(), kScanMostSms) / items;             // chunks that find room at once
+    p.chunks = 1, p.chunk = p.tokens;
+    if (warps == kScanMostWarps && scan_chunked(GRAD, room, p.tokens / (kScanMostCluster * kScanMostWarps * S))) {
+        const int round = warps * S, most = (int)std::min<long long>(room, p.tokens / (kScanLeastChunk * round));
+        p.chunk = ((p.tokens + most - 1) / most + round - 1) / round * round;
+        p.chunks = (p.tokens + p.chunk - 1) / p.chunk;
+    }
+    if (p.chunks > 1) {
+        static OncePerGpu map_once;
+        const size_t states = (size_t)p.batch * p.chunks * p.channels * sizeof(A), rings = ScanMapRing<T, G, V>::kBytes * kScanMostWarps;
+        char *const at = static_cast<char *>(ws) + sizeof(WsHead);
+        p.map_a = at, p.map_h = at + states, p.carry = at + 2 * states, p.map_drops = reinterpret_cast<int *>(at + 3 * states);
+        e = map_once.allow(scan_map_kernel<T, G, V, GRAD>, rings);
+        if (e == cudaSuccess) e = launch_beside(scan_map_kernel<T, G, V, GRAD>, dim3((unsigned)(items * p.chunks)), kScanCta, st, rings, p);
+        const unsigned ctas = (unsigned)((p.batch * p.channels + kScanCta - 1) / kScanCta);
+        if (e == cudaSuccess) e = launch_beside(scan_carry_kernel<A, GRAD>, dim3(ctas), kScanCta, st, (size_t)0, p);
+        if (e != cudaSuccess) return e;
+    } else if (warps == kScanMostWarps) {
+        // longer sequences of few channels over as many CTAs as all work at once
         while (cluster < kScanMostCluster && items <= 1000 && cluster * warps * S < p.tokens
-               && fit.clusters(kernel, gpu, 32 * warps, shared(cluster + 1), cluster + 1) >= items)
+               && fit.clusters(cluster_kernel, gpu, 32 * warps, shared(cluster + 1), cluster + 1) >= items)
             ++cluster;
-    return launch_beside(kernel, dim3((unsigned)(items * cluster)), 32 * warps, st, shared(cluster), p, cluster);
+    }
+    return launch_beside(cluster > 1 ? cluster_kernel : kernel, dim3((unsigned)(items * p.chunks * cluster)), 32 * warps, st, shared(cluster), p, cluster);
 }
 
 template <class T, class G>
-cudaError_t launch_scan(ScanParams p, bool grad, cudaStream_t st)
+cudaError_t launch_scan(ScanParams p, bool grad, void *ws, cudaStream_t st)
 {
     // a decoding step takes 5.9 us this way, 8.9 by segments (64 x 1 x 4096)
     if (!grad && p.tokens <= 4) {
@@ -80,7 +109,7 @@ cudaError_t launch_scan(ScanParams p, bool grad, cudaStream_t st)
         const long long threads = p.batch * ((p.channels + V - 1) / V);
         return launch_beside(scan_step_kernel<T, G, V>, dim3((unsigned)((threads + kScanCta - 1) / kScanCta)), kScanCta, st, (size_t)0, p);
     }
-    return grad ? scan_launch<T, G, true>(p, st) : scan_launch<T, G, false>(p, st);
+    return grad ? scan_launch<T, G, true>(p, ws, st) : scan_launch<T, G, false>(p, ws, st);
 }
 
 }  // namespace fo

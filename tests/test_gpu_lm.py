@@ -340,6 +340,34 @@ def test_scan_long_memory():
         c.check()
 
 
+@pytest.mark.parametrize("dtype,gate", PAIRS)
+@pytest.mark.parametrize("tokens,batch,channels", [(8192, 1, 33), (8200, 3, 66), (9001, 2, 200), (8193, 4, 1)])
+def test_scan_in_chunks(dtype, gate, tokens, batch, channels):
+    """Sequences that are long for their channels: ends in the first, a middle and the last chunk, at a border and nowhere, chunks with
+    resets and without."""
+    decay, mix = MODES[(tokens + PAIRS.index((dtype, gate))) % 9]
+    lengths = [tokens - 3, 4096, 700, 0][:batch] if batch > 1 else None
+    Scan(batch, tokens, channels, dtype, gate, decay, mix, reset=0.0004, lengths=lengths).check()
+    Scan(batch, tokens, channels, dtype, gate, "sigmoid", "rest", state=False, lengths=lengths, shift=1, pad=3).check()
+
+
+def test_scan_in_chunks_and_in_one():
+    """In place, without gradients of one result, and marks at the borders of all segments."""
+    c = Scan(2, 12288, 64, BF16, BF16, "sigmoid", "rest")
+    h, last = fo.fused_scan(c.x, c.gate, **c.how())
+    x, state = c.x.clone(), c.state.clone()
+    got = fo.fused_scan(x, c.gate, c.kind, c.mix, state, out=x, out_state=state)
+    assert torch.equal(got[0], h) and torch.equal(got[1], last) and got[0].data_ptr() == x.data_ptr()
+    zero = torch.zeros_like(c.dh)
+    a = fo.fused_scan_grad(None, c.x, c.gate, h, dlast=c.dlast, **c.how())
+    b = fo.fused_scan_grad(zero, c.x, c.gate, h, dlast=c.dlast, **c.how())
+    assert all(torch.equal(a[k], b[k]) for k in b)
+    c.reset = torch.zeros(2, 12288, dtype=torch.bool, device="cuda")
+    c.reset[0, ::64] = True
+    c.reset[1, 63::64] = True
+    c.check()
+
+
 def test_scan_missing_gradients():
     c = Scan(2, 33, 64, BF16, BF16, "sigmoid", "one")
     h, _ = fo.fused_scan(c.x, c.gate, **c.how())

@@ -76,19 +76,21 @@ def test_head_norm_grad_refusals(lib):
 
 def scan(lib, grad=False, **kw):
     v = dict(batch=2, tokens=8, channels=64, type=BF16, gate_type=BF16, decay=1, mix=1, x=0x1000, gate=0x2000, state=0, reset=0, lengths=0, at=(512, 64),
-             gate_at=(512, 64), reset_at=(8, 1), lengths_type=I64, h=0x3000, last=0x4000, dh=0x5000, dlast=0, dx=0x6000, dgate=0x6800, dstate=0)
+             gate_at=(512, 64), reset_at=(8, 1), lengths_type=I64, h=0x3000, last=0x4000, dh=0x5000, dlast=0, dx=0x6000, dgate=0x6800, dstate=0,
+             ws=0x10000, ws_bytes=1 << 30)
     v.update(kw)
     head = struct.pack("3q4i", *(v[k] for k in ("batch", "tokens", "channels", "type", "gate_type", "decay", "mix")))
     if not grad:
         return lib.fused_scan(head + struct.pack("5Q6qii2Q2q", v["x"], v["gate"], v["state"], v["reset"], v["lengths"], *v["at"], *v["gate_at"],
-                                                 *v["reset_at"], v["lengths_type"], 0, v["h"], v["last"], *v["at"]), None)
+                                                 *v["reset_at"], v["lengths_type"], 0, v["h"], v["last"], *v["at"]), v["ws"], v["ws_bytes"], None)
     return lib.fused_scan_grad(head + struct.pack("8Q10qii3Q4q", v["dh"], v["dlast"], v["x"], v["gate"], v["h"], v["state"], v["reset"], v["lengths"],
                                                   *v["at"], *v["at"], *v["gate_at"], *v["at"], *v["reset_at"], v["lengths_type"], 0, v["dx"], v["dgate"],
-                                                  v["dstate"], *v["at"], *v["gate_at"]), None)
+                                                  v["dstate"], *v["at"], *v["gate_at"]), v["ws"], v["ws_bytes"], None)
 
 
 def test_scan_refusals(lib):
-    assert lib.fused_scan(None, None) == -1 and lib.fused_scan_grad(None, None) == -1
+    assert lib.fused_scan(None, None, 0, None) == -1 and lib.fused_scan_grad(None, None, 0, None) == -1
+    assert lib.fused_scan_workspace_bytes() > 16384
     for grad in (False, True):
         one = lambda **kw: scan(lib, grad, **kw)  # noqa: E731
         assert one(batch=-1) == -2 and one(tokens=-1) == -2 and one(channels=-1) == -2
@@ -97,6 +99,8 @@ def test_scan_refusals(lib):
         assert one(lengths=0x7004) == -4 and one(at=(-1, 64)) == -2 and one(gate_at=(512, -1)) == -2 and one(reset_at=(-8, 1)) == -2
         assert one(x=0) == -1 and one(gate=0) == -1 and one(h=0) == -1 and one(x=0x1001) == -4 and one(gate=0x2001) == -4
         assert one(state=0x7002) == -4 and one(batch=1 << 30, channels=1 << 20) == -4
+        assert one(tokens=(1 << 30) + 1) == -4 and one(channels=(1 << 28) + 1) == -4
+        assert one(ws=0) == -5 and one(ws=0x10008) == -5 and one(ws_bytes=16384) == -5
         assert one(batch=0) == 0 and one(channels=0) == 0 and one(tokens=0, last=0) == 0
     assert scan(lib, True, dx=0) == -1 and scan(lib, True, dgate=0) == -1 and scan(lib, True, dgate=0x6801) == -4 and scan(lib, True, dstate=0x6802) == -4
     assert scan(lib, last=0x4002) == -4
