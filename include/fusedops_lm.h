@@ -108,6 +108,8 @@ size_t fused_head_norm_grad_workspace_bytes(int dim, int type);
  * `last` may be `state`.  1 - a is computed without the cancellation; 16-bit x goes through the hardware's
  * exponential and reciprocal, decays near 1 rounded to 32 bits all the same.
  * Element (b, t, c) of x, gate, h is at p[b * batch + t * token + c].  state and last: float (double for FO_F64), contiguous.
+ * Products of the decays over parts of the sequence are formed in 32 bits (64 for FO_F64): where they overflow, which takes decays above 1, or
+ * where a state is infinite, h may be NaN.  It is NaN, too, should the CTAs that share a sequence lose each other.
  * gate_type: `type`, or FO_F32 with a 16-bit type.  channels <= FO_SCAN_MAX_CHANNELS, tokens <= FO_SCAN_MAX_TOKENS.  h may be
  * x itself.  A decoding step is the call with tokens = 1.
  */
@@ -157,7 +159,8 @@ int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stre
  *     tail NULL:  p = softmax(v / temperature) over the entries;      loss = sum_k p_k (log p_k - log q_{id_k})
  *     tail given: p_k = exp(v_k / temperature - tail), the teacher's own shares (tail: the log-sum-exp of its whole row over
  *                 temperature), P = max(0, 1 - sum p) and Q = 1 - sum q_{id_k} all that is outside the entries;
- *                 loss as above + P log(P / Q)
+ *                 loss as above + P log(P / Q); where Q is zero (the entries are all the row, or the rest is masked) a P of at
+ *                 most 1 / 32 is what the rounding of v and tail has left, and taken as zero; a larger one makes the loss infinite
  * An entry with a negative id is none; one with an id >= vocab makes the row NaN.  Entries with the same id are one place of q
  * with several shares.  Without entries the first form's loss is zero; p_k = 0 adds nothing.
  * Gradient, times dloss of the row (float; NULL: 1):

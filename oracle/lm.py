@@ -187,6 +187,8 @@ def distill(logits, ids, values, tail, temperature):
             some = p > 0
             loss[r] = (p[some] * (np.log(p[some]) - logq[at][some])).sum()
             ratio = 0.0
+            if e[out].sum() == 0 and rest <= 1 / 32:         # the rounding of values and tail
+                rest = 0.0
             if rest > 0:
                 ratio = rest / (e[out].sum() / total)
                 loss[r] += rest * np.log(ratio)

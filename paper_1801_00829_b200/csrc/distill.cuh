@@ -99,6 +99,10 @@ __device__ __forceinline__ double teacher_value(const DistillParams &p, long lon
     return v * p.inv_t;
 }
 
+// P up to this is taken as zero where nothing of q lies outside the entries (they are the whole vocabulary, or the rest of it is
+// masked): it is what the rounding of values and tail has left.  A value of 16 is off by 2^-5 in bfloat16, and so is its share then.
+constexpr double kDistillNoise = 0.03125;
+
 // What all threads need to know of the entries besides the arrays.
 struct TeacherSums {
     double top_max, log_sum;            // log p = v / temperature - top_max - log_sum
@@ -275,7 +279,7 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     constexpr int E = 16 / (int)sizeof(T), kTogether = 4;
     extern __shared__ __align__(16) unsigned char distill_memory[];
     __shared__ DistillPart all_parts[kDistillRow / 32];
-    __shared__ double results[kDistillCta / 32][5];
+    __shared__ double results[kDistillCta / 32][6];
     __shared__ TeacherSums teachers[kDistillCta / 32];
     wait_for_earlier();
     const int number = threadIdx.x / p.team, lane = threadIdx.x & 31, step = p.team;
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     if (lane == 0) parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
     team.sync();
     // the row's
-    double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0;
+    double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0, rest = 0.0;
     if (warp == 0) {
         DistillPart d = {-CUDART_INF, 0.0, -CUDART_INF, 0.0, 0.0};
         if (lane < warps) d = parts[lane];
@@ -428,11 +432,13 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
         rest_of_row = distill_warp_sum(rest_of_row);
         total = rest_of_row + distill_warp_sum(d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - row_max) * p.inv_t) : 0.0);
         row_entries = distill_warp_sum(d.entries);
-        double factor = teacher.sum + teacher.rest;
-        if (teacher.rest > 0.0) factor -= teacher.rest * total / rest_of_row;
+        rest = rest_of_row == 0.0 && teacher.rest <= kDistillNoise ? 0.0 : teacher.rest;
+        double factor = teacher.sum + rest;
+        if (rest > 0.0) factor -= rest * total / rest_of_row;
         if (!(teacher.sum == teacher.sum)) factor = CUDART_NAN;           // an id outside the row
         const double inverse = 1.0 / total;
-        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor, result[3] = inverse, result[4] = (double)weight * p.inv_t * factor * inverse;
+        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor, result[3] = inverse, result[4] = (double)weight * p.inv_t * factor * inverse,
+                       result[5] = teacher.sum + rest;
     }
     if constexpr (STEP) {
         team.sync();
@@ -478,7 +484,7 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
         }
         if (ends) distill_put(at, other, dz, false, gradient(ragged(other)));
         team.sync();                                      // the entries' places have been written like the others
-        const double by = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
+        const double by = (double)weight * p.inv_t, s_all = result[5];
         for (int k = team.thread; k < p.top; k += step)
             if (t.place[k] >= 0) {
                 const double q = exp((t.z[k] - result[0]) * p.inv_t) * result[3];
@@ -489,7 +495,7 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     if (team.thread == 0) {
         const double log_total = row_max * p.inv_t + log(total);
         double loss = teacher.sum != 0.0 ? row_entries + teacher.sum * log_total : 0.0;
-        if (teacher.rest > 0.0) loss += teacher.rest * log(teacher.rest * total / rest_of_row);        // P (log P - log Q)
+        if (rest > 0.0) loss += rest * log(rest * total / rest_of_row);        // P (log P - log Q)
         if (!(teacher.sum == teacher.sum)) loss = CUDART_NAN;
         if (p.loss) static_cast<A *>(p.loss)[row] = A(loss);
         if (!STEP && p.stats) {
@@ -549,7 +555,9 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
     const int from = first * E - at.skip, to = last * E - at.skip;
     const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
     __syncthreads();
-    const double scale = (double)weight * p.inv_t, s_all = teacher.sum + teacher.rest;
+    // the statistics' S - P / Q is below sum p, unless P was taken as zero
+    const bool all = teacher.rest <= kDistillNoise && factor >= A(teacher.sum);
+    const double scale = (double)weight * p.inv_t, s_all = all ? teacher.sum : teacher.sum + teacher.rest;
     // an id outside the row is one in the statistics too, and makes them NaN
     const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (double)factor / (double)total);
     const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;

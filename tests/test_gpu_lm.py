@@ -514,6 +514,32 @@ def test_distill_masked_logits(dtype):
         assert (loss[4:] == 0).all() and (dz[4:] == 0).all() and torch.isfinite(dz[:4]).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_distill_entries_that_are_all_there_is(dtype):
+    """With a tail and nothing outside the entries, what rounding leaves of the teacher's other shares is not compared with nothing."""
+    for vocab in (1, 2, 17, 300):
+        c = Distill(400, vocab, vocab, F32 if dtype == F64 else dtype, True, temperature=0.7)
+        loss, _, dz = c.check()
+        assert torch.isfinite(loss).all() and torch.isfinite(dz).all()
+    c = Distill(300, 1000, 1000, F32 if dtype == F64 else dtype, True)
+    c.ids, c.values = c.ids[:, :12].contiguous(), c.values[:, :12].contiguous()
+    c.tail = c.values.to(c.tail.dtype).logsumexp(1)
+    free = torch.ones(300, 1000, dtype=torch.bool, device="cuda").scatter_(1, c.ids, False)
+    for bad in (float("-inf"), torch.finfo(c.dtype).min):
+        c.logits[free] = bad
+        loss, _, dz = c.check()
+        assert torch.isfinite(loss).all() and torch.isfinite(dz).all()
+    c.tail += 0.1                                            # a tenth of the teacher's shares lies where the student's are zero
+    assert torch.isinf(fo.fused_distill(*c.args(), **c.how())[0]).all()
+    if dtype == F64:                                         # in 64 bits the sums' last bits are the bound's too
+        c = Distill(500, 200, 200, F64, True)
+        loss, stats = fo.fused_distill(*c.args(), stats=True, **c.how())
+        want = ref.distill(host(c.logits), host(c.ids), host(c.values), host(c.tail), 1.0)[0]
+        # 200 additions in each of four sums of shares and probabilities, times logarithms below 32
+        assert np.abs(host(loss) - want).max() <= 4 * 200 * 32 * 2.0 ** -53
+        assert torch.isfinite(fo.fused_distill_grad(None, *c.args(), stats, **c.how())).all()
+
+
 def test_distill_is_cross_entropy_for_one_entry():
     rng = np.random.RandomState(3)
     z = made(rng, (50, 1003), F32, 3.0)
