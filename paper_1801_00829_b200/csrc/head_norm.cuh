@@ -63,7 +63,6 @@ __device__ __forceinline__ U head_all(A v)
     if constexpr (std::is_same<U, A>::value) return v;
     else return both(v);
 }
-template <class A> __device__ __forceinline__ Two<A> head_swap(Two<A> u) { return two(second(u), first(u)); }
 
 // What a lane holds of a vector: item i is the pieces at a[i] and b[i] (-1: none), of which ta and tb are turned.  Pieces that are
 // not turned against each other are dealt out so that neighbouring lanes have neighbouring pieces.
@@ -125,10 +124,12 @@ struct HeadWork {
     static constexpr int N = V == 1 ? 1 : V / 2;             // units of a piece
     static constexpr bool HALVES = PAIRING == FO_PAIR_HALVES || V == 1;
 
-    // Cosines and sines of a lane's pairs.  Halves: of the units of a piece, with the sine's negative; neighbours: (c, c) and (-s, s) for
-    // every unit, which is a pair, of both pieces.
+    // Cosines and sines of a lane's pairs.  Halves: of the units of a piece, with the sine's negative; neighbours: of every unit, which is a
+    // pair, of both pieces (turned value by value: two products and two sums, as many instructions as packed with the two values
+    // swapped, and half the registers).
+    using Angle = typename std::conditional<HALVES, U, A>::type;
     struct Angles {
-        U c[I][HALVES ? N : 2 * N], s[I][HALVES ? N : 2 * N], minus[HALVES ? I : 1][N];
+        Angle c[I][HALVES ? N : 2 * N], s[I][HALVES ? N : 2 * N], minus[HALVES ? I : 1][N];
     };
     // n values of both tables from `pair` on, of which the first `there` exist; NaN outside the table
     template <int M>
@@ -188,7 +189,7 @@ struct HeadWork {
                     A c[N], s[N];
                     table<N>(p, rows, k ? at.pair_b(i) : at.pair_a(i), k ? at.tb(i) : at.ta(i), c, s);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) g.c[i][k * N + j] = both(c[j]), g.s[i][k * N + j] = two(A(-SIGN) * s[j], A(SIGN) * s[j]);
+                    for (int j = 0; j < N; ++j) g.c[i][k * N + j] = c[j], g.s[i][k * N + j] = A(SIGN) * s[j];
                 }
             }
         }
@@ -213,6 +214,12 @@ struct HeadWork {
             if (!HALVES && at.tb(i)) ask(at.pair_b(i));
         }
     }
+    static __device__ __forceinline__ U turned(U u, A c, A s)
+    {
+        const A x = part(u, 0), y = part(u, 1);
+        if constexpr (V == 1) return u;
+        else return two(fused_ma(-y, s, x * c), fused_ma(x, s, y * c));
+    }
     // Turns a lane's pieces.
     static __device__ __forceinline__ void turn(const Items &at, const Angles &g, U (&a)[I][N], U (&b)[I][N])
     {
@@ -229,10 +236,10 @@ struct HeadWork {
             } else {
                 if (at.ta(i))
 #pragma unroll
-                    for (int j = 0; j < N; ++j) a[i][j] = fused_ma(head_swap(a[i][j]), g.s[i][j], a[i][j] * g.c[i][j]);
+                    for (int j = 0; j < N; ++j) a[i][j] = turned(a[i][j], g.c[i][j], g.s[i][j]);
                 if (at.tb(i))
 #pragma unroll
-                    for (int j = 0; j < N; ++j) b[i][j] = fused_ma(head_swap(b[i][j]), g.s[i][N + j], b[i][j] * g.c[i][N + j]);
+                    for (int j = 0; j < N; ++j) b[i][j] = turned(b[i][j], g.c[i][N + j], g.s[i][N + j]);
             }
         }
     }
@@ -329,6 +336,21 @@ struct HeadWork {
         else
 #pragma unroll
             for (int j = 0; j < N; ++j) f[j] = two(s[2 * j], s[2 * j + 1]);
+    }
+    // A piece of a vector in shared memory.
+    static __device__ __forceinline__ void shared_piece(const A *v, U (&f)[N])
+    {
+        if constexpr (V == 1) {
+            f[0] = *v;
+        } else {
+            constexpr int W = 16 / (int)sizeof(A);
+#pragma unroll
+            for (int j0 = 0; j0 < V; j0 += W) {
+                const HeadPiece<A, W> s = head_load<A, W>(v + j0);
+#pragma unroll
+                for (int j = 0; j < W; j += 2) f[(j0 + j) / 2] = two(s.v[j], s.v[j + 1]);
+            }
+        }
     }
     static __device__ __forceinline__ void weights(const HeadParams &p, const HeadTensor &t, const Items &at, U (&a)[I][N], U (&b)[I][N])
     {
@@ -539,6 +561,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     using U = typename W::U;
     constexpr int N = W::N;
     extern __shared__ __align__(16) unsigned char head_memory[];
+    __shared__ __align__(16) A weights[FO_HEAD_MAX_DIM + 16];
     wait_for_earlier();
     const int which = blockIdx.x >= (unsigned)p.ctas0;
     const HeadTensor &t = p.t[which];
@@ -566,8 +589,11 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         } else if (ahead.there()) enter();
     };
     for (int k = 0; k < ring.kTurns; ++k) issue();
-    U wa[I][N], wb[I][N], da[I][N], db[I][N], ea[BIAS ? I : 1][N], eb[BIAS ? I : 1][N];
-    W::weights(p, t, at, wa, wb);
+    U da[I][N], db[I][N], ea[BIAS ? I : 1][N], eb[BIAS ? I : 1][N];
+    // the weights, with zeros for pieces that are none (in registers they made the loop spill others)
+    for (int j = threadIdx.x; j < p.dim + V; j += kHeadCta)
+        weights[j] = j >= p.dim ? A(0) : !t.weight ? A(1) : p.wide_vec ? (A) static_cast<const float *>(t.weight)[j] : widen(static_cast<const T *>(t.weight)[j]);
+    __syncthreads();
     const U zero = head_all<U>(A(0));
 #pragma unroll
     for (int i = 0; i < I; ++i)
@@ -601,16 +627,19 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
             const A r = W::normalise(p.lanes, inv_dim, at, kind, on ? eps : A(1), a, b);
             U with_n = zero, alone = zero;
 #pragma unroll
-            for (int i = 0; i < I; ++i)
+            for (int i = 0; i < I; ++i) {
+                U wa[N], wb[N];
+                W::shared_piece(weights + (at.a[i] >= 0 ? at.a[i] : p.dim), wa), W::shared_piece(weights + (at.b[i] >= 0 ? at.b[i] : p.dim), wb);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     da[i][j] = fused_ma(u[i][j], a[i][j], da[i][j]);
                     db[i][j] = fused_ma(v[i][j], b[i][j], db[i][j]);
                     if (BIAS) ea[i][j] = ea[i][j] + u[i][j], eb[i][j] = eb[i][j] + v[i][j];
-                    u[i][j] = u[i][j] * wa[i][j], v[i][j] = v[i][j] * wb[i][j];
+                    u[i][j] = u[i][j] * wa[j], v[i][j] = v[i][j] * wb[j];
                     with_n = fused_ma(u[i][j], a[i][j], fused_ma(v[i][j], b[i][j], with_n));
                     alone = alone + (u[i][j] + v[i][j]);
                 }
+            }
             const U back = head_all<U>(-W::sum(with_n, p.lanes) * inv_dim), all = head_all<U>(r);
             const U mean = kind == FO_NORM_LAYER ? head_all<U>(-W::sum(alone, p.lanes) * inv_dim) : zero;
 #pragma unroll

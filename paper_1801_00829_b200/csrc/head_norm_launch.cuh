@@ -12,7 +12,7 @@ cudaError_t head_go(void (*kernel)(HeadParams), const HeadParams &p, int grid, c
     // the ring; in its place at the end the gradient's sums, a line for every group of lanes
     constexpr size_t lines = TENSORS == 2 ? (size_t)kHeadWarps * 64 * I * V * sizeof(Acc<T>) : 0, ring = HeadRing<T, V, I, TENSORS>::kBytes;
     constexpr size_t bytes = ring > lines ? ring : lines;
-    if (bytes > 48 * 1024) {
+    if (bytes + (FO_HEAD_MAX_DIM + 16) * sizeof(double) > 48 * 1024) {        // with the weights
         const cudaError_t e = once.allow(kernel, bytes);
         if (e != cudaSuccess) return e;
     }
