@@ -141,25 +141,34 @@ int head_lanes(int dim, int piece)
     return lanes;
 }
 
-// Cuts a call into tasks, of whole tokens where there are enough of them to occupy the GPU's warps and of a few heads
-// otherwise (one decoding step of 4 tokens: 40 warps instead of 8), and gives the tensors CTAs by their work.  Returns the grid.
+// Cuts a call into turns of the warps, the same number for each, and gives the tensors CTAs by their work.  Returns the grid.
 int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
 {
     const int groups = 32 / p.lanes;
     p.tokens = (int)std::max<long long>(tokens, 1), p.all_tokens = (int)(batch * tokens);
     const long long warps = (long long)sms * kHeadCtas * kHeadWarps;
-    // a task costs its turns and, for its token's cosines and sines, about one more
-    long long turns[2] = {0, 0}, ctas[2] = {0, 0};
-    for (int k = 0; k < count; ++k) turns[k] = (p.t[k].heads + groups - 1) / groups;
-    const long long all = p.all_tokens * (turns[0] + turns[1]), each = std::max<long long>(1, all / warps);
+    long long wide = 0, narrow = 0, ctas[2] = {0, 0}, cost[2] = {0, 0};
+    for (int k = 0; k < count; ++k)
+        wide += (long long)((p.all_tokens + groups - 1) / groups) * p.t[k].heads, narrow += (long long)p.all_tokens * ((p.t[k].heads + groups - 1) / groups);
+    // Blocks of several tokens, whose cosines and sines serve as many turns as there are heads, where that leaves every warp four turns
+    // (40 heads of 128 in bfloat16: 1024 tokens 8 us both ways, 4096 tokens 19 against 21, backwards 33 and 35), or at least one
+    // and a quarter of the turns less, because heads do not come out even with the groups (7 heads of 64, 4000 tokens: 5.5 and 9.1).  With
+    // few tokens the heads of one are side by side: a decoding step of 4 tokens is 40 warps of one turn, not one of 40.
+    p.wide = wide >= 4 * warps || (wide >= warps && 4 * wide <= 3 * narrow);
     for (int k = 0; k < count; ++k) {
         HeadTensor &t = p.t[k];
-        t.per_chunk = (int)std::max<long long>(1, std::min(each, turns[k])) * groups;
-        t.chunks = std::max(1, (t.heads + t.per_chunk - 1) / t.per_chunk);
-        const long long tasks = (long long)p.all_tokens * (t.heads ? t.chunks : 0);
-        const long long cost = turns[k] ? turns[k] + 1 : 0, both = (turns[0] ? turns[0] + 1 : 0) + (turns[1] ? turns[1] + 1 : 0);
-        const long long share = all ? std::max<long long>(1, (long long)sms * kHeadCtas * cost / std::max<long long>(1, both)) : 0;
-        ctas[k] = std::min((tasks + kHeadWarps - 1) / kHeadWarps, share);
+        t.blocks = p.wide ? (p.all_tokens + groups - 1) / groups : p.all_tokens;
+        t.turns = p.wide ? t.heads : (t.heads + groups - 1) / groups;
+        // a block costs its turns and, for the cosines and sines, about one more
+        cost[k] = t.turns ? (long long)t.blocks * (t.turns + 1) : 0;
+    }
+    for (int k = 0; k < count; ++k) {
+        HeadTensor &t = p.t[k];
+        const long long turns = (long long)t.blocks * t.turns;
+        const long long share = std::max<long long>(1, (long long)sms * kHeadCtas * cost[k] / std::max<long long>(1, cost[0] + cost[1]));
+        ctas[k] = std::min((turns + kHeadWarps - 1) / kHeadWarps, share);
+        if (ctas[k]) t.each = (int)((turns + ctas[k] * kHeadWarps - 1) / (ctas[k] * kHeadWarps));
+        else t.turns = 1;
     }
     p.ctas0 = (int)ctas[0];
     return (int)(ctas[0] + ctas[1]);

@@ -1,6 +1,7 @@
 // Head norms with rotation: y = R(position) norm(x) for every head's vector of queries and keys, and the gradient.
 //
-// A vector belongs to L lanes (a power of two up to 32), so that a warp works on 32 / L heads of one token at a time (a turn); a
+// A vector belongs to L lanes (a power of two up to 32), so that a warp works on 32 / L vectors at a time (a turn): on a head of as many
+// tokens or on as many heads of one token; a
 // lane holds I items of two pieces of V elements each: with halves the two pieces that are turned against each other, else two
 // neighbouring ones.  Everything of a vector stays in registers between its one load and its one store, and what a token's heads
 // share (cosines, sines, weights) is loaded once per token or once per CTA.  A lane's pieces of the next turns are on their way to
@@ -19,7 +20,8 @@ struct HeadTensor {
     const void *x, *dy;
     void *y;                            // the gradient's dx
     fo_strides x_at, dy_at, y_at;
-    int heads, kind, chunks, per_chunk; // a task: per_chunk heads of one token
+    int heads, kind;
+    int blocks, turns, each;            // blocks of tokens, turns of a block and of a warp
     const void *weight, *bias;
     double eps;
     void *partial_w, *partial_b;        // gradient: ctas lines of dim values each, or NULL
@@ -29,6 +31,7 @@ struct HeadParams {
     HeadTensor t[2];
     int ctas0;                          // CTAs [0, ctas0) work on tensor 0, the rest on tensor 1
     int tokens, all_tokens;             // of a sequence, and of all of them
+    int wide;                           // a block is as many tokens as a warp has groups; else it is one
     int dim, lanes, pairs, axes;
     int wide_vec, table_pieces, long_positions;
     int section_end[FO_MAX_AXES];
@@ -101,7 +104,8 @@ struct HeadRows {
 };
 __device__ __forceinline__ HeadRows head_rows(const HeadParams &p, unsigned token)
 {
-    HeadRows r;
+    HeadRows r = {};
+    if (token >= (unsigned)p.all_tokens) return r;
     const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
     const long long place = b * p.position_batch + t * p.position_token;
     const auto row_at = [&](long long at) {
@@ -432,30 +436,30 @@ struct HeadRing {
     }
 };
 
-// The turns of a warp, one behind the other: `h0` is the turn's first head (of the warp's first group), `end` the end of
-// the task's heads.
+// The turns of a warp, one behind the other, through blocks of tokens: in a turn the groups work on a head of a token each (wide), or on
+// as many heads of one token.  Every warp has the same number of turns and begins where the one before it ends, within a block.
 struct HeadTurns {
-    unsigned task, tasks, step, token;
-    int h0, end, groups;
-    __device__ __forceinline__ HeadTurns(const HeadParams &p, const HeadTensor &t, int cta, int ctas)
-        : task(cta * kHeadWarps + threadIdx.x / 32), tasks((unsigned)p.all_tokens * (unsigned)t.chunks), step(ctas * kHeadWarps), groups(32 / p.lanes)
+    int block, h0, left, by;            // h0: the first group's head; left: turns to come
+    int group, beside;                  // group: of the lane; beside: its head is h0 + beside
+    int wide, groups;
+    __device__ __forceinline__ HeadTurns(const HeadParams &p, const HeadTensor &t, int cta, int group_)
+        : group(group_), wide(p.wide), groups(32 / p.lanes)
     {
-        enter(t);
+        const unsigned first = (unsigned)(cta * kHeadWarps + (int)(threadIdx.x / 32)) * (unsigned)t.each, all = (unsigned)t.blocks * (unsigned)t.turns;
+        left = first < all ? (int)min(all - first, (unsigned)t.each) : 0;
+        by = wide ? 1 : groups, beside = wide ? 0 : group;
+        block = (int)(first / (unsigned)t.turns), h0 = (int)(first - (unsigned)block * (unsigned)t.turns) * by;
     }
-    __device__ __forceinline__ bool there() const { return task < tasks; }
-    __device__ __forceinline__ void enter(const HeadTensor &t)
-    {
-        token = task / (unsigned)t.chunks;
-        h0 = (int)((task - token * (unsigned)t.chunks) * (unsigned)t.per_chunk);
-        end = min(t.heads, h0 + t.per_chunk);
-    }
-    // true: a new task, of another token
+    __device__ __forceinline__ bool there() const { return left > 0; }
+    // the lane's token, of this block or a later one
+    __device__ __forceinline__ int token(int later = 0) const { return wide ? (block + later) * groups + group : block + later; }
+    __device__ __forceinline__ bool on(const HeadParams &p, const HeadTensor &t) const { return h0 + beside < t.heads && token() < p.all_tokens; }
+    // true: a new block
     __device__ __forceinline__ bool next(const HeadTensor &t)
     {
-        h0 += groups;
-        if (h0 < end) return false;
-        task += step;
-        if (there()) enter(t);
+        --left, h0 += by;
+        if (h0 < t.heads) return false;
+        h0 = 0, ++block;
         return true;
     }
 };
@@ -464,16 +468,17 @@ template <class T>
 struct HeadWay {
     T *at = nullptr;
     long long step;
-    __device__ __forceinline__ void enter(const HeadParams &p, const void *x, const fo_strides &s, const HeadTurns &turn, int group)
+    __device__ __forceinline__ void enter(const HeadParams &p, const void *x, const fo_strides &s, const HeadTurns &turn)
     {
-        const long long b = turn.token / (unsigned)p.tokens, t = turn.token - b * p.tokens;
-        at = static_cast<T *>(const_cast<void *>(x)) + b * s.batch + t * s.token + (turn.h0 + group) * s.head;
-        step = turn.groups * s.head;
+        const unsigned token = turn.token(), b = token / (unsigned)p.tokens, t = token - b * (unsigned)p.tokens;
+        at = static_cast<T *>(const_cast<void *>(x)) + b * s.batch + t * s.token + (turn.h0 + turn.beside) * s.head;
+        step = turn.by * s.head;
     }
     __device__ __forceinline__ void next() { at += step; }
 };
 
-// 8192 tokens with 32 + 8 heads of 128 in bfloat16
+// Bound by the instructions of a turn, about 260 of a warp (backwards 410), at the rate at which 16 warps an SM issue them, 0.55 to 0.6 of
+// a cycle: 4 x 2048 tokens with 32 + 8 heads of 128 in bfloat16 take 36 us (4.8 TB/s), backwards 59 us (4.3 TB/s).
 template <class T, int V, int I, int PAIRING>
 __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_norm_kernel(const __grid_constant__ HeadParams p)
 {
@@ -487,33 +492,32 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     const HeadTensor &t = p.t[which];
     const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, kind = t.kind;
     const A eps = A(t.eps), inv_dim = A(p.inv_dim);
-    const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
+    const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x;
     const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
-    HeadTurns ahead(p, t, cta, ctas), now = ahead;
+    HeadTurns ahead(p, t, cta, group), now = ahead;
     if (!now.there()) return;
     const bool bias = t.bias != nullptr;
     HeadRing<T, V, I, 1> ring(head_memory);
     HeadWay<T> x, y;
-    x.enter(p, t.x, t.x_at, ahead, group), y.enter(p, t.y, t.y_at, now, group);
+    x.enter(p, t.x, t.x_at, ahead), y.enter(p, t.y, t.y_at, now);
     auto issue = [&]() {
         const T *const rows[1] = {x.at};
         const bool there = ahead.there();
-        ring.issue(rows, at, there && ahead.h0 + group < ahead.end);
+        ring.issue(rows, at, there && ahead.on(p, t));
         if (!there) return;
         if (!ahead.next(t)) x.next();
-        else if (ahead.there()) x.enter(p, t.x, t.x_at, ahead, group);
+        else if (ahead.there()) x.enter(p, t.x, t.x_at, ahead);
     };
     for (int k = 0; k < ring.kTurns; ++k) issue();
     U wa[I][N], wb[I][N];
     W::weights(p, t, at, wa, wb);
     typename W::Angles g;
     HeadRows rows = {};
-    if (p.pairs) rows = head_rows(p, now.token);
+    if (p.pairs) rows = head_rows(p, now.token());
     for (bool fresh = true; now.there();) {
         if (fresh && p.pairs) {
             W::template angles<1>(p, at, rows, g);
-            const unsigned later = now.task + now.step;
-            if (later < now.tasks) rows = head_rows(p, later / (unsigned)t.chunks);
+            rows = head_rows(p, now.token(1));
         }
         U a[I][N], b[I][N];
         ring.arrived();
@@ -543,11 +547,11 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
             }
         }
         if (p.pairs) W::turn(at, g, a, b);
-        if (now.h0 + group < now.end) W::store(y.at, at, a, b);
+        if (now.on(p, t)) W::store(y.at, at, a, b);
         if (fresh && p.pairs) W::expect(p, at, rows);
         fresh = now.next(t);
         if (!fresh) y.next();
-        else if (now.there()) y.enter(p, t.y, t.y_at, now, group);
+        else if (now.there()) y.enter(p, t.y, t.y_at, now);
     }
 }
 
@@ -567,21 +571,21 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
     const HeadTensor &t = p.t[which];
     const int lane = threadIdx.x & (p.lanes - 1), group = (threadIdx.x & 31) / p.lanes, kind = t.kind;
     const A eps = A(t.eps), inv_dim = A(p.inv_dim);
-    const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x, ctas = which ? gridDim.x - p.ctas0 : p.ctas0;
+    const int cta = which ? blockIdx.x - p.ctas0 : blockIdx.x;
     const typename W::Items at(lane, p.lanes, p.dim, p.pairs);
     const bool normed = kind != FO_NORM_NONE;
-    HeadTurns ahead(p, t, cta, ctas), now = ahead;
+    HeadTurns ahead(p, t, cta, group), now = ahead;
     HeadRing<T, V, I, 2> ring(head_memory);
     HeadWay<T> x, dy, dx;
     auto enter = [&]() {
-        if (normed) x.enter(p, t.x, t.x_at, ahead, group);
-        dy.enter(p, t.dy, t.dy_at, ahead, group);
+        if (normed) x.enter(p, t.x, t.x_at, ahead);
+        dy.enter(p, t.dy, t.dy_at, ahead);
     };
-    if (now.there()) enter(), dx.enter(p, t.y, t.y_at, now, group);
+    if (now.there()) enter(), dx.enter(p, t.y, t.y_at, now);
     auto issue = [&]() {
         const T *const rows[2] = {dy.at, x.at};
         const bool there = ahead.there();
-        ring.issue(rows, at, there && ahead.h0 + group < ahead.end);
+        ring.issue(rows, at, there && ahead.on(p, t));
         if (!there) return;
         if (!ahead.next(t)) {
             if (normed) x.next();
@@ -604,12 +608,11 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         }
     typename W::Angles g;
     HeadRows rows = {};
-    if (p.pairs && now.there()) rows = head_rows(p, now.token);
+    if (p.pairs && now.there()) rows = head_rows(p, now.token());
     for (bool fresh = true; now.there();) {
         if (fresh && p.pairs) {
             W::template angles<-1>(p, at, rows, g);
-            const unsigned later = now.task + now.step;
-            if (later < now.tasks) rows = head_rows(p, later / (unsigned)t.chunks);
+            rows = head_rows(p, now.token(1));
         }
         U a[I][N], b[I][N], u[I][N], v[I][N];
         ring.arrived();
@@ -620,7 +623,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         }
         ring.taken();
         issue();
-        const bool on = now.h0 + group < now.end;
+        const bool on = now.on(p, t);
         if (p.pairs) W::turn(at, g, u, v);
         if (normed) {
             // a group without a head has zeros throughout, and with eps 0 its r would not be finite
@@ -654,7 +657,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         if (fresh && p.pairs) W::expect(p, at, rows);
         fresh = now.next(t);
         if (!fresh) dx.next();
-        else if (now.there()) dx.enter(p, t.y, t.y_at, now, group);
+        else if (now.there()) dx.enter(p, t.y, t.y_at, now);
     }
     if (!t.partial_w && !t.partial_b) return;
     // every group of lanes writes its sums (where the ring was), and they are added in order
