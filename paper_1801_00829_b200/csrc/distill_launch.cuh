@@ -2,6 +2,8 @@
 #pragma once
 
 #include "distill.cuh"
+#include <algorithm>
+
 #include "launch.cuh"
 
 namespace fo {
@@ -32,10 +34,13 @@ cudaError_t launch_distill(DistillParams p, DistillWay way, cudaStream_t st)
     if (way == kDistillLoss) return distill_row_launch<T, false>(p, st);
     if (way == kDistillStep) return distill_row_launch<T, true>(p, st);
     const long long pieces = ((long long)p.vocab * (int)sizeof(T) + 15 - (int)sizeof(T)) / 16 + 1;
-    // eight pieces a thread at most, and of short rows four
+    // As many pieces a thread as pay for what a CTA does besides: 24 of short rows (16384 x 8192 in bfloat16 with four 154 us, with 24 102),
+    // up to 32 of long ones (4096 x 128000: with eight 445 us, with 32 358); but of few rows so few, down to eight, that there are
+    // CTAs for all SMs (8 x 128000: 7 us, with 32 13).
     int threads = 32;
-    while (threads < kDistillCta && threads * 4 < pieces) threads *= 2;
-    const int parts = (int)((pieces + threads * 8 - 1) / (threads * 8));
+    while (threads < kDistillCta && threads * 24 < pieces) threads *= 2;
+    const long long least = (pieces + threads * 32 - 1) / (threads * 32), most = (pieces + threads * 8 - 1) / (threads * 8);
+    const int parts = (int)std::max(least, std::min(most, (5LL * sm_count() + p.rows - 1) / p.rows));
     p.slice = (int)((pieces + parts - 1) / parts);
     return launch_beside(distill_grad_kernel<T>, dim3((unsigned)p.rows, (unsigned)parts), threads, st, (size_t)(p.top + 3) / 4 * 4 * kTeacherBytes, p);
 }
