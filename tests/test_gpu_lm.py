@@ -139,6 +139,14 @@ def test_head_counts(dtype, batch, tokens, hq, hk):
     Heads(batch, tokens, hq, hk, 64, 64, dtype, bias=True, long=tokens % 2 == 1).check()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("batch,tokens,hq,hk,dim", [(3, 2501, 12, 4, 64), (1, 4003, 7, 3, 128), (2, 3001, 6, 0, 72), (1, 9001, 2, 1, 30)])
+def test_heads_of_many_tokens(dtype, batch, tokens, hq, hk, dim):
+    """Several tokens side by side in a warp, of which the last ones and those of two sequences are not as many."""
+    Heads(batch, tokens, hq, hk, dim, dim, dtype, kind="layer" if dim == 72 else "rms", bias=dim == 72,
+          pairing="pairs" if dim == 72 else "halves", sections=(12, 12, 12) if dim == 72 else None, layout="apart" if dim == 128 else "packed").check()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("shift,pad", [(1, 0), (0, 3), (4, 4), (8, 8), (2, 6)])
 def test_heads_anywhere(dtype, shift, pad):
