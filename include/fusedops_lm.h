@@ -133,8 +133,8 @@ typedef struct fo_scan {
 } fo_scan;
 
 int fused_scan(const fo_scan *a, void *ws, size_t ws_bytes, void *stream);
-/* Bytes of scratch for fused_scan and fused_scan_grad. */
-size_t fused_scan_workspace_bytes(void);
+/* Bytes of scratch for fused_scan and fused_scan_grad of so many tokens; 0: none is needed, and ws may be NULL. */
+size_t fused_scan_workspace_bytes(int64_t tokens);
 
 /* The gradient from dh and dlast (either may be NULL: zero) and the forward pass's inputs and h:
  *     l_t = dh_t + a_{t+1} l_{t+1}   (dlast where the sequence ends; nothing through a reset)

@@ -153,7 +153,7 @@ def load_library(path=None):
         lib.fused_head_norm_grad_workspace_bytes.argtypes = [i32, i32]
         lib.fused_head_norm_grad_workspace_bytes.restype = sz
         lib.fused_scan.argtypes = lib.fused_scan_grad.argtypes = [bp, vp, sz, vp]
-        lib.fused_scan_workspace_bytes.argtypes = []
+        lib.fused_scan_workspace_bytes.argtypes = [C.c_int64]
         lib.fused_scan_workspace_bytes.restype = sz
         for f in (lib.fused_head_norm, lib.fused_distill, lib.fused_distill_grad,
                   lib.fused_distill_step):

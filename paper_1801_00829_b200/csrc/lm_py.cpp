@@ -377,6 +377,17 @@ struct ScanArgs {
     }
 };
 
+// Long sequences take scratch; a decoding step that is captured into a graph takes none, and so the graph clears none.
+struct ScanScratch {
+    at::Tensor held;
+    void *at = nullptr;
+    size_t bytes;
+    ScanScratch(const ScanArgs &c, cudaStream_t st) : bytes(fused_scan_workspace_bytes(c.tokens))
+    {
+        if (bytes) held = workspace(c.gpu, st, bytes), at = held.data_ptr(), bytes = (size_t)held.numel();
+    }
+};
+
 }  // namespace
 
 // scan(x, gate, decay, mix, state, reset, lengths, out, out_state)
@@ -401,8 +412,8 @@ PyObject *scan_impl(PyObject *const *a)
     n.last = c.state(out_state ? out_state : &last, "out_state", out_state != nullptr);
     const OnGpu on(c.gpu);
     const cudaStream_t st = stream_of(c.gpu);
-    const at::Tensor ws = workspace(c.gpu, st, fused_scan_workspace_bytes());
-    check_status(fused_scan(&n, ws.data_ptr(), (size_t)ws.numel(), st), "fused_scan");
+    const ScanScratch ws(c, st);
+    check_status(fused_scan(&n, ws.at, ws.bytes, st), "fused_scan");
     if (out) written(*out);
     if (out_state) written(*out_state);
     PyObject *ho = given_or_new(a[7], h);
@@ -441,8 +452,8 @@ PyObject *scan_grad_impl(PyObject *const *a)
     }
     const OnGpu on(c.gpu);
     const cudaStream_t st = stream_of(c.gpu);
-    const at::Tensor ws = workspace(c.gpu, st, fused_scan_workspace_bytes());
-    check_status(fused_scan_grad(&n, ws.data_ptr(), (size_t)ws.numel(), st), "fused_scan_grad");
+    const ScanScratch ws(c, st);
+    check_status(fused_scan_grad(&n, ws.at, ws.bytes, st), "fused_scan_grad");
     return got.release();
 }
 

@@ -63,8 +63,11 @@ int pairs_if(const void *p, const fo_rows &s, int type, ScanTensor bit) { return
 
 int launch(const ScanParams &p, int type, int gate_type, bool grad, void *ws, size_t ws_bytes, cudaStream_t st)
 {
-    const int rc = check_workspace(ws, ws_bytes, fused_scan_workspace_bytes());
-    if (rc != FO_OK) return rc;
+    const size_t needed = fused_scan_workspace_bytes(p.tokens);
+    if (needed) {
+        const int rc = check_workspace(ws, ws_bytes, needed);
+        if (rc != FO_OK) return rc;
+    }
     cudaError_t e = cudaErrorInvalidValue;
 #define FO_CASE(t, g, T, G) \
     if (type == t && gate_type == g) e = launch_scan<T, G>(p, grad, ws, st);
@@ -80,8 +83,9 @@ using namespace fo;
 
 extern "C" {
 
-size_t fused_scan_workspace_bytes(void)
+size_t fused_scan_workspace_bytes(int64_t tokens)
 {
+    if (tokens < kScanLeastChunked) return 0;
     // three states and a mark of every chunk: of at most 64 channels each, and of as many as there are CTAs on all SMs
     return sizeof(WsHead) + (size_t)2 * kScanMostSms * (64 * 3 * sizeof(double) + sizeof(int));
 }

@@ -20,6 +20,7 @@ namespace fo {
 constexpr int kScanCta = 256;
 constexpr int kScanMostWarps = kScanCta / 32;
 constexpr int kScanMostCluster = 8;
+constexpr int kScanLeastChunked = 8 * kScanMostCluster * kScanMostWarps * 4;   // tokens: eight rounds of a cluster in segments of four
 constexpr int kScanMostSms = 256;       // chunks make CTAs for two on each of these at most
 
 enum ScanTensor { kScanX = 1, kScanGate = 2, kScanDh = 4, kScanH = 8, kScanOut = 16, kScanOutGate = 32, kScanNear = 64, kScanAll = 127 };

@@ -76,7 +76,7 @@ cudaError_t scan_launch(ScanParams p, void *ws, cudaStream_t st)
     const auto shared = [&](int k) { return Ring::kBytes * warps + Shared::bytes(warps, k); };
     const long long room = 2LL * std::min(sm_count(), kScanMostSms) / items;             // chunks that find room at once
     p.chunks = 1, p.chunk = p.tokens;
-    if (warps == kScanMostWarps && scan_chunked(GRAD, room, p.tokens / (kScanMostCluster * kScanMostWarps * S))) {
+    if (p.tokens >= kScanLeastChunked && scan_chunked(GRAD, room, p.tokens / (kScanMostCluster * kScanMostWarps * S))) {
         const int round = warps * S, most = (int)std::min<long long>(room, p.tokens / (kScanLeastChunk * round));
         p.chunk = ((p.tokens + most - 1) / most + round - 1) / round * round;
         p.chunks = (p.tokens + p.chunk - 1) / p.chunk;

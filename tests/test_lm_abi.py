@@ -90,7 +90,7 @@ def scan(lib, grad=False, **kw):
 
 def test_scan_refusals(lib):
     assert lib.fused_scan(None, None, 0, None) == -1 and lib.fused_scan_grad(None, None, 0, None) == -1
-    assert lib.fused_scan_workspace_bytes() > 16384
+    assert lib.fused_scan_workspace_bytes(1 << 30) > 16384 and lib.fused_scan_workspace_bytes(1) == 0
     for grad in (False, True):
         one = lambda **kw: scan(lib, grad, **kw)  # noqa: E731
         assert one(batch=-1) == -2 and one(tokens=-1) == -2 and one(channels=-1) == -2
@@ -100,7 +100,8 @@ def test_scan_refusals(lib):
         assert one(x=0) == -1 and one(gate=0) == -1 and one(h=0) == -1 and one(x=0x1001) == -4 and one(gate=0x2001) == -4
         assert one(state=0x7002) == -4 and one(batch=1 << 30, channels=1 << 20) == -4
         assert one(tokens=(1 << 30) + 1) == -4 and one(channels=(1 << 28) + 1) == -4
-        assert one(ws=0) == -5 and one(ws=0x10008) == -5 and one(ws_bytes=16384) == -5
+        for bad in (dict(ws=0), dict(ws=0x10008), dict(ws_bytes=16384)):
+            assert one(tokens=9000, **bad) == -5
         assert one(batch=0) == 0 and one(channels=0) == 0 and one(tokens=0, last=0) == 0
     assert scan(lib, True, dx=0) == -1 and scan(lib, True, dgate=0) == -1 and scan(lib, True, dgate=0x6801) == -4 and scan(lib, True, dstate=0x6802) == -4
     assert scan(lib, last=0x4002) == -4
