@@ -449,6 +449,12 @@ def test_distill_sizes(dtype, vocab):
                 values=F32 if dtype in (BF16, F16) and k else None).check()
 
 
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 120001), (F16, 131072), (F32, 70003), (F64, 30011)])
+def test_distill_long_rows(dtype, vocab):
+    """More rows than SMs, each of more pieces than a thread keeps on their way."""
+    Distill(160, vocab, 33, dtype, True, pad=vocab % 2, shift=vocab % 8).check()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("shift,pad", [(1, 0), (0, 1), (3, 5), (8, 8)])
 def test_distill_anywhere(dtype, shift, pad):
