@@ -98,13 +98,14 @@ struct HeadItems {
     __device__ __forceinline__ int pair_b(int i) const { return b[i] / 2; }
 };
 
-// The rows of the tables at which a token's positions lie; -1: outside.
+// The rows of the tables at which a token's positions lie; -1: outside, or there is no such token (and then perhaps no row either).
 struct HeadRows {
     int at[FO_MAX_AXES];
 };
 __device__ __forceinline__ HeadRows head_rows(const HeadParams &p, unsigned token)
 {
-    HeadRows r = {};
+    HeadRows r = {{-1, -1, -1, -1}};
+    static_assert(FO_MAX_AXES == 4, "a row for each axis");
     if (token >= (unsigned)p.all_tokens) return r;
     const long long b = token / (unsigned)p.tokens, t = token - b * p.tokens;
     const long long place = b * p.position_batch + t * p.position_token;
@@ -625,7 +626,7 @@ __global__ void __launch_bounds__(kHeadCta, sizeof(Acc<T>) == 8 ? 1 : 2) head_no
         ring.taken();
         issue();
         const bool on = now.on(p, t);
-        if (p.pairs) W::turn(at, g, u, v);
+        if (p.pairs && on) W::turn(at, g, u, v);           // a group without a head keeps its zeros, whatever the angles are
         if (normed) {
             // a group without a head has zeros throughout, and with eps 0 its r would not be finite
             const A r = W::normalise(p.lanes, inv_dim, at, kind, on ? eps : A(1), a, b);
