@@ -344,9 +344,10 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
                 if (t.place[k] >= 0) top_max = fmax(top_max, t.z[k]);
             }
         top_max = distill_warp_max(top_max), entries = distill_warp_sum(entries);
+        const double ref = top_max == -CUDART_INF ? 0.0 : top_max;        // the warp's entries may all be masked
         for (int k = step - 1 - team.thread; k < p.top; k += step)
             if (t.place[k] >= 0) {
-                top_sum += exp((t.z[k] - top_max) * p.inv_t);
+                top_sum += exp((t.z[k] - ref) * p.inv_t);
                 if (STEP) t.share[k] = teacher_share(t, p.top, k);
             }
         top_sum = distill_warp_sum(top_sum);

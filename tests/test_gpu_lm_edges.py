@@ -41,3 +41,76 @@ def test_heads_beside_a_table_row_that_no_token_uses(dtype, pairing, bad):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     got = fo.fused_head_norm_grad(c.dq, c.dk, c.q, c.k, **c.how())
     assert all(torch.equal(got[k], grads[k]) for k in grads)
+
+
+# ------------------------------------------------------------------------------------------------------------ distillation
+def compare(c):
+    """Loss, statistics and both gradients with the oracle.
+
+    As in test_gpu_lm.py, and: `top` shares are added up in 64 bits by the kernel and by the oracle, and their sum, and what it leaves of
+    1, is off by `top` additions and 32 units of a share in each (float64's other errors are no larger).  The exponent of an exponential
+    outside the entries is a distance to the largest logit and, where a student is sure, the logarithm of P / Q (at most 20 beyond the
+    distance), each rounded up to three times by the units of their sizes."""
+    top, t, u, values = c.ids.shape[1], c.temperature, unit(c.dtype), host(c.values)
+    want, stats, dz, q = ref.distill(host(c.logits), host(c.ids), values, host(c.tail), t)
+    weight, z = host(c.dloss)[:, None], host(c.logits)
+    delta, off = u * (2048 + 32), 2 * (top + 32) * 2.0 ** -53
+    with np.errstate(invalid="ignore"):
+        far = np.where(np.isfinite(z), np.abs(z - stats[0][:, None]) / t, 0.0)
+    ids = host(c.ids)
+    outside = np.ones(z.shape, dtype=bool)
+    for r, row in enumerate(ids):
+        outside[r, row[row >= 0]] = False
+    elsewhere = np.where(outside, q, 0.0).sum(1)             # Q
+    p = np.zeros(0) if c.tail is None else np.where(ids >= 0, np.exp(values / t - host(c.tail)[:, None]), 0.0).sum(1)
+    rest = np.zeros(len(z)) if c.tail is None else np.where(elsewhere > 0, np.maximum(1.0 - p, 0.0), 0.0)       # P
+    with np.errstate(divide="ignore", invalid="ignore"):
+        ratio = np.where(rest > 0, rest / elsewhere, 0.0)
+        eratio = np.where(rest > 0, 3 * delta * ratio + off / elsewhere, 0.0)
+    size = np.abs(want) + np.where(np.isfinite(values), np.abs(values), 0.0).max(1, initial=0.0) / t + 100.0
+    loss, kept = fo.fused_distill(*c.args(), stats=True, **c.how())
+    close(loss, want, 1.1 * delta + 2.0 ** -50 * size + off * (np.log(ratio + 1.0) + 40.0), "loss")
+    close(kept[0], stats[0], 0.0, "largest")
+    sure = ratio > 2.0 ** 60
+    close(kept[1], np.where(sure, -stats[1], stats[1]), delta * stats[1], "sum")
+    log = np.log(np.maximum(ratio, 1.0))
+    close(kept[2], np.where(sure, log, stats[2]), np.where(sure, eratio / np.maximum(ratio, 1.0) + 2 * u * log, eratio + 2 * u + off), "factor")
+    relative = delta + u * (16 + 6 * (far + 20.0))
+    edz = (q * (2.0 + np.where(outside, ratio[:, None], 0.0)) * relative + np.where(outside, q * eratio[:, None], 0.0) + 2.0 ** -44) / t
+    one, step = fo.fused_distill_step(c.dloss, *c.args(), **c.how())
+    assert torch.equal(one, loss)
+    close(step, weight * dz, weight * edz, "dz of the step")
+    close(fo.fused_distill_grad(c.dloss, *c.args(), kept, **c.how()), weight * dz, weight * edz, "dz")
+    return loss, kept, step
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("rows,vocab", [(9, 32000), (9, 700), (200, 700), (200, 5000), (200, 100)])
+def test_distill_minus_infinity_at_entries(dtype, tail, rows, vocab):
+    """A vocabulary that is masked for teacher and student alike, and masked logits at entries with shares and without."""
+    c = Distill(rows, vocab, 64, dtype, tail)
+    inf = float("inf")
+    for r in (0, 1, rows - 1):                               # five are allowed
+        keep = c.logits[r, c.ids[r, :5]].clone()
+        c.logits[r] = -inf
+        c.logits[r, c.ids[r, :5]] = keep
+        c.values[r, 5:] = -inf
+        if tail:
+            c.tail[r] = c.values[r, :5].to(c.tail.dtype).logsumexp(0)
+    for r, (low, high) in ((2, (32, 64)), (3, (0, 32)), (4, (40, 41)), (5, (1, 64))):
+        c.logits[r, c.ids[r, low:high]] = -inf
+        c.values[r, low:high] = -inf
+    c.logits[6, c.ids[6, 7]] = -inf                          # has a share: the loss is infinite, the gradient is not
+    c.logits[7, c.ids[7]] = -inf
+    loss, stats, dz = compare(c)
+    assert torch.isinf(loss[6:8]).all() and torch.isfinite(loss[:6]).all() and torch.isfinite(dz).all() and not torch.isnan(stats).any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(5, 50257), (300, 777)])
+def test_distill_a_masked_label(dtype, rows, vocab):
+    c = Distill(rows, vocab, 1, dtype, False)
+    c.logits[1, c.ids[1, 0]] = -float("inf")
+    loss, _, dz = compare(c)
+    assert torch.isinf(loss[1]) and torch.isfinite(loss[2:]).all() and torch.isfinite(dz).all()
