@@ -159,8 +159,9 @@ int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stre
  *     tail NULL:  p = softmax(v / temperature) over the entries;      loss = sum_k p_k (log p_k - log q_{id_k})
  *     tail given: p_k = exp(v_k / temperature - tail), the teacher's own shares (tail: the log-sum-exp of its whole row over
  *                 temperature), P = max(0, 1 - sum p) and Q = 1 - sum q_{id_k} all that is outside the entries;
- *                 loss as above + P log(P / Q); where Q is zero (the entries are all the row, or the rest is masked) a P of at
- *                 most 1 / 32 is what the rounding of v and tail has left, and taken as zero; a larger one makes the loss infinite
+ *                 loss as above + P log(P / Q); where Q is zero as a number of 64 bits (the entries are all the row, or the rest is
+ *                 masked) a P of at most 1 / 32 is what the rounding of v and tail has left, and taken as zero; a larger one makes the
+ *                 loss infinite
  * An entry with a negative id is none; one with an id >= vocab makes the row NaN.  Entries with the same id are one place of q
  * with several shares.  Without entries the first form's loss is zero; p_k = 0 adds nothing.
  * Gradient, times dloss of the row (float; NULL: 1):
@@ -169,7 +170,8 @@ int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stre
  * fused_distill writes loss and stats (either may be NULL), fused_distill_grad dz from stats and dloss, fused_distill_step loss
  * and dz in one pass over the logits.  The two with dloss do not look at a row whose dloss is zero: its dz, and the step's loss, are zero.
  * loss, stats, dloss, tail: float (double where type is FO_F64).  stats: 3 x rows, contiguous: the largest logit, the sum of
- * exp((z - largest) / temperature), and S - P / Q.  ids: int32 or int64; ids and values have rows of ld_ids, ld_values >= top.
+ * exp((z - largest) / temperature), and S - P / Q; where P / Q is above 2^60, minus the sum, and log(P / Q).
+ * ids: int32 or int64; ids and values have rows of ld_ids, ld_values >= top.
  * values_type: `type`, or FO_F32 with a 16-bit type.  What concerns the entries is computed in 64 bits.
  * dz may be the logits themselves.  Any address of an element and any ld >= vocab works; fast are logits and dz whose rows lie at
  * the same offset from a 16-byte boundary.

@@ -44,9 +44,14 @@ template <class T> __device__ __forceinline__ float distill_exp(float v)
 }
 template <class T> __device__ __forceinline__ double distill_exp(double v) { return exp(v); }
 template <class T>
+__device__ __forceinline__ constexpr double distill_unit_of()
+{
+    return sizeof(T) == 2 ? 1.4426950408889634074 : 1.0;
+}
+template <class T>
 __device__ __forceinline__ Acc<T> distill_unit(double inv_t)
 {
-    return Acc<T>(sizeof(T) == 2 ? inv_t * 1.4426950408889634074 : inv_t);
+    return Acc<T>(inv_t * distill_unit_of<T>());
 }
 template <class A> __device__ __forceinline__ A distill_floor() { return -A(CUDART_INF); }
 
@@ -103,6 +108,10 @@ __device__ __forceinline__ double teacher_value(const DistillParams &p, long lon
 // P up to this is taken as zero where nothing of q lies outside the entries (they are the whole vocabulary, or the rest of it is
 // masked): it is what the rounding of values and tail has left.  A value of 16 is off by 2^-5 in bfloat16, and so is its share then.
 constexpr double kDistillNoise = 0.03125;
+// A student is sure where P / Q is above this.  Q then comes near the smallest numbers of 32 bits, and P / Q near the largest: the gradient
+// outside, q (S - P / Q), is formed as -exp(z / T + log(P / Q) - ...), and what is kept of the row is that logarithm (S is below
+// its last bit), with a minus at the sum.
+constexpr double kDistillSure = 0x1p60;
 
 // What all threads need to know of the entries besides the arrays.
 struct TeacherSums {
@@ -273,6 +282,13 @@ __device__ __forceinline__ Packed<T, 16 / sizeof(T)> distill_piece(const T *at, 
 struct DistillPart {
     double rest_max, rest_sum, top_max, top_sum, entries;
 };
+// A row's sums, in shared memory: its threads' registers are for the pieces of the second reading.
+struct DistillResult {
+    double largest, total, factor;      // factor: S - P / Q
+    double log_share;                   // log(P / Q) of a student that is sure, else zero
+    double coef;                        // of exp(z / T - largest + log_share) outside the entries
+    double all, rest, ratio, entries;   // S, P, P / Q, and what the entries add to the loss
+};
 
 // Loss, and with STEP the gradient.  Bound by DRAM and by what of the second reading misses L2 (about half): 4096 x 128000 in bfloat16
 // with rows of padding 442 to 452 us, with all rows counting 491 (4.3 TB/s of one reading and one writing); short rows by what a row
@@ -284,14 +300,14 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     constexpr int E = 16 / (int)sizeof(T), kTogether = 4;
     extern __shared__ __align__(16) unsigned char distill_memory[];
     __shared__ DistillPart all_parts[kDistillRow / 32];
-    __shared__ double results[kDistillCta / 32][6];
+    __shared__ DistillResult results[kDistillCta / 32];
     __shared__ TeacherSums teachers[kDistillCta / 32];
     wait_for_earlier();
     const int number = threadIdx.x / p.team, lane = threadIdx.x & 31, step = p.team;
     const Team team = {(int)threadIdx.x - number * p.team, p.team, number};
     const int warp = team.thread >> 5, warps = p.team >> 5;
     DistillPart *const parts = all_parts + number * warps;
-    double *const result = results[number];
+    DistillResult &result = results[number];
     TeacherSums &teacher = teachers[number];
     const long long row = (long long)blockIdx.x * (blockDim.x / p.team) + number;
     if (row >= p.rows) return;
@@ -429,34 +445,34 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     if (lane == 0) parts[warp] = {(double)rest_max, (double)rest_sum, top_max, top_sum, entries};
     team.sync();
     // the row's
-    double row_max = 0.0, total = 0.0, rest_of_row = 0.0, row_entries = 0.0, rest = 0.0;
     if (warp == 0) {
         DistillPart d = {-CUDART_INF, 0.0, -CUDART_INF, 0.0, 0.0};
         if (lane < warps) d = parts[lane];
-        row_max = distill_warp_max(fmax(d.rest_max, d.top_max));
-        if (d.rest_sum != 0.0) rest_of_row = d.rest_sum * (double)distill_exp<T>(A(d.rest_max - row_max) * unit);
-        rest_of_row = distill_warp_sum(rest_of_row);
-        total = rest_of_row + distill_warp_sum(d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - row_max) * p.inv_t) : 0.0);
-        row_entries = distill_warp_sum(d.entries);
-        rest = rest_of_row == 0.0 && teacher.rest <= kDistillNoise ? 0.0 : teacher.rest;
-        double factor = teacher.sum + rest;
-        if (rest > 0.0) factor -= rest * total / rest_of_row;
+        const double rest_max = distill_warp_max(d.rest_max), row_max = fmax(rest_max, distill_warp_max(d.top_max));
+        // relative to the largest outside, and from there to the row's in 64 bits: zero only if Q is as a number of 64 bits
+        const double outside = distill_warp_sum(d.rest_sum != 0.0 ? d.rest_sum * (double)distill_exp<T>(A(d.rest_max - rest_max) * unit) : 0.0);
+        const double rest_of_row = outside != 0.0 ? outside * exp((rest_max - row_max) * p.inv_t) : 0.0;
+        const double total = rest_of_row + distill_warp_sum(d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - row_max) * p.inv_t) : 0.0);
+        const double row_entries = distill_warp_sum(d.entries);
+        const double rest = rest_of_row == 0.0 && teacher.rest <= kDistillNoise ? 0.0 : teacher.rest;
+        const double ratio = rest > 0.0 ? rest * total / rest_of_row : 0.0;
+        const bool sure = rest_of_row > 0.0 && ratio > kDistillSure;
+        const double log_share = sure ? log(rest) + log(total) - ((rest_max - row_max) * p.inv_t + log(outside)) : 0.0;
+        double factor = teacher.sum + rest - ratio;
         if (!(teacher.sum == teacher.sum)) factor = CUDART_NAN;           // an id outside the row
-        const double inverse = 1.0 / total;
-        if (lane == 0) result[0] = row_max, result[1] = total, result[2] = factor, result[3] = inverse, result[4] = (double)weight * p.inv_t * factor * inverse,
-                       result[5] = teacher.sum + rest;
+        if (lane == 0) result = {row_max, total, factor, log_share, (double)weight * p.inv_t * (sure ? -1.0 : factor) / total, teacher.sum + rest, rest, ratio, row_entries};
     }
     if constexpr (STEP) {
         team.sync();
-        const A m = A(result[0]), coef = A(result[4]);
+        const A m = A(result.largest), coef = A(result.coef), shift = A(result.log_share * distill_unit_of<T>());
         const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
-        const Two<A> less = both(-m), coefs = both(coef);
+        const Two<A> less = both(-m), coefs = both(coef), shifts = both(shift);
         auto gradient = [&](const Packed<T, E> &v) {
             Packed<T, E> out;
             if constexpr (sizeof(T) >= 4) out.clear();
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                const Two<A> x = (v.get2(e) + less) * scale;
+                const Two<A> x = fused_ma(v.get2(e) + less, scale, shifts);
                 out.put2(e, two(distill_exp<T>(first(x)), distill_exp<T>(second(x))) * coefs);
             }
             return out;
@@ -490,23 +506,25 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
         }
         if (ends) distill_put(at, other, dz, false, gradient(ragged(other)));
         team.sync();                                      // the entries' places have been written like the others
-        const double by = (double)weight * p.inv_t, s_all = result[5];
+        const double by = (double)weight * p.inv_t, s_all = result.all, inverse = 1.0 / result.total;
         for (int k = team.thread; k < p.top; k += step)
             if (t.place[k] >= 0) {
-                const double q = exp((t.z[k] - result[0]) * p.inv_t) * result[3];
+                const double q = exp((t.z[k] - result.largest) * p.inv_t) * inverse;
                 dz[t.place[k]] = narrow<T>(A(by * (q * s_all - t.share[k])));
             }
     }
     // what only the loss needs comes last
     if (team.thread == 0) {
-        const double log_total = row_max * p.inv_t + log(total);
-        double loss = teacher.sum != 0.0 ? row_entries + teacher.sum * log_total : 0.0;
-        if (rest > 0.0) loss += rest * log(rest * total / rest_of_row);        // P (log P - log Q)
+        const double log_total = result.largest * p.inv_t + log(result.total);
+        double loss = teacher.sum != 0.0 ? result.entries + teacher.sum * log_total : 0.0;
+        if (result.rest > 0.0) loss += result.rest * (result.log_share != 0.0 ? result.log_share : log(result.ratio));        // P (log P - log Q)
         if (!(teacher.sum == teacher.sum)) loss = CUDART_NAN;
         if (p.loss) static_cast<A *>(p.loss)[row] = A(loss);
         if (!STEP && p.stats) {
+            const bool sure = result.log_share != 0.0;
             A *const st = static_cast<A *>(p.stats);
-            st[row] = A(row_max), st[p.rows + row] = A(total), st[2 * p.rows + row] = A(result[2]);
+            st[row] = A(result.largest), st[p.rows + row] = A(sure ? -result.total : result.total);
+            st[2 * p.rows + row] = A(sure ? result.log_share : result.factor);
         }
     }
 }
@@ -552,7 +570,9 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
     };
     fetch(first + threadIdx.x);
     const A *const stats = static_cast<const A *>(p.stats);
-    const A m = stats[row], total = stats[p.rows + row], factor = stats[2 * p.rows + row];
+    const A m = stats[row], kept = stats[p.rows + row], factor = stats[2 * p.rows + row];
+    const bool sure = kept < A(0);
+    const A total = sure ? -kept : kept;
     teacher_read<T, true>(p, row, t, team, z);
     const double tail = p.tail ? (double)static_cast<const A *>(p.tail)[row] : 0.0;
     __syncthreads();                                                // before anything is written: dz may be the logits
@@ -562,9 +582,10 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
     const auto here = [&](int place) { return place >= 0 && place >= from && place < to; };
     const double scale = (double)weight * p.inv_t;
     // an id outside the row is one in the statistics too, and makes them NaN
-    const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (double)factor / (double)total);
+    const A unit = distill_unit<T>(p.inv_t), coef = A(scale * (sure ? -1.0 : (double)factor) / (double)total);
+    const A shift = sure ? A((double)factor * distill_unit_of<T>()) : A(0);
     const bool alike = (((uintptr_t)dz ^ (uintptr_t)z) & 15u) == 0;
-    const Two<A> less = both(-m), units = both(unit), coefs = both(coef);
+    const Two<A> less = both(-m), units = both(unit), coefs = both(coef), shifts = both(shift);
     for (int i0 = first + threadIdx.x; i0 < last; i0 += kTogether * blockDim.x) {
         if (i0 != first + (int)threadIdx.x) fetch(i0);
 #pragma unroll
@@ -575,7 +596,7 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
             if constexpr (sizeof(T) >= 4) out.clear();
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
-                const Two<A> x = (v[u].get2(e) + less) * units;
+                const Two<A> x = fused_ma(v[u].get2(e) + less, units, shifts);
                 out.put2(e, two(distill_exp<T>(fo::first(x)), distill_exp<T>(second(x))) * coefs);
             }
             distill_put(at, i, dz, alike, out);
@@ -583,7 +604,7 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
     }
     __syncthreads();
     // the statistics' S - P / Q is below sum p, unless P was taken as zero
-    const bool all = teacher.rest <= kDistillNoise && factor >= A(teacher.sum);
+    const bool all = !sure && teacher.rest <= kDistillNoise && factor >= A(teacher.sum);
     const double s_all = all ? teacher.sum : teacher.sum + teacher.rest;
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)
         if (here(t.place[k])) {

@@ -114,3 +114,22 @@ def test_distill_a_masked_label(dtype, rows, vocab):
     c.logits[1, c.ids[1, 0]] = -float("inf")
     loss, _, dz = compare(c)
     assert torch.isinf(loss[1]) and torch.isfinite(loss[2:]).all() and torch.isfinite(dz).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("temperature", [1.0, 0.5])
+@pytest.mark.parametrize("rows,vocab,top", [(6, 3000, 12), (300, 60, 5), (4, 40003, 70)])
+def test_distill_a_student_that_is_sure(dtype, temperature, rows, vocab, top):
+    """The teacher leaves a share outside the entries, where the student has next to nothing: down to exp(-680) (with the clamped logits' 8 or 16
+    more at both temperatures; beyond exp(-708) the oracle's own numbers lose bits)."""
+    rng = np.random.RandomState(vocab)
+    for gap in (20.0, 41.0, 60.0, 86.0, 89.0, 105.0, 200.0, 400.0, 660.0):
+        c = Distill(rows, vocab, top, dtype, True, temperature)
+        c.logits.clamp_(-4.0, 4.0)
+        c.logits.scatter_add_(1, c.ids, torch.full(c.ids.shape, gap * temperature, dtype=dtype, device="cuda"))
+        free = torch.ones(rows, vocab, dtype=torch.bool, device="cuda").scatter_(1, c.ids, False)
+        c.logits[0][free[0].logical_and(torch.arange(vocab, device="cuda") % 3 == 0)] = -float("inf")
+        left = torch.from_numpy(rng.choice([1e-6, 0.01, 0.03, 0.04, 0.2, 0.9], rows)).cuda()
+        c.tail = ((c.values.double() / temperature).logsumexp(1) - torch.log1p(-left)).to(wide(dtype))
+        loss, _, dz = compare(c)
+        assert torch.isfinite(loss).all() and torch.isfinite(dz).all()
