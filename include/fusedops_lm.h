@@ -170,7 +170,8 @@ int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stre
  * fused_distill writes loss and stats (either may be NULL), fused_distill_grad dz from stats and dloss, fused_distill_step loss
  * and dz in one pass over the logits.  The two with dloss do not look at a row whose dloss is zero: its dz, and the step's loss, are zero.
  * loss, stats, dloss, tail: float (double where type is FO_F64).  stats: 3 x rows, contiguous: the largest logit, the sum of
- * exp((z - largest) / temperature), and S - P / Q; where P / Q is above 2^60, minus the sum, and log(P / Q).
+ * exp((z - largest) / temperature), and S - P / Q, below sum p where P is not zero; where P / Q is above
+ * 2^60, minus the sum, and log(P / Q).
  * ids: int32 or int64; ids and values have rows of ld_ids, ld_values >= top.
  * values_type: `type`, or FO_F32 with a 16-bit type.  What concerns the entries is computed in 64 bits.
  * dz may be the logits themselves.  Any address of an element and any ld >= vocab works; fast are logits and dz whose rows lie at

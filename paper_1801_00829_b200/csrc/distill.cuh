@@ -55,6 +55,8 @@ __device__ __forceinline__ Acc<T> distill_unit(double inv_t)
 }
 template <class A> __device__ __forceinline__ A distill_floor() { return -A(CUDART_INF); }
 
+__device__ __forceinline__ float next_below(float v) { return nextafterf(v, -CUDART_INF_F); }
+__device__ __forceinline__ double next_below(double v) { return nextafter(v, -CUDART_INF); }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 
@@ -524,7 +526,10 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
             const bool sure = result.log_share != 0.0;
             A *const st = static_cast<A *>(p.stats);
             st[row] = A(result.largest), st[p.rows + row] = A(sure ? -result.total : result.total);
-            st[2 * p.rows + row] = A(sure ? result.log_share : result.factor);
+            // a P that counts leaves it below sum p, by a bit at least, and so the gradient knows that P counted
+            A factor = A(sure ? result.log_share : result.factor);
+            if (result.rest > 0.0 && !sure && factor >= A(teacher.sum)) factor = next_below(A(teacher.sum));
+            st[2 * p.rows + row] = factor;
         }
     }
 }
@@ -603,7 +608,7 @@ __global__ void __launch_bounds__(kDistillCta, 5) distill_grad_kernel(const __gr
         }
     }
     __syncthreads();
-    // the statistics' S - P / Q is below sum p, unless P was taken as zero
+    // the statistics' S - P / Q is below sum p where P counted; P was zero, or taken as zero, where it is not
     const bool all = !sure && teacher.rest <= kDistillNoise && factor >= A(teacher.sum);
     const double s_all = all ? teacher.sum : teacher.sum + teacher.rest;
     for (int k = threadIdx.x; k < p.top; k += blockDim.x)

@@ -133,3 +133,16 @@ def test_distill_a_student_that_is_sure(dtype, temperature, rows, vocab, top):
         c.tail = ((c.values.double() / temperature).logsumexp(1) - torch.log1p(-left)).to(wide(dtype))
         loss, _, dz = compare(c)
         assert torch.isfinite(loss).all() and torch.isfinite(dz).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(6, 3000), (300, 500)])
+def test_distill_a_student_with_almost_all_elsewhere(dtype, rows, vocab):
+    """The student's share outside is 1 but for rounding, the teacher's is small: it counts all the same, in both gradients."""
+    for low in (-6.0, -8.0, -10.0, -12.0, -30.0):
+        c = Distill(rows, vocab, 6, dtype, True)
+        c.logits.clamp_(-1.0, 1.0)
+        c.logits.scatter_(1, c.ids, low)
+        c.values[:, 3:] = -float("inf")                      # no share: the gradient there is q S
+        c.tail = (c.values.double().logsumexp(1) - np.log(1.0 - 0.03)).to(wide(dtype))
+        compare(c)
