@@ -450,16 +450,20 @@ __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_
     if (warp == 0) {
         DistillPart d = {-CUDART_INF, 0.0, -CUDART_INF, 0.0, 0.0};
         if (lane < warps) d = parts[lane];
-        const double rest_max = distill_warp_max(d.rest_max), row_max = fmax(rest_max, distill_warp_max(d.top_max));
-        // relative to the largest outside, and from there to the row's in 64 bits: zero only if Q is as a number of 64 bits
-        const double outside = distill_warp_sum(d.rest_sum != 0.0 ? d.rest_sum * (double)distill_exp<T>(A(d.rest_max - rest_max) * unit) : 0.0);
-        const double rest_of_row = outside != 0.0 ? outside * exp((rest_max - row_max) * p.inv_t) : 0.0;
+        const double row_max = distill_warp_max(fmax(d.rest_max, d.top_max));
+        // in 64 bits: zero only if Q is as a number of 64 bits
+        const double rest_of_row = distill_warp_sum(d.rest_sum != 0.0 ? d.rest_sum * exp((d.rest_max - row_max) * p.inv_t) : 0.0);
         const double total = rest_of_row + distill_warp_sum(d.top_sum != 0.0 ? d.top_sum * exp((d.top_max - row_max) * p.inv_t) : 0.0);
         const double row_entries = distill_warp_sum(d.entries);
         const double rest = rest_of_row == 0.0 && teacher.rest <= kDistillNoise ? 0.0 : teacher.rest;
         const double ratio = rest > 0.0 ? rest * total / rest_of_row : 0.0;
         const bool sure = rest_of_row > 0.0 && ratio > kDistillSure;
-        const double log_share = sure ? log(rest) + log(total) - ((rest_max - row_max) * p.inv_t + log(outside)) : 0.0;
+        double log_share = 0.0;
+        if (sure) {                                           // by logarithms, from the largest outside
+            const double rest_max = distill_warp_max(d.rest_max);
+            const double outside = distill_warp_sum(d.rest_sum != 0.0 ? d.rest_sum * exp((d.rest_max - rest_max) * p.inv_t) : 0.0);
+            log_share = log(rest) + log(total) - ((rest_max - row_max) * p.inv_t + log(outside));
+        }
         double factor = teacher.sum + rest - ratio;
         if (!(teacher.sum == teacher.sum)) factor = CUDART_NAN;           // an id outside the row
         if (lane == 0) result = {row_max, total, factor, log_share, (double)weight * p.inv_t * (sure ? -1.0 : factor) / total, teacher.sum + rest, rest, ratio, row_entries};
