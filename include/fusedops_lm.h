@@ -106,7 +106,8 @@ size_t fused_head_norm_grad_workspace_bytes(int dim, int type);
  * lengths[b] (int32 or int64; NULL: `tokens`), taken into 0 .. tokens: behind a sequence's end x and gate are not looked at,
  * and h is zero there.  last (NULL, or batch x channels) = h at the end: of the last token, or the state without tokens;
  * `last` may be `state`.  1 - a is computed without the cancellation; 16-bit x goes through the hardware's
- * exponential and reciprocal, decays near 1 rounded to 32 bits all the same.
+ * exponential, reciprocal and root, whatever the gate's type: the smaller of a sigmoid and 1 - a is off by some (10 + |gate|) 2^-23 of itself,
+ * the larger is rounded to 32 bits.
  * Element (b, t, c) of x, gate, h is at p[b * batch + t * token + c].  state and last: float (double for FO_F64), contiguous.
  * Products of the decays over parts of the sequence are formed in 32 bits (64 for FO_F64): where they overflow, which takes decays above 1, or
  * where a state is infinite, h may be NaN.  It is NaN, too, should the CTAs that share a sequence lose each other.

@@ -99,10 +99,9 @@ def mixed(a, rest, mix):
 
 def gate_error(gate, a, rest, kind):
     """By how many rounding units a may be off, and (relative) m(a).  The smaller of a and 1 - a is off by a few units of
-    itself and the exponent's own, which grows with the gate; the larger by its rounding.  Where a is 1 minus 1 / (1 + exp(gate)), the
-    sum is rounded by at most a unit of 1, its reciprocal, below 1, by another, and the difference not at all: 2 units of 1."""
+    itself and the exponent's own, which grows with the gate; the larger by its rounding, a unit of 1."""
     own = 0.0 if kind == "value" else 24.0 + 4.0 * np.abs(gate)
-    return (np.abs(a) + 2.0) * (0.0 if kind == "value" else 1.0) + np.minimum(np.abs(a), np.abs(rest)) * own, own + 8.0
+    return (np.abs(a) + 1.0) * (0.0 if kind == "value" else 1.0) + np.minimum(np.abs(a), np.abs(rest)) * own, own + 8.0
 
 
 def scan(x, gate, kind, mix, state, reset, lengths):

@@ -43,6 +43,32 @@ def test_heads_beside_a_table_row_that_no_token_uses(dtype, pairing, bad):
     assert all(torch.equal(got[k], grads[k]) for k in grads)
 
 
+# ------------------------------------------------------------------------------------------------------------ recurrence
+@pytest.mark.parametrize("dtype,gate", PAIRS)
+@pytest.mark.parametrize("mix", ["one", "rest", "root"])
+@pytest.mark.parametrize("tokens", [1, 3, 40, 700, 9001])
+def test_small_decays_are_right_relative_to_themselves(dtype, gate, mix, tokens):
+    """Every other token adds nothing, so that all of its h is a small decay times the h before it."""
+    rng = np.random.RandomState(tokens)
+    g = torch.from_numpy(rng.uniform(-18.0, -6.0, (2, tokens, 70))).to(gate).cuda()
+    x = torch.from_numpy(rng.uniform(500.0, 1000.0, (2, tokens, 70))).to(dtype).cuda()
+    x[:, ::2] = 0
+    state = torch.from_numpy(rng.uniform(500.0, 1000.0, (2, 70))).to(wide(dtype)).cuda()
+    h, last = fo.fused_scan(x, g, "sigmoid", mix, state)
+    gd = host(g)
+    a, rest = ref.decay(gd, "sigmoid")
+    m = ref.mixed(a, rest, mix) * host(x)
+    want, carry = np.zeros_like(gd), host(state)
+    for t in range(tokens):
+        want[:, t] = carry = a[:, t] * carry + m[:, t]
+    # a is off by 24 + 4 |gate| units of itself (exponent, exponential, reciprocal, product), and so is the h that it is all of; that
+    # before it by the 24 + 4 |gate| of m(a), and two more products and sums
+    relative = 2 * (24 + 4 * np.abs(gd) + 8) * unit(dtype)
+    close(h, want, np.abs(want) * relative, "h")
+    if tokens % 2:
+        close(last, carry, np.abs(carry) * relative[:, -1], "last")
+
+
 # ------------------------------------------------------------------------------------------------------------ distillation
 def compare(c):
     """Loss, statistics and both gradients with the oracle.
