@@ -125,7 +125,7 @@ struct ScanCopy {
     {
         row = lane / kRowPieces;
         const int at = lane % kRowPieces * 16;
-        bytes = min(16, channels * (int)sizeof(T) - at);
+        bytes = min(16, min(channels, W) * (int)sizeof(T) - at);         // (all channels' bytes may be 2^31)
         place = row * W * (int)sizeof(T) + at;
 #pragma unroll
         for (int j = 0; j < kTurns; ++j) {

@@ -69,6 +69,29 @@ def test_small_decays_are_right_relative_to_themselves(dtype, gate, mix, tokens)
         close(last, carry, np.abs(carry) * relative[:, -1], "last")
 
 
+def test_as_many_channels_as_there_may_be():
+    """2^28 channels in 64 bits are 2^31 bytes a row."""
+    channels = 1 << 28
+    x, gate = torch.rand(channels, dtype=F64, device="cuda"), torch.rand(channels, dtype=F64, device="cuda")
+    h, last = fo.fused_scan(x.expand(5, -1), gate.expand(5, -1), "value", "rest")
+    parts = (slice(0, 4096), slice(channels // 2 - 64, channels // 2 + 64), slice(channels - 4096, channels))
+    for part in parts:
+        want = torch.zeros_like(x[part])
+        for t in range(5):
+            want = gate[part] * want + (1.0 - gate[part]) * x[part]
+            assert (h[t, part] - want).abs().max() <= 16 * 2.0 ** -53
+        assert torch.equal(last[part], h[4, part])
+    del last
+    got = fo.fused_scan_grad(x.expand(5, -1), None, gate.expand(5, -1), h, "value", "one")
+    for part in parts:
+        want = torch.zeros_like(x[part])
+        for t in range(4, -1, -1):
+            want = x[part] + gate[part] * want
+            assert (got["x"][t, part] - want).abs().max() <= 32 * 2.0 ** -53
+            before = h[t - 1, part] if t else 0.0
+            assert (got["gate"][t, part] - want * before).abs().max() <= 64 * 2.0 ** -53
+
+
 # ------------------------------------------------------------------------------------------------------------ distillation
 def compare(c):
     """Loss, statistics and both gradients with the oracle.
