@@ -144,12 +144,12 @@ int head_lanes(int dim, int piece)
 // Cuts a call into turns of the warps, the same number for each, and gives the tensors CTAs by their work.  Returns the grid.
 int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
 {
-    const int groups = 32 / p.lanes;
+    const long long groups = 32 / p.lanes;                   // (tokens and heads come near 2^31)
     p.tokens = (int)std::max<long long>(tokens, 1), p.all_tokens = (int)(batch * tokens);
     const long long warps = (long long)sms * kHeadCtas * kHeadWarps;
     long long wide = 0, narrow = 0, ctas[2] = {0, 0}, cost[2] = {0, 0};
     for (int k = 0; k < count; ++k)
-        wide += (long long)((p.all_tokens + groups - 1) / groups) * p.t[k].heads, narrow += (long long)p.all_tokens * ((p.t[k].heads + groups - 1) / groups);
+        wide += (p.all_tokens + groups - 1) / groups * p.t[k].heads, narrow += p.all_tokens * ((p.t[k].heads + groups - 1) / groups);
     // Blocks of several tokens, whose cosines and sines serve as many turns as there are heads, where that leaves every warp four turns
     // (40 heads of 128 in bfloat16: 1024 tokens 8 us both ways, 4096 tokens 19 against 21, backwards 33 and 35), or at least one
     // and a quarter of the turns less, because heads do not come out even with the groups (7 heads of 64, 4000 tokens: 5.5 and 9.1).  With
@@ -157,10 +157,10 @@ int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
     p.wide = wide >= 4 * warps || (wide >= warps && 4 * wide <= 3 * narrow);
     for (int k = 0; k < count; ++k) {
         HeadTensor &t = p.t[k];
-        t.blocks = p.wide ? (p.all_tokens + groups - 1) / groups : p.all_tokens;
-        t.turns = p.wide ? t.heads : (t.heads + groups - 1) / groups;
+        t.blocks = p.wide ? (int)((p.all_tokens + groups - 1) / groups) : p.all_tokens;
+        t.turns = p.wide ? t.heads : (int)((t.heads + groups - 1) / groups);
         // a block costs its turns and, for the cosines and sines, about one more
-        cost[k] = t.turns ? (long long)t.blocks * (t.turns + 1) : 0;
+        cost[k] = t.turns ? t.blocks * (t.turns + 1LL) : 0;
     }
     for (int k = 0; k < count; ++k) {
         HeadTensor &t = p.t[k];

@@ -440,8 +440,8 @@ struct HeadRing {
 // The turns of a warp, one behind the other, through blocks of tokens: in a turn the groups work on a head of a token each (wide), or on
 // as many heads of one token.  Every warp has the same number of turns and begins where the one before it ends, within a block.
 struct HeadTurns {
-    unsigned block;
-    int h0, left, by;                   // h0: the first group's head; left: turns to come
+    unsigned block, h0;                 // h0: the first group's head
+    int left, by;                       // left: turns to come
     int group, beside;                  // group: of the lane; beside: its head is h0 + beside
     int wide, groups;
     __device__ __forceinline__ HeadTurns(const HeadParams &p, const HeadTensor &t, int cta, int group_)
@@ -450,17 +450,17 @@ struct HeadTurns {
         const unsigned first = (unsigned)(cta * kHeadWarps + (int)(threadIdx.x / 32)) * (unsigned)t.each, all = (unsigned)t.blocks * (unsigned)t.turns;
         left = first < all ? (int)min(all - first, (unsigned)t.each) : 0;
         by = wide ? 1 : groups, beside = wide ? 0 : group;
-        block = first / (unsigned)t.turns, h0 = (int)(first - block * (unsigned)t.turns) * by;
+        block = first / (unsigned)t.turns, h0 = (first - block * (unsigned)t.turns) * by;
     }
     __device__ __forceinline__ bool there() const { return left > 0; }
     // the lane's token, of this block or a later one
     __device__ __forceinline__ unsigned token(unsigned later = 0) const { return wide ? (block + later) * (unsigned)groups + group : block + later; }
-    __device__ __forceinline__ bool on(const HeadParams &p, const HeadTensor &t) const { return h0 + beside < t.heads && token() < (unsigned)p.all_tokens; }
+    __device__ __forceinline__ bool on(const HeadParams &p, const HeadTensor &t) const { return h0 + beside < (unsigned)t.heads && token() < (unsigned)p.all_tokens; }
     // true: a new block
     __device__ __forceinline__ bool next(const HeadTensor &t)
     {
         --left, h0 += by;
-        if (h0 < t.heads) return false;
+        if (h0 < (unsigned)t.heads) return false;
         h0 = 0, ++block;
         return true;
     }

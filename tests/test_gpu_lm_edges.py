@@ -43,6 +43,19 @@ def test_heads_beside_a_table_row_that_no_token_uses(dtype, pairing, bad):
     assert all(torch.equal(got[k], grads[k]) for k in grads)
 
 
+@pytest.mark.parametrize("tokens_first", [True, False])
+def test_as_many_vectors_as_there_may_be(tokens_first):
+    count = 2 ** 31 - 1
+    x = torch.empty(count, dtype=BF16, device="cuda").bernoulli_().mul_(2.0).sub_(1.0)
+    x = x.view(count, 1, 1) if tokens_first else x.view(1, count, 1)
+    norm = ("rms", torch.full((1,), 1.5, dtype=BF16, device="cuda"), None, 0.0)
+    y, _ = fo.fused_head_norm(x, q_norm=norm)
+    assert torch.equal(y, x * 1.5)
+    got = fo.fused_head_norm_grad(y, None, x, q_norm=norm, out_q=y)
+    # one value is its own norm: no gradient but what 1 / sqrt(x^2) is off by, two units; the sums of 1.5 in lines of 2^16 and then lines
+    assert got["q"].abs().max() <= 1.5 * 1.5 * 8 * 2.0 ** -24 and abs(got["q_w"].item() / (1.5 * count) - 1.0) <= 2.0 ** -8
+
+
 # ------------------------------------------------------------------------------------------------------------ recurrence
 @pytest.mark.parametrize("dtype,gate", PAIRS)
 @pytest.mark.parametrize("mix", ["one", "rest", "root"])
