@@ -153,8 +153,9 @@ int cut(HeadParams &p, int count, long long batch, long long tokens, int sms)
     // Blocks of several tokens, whose cosines and sines serve as many turns as there are heads, where that leaves every warp four turns
     // (40 heads of 128 in bfloat16: 1024 tokens 8 us both ways, 4096 tokens 19 against 21, backwards 33 and 35), or at least one
     // and a quarter of the turns less, because heads do not come out even with the groups (7 heads of 64, 4000 tokens: 5.5 and 9.1).  With
-    // few tokens the heads of one are side by side: a decoding step of 4 tokens is 40 warps of one turn, not one of 40.
-    p.wide = wide >= 4 * warps || (wide >= warps && 4 * wide <= 3 * narrow);
+    // few tokens the heads of one are side by side: a decoding step of 4 tokens is 40 warps of one turn, not one of 40; and so it is, however
+    // many heads, where the tokens leave groups idle (200000 heads of 64 of one token 12 us, in blocks of tokens 66).
+    p.wide = (wide >= 4 * warps && 4 * wide <= 5 * narrow) || (wide >= warps && 4 * wide <= 3 * narrow);
     for (int k = 0; k < count; ++k) {
         HeadTensor &t = p.t[k];
         t.blocks = p.wide ? (int)((p.all_tokens + groups - 1) / groups) : p.all_tokens;
