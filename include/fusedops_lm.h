@@ -177,7 +177,7 @@ int fused_scan_grad(const fo_scan_grad *a, void *ws, size_t ws_bytes, void *stre
  * values_type: `type`, or FO_F32 with a 16-bit type.  What concerns the entries is computed in 64 bits.
  * dz may be the logits themselves.  Any address of an element and any ld >= vocab works; fast are logits and dz whose rows lie at
  * the same offset from a 16-byte boundary.
- * top <= FO_DISTILL_MAX_TOP and vocab <= FO_DISTILL_MAX_VOCAB, else FO_ERR_UNSUPPORTED.
+ * 1e-300 <= temperature <= 1e300, top <= FO_DISTILL_MAX_TOP and vocab <= FO_DISTILL_MAX_VOCAB, else FO_ERR_UNSUPPORTED.
  */
 #define FO_DISTILL_MAX_TOP 1024
 #define FO_DISTILL_MAX_VOCAB (1 << 20)

@@ -16,7 +16,7 @@ int run_distill(const fo_distill *a, DistillWay way, void *stream)
     if (a->rows < 0 || a->vocab < 0 || a->top < 0) return FO_ERR_SHAPE;
     if (a->type < FO_F64 || a->type > FO_F16 || (a->ids_type != FO_I32 && a->ids_type != FO_I64)) return FO_ERR_UNSUPPORTED;
     if (a->values_type != a->type && !(a->values_type == FO_F32 && elem_bytes(a->type) == 2)) return FO_ERR_UNSUPPORTED;
-    if (!(a->temperature > 0.0) || a->temperature > 1e300) return FO_ERR_UNSUPPORTED;
+    if (!(a->temperature >= 1e-300) || a->temperature > 1e300) return FO_ERR_UNSUPPORTED;      // 1 / temperature is finite
     if (a->top > FO_DISTILL_MAX_TOP || a->rows > 0x7fffffffLL || a->vocab > FO_DISTILL_MAX_VOCAB) return FO_ERR_UNSUPPORTED;
     if (a->rows == 0) return FO_OK;
     const bool grad = way != kDistillLoss;

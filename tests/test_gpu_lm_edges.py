@@ -208,3 +208,27 @@ def test_distill_a_student_with_almost_all_elsewhere(dtype, rows, vocab):
         c.values[:, 3:] = -float("inf")                      # no share: the gradient there is q S
         c.tail = (c.values.double().logsumexp(1) - np.log(1.0 - 0.03)).to(wide(dtype))
         compare(c)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_distill_temperatures_out_of_all_bounds(dtype):
+    """Beyond the range of 32 bits: next to no difference between the logits, but for masked ones, and none that is not infinite."""
+    z = torch.tensor([[3.0, 1.0, -float("inf"), 2.0, -1.0] * 60, [0.0, 4.0, 1.0, -float("inf"), 2.0] * 60], dtype=dtype, device="cuda")
+    z[1, 1] = 5.0
+    ids, values = torch.tensor([[0, 1], [1, 2]], device="cuda"), torch.zeros(2, 2, dtype=dtype, device="cuda")
+    for temperature in (1e37, 1e39, 1e44, 1e46, 1e120, 1e299):
+        loss, stats = fo.fused_distill(z, ids, values, temperature=temperature, stats=True)
+        # the shares are halves, q is 1 / 240
+        assert (loss.double() - np.log(120.0)).abs().max() <= 2.0 ** -20 and (stats[1] == 240).all()
+        for dz in (fo.fused_distill_step(None, z, ids, values, temperature=temperature)[1], fo.fused_distill_grad(None, z, ids, values, stats, temperature=temperature)):
+            assert torch.isfinite(dz).all() and dz.abs().max() <= 1e-36
+    for temperature in (1e-37, 1e-39, 1e-44, 1e-120, 1e-299):
+        one = torch.tensor([[1], [1]], device="cuda")
+        loss, stats = fo.fused_distill(z, one, values[:, :1], temperature=temperature, stats=True)
+        assert stats[:, 1].tolist() == [5.0, 1.0, 1.0] and loss[1] == 0 and loss[0] > 1e37
+        for dz in (fo.fused_distill_step(None, z, one, values[:, :1], temperature=temperature)[1],
+                   fo.fused_distill_grad(None, z, one, values[:, :1], stats, temperature=temperature)):
+            assert (dz[1] == 0).all() and not torch.isnan(dz).any()
+    for temperature in (0.0, -1.0, float("nan"), float("inf"), 1e301, 1e-301):
+        with pytest.raises(fo.FusedOpsError):
+            fo.fused_distill(z, ids, values, temperature=temperature)
