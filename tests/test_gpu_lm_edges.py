@@ -128,7 +128,8 @@ def compare(c):
     rest = np.zeros(len(z)) if c.tail is None else np.where(elsewhere > 0, np.maximum(1.0 - p, 0.0), 0.0)       # P
     with np.errstate(divide="ignore", invalid="ignore"):
         ratio = np.where(rest > 0, rest / elsewhere, 0.0)
-        eratio = np.where(rest > 0, 3 * delta * ratio + off / elsewhere, 0.0)
+        # (also where one of the two has nothing left and the other a last bit)
+        eratio = np.where((elsewhere > 0) & (c.tail is not None), 3 * delta * ratio + off / elsewhere, 0.0)
     size = np.abs(want) + np.where(np.isfinite(values), np.abs(values), 0.0).max(1, initial=0.0) / t + 100.0
     loss, kept = fo.fused_distill(*c.args(), stats=True, **c.how())
     close(loss, want, 1.1 * delta + 2.0 ** -50 * size + off * (np.log(ratio + 1.0) + 40.0), "loss")
