@@ -414,9 +414,9 @@ __device__ __forceinline__ void scan_expect(unsigned bar, unsigned bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// False if what is waited for has not come after very many polls: then the results are NaN.  What has come was sent by other CTAs,
-// whose stores are a release at the cluster's scope: the wait acquires at that scope too (its default is the CTA's, which orders
-// nothing of another CTA).  It costs nothing that shows: 1 x 65536 x 2560, gates in 32 bits, 363 us, with the weaker wait 374 to 379.
+// False if what is waited for has not come after very many polls: then the results are NaN, and no later round waits (scan_join).  What
+// has come was sent by other CTAs, whose stores are a release at the cluster's scope: the wait acquires at that scope too (its default is the
+// CTA's, which orders nothing of another CTA).  1 x 65536 x 2560, gates in 32 bits: 363 us, with the weaker wait 374 to 379.
 __device__ __forceinline__ bool scan_await(unsigned bar, unsigned phase)
 {
     for (unsigned i = 0; i < (1u << 22); ++i) {
@@ -482,7 +482,7 @@ __device__ __forceinline__ U scan_joined(const ScanShared<U> &sh, int parity, un
 // for the next one, whose barrier lies between.  turn: the round's number.
 template <class A, class U>
 __device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int turn, unsigned rank, unsigned cluster, int warp, const ScanMap<U> &own,
-                                       bool resets, int drops, U &carry)
+                                       bool resets, int drops, U &carry, bool &lost)
 {
     const int lane = threadIdx.x & 31, warps = sh.warps, parity = turn & 1;
     if (warps == 1 && cluster == 1) {
@@ -517,10 +517,11 @@ __device__ __forceinline__ U scan_join(const ScanShared<U> &sh, int turn, unsign
             }
         }
         __syncwarp();
-        if (!scan_await(sh.bar(parity), (turn >> 1) & 1)) {
-            const U lost = scan_all<U>(A(NAN));
-            if (warp == warps - 1) sh.carry[(parity ^ 1) * 32] = lost;
-            return lost;
+        lost = lost || !scan_await(sh.bar(parity), (turn >> 1) & 1);         // no later round waits for what is lost
+        if (lost) {
+            const U none = scan_all<U>(A(NAN));
+            if (warp == warps - 1) sh.carry[(parity ^ 1) * 32] = none;
+            return none;
         }
         if (resets) {
             const int4 *const q = reinterpret_cast<const int4 *>(sh.cta_drops + parity * kScanMostCluster);
@@ -651,6 +652,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
     auto marks = [&](int t) -> unsigned char { return reset && at.lane < S && t + at.lane < end ? reset[(t + at.lane) * p.reset_at.token] : 0; };
     unsigned char mark = marks(t0);
     int turn = 0;
+    bool lost = false;
     for (int first = 0; first < at.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
@@ -683,7 +685,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
 #pragma unroll
             for (int s = 1; s < S; ++s) own.h = (drops >> s) & 1u ? m[s] : fused_ma(a[s], own.h, m[s]), own.a = own.a * a[s];
         }
-        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry);
+        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry, lost);
         if (easy && full && drops == 0) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -773,6 +775,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
     };
     unsigned char mark = marks(t0);
     int turn = 0;
+    bool lost = false;
     for (int first = 0; first < at.tokens; first += round, ++turn) {
         const unsigned drops = __ballot_sync(0xffffffffu, mark != 0);
         scan_arrived<Ring::kStages - 2>();
@@ -800,7 +803,7 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_con
             for (int s = 0; s < S; ++s)
                 if (t0 - s >= 0 && t0 - s < end) own.h = (drops >> s) & 1u ? none : a[s] * (d_of(s) + own.h), own.a = own.a * a[s];
         }
-        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry);
+        U in = scan_join<A>(sh, turn, at.rank, at.cluster, at.warp, own, reset != nullptr, drops != 0, carry, lost);
         auto finish = [&](auto decay, auto mix, auto masked) {
 #pragma unroll
             for (int s = 0; s < S; ++s) {
