@@ -48,7 +48,10 @@ inline const at::Tensor *tensor_of(PyObject *o, const char *name)
 {
     if (o == Py_None) return nullptr;
     if (!THPVariable_Check(o)) throw Refused(std::string(name) + " is not a tensor");
-    return &THPVariable_Unpack(o);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    // a view whose values are the negatives of what lies in memory (the imaginary part of a conjugate)
+    if (t.is_neg()) throw Refused(std::string(name) + " is a negative view: resolve_neg() it first");
+    return &t;
 }
 
 inline at::ScalarType dtype_of(PyObject *o, const char *name)
