@@ -124,8 +124,8 @@ __device__ __forceinline__ double teacher_value(const DistillParams &p, long lon
 // masked): it is what the rounding of values and tail has left.  A value of 16 is off by 2^-5 in bfloat16, and so is its share then.
 constexpr double kDistillNoise = 0.03125;
 // A student is sure where P / Q is above this.  Q then comes near the smallest numbers of 32 bits, and P / Q near the largest: the gradient
-// outside, q (S - P / Q), is formed as -exp(z / T + log(P / Q) - ...), and what is kept of the row is that logarithm (S is below
-// its last bit), with a minus at the sum.
+// outside, q (S - P / Q), is formed as -exp((z - largest) / T + log(P / Q)) over the row's sum, and what is kept of the row is that
+// logarithm (S is below its last bit), with a minus at the sum.
 constexpr double kDistillSure = 0x1p60;
 
 // What all threads need to know of the entries besides the arrays.
@@ -301,13 +301,13 @@ struct DistillPart {
 struct DistillResult {
     double largest, total, factor;      // factor: S - P / Q
     double log_share;                   // log(P / Q) of a student that is sure, else zero
-    double coef;                        // of exp(z / T - largest + log_share) outside the entries
+    double coef;                        // of exp((z - largest) / T + log_share) outside the entries
     double all, rest, ratio, entries;   // S, P, P / Q, and what the entries add to the loss
 };
 
 // Loss, and with STEP the gradient.  Bound by DRAM and by what of the second reading misses L2 (about half): 4096 x 128000 in bfloat16
-// with rows of padding 442 to 452 us, with all rows counting 491 (4.3 TB/s of one reading and one writing); short rows by what a row
-// costs besides, which other rows on the SM hide (16384 x 1000 88 us).
+// with rows of padding 441 to 457 us, with all rows counting 490 (4.3 TB/s of one reading and one writing); short rows by what a row
+// costs besides, which other rows on the SM hide (16384 x 1000 90 us).
 template <class T, bool STEP>
 __global__ void __launch_bounds__(kDistillBound, 1) distill_kernel(const __grid_constant__ DistillParams p)
 {

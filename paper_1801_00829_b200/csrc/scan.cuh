@@ -256,7 +256,7 @@ __device__ __forceinline__ void scan_exponential(float g, float &a, float &rest)
         rest = -expm1f(g);
         a = g > -0.5f ? 1.0f - rest : expf(g);
     } else {
-        // exp(g) - 1 by its series up to g^6 / 720 where it is small: the rest is below 2^-25 of it
+        // exp(g) - 1 by its series up to g^6 / 720 where it is small: what that leaves out is below 2^-24 of it
         float m = fused_ma(g, 1.0f / 720.0f, 1.0f / 120.0f);
         m = fused_ma(m, g, 1.0f / 24.0f);
         m = fused_ma(m, g, 1.0f / 6.0f);
@@ -603,7 +603,7 @@ struct ScanRing {
 };
 
 // Bound by DRAM where there are CTAs enough (8 x 4096 x 2048 in bfloat16 72 to 77 us, 5.3 TB/s and more), by the rounds' exchange in clusters (1 x 65536 x
-// 2560, gates in 32 bits, 374 us).  Segments of 16 tokens and rings of their own for the warps leave one barrier to a round.
+// 2560, gates in 32 bits, 352 to 358 us).  Segments of 16 tokens and rings of their own for the warps leave one barrier to a round.
 // CLUSTER: launched in clusters.  Without them the code for them costs 3 to 5 us of 75 to 163 (8 x 4096 x 2048 in bfloat16).
 template <class T, class G, int V, int S, bool CLUSTER>
 __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant__ ScanParams p)
@@ -707,7 +707,8 @@ __global__ void __launch_bounds__(kScanCta, 2) scan_kernel(const __grid_constant
 
 // The gradient: l_t = dh_t + u_{t+1}, u_t = a_t l_t is what comes to the token before (nothing through a reset), from the last token to
 // the first.  Segments are counted from the end, and a segment's map is that of u.  8 x 4096 x 2048 in bfloat16 154 to 165 us (4.9 TB/s), at 59 % of
-// issue; float32 is bound by the instructions of CUDA's exponential, division and root (5 x 777 x 1001 51 us, 1.8 TB/s).
+// issue; in float32 latencies come first, those of CUDA's exponential, division and root and of odd rows copied by elements (5 x 777 x 1001
+// 51 us, 1.8 TB/s, 44 % of issue).
 template <class T, class G, int V, int S, bool CLUSTER>
 __global__ void __launch_bounds__(kScanCta, 2) scan_grad_kernel(const __grid_constant__ ScanParams p)
 {

@@ -17,7 +17,7 @@ template <class T> constexpr int scan_tokens(bool grad) { return (sizeof(T) == 2
 // Whether a call's sequences are cut into chunks.  `room`: CTAs for each 32 V channels of a sequence that find a place at once; `rounds`: how
 // many the largest clusters would take.  Below eight the two more launches and the second reading cost more than they give
 // (bfloat16, 1 x 2048 x 512: in clusters 10 us forwards and 20 backwards, in chunks 16 and 24; 1 x 8192 x 1024: 33 and 70, 26 and
-// 40), and forwards, where all inputs are read twice, so it is when the clusters fill the GPU (1 x 65536 x 2560: 374 and 440;
+// 40), and forwards, where all inputs are read twice, so it is when the clusters fill the GPU (1 x 65536 x 2560, side by side: 374 and 440;
 // backwards, where two of four are, 660 and 478).
 inline bool scan_chunked(bool grad, long long room, long long rounds) { return rounds >= 8 && room >= (grad ? 4 : 16); }
 constexpr int kScanLeastChunk = 4;      // rounds; 1 x 65536 x 32 forwards: with four 39 us, two 41, eight 54
