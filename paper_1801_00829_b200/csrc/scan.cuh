@@ -221,7 +221,8 @@ __device__ __forceinline__ ScanPiece<T, V> scan_narrow(U u)
 // ------------------------------------------------------------------------------------------------ decays
 // a and 1 - a, both without cancellation.  A decay near 1 multiplies a state very many times, so that its error adds up over
 // 1 / (1 - a) tokens: it is 1 minus its small complement, and so rounded once.  EXACT (32- and 64-bit x): by CUDA's functions; else by
-// the hardware's exponential and reciprocal, whose relative error of a few 2^-23 is then one of the complement.
+// the hardware's exponential and reciprocal, whose relative error, up to (10 + |gate|) 2^-23 by the exponent's rounding, is then one of the smaller
+// of a decay and its complement.
 __device__ __forceinline__ float scan_exp2(float v)
 {
     float r;
