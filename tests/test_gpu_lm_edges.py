@@ -105,6 +105,54 @@ def test_as_many_channels_as_there_may_be():
             assert (got["gate"][t, part] - want * before).abs().max() <= 64 * 2.0 ** -53
 
 
+def test_as_many_tokens_as_there_may_be():
+    """2^30 tokens, in chunks; far back nothing is left of a state, so that windows of the sequence can be looked at by themselves."""
+    count, window, lead = 1 << 30, 300, 200                  # a is at most 0.73: 0.73^200 is 2^-90
+    x = torch.empty(count, 1, dtype=BF16, device="cuda").uniform_(-1.0, 1.0)
+    gate = torch.empty(count, 1, dtype=BF16, device="cuda").uniform_(-1.0, 1.0)
+    reset = torch.zeros(count, dtype=torch.bool, device="cuda")
+    places = [0, 12345, (1 << 29) - 150, count - window - lead]
+    for first in places:
+        reset[first + lead + 77] = True
+    state = torch.full((1,), 3.0, device="cuda")
+    h, last = fo.fused_scan(x, gate, "sigmoid", "rest", state, reset)
+    got = fo.fused_scan_grad(x, x, gate, h, "sigmoid", "rest", state, reset, dlast=state)
+    assert last.item() == pytest.approx(h[-1].item(), rel=2.0 ** -8, abs=2.0 ** -126)
+    for first in places:
+        part = slice(first, first + window + lead)
+        a = torch.sigmoid(gate[part, 0].double())
+        drop, xd, hd = reset[part], x[part, 0].double(), h[part, 0].double()
+        want, s = torch.zeros_like(a), state[0].double() if first == 0 else torch.zeros((), dtype=F64, device="cuda")
+        for t in range(window + lead):
+            s = (0.0 if drop[t] else a[t] * s) + (1.0 - a[t]) * xd[t]
+            want[t] = s
+        at = slice(0 if first == 0 else lead, window + lead)
+        # sums of numbers below 1 (3 with the state) in 32 bits, at most 4 of them in effect, and one rounding
+        assert ((want - hd)[at].abs() <= 2.0 ** -8 * want[at].abs() + 64 * 3 * 2.0 ** -24).all(), first
+        through, dx, dg = torch.zeros_like(s), torch.zeros_like(a), torch.zeros_like(a)
+        if first == places[-1]:
+            through = state[0].double()
+        for t in reversed(range(window + lead)):
+            lam = xd[t] + through
+            before = 0.0 if drop[t] else (hd[t - 1] if t else state[0].double())
+            dx[t], dg[t] = (1.0 - a[t]) * lam, a[t] * (1.0 - a[t]) * lam * (before - xd[t])
+            through = torch.zeros_like(s) if drop[t] else a[t] * lam
+        at = slice(1 if first else 0, window + lead if first == places[-1] else window)
+        for name, v in (("x", dx), ("gate", dg)):
+            assert ((v - got[name][part, 0].double())[at].abs() <= 2.0 ** -8 * v[at].abs() + 64 * 12 * 2.0 ** -24).all(), (name, first)
+    with pytest.raises(fo.FusedOpsError):
+        fo.fused_scan(x[:1].expand(count + 1, 1), gate[:1].expand(count + 1, 1), lengths=torch.zeros(1, dtype=torch.int64, device="cuda"), out=None)
+
+
+def test_as_many_sequences_as_there_may_be():
+    count = 2 ** 31 - 1
+    x = torch.empty(count, 1, 1, dtype=BF16, device="cuda").bernoulli_()
+    h, last = fo.fused_scan(x, x, "value", "one")
+    assert torch.equal(h, x) and torch.equal(last, x[:, 0].float())
+    _, again = fo.fused_scan(x, x, "value", "one", last, out=h, out_state=last)
+    assert again is last and torch.equal(h, x * 2.0) and torch.equal(last[-4096:], h[-4096:, 0].float())
+
+
 # ------------------------------------------------------------------------------------------------------------ distillation
 def compare(c):
     """Loss, statistics and both gradients with the oracle.
@@ -233,3 +281,10 @@ def test_distill_temperatures_out_of_all_bounds(dtype):
     for temperature in (0.0, -1.0, float("nan"), float("inf"), 1e301, 1e-301):
         with pytest.raises(fo.FusedOpsError):
             fo.fused_distill(z, ids, values, temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,shift", [(1 << 20, 0), ((1 << 20) - 3, 1)])
+def test_distill_as_many_logits_and_entries_as_there_may_be(dtype, vocab, shift):
+    for rows, tail in ((1, True), (3, False)):
+        compare(Distill(rows, vocab, 1024, dtype, tail, 0.7, shift=shift))
